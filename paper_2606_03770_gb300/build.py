@@ -38,7 +38,7 @@ def _stale(objs):
         return True
     t = os.path.getmtime(LIB)
     deps = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
-    deps.append(os.path.join(INCLUDE, "e2ga.h"))
+    deps += [os.path.join(INCLUDE, f) for f in ("e2ga.h", "e2ops.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

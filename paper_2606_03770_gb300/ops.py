@@ -1,0 +1,368 @@
+"""Binding of the block operators' C ABI (include/e2ops.h) for torch tensors.
+
+What one served decoder block and its output layer are made of, in the
+precisions the deployment search plans with:
+
+* ``quant_matmul``: products with 4-bit weights and group scales, with the
+  residual add or the gated (SwiGLU) form;
+* ``cache_append`` / ``cache_read`` / ``cache_attend``: a paged 4-bit cache of
+  keys and values, written with the position rotation on the way, read back,
+  and attended to by decode batches and prompts;
+* ``token_logprobs``: log probabilities of given tokens, entropy and top
+  alternatives.
+
+Each function checks its tensors, allocates outputs that are not given, and
+enqueues on the current stream of the tensors' device.  Formulas, layouts and what
+happens to values out of range are in include/e2ops.h.  There is no CPU
+fallback: without the library, or with tensors off the GPU, the calls raise.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from . import e2ga
+from .e2ga import E2_OK
+
+E2_F16, E2_BF16, E2_F32 = 0, 1, 2
+E2_CACHE_GROUP, E2_MAX_TOP, E2_MAX_COLS = 64, 32, 1 << 20
+DTYPES = {torch.float16: E2_F16, torch.bfloat16: E2_BF16, torch.float32: E2_F32}
+_P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
+
+
+class e2_quant_weight(C.Structure):
+    _fields_ = [("rows", _I), ("cols", _I), ("group", _I), ("codes", _P), ("scales", _P), ("mins", _P)]
+
+
+class e2_matmul_args(C.Structure):
+    _fields_ = [("tokens", _I), ("dtype", _I), ("gated", _I), ("x", _P), ("x_stride", _L), ("residual", _P),
+                ("residual_stride", _L), ("y", _P), ("y_stride", _L)]
+
+
+class e2_cache(C.Structure):
+    _fields_ = [("pages", _I), ("page_size", _I), ("kv_heads", _I), ("head_dim", _I), ("k_codes", _P),
+                ("k_scales", _P), ("v_codes", _P), ("v_scales", _P)]
+
+
+class e2_append_args(C.Structure):
+    _fields_ = [("tokens", _I), ("dtype", _I), ("q_heads", _I), ("rot", _I), ("interleaved", _I),
+                ("table_rows", _I), ("slots", _P), ("positions", _P), ("cos", _P), ("sin", _P), ("k", _P),
+                ("k_stride", _L), ("v", _P), ("v_stride", _L), ("q", _P), ("q_stride", _L), ("q_out", _P),
+                ("q_out_stride", _L)]
+
+
+class e2_attend_args(C.Structure):
+    _fields_ = [("tokens", _I), ("dtype", _I), ("q_heads", _I), ("batch", _I), ("table", _P), ("table_cols", _I),
+                ("table_stride", _L),
+                ("lens", _P), ("starts", _P), ("max_new", _I), ("max_len", _I), ("scale", C.c_float),
+                ("window", _I), ("q", _P), ("q_stride", _L), ("out", _P), ("out_stride", _L)]
+
+
+class e2_logprobs_args(C.Structure):
+    _fields_ = [("rows", _I), ("vocab", _I), ("dtype", _I), ("top", _I), ("logits", _P), ("stride", _L),
+                ("tokens", _P), ("logprob", _P), ("entropy", _P), ("values", _P), ("ids", _P)]
+
+
+# name -> (restype, argtypes); the exported surface of include/e2ops.h
+SIGNATURES = {
+    "e2_ops_error": (C.c_char_p, []),
+    "e2_quant_matmul_workspace": (C.c_size_t, [_I] * 3),
+    "e2_quant_matmul": (C.c_int, [_P, _P, _P, C.c_size_t, _P]),
+    "e2_cache_append": (C.c_int, [_P, _P, _P]),
+    "e2_cache_read": (C.c_int, [_P, _P, _I, _I, _P, _L, _P, _L, _P]),
+    "e2_cache_attend_workspace": (C.c_size_t, [_P, _P]),
+    "e2_cache_attend": (C.c_int, [_P, _P, _P, C.c_size_t, _P]),
+    "e2_token_logprobs": (C.c_int, [_P, _P]),
+}
+_lib = None
+
+
+def load():
+    """The library with the operators' signatures; raises if it is not built."""
+    global _lib
+    if _lib is None:
+        lib = e2ga.load()
+        for name, (res, args) in SIGNATURES.items():
+            f = getattr(lib, name)
+            f.restype, f.argtypes = res, args
+        _lib = lib
+    return _lib
+
+
+def _check(status, where):
+    if status != E2_OK:
+        raise e2ga.E2Error(status, where, load().e2_ops_error().decode())
+
+
+def _need(cond, text):
+    if not cond:
+        raise ValueError(text)
+
+
+def _tensor(x, name, dtypes, shape, device=None):
+    """x is a tensor on the GPU with one of these types, this shape (None: any
+    size) and contiguous rows."""
+    _need(isinstance(x, torch.Tensor) and x.is_cuda, f"{name} must be a tensor on the GPU")
+    _need(device is None or x.device == device, f"{name} must be on {device}")
+    _need(x.dtype in dtypes, f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {x.dtype}")
+    s = x.shape
+    _need(len(s) == len(shape) and all(b is None or a == b for a, b in zip(s, shape)),
+          f"{name} has shape {tuple(s)}, not {tuple('any' if b is None else b for b in shape)}")
+    _need(s[-1] <= 1 or x.stride(-1) == 1, f"{name} must be contiguous in its last axis")
+
+
+_HALF = (torch.float16, torch.bfloat16)
+_FLOAT = (torch.float16, torch.bfloat16, torch.float32)
+
+
+def _stride(x):
+    """Row stride (a single row's does not matter)."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _rows(x, name):
+    """Token stride of [tokens][heads][dim], whose heads lie side by side."""
+    _need(x.shape[1] <= 1 or x.stride(1) == x.shape[2], f"{name}: a token's heads must lie side by side")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
+class _On:
+    """The tensors' device as the current one, and its current stream."""
+
+    def __init__(self, device):
+        self.device = device
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard:
+            self.guard.__exit__(*exc)
+
+
+# ---- products with 4-bit weights --------------------------------------------------
+class QuantWeight:
+    """4-bit weights [rows][cols]: ``codes`` uint8 [rows, cols / 2] (column 2j
+    in the low four bits), ``scales`` float16 [rows, cols / group] and, for
+    scale * code + min instead of scale * (code - 8), ``mins`` like scales.
+    Holds views of the tensors, no copies."""
+
+    def __init__(self, codes, scales, mins=None):
+        _tensor(codes, "codes", (torch.uint8,), (None, None))
+        rows, cols = codes.shape[0], 2 * codes.shape[1]
+        _tensor(scales, "scales", (torch.float16,), (rows, None), codes.device)
+        groups = scales.shape[1]
+        _need(groups > 0 and cols % groups == 0 and cols // groups in (32, 64, 128),
+              "scales must have one column per 32, 64 or 128 columns of weights")
+        for x, n in ((codes, "codes"), (scales, "scales")) + (((mins, "mins"),) if mins is not None else ()):
+            _need(x.is_contiguous(), f"{n} must be contiguous")
+        if mins is not None:
+            _tensor(mins, "mins", (torch.float16,), (rows, groups), codes.device)
+        self.rows, self.cols, self.group, self.device = rows, cols, cols // groups, codes.device
+        self.codes, self.scales, self.mins = codes, scales, mins
+        self.struct = e2_quant_weight(rows, cols, self.group, codes.data_ptr(), scales.data_ptr(),
+                                      mins.data_ptr() if mins is not None else None)
+        self.ref = C.byref(self.struct)
+
+    def dequantize(self):
+        """The weights in float32 (plain torch; for checks and inspection)."""
+        c = torch.stack([self.codes & 15, self.codes >> 4], -1).flatten(1).float()
+        s = self.scales.float().repeat_interleave(self.group, 1)
+        if self.mins is None:
+            return (c - 8) * s
+        return c * s + self.mins.float().repeat_interleave(self.group, 1)
+
+
+def quantize_weight(w, group=64, symmetric=True):
+    """Round a float weight [rows, cols] to 4 bits with group scales (plain
+    torch; done once, when a model is loaded)."""
+    _need(w.dim() == 2 and group in (32, 64, 128) and w.shape[1] % group == 0,
+          "w must be [rows, cols], cols a multiple of the group (32, 64 or 128)")
+    x = w.float().unflatten(1, (-1, group))
+    if symmetric:
+        scales = (x.abs().amax(-1) / 7).half()
+        s = scales.float()[..., None]
+        q = torch.where(s > 0, torch.round(x / s) + 8, 8.0)
+        mins = None
+    else:
+        lo = x.amin(-1)
+        mins, scales = lo.half(), ((x.amax(-1) - lo) / 15).half()
+        s = scales.float()[..., None]
+        q = torch.where(s > 0, torch.round((x - mins.float()[..., None]) / s), 0.0)
+    q = q.clamp(0, 15).to(torch.uint8).flatten(1)
+    return QuantWeight((q[:, 0::2] | (q[:, 1::2] << 4)).contiguous(), scales.contiguous(),
+                       mins.contiguous() if mins is not None else None)
+
+
+def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
+    """x [tokens, cols] times the weights' rows (+ residual): [tokens, rows],
+    or, ``gated``, silu(x W_gate) * (x W_up) [tokens, rows / 2]."""
+    _tensor(x, "x", _HALF, (None, w.cols), w.device)
+    tokens, outs = x.shape[0], w.rows // 2 if gated else w.rows
+    if residual is not None:
+        _tensor(residual, "residual", (x.dtype,), (tokens, outs), w.device)
+    if out is None:
+        out = torch.empty((tokens, outs), dtype=x.dtype, device=w.device)
+    else:
+        _tensor(out, "out", (x.dtype,), (tokens, outs), w.device)
+    lib = load()
+    a = e2_matmul_args(tokens, DTYPES[x.dtype], bool(gated), x.data_ptr(), _stride(x),
+                       residual.data_ptr() if residual is not None else None,
+                       _stride(residual) if residual is not None else 0, out.data_ptr(),
+                       _stride(out))
+    need = lib.e2_quant_matmul_workspace(w.rows, w.cols, tokens)
+    if need and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=w.device)
+    with _On(w.device) as stream:
+        _check(lib.e2_quant_matmul(w.ref, C.byref(a), workspace.data_ptr() if need else None,
+                                   workspace.numel() if need else 0, stream), "e2_quant_matmul")
+    return out
+
+
+# ---- the cache ------------------------------------------------------------------------
+class Cache:
+    """A paged 4-bit cache over four tensors: codes uint8
+    [pages, kv_heads, page_size, head_dim / 2] and scales float16
+    [pages, kv_heads, page_size, head_dim / 64, 2] of keys and of values."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        _tensor(k_codes, "k_codes", (torch.uint8,), (None,) * 4)
+        pages, heads, page, half = k_codes.shape
+        _need(half in (32, 64), "head_dim must be 64 or 128")
+        _need(page in (16, 32, 64, 128, 256), "page_size must be 16, 32, 64, 128 or 256")
+        _tensor(v_codes, "v_codes", (torch.uint8,), k_codes.shape, k_codes.device)
+        for x, n in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+            _tensor(x, n, (torch.float16,), (pages, heads, page, 2 * half // E2_CACHE_GROUP, 2), k_codes.device)
+        for x in (k_codes, k_scales, v_codes, v_scales):
+            _need(x.is_contiguous(), "cache tensors must be contiguous")
+        self.pages, self.kv_heads, self.page_size, self.head_dim = pages, heads, page, 2 * half
+        self.device = k_codes.device
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.struct = e2_cache(pages, page, heads, 2 * half, k_codes.data_ptr(), k_scales.data_ptr(),
+                               v_codes.data_ptr(), v_scales.data_ptr())
+        self.ref = C.byref(self.struct)
+
+    @classmethod
+    def empty(cls, pages, page_size, kv_heads, head_dim, device="cuda"):
+        """A cache of zeros (every token reads as zeros)."""
+        shape = (pages, kv_heads, page_size)
+        codes = [torch.zeros(*shape, head_dim // 2, dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.zeros(*shape, head_dim // E2_CACHE_GROUP, 2, dtype=torch.float16, device=device)
+                  for _ in range(2)]
+        return cls(codes[0], scales[0], codes[1], scales[1])
+
+
+def cache_append(cache, k, v, slots, positions, cos, sin, q=None, q_out=None, interleaved=False):
+    """Append keys (turned by their positions) and values [tokens, kv_heads,
+    head_dim] at ``slots`` (int64; page * page_size + token in page; -1: none).
+    Returns the turned queries (``q_out``, allocated unless given), or None."""
+    dev, D = cache.device, cache.head_dim
+    _tensor(k, "k", _HALF, (None, cache.kv_heads, D), dev)
+    tokens = k.shape[0]
+    _tensor(v, "v", (k.dtype,), (tokens, cache.kv_heads, D), dev)
+    _tensor(slots, "slots", (torch.int64,), (tokens,), dev)
+    _tensor(positions, "positions", (torch.int32,), (tokens,), dev)
+    _tensor(cos, "cos", (torch.float32,), (None, None), dev)
+    _tensor(sin, "sin", (torch.float32,), cos.shape, dev)
+    _need(cos.is_contiguous() and sin.is_contiguous(), "cos and sin must be contiguous")
+    rot = 2 * cos.shape[1]
+    heads = qs = qos = 0
+    if q is not None:
+        _tensor(q, "q", (k.dtype,), (tokens, None, D), dev)
+        heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((tokens, heads, D), dtype=q.dtype, device=dev)
+        else:
+            _tensor(q_out, "q_out", (k.dtype,), q.shape, dev)
+        qs, qos = _rows(q, "q"), _rows(q_out, "q_out")
+    else:
+        _need(q_out is None, "q_out without q")
+    a = e2_append_args(tokens, DTYPES[k.dtype], heads, rot, bool(interleaved), cos.shape[0], slots.data_ptr(),
+                       positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), k.data_ptr(), _rows(k, "k"),
+                       v.data_ptr(), _rows(v, "v"), q.data_ptr() if heads else None, qs,
+                       q_out.data_ptr() if heads else None, qos)
+    with _On(dev) as stream:
+        _check(load().e2_cache_append(cache.ref, C.byref(a), stream), "e2_cache_append")
+    return q_out
+
+
+def cache_read(cache, slots, dtype=torch.bfloat16):
+    """The keys and values at ``slots``, as the values their codes stand for."""
+    _tensor(slots, "slots", (torch.int64,), (None,), cache.device)
+    _need(dtype in DTYPES, "dtype must be float16, bfloat16 or float32")
+    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    k, v = (torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
+    row = shape[1] * shape[2]
+    with _On(cache.device) as stream:
+        _check(load().e2_cache_read(cache.ref, slots.data_ptr(), shape[0], DTYPES[dtype], k.data_ptr(), row,
+                                    v.data_ptr(), row, stream), "e2_cache_read")
+    return k, v
+
+
+def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scale=None, window=0, out=None,
+                 workspace=None):
+    """Attention of the queries q [tokens, q_heads, head_dim] of a batch of
+    requests over the cache (their own keys already appended): ``table`` int32
+    [batch, pages], ``lens`` int32 [batch] cached tokens, ``starts`` int32
+    [batch + 1] first query of each request.  ``max_new`` and ``max_len``, the
+    largest counts of queries and of cached tokens, are read from the device
+    (a synchronisation) unless given.  scale: 1/sqrt(head_dim) unless given."""
+    dev = cache.device
+    _tensor(q, "q", _HALF, (None, None, cache.head_dim), dev)
+    tokens, heads = q.shape[:2]
+    _tensor(table, "table", (torch.int32,), (None, None), dev)
+    batch = table.shape[0]
+    _tensor(lens, "lens", (torch.int32,), (batch,), dev)
+    _tensor(starts, "starts", (torch.int32,), (batch + 1,), dev)
+    if max_new is None:
+        max_new = int((starts[1:] - starts[:-1]).max()) if batch else 0
+    if max_len is None:
+        max_len = int(lens.max()) if batch else 0
+    if out is None:
+        # (tokens outside every request are not written)
+        out = torch.zeros_like(q, memory_format=torch.contiguous_format) if batch == 0 else \
+            torch.empty((tokens, heads, cache.head_dim), dtype=q.dtype, device=dev)
+    else:
+        _tensor(out, "out", (q.dtype,), q.shape, dev)
+    lib = load()
+    a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), table.shape[1],
+                       _stride(table), lens.data_ptr(), starts.data_ptr(),
+                       max_new, max_len, 1 / math.sqrt(cache.head_dim) if scale is None else scale, window,
+                       q.data_ptr(), _rows(q, "q"), out.data_ptr(), _rows(out, "out"))
+    with _On(dev) as stream:
+        need = lib.e2_cache_attend_workspace(cache.ref, C.byref(a))
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check(lib.e2_cache_attend(cache.ref, C.byref(a), workspace.data_ptr() if need else None,
+                                   workspace.numel() if need else 0, stream), "e2_cache_attend")
+    return out
+
+
+# ---- the output layer --------------------------------------------------------------------
+def token_logprobs(logits, tokens=None, top=0, entropy=True):
+    """(logprob, entropy, values, ids) of logits [rows, vocab]: the log
+    probability of tokens[row] (int32; None without tokens), the entropy (None
+    unless asked for), and the ``top`` largest log probabilities with their indices
+    [rows, top], equal ones by their index.  All float32 / int32."""
+    _tensor(logits, "logits", _FLOAT, (None, None))
+    rows, vocab = logits.shape
+    dev = logits.device
+    _need(0 <= top <= E2_MAX_TOP, f"top must be in 0..{E2_MAX_TOP}")
+    if tokens is not None:
+        _tensor(tokens, "tokens", (torch.int32,), (rows,), dev)
+    f = lambda *s: torch.empty(s, dtype=torch.float32, device=dev)  # noqa: E731
+    logprob = f(rows) if tokens is not None else None
+    ent = f(rows) if entropy else None
+    values, ids = f(rows, top), torch.empty((rows, top), dtype=torch.int32, device=dev)
+    a = e2_logprobs_args(rows, vocab, DTYPES[logits.dtype], top, logits.data_ptr(), _stride(logits),
+                         tokens.data_ptr() if tokens is not None else None,
+                         logprob.data_ptr() if tokens is not None else None, ent.data_ptr() if entropy else None,
+                         values.data_ptr(), ids.data_ptr())
+    with _On(dev) as stream:
+        _check(load().e2_token_logprobs(C.byref(a), stream), "e2_token_logprobs")
+    return logprob, ent, values, ids

@@ -1,0 +1,252 @@
+"""e2_cache_attend against 64 bits: head layouts, lengths, windows, pages, empty
+rows, and what is out of range."""
+import math
+
+import pytest
+import torch
+
+import ops_reference as R
+
+pytestmark = pytest.mark.gpu
+HALF, BF = torch.float16, torch.bfloat16
+
+
+def setup(lens, news, Hkv, G, D, page, dtype=BF, seed=0, extra_cols=0, spread=False):
+    from paper_2606_03770_gb300 import ops
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    B, cols = len(lens), max(1, -(-max(lens + [1]) // page)) + extra_cols
+    pages = B * cols + 2
+    cache = ops.Cache.empty(pages, page, Hkv, D)
+    for c in (cache.k_codes, cache.v_codes):
+        c.copy_(torch.randint(0, 256, c.shape, generator=g, device="cuda"))
+    for s in (cache.k_scales, cache.v_scales):
+        d = 0.1 + 0.2 * torch.rand(s.shape[:-1], generator=g, device="cuda")
+        if spread:                                   # values of very different sizes, some constant groups
+            d = d * 10.0 ** torch.randint(-3, 3, s.shape[:-1], generator=g, device="cuda")
+            d[torch.rand(d.shape, generator=g, device="cuda") < 0.1] = 0
+        m = -7.5 * d + 0.3 * torch.randn(d.shape, generator=g, device="cuda")
+        s.copy_(torch.stack([d, m], -1))
+    if spread:
+        cache.k_scales.mul_(0.05)
+    table = torch.randperm(pages, generator=g, device="cuda")[:B * cols].reshape(B, cols).int()
+    T = sum(news)
+    q = torch.randn(T, Hkv * G, D, generator=g, device="cuda").to(dtype)
+    starts = torch.tensor([0] + list(torch.tensor(news).cumsum(0)), dtype=torch.int32, device="cuda")
+    return cache, q, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), starts
+
+
+def check(lens, news, Hkv, G, D, page, dtype=BF, window=0, scale=None, **kw):
+    from paper_2606_03770_gb300 import ops
+    s = setup(lens, news, Hkv, G, D, page, dtype, **kw)
+    out = ops.cache_attend(*s, max_new=max(news), max_len=max(lens), window=window, scale=scale)
+    want, lim, _ = R.attend(*s, 1 / math.sqrt(D) if scale is None else scale, window)
+    R.close(out, want, lim, "out")
+    return s, out
+
+
+@pytest.mark.parametrize("Hkv,G", [(1, 1), (2, 3), (1, 5), (3, 7), (8, 8), (1, 16), (2, 20), (1, 40), (32, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_heads(Hkv, G, D):
+    check([37, 200], [1, 1], Hkv, G, D, 16)
+
+
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 63, 64, 65, 127, 129, 255, 257, 1000])
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_lengths_one_token(length, page):
+    check([length], [1], 1, 8, 128, page)
+    check([length], [1], 2, 3, 64, page, HALF)
+
+
+@pytest.mark.parametrize("new", [2, 3, 4, 8, 9, 17, 40, 64, 100])
+def test_several_queries(new):
+    check([new], [new], 1, 4, 64, 32)                   # a prompt from its start
+    check([new + 77], [new], 2, 8 if new < 20 else 2, 128, 16, HALF)
+
+
+@pytest.mark.parametrize("window", [1, 5, 16, 128, 1000])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_windows(window, dtype):
+    check([300, 40, 129], [1, 1, 1], 2, 4, 128, 32, dtype, window)
+    check([300, 40, 129], [5, 40, 1], 1, 8, 64, 16, dtype, window)
+
+
+def test_ragged_batches_with_empty_requests():
+    check([0, 1, 500, 33, 0, 64], [0, 1, 3, 2, 0, 1], 3, 7, 64, 16, HALF, 128)
+    check([0, 1, 500, 33, 0, 64, 7], [0, 1, 20, 33, 0, 1, 7], 2, 5, 128, 64)
+    check([70, 3000, 1], [64, 1, 1], 1, 8, 128, 64)
+
+
+def test_queries_before_the_first_key_are_zero():
+    """More queries than cached tokens: the first of them see nothing."""
+    s, out = check([3], [5], 2, 4, 128, 16)
+    assert bool((out[:2] == 0).all()) and bool((out[2:] != 0).any())
+    s, out = check([0], [2], 1, 2, 64, 16)
+    assert bool((out == 0).all())
+    s, out = check([4, 80], [20, 70], 1, 8, 64, 16)
+    assert bool((out[:16] == 0).all())
+
+
+@pytest.mark.parametrize("B,length", [(1, 20000), (3, 4097), (16, 700)])
+def test_long_contexts_are_split(B, length):
+    check([length - 3 * b for b in range(B)], [1] * B, 1, 8, 128, 64)
+    check([length - 3 * b for b in range(B)], [1] * B, 2, 1, 64, 16)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_scores_of_all_sizes(new):
+    check([200], [new], 2, 4, 128, 16, scale=0.0)
+    check([200], [new], 2, 4, 128, 16, scale=-0.05)
+    check([200], [new], 2, 4, 64, 16, scale=2.0)          # one key takes nearly all the weight
+
+
+@pytest.mark.parametrize("new", [1, 4, 33])
+def test_values_of_all_sizes(new):
+    check([150, 400], [new, 1], 2, 4, 128, 16, spread=True)
+    check([150, 400], [new, 1], 1, 3, 64, 16, HALF, spread=True)
+
+
+@pytest.mark.parametrize("new", [1, 2, 40])
+def test_queries_of_all_sizes(new):
+    """bf16 queries beyond fp16's range, and far below it."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([90], [new], 1, 4, 128, 16)
+    q[:, 0] *= 1e6
+    q[:, 1] *= 1e-9
+    q[:, 2] = 0
+    for scale in (1e-6, 1e-3):
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=90, scale=scale)
+        R.close(out, *R.attend(cache, q, table, lens, starts, scale, 0)[:2])
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_pages_outside_the_cache_are_not_seen(new):
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([200, 200], [new, 1], 2, 4, 128, 16)
+    table[0, 2], table[0, 5], table[1, 0] = -1, cache.pages, 2 ** 31 - 1
+    out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=200)
+    R.close(out, *R.attend(cache, q, table, lens, starts, 128 ** -0.5, 0)[:2])
+    table[0] = -1
+    out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=200)
+    assert bool((out[:new] == 0).all())
+
+
+@pytest.mark.parametrize("new", [1, 24])
+def test_hidden_keys_do_not_matter(new):
+    """NaN and huge values in keys that the mask hides, and past the end."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([100], [new], 1, 8, 128, 16)
+    a = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=100, window=20)
+    for s in (cache.k_scales, cache.v_scales):
+        page, at = table[0, 100 // 16].item(), 100 % 16
+        s[page, :, at:] = math.nan
+        for j in range(0, 100 - new - 20):                   # before every window
+            s[table[0, j // 16].item(), :, j % 16] = math.nan if j % 2 else math.inf
+    b = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=100, window=20)
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("new", [1, 24])
+def test_nan_in_a_seen_key_reaches_its_heads_only(new):
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([100], [new], 2, 4, 64, 16)
+    a = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=100)
+    cache.k_scales[table[0, 1], 0, 3] = math.nan
+    b = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=100)
+    assert bool(torch.isnan(b[:, :4]).all()) and torch.equal(a[:, 4:], b[:, 4:])
+
+
+def test_hints_larger_lengths_and_tokens_outside_requests():
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([300, 120], [3, 40], 2, 4, 128, 16, extra_cols=2)
+    want, lim, _ = R.attend(cache, q, table, lens, starts, 128 ** -0.5, 0)
+    for new, length in ((40, 300), (1, 1), (43, 5000), (0, 0), (2, 40)):
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=length)
+        R.close(out, want, lim, (new, length))
+    R.close(ops.cache_attend(cache, q, table, lens, starts), want, lim)        # read from the device
+    part = torch.tensor([1, 3, 20], dtype=torch.int32, device="cuda")          # tokens 0 and 20.. belong to none
+    want, lim, written = R.attend(cache, q, table, lens, part, 128 ** -0.5, 0)
+    out = torch.full_like(q, 9.0)
+    ops.cache_attend(cache, q, table, lens, part, max_new=17, max_len=300, out=out)
+    R.close(out[written], want[written], lim[written])
+    assert bool((out[~written] == 9).all())
+    bad = torch.tensor([-5, 2, 4000], dtype=torch.int32, device="cuda")        # starts out of range
+    want, lim, written = R.attend(cache, q, table, lens, bad, 128 ** -0.5, 0)
+    out = ops.cache_attend(cache, q, table, lens, bad, max_new=40, max_len=300)
+    R.close(out[written], want[written], lim[written])
+
+
+def test_table_narrower_than_its_rows_and_strided_queries():
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([60, 50], [1, 2], 2, 4, 64, 16, extra_cols=3)
+    wide = torch.zeros(3, 8 * 64 + 16, device="cuda", dtype=BF)
+    qs = wide[:, 8:-8].unflatten(1, (8, 64))
+    qs.copy_(q)
+    want, lim, _ = R.attend(cache, q, table[:, :2], lens, starts, 0.125, 0)    # keys from 32 on are not there
+    out = wide.clone()
+    o = out[:, 8:-8].unflatten(1, (8, 64))
+    ops.cache_attend(cache, qs, table[:, :2], lens, starts, max_new=2, max_len=60, out=o)
+    R.close(o, want, lim)
+    assert torch.equal(out[:, :8], wide[:, :8]) and torch.equal(out[:, -8:], wide[:, -8:])
+
+
+@pytest.mark.parametrize("news", [[1, 1], [30, 1]])
+def test_same_bits_again_on_another_stream_and_in_a_graph(news):
+    from paper_2606_03770_gb300 import ops
+    s = setup([5000, 3000], news, 2, 8, 128, 64)
+    kw = dict(max_new=max(news), max_len=5000)
+    a = ops.cache_attend(*s, **kw)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    out = torch.empty_like(a)
+    with torch.cuda.stream(st):
+        rest = [ops.cache_attend(*s, **kw) for _ in range(4)]
+        graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        ops.cache_attend(*s, out=out, **kw)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for b in rest) and torch.equal(a, out)
+
+
+def test_cache_beyond_31_bits_of_bytes():
+    from paper_2606_03770_gb300 import ops
+    pages, page, H, D = 70000, 256, 2, 128            # 2.3 GB of codes each
+    codes = [torch.empty(pages, H, page, D // 2, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.empty(pages, H, page, 2, 2, dtype=HALF, device="cuda") for _ in range(2)]
+    cache = ops.Cache(codes[0], scales[0], codes[1], scales[1])
+    g = torch.Generator(device="cuda").manual_seed(5)
+    table = torch.tensor([[pages - 1, pages - 2, 0, pages // 2]], dtype=torch.int32, device="cuda")
+    for c, s in zip(codes, scales):
+        for p in table[0].tolist():
+            c[p] = torch.randint(0, 256, c[p].shape, generator=g, device="cuda")
+            s[p] = 0.1 * torch.randn(s[p].shape, generator=g, device="cuda")
+    for new in (1, 40):
+        q = torch.randn(new, 8, D, generator=g, device="cuda").to(BF)
+        lens = torch.tensor([1000], dtype=torch.int32, device="cuda")
+        starts = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=1000)
+        R.close(out, *R.attend(cache, q, table, lens, starts, D ** -0.5, 0)[:2])
+
+
+def test_empty_and_refusals():
+    from paper_2606_03770_gb300 import e2ga, ops
+    cache, q, table, lens, starts = setup([20, 20], [1, 2], 2, 2, 64, 16)
+    kw = dict(max_new=2, max_len=20)
+    assert ops.cache_attend(cache, q[:0], table[:0], lens[:0], starts[:1]).shape == (0, 4, 64)
+    for bad in ((q.float(), table, lens, starts), (q[..., :32], table, lens, starts), (q, table.long(), lens, starts),
+                (q, table, lens[:1], starts), (q, table, lens, starts[:2]), (q.cpu(), table, lens, starts)):
+        with pytest.raises(ValueError):
+            ops.cache_attend(cache, *bad, **kw)
+    with pytest.raises(e2ga.E2Error, match="multiple of kv_heads"):
+        ops.cache_attend(cache, q[:, :3].contiguous(), table, lens, starts, **kw)
+    with pytest.raises(e2ga.E2Error, match="finite"):
+        ops.cache_attend(cache, q, table, lens, starts, scale=math.inf, **kw)
+    with pytest.raises(e2ga.E2Error, match="window"):
+        ops.cache_attend(cache, q, table, lens, starts, window=-1, **kw)
+    with pytest.raises(e2ga.E2Error, match="table_cols"):
+        ops.cache_attend(cache, q, table[:, :0], lens, starts, **kw)
+    with pytest.raises(e2ga.E2Error, match="16-byte"):
+        ops.cache_attend(cache, torch.zeros(3, 260, device="cuda", dtype=BF)[:, 1:257].unflatten(1, (4, 64)), table, lens,
+                         starts, **kw)

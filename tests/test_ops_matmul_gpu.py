@@ -1,0 +1,164 @@
+"""e2_quant_matmul against 64 bits: types, groups, odd sizes, strides, refusals."""
+import math
+
+import pytest
+import torch
+
+import ops_reference as R
+
+pytestmark = pytest.mark.gpu
+HALF, BF = torch.float16, torch.bfloat16
+
+
+def make(rows, cols, group, mins, seed=0):
+    from paper_2606_03770_gb300 import ops
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (rows, cols // 2), generator=g, device="cuda", dtype=torch.uint8)
+    s = ((0.5 + torch.rand(rows, cols // group, generator=g, device="cuda")) * (0.2 / math.sqrt(cols))).half()
+    m = (-(5 + 5 * torch.rand(s.shape, generator=g, device="cuda")) * s).half() if mins else None
+    return ops.QuantWeight(codes, s, m), g
+
+
+def randn(g, *shape, dtype=BF):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def check(tokens, rows, cols, group=64, dtype=BF, mins=False, gated=False, residual=False, spread=False):
+    from paper_2606_03770_gb300 import ops
+    w, g = make(rows, cols, group, mins, tokens + rows + cols)
+    x = randn(g, tokens, cols, dtype=dtype)
+    if spread:                 # rows of very different sizes, columns too
+        x *= (10.0 ** torch.linspace(-4, 3, tokens, device="cuda"))[:, None].to(dtype)
+        x[:, ::17] *= 30
+    r = randn(g, tokens, rows // 2 if gated else rows, dtype=dtype) if residual else None
+    y = ops.quant_matmul(x, w, residual=r, gated=gated)
+    assert y.dtype == dtype
+    R.close(y, *R.matmul(x, w, r, gated), "y")
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 7, 8, 9, 16, 17, 31, 33, 64, 65, 127, 130, 300])
+@pytest.mark.parametrize("rows,cols,group", [(96, 512, 64), (257, 1376, 32), (33, 128, 128)])
+def test_tokens(tokens, rows, cols, group):
+    check(tokens, rows, cols, group, mins=tokens % 2 == 0)
+
+
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 127, 128, 129, 1001])
+@pytest.mark.parametrize("cols", [32, 64, 96, 992, 2080])
+def test_rows_and_columns(rows, cols):
+    check(3, rows, cols, 32, dtype=HALF, mins=True)
+    check(140, rows, cols, 32, dtype=HALF)
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("mins", [False, True])
+@pytest.mark.parametrize("tokens", [1, 5, 40, 200])
+def test_forms(dtype, group, mins, tokens):
+    check(tokens, 320, 1280, group, dtype, mins, residual=True)
+    check(tokens, 2 * 161, 1280, group, dtype, mins, gated=True)
+    check(tokens, 2 * 161, 1280, group, dtype, mins, gated=True, residual=True)
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 24, 150])
+def test_workload_widths(tokens):
+    check(tokens, 4096, 11008)                       # the 4096-wide model's way back down
+    check(tokens, 8192 + 2 * 1024, 8192, mins=True)   # queries, keys and values of the 8192-wide model
+
+
+@pytest.mark.parametrize("tokens", [1, 6, 20, 129])
+def test_rows_of_different_magnitude(tokens):
+    check(tokens, 200, 2048, spread=True)
+    check(tokens, 200, 2048, mins=True, spread=True)
+
+
+@pytest.mark.parametrize("tokens", [3, 70])
+def test_strides_outputs_and_in_place_residual(tokens):
+    from paper_2606_03770_gb300 import ops
+    w, g = make(100, 256, 64, False)
+    wide = randn(g, tokens, 256 + 24)
+    x = wide[:, 8:264]
+    buf = torch.full((tokens, 111), 7.0, device="cuda", dtype=BF)
+    r = randn(g, tokens, 100)
+    buf[:, 5:105] = r
+    ops.quant_matmul(x, w, residual=buf[:, 5:105], out=buf[:, 5:105])
+    R.close(buf[:, 5:105], *R.matmul(x, w, r))
+    assert bool((buf[:, :5] == 7).all()) and bool((buf[:, 105:] == 7).all())
+
+
+@pytest.mark.parametrize("tokens", [2, 100])
+def test_values_that_are_not_finite_stay_in_their_rows(tokens):
+    from paper_2606_03770_gb300 import ops
+    w, g = make(64, 256, 64, True)
+    x = randn(g, tokens, 256)
+    y0 = ops.quant_matmul(x, w)
+    x[0, 3], x[1, 200] = math.nan, math.inf
+    y = ops.quant_matmul(x, w)
+    assert bool(torch.isnan(y[0]).all())
+    assert not bool(torch.isfinite(y[1]).any())
+    assert torch.equal(y[2:], y0[2:])
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 200])
+def test_same_inputs_same_bits_also_on_another_stream(tokens):
+    from paper_2606_03770_gb300 import ops
+    w, g = make(512, 4096, 64, False)
+    x = randn(g, tokens, 4096)
+    y = ops.quant_matmul(x, w)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        z = [ops.quant_matmul(x, w) for _ in range(3)]
+    s.synchronize()
+    assert all(torch.equal(y, v) for v in z)
+
+
+def test_captured_in_a_graph():
+    from paper_2606_03770_gb300 import ops
+    w, g = make(512, 1024, 64, False)
+    for tokens in (4, 150):
+        x = randn(g, tokens, 1024)
+        out = torch.empty(tokens, 512, device="cuda", dtype=BF)
+        ws = torch.empty(ops.load().e2_quant_matmul_workspace(512, 1024, tokens) + 1, device="cuda", dtype=torch.uint8)
+        ops.quant_matmul(x, w, out=out, workspace=ws)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ops.quant_matmul(x, w, out=out, workspace=ws)
+        x.copy_(randn(g, tokens, 1024))
+        graph.replay()
+        R.close(out, *R.matmul(x, w))
+
+
+def test_quantize_weight_rounds_to_the_nearest_code():
+    from paper_2606_03770_gb300 import ops
+    g = torch.Generator(device="cuda").manual_seed(3)
+    a = torch.randn(40, 256, generator=g, device="cuda")
+    a[5] = 0
+    for symmetric in (True, False):
+        w = ops.quantize_weight(a, 64, symmetric)
+        step = w.scales.double().repeat_interleave(64, 1)
+        # half a step, and the roundings of scale and minimum to fp16
+        lim = step / 2 + 2.0 ** -11 * (16 * step + a.abs().amax(1, keepdim=True)) + 1e-7
+        assert bool(((R.weight(w) - a.double()).abs() <= lim).all())
+
+
+def test_empty_and_refusals():
+    from paper_2606_03770_gb300 import e2ga, ops
+    w, g = make(64, 256, 64, False)
+    assert ops.quant_matmul(torch.empty(0, 256, device="cuda", dtype=BF), w).shape == (0, 64)
+    x = randn(g, 2, 256)
+    for bad in (x.float(), x[:, :128], x.cpu()):
+        with pytest.raises(ValueError):
+            ops.quant_matmul(bad, w)
+    with pytest.raises(ValueError):
+        ops.quant_matmul(x, w, residual=randn(g, 2, 63))
+    with pytest.raises(e2ga.E2Error, match="16-byte"):
+        ops.quant_matmul(randn(g, 2, 264)[:, 1:257], w)
+    with pytest.raises(e2ga.E2Error, match="16-byte"):
+        ops.quant_matmul(randn(g, 2, 260)[:, :256], w)
+    with pytest.raises(e2ga.E2Error, match="16-byte"):
+        ops.quant_matmul(randn(g, 1, 256).expand(2, 256), w)
+    odd, _ = make(33, 256, 64, False)
+    with pytest.raises(e2ga.E2Error, match="even"):
+        ops.quant_matmul(x, odd, gated=True)
+    with pytest.raises(ValueError, match="one column per"):
+        ops.QuantWeight(w.codes, torch.ones(64, 16, device="cuda", dtype=HALF))
