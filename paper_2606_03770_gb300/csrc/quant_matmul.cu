@@ -1,63 +1,35 @@
 // quant_matmul.cu -- e2_quant_matmul: products with 4-bit weights.
-#include "ops_common.cuh"
+#include "quant_matmul.cuh"
 
 namespace e2ops {
 namespace {
 
-struct MatmulParams {
-    int rows, cols, group, tokens, gated;
-    const uint8_t *codes;
-    const __half *scales, *mins;
-    const void *x, *residual;
-    void *y;
-    int64_t x_stride, residual_stride, y_stride;
-};
-
-constexpr int kTokens = 8;
-
-// A warp per output row, its lanes over words of eight columns.
-template <class T> __global__ void __launch_bounds__(128) row_kernel(const MatmulParams p)
+FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins, int sms)
 {
-    const int outs = p.gated ? p.rows / 2 : p.rows;
-    const int row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x % 32;
-    if (row >= outs) return;
-    const int t0 = blockIdx.y * kTokens, nt = min(kTokens, p.tokens - t0);
-    float sum[2][kTokens] = {};
-    for (int part = 0; part <= p.gated; ++part) {
-        const int64_t r = row + (int64_t)part * outs;
-        const uint32_t *w = reinterpret_cast<const uint32_t *>(p.codes + r * (p.cols / 2));
-        const int groups = p.cols / p.group;
-        for (int j = lane; j < p.cols / 8; j += 32) {
-            const uint32_t c = w[j];
-            const float s = __half2float(p.scales[r * groups + 8 * j / p.group]);
-            const float m = p.mins ? __half2float(p.mins[r * groups + 8 * j / p.group]) : -8.0f * s;
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __fmaf_rn((float)(c >> (4 * i) & 15), s, m);
-#pragma unroll
-            for (int t = 0; t < kTokens; ++t)
-                if (t < nt) {
-                    float x[8];
-                    unpack8<T>(*reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + (t0 + t) * p.x_stride + 8 * j), x);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[part][t] = __fmaf_rn(v[i], x[i], sum[part][t]);
-                }
+    FewPlan best{};
+    double best_t = 1e30;
+    const int nt = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4, live = tokens < 8 * nt ? tokens : 8 * nt;
+    const int chunks = (cols + kChunk - 1) / kChunk;
+    const int per = kChunk / group, stage = 32 * kRowBytes + 32 * per * 2 * (mins ? 2 : 1);
+    int x_cols = kChunk;
+    while (x_cols < 8192 && live * x_cols * 4 <= (nt == 1 ? 16 : 32) * 1024) x_cols *= 2;
+    const size_t smem = (size_t)kWarps * kStages * stage + (size_t)live * x_row_bytes(x_cols) +
+                        (mins ? (size_t)live * (x_cols / group) * 4 : 0);
+    const int fit = (int)(kSmemPerSm / (smem + 1024)), resident = fit < 4 ? fit : 4;
+    const int slabs = (tokens + 8 * nt - 1) / (8 * nt);
+    for (int wk = 1; wk <= kWarps; wk *= 2)
+        for (int split = 1; split <= 8; split *= 2) {
+            if (wk * kChunk > x_cols || (split > 1 && split * wk > chunks)) continue;
+            const int rb = 32 * (kWarps / wk);
+            const double blocks = (double)((rows + rb - 1) / rb) * split * slabs;
+            const double turns = (double)(int64_t)((blocks + sms - 1) / sms);
+            const double bytes = (double)((chunks + split - 1) / split) * kChunk * (rb * 0.54 + live * 1.0);
+            const double together = turns < resident ? turns : resident;
+            const double rate = 28.0 * together < 45.0 ? 28.0 * together : 45.0;      // bytes per ns and SM
+            const double t = turns * bytes / rate + (split > 1 ? 700 : 0) + (wk > 1 ? 100 : 0);
+            if (t < best_t) best_t = t, best = FewPlan{nt, wk, split, x_cols, smem};
         }
-    }
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t)
-        for (int o = 16; o; o >>= 1) {
-            sum[0][t] += __shfl_xor_sync(~0u, sum[0][t], o);
-            sum[1][t] += __shfl_xor_sync(~0u, sum[1][t], o);
-        }
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t)
-        if (lane == t && t < nt) {
-            float y = sum[0][t];
-            if (p.gated) y = y / (1.0f + expf(-y)) * sum[1][t];
-            if (p.residual) y += to_float(static_cast<const T *>(p.residual)[(t0 + t) * p.residual_stride + row]);
-            static_cast<T *>(p.y)[(t0 + t) * p.y_stride + row] = from_float<T>(y);
-        }
+    return best;
 }
 
 }  // namespace
@@ -95,9 +67,10 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
     MatmulParams p{w->rows, w->cols, w->group, a->tokens, a->gated != 0, w->codes,
                    reinterpret_cast<const __half *>(w->scales), reinterpret_cast<const __half *>(w->mins),
                    a->x, a->residual, a->y, a->x_stride, a->residual_stride, a->y_stride};
-    const dim3 grid((outs + 3) / 4, (a->tokens + kTokens - 1) / kTokens);
+    const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr, dev.sms);
+    const int per = kChunk / w->group;
+    FewParams q{p, outs, f.wk, f.split, __builtin_ctz((unsigned)(f.x_cols / 8)), f.x_cols,
+                w->cols % kChunk == 0 && aligned(w->scales, per * 2) && aligned(w->mins, per * 2)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a->dtype == E2_F16) row_kernel<__half><<<grid, 128, 0, s>>>(p);
-    else row_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
-    return cuda_status(cudaGetLastError());
+    return a->dtype == E2_F16 ? launch_few_f16(q, f, dev.id, s) : launch_few_bf16(q, f, dev.id, s);
 }
