@@ -9,25 +9,32 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins, int sms)
     FewPlan best{};
     double best_t = 1e30;
     const int nt = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4, live = tokens < 8 * nt ? tokens : 8 * nt;
-    const int chunks = (cols + kChunk - 1) / kChunk;
-    const int per = kChunk / group, stage = 32 * kRowBytes + 32 * per * 2 * (mins ? 2 : 1);
-    int x_cols = kChunk;
-    while (x_cols < 8192 && live * x_cols * 4 <= (nt == 1 ? 16 : 32) * 1024) x_cols *= 2;
-    const size_t smem = (size_t)kWarps * kStages * stage + (size_t)live * x_row_bytes(x_cols) +
-                        (mins ? (size_t)live * (x_cols / group) * 4 : 0);
-    const int fit = (int)(kSmemPerSm / (smem + 1024)), resident = fit < 4 ? fit : 4;
+    const bool prepare = tokens > 2;
+    const int chunks = (cols + kChunk - 1) / kChunk, x_pad = chunks * kChunk;
+    const int per = kChunk / group, stage = kRows * (kRowBytes + per * 2 * (mins ? 2 : 1));
     const int slabs = (tokens + 8 * nt - 1) / (8 * nt);
+    int x_cols = 512;
+    if (!prepare)
+        while (x_cols < 4096 && live * x_cols / 4 <= kOctets * 32 * kWarps) x_cols *= 2;
     for (int wk = 1; wk <= kWarps; wk *= 2)
         for (int split = 1; split <= 8; split *= 2) {
-            if (wk * kChunk > x_cols || (split > 1 && split * wk > chunks)) continue;
-            const int rb = 32 * (kWarps / wk);
+            if (split > 1 && split * wk > chunks) continue;
+            // (a prepared segment is one stage of each warp: the kernel's waits count on it)
+            const int xc = prepare || wk * kChunk > x_cols ? wk * kChunk : x_cols;
+            const size_t smem = (size_t)kWarps * ring_stages(nt) * stage +
+                                (prepare ? 2 : 1) * ((size_t)live * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
+            const int fit = (int)(kSmemPerSm / (smem + 1024 + 1024)), most = most_resident(nt);
+            if (fit < 1) continue;
+            const int resident = fit < most ? fit : most;
+            const int rb = kRows * (kWarps / wk);
             const double blocks = (double)((rows + rb - 1) / rb) * split * slabs;
             const double turns = (double)(int64_t)((blocks + sms - 1) / sms);
             const double bytes = (double)((chunks + split - 1) / split) * kChunk * (rb * 0.54 + live * 1.0);
             const double together = turns < resident ? turns : resident;
-            const double rate = 28.0 * together < 45.0 ? 28.0 * together : 45.0;      // bytes per ns and SM
+            const double rate = 16.0 * together < 45.0 ? 16.0 * together : 45.0;      // bytes per ns and SM
             const double t = turns * bytes / rate + (split > 1 ? 700 : 0) + (wk > 1 ? 100 : 0);
-            if (t < best_t) best_t = t, best = FewPlan{nt, wk, split, x_cols, smem};
+            if (t < best_t)
+                best_t = t, best = FewPlan{nt, wk, split, xc, x_pad, prepare, smem, prepare ? slabs * slab_bytes(nt, x_pad, 32) : 0};
         }
     return best;
 }
@@ -37,7 +44,12 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins, int sms)
 
 using namespace e2ops;
 
-extern "C" size_t e2_quant_matmul_workspace(int32_t, int32_t, int32_t) { return 0; }
+extern "C" size_t e2_quant_matmul_workspace(int32_t rows, int32_t cols, int32_t tokens)
+{
+    if (rows < 1 || cols < 1 || cols > E2_MAX_COLS || tokens < 1) return 0;
+    // (smaller groups have more sums)
+    return plan_few(rows, cols, tokens, 32, true, 152).workspace;
+}
 
 extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a, void *workspace,
                                size_t workspace_bytes, void *stream)
@@ -64,13 +76,19 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
         if (p && !on_device(p, dev.id)) return fail(E2_EINVAL, "arrays must be memory of the current device");
     const size_t need = e2_quant_matmul_workspace(w->rows, w->cols, a->tokens);
     if (need && (!workspace || workspace_bytes < need)) return fail(E2_ENOMEM, "workspace too small");
+    if (need && (!aligned(workspace, 256) || !on_device(workspace, dev.id)))
+        return fail(E2_EINVAL, "workspace must be 256-byte aligned memory of the current device");
     MatmulParams p{w->rows, w->cols, w->group, a->tokens, a->gated != 0, w->codes,
                    reinterpret_cast<const __half *>(w->scales), reinterpret_cast<const __half *>(w->mins),
                    a->x, a->residual, a->y, a->x_stride, a->residual_stride, a->y_stride};
     const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr, dev.sms);
-    const int per = kChunk / w->group;
+    // how the scales' rows are aligned
+    const int wide = w->group == 128 ? 8 : 16, groups = w->cols / w->group;
+    auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(w->scales, to) && aligned(w->mins, to); };
+    const int by = w->cols % kChunk == 0 && all_aligned(wide) ? wide : all_aligned(4) ? 4 : 2;
     FewParams q{p, outs, f.wk, f.split, __builtin_ctz((unsigned)(f.x_cols / 8)), f.x_cols,
-                w->cols % kChunk == 0 && aligned(w->scales, per * 2) && aligned(w->mins, per * 2)};
+                by,
+                static_cast<const uint8_t *>(workspace), f.x_pad};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return a->dtype == E2_F16 ? launch_few_f16(q, f, dev.id, s) : launch_few_bf16(q, f, dev.id, s);
 }

@@ -20,41 +20,57 @@ struct MatmulParams {
 
 // ---- few tokens --------------------------------------------------------------
 //
-// Bound by reading the weights.  y^T = W x^T on the warp-level tensor cores: the
-// weights are the 16-row operand, eight tokens the other, so a code is unpacked
-// once and no row is padding.  A warp owns 32 rows and streams them
-// through a ring of its own in shared memory (asynchronous copies of whole 128-byte
-// lines, no block barrier), three stages of 256 columns deep.  Codes less 8 are
-// exact in 16 bits, so the tensor cores' sums hold no rounded weight; each group's sum
-// is scaled in 32 bits.  x lies in shared memory in the order of the codes'
-// nibbles, a segment of columns at a time.  Few rows are split over columns, among a block's
-// warps (WK) and the blocks of a cluster, and joined in a fixed order.
+// Bound by reading the weights, then by the instructions that unpack them.  y^T = W
+// x^T on the warp-level tensor cores: the weights are the 16-row operand, eight
+// tokens the other, so a code is unpacked once and no row is padding.  A warp owns
+// 16 rows and streams them through a ring of its own in shared memory, two or three
+// stages of 512 columns, without a block barrier: 256 bytes of a row at a time come at 6.2
+// TB/s, 128 bytes of 32 rows at 5.8, and at 4.4 where rows are 14 KB apart.
+//
+// A code in the low four bits of a 16-bit word is the fp16 number code x 2^-24, in
+// the next four code x 2^-20 (both subnormal, exact, and the tensor cores take
+// them as they are): unpacking a word is one shift and four ANDs, and the sums hold no
+// rounded weight.  x goes to fp16 with a power of two per token and segment (its
+// largest value to 2^14..2^15: lossless over 24 binades below it), the columns
+// that meet high nibbles with another 1/16.  The 8 that codes are off by is taken out by
+// starting each group's sum at -8 sum x; each group's sum is scaled in 32 bits.
+// Few rows are split over columns, among a block's warps (wk) and the blocks of a
+// cluster (split), and joined in a fixed order.
 
-constexpr int kChunk = 256;                  // columns of a stage
-constexpr int kStages = 3;
+constexpr int kRows = 16;                    // of a warp
+constexpr int kChunk = 512;                  // columns of a stage
 constexpr int kRowBytes = kChunk / 2 + 16;   // (a stage's rows 16 bytes apart in banks)
 constexpr int kWarps = 4;
 
 constexpr int kSmemPerSm = 227 * 1024;
 
-// The launch of `tokens` tokens: how the columns are split.
+// The launch of `tokens` tokens: how the columns are split, and whether x is prepared.
 struct FewPlan {
-    int nt, wk, split, x_cols;
-    size_t smem;
+    int nt, wk, split, x_cols, x_pad;
+    bool prepare;
+    size_t smem, workspace;
 };
+
+// Stages of a warp's ring and resident blocks: what shared memory and registers hold.
+__host__ __device__ constexpr int ring_stages(int nt) { return nt == 1 ? 3 : 2; }
+__host__ __device__ constexpr int most_resident(int nt) { return nt == 4 ? 2 : 3; }
 
 template <int G, bool MINS> struct Stage {
     static constexpr int kPer = kChunk / G;                                 // scales of a row
-    static constexpr int kScaleBytes = 32 * kPer * 2;
-    static constexpr int kBytes = 32 * kRowBytes + kScaleBytes * (MINS ? 2 : 1);
+    static constexpr int kScaleBytes = kRows * kPer * 2;
+    static constexpr int kBytes = kRows * kRowBytes + kScaleBytes * (MINS ? 2 : 1);
 };
 
 struct FewParams {
     MatmulParams m;
-    int outs, wk, split, x_shift, x_cols, scales_aligned;
+    int outs, wk, split, x_shift, x_cols, scales_by;     // scales copied by 16 or 8 bytes, by 4, or one by one (2)
+    // x as prepared (PREP), per 8 NT tokens: fp16 octets [token][x_pad], the groups'
+    // sums [x_pad / group][8 NT], and 2^24 / the token's power of two
+    const uint8_t *prepared;
+    int x_pad;
 };
 
-// The bytes of x in shared memory, per token and segment (rows half a 128-byte line apart in banks).
+// x's bytes in shared memory per token and segment (rows half a 128-byte line apart in banks).
 __host__ __device__ constexpr int x_row_bytes(int cols) { return cols * 2 + 64; }
 
 __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int rank)
@@ -82,19 +98,99 @@ __device__ __forceinline__ void finish(const MatmulParams &p, int token, int row
     static_cast<T *>(p.y)[token * p.y_stride + row] = from_float<T>(y);
 }
 
-template <class T, int G, bool MINS, int NT>
-__global__ void __launch_bounds__(32 * kWarps, NT == 4 ? 2 : 3) few_kernel(const FewParams q)
+// Octets of x that a thread stages when x is not prepared.
+constexpr int kOctets = 8;
+
+// Bytes of a prepared slab of 8 nt tokens.
+__host__ __device__ constexpr size_t slab_bytes(int nt, int x_pad, int group)
 {
-    constexpr bool BF = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+    return (size_t)8 * nt * x_pad * 2 + (size_t)x_pad / group * 8 * nt * 4 + 256;
+}
+
+// 2^k that brings the largest magnitude (16 bits of T) to 2^14..2^15, k within fp32's normal range.
+template <class T> __device__ __forceinline__ int power_for(unsigned bits)
+{
+    T top;
+    *reinterpret_cast<uint16_t *>(&top) = (uint16_t)bits;
+    return bits ? min(14 + 127 - (int)(__float_as_uint(to_float(top)) >> 23), 126) : 0;
+}
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
+
+// The larger 16-bit magnitude of an octet.
+__device__ __forceinline__ unsigned octet_largest(const uint4 &v)
+{
+    const unsigned m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    return max(m & 0xffffu, m >> 16);
+}
+
+// An octet times f in fp16, in the order of the codes' nibbles, those that meet high
+// nibbles with 1/16; and its sum.
+template <class T> __device__ __forceinline__ uint4 octet_convert(const uint4 &v, float f, float &sum)
+{
+    float x[8];
+    unpack8<T>(v, x);
+    sum = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        x[j] *= f;
+        sum += x[j];
+    }
+    const __half2 h[4] = {__floats2half2_rn(x[0], x[4]), __floats2half2_rn(x[1] * 0.0625f, x[5] * 0.0625f),
+                          __floats2half2_rn(x[2], x[6]), __floats2half2_rn(x[3] * 0.0625f, x[7] * 0.0625f)};
+    return *reinterpret_cast<const uint4 *>(h);
+}
+
+// Sums as the product needs them (code 1 is 2^-24): for mins, or -8 of them.
+template <bool MINS> __device__ __forceinline__ float group_sum(float sum) { return MINS ? sum * 0x1p-24f : sum * -0x1p-21f; }
+
+// x prepared once for all blocks: a block per token.
+template <class T, int G, bool MINS> __global__ void __launch_bounds__(512) prepare_kernel(const FewParams q, uint8_t *to, int nt)
+{
+    __shared__ unsigned largest;
+    asm volatile("griddepcontrol.launch_dependents;");
+    const MatmulParams &p = q.m;
+    const int tok = blockIdx.x, col = tok % (8 * nt), octets = q.x_pad / 8;
+    if (threadIdx.x == 0) largest = 0;
+    __syncthreads();
+    const T *x = static_cast<const T *>(p.x) + tok * p.x_stride;
+    unsigned m = 0;
+    for (int o = threadIdx.x; o < p.cols / 8; o += blockDim.x) m = max(m, octet_largest(reinterpret_cast<const uint4 *>(x)[o]));
+    m = __reduce_max_sync(~0u, m);
+    if (threadIdx.x % 32 == 0) atomicMax(&largest, m);
+    __syncthreads();
+    const int k = power_for<T>(largest);
+    const float f = power_of_two(k);
+    uint8_t *slab = to + tok / (8 * nt) * slab_bytes(nt, q.x_pad, G);
+    uint4 *out = reinterpret_cast<uint4 *>(slab) + (size_t)col * octets;
+    float *sums = reinterpret_cast<float *>(slab + (size_t)8 * nt * q.x_pad * 2);
+    // (x_pad is a multiple of 512 columns: whole warps)
+    for (int o = threadIdx.x; o < octets; o += blockDim.x) {
+        uint4 v{0, 0, 0, 0};
+        if (o < p.cols / 8) v = reinterpret_cast<const uint4 *>(x)[o];
+        float sum;
+        out[o] = octet_convert<T>(v, f, sum);
+#pragma unroll
+        for (int d = 1; d < G / 8; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
+        if (o % (G / 8) == 0) sums[o / (G / 8) * (8 * nt) + col] = group_sum<MINS>(sum);
+    }
+    if (threadIdx.x == 0) sums[(size_t)q.x_pad / G * 8 * nt + col] = power_of_two(-k);
+}
+
+template <class T, int G, bool MINS, int NT, bool PREP>
+__global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(const FewParams q)
+{
     using St = Stage<G, MINS>;
-    constexpr int kPer = St::kPer;
-    const int WK = q.wk, RB = 32 * (kWarps / WK);
+    constexpr int kPer = St::kPer, kStages = ring_stages(NT);
+    const int WK = q.wk, RB = kRows * (kWarps / WK);
     extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ unsigned largest[2][8];                             // |x| bits per token, alternating segments
+    __shared__ float unscale[8 * NT];                              // 1 / the token's power of two
     const MatmulParams &p = q.m;
     const int t0 = blockIdx.y * 8 * NT, nt = min(8 * NT, p.tokens - t0);
     uint8_t *ring = smem;
-    uint8_t *xs = smem + kWarps * kStages * St::kBytes;
-    float *sx = reinterpret_cast<float *>(xs + nt * x_row_bytes(q.x_cols));
+    // x (PREP: two segments), and the groups' sums [x_cols / G][8 NT] of each
+    const int sum_bytes = q.x_cols / G * 8 * NT * 4, seg_bytes = sum_bytes + nt * x_row_bytes(q.x_cols);
+    uint8_t *xseg = smem + kWarps * kStages * St::kBytes;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, wr = warp / WK, wk = warp % WK;
     const int g = lane / 4, t = lane % 4;
     const int rank = blockIdx.x % q.split, block = blockIdx.x / q.split;
@@ -102,174 +198,247 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 4 ? 2 : 3) few_kernel(const
     const int c0 = (int)((int64_t)chunks * rank / q.split), c1 = (int)((int64_t)chunks * (rank + 1) / q.split);
     const int groups = p.cols / G;
 
-    // rows of this warp: gated, 16 rows that gate and the 16 that they gate
-    const int first = block * (p.gated ? RB / 2 : RB) + wr * (p.gated ? 16 : 32);
-    const int64_t jump = p.gated ? (int64_t)q.outs - 16 : 0;      // from ring row 16 on
-    auto source_row = [&](int r) { return (int64_t)first + r + (r >= 16 ? jump : 0); };
-    auto row_valid = [&](int r) { return first + (p.gated ? r % 16 : r) < q.outs; };
-
+    // rows of this warp (gated: 8 rows that gate and the 8 that they gate); past the
+    // last row the last one is read again, and its results are dropped
+    const int first = block * (p.gated ? RB / 2 : RB) + wr * (p.gated ? 8 : 16);
+    const int second = p.gated ? q.outs + first : first + 8;
+    auto row_of = [&](int r) {
+        const int limit = p.gated && r >= 8 ? 2 * q.outs : q.outs;
+        return (int64_t)min(r < 8 ? first + r : second + r - 8, limit - 1);
+    };
     const uint32_t my_ring = smem_addr(ring) + warp * kStages * St::kBytes;
-    // lane l copies 16 bytes (l % 8) of rows l / 8 + 4 i
-    const int part = lane % 8;
-    unsigned valid = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) valid |= (unsigned)row_valid(lane / 8 + 4 * i) << i;
+    // lane l copies 16 bytes (l % 16) of ring rows l / 16 + 2 i
+    const int part = lane % 16;
     const int64_t row_bytes = p.cols / 2;
-    const uint8_t *src = p.codes + source_row(lane / 8) * row_bytes + part * 16;
-    const bool my_row = row_valid(lane);
-    const __half *my_scales = p.scales + source_row(lane) * groups, *my_mins = MINS ? p.mins + source_row(lane) * groups : nullptr;
+    const uint8_t *base[2] = {p.codes + row_of(0) * row_bytes, p.codes + row_of(8) * row_bytes};
+    uint32_t offset[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        offset[i] = (uint32_t)((row_of(lane / 16 + 2 * i) - row_of(i < 4 ? 0 : 8)) * row_bytes);
+    // its part of the scales' wide copies
+    constexpr int kWide = kPer * 2 < 16 ? kPer * 2 : 16, kWideLanes = kRows * kPer * 2 / kWide;
+    const int64_t wide = row_of(lane * kRows / kWideLanes % kRows) * groups + lane % (kWideLanes / kRows) * (kWide / 2);
 
     auto issue = [&](int c, int slot) {
         if (c < c1) {
-            const uint32_t dst = my_ring + slot * St::kBytes;
-            const bool in = c * kChunk + part * 32 < p.cols;
-            const uint8_t *s = src + (int64_t)c * (kChunk / 2);
+            const uint32_t dst = my_ring + slot * St::kBytes, code_dst = dst + (lane / 16) * kRowBytes + part * 16;
+            // (past the last column any codes will do: x is 0 there)
+            const int at = c * (kChunk / 2) + (c * kChunk + part * 32 < p.cols ? part * 16 : 0);
+            const uint8_t *s[2] = {base[0] + at, base[1] + at};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool take = in && (valid >> i & 1);
-                const int64_t at = 4 * i * row_bytes + (i >= 4 ? jump * row_bytes : 0);
-                copy_async16(dst + (lane / 8 + 4 * i) * kRowBytes + part * 16, take ? s + at : p.codes, take);
-            }
-            // a lane per row: the chunk's scales
-            const uint32_t sd = dst + 32 * kRowBytes + lane * kPer * 2;
-            if (q.scales_aligned) {
+            for (int i = 0; i < 8; ++i) copy_async16(code_dst + 2 * i * kRowBytes, s[i / 4] + offset[i], true);
+            const uint32_t scale_dst = dst + kRows * kRowBytes;
+            if (q.scales_by > 4) {
+                if (lane < kWideLanes)
 #pragma unroll
-                for (int w = 0; w < (MINS ? 2 : 1); ++w) {
-                    const __half *f = (w ? my_mins : my_scales) + c * kPer;
-                    const bool take = my_row;
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(sd + w * St::kScaleBytes),
-                                 "l"(take ? f : p.scales), "n"(kPer * 2), "r"(take ? kPer * 2 : 0)
-                                 : "memory");
-                }
+                    for (int w = 0; w < (MINS ? 2 : 1); ++w)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(scale_dst + w * St::kScaleBytes + lane * kWide),
+                                     "l"((w ? p.mins : p.scales) + wide + c * kPer), "n"(kWide)
+                                     : "memory");
             } else {
+                // pairs of scales, zeros past the last group
 #pragma unroll
-                for (int w = 0; w < (MINS ? 2 : 1); ++w)
+                for (int i = 0; i < kPer / 4; ++i) {
+                    const int pair = i * 32 + lane, r = pair / (kPer / 2), j = pair % (kPer / 2) * 2, at = c * kPer + j;
+                    const int64_t from = row_of(r) * groups + at;
 #pragma unroll
-                    for (int j = 0; j < kPer; ++j) {
-                        const int at = c * kPer + j;
-                        uint16_t v = 0;
-                        if (my_row && at < groups) v = __half_as_ushort((w ? my_mins : my_scales)[at]);
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(sd + w * St::kScaleBytes + 2 * j), "h"(v) : "memory");
+                    for (int w = 0; w < (MINS ? 2 : 1); ++w) {
+                        const __half *f = w ? p.mins : p.scales;
+                        const uint32_t to = scale_dst + w * St::kScaleBytes + pair * 4;
+                        if (q.scales_by == 4) {
+                            copy_async4(to, at < groups ? f + from : f, at < groups);
+                        } else {
+                            const uint32_t lo = at < groups ? __half_as_ushort(f[from]) : 0u;
+                            const uint32_t hi = at + 1 < groups ? __half_as_ushort(f[from + 1]) : 0u;
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(lo | hi << 16) : "memory");
+                        }
                     }
+                }
             }
         }
         copy_commit();
     };
 
-    float y[2][NT][4] = {};
-    int next = c0 + wk;                                            // the next chunk to fetch
+    // a prepared segment on its way to shared memory
+    auto issue_x = [&](int seg, int buffer) {
+        const uint8_t *slab = q.prepared + blockIdx.y * slab_bytes(NT, q.x_pad, G);
+        const uint32_t dst = smem_addr(xseg) + buffer * seg_bytes;
+        const int live = min(q.x_cols, q.x_pad - seg * kChunk), per_row = live / 8;
+        const uint8_t *sums = slab + (size_t)8 * NT * q.x_pad * 2 + (size_t)seg * kPer * 8 * NT * 4;
+        for (int i = threadIdx.x; i < live / G * 2 * NT; i += 32 * kWarps) copy_async16(dst + i * 16, sums + i * 16, true);
+        for (int tok = warp; tok < nt; tok += kWarps)
+            for (int o = lane; o < per_row; o += 32)
+                copy_async16(dst + sum_bytes + tok * x_row_bytes(q.x_cols) + o * 16,
+                             slab + ((size_t)tok * q.x_pad + seg * kChunk + o * 8) * 2, true);
+    };
+
+    float y[NT][4] = {};
+    int next = c0 + wk, slot = 0;                                  // the next chunk to fetch
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i, next += WK) issue(next, i);
-    int slot = 0;
+    if constexpr (PREP) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (c0 < c1) issue_x(c0, 0);
+        copy_commit();
+        if (threadIdx.x < nt)
+            unscale[threadIdx.x] = reinterpret_cast<const float *>(
+                q.prepared + blockIdx.y * slab_bytes(NT, q.x_pad, G) + (size_t)8 * NT * q.x_pad * 2)[(size_t)q.x_pad / G * 8 * NT + threadIdx.x];
+    } else {
+        if (threadIdx.x < 8) largest[0][threadIdx.x] = 0;
+    }
 
-    const int octets = q.x_cols / 8;
-    for (int seg = c0; seg < c1; seg += q.x_cols / kChunk) {
-        __syncthreads();
-        // x: octets in the codes' order, zeros past the last column, groups' sums beside
-        const int total = nt * octets;
-        for (int base = 0; base < total; base += 8 * 32 * kWarps) {
-            uint4 v[8];
+    const int octets = q.x_cols / 8, total = nt * octets;          // not prepared: total <= kOctets * threads
+    int flip = 0;
+    for (int seg = c0; seg < c1; seg += q.x_cols / kChunk, flip ^= 1) {
+        float *sx = reinterpret_cast<float *>(xseg + (PREP ? flip * seg_bytes : 0));
+        uint8_t *xs = reinterpret_cast<uint8_t *>(sx) + sum_bytes;
+        if constexpr (PREP) {
+            // (newer than the segment's copy: nothing of the first's, else a stage or more)
+            if (seg == c0) copy_wait<0>();
+            else copy_wait<1>();
+            __syncthreads();
+            if (seg + q.x_cols / kChunk < c1) issue_x(seg + q.x_cols / kChunk, flip ^ 1);
+            copy_commit();
+        } else {
+            __syncthreads();
+            uint4 v[kOctets];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = base + i * 32 * kWarps + threadIdx.x;
-                const int tok = at >> q.x_shift, o = at & (octets - 1), col = seg * kChunk + o * 8;
+            for (int i = 0; i < kOctets; ++i) {
+                const int at = i * 32 * kWarps + threadIdx.x;
+                const int tok = at >> q.x_shift, col = seg * kChunk + (at & (octets - 1)) * 8;
                 v[i] = uint4{0, 0, 0, 0};
                 if (at < total && col < p.cols)
                     v[i] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + (t0 + tok) * p.x_stride + col);
             }
+            if (threadIdx.x < 8) largest[flip ^ 1][threadIdx.x] = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = base + i * 32 * kWarps + threadIdx.x;
-                const int tok = at >> q.x_shift, o = at & (octets - 1);
-                if (MINS) {
-                    float e[8], sum = 0;
-                    unpack8<T>(v[i], e);
+            for (int i = 0; i < kOctets; ++i) {
+                // (a warp's 32 octets are of one token)
+                const unsigned m = __reduce_max_sync(~0u, octet_largest(v[i]));
+                const int at = i * 32 * kWarps + threadIdx.x;
+                if (lane == 0 && at < total) atomicMax(&largest[flip][at >> q.x_shift], m);
+            }
+            __syncthreads();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum += e[j];
+            for (int i = 0; i < kOctets; ++i) {
+                const int at = i * 32 * kWarps + threadIdx.x;
+                const int tok = at < total ? at >> q.x_shift : 0, o = at & (octets - 1);
+                const int k = power_for<T>(largest[flip][tok]);
+                float sum;
+                const uint4 w = octet_convert<T>(v[i], power_of_two(k), sum);
 #pragma unroll
-                    for (int d = 1; d < G / 8; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
-                    if (at < total && o % (G / 8) == 0) sx[tok * (q.x_cols / G) + o / (G / 8)] = sum;
-                }
+                for (int d = 1; d < G / 8; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
                 if (at < total) {
-                    uint4 w;
-                    w.x = __byte_perm(v[i].x, v[i].z, 0x5410);
-                    w.y = __byte_perm(v[i].x, v[i].z, 0x7632);
-                    w.z = __byte_perm(v[i].y, v[i].w, 0x5410);
-                    w.w = __byte_perm(v[i].y, v[i].w, 0x7632);
+                    if (o % (G / 8) == 0) sx[o / (G / 8) * (8 * NT) + tok] = group_sum<MINS>(sum);
+                    if (o == 0) unscale[tok] = power_of_two(-k);
                     *reinterpret_cast<uint4 *>(xs + tok * x_row_bytes(q.x_cols) + o * 16) = w;
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
         const int seg_end = min(seg + q.x_cols / kChunk, c1);
+        float ys[NT][4];                                           // (prepared: one scale for all of x)
+#pragma unroll
+        for (int i = 0; i < 4 * NT; ++i) (&ys[0][0])[i] = PREP ? (&y[0][0])[i] : 0.0f;
         for (int c = seg + wk; c < seg_end; c += WK) {
-            copy_wait<kStages - 2>();
+            // (prepared: the next segment's copy is newer too)
+            copy_wait<PREP ? kStages - 1 : kStages - 2>();
             __syncwarp();
             issue(next, slot == 0 ? kStages - 1 : slot - 1);
             next += WK;
-            const uint32_t st = my_ring + slot * St::kBytes;
+            const uint8_t *st = ring + (warp * kStages + slot) * St::kBytes;
             slot = slot == kStages - 1 ? 0 : slot + 1;
-            // matrix i of a load: ring rows 8 i ..
-            const uint32_t mat = st + lane * kRowBytes;
-            __half2 sc[4][(kPer + 1) / 2], mn[4][MINS ? (kPer + 1) / 2 : 1];
+            // matrices of a load: rows 0-7 and 8-15 of 32 columns, and of the next 32
+            const uint32_t mat = smem_addr(st) + lane % 16 * kRowBytes + lane / 16 * 16;
+            constexpr int kVec = kPer * 2 < 16 ? 1 : kPer * 2 / 16;
+            union Scales {
+                uint4 v[kVec];
+                uint2 d;
+                __half h[kPer < 8 ? 8 : kPer];
+            } sc[2], mn[MINS ? 2 : 1];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 2; ++r) {
+                const uint8_t *f = st + kRows * kRowBytes + (g + 8 * r) * kPer * 2;
+                if constexpr (kPer == 4) {
+                    sc[r].d = *reinterpret_cast<const uint2 *>(f);
+                    if (MINS) mn[r].d = *reinterpret_cast<const uint2 *>(f + St::kScaleBytes);
+                } else {
 #pragma unroll
-                for (int j = 0; j < kPer / 2; ++j) {
-                    const uint8_t *f = ring + (st - smem_addr(ring)) + 32 * kRowBytes + (g + 8 * r) * kPer * 2 + 4 * j;
-                    sc[r][j] = *reinterpret_cast<const __half2 *>(f);
-                    if (MINS) mn[r][j] = *reinterpret_cast<const __half2 *>(f + St::kScaleBytes);
+                    for (int j = 0; j < kVec; ++j) {
+                        sc[r].v[j] = reinterpret_cast<const uint4 *>(f)[j];
+                        if (MINS) mn[r].v[j] = reinterpret_cast<const uint4 *>(f + St::kScaleBytes)[j];
+                    }
                 }
+            }
             const uint8_t *xb[NT];
+            const float *sb = sx + (c - seg) * kPer * (8 * NT) + 2 * t;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
                 xb[n] = xs + min(8 * n + g, nt - 1) * x_row_bytes(q.x_cols) + (c - seg) * kChunk * 2 + t * 16;
+            // (the next operands are on their way while these are multiplied)
+            uint32_t w[2][4];
+            uint4 b[2][NT];
+            auto fetch_w = [&](int at) { load_matrices(w[at / 2 % 2], mat + at * 16); };
+            auto fetch_x = [&](int at) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) b[at % 2][n] = *reinterpret_cast<const uint4 *>(xb[n] + at * 64);
+            };
+            fetch_w(0);
+            fetch_x(0);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
-                float acc[2][NT][4] = {};
+                float acc[NT][4];
+                float2 sums[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sums[n] = *reinterpret_cast<const float2 *>(sb + j * (8 * NT) + 8 * n);
 #pragma unroll
                 for (int u = 0; u < G / 32; ++u) {
                     const int at = j * (G / 32) + u;
-                    uint32_t w[4];
-                    load_matrices(w, mat + at * 16);
-                    uint4 b[NT];
+                    if (at % 2 == 0 && at + 2 < kChunk / 32) fetch_w(at + 2);
+                    if (at + 1 < kChunk / 32) fetch_x(at + 1);
+                    const uint32_t lo = 0x000f000fu, hi = 0x00f000f0u;
+                    const uint32_t a = w[at / 2 % 2][at % 2 * 2], d = w[at / 2 % 2][at % 2 * 2 + 1], a8 = a >> 8, d8 = d >> 8;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) b[n] = *reinterpret_cast<const uint4 *>(xb[n] + at * 64);
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        uint32_t a[4], d[4];
-                        centred_codes<BF>(w[2 * m], a);
-                        centred_codes<BF>(w[2 * m + 1], d);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            multiply<BF>(acc[m][n], a[0], d[0], a[1], d[1], b[n].x, b[n].y);
-                            multiply<BF>(acc[m][n], a[2], d[2], a[3], d[3], b[n].z, b[n].w);
-                        }
+                    for (int n = 0; n < NT; ++n) {
+                        const float start[4] = {MINS ? 0.0f : sums[n].x, MINS ? 0.0f : sums[n].y,
+                                                MINS ? 0.0f : sums[n].x, MINS ? 0.0f : sums[n].y};
+                        const uint4 &x = b[at % 2][n];
+                        if (u == 0) multiply(acc[n], a & lo, d & lo, a & hi, d & hi, x.x, x.y, start);
+                        else multiply(acc[n], a & lo, d & lo, a & hi, d & hi, x.x, x.y, acc[n]);
+                        multiply(acc[n], a8 & lo, d8 & lo, a8 & hi, d8 & hi, x.z, x.w, acc[n]);
                     }
                 }
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int r = 0; r < 2; ++r) {
+                    const float s = __half2float(sc[r].h[j]), z = MINS ? __half2float(mn[MINS ? r : 0].h[j]) : 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const __half2 s2 = sc[2 * m + r][j / 2];
-                        const float s = __half2float(j % 2 ? __high2half(s2) : __low2half(s2));
-                        float z = 0;
-                        if (MINS) {
-                            const __half2 m2 = mn[2 * m + r][j / 2];
-                            z = __fmaf_rn(8.0f, s, __half2float(j % 2 ? __high2half(m2) : __low2half(m2)));
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float v = __fmaf_rn(s, acc[n][2 * r + e], ys[n][2 * r + e]);
+                            if (MINS) v = __fmaf_rn(z, e ? sums[n].y : sums[n].x, v);
+                            ys[n][2 * r + e] = v;
                         }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float v = __fmaf_rn(s, acc[m][n][2 * r + e], y[m][n][2 * r + e]);
-                                if (MINS)
-                                    v = __fmaf_rn(z, sx[min(8 * n + 2 * t + e, nt - 1) * (q.x_cols / G) + (c - seg) * kPer + j], v);
-                                y[m][n][2 * r + e] = v;
-                            }
-                    }
+                }
             }
         }
+        if constexpr (PREP) {
+#pragma unroll
+            for (int i = 0; i < 4 * NT; ++i) (&y[0][0])[i] = (&ys[0][0])[i];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = unscale[min(2 * t + e % 2, nt - 1)];
+                y[0][e] = __fmaf_rn(ys[0][e] * 0x1p24f, f, y[0][e]);
+            }
+        }
+    }
+    if constexpr (PREP) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                y[n][e] = y[n][e] * 0x1p24f * unscale[min(8 * n + 2 * t + e % 2, nt - 1)];
     }
 
     if (WK == 1 && q.split == 1) {
@@ -277,14 +446,10 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 4 ? 2 : 3) few_kernel(const
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int tok = 8 * n + 2 * t + e % 2, r = first + g + 8 * (e / 2);
-                if (tok >= nt) continue;
-                if (p.gated) {
-                    if (r < q.outs) finish<T>(p, t0 + tok, r, y[0][n][e], y[1][n][e]);
-                } else {
-                    if (r < q.outs) finish<T>(p, t0 + tok, r, y[0][n][e], 0.0f);
-                    if (r + 16 < q.outs) finish<T>(p, t0 + tok, r + 16, y[1][n][e], 0.0f);
-                }
+                // rows g and g + 8: two outputs, or what gates and what is gated
+                const int tok = 8 * n + 2 * t + e % 2, r = first + g + (p.gated ? 0 : 8 * (e / 2));
+                if (tok >= nt || r >= q.outs || (p.gated && e >= 2)) continue;
+                finish<T>(p, t0 + tok, r, y[n][e], y[n][e | 2]);
             }
         return;
     }
@@ -293,12 +458,10 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 4 ? 2 : 3) few_kernel(const
     __syncthreads();
     float *red = reinterpret_cast<float *>(ring);                  // [WK][RB][8 NT]
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                red[(wk * RB + wr * 32 + 16 * m + g + 8 * (e / 2)) * (8 * NT) + 8 * n + 2 * t + e % 2] = y[m][n][e];
+        for (int e = 0; e < 4; ++e)
+            red[(wk * RB + wr * kRows + g + 8 * (e / 2)) * (8 * NT) + 8 * n + 2 * t + e % 2] = y[n][e];
     __syncthreads();
     if (WK > 1) {
         for (int i = threadIdx.x; i < RB * 8 * NT; i += 32 * kWarps) {
@@ -310,57 +473,66 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 4 ? 2 : 3) few_kernel(const
     }
     if (q.split > 1) cluster_barrier();
     const uint32_t mine = smem_addr(red);
-    auto total = [&](int i) {
+    auto joined = [&](int i) {
         if (q.split == 1) return red[i];
         float v = 0;
         for (int k = 0; k < q.split; ++k) v += peer_load(peer_addr(mine + 4 * i, k));
         return v;
     };
-    const int rows = p.gated ? RB / 2 : RB, base = block * rows;
+    const int rows = p.gated ? RB / 2 : RB, out0 = block * rows;
     for (int i = threadIdx.x + rank * 32 * kWarps; i < rows * 8 * NT; i += 32 * kWarps * q.split) {
         // rows vary fastest: neighbouring outputs
         const int r = i % rows, tok = i / rows;
-        if (tok >= nt || base + r >= q.outs) continue;
+        if (tok >= nt || out0 + r >= q.outs) continue;
         if (p.gated) {
-            const int at = (r / 16 * 32 + r % 16) * (8 * NT) + tok;
-            finish<T>(p, t0 + tok, base + r, total(at), total(at + 16 * 8 * NT));
+            const int at = (r / 8 * 16 + r % 8) * (8 * NT) + tok;
+            finish<T>(p, t0 + tok, out0 + r, joined(at), joined(at + 8 * 8 * NT));
         } else {
-            finish<T>(p, t0 + tok, base + r, total(r * (8 * NT) + tok), 0.0f);
+            finish<T>(p, t0 + tok, out0 + r, joined(r * (8 * NT) + tok), 0.0f);
         }
     }
     if (q.split > 1) cluster_barrier();                            // (peers may still read)
 }
 
-template <class T, int G, bool MINS, int NT>
+template <class T, int G, bool MINS, int NT, bool PREP>
 int launch_few(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
 {
     static std::atomic<uint64_t> ready{0};                         // devices that have the attribute set
-    auto kernel = few_kernel<T, G, MINS, NT>;
+    auto kernel = few_kernel<T, G, MINS, NT, PREP>;
     if (!(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm - 2048);
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    const int rb = (q.m.gated ? 16 : 32) * (kWarps / q.wk);
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)f.split;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    if (PREP) prepare_kernel<T, G, MINS><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, const_cast<uint8_t *>(q.prepared), NT);
+    const int rb = (q.m.gated ? 8 : 16) * (kWarps / q.wk);
+    cudaLaunchAttribute at[2]{};
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((q.outs + rb - 1) / rb * f.split), (unsigned)((q.m.tokens + 8 * NT - 1) / (8 * NT)));
     cfg.blockDim = dim3(32 * kWarps);
     cfg.dynamicSmemBytes = f.smem;
     cfg.stream = s;
-    cfg.attrs = &at;
-    cfg.numAttrs = f.split > 1 ? 1 : 0;
+    cfg.attrs = at;
+    if (f.split > 1) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        at[cfg.numAttrs].val.clusterDim.x = (unsigned)f.split;
+        at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    if (PREP) {
+        // placed while x is prepared: fetches its first weights, then waits
+        at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
     return cuda_status(cudaLaunchKernelEx(&cfg, kernel, q));
 }
 
 template <class T, int G, bool MINS> int launch_group(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
 {
-    return f.nt == 1   ? launch_few<T, G, MINS, 1>(q, f, dev, s)
-           : f.nt == 2 ? launch_few<T, G, MINS, 2>(q, f, dev, s)
-                       : launch_few<T, G, MINS, 4>(q, f, dev, s);
+    if (f.nt == 1)
+        return f.prepare ? launch_few<T, G, MINS, 1, true>(q, f, dev, s) : launch_few<T, G, MINS, 1, false>(q, f, dev, s);
+    return f.nt == 2 ? launch_few<T, G, MINS, 2, true>(q, f, dev, s) : launch_few<T, G, MINS, 4, true>(q, f, dev, s);
 }
 
 template <class T> int launch_type(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
