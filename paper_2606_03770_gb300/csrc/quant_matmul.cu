@@ -4,39 +4,40 @@
 namespace e2ops {
 namespace {
 
-FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins, int sms)
+// Blocks to have at least: 1.6 per multiprocessor keep the memory busy (one where 32
+// tokens leave room for two).
+constexpr int kFewBlocks = 250, kFewBlocks32 = 150;
+
+// Rows alone where they make enough blocks; else columns are split: in two by a
+// cluster, further among the four warps of a block first (no cluster to join), then by
+// clusters of up to eight.  Measured, us (one token, 64 columns a group; joined by warps x
+// clusters): 4096 x 4096 4x1 6.8, 1x4 7.1, 2x2 7.9; 10240 x 8192 1x2 15.8, 2x1 17.6, 4x1
+// 18.9, 1x1 28; 57344 x 8192 1x1 56, 1x2 57, 2x1 62; 1024 x 16384 4x4 8.5, 1x8 11.
+FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
 {
-    FewPlan best{};
-    double best_t = 1e30;
     const int nt = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4, live = tokens < 8 * nt ? tokens : 8 * nt;
-    const bool prepare = tokens > 2;
     const int chunks = (cols + kChunk - 1) / kChunk, x_pad = chunks * kChunk;
     const int per = kChunk / group, stage = kRows * (kRowBytes + per * 2 * (mins ? 2 : 1));
-    const int slabs = (tokens + 8 * nt - 1) / (8 * nt);
-    int x_cols = 512;
-    if (!prepare)
-        while (x_cols < 4096 && live * x_cols / 4 <= kOctets * 32 * kWarps) x_cols *= 2;
-    for (int wk = 1; wk <= kWarps; wk *= 2)
-        for (int split = 1; split <= 8; split *= 2) {
-            if (split > 1 && split * wk > chunks) continue;
-            // (a prepared segment is one stage of each warp: the kernel's waits count on it)
-            const int xc = prepare || wk * kChunk > x_cols ? wk * kChunk : x_cols;
-            const size_t smem = (size_t)kWarps * ring_stages(nt) * stage +
-                                (prepare ? 2 : 1) * ((size_t)live * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
-            const int fit = (int)(kSmemPerSm / (smem + 1024 + 1024)), most = most_resident(nt);
-            if (fit < 1) continue;
-            const int resident = fit < most ? fit : most;
-            const int rb = kRows * (kWarps / wk);
-            const double blocks = (double)((rows + rb - 1) / rb) * split * slabs;
-            const double turns = (double)(int64_t)((blocks + sms - 1) / sms);
-            const double bytes = (double)((chunks + split - 1) / split) * kChunk * (rb * 0.54 + live * 1.0);
-            const double together = turns < resident ? turns : resident;
-            const double rate = 16.0 * together < 45.0 ? 16.0 * together : 45.0;      // bytes per ns and SM
-            const double t = turns * bytes / rate + (split > 1 ? 700 : 0) + (wk > 1 ? 100 : 0);
-            if (t < best_t)
-                best_t = t, best = FewPlan{nt, wk, split, xc, x_pad, prepare, smem, prepare ? slabs * slab_bytes(nt, x_pad, 32) : 0};
-        }
-    return best;
+    const int slabs = (tokens + 8 * nt - 1) / (8 * nt), want = nt == 4 ? kFewBlocks32 : kFewBlocks;
+    auto plan = [&](int wk, int split) {
+        // all of x at once where that leaves room, else a stage of each warp at a time, two in turn
+        const int mine = (chunks + split - 1) / split * kChunk;
+        const bool whole = (size_t)live * mine * 2 <= 25 * 1024;
+        const int xc = whole ? mine : wk * kChunk;
+        const size_t smem = (size_t)kWarps * ring_stages(nt) * stage +
+                            (whole ? 1 : 2) * ((size_t)live * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
+        return FewPlan{nt, wk, split, xc, x_pad, smem, slabs * slab_bytes(nt, x_pad, 32)};
+    };
+    auto blocks = [&](int wk, int split) {
+        const int rb = kRows * kWarps / wk;
+        return (int64_t)((rows + rb - 1) / rb) * split * slabs;
+    };
+    if (blocks(1, 1) >= want || chunks == 1) return plan(1, 1);
+    if (blocks(1, 2) >= want) return plan(1, 2);
+    int wk = kWarps, split = 1;
+    while (wk > 1 && plan(wk, split).smem > (size_t)kSmemPerSm / 2 - 2048) wk /= 2;
+    while (split < 8 && blocks(wk, split) < want && wk * split * 2 <= chunks) split *= 2;
+    return plan(wk, split);
 }
 
 }  // namespace
@@ -48,7 +49,7 @@ extern "C" size_t e2_quant_matmul_workspace(int32_t rows, int32_t cols, int32_t 
 {
     if (rows < 1 || cols < 1 || cols > E2_MAX_COLS || tokens < 1) return 0;
     // (smaller groups have more sums)
-    return plan_few(rows, cols, tokens, 32, true, 152).workspace;
+    return plan_few(rows, cols, tokens, 32, true).workspace;
 }
 
 extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a, void *workspace,
@@ -78,17 +79,19 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
     if (need && (!workspace || workspace_bytes < need)) return fail(E2_ENOMEM, "workspace too small");
     if (need && (!aligned(workspace, 256) || !on_device(workspace, dev.id)))
         return fail(E2_EINVAL, "workspace must be 256-byte aligned memory of the current device");
-    MatmulParams p{w->rows, w->cols, w->group, a->tokens, a->gated != 0, w->codes,
+    MatmulParams p{w->rows, w->cols, w->group, a->tokens, a->gated != 0, a->dtype == E2_F16, w->codes,
                    reinterpret_cast<const __half *>(w->scales), reinterpret_cast<const __half *>(w->mins),
                    a->x, a->residual, a->y, a->x_stride, a->residual_stride, a->y_stride};
-    const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr, dev.sms);
+    const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr);
     // how the scales' rows are aligned
     const int wide = w->group == 128 ? 8 : 16, groups = w->cols / w->group;
     auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(w->scales, to) && aligned(w->mins, to); };
     const int by = w->cols % kChunk == 0 && all_aligned(wide) ? wide : all_aligned(4) ? 4 : 2;
-    FewParams q{p, outs, f.wk, f.split, __builtin_ctz((unsigned)(f.x_cols / 8)), f.x_cols,
+    FewParams q{p, outs, f.wk, f.split, f.x_cols,
                 by,
                 static_cast<const uint8_t *>(workspace), f.x_pad};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return a->dtype == E2_F16 ? launch_few_f16(q, f, dev.id, s) : launch_few_bf16(q, f, dev.id, s);
+    return w->group == 32   ? launch_few_32(q, f, dev.id, s)
+           : w->group == 64 ? launch_few_64(q, f, dev.id, s)
+                            : launch_few_128(q, f, dev.id, s);
 }

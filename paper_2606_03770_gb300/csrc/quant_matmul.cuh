@@ -10,7 +10,7 @@
 namespace e2ops {
 
 struct MatmulParams {
-    int rows, cols, group, tokens, gated;
+    int rows, cols, group, tokens, gated, half;                // half: x, residual and y are fp16, else bf16
     const uint8_t *codes;
     const __half *scales, *mins;
     const void *x, *residual;
@@ -30,9 +30,9 @@ struct MatmulParams {
 // A code in the low four bits of a 16-bit word is the fp16 number code x 2^-24, in
 // the next four code x 2^-20 (both subnormal, exact, and the tensor cores take
 // them as they are): unpacking a word is one shift and four ANDs, and the sums hold no
-// rounded weight.  x goes to fp16 with a power of two per token and segment (its
-// largest value to 2^14..2^15: lossless over 24 binades below it), the columns
-// that meet high nibbles with another 1/16.  The 8 that codes are off by is taken out by
+// rounded weight.  x goes to fp16 with a power of two per token (its largest
+// value to 2^14..2^15: lossless over 24 binades below it), the columns that meet high
+// nibbles with another 1/16, once in a kernel before.  The 8 that codes are off by is taken out by
 // starting each group's sum at -8 sum x; each group's sum is scaled in 32 bits.
 // Few rows are split over columns, among a block's warps (wk) and the blocks of a
 // cluster (split), and joined in a fixed order.
@@ -44,10 +44,9 @@ constexpr int kWarps = 4;
 
 constexpr int kSmemPerSm = 227 * 1024;
 
-// The launch of `tokens` tokens: how the columns are split, and whether x is prepared.
+// The launch of `tokens` tokens: how the columns are split.
 struct FewPlan {
     int nt, wk, split, x_cols, x_pad;
-    bool prepare;
     size_t smem, workspace;
 };
 
@@ -63,8 +62,8 @@ template <int G, bool MINS> struct Stage {
 
 struct FewParams {
     MatmulParams m;
-    int outs, wk, split, x_shift, x_cols, scales_by;     // scales copied by 16 or 8 bytes, by 4, or one by one (2)
-    // x as prepared (PREP), per 8 NT tokens: fp16 octets [token][x_pad], the groups'
+    int outs, wk, split, x_cols, scales_by;     // scales copied by 16 or 8 bytes, by 4, or one by one (2)
+    // x as prepared, per 8 NT tokens: fp16 octets [token][x_pad], the groups'
     // sums [x_pad / group][8 NT], and 2^24 / the token's power of two
     const uint8_t *prepared;
     int x_pad;
@@ -91,15 +90,17 @@ __device__ __forceinline__ void cluster_barrier()
 }
 
 template <class T>
-__device__ __forceinline__ void finish(const MatmulParams &p, int token, int row, float a, float b)
+__device__ __forceinline__ void finish_as(const MatmulParams &p, int token, int row, float a, float b)
 {
     float y = p.gated ? a / (1.0f + expf(-a)) * b : a;
     if (p.residual) y += to_float(static_cast<const T *>(p.residual)[token * p.residual_stride + row]);
     static_cast<T *>(p.y)[token * p.y_stride + row] = from_float<T>(y);
 }
-
-// Octets of x that a thread stages when x is not prepared.
-constexpr int kOctets = 8;
+__device__ __forceinline__ void finish(const MatmulParams &p, int token, int row, float a, float b)
+{
+    if (p.half) finish_as<__half>(p, token, row, a, b);
+    else finish_as<__nv_bfloat16>(p, token, row, a, b);
+}
 
 // Bytes of a prepared slab of 8 nt tokens.
 __host__ __device__ constexpr size_t slab_bytes(int nt, int x_pad, int group)
@@ -176,19 +177,18 @@ template <class T, int G, bool MINS> __global__ void __launch_bounds__(512) prep
     if (threadIdx.x == 0) sums[(size_t)q.x_pad / G * 8 * nt + col] = power_of_two(-k);
 }
 
-template <class T, int G, bool MINS, int NT, bool PREP>
+template <int G, bool MINS, int NT>
 __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(const FewParams q)
 {
     using St = Stage<G, MINS>;
     constexpr int kPer = St::kPer, kStages = ring_stages(NT);
     const int WK = q.wk, RB = kRows * (kWarps / WK);
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ unsigned largest[2][8];                             // |x| bits per token, alternating segments
     __shared__ float unscale[8 * NT];                              // 1 / the token's power of two
     const MatmulParams &p = q.m;
     const int t0 = blockIdx.y * 8 * NT, nt = min(8 * NT, p.tokens - t0);
     uint8_t *ring = smem;
-    // x (PREP: two segments), and the groups' sums [x_cols / G][8 NT] of each
+    // x (one segment, or two in turn), and the groups' sums [x_cols / G][8 NT] of each
     const int sum_bytes = q.x_cols / G * 8 * NT * 4, seg_bytes = sum_bytes + nt * x_row_bytes(q.x_cols);
     uint8_t *xseg = smem + kWarps * kStages * St::kBytes;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, wr = warp / WK, wk = warp % WK;
@@ -276,73 +276,28 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
     int next = c0 + wk, slot = 0;                                  // the next chunk to fetch
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i, next += WK) issue(next, i);
-    if constexpr (PREP) {
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        if (c0 < c1) issue_x(c0, 0);
-        copy_commit();
-        if (threadIdx.x < nt)
-            unscale[threadIdx.x] = reinterpret_cast<const float *>(
-                q.prepared + blockIdx.y * slab_bytes(NT, q.x_pad, G) + (size_t)8 * NT * q.x_pad * 2)[(size_t)q.x_pad / G * 8 * NT + threadIdx.x];
-    } else {
-        if (threadIdx.x < 8) largest[0][threadIdx.x] = 0;
-    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    issue_x(c0, 0);
+    copy_commit();
+    if (threadIdx.x < nt)
+        unscale[threadIdx.x] = reinterpret_cast<const float *>(
+            q.prepared + blockIdx.y * slab_bytes(NT, q.x_pad, G) + (size_t)8 * NT * q.x_pad * 2)[(size_t)q.x_pad / G * 8 * NT + threadIdx.x];
 
-    const int octets = q.x_cols / 8, total = nt * octets;          // not prepared: total <= kOctets * threads
     int flip = 0;
     for (int seg = c0; seg < c1; seg += q.x_cols / kChunk, flip ^= 1) {
-        float *sx = reinterpret_cast<float *>(xseg + (PREP ? flip * seg_bytes : 0));
+        float *sx = reinterpret_cast<float *>(xseg + flip * seg_bytes);
         uint8_t *xs = reinterpret_cast<uint8_t *>(sx) + sum_bytes;
-        if constexpr (PREP) {
-            // (newer than the segment's copy: nothing of the first's, else a stage or more)
-            if (seg == c0) copy_wait<0>();
-            else copy_wait<1>();
-            __syncthreads();
-            if (seg + q.x_cols / kChunk < c1) issue_x(seg + q.x_cols / kChunk, flip ^ 1);
-            copy_commit();
-        } else {
-            __syncthreads();
-            uint4 v[kOctets];
-#pragma unroll
-            for (int i = 0; i < kOctets; ++i) {
-                const int at = i * 32 * kWarps + threadIdx.x;
-                const int tok = at >> q.x_shift, col = seg * kChunk + (at & (octets - 1)) * 8;
-                v[i] = uint4{0, 0, 0, 0};
-                if (at < total && col < p.cols)
-                    v[i] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + (t0 + tok) * p.x_stride + col);
-            }
-            if (threadIdx.x < 8) largest[flip ^ 1][threadIdx.x] = 0;
-#pragma unroll
-            for (int i = 0; i < kOctets; ++i) {
-                // (a warp's 32 octets are of one token)
-                const unsigned m = __reduce_max_sync(~0u, octet_largest(v[i]));
-                const int at = i * 32 * kWarps + threadIdx.x;
-                if (lane == 0 && at < total) atomicMax(&largest[flip][at >> q.x_shift], m);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kOctets; ++i) {
-                const int at = i * 32 * kWarps + threadIdx.x;
-                const int tok = at < total ? at >> q.x_shift : 0, o = at & (octets - 1);
-                const int k = power_for<T>(largest[flip][tok]);
-                float sum;
-                const uint4 w = octet_convert<T>(v[i], power_of_two(k), sum);
-#pragma unroll
-                for (int d = 1; d < G / 8; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
-                if (at < total) {
-                    if (o % (G / 8) == 0) sx[o / (G / 8) * (8 * NT) + tok] = group_sum<MINS>(sum);
-                    if (o == 0) unscale[tok] = power_of_two(-k);
-                    *reinterpret_cast<uint4 *>(xs + tok * x_row_bytes(q.x_cols) + o * 16) = w;
-                }
-            }
-            __syncthreads();
-        }
+        // (newer than the segment's copy: nothing of the first's, else a stage or more)
+        if (seg == c0) copy_wait<0>();
+        else copy_wait<1>();
+        __syncthreads();
+        if (seg + q.x_cols / kChunk < c1) issue_x(seg + q.x_cols / kChunk, flip ^ 1);
+        copy_commit();
         const int seg_end = min(seg + q.x_cols / kChunk, c1);
-        float ys[NT][4];                                           // (prepared: one scale for all of x)
-#pragma unroll
-        for (int i = 0; i < 4 * NT; ++i) (&ys[0][0])[i] = PREP ? (&y[0][0])[i] : 0.0f;
         for (int c = seg + wk; c < seg_end; c += WK) {
-            // (prepared: the next segment's copy is newer too)
-            copy_wait<PREP ? kStages - 1 : kStages - 2>();
+            // (the segment's first stage: the next segment's copy is newer too)
+            if (c == seg + wk) copy_wait<kStages - 1>();
+            else copy_wait<kStages - 2>();
             __syncwarp();
             issue(next, slot == 0 ? kStages - 1 : slot - 1);
             next += WK;
@@ -415,31 +370,18 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float v = __fmaf_rn(s, acc[n][2 * r + e], ys[n][2 * r + e]);
+                            float v = __fmaf_rn(s, acc[n][2 * r + e], y[n][2 * r + e]);
                             if (MINS) v = __fmaf_rn(z, e ? sums[n].y : sums[n].x, v);
-                            ys[n][2 * r + e] = v;
+                            y[n][2 * r + e] = v;
                         }
                 }
             }
         }
-        if constexpr (PREP) {
-#pragma unroll
-            for (int i = 0; i < 4 * NT; ++i) (&y[0][0])[i] = (&ys[0][0])[i];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float f = unscale[min(2 * t + e % 2, nt - 1)];
-                y[0][e] = __fmaf_rn(ys[0][e] * 0x1p24f, f, y[0][e]);
-            }
-        }
     }
-    if constexpr (PREP) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                y[n][e] = y[n][e] * 0x1p24f * unscale[min(8 * n + 2 * t + e % 2, nt - 1)];
-    }
+        for (int e = 0; e < 4; ++e) y[n][e] = y[n][e] * 0x1p24f * unscale[min(8 * n + 2 * t + e % 2, nt - 1)];
 
     if (WK == 1 && q.split == 1) {
 #pragma unroll
@@ -449,7 +391,7 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
                 // rows g and g + 8: two outputs, or what gates and what is gated
                 const int tok = 8 * n + 2 * t + e % 2, r = first + g + (p.gated ? 0 : 8 * (e / 2));
                 if (tok >= nt || r >= q.outs || (p.gated && e >= 2)) continue;
-                finish<T>(p, t0 + tok, r, y[n][e], y[n][e | 2]);
+                finish(p, t0 + tok, r, y[n][e], y[n][e | 2]);
             }
         return;
     }
@@ -486,25 +428,26 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
         if (tok >= nt || out0 + r >= q.outs) continue;
         if (p.gated) {
             const int at = (r / 8 * 16 + r % 8) * (8 * NT) + tok;
-            finish<T>(p, t0 + tok, out0 + r, joined(at), joined(at + 8 * 8 * NT));
+            finish(p, t0 + tok, out0 + r, joined(at), joined(at + 8 * 8 * NT));
         } else {
-            finish<T>(p, t0 + tok, out0 + r, joined(r * (8 * NT) + tok), 0.0f);
+            finish(p, t0 + tok, out0 + r, joined(r * (8 * NT) + tok), 0.0f);
         }
     }
     if (q.split > 1) cluster_barrier();                            // (peers may still read)
 }
 
-template <class T, int G, bool MINS, int NT, bool PREP>
-int launch_few(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
+template <int G, bool MINS, int NT> int launch_few(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
 {
     static std::atomic<uint64_t> ready{0};                         // devices that have the attribute set
-    auto kernel = few_kernel<T, G, MINS, NT, PREP>;
+    auto kernel = few_kernel<G, MINS, NT>;
     if (!(ready.load(std::memory_order_relaxed) >> dev & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm - 2048);
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    if (PREP) prepare_kernel<T, G, MINS><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, const_cast<uint8_t *>(q.prepared), NT);
+    uint8_t *to = const_cast<uint8_t *>(q.prepared);
+    if (q.m.half) prepare_kernel<__half, G, MINS><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, to, NT);
+    else prepare_kernel<__nv_bfloat16, G, MINS><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, to, NT);
     const int rb = (q.m.gated ? 8 : 16) * (kWarps / q.wk);
     cudaLaunchAttribute at[2]{};
     cudaLaunchConfig_t cfg{};
@@ -513,40 +456,30 @@ int launch_few(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
     cfg.dynamicSmemBytes = f.smem;
     cfg.stream = s;
     cfg.attrs = at;
-    if (f.split > 1) {
-        at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-        at[cfg.numAttrs].val.clusterDim.x = (unsigned)f.split;
-        at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
-        ++cfg.numAttrs;
-    }
-    if (PREP) {
-        // placed while x is prepared: fetches its first weights, then waits
-        at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-        ++cfg.numAttrs;
-    }
+    // placed while x is prepared: fetches its first weights, then waits
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)f.split;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.numAttrs = f.split > 1 ? 2 : 1;
     return cuda_status(cudaLaunchKernelEx(&cfg, kernel, q));
 }
 
-template <class T, int G, bool MINS> int launch_group(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
+template <int G> int launch_few_group(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
 {
-    if (f.nt == 1)
-        return f.prepare ? launch_few<T, G, MINS, 1, true>(q, f, dev, s) : launch_few<T, G, MINS, 1, false>(q, f, dev, s);
-    return f.nt == 2 ? launch_few<T, G, MINS, 2, true>(q, f, dev, s) : launch_few<T, G, MINS, 4, true>(q, f, dev, s);
+    if (q.m.mins)
+        return f.nt == 1   ? launch_few<G, true, 1>(q, f, dev, s)
+               : f.nt == 2 ? launch_few<G, true, 2>(q, f, dev, s)
+                           : launch_few<G, true, 4>(q, f, dev, s);
+    return f.nt == 1   ? launch_few<G, false, 1>(q, f, dev, s)
+           : f.nt == 2 ? launch_few<G, false, 2>(q, f, dev, s)
+                       : launch_few<G, false, 4>(q, f, dev, s);
 }
 
-template <class T> int launch_type(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
-{
-    const bool mins = q.m.mins != nullptr;
-    if (q.m.group == 32) return mins ? launch_group<T, 32, true>(q, f, dev, s) : launch_group<T, 32, false>(q, f, dev, s);
-    if (q.m.group == 64) return mins ? launch_group<T, 64, true>(q, f, dev, s) : launch_group<T, 64, false>(q, f, dev, s);
-    return mins ? launch_group<T, 128, true>(q, f, dev, s) : launch_group<T, 128, false>(q, f, dev, s);
-}
-
-
-
-// One translation unit per type of x.
-int launch_few_f16(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
-int launch_few_bf16(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
+// One translation unit per group size.
+int launch_few_32(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
+int launch_few_64(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
+int launch_few_128(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
 
 }  // namespace e2ops
