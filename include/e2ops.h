@@ -143,7 +143,7 @@ int e2_cache_read(const e2_cache *c, const int64_t *slots, int32_t tokens, int32
  * max_new and max_len are the largest new and lens: they shape the launch, larger ones on
  * the device only cost time.  Keys of pages outside the cache are not seen, nor
  * those from table_cols * page_size on; a token of q outside every request is not
- * written.
+ * written.  batch * kv_heads is at most 65535.
  * workspace: e2_cache_attend_workspace() bytes (0: may be NULL), 256-byte
  * aligned, contents of no consequence. */
 typedef struct {

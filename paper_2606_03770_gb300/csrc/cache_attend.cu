@@ -1,5 +1,8 @@
 // cache_attend.cu -- e2_cache_attend: attention over the paged 4-bit cache.
-#include "ops_common.cuh"
+#include <atomic>
+#include <type_traits>
+
+#include "ops_x.cuh"
 
 namespace e2ops {
 
@@ -8,7 +11,7 @@ int check_cache(const e2_cache *c, int dev);
 namespace {
 
 struct AttendParams {
-    int pages, page_shift, kv_heads, tokens, q_heads, batch, window, table_cols;
+    int pages, page_shift, kv_heads, tokens, q_heads, batch, window, table_cols, splits;
     int64_t table_stride, q_stride, out_stride;
     const uint8_t *codes[2];
     const __half2 *scales[2];
@@ -16,52 +19,540 @@ struct AttendParams {
     float scale;
     const void *q;
     void *out;
+    float *parts;            // [tokens][q_heads][splits][D + 2]: a split's sums, maximum and sum of weights
 };
 
-// A warp per (token, query head), its lanes over the head's elements.
-template <class T, int D> __global__ void __launch_bounds__(128) head_kernel(const AttendParams p)
-{
-    constexpr int E = D / 32;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32;
-    if (unit >= (int64_t)p.tokens * p.q_heads) return;
-    const int t = (int)(unit / p.q_heads), h = (int)(unit % p.q_heads), kv = h / (p.q_heads / p.kv_heads);
-    int r = 0;
-    while (r < p.batch && !(p.starts[r] <= t && t < p.starts[r + 1])) ++r;
-    if (r == p.batch) return;
-    const int64_t pos = (int64_t)p.lens[r] - p.starts[r + 1] + t;
-    float q[E], o[E] = {}, top = -INFINITY, sum = 0;
-    const T *qp = static_cast<const T *>(p.q) + t * p.q_stride + h * D + lane * E;
-#pragma unroll
-    for (int i = 0; i < E; ++i) q[i] = to_float(qp[i]) * p.scale;
-    int64_t first = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
-    for (int64_t j = first; j <= pos; ++j) {
-        const int64_t at = j >> p.page_shift;
-        if (at >= p.table_cols) break;
-        const int page = p.table[r * p.table_stride + at];
-        if (page < 0 || page >= p.pages) continue;
-        const int64_t vec = ((((int64_t)page * p.kv_heads + kv) << p.page_shift) + (j & ((1 << p.page_shift) - 1)));
-        float x[2][E];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const uint8_t *c = p.codes[n] + vec * (D / 2) + lane * E / 2;
-            const float2 dm = __half22float2(p.scales[n][vec * (D / E2_CACHE_GROUP) + lane * E / E2_CACHE_GROUP]);
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[n][i] = __fmaf_rn((float)(c[i / 2] >> (4 * (i % 2)) & 15), dm.x, dm.y);
-        }
-        float a = 0;
-#pragma unroll
-        for (int i = 0; i < E; ++i) a = __fmaf_rn(q[i], x[0][i], a);
-        for (int k = 16; k; k >>= 1) a += __shfl_xor_sync(~0u, a, k);
-        const float now = fmaxf(top, a), f = expf(top - now), e = expf(a - now);
-        sum = __fmaf_rn(sum, f, e);
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[i] = __fmaf_rn(o[i], f, e * x[1][i]);
-        top = now;
+// One request and KV head: its queries, times the query heads that share the KV head,
+// are rows, row = query * share + head.
+struct Rows {
+    int start, share;
+    int64_t count, first_pos;                // rows; position of the first query
+    __device__ Rows(const AttendParams &p, int request)
+    {
+        start = p.starts[request];
+        share = p.q_heads / p.kv_heads;
+        const int64_t queries = (int64_t)p.starts[request + 1] - start;
+        count = queries > 0 ? queries * share : 0;
+        first_pos = p.lens[request] - (queries > 0 ? queries : 0);
     }
-    T *op = static_cast<T *>(p.out) + t * p.out_stride + h * D + lane * E;
+    __device__ int64_t pos(int64_t row) const { return first_pos + row / share; }
+    __device__ int64_t token(int64_t row) const { return start + row / share; }
+    __device__ int head(int kv, int64_t row) const { return kv * share + (int)(row % share); }
+    __device__ bool live(const AttendParams &p, int64_t row) const
+    {
+        return row < count && token(row) >= 0 && token(row) < p.tokens;
+    }
+};
+
+// ---- a few rows ------------------------------------------------------------------
+//
+// Bound by reading the cache.  S^T = K q^T and O^T = V^T P^T on the warp-level
+// tensor cores, keys and then dimensions being the 16-row operand and eight rows the
+// other, so that one query head per KV head wastes no cache read.  A warp streams
+// tiles of 32 keys through a ring of its own (no block barrier) and keeps its own running
+// maximum; warps, and splits of a long context over blocks, are joined at the end in
+// a fixed order.
+//
+// A code in the low four bits of a 16-bit word is the fp16 number code x 2^-24, in the
+// next four code x 2^-20 (subnormal, exact): codes go to the tensor cores after one shift
+// and four ANDs a word.  For the keys the queries carry the other 1/16 and a power of
+// two each; a key's scale and minimum are applied to its sums in 32 bits.  The values'
+// words are loaded transposed, which pairs two keys of one dimension; their scales
+// multiply the weights before these are rounded to fp16, against a running power of two so
+// that neither range ends; fp16 outputs take the rounding's rest in a second product.
+// Minima are summed in 32 bits.
+
+constexpr int kFewWarps = 4, kTile = 32, kFewStages = 3;
+
+template <int D> struct FewStage {
+    static constexpr int kKeyBytes = D / 2 + 16, kCodes = kTile * kKeyBytes, kScales = kTile * (D / E2_CACHE_GROUP) * 4;
+    static constexpr int kBytes = 2 * kCodes + 2 * kScales + 16;
+};
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, NT == 1 ? 3 : 2) few_kernel(const AttendParams p)
+{
+    using St = FewStage<D>;
+    constexpr int U = D / 32, GR = D / E2_CACHE_GROUP, C = 8 * NT;
+    constexpr bool kRest = std::is_same<T, __half>::value;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
+    const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, split = blockIdx.x;
+    const Rows rows(p, request);
+    const int page_mask = (1 << p.page_shift) - 1;
+    const int32_t *table = p.table + request * p.table_stride;
+    uint8_t *ring = smem + warp * kFewStages * St::kBytes;
+    const uint32_t ring_at = smem_addr(ring);
+
+    for (int64_t row0 = (int64_t)blockIdx.z * C; row0 < rows.count; row0 += (int64_t)gridDim.z * C) {
+        // the keys that some row sees, in tiles; this split's
+        const int64_t last = min(row0 + C, rows.count) - 1;
+        const int64_t lo = p.window > 0 ? max(rows.pos(row0) - p.window + 1, (int64_t)0) : 0;
+        const int64_t hi = min(rows.pos(last) + 1, (int64_t)p.table_cols << p.page_shift);
+        const int64_t tile_lo = lo / kTile, tiles = hi > lo ? (hi + kTile - 1) / kTile - tile_lo : 0;
+        const int64_t units = (tiles + kFewWarps - 1) / kFewWarps, per = (units + p.splits - 1) / p.splits * kFewWarps;
+        const int64_t first = tile_lo + split * per, end = min(first + per, tile_lo + tiles);
+
+        // queries: this lane's column g of each eight, octets t of each 32 elements
+        uint4 qf[NT][U];
+        float q_sum[NT][GR][2], q_scale[NT][2];          // of columns 2t, 2t + 1
+        int64_t seen_hi[NT][2], seen_lo[NT][2];
 #pragma unroll
-    for (int i = 0; i < E; ++i) op[i] = from_float<T>(sum > 0 ? o[i] / sum : sum);
+        for (int n = 0; n < NT; ++n) {
+            const int64_t row = row0 + 8 * n + g;
+            const bool live = rows.live(p, row);
+            const T *src = static_cast<const T *>(p.q) + (live ? rows.token(row) * p.q_stride + rows.head(kv, row) * D : 0);
+            unsigned top = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                qf[n][u] = live ? *reinterpret_cast<const uint4 *>(src + 32 * u + 8 * t) : uint4{0, 0, 0, 0};
+                top = max(top, octet_largest(qf[n][u]));
+            }
+            top = max(top, __shfl_xor_sync(~0u, top, 1));
+            top = max(top, __shfl_xor_sync(~0u, top, 2));
+            const int k = power_for<T>(top);
+            float sum[GR];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float s;
+                qf[n][u] = octet_convert<T>(qf[n][u], power_of_two(k), s);
+                sum[u / 2] = u % 2 ? sum[u / 2] + s : s;
+            }
+#pragma unroll
+            for (int j = 0; j < GR; ++j) {
+                sum[j] += __shfl_xor_sync(~0u, sum[j], 1);
+                sum[j] += __shfl_xor_sync(~0u, sum[j], 2);
+            }
+            // scores to base 2; a code 1 counts 2^-24
+            const float f = p.scale * 1.4426950408889634f * power_of_two(-k);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                q_scale[n][e] = __shfl_sync(~0u, f, (2 * t + e) * 4);
+#pragma unroll
+                for (int j = 0; j < GR; ++j) q_sum[n][j][e] = __shfl_sync(~0u, sum[j], (2 * t + e) * 4);
+                const int64_t at = row0 + 8 * n + 2 * t + e;
+                const bool seen = rows.live(p, at);
+                seen_hi[n][e] = seen ? rows.pos(at) : -1;
+                seen_lo[n][e] = seen && p.window > 0 ? rows.pos(at) - p.window + 1 : 0;
+            }
+        }
+        // tiles in this range need no mask for any column
+        const int64_t full_lo = p.window > 0 ? rows.pos(last) - p.window + 1 : 0, full_hi = rows.pos(row0);
+        const bool all_live = row0 + C <= rows.count && rows.live(p, row0) && rows.live(p, last);
+
+        int64_t ahead = first + warp;                    // the next tile to fetch
+        int pages[2];
+        auto look_up = [&](int64_t tile) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t j = tile * kTile + 16 * h;
+                pages[h] = tile < end && j < hi ? table[j >> p.page_shift] : -1;
+            }
+        };
+        auto issue = [&](int slot) {
+            if (ahead < end) {
+                const uint32_t dst = ring_at + slot * St::kBytes;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool there = pages[h] >= 0 && pages[h] < p.pages;
+                    const int64_t vec = ((((int64_t)(there ? pages[h] : 0) * p.kv_heads + kv) << p.page_shift) +
+                                         ((ahead * kTile + 16 * h) & page_mask));
+                    constexpr int kParts = D / 32;       // 16-byte parts of a key
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+                        for (int i = 0; i < kParts / 2; ++i) {
+                            const int e = i * 32 + lane, key = e / kParts, part = e % kParts;
+                            copy_async16(dst + w * St::kCodes + (16 * h + key) * St::kKeyBytes + part * 16,
+                                         p.codes[w] + (vec + key) * (D / 2) + part * 16, there);
+                        }
+                    }
+                    // 16 keys' scales: 4 GR pieces, keys' and values'
+                    if (lane < 8 * GR) {
+                        const int w = lane / (4 * GR), e = lane % (4 * GR);
+                        copy_async16(dst + 2 * St::kCodes + w * St::kScales + h * 64 * GR + e * 16,
+                                     reinterpret_cast<const uint8_t *>(p.scales[w] + vec * GR) + e * 16, there);
+                    }
+                    if (lane == 0)
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * St::kCodes + 2 * St::kScales + 4 * h),
+                                     "r"((uint32_t)there)
+                                     : "memory");
+                }
+            }
+            copy_commit();
+            ahead += kFewWarps;
+            look_up(ahead);
+        };
+
+        float o[U][2][NT][4] = {};                       // sums for dimensions 32 u + 4 g + {0, 1}, {2, 3}
+        float low[NT][GR][2] = {}, sum[NT][2] = {};      // minima's sums, weights' sums: this lane's keys
+        float top[NT][2];                                // maxima, a little stale at times
+        float v_power = 0x1p40f;                         // 1 / a power of two: no scale so far is twice as large
+#pragma unroll
+        for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
+        look_up(ahead);
+        bool started = false;
+#pragma unroll
+        for (int i = 0; i < kFewStages - 1; ++i) issue(i);
+        int slot = 0;
+        for (int64_t tile = first + warp; tile < end; tile += kFewWarps) {
+            copy_wait<kFewStages - 2>();
+            __syncwarp();
+            issue(slot == 0 ? kFewStages - 1 : slot - 1);
+            const uint8_t *st = ring + slot * St::kBytes;
+            const uint32_t st_at = ring_at + slot * St::kBytes;
+            slot = slot == kFewStages - 1 ? 0 : slot + 1;
+            const uint2 there = *reinterpret_cast<const uint2 *>(st + 2 * St::kCodes + 2 * St::kScales);
+
+            // scores: keys 16 m + g + 8 r, columns 8 n + 2 t + e
+            float s[2][2][NT][2];
+            const uint32_t lo4 = 0x000f000fu, hi4 = 0x00f000f0u;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                float acc[GR][NT][4];
+                const uint32_t mat = st_at + (16 * m + lane % 16) * St::kKeyBytes + lane / 16 * 16;
+#pragma unroll
+                for (int u = 0; u < U; u += 2) {
+                    uint32_t w[4];
+                    load_matrices(w, mat + u * 16);
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint32_t a = w[2 * v], d = w[2 * v + 1], a8 = a >> 8, d8 = d >> 8;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint4 &x = qf[n][u + v];
+                            const float zero[4] = {0, 0, 0, 0};
+                            if (v == 0) multiply(acc[u / 2][n], a & lo4, d & lo4, a & hi4, d & hi4, x.x, x.y, zero);
+                            else multiply(acc[u / 2][n], a & lo4, d & lo4, a & hi4, d & hi4, x.x, x.y, acc[u / 2][n]);
+                            multiply(acc[u / 2][n], a8 & lo4, d8 & lo4, a8 & hi4, d8 & hi4, x.z, x.w, acc[u / 2][n]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float2 dm[GR];
+                    const __half2 *sc = reinterpret_cast<const __half2 *>(st + 2 * St::kCodes) + (16 * m + g + 8 * r) * GR;
+#pragma unroll
+                    for (int j = 0; j < GR; ++j) {
+                        dm[j] = __half22float2(sc[j]);
+                        dm[j].x *= 0x1p24f;
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float x = 0;
+#pragma unroll
+                            for (int j = 0; j < GR; ++j)
+                                x = __fmaf_rn(dm[j].x, acc[j][n][2 * r + e], __fmaf_rn(dm[j].y, q_sum[n][j][e], x));
+                            s[m][r][n][e] = x * q_scale[n][e];
+                        }
+                }
+            }
+            // masks, where the tile is not seen whole by every column
+            const int64_t key0 = tile * kTile;
+            const bool whole = all_live && key0 >= full_lo && key0 + kTile - 1 <= full_hi && there.x && there.y;
+            unsigned hidden[NT][2] = {};                  // bit 2 m + r
+            if (!whole) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int64_t key = key0 + 16 * m + g + 8 * r;
+                        const bool in = (m ? there.y : there.x) != 0 && key < hi;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (!in || key > seen_hi[n][e] || key < seen_lo[n][e]) {
+                                    s[m][r][n][e] = -INFINITY;
+                                    hidden[n][e] |= 1u << (2 * m + r);
+                                }
+                    }
+            }
+            unsigned every = ~0u;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) every &= hidden[n][0] & hidden[n][1];
+            // values' scales of this lane's keys
+            float2 vs[2][2][GR];
+            float most = 0;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int j = 0; j < GR; ++j) {
+                        vs[m][r][j] = __half22float2(reinterpret_cast<const __half2 *>(
+                            st + 2 * St::kCodes + St::kScales)[(16 * m + g + 8 * r) * GR + j]);
+                        // (not of keys hidden from all of this lane's columns; an infinite one counts as fp16's largest)
+                        if (whole || !(every >> (2 * m + r) & 1)) most = fmaxf(most, fminf(fabsf(vs[m][r][j].x), 65504.0f));
+                    }
+            // a new maximum, or scale, only where the old one is exceeded by a factor
+            // of four (or two): then all sums so far are brought to the new one
+            bool renew = !started || most * v_power >= 2.0f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    renew |= fmaxf(fmaxf(s[0][0][n][e], s[0][1][n][e]), fmaxf(s[1][0][n][e], s[1][1][n][e])) > top[n][e] + 2.0f;
+            if (__any_sync(~0u, renew)) {
+                started = true;
+#pragma unroll
+                for (int k = 16; k; k >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, k));
+                const float power = most > 0 ? power_of_two(127 - (int)(__float_as_uint(most) >> 23)) : v_power;
+                const float now = fminf(v_power, power), back = now / v_power;
+                v_power = now;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float x = fmaxf(fmaxf(s[0][0][n][e], s[0][1][n][e]), fmaxf(s[1][0][n][e], s[1][1][n][e]));
+#pragma unroll
+                        for (int k = 4; k < 32; k *= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, k));
+                        const float was = top[n][e], is = fmaxf(was, x);
+                        const float f = was == is || was == -INFINITY ? (was == is ? 1.0f : 0.0f) : power2(was - is);
+                        top[n][e] = is;
+                        sum[n][e] *= f;
+#pragma unroll
+                        for (int j = 0; j < GR; ++j) low[n][j][e] *= f;
+                        const float fo = f * back;
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) {
+                                o[u][v][n][e] *= fo;
+                                o[u][v][n][2 + e] *= fo;
+                            }
+                    }
+            }
+            // weights, times 2^11; and with the values' scales, in fp16, keys in pairs
+            uint32_t pb[GR][2][NT][2], pr[kRest ? GR : 1][2][NT][2];
+            auto weigh = [&](auto masked) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            float w[2];
+                            bool out[2] = {false, false};
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                w[e] = power2(s[m][r][n][e] - (top[n][e] == -INFINITY ? 0.0f : top[n][e]));
+                                sum[n][e] += w[e];
+                                if (masked.value) out[e] = hidden[n][e] >> (2 * m + r) & 1;
+                            }
+#pragma unroll
+                            for (int j = 0; j < GR; ++j) {
+                                const float2 &v = vs[m][r][j];
+                                const float f = v.x * v_power * 2048.0f;
+                                float x[2];
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    // (a hidden key's scale may be anything)
+                                    low[n][j][e] = __fmaf_rn(w[e], out[e] ? 0.0f : v.y, low[n][j][e]);
+                                    x[e] = w[e] * (out[e] ? 0.0f : f);
+                                }
+                                const uint32_t h = pack_half(x[0], x[1]);
+                                pb[j][m][n][r] = transpose8x8(h);
+                                if constexpr (kRest) {
+                                    const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                                    pr[j][m][n][r] = transpose8x8(pack_half(x[0] - back.x, x[1] - back.y));
+                                }
+                            }
+                        }
+            };
+            if (whole) weigh(std::false_type{});
+            else weigh(std::true_type{});
+            // values: matrices of a load are keys 0-7, 8-15, 16-23, 24-31 of 32 dimensions
+            const uint32_t mat = st_at + St::kCodes + lane * St::kKeyBytes;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                uint32_t w[4];
+                load_matrices_t(w, mat + u * 16);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const uint32_t a = w[2 * m], d = w[2 * m + 1], a8 = a >> 8, d8 = d >> 8;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t b0 = pb[u / 2][m][n][0], b1 = pb[u / 2][m][n][1];
+                        multiply(o[u][0][n], a & lo4, a & hi4, d & lo4, d & hi4, b0, b1, o[u][0][n]);
+                        multiply(o[u][1][n], a8 & lo4, a8 & hi4, d8 & lo4, d8 & hi4, b0, b1, o[u][1][n]);
+                        if constexpr (kRest) {
+                            const uint32_t c0 = pr[u / 2][m][n][0], c1 = pr[u / 2][m][n][1];
+                            multiply(o[u][0][n], a & lo4, a & hi4, d & lo4, d & hi4, c0, c1, o[u][0][n]);
+                            multiply(o[u][1][n], a8 & lo4, a8 & hi4, d8 & lo4, d8 & hi4, c0, c1, o[u][1][n]);
+                        }
+                    }
+                }
+            }
+        }
+        copy_wait<0>();
+        asm volatile("griddepcontrol.launch_dependents;");
+
+        // this warp's sums, whole: [C] maxima, [C] weights, [C][D + 1] sums (rows apart in banks)
+        __syncthreads();
+        float *mine = reinterpret_cast<float *>(smem) + warp * (C * (D + 3));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c = 8 * n + 2 * t + e;
+#pragma unroll
+                for (int k = 4; k < 32; k *= 2) {
+                    sum[n][e] += __shfl_xor_sync(~0u, sum[n][e], k);
+#pragma unroll
+                    for (int j = 0; j < GR; ++j) low[n][j][e] += __shfl_xor_sync(~0u, low[n][j][e], k);
+                }
+                if (g == 0) mine[c] = top[n][e], mine[C + c] = sum[n][e];
+                // codes count 2^-24 (2^-20 the second and fourth), weights 2^11
+                const float f = 0x1p13f / v_power;
+                float *to = mine + 2 * C + c * (D + 1) + 4 * g;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float z = low[n][u / 2][e];
+                    to[32 * u] = __fmaf_rn(o[u][0][n][e], f, z);
+                    to[32 * u + 1] = __fmaf_rn(o[u][0][n][2 + e], f * 0.0625f, z);
+                    to[32 * u + 2] = __fmaf_rn(o[u][1][n][e], f, z);
+                    to[32 * u + 3] = __fmaf_rn(o[u][1][n][2 + e], f * 0.0625f, z);
+                }
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < C * D; i += 32 * kFewWarps) {
+            const int c = i / D, d = i % D;
+            const int64_t row = row0 + c;
+            if (!rows.live(p, row)) continue;
+            const float *all = reinterpret_cast<const float *>(smem);
+            float best = -INFINITY, total = 0, x = 0;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) best = fmaxf(best, all[w * (C * (D + 3)) + c]);
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const float *from = all + w * (C * (D + 3));
+                const float f = from[c] == -INFINITY ? 0.0f : power2(from[c] - best);
+                if (from[c] == -INFINITY && !(from[C + c] != from[C + c])) continue;
+                total = __fmaf_rn(from[C + c], f, total);
+                x = __fmaf_rn(from[2 * C + c * (D + 1) + d], f, x);
+            }
+            const int head = rows.head(kv, row);
+            if (p.splits == 1) {
+                static_cast<T *>(p.out)[rows.token(row) * p.out_stride + head * D + d] =
+                    from_float<T>(total > 0 ? x / total : total);
+            } else {
+                float *to = p.parts + ((rows.token(row) * p.q_heads + head) * p.splits + split) * (D + 2);
+                to[d] = x;
+                if (d == 0) to[D] = best, to[D + 1] = total;
+            }
+        }
+        __syncthreads();                                 // (the next rows' tiles overwrite the sums)
+    }
+}
+
+// A split context's parts, joined in order: a warp per row.
+template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(const AttendParams p)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, lane = threadIdx.x % 32;
+    const Rows rows(p, request);
+    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 32; row < rows.count; row += (int64_t)gridDim.x * 4) {
+        if (!rows.live(p, row)) continue;
+        const int head = rows.head(kv, row);
+        const float *from = p.parts + (rows.token(row) * p.q_heads + head) * p.splits * (D + 2);
+        float best = -INFINITY, total = 0, x[D / 32] = {};
+        for (int k = lane; k < p.splits; k += 32) best = fmaxf(best, from[k * (D + 2) + D]);
+#pragma unroll
+        for (int k = 16; k; k >>= 1) best = fmaxf(best, __shfl_xor_sync(~0u, best, k));
+        for (int k = 0; k < p.splits; ++k) {
+            const float *at = from + k * (D + 2);
+            const float top = at[D], weights = at[D + 1];
+            if (top == -INFINITY && weights == 0) continue;            // nothing seen
+            const float f = top == -INFINITY ? 1.0f : power2(top - best);
+            total = __fmaf_rn(weights, f, total);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) x[i] = __fmaf_rn(at[32 * i + lane], f, x[i]);
+        }
+        T *out = static_cast<T *>(p.out) + rows.token(row) * p.out_stride + head * D;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) out[32 * i + lane] = from_float<T>(total > 0 ? x[i] / total : total);
+    }
+}
+
+struct Plan {
+    int nt, slabs, splits;
+};
+
+// Rows by eight or sixteen; keys split until every multiprocessor has its three (two)
+// blocks, no finer than 128 keys.
+Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
+{
+    Plan f;
+    const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
+    f.nt = rows <= 8 ? 1 : 2;
+    const int64_t slabs = (rows + 8 * f.nt - 1) / (8 * f.nt);
+    f.slabs = (int)(slabs < 65535 ? slabs : 65535);
+    int64_t keys = a->max_len;
+    if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
+    const int64_t units = (keys + kTile * kFewWarps - 1) / (kTile * kFewWarps);
+    int64_t splits = (int64_t)sms * (f.nt == 1 ? 3 : 2) / ((int64_t)a->batch * c->kv_heads * slabs);
+    if (splits > units) splits = units;
+    f.splits = (int)(splits < 1 ? 1 : splits > 128 ? 128 : splits);
+    return f;
+}
+
+size_t workspace_for(const e2_cache *c, const e2_attend_args *a, const Plan &f)
+{
+    return f.splits > 1 ? (size_t)a->tokens * a->q_heads * f.splits * (c->head_dim + 2) * sizeof(float) : 0;
+}
+
+template <class K> int launch(K kernel, const AttendParams &p, dim3 grid, size_t smem, bool early, int dev,
+                              std::atomic<uint64_t> &ready, cudaStream_t s)
+{
+    if (smem > 48 * 1024 && !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return cuda_status(e);
+        ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = &at;
+    cfg.numAttrs = early ? 1 : 0;
+    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
+}
+
+template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
+{
+    static std::atomic<uint64_t> ready[2];               // devices that have the attribute set
+    const size_t smem = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes;
+    const unsigned pairs = (unsigned)p.batch * p.kv_heads;
+    const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
+    const int st = f.nt == 1 ? launch(few_kernel<T, D, 1>, p, grid, smem, false, dev, ready[0], s)
+                             : launch(few_kernel<T, D, 2>, p, grid, smem, false, dev, ready[1], s);
+    if (st != E2_OK || f.splits == 1) return st;
+    const int64_t blocks = ((int64_t)f.slabs * 8 * f.nt + 3) / 4;
+    return launch(join_kernel<T, D>, p, dim3((unsigned)blocks, pairs), 0, true, dev, ready[0], s);
 }
 
 int check_args(const e2_cache *c, const e2_attend_args *a)
@@ -82,7 +573,12 @@ int check_args(const e2_cache *c, const e2_attend_args *a)
 
 using namespace e2ops;
 
-extern "C" size_t e2_cache_attend_workspace(const e2_cache *, const e2_attend_args *) { return 0; }
+extern "C" size_t e2_cache_attend_workspace(const e2_cache *c, const e2_attend_args *a)
+{
+    Device dev;
+    if (!c || c->kv_heads < 1 || check_args(c, a) || a->tokens == 0 || a->batch == 0 || current_device(&dev)) return 0;
+    return workspace_for(c, a, plan(c, a, dev.sms));
+}
 
 extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace, size_t workspace_bytes,
                                void *stream)
@@ -100,17 +596,19 @@ extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void 
     const void *ptrs[] = {a->q, a->out, a->table, a->lens, a->starts};
     for (const void *p : ptrs)
         if (!on_device(p, dev.id)) return fail(E2_EINVAL, "arrays must be memory of the current device");
-    const size_t need = e2_cache_attend_workspace(c, a);
+    if ((int64_t)a->batch * c->kv_heads > 65535) return fail(E2_EINVAL, "batch * kv_heads must not exceed 65535");
+    const Plan f = plan(c, a, dev.sms);
+    const size_t need = workspace_for(c, a, f);
     if (need && (!workspace || workspace_bytes < need)) return fail(E2_ENOMEM, "workspace too small");
-    AttendParams p{c->pages, __builtin_ctz((unsigned)c->page_size), c->kv_heads, a->tokens, a->q_heads, a->batch, a->window, a->table_cols,
-                   a->table_stride, a->q_stride, a->out_stride, {c->k_codes, c->v_codes},
+    if (need && (!aligned(workspace, 256) || !on_device(workspace, dev.id)))
+        return fail(E2_EINVAL, "workspace must be 256-byte aligned memory of the current device");
+    AttendParams p{c->pages, __builtin_ctz((unsigned)c->page_size), c->kv_heads, a->tokens, a->q_heads, a->batch, a->window,
+                   a->table_cols, f.splits, a->table_stride, a->q_stride, a->out_stride, {c->k_codes, c->v_codes},
                    {reinterpret_cast<const __half2 *>(c->k_scales), reinterpret_cast<const __half2 *>(c->v_scales)},
-                   a->table, a->lens, a->starts, a->scale, a->q, a->out};
-    const int64_t blocks = ((int64_t)a->tokens * a->q_heads + 3) / 4;
-    if (blocks > 0x7fffffff) return fail(E2_EINVAL, "too many tokens for one call");
+                   a->table, a->lens, a->starts, a->scale, a->q, a->out, static_cast<float *>(workspace)};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool half = a->dtype == E2_F16;
-    void (*f)(AttendParams) = c->head_dim == 64 ? (half ? head_kernel<__half, 64> : head_kernel<__nv_bfloat16, 64>)
-                                                : (half ? head_kernel<__half, 128> : head_kernel<__nv_bfloat16, 128>);
-    f<<<(unsigned)blocks, 128, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return cuda_status(cudaGetLastError());
+    if (c->head_dim == 64)
+        return half ? launch_attend<__half, 64>(p, f, dev.id, s) : launch_attend<__nv_bfloat16, 64>(p, f, dev.id, s);
+    return half ? launch_attend<__half, 128>(p, f, dev.id, s) : launch_attend<__nv_bfloat16, 128>(p, f, dev.id, s);
 }

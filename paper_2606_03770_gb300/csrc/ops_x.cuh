@@ -1,0 +1,42 @@
+// ops_x.cuh -- 16-bit activations as the operand that meets 4-bit codes: fp16
+// times a power of two, in the order of the codes' nibbles.
+#pragma once
+
+#include "ops_mma.cuh"
+
+namespace e2ops {
+
+// 2^k that brings the largest magnitude (16 bits of T) to 2^14..2^15, k within fp32's normal range.
+template <class T> __device__ __forceinline__ int power_for(unsigned bits)
+{
+    T top;
+    *reinterpret_cast<uint16_t *>(&top) = (uint16_t)bits;
+    return bits ? min(14 + 127 - (int)(__float_as_uint(to_float(top)) >> 23), 126) : 0;
+}
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
+
+// The larger 16-bit magnitude of an octet.
+__device__ __forceinline__ unsigned octet_largest(const uint4 &v)
+{
+    const unsigned m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    return max(m & 0xffffu, m >> 16);
+}
+
+// An octet times f in fp16, in the order of the codes' nibbles, those that meet high
+// nibbles with 1/16; and its sum.
+template <class T> __device__ __forceinline__ uint4 octet_convert(const uint4 &v, float f, float &sum)
+{
+    float x[8];
+    unpack8<T>(v, x);
+    sum = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        x[j] *= f;
+        sum += x[j];
+    }
+    const __half2 h[4] = {__floats2half2_rn(x[0], x[4]), __floats2half2_rn(x[1] * 0.0625f, x[5] * 0.0625f),
+                          __floats2half2_rn(x[2], x[6]), __floats2half2_rn(x[3] * 0.0625f, x[7] * 0.0625f)};
+    return *reinterpret_cast<const uint4 *>(h);
+}
+
+}  // namespace e2ops

@@ -5,7 +5,7 @@
 #include <atomic>
 #include <type_traits>
 
-#include "ops_mma.cuh"
+#include "ops_x.cuh"
 
 namespace e2ops {
 
@@ -106,39 +106,6 @@ __device__ __forceinline__ void finish(const MatmulParams &p, int token, int row
 __host__ __device__ constexpr size_t slab_bytes(int nt, int x_pad, int group)
 {
     return (size_t)8 * nt * x_pad * 2 + (size_t)x_pad / group * 8 * nt * 4 + 256;
-}
-
-// 2^k that brings the largest magnitude (16 bits of T) to 2^14..2^15, k within fp32's normal range.
-template <class T> __device__ __forceinline__ int power_for(unsigned bits)
-{
-    T top;
-    *reinterpret_cast<uint16_t *>(&top) = (uint16_t)bits;
-    return bits ? min(14 + 127 - (int)(__float_as_uint(to_float(top)) >> 23), 126) : 0;
-}
-__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
-
-// The larger 16-bit magnitude of an octet.
-__device__ __forceinline__ unsigned octet_largest(const uint4 &v)
-{
-    const unsigned m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-    return max(m & 0xffffu, m >> 16);
-}
-
-// An octet times f in fp16, in the order of the codes' nibbles, those that meet high
-// nibbles with 1/16; and its sum.
-template <class T> __device__ __forceinline__ uint4 octet_convert(const uint4 &v, float f, float &sum)
-{
-    float x[8];
-    unpack8<T>(v, x);
-    sum = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x[j] *= f;
-        sum += x[j];
-    }
-    const __half2 h[4] = {__floats2half2_rn(x[0], x[4]), __floats2half2_rn(x[1] * 0.0625f, x[5] * 0.0625f),
-                          __floats2half2_rn(x[2], x[6]), __floats2half2_rn(x[3] * 0.0625f, x[7] * 0.0625f)};
-    return *reinterpret_cast<const uint4 *>(h);
 }
 
 // Sums as the product needs them (code 1 is 2^-24): for mins, or -8 of them.
