@@ -62,7 +62,7 @@ struct Rows {
 // that neither range ends; fp16 outputs take the rounding's rest in a second product.
 // Minima are summed in 32 bits.
 
-constexpr int kFewWarps = 4, kTile = 32, kFewStages = 3;
+constexpr int kFewWarps = 4, kTile = 32, kFewStages = 3, kMostSplits = 128;
 
 template <int D> struct FewStage {
     static constexpr int kKeyBytes = D / 2 + 16, kCodes = kTile * kKeyBytes, kScales = kTile * (D / E2_CACHE_GROUP) * 4;
@@ -87,7 +87,7 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, NT == 1 ? 3 : 2) few_kernel(const AttendParams p)
+template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, 3) few_kernel(const AttendParams p)
 {
     using St = FewStage<D>;
     constexpr int U = D / 32, GR = D / E2_CACHE_GROUP, C = 8 * NT;
@@ -104,65 +104,20 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
     for (int64_t row0 = (int64_t)blockIdx.z * C; row0 < rows.count; row0 += (int64_t)gridDim.z * C) {
         // the keys that some row sees, in tiles; this split's
         const int64_t last = min(row0 + C, rows.count) - 1;
-        const int64_t lo = p.window > 0 ? max(rows.pos(row0) - p.window + 1, (int64_t)0) : 0;
-        const int64_t hi = min(rows.pos(last) + 1, (int64_t)p.table_cols << p.page_shift);
-        const int64_t tile_lo = lo / kTile, tiles = hi > lo ? (hi + kTile - 1) / kTile - tile_lo : 0;
-        const int64_t units = (tiles + kFewWarps - 1) / kFewWarps, per = (units + p.splits - 1) / p.splits * kFewWarps;
-        const int64_t first = tile_lo + split * per, end = min(first + per, tile_lo + tiles);
+        // (32 bits: lengths stop 64 short of 2^31)
+        const int lo = p.window > 0 ? (int)max(rows.pos(row0) - p.window + 1, (int64_t)0) : 0;
+        const int hi = (int)min(min(rows.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
+        const int tile_lo = lo / kTile, tiles = hi > lo ? (hi + kTile - 1) / kTile - tile_lo : 0;
+        const int units = (tiles + kFewWarps - 1) / kFewWarps, per = (units + p.splits - 1) / p.splits * kFewWarps;
+        const int first = (int)min((int64_t)tile_lo + (int64_t)split * per, (int64_t)tile_lo + tiles);
+        const int end = min(first + per, tile_lo + tiles);
 
-        // queries: this lane's column g of each eight, octets t of each 32 elements
-        uint4 qf[NT][U];
-        float q_sum[NT][GR][2], q_scale[NT][2];          // of columns 2t, 2t + 1
-        int64_t seen_hi[NT][2], seen_lo[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int64_t row = row0 + 8 * n + g;
-            const bool live = rows.live(p, row);
-            const T *src = static_cast<const T *>(p.q) + (live ? rows.token(row) * p.q_stride + rows.head(kv, row) * D : 0);
-            unsigned top = 0;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                qf[n][u] = live ? *reinterpret_cast<const uint4 *>(src + 32 * u + 8 * t) : uint4{0, 0, 0, 0};
-                top = max(top, octet_largest(qf[n][u]));
-            }
-            top = max(top, __shfl_xor_sync(~0u, top, 1));
-            top = max(top, __shfl_xor_sync(~0u, top, 2));
-            const int k = power_for<T>(top);
-            float sum[GR];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float s;
-                qf[n][u] = octet_convert<T>(qf[n][u], power_of_two(k), s);
-                sum[u / 2] = u % 2 ? sum[u / 2] + s : s;
-            }
-#pragma unroll
-            for (int j = 0; j < GR; ++j) {
-                sum[j] += __shfl_xor_sync(~0u, sum[j], 1);
-                sum[j] += __shfl_xor_sync(~0u, sum[j], 2);
-            }
-            // scores to base 2; a code 1 counts 2^-24
-            const float f = p.scale * 1.4426950408889634f * power_of_two(-k);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                q_scale[n][e] = __shfl_sync(~0u, f, (2 * t + e) * 4);
-#pragma unroll
-                for (int j = 0; j < GR; ++j) q_sum[n][j][e] = __shfl_sync(~0u, sum[j], (2 * t + e) * 4);
-                const int64_t at = row0 + 8 * n + 2 * t + e;
-                const bool seen = rows.live(p, at);
-                seen_hi[n][e] = seen ? rows.pos(at) : -1;
-                seen_lo[n][e] = seen && p.window > 0 ? rows.pos(at) - p.window + 1 : 0;
-            }
-        }
-        // tiles in this range need no mask for any column
-        const int64_t full_lo = p.window > 0 ? rows.pos(last) - p.window + 1 : 0, full_hi = rows.pos(row0);
-        const bool all_live = row0 + C <= rows.count && rows.live(p, row0) && rows.live(p, last);
-
-        int64_t ahead = first + warp;                    // the next tile to fetch
+        int ahead = first + warp;                    // the next tile to fetch
         int pages[2];
-        auto look_up = [&](int64_t tile) {
+        auto look_up = [&](int tile) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t j = tile * kTile + 16 * h;
+                const int j = tile * kTile + 16 * h;
                 pages[h] = tile < end && j < hi ? table[j >> p.page_shift] : -1;
             }
         };
@@ -200,19 +155,71 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             ahead += kFewWarps;
             look_up(ahead);
         };
+        look_up(ahead);
+#pragma unroll
+        for (int i = 0; i < kFewStages - 1; ++i) issue(i);
+
+        // queries: this lane's column g of each eight, octets t of each 32 elements
+        uint4 *q_shared = reinterpret_cast<uint4 *>(smem + kFewWarps * kFewStages * St::kBytes);   // [NT][U][32]
+        __syncthreads();
+        float q_sum[NT][GR][2], q_scale[NT][2];          // of columns 2t, 2t + 1
+        int seen_hi[NT][2], seen_lo[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int64_t row = row0 + 8 * n + g;
+            const bool live = rows.live(p, row);
+            const T *src = static_cast<const T *>(p.q) + (live ? rows.token(row) * p.q_stride + rows.head(kv, row) * D : 0);
+            unsigned top = 0;
+            uint4 qf[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                qf[u] = live ? *reinterpret_cast<const uint4 *>(src + 32 * u + 8 * t) : uint4{0, 0, 0, 0};
+                top = max(top, octet_largest(qf[u]));
+            }
+            top = max(top, __shfl_xor_sync(~0u, top, 1));
+            top = max(top, __shfl_xor_sync(~0u, top, 2));
+            const int k = power_for<T>(top);
+            float sum[GR];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float s;
+                qf[u] = octet_convert<T>(qf[u], p.scale < 0 ? -power_of_two(k) : power_of_two(k), s);
+                if (warp == 0) q_shared[(n * U + u) * 32 + lane] = qf[u];
+                sum[u / 2] = u % 2 ? sum[u / 2] + s : s;
+            }
+#pragma unroll
+            for (int j = 0; j < GR; ++j) {
+                sum[j] += __shfl_xor_sync(~0u, sum[j], 1);
+                sum[j] += __shfl_xor_sync(~0u, sum[j], 2);
+            }
+            // scores to base 2; a code 1 counts 2^-24
+            const float f = fabsf(p.scale) * 1.4426950408889634f * power_of_two(-k);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                q_scale[n][e] = __shfl_sync(~0u, f, (2 * t + e) * 4);
+#pragma unroll
+                for (int j = 0; j < GR; ++j) q_sum[n][j][e] = __shfl_sync(~0u, sum[j], (2 * t + e) * 4);
+                const int64_t at = row0 + 8 * n + 2 * t + e;
+                const bool seen = rows.live(p, at);
+                seen_hi[n][e] = seen ? (int)rows.pos(at) : -1;
+                seen_lo[n][e] = seen && p.window > 0 ? (int)max(rows.pos(at) - p.window + 1, (int64_t)0) : 0;
+            }
+        }
+        __syncthreads();
+        // tiles in this range need no mask for any column
+        const int full_lo = p.window > 0 ? (int)max(rows.pos(last) - p.window + 1, (int64_t)0) : 0;
+        const int full_hi = (int)max(rows.pos(row0), (int64_t)-1);
+        const bool all_live = row0 + C <= rows.count && rows.live(p, row0) && rows.live(p, last);
 
         float o[U][2][NT][4] = {};                       // sums for dimensions 32 u + 4 g + {0, 1}, {2, 3}
         float low[NT][GR][2] = {}, sum[NT][2] = {};      // minima's sums, weights' sums: this lane's keys
-        float top[NT][2];                                // maxima, a little stale at times
+        float top[NT][2], limit[NT][2];                  // maxima, a little stale at times: scores up to limit do not renew them
         float v_power = 0x1p40f;                         // 1 / a power of two: no scale so far is twice as large
 #pragma unroll
         for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
-        look_up(ahead);
         bool started = false;
-#pragma unroll
-        for (int i = 0; i < kFewStages - 1; ++i) issue(i);
         int slot = 0;
-        for (int64_t tile = first + warp; tile < end; tile += kFewWarps) {
+        for (int tile = first + warp; tile < end; tile += kFewWarps) {
             copy_wait<kFewStages - 2>();
             __syncwarp();
             issue(slot == 0 ? kFewStages - 1 : slot - 1);
@@ -221,7 +228,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             slot = slot == kFewStages - 1 ? 0 : slot + 1;
             const uint2 there = *reinterpret_cast<const uint2 *>(st + 2 * St::kCodes + 2 * St::kScales);
 
-            // scores: keys 16 m + g + 8 r, columns 8 n + 2 t + e
+            // scores, but for q_scale: keys 16 m + g + 8 r, columns 8 n + 2 t + e
             float s[2][2][NT][2];
             const uint32_t lo4 = 0x000f000fu, hi4 = 0x00f000f0u;
 #pragma unroll
@@ -237,7 +244,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                         const uint32_t a = w[2 * v], d = w[2 * v + 1], a8 = a >> 8, d8 = d >> 8;
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint4 &x = qf[n][u + v];
+                            const uint4 x = q_shared[(n * U + u + v) * 32 + lane];
                             const float zero[4] = {0, 0, 0, 0};
                             if (v == 0) multiply(acc[u / 2][n], a & lo4, d & lo4, a & hi4, d & hi4, x.x, x.y, zero);
                             else multiply(acc[u / 2][n], a & lo4, d & lo4, a & hi4, d & hi4, x.x, x.y, acc[u / 2][n]);
@@ -262,12 +269,12 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
 #pragma unroll
                             for (int j = 0; j < GR; ++j)
                                 x = __fmaf_rn(dm[j].x, acc[j][n][2 * r + e], __fmaf_rn(dm[j].y, q_sum[n][j][e], x));
-                            s[m][r][n][e] = x * q_scale[n][e];
+                            s[m][r][n][e] = x;
                         }
                 }
             }
             // masks, where the tile is not seen whole by every column
-            const int64_t key0 = tile * kTile;
+            const int key0 = tile * kTile;
             const bool whole = all_live && key0 >= full_lo && key0 + kTile - 1 <= full_hi && there.x && there.y;
             unsigned hidden[NT][2] = {};                  // bit 2 m + r
             if (!whole) {
@@ -275,7 +282,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const int64_t key = key0 + 16 * m + g + 8 * r;
+                        const int key = key0 + 16 * m + g + 8 * r;
                         const bool in = (m ? there.y : there.x) != 0 && key < hi;
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
@@ -311,7 +318,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    renew |= fmaxf(fmaxf(s[0][0][n][e], s[0][1][n][e]), fmaxf(s[1][0][n][e], s[1][1][n][e])) > top[n][e] + 2.0f;
+                    renew |= fmaxf(fmaxf(s[0][0][n][e], s[0][1][n][e]), fmaxf(s[1][0][n][e], s[1][1][n][e])) > limit[n][e];
             if (__any_sync(~0u, renew)) {
                 started = true;
 #pragma unroll
@@ -326,9 +333,12 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                         float x = fmaxf(fmaxf(s[0][0][n][e], s[0][1][n][e]), fmaxf(s[1][0][n][e], s[1][1][n][e]));
 #pragma unroll
                         for (int k = 4; k < 32; k *= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, k));
+                        // (hidden is -inf whatever the scale, 0 too)
+                        x = x == -INFINITY ? x : x * q_scale[n][e];
                         const float was = top[n][e], is = fmaxf(was, x);
                         const float f = was == is || was == -INFINITY ? (was == is ? 1.0f : 0.0f) : power2(was - is);
                         top[n][e] = is;
+                        limit[n][e] = q_scale[n][e] > 0 ? (is + 2.0f) / q_scale[n][e] : INFINITY;
                         sum[n][e] *= f;
 #pragma unroll
                         for (int j = 0; j < GR; ++j) low[n][j][e] *= f;
@@ -344,6 +354,11 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             }
             // weights, times 2^11; and with the values' scales, in fp16, keys in pairs
             uint32_t pb[GR][2][NT][2], pr[kRest ? GR : 1][2][NT][2];
+            float base[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) base[n][e] = top[n][e] == -INFINITY ? 0.0f : top[n][e];
             auto weigh = [&](auto masked) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
@@ -355,7 +370,9 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                             bool out[2] = {false, false};
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                w[e] = power2(s[m][r][n][e] - (top[n][e] == -INFINITY ? 0.0f : top[n][e]));
+                                w[e] = masked.value && (hidden[n][e] >> (2 * m + r) & 1)
+                                           ? 0.0f
+                                           : power2(__fmaf_rn(s[m][r][n][e], q_scale[n][e], -base[n][e]));
                                 sum[n][e] += w[e];
                                 if (masked.value) out[e] = hidden[n][e] >> (2 * m + r) & 1;
                             }
@@ -465,32 +482,55 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
     }
 }
 
-// A split context's parts, joined in order: a warp per row.
+// A split context's parts, joined in a fixed order: a block per row, its warps over
+// the parts.
 template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(const AttendParams p)
 {
+    __shared__ float factor[kMostSplits], partial[3][D];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, lane = threadIdx.x % 32;
+    const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const Rows rows(p, request);
-    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 32; row < rows.count; row += (int64_t)gridDim.x * 4) {
+    for (int64_t row = blockIdx.x; row < rows.count; row += gridDim.x) {
         if (!rows.live(p, row)) continue;
         const int head = rows.head(kv, row);
         const float *from = p.parts + (rows.token(row) * p.q_heads + head) * p.splits * (D + 2);
-        float best = -INFINITY, total = 0, x[D / 32] = {};
+        // every warp: the maximum, the parts' factors, the weights' sum
+        float best = -INFINITY, total = 0;
         for (int k = lane; k < p.splits; k += 32) best = fmaxf(best, from[k * (D + 2) + D]);
 #pragma unroll
         for (int k = 16; k; k >>= 1) best = fmaxf(best, __shfl_xor_sync(~0u, best, k));
-        for (int k = 0; k < p.splits; ++k) {
-            const float *at = from + k * (D + 2);
-            const float top = at[D], weights = at[D + 1];
-            if (top == -INFINITY && weights == 0) continue;            // nothing seen
-            const float f = top == -INFINITY ? 1.0f : power2(top - best);
+        for (int k = lane; k < p.splits; k += 32) {
+            const float top = from[k * (D + 2) + D], weights = from[k * (D + 2) + D + 1];
+            // (a part without a maximum saw nothing, or NaN)
+            const float f = top == -INFINITY ? (weights == 0 ? 0.0f : weights) : power2(top - best);
+            if (warp == 0) factor[k] = f;
             total = __fmaf_rn(weights, f, total);
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) x[i] = __fmaf_rn(at[32 * i + lane], f, x[i]);
         }
-        T *out = static_cast<T *>(p.out) + rows.token(row) * p.out_stride + head * D;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) out[32 * i + lane] = from_float<T>(total > 0 ? x[i] / total : total);
+        for (int k = 16; k; k >>= 1) total += __shfl_xor_sync(~0u, total, k);
+        __syncthreads();
+        float x[D / 32] = {};
+#pragma unroll 4
+        for (int k = warp; k < p.splits; k += 4) {
+            const float f = factor[k];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) x[i] = __fmaf_rn(from[k * (D + 2) + 32 * i + lane], f, x[i]);
+        }
+        if (warp > 0) {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) partial[warp - 1][32 * i + lane] = x[i];
+        }
+        __syncthreads();
+        if (warp == 0) {
+            T *out = static_cast<T *>(p.out) + rows.token(row) * p.out_stride + head * D;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const int d = 32 * i + lane;
+                const float v = x[i] + partial[0][d] + partial[1][d] + partial[2][d];
+                out[d] = from_float<T>(total > 0 ? v / total : total);
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -498,7 +538,7 @@ struct Plan {
     int nt, slabs, splits;
 };
 
-// Rows by eight or sixteen; keys split until every multiprocessor has its three (two)
+// Rows by eight or sixteen; keys split until every multiprocessor has its three
 // blocks, no finer than 128 keys.
 Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
 {
@@ -510,9 +550,9 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
     int64_t keys = a->max_len;
     if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
     const int64_t units = (keys + kTile * kFewWarps - 1) / (kTile * kFewWarps);
-    int64_t splits = (int64_t)sms * (f.nt == 1 ? 3 : 2) / ((int64_t)a->batch * c->kv_heads * slabs);
+    int64_t splits = (int64_t)sms * 3 / ((int64_t)a->batch * c->kv_heads * slabs);
     if (splits > units) splits = units;
-    f.splits = (int)(splits < 1 ? 1 : splits > 128 ? 128 : splits);
+    f.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     return f;
 }
 
@@ -545,14 +585,13 @@ template <class K> int launch(K kernel, const AttendParams &p, dim3 grid, size_t
 template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
 {
     static std::atomic<uint64_t> ready[2];               // devices that have the attribute set
-    const size_t smem = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes;
+    const size_t ring = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes, smem = ring + (size_t)f.nt * (D / 32) * 512;
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
     const int st = f.nt == 1 ? launch(few_kernel<T, D, 1>, p, grid, smem, false, dev, ready[0], s)
                              : launch(few_kernel<T, D, 2>, p, grid, smem, false, dev, ready[1], s);
     if (st != E2_OK || f.splits == 1) return st;
-    const int64_t blocks = ((int64_t)f.slabs * 8 * f.nt + 3) / 4;
-    return launch(join_kernel<T, D>, p, dim3((unsigned)blocks, pairs), 0, true, dev, ready[0], s);
+    return launch(join_kernel<T, D>, p, dim3((unsigned)f.slabs * 8 * f.nt, pairs), 0, true, dev, ready[0], s);
 }
 
 int check_args(const e2_cache *c, const e2_attend_args *a)
