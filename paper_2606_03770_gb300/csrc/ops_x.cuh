@@ -39,4 +39,36 @@ template <class T> __device__ __forceinline__ uint4 octet_convert(const uint4 &v
     return *reinterpret_cast<const uint4 *>(h);
 }
 
+// The same times f, all alike.
+template <class T> __device__ __forceinline__ uint4 octet_in_order(const uint4 &v, float f)
+{
+    float x[8];
+    unpack8<T>(v, x);
+    const __half2 h[4] = {__floats2half2_rn(x[0] * f, x[4] * f), __floats2half2_rn(x[1] * f, x[5] * f),
+                          __floats2half2_rn(x[2] * f, x[6] * f), __floats2half2_rn(x[3] * f, x[7] * f)};
+    return *reinterpret_cast<const uint4 *>(h);
+}
+
+// A word's eight codes c as m + d c in fp16, rounded once, in the same order.  A code
+// in the low bits of 1024's fp16 makes 1024 + c, in the next four 1024 + 16 c.  The
+// largest value may pass fp16's range by the rounding of d: it stays fp16's largest
+// (NaN stays NaN).
+__device__ __forceinline__ uint4 unpack_word(uint32_t w, __half2 d, __half2 m)
+{
+    const uint32_t v = w >> 8;
+    uint32_t q[4] = {(w & 0x000f000fu) | 0x64006400u, (w & 0x00f000f0u) | 0x64006400u, (v & 0x000f000fu) | 0x64006400u,
+                     (v & 0x00f000f0u) | 0x64006400u};
+    const __half2 off = __float2half2_rn(-1024.0f), sixteenth = __float2half2_rn(0.0625f), high = __float2half2_rn(-64.0f);
+    const __half2 most = __float2half2_rn(65504.0f);
+    uint4 out;
+    __half2 *o = reinterpret_cast<__half2 *>(&out);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 x = *reinterpret_cast<const __half2 *>(&q[i]);
+        const __half2 c = i % 2 ? __hfma2(x, sixteenth, high) : __hadd2(x, off);
+        o[i] = __hmin2_nan(__hfma2(c, d, m), most);
+    }
+    return out;
+}
+
 }  // namespace e2ops
