@@ -1,5 +1,6 @@
 // ops_mma.cuh -- PTX wrappers of the operators' warp-level products: 16 x 8 x 16
-// multiply-accumulate, matrix loads from shared memory, asynchronous copies.
+// multiply-accumulate, matrix loads from shared memory, asynchronous copies,
+// clusters.
 #pragma once
 
 #include "ops_common.cuh"
@@ -42,6 +43,24 @@ __device__ __forceinline__ void multiply(float (&d)[4], uint32_t a0, uint32_t a1
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+
+// Shared memory of the other blocks of a cluster.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int rank)
+{
+    uint32_t d;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
+    return d;
+}
+__device__ __forceinline__ float peer_load(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
 }  // namespace e2ops

@@ -72,23 +72,6 @@ struct FewParams {
 // x's bytes in shared memory per token and segment (rows half a 128-byte line apart in banks).
 __host__ __device__ constexpr int x_row_bytes(int cols) { return cols * 2 + 64; }
 
-__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int rank)
-{
-    uint32_t d;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
-    return d;
-}
-__device__ __forceinline__ float peer_load(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_barrier()
-{
-    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-}
-
 template <class T>
 __device__ __forceinline__ void finish_as(const MatmulParams &p, int token, int row, float a, float b)
 {
