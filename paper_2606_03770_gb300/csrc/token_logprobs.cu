@@ -6,15 +6,18 @@ namespace e2ops {
 namespace {
 
 // One pass over a row, by a block or, where there are few rows, by the blocks of a
-// cluster; bound by reading it.  A thread keeps the maximum m of what it has read, sum
-// e and sum e (x - m), e = exp(x - m), all in 32 bits, and brings them to a new maximum
-// when one comes.  The differences are taken before the exponent's scaling, so that
-// logits of any size keep their digits.
-//
+// cluster; bound by reading it (fp32) or by its seven operations an element (16 bits).
+// A thread keeps the maximum m of what it has read, sum w and sum w t, with w = 2^t, t = x
+// log2 e - c and c = m log2 e rounded once, all in 32 bits, and brings them to a new
+// maximum when one comes.  The product in t is not rounded before c is taken off, and c is the
+// same for all, so logits of any size keep their digits; what c was rounded by comes back at
+// the end.
+
 // Alternatives: a warp keeps the best so far sorted over its lanes, (value, then lower
-// index), and looks at eight elements a lane only when some maximum of eight beats its
-// last one, or what any warp of the block has as its last.  The first elements are let in
-// through the `top`-th largest of the lanes' maxima, which `top` of them reach.
+// index), and looks at eight elements a lane only when some maximum of eight beats a
+// bound: the `top`-th largest of 64 lanes' maxima so far, the largest few of each warp of the
+// block, which `top` elements reach.  Warps publish theirs at rounds 0, 2, 8 and 32, and
+// the first warp draws the bound, from old ones too, which bound as well.
 
 constexpr int kMostThreads = 512, kMostWarps = kMostThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f, kNegligible = -1e30f;
@@ -29,8 +32,12 @@ struct LogprobParams {
 };
 
 struct Sums {
-    float m, s, u;                       // maximum (-inf: nothing), sum e, sum e (x - m)
+    float m, s, u;                       // maximum (-inf: nothing), sum w, sum w t
 };
+
+// Maxima from here on (in magnitude) do not go through c: its rounding, a power of two
+// in every w, would grow with it.
+constexpr float kHuge = 65536.0f;
 
 __device__ __forceinline__ float power2(float x)
 {
@@ -45,12 +52,23 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
     return y;
 }
 
+__device__ __forceinline__ float centre(float m) { return m * kLog2e; }
+
+// One more element; 2^t stays out of sum w t where it is 0 (-inf times 0).
+__device__ __forceinline__ void add(Sums &a, float t)
+{
+    t = fmaxf(t, kNegligible);
+    const float w = power2(t);
+    a.s += w;
+    a.u = __fmaf_rn(w, t, a.u);
+}
+
 // a's sums brought to the maximum m >= a.m.
 __device__ __forceinline__ Sums rebase(const Sums &a, float m)
 {
     if (a.m == -INFINITY) return Sums{m, 0.0f, 0.0f};
-    const float d = a.m - m, f = power2(d * kLog2e);
-    // (u + d s before the factor: both shrink together)
+    const bool plain = fmaxf(fabsf(m), fabsf(a.m)) < kHuge;
+    const float d = plain ? centre(a.m) - centre(m) : (a.m - m) * kLog2e, f = power2(d);
     return Sums{m, a.s * f, f == 0.0f ? 0.0f : f * __fmaf_rn(d, a.s, a.u)};
 }
 __device__ __forceinline__ Sums merge(const Sums &a, const Sums &b)
@@ -92,15 +110,15 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     constexpr int kVec = 16 / sizeof(T), kLoads = 8 / kVec;       // eight elements a lane: one load, or two
     __shared__ Sums warp_sums[kMostWarps];
     __shared__ int any_bad[kMostWarps];
-    __shared__ unsigned floor_bits;                               // what some warp has as its last
+    __shared__ float floor_value;
+    __shared__ float published[64];                               // lanes' maxima, the largest of each warp
     __shared__ float list_v[kMostWarps][E2_MAX_TOP];
     __shared__ int list_id[kMostWarps][E2_MAX_TOP];
-    __shared__ Sums block_sums;
-    __shared__ int block_bad;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
     const int rank = blockIdx.x % p.split, row = blockIdx.x / p.split;
     const T *x = static_cast<const T *>(p.logits) + row * p.stride;
-    if (threadIdx.x == 0) floor_bits = ordered(-INFINITY);
+    if (TOP && threadIdx.x < 64) published[threadIdx.x] = -INFINITY;
+    if (TOP && threadIdx.x == 0) floor_value = -INFINITY;
     __syncthreads();
 
     // elements before the first 16-byte boundary, whole vectors, the rest
@@ -113,7 +131,6 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     Best best;
     best.clear();
     float last = -INFINITY;                                       // below it nothing is let in
-    bool first = true;
 
     // eight elements of each lane, -inf where there are none; element j is index(j)
     auto take = [&](const float (&e)[8], auto index) {
@@ -123,36 +140,20 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
         bad |= !(m < INFINITY);
         if (m > a.m) a = rebase(a, m);
         const float base = a.m == -INFINITY ? 0.0f : a.m;
+        if (fabsf(base) < kHuge) {
+            const float c = centre(base);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = fmaxf(e[j] - base, kNegligible), w = power2(d * kLog2e);
-            a.s += w;
-            a.u = __fmaf_rn(w, d, a.u);
+            for (int j = 0; j < 8; ++j) add(a, __fmaf_rn(e[j], kLog2e, -c));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) add(a, (e[j] - base) * kLog2e);
         }
         if (!TOP) return;
-        if (first) {
-            // the `top`-th largest of the lanes' maxima: sorted over the lanes
-            float v = m;
-#pragma unroll
-            for (int k = 2; k <= 32; k *= 2)
-#pragma unroll
-                for (int j = k / 2; j; j /= 2) {
-                    const float o = __shfl_xor_sync(~0u, v, j);
-                    const bool up = ((lane & k) == 0) == ((lane & j) == 0);   // (larger ones to lower lanes)
-                    v = up ? fmaxf(v, o) : fminf(v, o);
-                }
-            const float bound = __shfl_sync(~0u, v, p.top - 1);
-            // (fewer lanes than that have any: again next time)
-            if (bound > -INFINITY) {
-                first = false;
-                last = fmaxf(last, below(bound));                 // equal ones are let in
-            }
-        }
+        last = fmaxf(last, *reinterpret_cast<volatile float *>(&floor_value));
         if (!__any_sync(~0u, m > last)) return;
-        const float others = unordered(*reinterpret_cast<volatile unsigned *>(&floor_bits));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            unsigned b = __ballot_sync(~0u, e[j] > last && e[j] >= others);
+            unsigned b = __ballot_sync(~0u, e[j] > last);
             while (b) {
                 const int from = __ffs(b) - 1;
                 b &= b - 1;
@@ -161,22 +162,42 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
                 best.insert(v, at, lane);
             }
         }
-        const float worst = __shfl_sync(~0u, best.v, p.top - 1);
-        // (only elements of later rounds come after this: equal ones have higher indices)
-        last = fmaxf(last, worst);
-        if (worst > -INFINITY) {
-            if (lane == 0) atomicMax(&floor_bits, ordered(worst));
-            if (others > -INFINITY) last = fmaxf(last, below(others));
+        // (elements of later rounds have higher indices: equal ones stay out)
+        last = fmaxf(last, __shfl_sync(~0u, best.v, p.top - 1));
+    };
+    const int share = 64 / warps;                                 // published values of a warp
+    auto publish = [&](float m) {
+        unsigned o = ordered(m);
+        for (int i = 0; i < share; ++i) {
+            const unsigned most = __reduce_max_sync(~0u, o);
+            if (lane == 0) reinterpret_cast<volatile float *>(published)[warp * share + i] = unordered(most);
+            // (one lane's, where several have it)
+            if (lane == __ffs(__ballot_sync(~0u, o == most)) - 1) o = 0;
         }
     };
-
-    if (rank == 0 && warp == 0 && head > 0) {
-        float e[8];
+    // The `top`-th largest published value, by the first warp: below it nothing is let in.
+    auto draw_bound = [&] {
+        const volatile float *from = published;
+        float a = from[lane], b = from[lane + 32];
+        auto exchange = [&](float &v, int j, bool larger) {
+            const float o = __shfl_xor_sync(~0u, v, j);
+            v = larger ? fmaxf(v, o) : fminf(v, o);
+        };
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = -INFINITY;
-        if (lane < head) e[0] = to_float(x[lane]);
-        take(e, [&](int) { return lane; });
-    }
+        for (int k = 2; k <= 32; k *= 2)
+#pragma unroll
+            for (int j = k / 2; j; j /= 2) {
+                exchange(a, j, ((lane & k) == 0) == ((lane & j) == 0));     // falling over the lanes
+                exchange(b, j, ((lane & k) == 0) != ((lane & j) == 0));     // rising
+            }
+        // the larger half of both, sorted
+        a = fmaxf(a, b);
+#pragma unroll
+        for (int j = 16; j; j /= 2) exchange(a, j, (lane & j) == 0);
+        const float bound = __shfl_sync(~0u, a, p.top - 1);
+        if (lane == 0 && bound > -INFINITY && bound < INFINITY) *reinterpret_cast<volatile float *>(&floor_value) = below(bound);
+    };
+
     const uint4 *vec = reinterpret_cast<const uint4 *>(x + head);
     const int step = warps * 32 * kLoads;
     auto load = [&](uint4 (&w)[kLoads], int at) {
@@ -187,16 +208,43 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     int at = v0 + warp * 32 * kLoads;
     uint4 ahead[kLoads];
     load(ahead, at);
-    for (; at < v1; at += step) {
-        uint4 now[kLoads];
+    auto element = [&](const uint4 (&w)[kLoads], int j) {
+        return at + 32 * (j / kVec) + lane < v1 ? to_float(reinterpret_cast<const T *>(w)[j]) : -INFINITY;
+    };
+    auto index = [&](int j) { return head + (at + 32 * (j / kVec) + lane) * kVec + j % kVec; };
+    if (TOP) {
+        float m = element(ahead, 0);
 #pragma unroll
-        for (int l = 0; l < kLoads; ++l) now[l] = ahead[l];
-        load(ahead, at + step);
+        for (int j = 1; j < 8; ++j) m = fmaxf(m, element(ahead, j));
+        publish(m);
+        __syncthreads();
+        if (warp == 0) draw_bound();
+        __syncthreads();
+    }
+    if (rank == 0 && warp == 0 && head > 0) {
         float e[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            e[j] = at + 32 * (j / kVec) + lane < v1 ? to_float(reinterpret_cast<const T *>(now)[j]) : -INFINITY;
-        take(e, [&](int j) { return head + (at + 32 * (j / kVec) + lane) * kVec + j % kVec; });
+        for (int j = 0; j < 8; ++j) e[j] = -INFINITY;
+        if (lane < head) e[0] = to_float(x[lane]);
+        take(e, [&](int) { return lane; });
+    }
+    int round = 0;
+    for (; at + 32 * kLoads <= v1; at += step, ++round) {         // whole rounds, then at most one that is not
+        float e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = to_float(reinterpret_cast<const T *>(ahead)[j]);
+        load(ahead, at + step);
+        take(e, index);
+        if (TOP && (round == 2 || round == 8 || round == 32)) {
+            publish(a.m);
+            if (warp == 0) draw_bound();
+        }
+    }
+    if (at < v1) {
+        float e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = element(ahead, j);
+        take(e, index);
     }
     if (rank == p.split - 1 && warp == warps - 1 && tail < p.vocab) {
         float e[8];
@@ -214,63 +262,65 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     if (lane == 0) warp_sums[warp] = a, any_bad[warp] = bad;
     if (TOP && lane < p.top) list_v[warp][lane] = best.v, list_id[warp][lane] = best.id;
     __syncthreads();
-    if (warp == 0) {
-        Sums total = warp_sums[0];
-        int spoilt = any_bad[0];
-        for (int w = 1; w < warps; ++w) total = merge(total, warp_sums[w]), spoilt |= any_bad[w];
-        if (lane == 0) block_sums = total, block_bad = spoilt;
-        if (TOP) {
-            const float least = unordered(floor_bits);
-            for (int w = 1; w < warps; ++w) {
-                const float v = lane < p.top ? list_v[w][lane] : -INFINITY;
-                const int id = lane < p.top ? list_id[w][lane] : 0x7fffffff;
-                unsigned b = __ballot_sync(~0u, v >= least && v > -INFINITY);
-                while (b) {
-                    const int from = __ffs(b) - 1;
-                    b &= b - 1;
-                    best.insert(__shfl_sync(~0u, v, from), __shfl_sync(~0u, id, from), lane);
-                }
+    // sums of `n` lanes, over the lanes
+    auto join = [&](Sums mine, int n) {
+        if (lane >= n) mine = Sums{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 1; k < 32; k *= 2)
+            mine = merge(mine, Sums{__shfl_xor_sync(~0u, mine.m, k), __shfl_xor_sync(~0u, mine.s, k), __shfl_xor_sync(~0u, mine.u, k)});
+        return mine;
+    };
+    // the lists of `n` others, all their elements at once, 32 at a time
+    auto join_lists = [&](int n, float least, auto fetch) {
+        for (int c = lane; c - lane < n * p.top; c += 32) {
+            float v = -INFINITY;
+            int id = 0x7fffffff;
+            if (c < n * p.top) fetch(c / p.top, c % p.top, v, id);
+            unsigned b = __ballot_sync(~0u, v >= least && v > -INFINITY);
+            while (b) {
+                const int from = __ffs(b) - 1;
+                b &= b - 1;
+                best.insert(__shfl_sync(~0u, v, from), __shfl_sync(~0u, id, from), lane);
             }
-            if (p.split > 1 && lane < p.top) list_v[0][lane] = best.v, list_id[0][lane] = best.id;
         }
+    };
+    Sums total{-INFINITY, 0.0f, 0.0f};
+    bool spoilt = false;
+    if (warp == 0) {
+        total = join(warp_sums[lane % warps], warps);
+        spoilt = __any_sync(~0u, any_bad[lane % warps]);
+        // (its own bound holds for the block; equal ones count)
+        if (TOP)
+            join_lists(warps - 1, last, [&](int w, int j, float &v, int &id) { v = list_v[w + 1][j], id = list_id[w + 1][j]; });
     }
     if (p.split > 1) {
+        if (warp == 0) {
+            __syncwarp();
+            if (lane == 0) warp_sums[0] = total, any_bad[0] = spoilt;
+            if (TOP && lane < p.top) list_v[0][lane] = best.v, list_id[0][lane] = best.id;
+        }
         cluster_barrier();
         if (rank == 0 && warp == 0) {
-            Sums total = block_sums;
-            int spoilt = block_bad;
-            const uint32_t sums_at = smem_addr(&block_sums), bad_at = smem_addr(&block_bad);
-            for (int r = 1; r < p.split; ++r) {
-                const uint32_t s = peer_addr(sums_at, r);
-                total = merge(total, Sums{peer_load(s), peer_load(s + 4), peer_load(s + 8)});
-                spoilt |= __float_as_int(peer_load(peer_addr(bad_at, r)));
-                if (TOP) {
-                    float v = -INFINITY;
-                    int id = 0x7fffffff;
-                    if (lane < p.top) {
-                        v = peer_load(peer_addr(smem_addr(&list_v[0][lane]), r));
-                        id = __float_as_int(peer_load(peer_addr(smem_addr(&list_id[0][lane]), r)));
-                    }
-                    const float worst = __shfl_sync(~0u, best.v, p.top - 1);
-                    unsigned b = __ballot_sync(~0u, v >= worst && v > -INFINITY);
-                    while (b) {
-                        const int from = __ffs(b) - 1;
-                        b &= b - 1;
-                        best.insert(__shfl_sync(~0u, v, from), __shfl_sync(~0u, id, from), lane);
-                    }
-                }
-            }
-            if (lane == 0) block_sums = total, block_bad = spoilt;
+            const int r = lane % p.split;
+            const uint32_t at = peer_addr(smem_addr(&warp_sums[0]), r);
+            total = join(Sums{peer_load(at), peer_load(at + 4), peer_load(at + 8)}, p.split);
+            spoilt = __any_sync(~0u, __float_as_int(peer_load(peer_addr(smem_addr(&any_bad[0]), r))));
+            if (TOP)
+                join_lists(p.split - 1, __shfl_sync(~0u, best.v, p.top - 1), [&](int w, int j, float &v, int &id) {
+                    v = peer_load(peer_addr(smem_addr(&list_v[0][j]), w + 1));
+                    id = __float_as_int(peer_load(peer_addr(smem_addr(&list_id[0][j]), w + 1)));
+                });
         }
         cluster_barrier();                                        // (peers have been read)
     }
     if (rank != 0 || warp != 0) return;
-    __syncwarp();
-    const Sums total = block_sums;
-    const bool spoilt = block_bad, empty = total.m == -INFINITY;
-    const float nan = __int_as_float(0x7fc00000), ln = empty ? 0.0f : logf(total.s), lse = empty ? 0.0f : total.m + ln;
+    const bool empty = total.m == -INFINITY;
+    const float nan = __int_as_float(0x7fc00000), kLn2 = 0.6931471805599453f, ln = empty ? 0.0f : logf(total.s);
+    // c was off by this
+    const float rest = empty || !(fabsf(total.m) < kHuge) ? 0.0f : __fmaf_rn(total.m, kLog2e, -centre(total.m));
+    const float lse = empty ? 0.0f : total.m + __fmaf_rn(-rest, kLn2, ln);
     if (lane == 0) {
-        if (p.entropy) p.entropy[row] = spoilt ? nan : empty ? 0.0f : ln - total.u / total.s;
+        if (p.entropy) p.entropy[row] = spoilt ? nan : empty ? 0.0f : __fmaf_rn(-total.u / total.s, kLn2, ln);
         if (p.logprob) {
             const int y = p.tokens[row];
             p.logprob[row] = spoilt || y < 0 || y >= p.vocab ? nan : to_float(x[y]) - lse;
