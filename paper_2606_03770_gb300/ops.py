@@ -19,7 +19,6 @@ fallback: without the library, or with tensors off the GPU, the calls raise.
 from __future__ import annotations
 
 import ctypes as C
-import math
 
 import torch
 
@@ -91,11 +90,6 @@ def load():
     return _lib
 
 
-def _check(status, where):
-    if status != E2_OK:
-        raise e2ga.E2Error(status, where, load().e2_ops_error().decode())
-
-
 def _need(cond, text):
     if not cond:
         raise ValueError(text)
@@ -103,14 +97,31 @@ def _need(cond, text):
 
 def _tensor(x, name, dtypes, shape, device=None):
     """x is a tensor on the GPU with one of these types, this shape (None: any
-    size) and contiguous rows."""
-    _need(isinstance(x, torch.Tensor) and x.is_cuda, f"{name} must be a tensor on the GPU")
-    _need(device is None or x.device == device, f"{name} must be on {device}")
-    _need(x.dtype in dtypes, f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {x.dtype}")
+    size) and contiguous rows; returns its shape."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda):
+        raise ValueError(f"{name} must be a tensor on the GPU")
+    if device is not None and x.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if x.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {x.dtype}")
     s = x.shape
-    _need(len(s) == len(shape) and all(b is None or a == b for a, b in zip(s, shape)),
-          f"{name} has shape {tuple(s)}, not {tuple('any' if b is None else b for b in shape)}")
-    _need(s[-1] <= 1 or x.stride(-1) == 1, f"{name} must be contiguous in its last axis")
+    ok = len(s) == len(shape)
+    if ok:
+        for a, b in zip(s, shape):
+            ok = ok and (b is None or a == b)
+    if not ok:
+        raise ValueError(f"{name} has shape {tuple(s)}, not {tuple('any' if b is None else b for b in shape)}")
+    if s[-1] > 1 and x.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last axis")
+    return s
+
+
+def _like(x, name, dtype, shape, device):
+    """_tensor for one type and a whole shape: a few comparisons where all is
+    well (these run on every call of an operator)."""
+    if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.shape == shape and x.device == device
+            and x.stride(-1) == 1):
+        _tensor(x, name, (dtype,), shape, device)
 
 
 _HALF = (torch.float16, torch.bfloat16)
@@ -124,25 +135,28 @@ def _stride(x):
 
 def _rows(x, name):
     """Token stride of [tokens][heads][dim], whose heads lie side by side."""
-    _need(x.shape[1] <= 1 or x.stride(1) == x.shape[2], f"{name}: a token's heads must lie side by side")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+    tokens, heads, dim = x.shape
+    if heads > 1 and x.stride(1) != dim:
+        raise ValueError(f"{name}: a token's heads must lie side by side")
+    return x.stride(0) if tokens > 1 else heads * dim
 
 
-class _On:
-    """The tensors' device as the current one, and its current stream."""
+def _stream(device):
+    """The device's current stream, as a number."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
-    def __init__(self, device):
-        self.device = device
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
+def _call(name, device, *args):
+    """Calls a function of the library on the device's current stream, with
+    the device as the current one."""
+    f = getattr(_lib or load(), name)
+    if torch._C._cuda_getDevice() == device.index:
+        status = f(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = f(*args, _stream(device))
+    if status != E2_OK:
+        raise e2ga.E2Error(status, name, load().e2_ops_error().decode())
 
 
 # ---- products with 4-bit weights --------------------------------------------------
@@ -202,25 +216,26 @@ def quantize_weight(w, group=64, symmetric=True):
 def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
     """x [tokens, cols] times the weights' rows (+ residual): [tokens, rows],
     or, ``gated``, silu(x W_gate) * (x W_up) [tokens, rows / 2]."""
-    _tensor(x, "x", _HALF, (None, w.cols), w.device)
-    tokens, outs = x.shape[0], w.rows // 2 if gated else w.rows
+    dev = w.device
+    tokens = _tensor(x, "x", _HALF, (None, w.cols), dev)[0] if not (
+        isinstance(x, torch.Tensor) and x.dtype in _HALF and x.dim() == 2 and x.shape[1] == w.cols
+        and x.device == dev and x.stride(1) == 1) else x.shape[0]
+    outs = w.rows // 2 if gated else w.rows
+    dtype, shape = x.dtype, (tokens, outs)
     if residual is not None:
-        _tensor(residual, "residual", (x.dtype,), (tokens, outs), w.device)
+        _like(residual, "residual", dtype, shape, dev)
     if out is None:
-        out = torch.empty((tokens, outs), dtype=x.dtype, device=w.device)
+        out = torch.empty(shape, dtype=dtype, device=dev)
     else:
-        _tensor(out, "out", (x.dtype,), (tokens, outs), w.device)
-    lib = load()
-    a = e2_matmul_args(tokens, DTYPES[x.dtype], bool(gated), x.data_ptr(), _stride(x),
+        _like(out, "out", dtype, shape, dev)
+    a = e2_matmul_args(tokens, DTYPES[dtype], bool(gated), x.data_ptr(), _stride(x),
                        residual.data_ptr() if residual is not None else None,
-                       _stride(residual) if residual is not None else 0, out.data_ptr(),
-                       _stride(out))
-    need = lib.e2_quant_matmul_workspace(w.rows, w.cols, tokens)
-    if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=w.device)
-    with _On(w.device) as stream:
-        _check(lib.e2_quant_matmul(w.ref, C.byref(a), workspace.data_ptr() if need else None,
-                                   workspace.numel() if need else 0, stream), "e2_quant_matmul")
+                       _stride(residual) if residual is not None else 0, out.data_ptr(), _stride(out))
+    if workspace is None:
+        need = (_lib or load()).e2_quant_matmul_workspace(w.rows, w.cols, tokens)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call("e2_quant_matmul", dev, w.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
+          workspace.numel() if workspace is not None else 0)
     return out
 
 
@@ -261,46 +276,43 @@ def cache_append(cache, k, v, slots, positions, cos, sin, q=None, q_out=None, in
     """Append keys (turned by their positions) and values [tokens, kv_heads,
     head_dim] at ``slots`` (int64; page * page_size + token in page; -1: none).
     Returns the turned queries (``q_out``, allocated unless given), or None."""
-    dev, D = cache.device, cache.head_dim
-    _tensor(k, "k", _HALF, (None, cache.kv_heads, D), dev)
-    tokens = k.shape[0]
-    _tensor(v, "v", (k.dtype,), (tokens, cache.kv_heads, D), dev)
-    _tensor(slots, "slots", (torch.int64,), (tokens,), dev)
-    _tensor(positions, "positions", (torch.int32,), (tokens,), dev)
-    _tensor(cos, "cos", (torch.float32,), (None, None), dev)
-    _tensor(sin, "sin", (torch.float32,), cos.shape, dev)
+    dev, D, dtype = cache.device, cache.head_dim, k.dtype
+    tokens = _tensor(k, "k", _HALF, (None, cache.kv_heads, D), dev)[0]
+    _like(v, "v", dtype, (tokens, cache.kv_heads, D), dev)
+    _like(slots, "slots", torch.int64, (tokens,), dev)
+    _like(positions, "positions", torch.int32, (tokens,), dev)
+    table_rows, half = _tensor(cos, "cos", (torch.float32,), (None, None), dev)
+    _like(sin, "sin", torch.float32, (table_rows, half), dev)
     _need(cos.is_contiguous() and sin.is_contiguous(), "cos and sin must be contiguous")
-    rot = 2 * cos.shape[1]
     heads = qs = qos = 0
     if q is not None:
-        _tensor(q, "q", (k.dtype,), (tokens, None, D), dev)
-        heads = q.shape[1]
+        heads = _tensor(q, "q", (dtype,), (tokens, None, D), dev)[1]
         if q_out is None:
-            q_out = torch.empty((tokens, heads, D), dtype=q.dtype, device=dev)
+            q_out = torch.empty((tokens, heads, D), dtype=dtype, device=dev)
         else:
-            _tensor(q_out, "q_out", (k.dtype,), q.shape, dev)
+            _like(q_out, "q_out", dtype, (tokens, heads, D), dev)
         qs, qos = _rows(q, "q"), _rows(q_out, "q_out")
     else:
         _need(q_out is None, "q_out without q")
-    a = e2_append_args(tokens, DTYPES[k.dtype], heads, rot, bool(interleaved), cos.shape[0], slots.data_ptr(),
+    a = e2_append_args(tokens, DTYPES[dtype], heads, 2 * half, bool(interleaved), table_rows, slots.data_ptr(),
                        positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), k.data_ptr(), _rows(k, "k"),
                        v.data_ptr(), _rows(v, "v"), q.data_ptr() if heads else None, qs,
                        q_out.data_ptr() if heads else None, qos)
-    with _On(dev) as stream:
-        _check(load().e2_cache_append(cache.ref, C.byref(a), stream), "e2_cache_append")
+    _call("e2_cache_append", dev, cache.ref, C.byref(a))
     return q_out
 
 
 def cache_read(cache, slots, dtype=torch.bfloat16):
     """The keys and values at ``slots``, as the values their codes stand for."""
-    _tensor(slots, "slots", (torch.int64,), (None,), cache.device)
+    dev = cache.device
+    tokens = _tensor(slots, "slots", (torch.int64,), (None,), dev)[0]
     _need(dtype in DTYPES, "dtype must be float16, bfloat16 or float32")
-    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
-    k, v = (torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
+    shape = (tokens, cache.kv_heads, cache.head_dim)
+    k = torch.empty(shape, dtype=dtype, device=dev)
+    v = torch.empty(shape, dtype=dtype, device=dev)
     row = shape[1] * shape[2]
-    with _On(cache.device) as stream:
-        _check(load().e2_cache_read(cache.ref, slots.data_ptr(), shape[0], DTYPES[dtype], k.data_ptr(), row,
-                                    v.data_ptr(), row, stream), "e2_cache_read")
+    _call("e2_cache_read", dev, cache.ref, slots.data_ptr(), tokens, DTYPES[dtype], k.data_ptr(), row, v.data_ptr(),
+          row)
     return k, v
 
 
@@ -313,33 +325,28 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
     largest counts of queries and of cached tokens, are read from the device
     (a synchronisation) unless given.  scale: 1/sqrt(head_dim) unless given."""
     dev = cache.device
-    _tensor(q, "q", _HALF, (None, None, cache.head_dim), dev)
-    tokens, heads = q.shape[:2]
-    _tensor(table, "table", (torch.int32,), (None, None), dev)
-    batch = table.shape[0]
-    _tensor(lens, "lens", (torch.int32,), (batch,), dev)
-    _tensor(starts, "starts", (torch.int32,), (batch + 1,), dev)
+    tokens, heads, _ = _tensor(q, "q", _HALF, (None, None, cache.head_dim), dev)
+    batch, cols = _tensor(table, "table", (torch.int32,), (None, None), dev)
+    _like(lens, "lens", torch.int32, (batch,), dev)
+    _like(starts, "starts", torch.int32, (batch + 1,), dev)
     if max_new is None:
         max_new = int((starts[1:] - starts[:-1]).max()) if batch else 0
     if max_len is None:
         max_len = int(lens.max()) if batch else 0
     if out is None:
         # (tokens outside every request are not written)
-        out = torch.zeros_like(q, memory_format=torch.contiguous_format) if batch == 0 else \
-            torch.empty((tokens, heads, cache.head_dim), dtype=q.dtype, device=dev)
+        out = (torch.empty if batch else torch.zeros)((tokens, heads, cache.head_dim), dtype=q.dtype, device=dev)
     else:
-        _tensor(out, "out", (q.dtype,), q.shape, dev)
-    lib = load()
-    a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), table.shape[1],
-                       _stride(table), lens.data_ptr(), starts.data_ptr(),
-                       max_new, max_len, 1 / math.sqrt(cache.head_dim) if scale is None else scale, window,
-                       q.data_ptr(), _rows(q, "q"), out.data_ptr(), _rows(out, "out"))
-    with _On(dev) as stream:
-        need = lib.e2_cache_attend_workspace(cache.ref, C.byref(a))
-        if need and workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _check(lib.e2_cache_attend(cache.ref, C.byref(a), workspace.data_ptr() if need else None,
-                                   workspace.numel() if need else 0, stream), "e2_cache_attend")
+        _like(out, "out", q.dtype, (tokens, heads, cache.head_dim), dev)
+    a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), cols, _stride(table),
+                       lens.data_ptr(), starts.data_ptr(), max_new, max_len,
+                       cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), _rows(q, "q"),
+                       out.data_ptr(), _rows(out, "out"))
+    if workspace is None:
+        need = (_lib or load()).e2_cache_attend_workspace(cache.ref, C.byref(a))
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call("e2_cache_attend", dev, cache.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
+          workspace.numel() if workspace is not None else 0)
     return out
 
 
@@ -349,20 +356,18 @@ def token_logprobs(logits, tokens=None, top=0, entropy=True):
     probability of tokens[row] (int32; None without tokens), the entropy (None
     unless asked for), and the ``top`` largest log probabilities with their indices
     [rows, top], equal ones by their index.  All float32 / int32."""
-    _tensor(logits, "logits", _FLOAT, (None, None))
-    rows, vocab = logits.shape
+    rows, vocab = _tensor(logits, "logits", _FLOAT, (None, None))
     dev = logits.device
     _need(0 <= top <= E2_MAX_TOP, f"top must be in 0..{E2_MAX_TOP}")
     if tokens is not None:
-        _tensor(tokens, "tokens", (torch.int32,), (rows,), dev)
-    f = lambda *s: torch.empty(s, dtype=torch.float32, device=dev)  # noqa: E731
-    logprob = f(rows) if tokens is not None else None
-    ent = f(rows) if entropy else None
-    values, ids = f(rows, top), torch.empty((rows, top), dtype=torch.int32, device=dev)
+        _like(tokens, "tokens", torch.int32, (rows,), dev)
+    f32 = dict(dtype=torch.float32, device=dev)
+    logprob = torch.empty(rows, **f32) if tokens is not None else None
+    ent = torch.empty(rows, **f32) if entropy else None
+    values, ids = torch.empty((rows, top), **f32), torch.empty((rows, top), dtype=torch.int32, device=dev)
     a = e2_logprobs_args(rows, vocab, DTYPES[logits.dtype], top, logits.data_ptr(), _stride(logits),
                          tokens.data_ptr() if tokens is not None else None,
                          logprob.data_ptr() if tokens is not None else None, ent.data_ptr() if entropy else None,
                          values.data_ptr(), ids.data_ptr())
-    with _On(dev) as stream:
-        _check(load().e2_token_logprobs(C.byref(a), stream), "e2_token_logprobs")
+    _call("e2_token_logprobs", dev, C.byref(a))
     return logprob, ent, values, ids
