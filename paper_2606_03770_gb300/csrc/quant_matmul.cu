@@ -40,6 +40,9 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
     return plan(wk, split);
 }
 
+// From so many tokens on the block-wide products (measured: MEASURE).
+constexpr int kMany = 33;
+
 }  // namespace
 }  // namespace e2ops
 
@@ -47,9 +50,13 @@ using namespace e2ops;
 
 extern "C" size_t e2_quant_matmul_workspace(int32_t rows, int32_t cols, int32_t tokens)
 {
-    if (rows < 1 || cols < 1 || cols > E2_MAX_COLS || tokens < 1) return 0;
-    // (smaller groups have more sums)
-    return plan_few(rows, cols, tokens, 32, true).workspace;
+    Device dev;
+    if (rows < 1 || cols < 1 || cols > E2_MAX_COLS || tokens < 1 || current_device(&dev)) return 0;
+    // the larger of what groups of any size, with and without gates, need
+    if (tokens < kMany) return plan_few(rows, cols, tokens, 32, true).workspace;
+    const size_t plain = plan_many(rows, false, cols, tokens, dev.sms).workspace;
+    const size_t gated = rows % 2 ? 0 : plan_many(rows / 2, true, cols, tokens, dev.sms).workspace;
+    return plain > gated ? plain : gated;
 }
 
 extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a, void *workspace,
@@ -82,6 +89,11 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
     MatmulParams p{w->rows, w->cols, w->group, a->tokens, a->gated != 0, a->dtype == E2_F16, w->codes,
                    reinterpret_cast<const __half *>(w->scales), reinterpret_cast<const __half *>(w->mins),
                    a->x, a->residual, a->y, a->x_stride, a->residual_stride, a->y_stride};
+    if (a->tokens >= kMany) {
+        const ManyPlan f = plan_many(outs, p.gated, w->cols, a->tokens, dev.sms);
+        if (f.tiles > 65535) return fail(E2_EINVAL, "too many tokens for one call");
+        return launch_many(p, f, workspace, outs, dev.id, static_cast<cudaStream_t>(stream));
+    }
     const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr);
     // how the scales' rows are aligned
     const int wide = w->group == 128 ? 8 : 16, groups = w->cols / w->group;

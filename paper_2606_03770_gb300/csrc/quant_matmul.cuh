@@ -427,6 +427,14 @@ template <int G> int launch_few_group(const FewParams &q, const FewPlan &f, int 
                        : launch_few<G, false, 4>(q, f, dev, s);
 }
 
+// The launch of a prompt (quant_matmul_many.cu).
+struct ManyPlan {
+    int tile, tiles, split, stages, columns;
+    size_t image, workspace;
+};
+ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms);
+int launch_many(const MatmulParams &m, const ManyPlan &f, void *workspace, int outs, int dev, cudaStream_t s);
+
 // One translation unit per group size.
 int launch_few_32(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
 int launch_few_64(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s);
