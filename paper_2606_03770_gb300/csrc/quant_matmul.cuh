@@ -429,7 +429,7 @@ template <int G> int launch_few_group(const FewParams &q, const FewPlan &f, int 
 
 // The launch of a prompt (quant_matmul_many.cu).
 struct ManyPlan {
-    int tile, tiles, split, stages, columns;
+    int tile, tiles, split, stages, depth;
     size_t image, workspace;
 };
 ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms);
