@@ -3,12 +3,10 @@
 // Bound by the fifth-generation tensor cores.  A block takes 128 weight rows (gated: 128
 // that gate and the 128 that they gate) and up to 256 tokens (128): D[rows][tokens] = W
 // x^T, W and D in tensor memory, x in shared memory.  One warp copies x, prepared beforehand
-// as the images of its stages (one bulk copy each), one issues the products, eight
-// unpack weights, four every other stage: a thread a row's 64 columns, from registers that
-// are loaded stages ahead, to fp16 with their scale, one rounding (2^-11 of a weight;
-// |W| up to 65504).  (Unpacked into shared memory instead, a stage took 520 ns whatever its
-// tokens: the fence that the products need after such writes waits for the loads ahead as
-// well.)  Elements stay in the order that unpacking leaves (0, 4, 1, 5, 2, 6, 3, 7 of each
+// as the images of its stages (one bulk copy each), one issues the products, sixteen
+// unpack weights, four a stage: a thread a row's 64 columns, to fp16 with their scale, one
+// rounding (2^-11 of a weight; |W| up to 65504).  (Unpacked into shared memory instead, a stage took 520 ns whatever its
+// tokens, and 370 with each thread loading its own row, a line a lane.)  Elements stay in the order that unpacking leaves (0, 4, 1, 5, 2, 6, 3, 7 of each
 // eight), x is put into the same one.  Few rows are split over columns by the blocks of a
 // cluster, whose sums are joined in a fixed order through shared memory.
 //
@@ -21,18 +19,26 @@
 namespace e2ops {
 namespace {
 
-constexpr int kTileRows = 128, kStageCols = 64, kUnpackWarps = 8, kThreads = 32 * (2 + kUnpackWarps);
-constexpr int kAhead = 3;                                    // a warp's stages of codes in registers
+constexpr int kTileRows = 128, kStageCols = 64, kTeams = 4, kUnpackWarps = 4 * kTeams, kThreads = 32 * (2 + kUnpackWarps);
+constexpr int kRaw = 3;                                      // chunks of codes in shared memory
 // Tensor memory, all of it: sums first, then the stages of unpacked weights, 32 columns each.
 constexpr int kColumns = 512, kWeightColumns = 256, kWeightStages = 8;
-constexpr int kMostX = 8;                                    // stages of x
 
 struct ManyParams {
     MatmulParams m;
-    int outs, tile, tiles, split, stages, depth;             // tokens of a tile; stages of x in shared memory
+    int outs, tile, tiles, split, stages, depth;             // tokens of a tile; stages in flight
+    int scales_by;                                           // scales copied by a chunk's row, by 4 bytes, or one by one (2)
     const uint8_t *prepared;                                 // [tiles][cols / 64][tile][128 bytes], then scales per token
     const float *unscale;
 };
+
+// True in one thread of the warp.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes;
+}
 
 __device__ __forceinline__ void barrier_init(uint32_t at, int count)
 {
@@ -46,16 +52,15 @@ __device__ __forceinline__ void barrier_expect(uint32_t at, uint32_t bytes)
 {
     asm volatile("{\n.reg .b64 state;\nmbarrier.arrive.expect_tx.shared::cta.b64 state, [%0], %1;\n}" ::"r"(at), "r"(bytes) : "memory");
 }
-// Whether the phase ended, within a second or so (a million polls of up to a microsecond).
-__device__ bool barrier_wait(uint32_t at, uint32_t parity)
+// Whether the phase ended, within some seconds (a poll suspends the thread for a while).
+__device__ __forceinline__ bool barrier_wait(uint32_t at, uint32_t parity)
 {
-    for (int i = 0; i < (1 << 20); ++i) {
+    for (int i = 0; i < (1 << 22); ++i) {
         uint32_t done;
-        asm volatile(
-            "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
-            : "=r"(done)
-            : "r"(at), "r"(parity), "r"(1000u)
-            : "memory");
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done)
+                     : "r"(at), "r"(parity)
+                     : "memory");
         if (done) return true;
     }
     return false;
@@ -145,24 +150,34 @@ template <class T> __global__ void __launch_bounds__(512) image_kernel(const Man
     if (threadIdx.x == 0) unscale[tok] = power_of_two(-k);
 }
 
+// A chunk of codes and scales as they lie in shared memory (rows 16 bytes apart in banks).
+template <int G, bool MINS, int MT> struct Chunk {
+    static constexpr int kStages = kTeams / MT, kColumns = kStages * kStageCols, kPer = kColumns / G;
+    static constexpr int kRowBytes = kColumns / 2 + 16, kCodes = MT * kTileRows * kRowBytes;
+    static constexpr int kBytes = kCodes + MT * kTileRows * kPer * 2 * (MINS ? 2 : 1);
+};
+
 template <int G, bool MINS, int MT> __global__ void __launch_bounds__(kThreads, 1) many_kernel(const ManyParams q)
 {
     extern __shared__ uint8_t dynamic[];
     uint8_t *smem = dynamic + (1024 - smem_addr(dynamic) % 1024) % 1024;     // (swizzled tiles start on 1024 bytes)
-    __shared__ __align__(8) uint64_t barriers[2 * kMostX + 2 * kWeightStages + 1];
+    __shared__ __align__(8) uint64_t barriers[2 * kWeightStages + 1];
     __shared__ uint32_t tensor_memory;
     __shared__ int failed;
-    constexpr int kStep = kWeightColumns / MT, kDepthW = kWeightStages / MT;     // sums of a row tile; stages of weights
+    constexpr int kStep = kWeightColumns / MT;                  // columns of a row tile's sums
     const MatmulParams &p = q.m;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int rank = blockIdx.x % q.split, block = blockIdx.x / q.split;
     const uint32_t stage_bytes = (uint32_t)q.tile * 128;
-    const int s0 = (int)((int64_t)q.stages * rank / q.split), s1 = (int)((int64_t)q.stages * (rank + 1) / q.split), n = s1 - s0;
-    const uint32_t ring = smem_addr(smem), full_x = smem_addr(barriers), empty_x = full_x + 8 * kMostX;
-    const uint32_t full_w = empty_x + 8 * kMostX, empty_w = full_w + 8 * kWeightStages, done = empty_w + 8 * kWeightStages;
+    // this block's stages, whole chunks
+    constexpr int kChunkStages = kTeams / MT;
+    const int all_chunks = (q.stages + kChunkStages - 1) / kChunkStages;
+    const int s0 = (int)((int64_t)all_chunks * rank / q.split) * kChunkStages;
+    const int n = min((int)((int64_t)all_chunks * (rank + 1) / q.split) * kChunkStages, q.stages) - s0;
+    // a stage is full when x and the unpacked weights are there, empty when its products are done
+    const uint32_t ring = smem_addr(smem), full = smem_addr(barriers), empty = full + 8 * kWeightStages, done = empty + 8 * kWeightStages;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < q.depth; ++i) barrier_init(full_x + 8 * i, 1), barrier_init(empty_x + 8 * i, 1);
-        for (int i = 0; i < kDepthW; ++i) barrier_init(full_w + 8 * i, kUnpackWarps / 2), barrier_init(empty_w + 8 * i, 1);
+        for (int i = 0; i < q.depth; ++i) barrier_init(full + 8 * i, 1 + 4 * MT), barrier_init(empty + 8 * i, 1);
         barrier_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
@@ -179,128 +194,162 @@ template <int G, bool MINS, int MT> __global__ void __launch_bounds__(kThreads, 
 
     if (warp == 0) {
         // x: a stage's image by one copy
-        if (lane == 0) {
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            const uint8_t *from = q.prepared + ((size_t)blockIdx.y * q.stages + s0) * stage_bytes;
-            int i = 0, slot = 0, phase = 1;
-            for (; i < n; ++i) {
-                if (!barrier_wait(empty_x + 8 * slot, phase)) break;
-                barrier_expect(full_x + 8 * slot, stage_bytes);
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        const uint8_t *from = q.prepared + ((size_t)blockIdx.y * q.stages + s0) * stage_bytes;
+        int i = 0, slot = 0, phase = 1;
+        for (; i < n; ++i) {
+            if (!__all_sync(~0u, barrier_wait(empty + 8 * slot, phase))) break;
+            if (elected()) {
+                barrier_expect(full + 8 * slot, stage_bytes);
                 asm volatile(
                     "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring + slot * stage_bytes),
-                    "l"(from + (size_t)i * stage_bytes), "r"(stage_bytes), "r"(full_x + 8 * slot)
+                    "l"(from + (size_t)i * stage_bytes), "r"(stage_bytes), "r"(full + 8 * slot)
                     : "memory");
-                if (++slot == q.depth) slot = 0, phase ^= 1;
             }
-            if (i < n) {
-                failed = 1;
-                for (int j = i > q.depth ? i - q.depth : 0; j < i; ++j) barrier_wait(full_x + 8 * (j % q.depth), j / q.depth & 1);
-            }
+            __syncwarp();
+            if (++slot == q.depth) slot = 0, phase ^= 1;
+        }
+        if (i < n) {
+            // the copies in flight have no waiter of their own: their stages are given up on after a while
+            failed = 1;
+            for (int j = i > q.depth ? i - q.depth : 0; j < i; ++j) barrier_wait(full + 8 * (j % q.depth), j / q.depth & 1);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t kind = 1u << 4 | (uint32_t)(q.tile >> 3) << 17 | (uint32_t)(kTileRows >> 4) << 24;
-            bool ok = true;
-            int slot = 0, phase = 0;
-            for (int i = 0; i < n; ++i) {
-                const int w = i % kDepthW;
-                ok = barrier_wait(full_x + 8 * slot, phase) && barrier_wait(full_w + 8 * w, i / kDepthW & 1);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        // products: the whole warp waits, one thread issues
+        const uint32_t kind = 1u << 4 | (uint32_t)(q.tile >> 3) << 17 | (uint32_t)(kTileRows >> 4) << 24;
+        bool ok = true;
+        int slot = 0, phase = 0;
+        for (int i = 0; i < n; ++i) {
+            ok = __all_sync(~0u, barrier_wait(full + 8 * slot, phase));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (elected()) {
                 const uint64_t b = operand(ring + slot * stage_bytes);
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
                     for (int k = 0; k < kStageCols / 16; ++k)
-                        issue_product(d + t * kStep, weights + (w * MT + t) * 32 + 8 * k, b + 2 * k, kind, i > 0 || k > 0);
-                commit_products(empty_x + 8 * slot);
-                commit_products(empty_w + 8 * w);
-                if (++slot == q.depth) slot = 0, phase ^= 1;
+                        issue_product(d + t * kStep, weights + (slot * MT + t) * 32 + 8 * k, b + 2 * k, kind, i > 0 || k > 0);
+                commit_products(empty + 8 * slot);
             }
-            if (!ok) failed = 1;
-            commit_products(done);
-            if (!barrier_wait(done, 0)) failed = 1;
+            __syncwarp();
+            if (++slot == q.depth) slot = 0, phase ^= 1;
         }
+        if (!ok) failed = 1;
+        if (elected()) commit_products(done);
+        __syncwarp();
+        if (!__all_sync(~0u, barrier_wait(done, 0))) failed = 1;
     } else {
-        // weights: a thread a row; warps 2-5 even stages, 6-9 odd ones
-        const int team = (warp - 2) / 4, quarter = warp % 4, r = 32 * quarter + lane;
-        const int groups = p.cols / G;
-        constexpr int kScales = G == 32 ? 2 : 1;
-        const uint8_t *codes[MT];
-        const __half *scales[MT], *mins[MT];
+        // weights, in chunks: 128 rows of 256 columns, four stages (gated: two times 128 rows of
+        // 128 columns).  The four warps of a quarter of the rows copy it together, whole runs
+        // of a row; then each, of another team, unpacks one stage (gated: of one of the two), a
+        // thread a row.
+        const int team = (warp - 2) / 4, quarter = warp % 4, t = team % MT;
+        using Ch = Chunk<G, MINS, MT>;
+        const int groups = p.cols / G, chunks = (n + Ch::kStages - 1) / Ch::kStages;
+        uint8_t *raw = smem + q.depth * stage_bytes;
+        // (past the last row the last one is read again, and its results are dropped)
+        auto source = [&](int r, int tile) { return (int64_t)min(block * kTileRows + r, q.outs - 1) + (int64_t)tile * q.outs; };
+        auto copy = [&](int c) {
+            if (c < chunks) {
+                const uint32_t to = smem_addr(raw) + c % kRaw * Ch::kBytes;
+                constexpr int kPieces = Ch::kColumns / 32, kRowsAtOnce = 32 / kPieces;      // 16 bytes of codes
+                const int col0 = (s0 + c * Ch::kStages) * kStageCols, part = lane % kPieces;
+                // (past the last column any codes will do: x is 0 there)
+                const int at = col0 / 2 + (col0 + part * 32 < p.cols ? part * 16 : -(col0 / 2));
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            // (past the last row the last one is read again, and its results are dropped)
-            const int64_t row = min(block * kTileRows + r, q.outs - 1) + (int64_t)t * q.outs;
-            codes[t] = p.codes + row * (p.cols / 2);
-            scales[t] = p.scales + row * groups;
-            mins[t] = MINS ? p.mins + row * groups : nullptr;
-        }
-        uint4 w[kAhead][MT][2];
-        __half sc[kAhead][MT][kScales], mn[kAhead][MT][kScales];
-        auto fetch = [&](int i, int at) {
-            const int col = (s0 + i) * kStageCols;
-            // (a last stage may have 32 columns; what is past them is 0, as x is)
-            const bool in = i < n, whole = in && col + 32 < p.cols;
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                w[at][t][0] = in ? *reinterpret_cast<const uint4 *>(codes[t] + col / 2) : uint4{0, 0, 0, 0};
-                w[at][t][1] = whole ? *reinterpret_cast<const uint4 *>(codes[t] + col / 2 + 16) : uint4{0, 0, 0, 0};
-#pragma unroll
-                for (int j = 0; j < kScales; ++j) {
-                    const bool there = j ? whole : in;
-                    sc[at][t][j] = there ? scales[t][col / G + j] : __half(0.0f);
-                    mn[at][t][j] = MINS && there ? mins[t][col / G + j] : __half(0.0f);
+                for (int i = 0; i < 8 * MT / kRowsAtOnce; ++i) {
+                    const int e = team * 8 * MT + i * kRowsAtOnce + lane / kPieces, r = 32 * quarter + e % 32, tile = e / 32;
+                    copy_async16(to + (tile * kTileRows + r) * Ch::kRowBytes + part * 16, p.codes + source(r, tile) * (p.cols / 2) + at, true);
                 }
-            }
-        };
+                // scales: teams take the rows of a tile in turn, and of scales and minima
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) fetch(team + 2 * a, a);
-        bool ok = true;
-        for (int i0 = team; i0 < n && ok; i0 += 2 * kAhead) {
+                for (int k = 0; k < MT * (MINS ? 2 : 1); ++k) {
+                    if (k % kTeams != team) continue;
+                    const int tile = k % MT, r = 32 * quarter + lane;
+                    const __half *f = (k / MT ? p.mins : p.scales) + source(r, tile) * groups;
+                    const uint32_t dst = to + Ch::kCodes + (k * kTileRows + r) * (Ch::kPer * 2);
+                    const int g0 = col0 / G;
+                    if constexpr (Ch::kPer == 1) {
+                        const uint16_t v = g0 < groups ? __half_as_ushort(f[g0]) : 0;
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst), "h"(v) : "memory");
+                    } else if (q.scales_by > 4) {
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(f + g0), "n"(Ch::kPer * 2) : "memory");
+                    } else {
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const int i = i0 + 2 * a, slot = i % kDepthW;
-                if (i >= n || !ok) break;
-                uint32_t v[MT][32];
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const __half2 ds = __half2half2(sc[a][t][kScales == 2 ? h : 0]), ms = __half2half2(mn[a][t][kScales == 2 ? h : 0]);
-                        scale_word<MINS>(&v[t][16 * h], w[a][t][h].x, ds, ms);
-                        scale_word<MINS>(&v[t][16 * h + 4], w[a][t][h].y, ds, ms);
-                        scale_word<MINS>(&v[t][16 * h + 8], w[a][t][h].z, ds, ms);
-                        scale_word<MINS>(&v[t][16 * h + 12], w[a][t][h].w, ds, ms);
+                        for (int j = 0; j < Ch::kPer; j += 2) {
+                            if (q.scales_by == 4) {
+                                copy_async4(dst + 2 * j, g0 + j < groups ? f + g0 + j : f, g0 + j < groups);
+                            } else {
+                                const uint32_t lo = g0 + j < groups ? __half_as_ushort(f[g0 + j]) : 0u;
+                                const uint32_t hi = g0 + j + 1 < groups ? __half_as_ushort(f[g0 + j + 1]) : 0u;
+                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * j), "r"(lo | hi << 16) : "memory");
+                            }
+                        }
                     }
-                fetch(i + 2 * kAhead, a);
-                ok = __all_sync(~0u, barrier_wait(empty_w + 8 * slot, (i / kDepthW & 1) ^ 1));
-                if (ok) {
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                    for (int t = 0; t < MT; ++t)
-                        store_columns(weights + ((uint32_t)(32 * quarter) << 16) + (slot * MT + t) * 32, v[t]);
-                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive(full_w + 8 * slot);
-                } else if (lane == 0) {
-                    failed = 1;
                 }
             }
+            copy_commit();
+        };
+        copy(0);
+        copy(1);
+        bool ok = true;
+        for (int c = 0; c < chunks; ++c) {
+            copy_wait<1>();
+            // the chunk is there, and the one before is done with, for the quarter's four warps
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + quarter) : "memory");
+            copy(c + 2);
+            const int i = c * Ch::kStages + team / MT, slot = i % q.depth, round = i / q.depth;
+            ok = ok && !*reinterpret_cast<volatile int *>(&failed);
+            ok = __all_sync(~0u, ok);
+            if (i >= n || !ok) continue;
+            const int r = 32 * quarter + lane, from = i % Ch::kStages;
+            const uint8_t *chunk = raw + c % kRaw * Ch::kBytes;
+            const uint4 *w = reinterpret_cast<const uint4 *>(chunk + (t * kTileRows + r) * Ch::kRowBytes + from * 32);
+            const uint4 w0 = w[0], w1 = w[1];
+            const __half *sc = reinterpret_cast<const __half *>(chunk + Ch::kCodes + (t * kTileRows + r) * (Ch::kPer * 2));
+            const __half *mn = sc + MT * kTileRows * Ch::kPer;
+            const int g0 = from * kStageCols / G, g1 = (from * kStageCols + 32) / G;
+            uint32_t v[32];
+            {
+                const __half2 ds = __half2half2(sc[g0]), ms = __half2half2(MINS ? mn[g0] : __half(0.0f));
+                scale_word<MINS>(&v[0], w0.x, ds, ms);
+                scale_word<MINS>(&v[4], w0.y, ds, ms);
+                scale_word<MINS>(&v[8], w0.z, ds, ms);
+                scale_word<MINS>(&v[12], w0.w, ds, ms);
+            }
+            {
+                const __half2 ds = __half2half2(sc[g1]), ms = __half2half2(MINS ? mn[g1] : __half(0.0f));
+                scale_word<MINS>(&v[16], w1.x, ds, ms);
+                scale_word<MINS>(&v[20], w1.y, ds, ms);
+                scale_word<MINS>(&v[24], w1.z, ds, ms);
+                scale_word<MINS>(&v[28], w1.w, ds, ms);
+            }
+            ok = __all_sync(~0u, barrier_wait(empty + 8 * slot, (round & 1) ^ 1));
+            if (ok) {
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                store_columns(weights + ((uint32_t)(32 * quarter) << 16) + (slot * MT + t) * 32, v);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(full + 8 * slot);
+            } else if (lane == 0) {
+                failed = 1;
+            }
         }
+        copy_wait<0>();
     }
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // (unscale comes from the kernel before, too)
     const bool bad = *reinterpret_cast<volatile int *>(&failed);
 
-    // outputs: lanes are rows, columns tokens; the unpacking warps take them, two to 32 lanes
+    // outputs: lanes are rows, columns tokens; the unpacking warps take them, four to 32 lanes
     const int token0 = blockIdx.y * q.tile, live = min(q.tile, p.tokens - token0);
     const float nan = __int_as_float(0x7fc00000);
     if (warp >= 2) {
         const int quarter = warp % 4, row = 32 * quarter + lane, out = block * kTileRows + row;
-        for (int c = (warp - 2) / 4 * 16; c < live; c += 32) {
+        for (int c = (warp - 2) / 4 * 16; c < live; c += 16 * kTeams) {
             uint32_t v[MT][16];
 #pragma unroll
             for (int t = 0; t < MT; ++t) load_columns(v[t], d + ((uint32_t)(32 * quarter) << 16) + t * kStep + c);
@@ -364,7 +413,7 @@ template <int G, bool MINS, int MT> int launch_many_as(const ManyParams &q, cons
     cfg.gridDim = dim3((unsigned)((q.outs + kTileRows - 1) / kTileRows * q.split), (unsigned)q.tiles);
     cfg.blockDim = dim3(kThreads);
     // (never two blocks on a multiprocessor: tensor memory is for one)
-    const size_t ring = (size_t)q.depth * q.tile * 128 + 1024, sums = q.split > 1 ? (size_t)MT * q.tile * kTileRows * 4 + 1024 : 0;
+    const size_t ring = (size_t)q.depth * q.tile * 128 + kRaw * Chunk<G, MINS, MT>::kBytes + 1024, sums = q.split > 1 ? (size_t)MT * q.tile * kTileRows * 4 + 1024 : 0;
     cfg.dynamicSmemBytes = std::max(std::max(ring, sums), (size_t)kSmemPerSm / 2);
     cfg.stream = s;
     cfg.attrs = at;
@@ -403,8 +452,8 @@ ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms)
             const double t = turns * (stage * ((stages + split - 1) / split) + 4000.0 + mt * 12.0 * tile + (split > 1 ? 2500.0 : 0.0));
             if (t < least) {
                 least = t;
-                const int fit = 200 * 1024 / (tile * 128);
-                best = ManyPlan{tile, tiles, split, stages, fit < kMostX ? fit : kMostX, (size_t)tiles * stages * tile * 128, 0};
+                const int fit = 140 * 1024 / (tile * 128);
+                best = ManyPlan{tile, tiles, split, stages, fit < kWeightStages / mt ? fit : kWeightStages / mt, (size_t)tiles * stages * tile * 128, 0};
                 best.workspace = best.image + (size_t)tokens * 4;
             }
         }
@@ -414,8 +463,12 @@ ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms)
 
 int launch_many(const MatmulParams &m, const ManyPlan &f, void *workspace, int outs, int dev, cudaStream_t s)
 {
-    ManyParams q{m, outs, f.tile, f.tiles, f.split, f.stages, f.depth, static_cast<const uint8_t *>(workspace),
+    ManyParams q{m, outs, f.tile, f.tiles, f.split, f.stages, f.depth, 0, static_cast<const uint8_t *>(workspace),
                  reinterpret_cast<const float *>(static_cast<const uint8_t *>(workspace) + f.image)};
+    // how a chunk's rows of scales are aligned
+    const int columns = kStageCols * kTeams / (m.gated ? 2 : 1), wide = columns / m.group * 2, groups = m.cols / m.group;
+    auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(m.scales, to) && aligned(m.mins, to); };
+    q.scales_by = wide >= 4 && m.cols % columns == 0 && all_aligned(wide) ? 16 : wide >= 4 && all_aligned(4) ? 4 : 2;
     return m.group == 32   ? launch_many_group<32>(q, f, dev, s)
            : m.group == 64 ? launch_many_group<64>(q, f, dev, s)
                            : launch_many_group<128>(q, f, dev, s);
