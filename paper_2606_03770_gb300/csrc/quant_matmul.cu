@@ -41,7 +41,7 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
 }
 
 // From so many tokens on the block-wide products (measured: MEASURE).
-constexpr int kMany = 33;
+constexpr int kMany = 17;
 
 }  // namespace
 }  // namespace e2ops
