@@ -20,6 +20,7 @@ namespace e2ops {
 namespace {
 
 constexpr int kTileRows = 128, kStageCols = 64, kTeams = 4, kUnpackWarps = 4 * kTeams, kThreads = 32 * (2 + kUnpackWarps);
+constexpr int kMostSplit = 8;
 constexpr int kRaw = 3;                                      // chunks of codes in shared memory
 // Tensor memory, all of it: sums first, then the stages of unpacked weights, 32 columns each.
 constexpr int kColumns = 512, kWeightColumns = 256, kWeightStages = 8;
@@ -395,17 +396,28 @@ template <int G, bool MINS, int MT> __global__ void __launch_bounds__(kThreads, 
     if (q.split > 1) {
         __syncthreads();
         cluster_barrier();
-        // each block of the cluster joins its share of the tokens
+        // each block of the cluster joins its share of the tokens, four rows a thread
         const uint32_t mine = smem_addr(smem);
-        for (int at = rank * kThreads + threadIdx.x; at < live * kTileRows; at += q.split * kThreads) {
-            const int c = at / kTileRows, row = at % kTileRows, out = block * kTileRows + row;
-            if (out >= q.outs) continue;
-            float v[MT] = {};
-            for (int k = 0; k < q.split; ++k)
+        for (int at = rank * kThreads + threadIdx.x; at < live * (kTileRows / 4); at += q.split * kThreads) {
+            const int c = at / (kTileRows / 4), row = at % (kTileRows / 4) * 4, out = block * kTileRows + row;
+            float4 v[MT][kMostSplit];
 #pragma unroll
-                for (int t = 0; t < MT; ++t) v[t] += peer_load(peer_addr(mine + ((t * q.tile + c) * kTileRows + row) * 4, k));
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int k = 0; k < kMostSplit; ++k)
+                    if (k < q.split) v[t][k] = peer_load4(peer_addr(mine + ((t * q.tile + c) * kTileRows + row) * 4, k));
+            float4 sum[MT] = {};
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int k = 0; k < kMostSplit; ++k)
+                    if (k < q.split) sum[t].x += v[t][k].x, sum[t].y += v[t][k].y, sum[t].z += v[t][k].z, sum[t].w += v[t][k].w;
             const float f = q.unscale[token0 + c];
-            finish(p, token0 + c, out, v[0] * f, v[MT - 1] * f);
+            const float4 &g = sum[0], &h = sum[MT - 1];
+            if (out < q.outs) finish(p, token0 + c, out, g.x * f, h.x * f);
+            if (out + 1 < q.outs) finish(p, token0 + c, out + 1, g.y * f, h.y * f);
+            if (out + 2 < q.outs) finish(p, token0 + c, out + 2, g.z * f, h.z * f);
+            if (out + 3 < q.outs) finish(p, token0 + c, out + 3, g.w * f, h.w * f);
         }
         cluster_barrier();                                               // (peers may still read)
     }
@@ -465,11 +477,11 @@ ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms)
     for (int tile = 32; tile <= 256 / mt; tile += 16) {
         const int tiles = (tokens + tile - 1) / tile;
         if (tile > 32 && (tokens + tiles - 1) / tiles <= tile - 16) continue;                  // (a smaller one does as well)
-        for (int split = 1; split <= 8; split *= 2) {
+        for (int split = 1; split <= kMostSplit; split *= 2) {
             if (split > 1 && stages / split < 8) continue;
             const double turns = (double)(((int64_t)row_tiles * tiles * split + sms - 1) / sms);
-            const double stage = mt * (2.0 * tile > 400.0 ? 2.0 * tile : 400.0);
-            const double t = turns * (stage * ((stages + split - 1) / split) + 4000.0 + mt * 12.0 * tile + (split > 1 ? 2500.0 : 0.0));
+            const double stage = mt * (2.0 * tile > 430.0 ? 2.0 * tile : 430.0);
+            const double t = turns * (stage * ((stages + split - 1) / split) + 4000.0 + mt * 12.0 * tile + (split > 1 ? 3000.0 + mt * 16.0 * tile : 0.0));
             if (t < least) {
                 least = t;
                 const int fit = 140 * 1024 / (tile * 128);
