@@ -2,47 +2,13 @@
 #include <atomic>
 #include <type_traits>
 
-#include "ops_x.cuh"
+#include "cache_attend.cuh"
 
 namespace e2ops {
 
 int check_cache(const e2_cache *c, int dev);
 
 namespace {
-
-struct AttendParams {
-    int pages, page_shift, kv_heads, tokens, q_heads, batch, window, table_cols, splits;
-    int64_t table_stride, q_stride, out_stride;
-    const uint8_t *codes[2];
-    const __half2 *scales[2];
-    const int32_t *table, *lens, *starts;
-    float scale;
-    const void *q;
-    void *out;
-    float *parts;            // [tokens][q_heads][splits][D + 2]: a split's sums, maximum and sum of weights
-};
-
-// One request and KV head: its queries, times the query heads that share the KV head,
-// are rows, row = query * share + head.
-struct Rows {
-    int start, share;
-    int64_t count, first_pos;                // rows; position of the first query
-    __device__ Rows(const AttendParams &p, int request)
-    {
-        start = p.starts[request];
-        share = p.q_heads / p.kv_heads;
-        const int64_t queries = (int64_t)p.starts[request + 1] - start;
-        count = queries > 0 ? queries * share : 0;
-        first_pos = p.lens[request] - (queries > 0 ? queries : 0);
-    }
-    __device__ int64_t pos(int64_t row) const { return first_pos + row / share; }
-    __device__ int64_t token(int64_t row) const { return start + row / share; }
-    __device__ int head(int kv, int64_t row) const { return kv * share + (int)(row % share); }
-    __device__ bool live(const AttendParams &p, int64_t row) const
-    {
-        return row < count && token(row) >= 0 && token(row) < p.tokens;
-    }
-};
 
 // ---- a few rows ------------------------------------------------------------------
 //
@@ -75,18 +41,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
-__device__ __forceinline__ float power2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
-{
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
 template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, 3) few_kernel(const AttendParams p)
 {
     using St = FewStage<D>;
@@ -839,10 +793,10 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
 
 // From here on the rows of a request and KV head go to many_kernel (measured, us:
 // MEASURE).
-constexpr int kMany = 33;
+constexpr int kMany = 33, kPrompt = 65;
 
 struct Plan {
-    int nt, slabs, splits;      // nt 0: many_kernel
+    int nt, slabs, splits;      // nt 0: many_kernel, -1: the prompts'
 };
 
 // Rows by eight or sixteen, or by 64; keys split until every multiprocessor has its
@@ -851,15 +805,15 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
 {
     Plan f;
     const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
-    f.nt = rows >= kMany ? 0 : rows <= 8 ? 1 : 2;
-    const int at_once = f.nt ? 8 * f.nt : kManyRows;
+    f.nt = rows >= kPrompt ? -1 : rows >= kMany ? 0 : rows <= 8 ? 1 : 2;
+    const int at_once = f.nt < 0 ? kPromptRows : f.nt ? 8 * f.nt : kManyRows;
     const int64_t slabs = (rows + at_once - 1) / at_once;
     f.slabs = (int)(slabs < 65535 ? slabs : 65535);
     int64_t keys = a->max_len;
     if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
-    const int least = f.nt ? kTile * kFewWarps : 4 * kManyKeys;
+    const int least = f.nt > 0 ? kTile * kFewWarps : 4 * kManyKeys;
     const int64_t units = (keys + least - 1) / least;
-    int64_t splits = (int64_t)sms * 3 / ((int64_t)a->batch * c->kv_heads * slabs);
+    int64_t splits = (int64_t)sms * (f.nt < 0 ? 1 : 3) / ((int64_t)a->batch * c->kv_heads * slabs);
     if (splits > units) splits = units;
     f.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     return f;
@@ -898,7 +852,9 @@ template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
     int st;
-    if (f.nt == 0) {
+    if (f.nt < 0) {
+        st = launch_prompt(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s);
+    } else if (f.nt == 0) {
         const dim3 blocks((unsigned)f.slabs, pairs, (unsigned)f.splits);
         st = launch(many_kernel<T, D>, p, blocks, ManyShared<D>::kBytes, false, dev, ready[2], s);
     } else {
@@ -906,7 +862,7 @@ template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f
                        : launch(few_kernel<T, D, 2>, p, grid, smem, false, dev, ready[1], s);
     }
     if (st != E2_OK || f.splits == 1) return st;
-    return launch(join_kernel<T, D>, p, dim3((unsigned)f.slabs * (f.nt ? 8 * f.nt : kManyRows), pairs), 0, true, dev, ready[0], s);
+    return launch(join_kernel<T, D>, p, dim3((unsigned)f.slabs * (f.nt < 0 ? kPromptRows : f.nt ? 8 * f.nt : kManyRows), pairs), 0, true, dev, ready[0], s);
 }
 
 int check_args(const e2_cache *c, const e2_attend_args *a)

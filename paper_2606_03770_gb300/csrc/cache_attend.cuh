@@ -1,0 +1,61 @@
+// cache_attend.cuh -- what the kernels of e2_cache_attend share.
+#pragma once
+
+#include <atomic>
+#include <type_traits>
+
+#include "ops_x.cuh"
+
+namespace e2ops {
+
+struct AttendParams {
+    int pages, page_shift, kv_heads, tokens, q_heads, batch, window, table_cols, splits;
+    int64_t table_stride, q_stride, out_stride;
+    const uint8_t *codes[2];
+    const __half2 *scales[2];
+    const int32_t *table, *lens, *starts;
+    float scale;
+    const void *q;
+    void *out;
+    float *parts;            // [tokens][q_heads][splits][D + 2]: a split's sums, maximum and sum of weights
+};
+
+// One request and KV head: its queries, times the query heads that share the KV head,
+// are rows, row = query * share + head.
+struct Rows {
+    int start, share;
+    int64_t count, first_pos;                // rows; position of the first query
+    __device__ Rows(const AttendParams &p, int request)
+    {
+        start = p.starts[request];
+        share = p.q_heads / p.kv_heads;
+        const int64_t queries = (int64_t)p.starts[request + 1] - start;
+        count = queries > 0 ? queries * share : 0;
+        first_pos = p.lens[request] - (queries > 0 ? queries : 0);
+    }
+    __device__ int64_t pos(int64_t row) const { return first_pos + row / share; }
+    __device__ int64_t token(int64_t row) const { return start + row / share; }
+    __device__ int head(int kv, int64_t row) const { return kv * share + (int)(row % share); }
+    __device__ bool live(const AttendParams &p, int64_t row) const
+    {
+        return row < count && token(row) >= 0 && token(row) < p.tokens;
+    }
+};
+
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// The rows of a prompt (cache_attend_prompt.cu): blocks of kPromptRows, `splits` parts of the keys.
+constexpr int kPromptRows = 256;
+int launch_prompt(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s);
+
+}  // namespace e2ops

@@ -75,7 +75,8 @@ __host__ __device__ constexpr int x_row_bytes(int cols) { return cols * 2 + 64; 
 template <class T>
 __device__ __forceinline__ void finish_as(const MatmulParams &p, int token, int row, float a, float b)
 {
-    float y = p.gated ? a / (1.0f + expf(-a)) * b : a;
+    // (a few units in the last of 24 bits, before the rounding to 16)
+    float y = p.gated ? __fdividef(a, 1.0f + __expf(-a)) * b : a;
     if (p.residual) y += to_float(static_cast<const T *>(p.residual)[token * p.residual_stride + row]);
     static_cast<T *>(p.y)[token * p.y_stride + row] = from_float<T>(y);
 }
