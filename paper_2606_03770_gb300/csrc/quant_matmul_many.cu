@@ -286,7 +286,7 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
         for (int c = (warp - 2) / 4 * 16; c < live; c += 16 * kTeams) {
             uint32_t v[16];
             load_columns(v, d + ((uint32_t)(32 * quarter) << 16) + c);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            loaded(v);
 #pragma unroll
             for (int e = 0; e < 16; ++e) take(c + e, bad ? nan : __uint_as_float(v[e]));
         }
