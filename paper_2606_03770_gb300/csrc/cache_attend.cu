@@ -436,309 +436,6 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
     }
 }
 
-// ---- many rows -------------------------------------------------------------------
-//
-// Prompts.  Bound by the tensor cores.  Tiles of 64 keys are dequantised into
-// shared memory once per block (fp16, one rounding: 2^-12 of a value) and met by 64
-// rows, 16 a warp.  Elements stay in the order that unpacking leaves (0, 4, 1, 5, 2, 6,
-// 3, 7 of each eight), the queries are put into the same one, and the outputs taken
-// out of it at the end.  Weights go to fp16 times 2^14 (2^-12 each; fp16 outputs take
-// the rounding's rest in a second product).  A weight of 0 does not stop a NaN among the
-// values, so values that are not finite are held back as zeros, and rows that do
-// see their keys are made NaN.
-
-constexpr int kManyRows = 64, kManyKeys = 64;
-
-template <int D> struct ManyShared {
-    static constexpr int kKeyBytes = 2 * D + 16;                          // fp16 rows, 16 bytes apart in banks
-    static constexpr int kTile = kManyKeys * kKeyBytes;                   // keys; then values
-    static constexpr int kCodes = kManyKeys * (D / 2), kScales = kManyKeys * (D / E2_CACHE_GROUP) * 4;
-    static constexpr int kRaw = 2 * kCodes + 2 * kScales;                 // a tile as it is cached; two of them
-    static constexpr int kBytes = 2 * kTile + 2 * kRaw;
-};
-
-template <class T, int D> __global__ void __launch_bounds__(128, 3) many_kernel(const AttendParams p)
-{
-    using Sh = ManyShared<D>;
-    constexpr int GR = D / E2_CACHE_GROUP, KS = D / 16, NK = kManyKeys / 8, ND = D / 8;
-    constexpr bool kRest = std::is_same<T, __half>::value;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float row_scale[kManyRows];
-    __shared__ __align__(4) uint8_t there[2][4];                        // per raw tile: whether each 16 keys are there
-    __shared__ unsigned bad[2][GR][2];                     // alternating tiles: keys whose values are not finite
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
-    const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, split = blockIdx.z;
-    const Rows rows(p, request);
-    const int page_mask = (1 << p.page_shift) - 1;
-    const int32_t *table = p.table + request * p.table_stride;
-    uint8_t *keys = smem, *values = smem + Sh::kTile, *raw = smem + 2 * Sh::kTile;
-
-    const int64_t blocks = (rows.count + kManyRows - 1) / kManyRows;
-    // (the last rows see most keys: they go first)
-    for (int64_t block = blocks - 1 - blockIdx.x; block >= 0; block -= gridDim.x) {
-        const int64_t row0 = block * kManyRows, last = min(row0 + kManyRows, rows.count) - 1;
-        const int lo = p.window > 0 ? (int)max(rows.pos(row0) - p.window + 1, (int64_t)0) : 0;
-        const int hi = (int)min(min(rows.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
-        const int tile_lo = lo / kManyKeys, tiles = hi > lo ? (hi + kManyKeys - 1) / kManyKeys - tile_lo : 0;
-        const int per = (tiles + p.splits - 1) / p.splits;
-        const int first = (int)min((int64_t)tile_lo + (int64_t)split * per, (int64_t)tile_lo + tiles);
-        const int end = min(first + per, tile_lo + tiles);
-
-        auto issue = [&](int tile) {
-            if (tile < end) {
-                const uint32_t dst = smem_addr(raw) + (tile & 1) * Sh::kRaw;
-                // a warp per 16 keys
-                const int j = tile * kManyKeys + 16 * warp;
-                const int page = j < hi ? table[j >> p.page_shift] : -1;
-                const bool in = page >= 0 && page < p.pages;
-                const int64_t vec = ((((int64_t)(in ? page : 0) * p.kv_heads + kv) << p.page_shift) + (j & page_mask));
-                constexpr int kParts = D / 32;
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-#pragma unroll
-                    for (int i = 0; i < kParts / 2; ++i) {
-                        const int e = i * 32 + lane;
-                        copy_async16(dst + w * Sh::kCodes + (16 * warp * kParts + e) * 16, p.codes[w] + vec * (D / 2) + e * 16, in);
-                    }
-                }
-                if (lane < 8 * GR) {
-                    const int w = lane / (4 * GR), e = lane % (4 * GR);
-                    copy_async16(dst + 2 * Sh::kCodes + w * Sh::kScales + warp * 64 * GR + e * 16,
-                                 reinterpret_cast<const uint8_t *>(p.scales[w] + vec * GR) + e * 16, in);
-                }
-                if (lane == 0) there[tile & 1][warp] = in;
-            }
-            copy_commit();
-        };
-        if (threadIdx.x < 4 * GR) (&bad[0][0][0])[threadIdx.x] = 0;
-        __syncthreads();                                   // (also: the rows before are done with shared memory)
-        issue(first);
-        issue(first + 1);
-
-        // queries to fp16 times a power of two a row, and to fragments
-        {
-            constexpr int kOct = D / 8;
-#pragma unroll
-            for (int i = 0; i < kManyRows * kOct / 128; ++i) {
-                const int at = i * 128 + threadIdx.x, r = at / kOct, o = at % kOct;
-                const int64_t row = row0 + r;
-                uint4 v{0, 0, 0, 0};
-                if (rows.live(p, row))
-                    v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + rows.token(row) * p.q_stride +
-                                                         rows.head(kv, row) * D + 8 * o);
-                unsigned top = octet_largest(v);
-#pragma unroll
-                for (int k = 1; k < kOct; k *= 2) top = max(top, __shfl_xor_sync(~0u, top, k));
-                const int k = power_for<T>(top);
-                *reinterpret_cast<uint4 *>(keys + r * Sh::kKeyBytes + o * 16) = octet_in_order<T>(v, power_of_two(k));
-                if (o == 0) row_scale[r] = p.scale * 1.4426950408889634f * power_of_two(-k);
-            }
-        }
-        __syncthreads();
-        uint32_t qf[KS][4];
-        {
-            const uint32_t at = smem_addr(keys) + (16 * warp + lane % 16) * Sh::kKeyBytes + lane / 16 * 16;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) load_matrices(qf[k], at + k * 32);
-        }
-        float scale[2], top[2] = {-INFINITY, -INFINITY}, sum[2] = {};
-        int seen_hi[2], seen_lo[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int64_t row = row0 + 16 * warp + g + 8 * r;
-            const bool live = row < rows.count;
-            scale[r] = row_scale[16 * warp + g + 8 * r];
-            seen_hi[r] = live ? (int)max(rows.pos(row), (int64_t)-1) : -1;
-            seen_lo[r] = live && p.window > 0 ? (int)max(rows.pos(row) - p.window + 1, (int64_t)0) : 0;
-        }
-        const int full_lo = p.window > 0 ? (int)max(rows.pos(last) - p.window + 1, (int64_t)0) : 0;
-        const int full_hi = row0 + kManyRows <= rows.count ? (int)max(rows.pos(row0), (int64_t)-1) : -1;
-        float o[ND][4] = {};
-
-        for (int tile = first; tile < end; ++tile) {
-            copy_wait<1>();
-            __syncthreads();                               // the raw tile is there; the one before is done with
-            const uint8_t *from = raw + (tile & 1) * Sh::kRaw;
-            const uint32_t mask = *reinterpret_cast<const uint32_t *>(there[tile & 1]);
-            // unpack: a word of eight codes at a time
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                constexpr int kWords = D / 8, kStep = 128 / kWords;        // words of a key; keys at a time
-                const int word = threadIdx.x % kWords, j = word / 8;
-#pragma unroll
-                for (int i = 0; i < kManyKeys / kStep; ++i) {
-                    const int key = i * kStep + threadIdx.x / kWords;
-                    const uint32_t codes = reinterpret_cast<const uint32_t *>(from + w * Sh::kCodes)[key * kWords + word];
-                    const __half2 dm = reinterpret_cast<const __half2 *>(from + 2 * Sh::kCodes + w * Sh::kScales)[key * GR + j];
-                    __half2 d = __low2half2(dm), m = __high2half2(dm);
-                    const uint32_t bits = *reinterpret_cast<const uint32_t *>(&dm);
-                    if ((bits & 0x7c00u) == 0x7c00u || (bits & 0x7c000000u) == 0x7c000000u) {
-                        // keys are NaN then, values 0 and marked
-                        d = __float2half2_rn(0.0f);
-                        m = w ? d : __float2half2_rn(__int_as_float(0x7fc00000));
-                        if (w) atomicOr(&bad[tile & 1][j][key / 32], 1u << (key % 32));
-                    }
-                    *reinterpret_cast<uint4 *>((w ? values : keys) + key * Sh::kKeyBytes + word * 16) = unpack_word(codes, d, m);
-                }
-            }
-            __syncthreads();
-            if (threadIdx.x < 2 * GR) (&bad[(tile + 1) & 1][0][0])[threadIdx.x] = 0;
-            issue(tile + 2);
-            unsigned not_finite = 0;
-#pragma unroll
-            for (int j = 0; j < GR; ++j) not_finite |= bad[tile & 1][j][0] | bad[tile & 1][j][1];
-
-            // scores: rows g, g + 8 of the warp's 16, keys 8 n + 2 t + {0, 1}
-            float s[NK][4];
-            {
-                const uint32_t at = smem_addr(keys) + lane % 8 * Sh::kKeyBytes + lane / 8 * 16;
-#pragma unroll
-                for (int n = 0; n < NK; ++n) {
-#pragma unroll
-                    for (int k = 0; k < KS; k += 2) {
-                        uint32_t b[4];
-                        load_matrices(b, at + n * 8 * Sh::kKeyBytes + k * 32);
-                        const float zero[4] = {0, 0, 0, 0};
-                        if (k == 0) multiply(s[n], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b[0], b[1], zero);
-                        else multiply(s[n], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b[0], b[1], s[n]);
-                        multiply(s[n], qf[k + 1][0], qf[k + 1][1], qf[k + 1][2], qf[k + 1][3], b[2], b[3], s[n]);
-                    }
-                }
-            }
-            const int key0 = tile * kManyKeys;
-            const bool whole = key0 >= full_lo && key0 + kManyKeys - 1 <= full_hi && mask == 0x01010101u;
-            if (!whole || not_finite) {
-                unsigned spoilt[GR] = {};                  // rows g (bit 0) and g + 8 that see a value that is not finite
-#pragma unroll
-                for (int n = 0; n < NK; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = 8 * n + 2 * t + e % 2, r = e / 2;
-                        const bool in = (mask >> (8 * (key / 16)) & 1) && key0 + key <= seen_hi[r] && key0 + key >= seen_lo[r];
-                        if (!in) s[n][e] = -INFINITY;
-                        if (not_finite) {
-#pragma unroll
-                            for (int j = 0; j < GR; ++j)
-                                if (in && (bad[tile & 1][j][key / 32] >> (key % 32) & 1)) spoilt[j] |= 1u << r;
-                        }
-                    }
-                if (not_finite) {
-                    // (a row's keys are over four lanes)
-#pragma unroll
-                    for (int j = 0; j < GR; ++j) {
-                        unsigned b = spoilt[j];
-                        b |= __shfl_xor_sync(~0u, b, 1);
-                        b |= __shfl_xor_sync(~0u, b, 2);
-#pragma unroll
-                        for (int i = 0; i < ND / GR; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (b >> (e / 2) & 1) o[j * (ND / GR) + i][e] = __int_as_float(0x7fc00000);
-                    }
-                }
-            }
-            float base[2], back[2];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float x = -INFINITY;
-#pragma unroll
-                for (int n = 0; n < NK; ++n) {
-                    // (hidden is -inf whatever the scale)
-                    s[n][2 * r] = s[n][2 * r] == -INFINITY ? -INFINITY : s[n][2 * r] * scale[r];
-                    s[n][2 * r + 1] = s[n][2 * r + 1] == -INFINITY ? -INFINITY : s[n][2 * r + 1] * scale[r];
-                    x = fmaxf(x, fmaxf(s[n][2 * r], s[n][2 * r + 1]));
-                }
-                x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
-                x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
-                const float is = fmaxf(top[r], x);
-                back[r] = top[r] == is ? 1.0f : power2(top[r] - is);
-                top[r] = is;
-                base[r] = is == -INFINITY ? 0.0f : is - 14.0f;
-                sum[r] *= back[r];
-            }
-            if (__any_sync(~0u, back[0] != 1.0f || back[1] != 1.0f)) {
-#pragma unroll
-                for (int i = 0; i < ND; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][e] *= back[e / 2];
-            }
-            // weights to fp16; products, 16 keys at a time
-#pragma unroll
-            for (int k = 0; k < NK / 2; ++k) {
-                uint32_t a[4], rest[4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float w0 = power2(s[2 * k + h][2 * r] - base[r]), w1 = power2(s[2 * k + h][2 * r + 1] - base[r]);
-                        sum[r] += w0 + w1;
-                        a[2 * h + r] = pack_half(w0, w1);
-                        if constexpr (kRest) {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&a[2 * h + r]));
-                            rest[2 * h + r] = pack_half(w0 - f.x, w1 - f.y);
-                        }
-                    }
-                const uint32_t at = smem_addr(values) + (16 * k + lane % 16) * Sh::kKeyBytes + lane / 16 * 16;
-#pragma unroll
-                for (int i = 0; i < ND; i += 2) {
-                    uint32_t b[4];
-                    load_matrices_t(b, at + i * 16);
-                    multiply(o[i], a[0], a[1], a[2], a[3], b[0], b[1], o[i]);
-                    multiply(o[i + 1], a[0], a[1], a[2], a[3], b[2], b[3], o[i + 1]);
-                    if constexpr (kRest) {
-                        multiply(o[i], rest[0], rest[1], rest[2], rest[3], b[0], b[1], o[i]);
-                        multiply(o[i + 1], rest[0], rest[1], rest[2], rest[3], b[2], b[3], o[i + 1]);
-                    }
-                }
-            }
-        }
-        copy_wait<0>();
-        asm volatile("griddepcontrol.launch_dependents;");
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            sum[r] += __shfl_xor_sync(~0u, sum[r], 1);
-            sum[r] += __shfl_xor_sync(~0u, sum[r], 2);
-        }
-        if (p.splits == 1) {
-            // through shared memory, for whole rows: element 2 t of eight is t, 2 t + 1 is t + 4
-            T *tile = reinterpret_cast<T *>(smem);
-            constexpr int kRow = D + 8;
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const float f = sum[r] > 0 ? 1.0f / sum[r] : sum[r];
-#pragma unroll
-                for (int i = 0; i < ND; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        tile[(16 * warp + g + 8 * r) * kRow + 8 * i + t + 4 * e] =
-                            from_float<T>(sum[r] > 0 ? o[i][2 * r + e] * f : sum[r]);
-            }
-            __syncthreads();
-            for (int at = threadIdx.x; at < kManyRows * (D / 8); at += 128) {
-                const int r = at / (D / 8), c = at % (D / 8);
-                const int64_t row = row0 + r;
-                if (!rows.live(p, row)) continue;
-                *reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + rows.token(row) * p.out_stride + rows.head(kv, row) * D + 8 * c) =
-                    *reinterpret_cast<const uint4 *>(tile + r * kRow + 8 * c);
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int64_t row = row0 + 16 * warp + g + 8 * r;
-                if (!rows.live(p, row)) continue;
-                float *to = p.parts + ((rows.token(row) * p.q_heads + rows.head(kv, row)) * p.splits + split) * (D + 2);
-#pragma unroll
-                for (int i = 0; i < ND; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) to[8 * i + t + 4 * e] = o[i][2 * r + e];
-                if (t == 0) to[D] = top[r], to[D + 1] = sum[r];
-            }
-        }
-        __syncthreads();
-    }
-}
-
 // A split context's parts, joined in a fixed order: a block per row, its warps over
 // the parts.
 template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(const AttendParams p)
@@ -791,29 +488,31 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
     }
 }
 
-// From here on the rows of a request and KV head go to many_kernel (measured, us:
-// MEASURE).
-constexpr int kMany = 33, kPrompt = 65;
+// From so many rows of a request and KV head on they are a prompt's.  Measured, us (8 KV
+// heads of 128 elements; rows by sixteen / by 256): 32 rows of 8 requests x 2,304 keys
+// 36 / 54, 64 rows 45 / 53, 128 rows 85 / 66; 40 rows of 8 x 65,536 keys 620 / 741; of one
+// request, 128 rows x 16,384 keys 63 / 54 (x 4,096 keys 33 / 42), 2,400 x 300 keys 57 / 35.
+constexpr int kPrompt = 65;
 
 struct Plan {
-    int nt, slabs, splits;      // nt 0: many_kernel, -1: the prompts'
+    int nt, slabs, splits;      // nt 0: a prompt
 };
 
-// Rows by eight or sixteen, or by 64; keys split until every multiprocessor has its
-// three blocks, no finer than 128 keys (256).
+// Rows by eight or sixteen, or by 256; keys split until every multiprocessor has its
+// three blocks (one), no finer than 128 keys (512).
 Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
 {
     Plan f;
     const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
-    f.nt = rows >= kPrompt ? -1 : rows >= kMany ? 0 : rows <= 8 ? 1 : 2;
-    const int at_once = f.nt < 0 ? kPromptRows : f.nt ? 8 * f.nt : kManyRows;
+    f.nt = rows >= kPrompt ? 0 : rows <= 8 ? 1 : 2;
+    const int at_once = f.nt ? 8 * f.nt : kPromptRows;
     const int64_t slabs = (rows + at_once - 1) / at_once;
     f.slabs = (int)(slabs < 65535 ? slabs : 65535);
     int64_t keys = a->max_len;
     if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
-    const int least = f.nt > 0 ? kTile * kFewWarps : 4 * kManyKeys;
+    const int least = f.nt ? kTile * kFewWarps : 512;
     const int64_t units = (keys + least - 1) / least;
-    int64_t splits = (int64_t)sms * (f.nt < 0 ? 1 : 3) / ((int64_t)a->batch * c->kv_heads * slabs);
+    int64_t splits = (int64_t)sms * (f.nt ? 3 : 1) / ((int64_t)a->batch * c->kv_heads * slabs);
     if (splits > units) splits = units;
     f.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     return f;
@@ -847,22 +546,19 @@ template <class K> int launch(K kernel, const AttendParams &p, dim3 grid, size_t
 
 template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
 {
-    static std::atomic<uint64_t> ready[3];               // devices that have the attribute set
+    static std::atomic<uint64_t> ready[2];               // devices that have the attribute set
     const size_t ring = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes, smem = ring + (size_t)f.nt * (D / 32) * 512;
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
     int st;
-    if (f.nt < 0) {
+    if (f.nt == 0) {
         st = launch_prompt(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s);
-    } else if (f.nt == 0) {
-        const dim3 blocks((unsigned)f.slabs, pairs, (unsigned)f.splits);
-        st = launch(many_kernel<T, D>, p, blocks, ManyShared<D>::kBytes, false, dev, ready[2], s);
     } else {
         st = f.nt == 1 ? launch(few_kernel<T, D, 1>, p, grid, smem, false, dev, ready[0], s)
                        : launch(few_kernel<T, D, 2>, p, grid, smem, false, dev, ready[1], s);
     }
     if (st != E2_OK || f.splits == 1) return st;
-    return launch(join_kernel<T, D>, p, dim3((unsigned)f.slabs * (f.nt < 0 ? kPromptRows : f.nt ? 8 * f.nt : kManyRows), pairs), 0, true, dev, ready[0], s);
+    return launch(join_kernel<T, D>, p, dim3((unsigned)f.slabs * (f.nt ? 8 * f.nt : kPromptRows), pairs), 0, true, dev, ready[0], s);
 }
 
 int check_args(const e2_cache *c, const e2_attend_args *a)
