@@ -4,9 +4,8 @@
 namespace e2ops {
 namespace {
 
-// Blocks to have at least: 1.6 per multiprocessor keep the memory busy (one where 32
-// tokens leave room for two).
-constexpr int kFewBlocks = 250, kFewBlocks32 = 150;
+// Blocks to have at least: 1.6 per multiprocessor keep the memory busy.
+constexpr int kFewBlocks = 250;
 
 // Rows alone where they make enough blocks; else columns are split: in two by a
 // cluster, further among the four warps of a block first (no cluster to join), then by
@@ -15,32 +14,33 @@ constexpr int kFewBlocks = 250, kFewBlocks32 = 150;
 // 18.9, 1x1 28; 57344 x 8192 1x1 56, 1x2 57, 2x1 62; 1024 x 16384 4x4 8.5, 1x8 11.
 FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
 {
-    const int nt = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4, live = tokens < 8 * nt ? tokens : 8 * nt;
+    const int nt = tokens <= 8 ? 1 : 2;
     const int chunks = (cols + kChunk - 1) / kChunk, x_pad = chunks * kChunk;
     const int per = kChunk / group, stage = kRows * (kRowBytes + per * 2 * (mins ? 2 : 1));
-    const int slabs = (tokens + 8 * nt - 1) / (8 * nt), want = nt == 4 ? kFewBlocks32 : kFewBlocks;
     auto plan = [&](int wk, int split) {
         // all of x at once where that leaves room, else a stage of each warp at a time, two in turn
         const int mine = (chunks + split - 1) / split * kChunk;
-        const bool whole = (size_t)live * mine * 2 <= 25 * 1024;
+        const bool whole = (size_t)tokens * mine * 2 <= 25 * 1024;
         const int xc = whole ? mine : wk * kChunk;
         const size_t smem = (size_t)kWarps * ring_stages(nt) * stage +
-                            (whole ? 1 : 2) * ((size_t)live * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
-        return FewPlan{nt, wk, split, xc, x_pad, smem, slabs * slab_bytes(nt, x_pad, 32)};
+                            (whole ? 1 : 2) * ((size_t)tokens * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
+        return FewPlan{nt, wk, split, xc, x_pad, smem, prepared_bytes(nt, x_pad, 32)};
     };
     auto blocks = [&](int wk, int split) {
         const int rb = kRows * kWarps / wk;
-        return (int64_t)((rows + rb - 1) / rb) * split * slabs;
+        return (int64_t)((rows + rb - 1) / rb) * split;
     };
-    if (blocks(1, 1) >= want || chunks == 1) return plan(1, 1);
-    if (blocks(1, 2) >= want) return plan(1, 2);
+    if (blocks(1, 1) >= kFewBlocks || chunks == 1) return plan(1, 1);
+    if (blocks(1, 2) >= kFewBlocks) return plan(1, 2);
     int wk = kWarps, split = 1;
     while (wk > 1 && plan(wk, split).smem > (size_t)kSmemPerSm / 2 - 2048) wk /= 2;
-    while (split < 8 && blocks(wk, split) < want && wk * split * 2 <= chunks) split *= 2;
+    while (split < 8 && blocks(wk, split) < kFewBlocks && wk * split * 2 <= chunks) split *= 2;
     return plan(wk, split);
 }
 
-// From so many tokens on the block-wide products (measured: MEASURE).
+// From so many tokens on x is a tile of its own for the block-wide products.  Measured at 17
+// tokens, us (by eights / as a tile): 8192 x 28672 81 / 67, 57344 x 8192 gated 133 / 124,
+// 4096 x 4096 12.5 / 11.
 constexpr int kMany = 17;
 
 }  // namespace
@@ -99,9 +99,7 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
     const int wide = w->group == 128 ? 8 : 16, groups = w->cols / w->group;
     auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(w->scales, to) && aligned(w->mins, to); };
     const int by = w->cols % kChunk == 0 && all_aligned(wide) ? wide : all_aligned(4) ? 4 : 2;
-    FewParams q{p, outs, f.wk, f.split, f.x_cols,
-                by,
-                static_cast<const uint8_t *>(workspace), f.x_pad};
+    FewParams q{p, outs, f.wk, f.split, f.x_cols, by, static_cast<const uint8_t *>(workspace), f.x_pad};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return w->group == 32   ? launch_few_32(q, f, dev.id, s)
            : w->group == 64 ? launch_few_64(q, f, dev.id, s)

@@ -50,9 +50,8 @@ struct FewPlan {
     size_t smem, workspace;
 };
 
-// Stages of a warp's ring and resident blocks: what shared memory and registers hold.
+// Stages of a warp's ring: what shared memory holds of three blocks.
 __host__ __device__ constexpr int ring_stages(int nt) { return nt == 1 ? 3 : 2; }
-__host__ __device__ constexpr int most_resident(int nt) { return nt == 4 ? 2 : 3; }
 
 template <int G, bool MINS> struct Stage {
     static constexpr int kPer = kChunk / G;                                 // scales of a row
@@ -63,8 +62,8 @@ template <int G, bool MINS> struct Stage {
 struct FewParams {
     MatmulParams m;
     int outs, wk, split, x_cols, scales_by;     // scales copied by 16 or 8 bytes, by 4, or one by one (2)
-    // x as prepared, per 8 NT tokens: fp16 octets [token][x_pad], the groups'
-    // sums [x_pad / group][8 NT], and 2^24 / the token's power of two
+    // x as prepared: fp16 octets [8 NT tokens][x_pad], the groups' sums
+    // [x_pad / group][8 NT], and 1 / the token's power of two
     const uint8_t *prepared;
     int x_pad;
 };
@@ -86,8 +85,8 @@ __device__ __forceinline__ void finish(const MatmulParams &p, int token, int row
     else finish_as<__nv_bfloat16>(p, token, row, a, b);
 }
 
-// Bytes of a prepared slab of 8 nt tokens.
-__host__ __device__ constexpr size_t slab_bytes(int nt, int x_pad, int group)
+// Bytes of 8 nt prepared tokens.
+__host__ __device__ constexpr size_t prepared_bytes(int nt, int x_pad, int group)
 {
     return (size_t)8 * nt * x_pad * 2 + (size_t)x_pad / group * 8 * nt * 4 + 256;
 }
@@ -101,7 +100,7 @@ template <class T, int G, bool MINS> __global__ void __launch_bounds__(512) prep
     __shared__ unsigned largest;
     asm volatile("griddepcontrol.launch_dependents;");
     const MatmulParams &p = q.m;
-    const int tok = blockIdx.x, col = tok % (8 * nt), octets = q.x_pad / 8;
+    const int tok = blockIdx.x, octets = q.x_pad / 8;
     if (threadIdx.x == 0) largest = 0;
     __syncthreads();
     const T *x = static_cast<const T *>(p.x) + tok * p.x_stride;
@@ -112,9 +111,8 @@ template <class T, int G, bool MINS> __global__ void __launch_bounds__(512) prep
     __syncthreads();
     const int k = power_for<T>(largest);
     const float f = power_of_two(k);
-    uint8_t *slab = to + tok / (8 * nt) * slab_bytes(nt, q.x_pad, G);
-    uint4 *out = reinterpret_cast<uint4 *>(slab) + (size_t)col * octets;
-    float *sums = reinterpret_cast<float *>(slab + (size_t)8 * nt * q.x_pad * 2);
+    uint4 *out = reinterpret_cast<uint4 *>(to) + (size_t)tok * octets;
+    float *sums = reinterpret_cast<float *>(to + (size_t)8 * nt * q.x_pad * 2);
     // (x_pad is a multiple of 512 columns: whole warps)
     for (int o = threadIdx.x; o < octets; o += blockDim.x) {
         uint4 v{0, 0, 0, 0};
@@ -123,13 +121,13 @@ template <class T, int G, bool MINS> __global__ void __launch_bounds__(512) prep
         out[o] = octet_convert<T>(v, f, sum);
 #pragma unroll
         for (int d = 1; d < G / 8; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
-        if (o % (G / 8) == 0) sums[o / (G / 8) * (8 * nt) + col] = group_sum<MINS>(sum);
+        if (o % (G / 8) == 0) sums[o / (G / 8) * (8 * nt) + tok] = group_sum<MINS>(sum);
     }
-    if (threadIdx.x == 0) sums[(size_t)q.x_pad / G * 8 * nt + col] = power_of_two(-k);
+    if (threadIdx.x == 0) sums[(size_t)q.x_pad / G * 8 * nt + tok] = power_of_two(-k);
 }
 
 template <int G, bool MINS, int NT>
-__global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(const FewParams q)
+__global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
 {
     using St = Stage<G, MINS>;
     constexpr int kPer = St::kPer, kStages = ring_stages(NT);
@@ -137,7 +135,7 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float unscale[8 * NT];                              // 1 / the token's power of two
     const MatmulParams &p = q.m;
-    const int t0 = blockIdx.y * 8 * NT, nt = min(8 * NT, p.tokens - t0);
+    const int nt = p.tokens;
     uint8_t *ring = smem;
     // x (one segment, or two in turn), and the groups' sums [x_cols / G][8 NT] of each
     const int sum_bytes = q.x_cols / G * 8 * NT * 4, seg_bytes = sum_bytes + nt * x_row_bytes(q.x_cols);
@@ -212,15 +210,14 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
 
     // a prepared segment on its way to shared memory
     auto issue_x = [&](int seg, int buffer) {
-        const uint8_t *slab = q.prepared + blockIdx.y * slab_bytes(NT, q.x_pad, G);
         const uint32_t dst = smem_addr(xseg) + buffer * seg_bytes;
         const int live = min(q.x_cols, q.x_pad - seg * kChunk), per_row = live / 8;
-        const uint8_t *sums = slab + (size_t)8 * NT * q.x_pad * 2 + (size_t)seg * kPer * 8 * NT * 4;
+        const uint8_t *sums = q.prepared + (size_t)8 * NT * q.x_pad * 2 + (size_t)seg * kPer * 8 * NT * 4;
         for (int i = threadIdx.x; i < live / G * 2 * NT; i += 32 * kWarps) copy_async16(dst + i * 16, sums + i * 16, true);
         for (int tok = warp; tok < nt; tok += kWarps)
             for (int o = lane; o < per_row; o += 32)
                 copy_async16(dst + sum_bytes + tok * x_row_bytes(q.x_cols) + o * 16,
-                             slab + ((size_t)tok * q.x_pad + seg * kChunk + o * 8) * 2, true);
+                             q.prepared + ((size_t)tok * q.x_pad + seg * kChunk + o * 8) * 2, true);
     };
 
     float y[NT][4] = {};
@@ -232,7 +229,7 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
     copy_commit();
     if (threadIdx.x < nt)
         unscale[threadIdx.x] = reinterpret_cast<const float *>(
-            q.prepared + blockIdx.y * slab_bytes(NT, q.x_pad, G) + (size_t)8 * NT * q.x_pad * 2)[(size_t)q.x_pad / G * 8 * NT + threadIdx.x];
+            q.prepared + (size_t)8 * NT * q.x_pad * 2)[(size_t)q.x_pad / G * 8 * NT + threadIdx.x];
 
     int flip = 0;
     for (int seg = c0; seg < c1; seg += q.x_cols / kChunk, flip ^= 1) {
@@ -342,7 +339,7 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
                 // rows g and g + 8: two outputs, or what gates and what is gated
                 const int tok = 8 * n + 2 * t + e % 2, r = first + g + (p.gated ? 0 : 8 * (e / 2));
                 if (tok >= nt || r >= q.outs || (p.gated && e >= 2)) continue;
-                finish(p, t0 + tok, r, y[n][e], y[n][e | 2]);
+                finish(p, tok, r, y[n][e], y[n][e | 2]);
             }
         return;
     }
@@ -379,9 +376,9 @@ __global__ void __launch_bounds__(32 * kWarps, most_resident(NT)) few_kernel(con
         if (tok >= nt || out0 + r >= q.outs) continue;
         if (p.gated) {
             const int at = (r / 8 * 16 + r % 8) * (8 * NT) + tok;
-            finish(p, t0 + tok, out0 + r, joined(at), joined(at + 8 * 8 * NT));
+            finish(p, tok, out0 + r, joined(at), joined(at + 8 * 8 * NT));
         } else {
-            finish(p, t0 + tok, out0 + r, joined(r * (8 * NT) + tok), 0.0f);
+            finish(p, tok, out0 + r, joined(r * (8 * NT) + tok), 0.0f);
         }
     }
     if (q.split > 1) cluster_barrier();                            // (peers may still read)
@@ -402,7 +399,7 @@ template <int G, bool MINS, int NT> int launch_few(const FewParams &q, const Few
     const int rb = (q.m.gated ? 8 : 16) * (kWarps / q.wk);
     cudaLaunchAttribute at[2]{};
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((q.outs + rb - 1) / rb * f.split), (unsigned)((q.m.tokens + 8 * NT - 1) / (8 * NT)));
+    cfg.gridDim = dim3((unsigned)((q.outs + rb - 1) / rb * f.split));
     cfg.blockDim = dim3(32 * kWarps);
     cfg.dynamicSmemBytes = f.smem;
     cfg.stream = s;
@@ -420,12 +417,8 @@ template <int G, bool MINS, int NT> int launch_few(const FewParams &q, const Few
 template <int G> int launch_few_group(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)
 {
     if (q.m.mins)
-        return f.nt == 1   ? launch_few<G, true, 1>(q, f, dev, s)
-               : f.nt == 2 ? launch_few<G, true, 2>(q, f, dev, s)
-                           : launch_few<G, true, 4>(q, f, dev, s);
-    return f.nt == 1   ? launch_few<G, false, 1>(q, f, dev, s)
-           : f.nt == 2 ? launch_few<G, false, 2>(q, f, dev, s)
-                       : launch_few<G, false, 4>(q, f, dev, s);
+        return f.nt == 1 ? launch_few<G, true, 1>(q, f, dev, s) : launch_few<G, true, 2>(q, f, dev, s);
+    return f.nt == 1 ? launch_few<G, false, 1>(q, f, dev, s) : launch_few<G, false, 2>(q, f, dev, s);
 }
 
 // The launch of a prompt (quant_matmul_many.cu).
