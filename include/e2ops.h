@@ -55,8 +55,11 @@ typedef struct {
  * gated != 0: rows = 2 F, the first F rows gate the others, y [tokens][F]:
  * y[t][f] = a / (1 + exp(-a)) * b (+ residual), a from row f, b from row F + f.
  * x, residual (or NULL) and y are fp16 or bf16 (dtype); x 16-byte aligned, its
- * row stride a multiple of 8.  Sums are in 32 bits, y is rounded once.  y may
- * not overlap x or the weights; it may be residual itself.
+ * row stride a multiple of 8.  Sums are in 32 bits, y is rounded once; x goes to
+ * the tensor cores as fp16 times a power of two per token (values below 2^-24 of the
+ * token's largest lose bits).  From 17 tokens on W does too, rounded once to fp16
+ * (2^-12 of a weight; what passes 65,504 stays there).  y may not overlap x or
+ * the weights; it may be residual itself.
  * workspace: e2_quant_matmul_workspace() bytes (0: may be NULL), 256-byte
  * aligned, contents of no consequence. */
 typedef struct {

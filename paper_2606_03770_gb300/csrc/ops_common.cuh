@@ -34,6 +34,36 @@ template <> __device__ __forceinline__ float from_float<float>(float x) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+// A kernel launched `early` is placed once all blocks of the one before it in its stream have
+// called allow_next (or are gone); wait_before returns when that one is done and what it wrote
+// can be seen.
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;"); }
+
+// Launches a kernel in clusters of `cluster` blocks.
+template <class P>
+int launch(void (*kernel)(P), dim3 grid, int threads, size_t smem, int cluster, bool early, cudaStream_t s, const P &p)
+{
+    cudaLaunchAttribute at[2]{};
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    if (early) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        at[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+        at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
+}
+
 // Eight 16-bit elements as they lie in memory, in 32 bits.
 template <class T> __device__ __forceinline__ void unpack8(const uint4 &w, float (&x)[8])
 {

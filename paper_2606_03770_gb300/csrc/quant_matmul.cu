@@ -7,6 +7,13 @@ namespace {
 // Blocks to have at least: 1.6 per multiprocessor keep the memory busy.
 constexpr int kFewBlocks = 250;
 
+// So few elements of x a block prepares for itself: one launch and no workspace, where weights
+// are read in less time than that costs the caller.  Measured, us a call (a graph's; by
+// blocks / by a kernel before): 4096 x 4096, 1 token 13.6 / 17.2 (6.4 / 5.9), 1001 x 1376, 5
+// tokens 14.3 / 19.7 (7.4 / 6.0); 57344 x 8192, 1 token (50 / 48).
+constexpr size_t kOwn = kOwnOctets * 32 * kWarps * 8;
+constexpr int64_t kOwnWeights = 1 << 27;
+
 // Rows alone where they make enough blocks; else columns are split: in two by a
 // cluster, further among the four warps of a block first (no cluster to join), then by
 // clusters of up to eight.  Measured, us (one token, 64 columns a group; joined by warps x
@@ -24,7 +31,8 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
         const int xc = whole ? mine : wk * kChunk;
         const size_t smem = (size_t)kWarps * ring_stages(nt) * stage +
                             (whole ? 1 : 2) * ((size_t)tokens * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
-        return FewPlan{nt, wk, split, xc, x_pad, smem, prepared_bytes(nt, x_pad, 32)};
+        const bool own = (size_t)tokens * mine <= kOwn && (int64_t)rows * cols <= kOwnWeights;
+        return FewPlan{nt, wk, split, xc, x_pad, smem, own ? 0 : prepared_bytes(nt, x_pad, 32)};
     };
     auto blocks = [&](int wk, int split) {
         const int rb = kRows * kWarps / wk;
@@ -53,7 +61,13 @@ extern "C" size_t e2_quant_matmul_workspace(int32_t rows, int32_t cols, int32_t 
     Device dev;
     if (rows < 1 || cols < 1 || cols > E2_MAX_COLS || tokens < 1 || current_device(&dev)) return 0;
     // the larger of what groups of any size, with and without gates, need
-    if (tokens < kMany) return plan_few(rows, cols, tokens, 32, true).workspace;
+    size_t few = 0;
+    for (int group = 32; tokens < kMany && group <= 128; group *= 2)
+        for (int mins = 0; mins < 2; ++mins) {
+            const size_t one = plan_few(rows, cols, tokens, group, mins).workspace;
+            few = one > few ? one : few;
+        }
+    if (tokens < kMany) return few;
     const size_t plain = plan_many(rows, false, cols, tokens, dev.sms).workspace;
     const size_t gated = rows % 2 ? 0 : plan_many(rows / 2, true, cols, tokens, dev.sms).workspace;
     return plain > gated ? plain : gated;
@@ -99,7 +113,7 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
     const int wide = w->group == 128 ? 8 : 16, groups = w->cols / w->group;
     auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(w->scales, to) && aligned(w->mins, to); };
     const int by = w->cols % kChunk == 0 && all_aligned(wide) ? wide : all_aligned(4) ? 4 : 2;
-    FewParams q{p, outs, f.wk, f.split, f.x_cols, by, static_cast<const uint8_t *>(workspace), f.x_pad};
+    FewParams q{p, outs, f.wk, f.split, f.x_cols, by, f.workspace ? static_cast<uint8_t *>(workspace) : nullptr, f.x_pad};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return w->group == 32   ? launch_few_32(q, f, dev.id, s)
            : w->group == 64 ? launch_few_64(q, f, dev.id, s)

@@ -42,6 +42,8 @@ constexpr int kChunk = 512;                  // columns of a stage
 constexpr int kRowBytes = kChunk / 2 + 16;   // (a stage's rows 16 bytes apart in banks)
 constexpr int kWarps = 4;
 
+constexpr int kOwnOctets = 8;                // octets of x that a thread prepares of its own block's
+
 constexpr int kSmemPerSm = 227 * 1024;
 
 // The launch of `tokens` tokens: how the columns are split.
@@ -63,8 +65,8 @@ struct FewParams {
     MatmulParams m;
     int outs, wk, split, x_cols, scales_by;     // scales copied by 16 or 8 bytes, by 4, or one by one (2)
     // x as prepared: fp16 octets [8 NT tokens][x_pad], the groups' sums
-    // [x_pad / group][8 NT], and 1 / the token's power of two
-    const uint8_t *prepared;
+    // [x_pad / group][8 NT], and 1 / the token's power of two (null: blocks make it themselves)
+    uint8_t *prepared;
     int x_pad;
 };
 
@@ -95,10 +97,12 @@ __host__ __device__ constexpr size_t prepared_bytes(int nt, int x_pad, int group
 template <bool MINS> __device__ __forceinline__ float group_sum(float sum) { return MINS ? sum * 0x1p-24f : sum * -0x1p-21f; }
 
 // x prepared once for all blocks: a block per token.
-template <class T, int G, bool MINS> __global__ void __launch_bounds__(512) prepare_kernel(const FewParams q, uint8_t *to, int nt)
+template <class T, int G, bool MINS, int NT> __global__ void __launch_bounds__(512) prepare_kernel(const FewParams q)
 {
+    constexpr int nt = NT;
+    uint8_t *to = q.prepared;
     __shared__ unsigned largest;
-    asm volatile("griddepcontrol.launch_dependents;");
+    allow_next();
     const MatmulParams &p = q.m;
     const int tok = blockIdx.x, octets = q.x_pad / 8;
     if (threadIdx.x == 0) largest = 0;
@@ -134,6 +138,7 @@ __global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
     const int WK = q.wk, RB = kRows * (kWarps / WK);
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float unscale[8 * NT];                              // 1 / the token's power of two
+    __shared__ unsigned largest[8 * NT];
     const MatmulParams &p = q.m;
     const int nt = p.tokens;
     uint8_t *ring = smem;
@@ -208,6 +213,47 @@ __global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
         copy_commit();
     };
 
+    // this block's columns of x as prepare_kernel leaves them, with powers of two of their own
+    auto own_x = [&](auto type) {
+        using T = decltype(type);
+        float *sx = reinterpret_cast<float *>(xseg);
+        uint8_t *xs = reinterpret_cast<uint8_t *>(sx) + sum_bytes;
+        const int live = min(q.x_cols, q.x_pad - c0 * kChunk), per_row = live / 8;       // (whole warps: 64 octets a chunk)
+        uint4 v[kOwnOctets];
+        // octets [token][per_row] in turn
+        int tok = 0, o = threadIdx.x;
+        auto wrap = [&] {
+            for (; o >= per_row; o -= per_row) ++tok;
+        };
+        wrap();
+#pragma unroll
+        for (int j = 0; j < kOwnOctets; ++j, o += 32 * kWarps, wrap()) {
+            const int col = c0 * kChunk + o * 8;
+            v[j] = uint4{0, 0, 0, 0};
+            if (tok < nt && col < p.cols) v[j] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + tok * p.x_stride + col);
+        }
+        tok = 0, o = threadIdx.x, wrap();
+#pragma unroll
+        for (int j = 0; j < kOwnOctets; ++j, o += 32 * kWarps, wrap()) {
+            if (tok >= nt) break;
+            const unsigned m = __reduce_max_sync(~0u, octet_largest(v[j]));
+            if (lane == 0) atomicMax(&largest[tok], m);
+        }
+        __syncthreads();
+        tok = 0, o = threadIdx.x, wrap();
+#pragma unroll
+        for (int j = 0; j < kOwnOctets; ++j, o += 32 * kWarps, wrap()) {
+            if (tok >= nt) break;
+            float sum;
+            *reinterpret_cast<uint4 *>(xs + tok * x_row_bytes(q.x_cols) + o * 16) =
+                octet_convert<T>(v[j], power_of_two(power_for<T>(largest[tok])), sum);
+#pragma unroll
+            for (int d = 1; d < G / 8; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
+            if (o % (G / 8) == 0) sx[o / (G / 8) * (8 * NT) + tok] = group_sum<MINS>(sum);
+        }
+        if (threadIdx.x < nt) unscale[threadIdx.x] = power_of_two(-power_for<T>(largest[threadIdx.x]));
+    };
+
     // a prepared segment on its way to shared memory
     auto issue_x = [&](int seg, int buffer) {
         const uint32_t dst = smem_addr(xseg) + buffer * seg_bytes;
@@ -224,10 +270,17 @@ __global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
     int next = c0 + wk, slot = 0;                                  // the next chunk to fetch
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i, next += WK) issue(next, i);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    issue_x(c0, 0);
+    if (!q.prepared) {
+        if (threadIdx.x < 8 * NT) largest[threadIdx.x] = 0;
+        __syncthreads();
+        if (p.half) own_x(__half{});
+        else own_x(__nv_bfloat16{});
+    } else {
+        wait_before();
+        issue_x(c0, 0);
+    }
     copy_commit();
-    if (threadIdx.x < nt)
+    if (q.prepared && threadIdx.x < nt)
         unscale[threadIdx.x] = reinterpret_cast<const float *>(
             q.prepared + (size_t)8 * NT * q.x_pad * 2)[(size_t)q.x_pad / G * 8 * NT + threadIdx.x];
 
@@ -236,15 +289,16 @@ __global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
         float *sx = reinterpret_cast<float *>(xseg + flip * seg_bytes);
         uint8_t *xs = reinterpret_cast<uint8_t *>(sx) + sum_bytes;
         // (newer than the segment's copy: nothing of the first's, else a stage or more)
-        if (seg == c0) copy_wait<0>();
-        else copy_wait<1>();
+        if (seg != c0) copy_wait<1>();
+        else if (q.prepared) copy_wait<0>();
         __syncthreads();
         if (seg + q.x_cols / kChunk < c1) issue_x(seg + q.x_cols / kChunk, flip ^ 1);
         copy_commit();
         const int seg_end = min(seg + q.x_cols / kChunk, c1);
         for (int c = seg + wk; c < seg_end; c += WK) {
             // (the segment's first stage: the next segment's copy is newer too)
-            if (c == seg + wk) copy_wait<kStages - 1>();
+            if (c == seg + wk && !q.prepared) copy_wait<kStages>();
+            else if (c == seg + wk) copy_wait<kStages - 1>();
             else copy_wait<kStages - 2>();
             __syncwarp();
             issue(next, slot == 0 ? kStages - 1 : slot - 1);
@@ -393,25 +447,13 @@ template <int G, bool MINS, int NT> int launch_few(const FewParams &q, const Few
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    uint8_t *to = const_cast<uint8_t *>(q.prepared);
-    if (q.m.half) prepare_kernel<__half, G, MINS><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, to, NT);
-    else prepare_kernel<__nv_bfloat16, G, MINS><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, to, NT);
+    if (q.prepared) {
+        auto prepare = q.m.half ? prepare_kernel<__half, G, MINS, NT> : prepare_kernel<__nv_bfloat16, G, MINS, NT>;
+        if (int st = launch<FewParams>(prepare, dim3((unsigned)q.m.tokens), 512, 0, 1, false, s, q)) return st;
+    }
     const int rb = (q.m.gated ? 8 : 16) * (kWarps / q.wk);
-    cudaLaunchAttribute at[2]{};
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((q.outs + rb - 1) / rb * f.split));
-    cfg.blockDim = dim3(32 * kWarps);
-    cfg.dynamicSmemBytes = f.smem;
-    cfg.stream = s;
-    cfg.attrs = at;
-    // placed while x is prepared: fetches its first weights, then waits
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)f.split;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.numAttrs = f.split > 1 ? 2 : 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, q));
+    const unsigned blocks = (unsigned)((q.outs + rb - 1) / rb * f.split);
+    return launch<FewParams>(kernel, dim3(blocks), 32 * kWarps, f.smem, f.split, q.prepared != nullptr, s, q);
 }
 
 template <int G> int launch_few_group(const FewParams &q, const FewPlan &f, int dev, cudaStream_t s)

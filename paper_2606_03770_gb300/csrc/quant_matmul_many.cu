@@ -31,8 +31,8 @@ struct ManyParams {
     MatmulParams m;
     int outs, tile, tiles, split, stages, depth;             // tokens of a tile; stages in flight
     int scales_by;                                           // scales copied by a chunk's row, by 4 bytes, or one by one (2)
-    const uint8_t *prepared;                                 // [tiles][cols / 64][tile][128 bytes], then scales per token
-    const float *unscale;
+    uint8_t *prepared;                                 // [tiles][cols / 64][tile][128 bytes], then scales per token
+    float *unscale;
 };
 
 // A word's eight codes, less 8 where there are no minima, times d plus m.
@@ -53,10 +53,12 @@ template <bool MINS> __device__ __forceinline__ void scale_word(uint32_t *out, u
 }
 
 // x as the images of its stages: a block per token.
-template <class T> __global__ void __launch_bounds__(512) image_kernel(const ManyParams q, uint8_t *to, float *unscale)
+template <class T> __global__ void __launch_bounds__(512) image_kernel(const ManyParams q)
 {
     __shared__ unsigned largest;
-    asm volatile("griddepcontrol.launch_dependents;");
+    uint8_t *to = q.prepared;
+    float *unscale = q.unscale;
+    allow_next();
     const MatmulParams &p = q.m;
     const int tok = blockIdx.x, octets = q.stages * 8, row = tok % q.tile;
     if (threadIdx.x == 0) largest = 0;
@@ -120,7 +122,7 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
 
     if (warp == 0) {
         // x: a stage's image by one copy
-        asm volatile("griddepcontrol.wait;" ::: "memory");
+        wait_before();
         const uint8_t *from = q.prepared + ((size_t)blockIdx.y * q.stages + s0) * stage_bytes;
         int i = 0, slot = 0, phase = 1;
         for (; i < n; ++i) {
@@ -273,7 +275,7 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
     }
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");                  // (unscale comes from the kernel before, too)
+    wait_before();                  // (unscale comes from the kernel before, too)
     const bool bad = *reinterpret_cast<volatile int *>(&failed);
 
     // outputs: lanes are rows, columns tokens; the unpacking warps take them, four to 32 lanes.
@@ -345,28 +347,16 @@ template <int G, bool MINS> int launch_many_as(const ManyParams &q, const ManyPl
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    uint8_t *to = const_cast<uint8_t *>(q.prepared);
-    float *unscale = const_cast<float *>(q.unscale);
-    if (q.m.half) image_kernel<__half><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, to, unscale);
-    else image_kernel<__nv_bfloat16><<<(unsigned)q.m.tokens, 512, 0, s>>>(q, to, unscale);
+    if (int st = launch<ManyParams>(q.m.half ? image_kernel<__half> : image_kernel<__nv_bfloat16>,
+                                    dim3((unsigned)q.m.tokens), 512, 0, 1, false, s, q))
+        return st;
     const int rows_out = q.m.gated ? kTileRows / 2 : kTileRows;
-    cudaLaunchAttribute at[2]{};
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((q.outs + rows_out - 1) / rows_out * q.split), (unsigned)q.tiles);
-    cfg.blockDim = dim3(kThreads);
+    const dim3 grid((unsigned)((q.outs + rows_out - 1) / rows_out * q.split), (unsigned)q.tiles);
     // (never two blocks on a multiprocessor: tensor memory is for one)
     const size_t ring = (size_t)q.depth * q.tile * 128 + kRaw * Chunk<G, MINS>::kBytes + 1024;
     const size_t sums = q.split > 1 ? (size_t)q.tile * kTileRows * 4 + 1024 : q.m.gated ? (size_t)q.tile * kTileRows * 2 + 1024 : 0;
-    cfg.dynamicSmemBytes = std::max(std::max(ring, sums), (size_t)kSmemPerSm / 2);
-    cfg.stream = s;
-    cfg.attrs = at;
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)f.split;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.numAttrs = f.split > 1 ? 2 : 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, q));
+    const size_t smem = std::max(std::max(ring, sums), (size_t)kSmemPerSm / 2);
+    return launch<ManyParams>(kernel, grid, kThreads, smem, f.split, true, s, q);
 }
 
 template <int G> int launch_many_group(const ManyParams &q, const ManyPlan &f, int dev, cudaStream_t s)
@@ -405,8 +395,8 @@ ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms)
 
 int launch_many(const MatmulParams &m, const ManyPlan &f, void *workspace, int outs, int dev, cudaStream_t s)
 {
-    ManyParams q{m, outs, f.tile, f.tiles, f.split, f.stages, f.depth, 0, static_cast<const uint8_t *>(workspace),
-                 reinterpret_cast<const float *>(static_cast<const uint8_t *>(workspace) + f.image)};
+    ManyParams q{m, outs, f.tile, f.tiles, f.split, f.stages, f.depth, 0, static_cast<uint8_t *>(workspace),
+                 reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + f.image)};
     // how a chunk's rows of scales are aligned
     const int wide = kChunkColumns / m.group * 2, groups = m.cols / m.group;
     auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(m.scales, to) && aligned(m.mins, to); };
