@@ -103,7 +103,27 @@ struct Best {
         if (lane == place) v = x, id = at;
         else if (lane > place) v = pv, id = pid;
     }
+    // in the order of unsigned integers (either zero the same), 0: none
+    __device__ uint64_t key() const { return v > -INFINITY ? (uint64_t)ordered(v + 0.0f) << 32 | ~(unsigned)id : 0; }
+    __device__ void from(uint64_t k)
+    {
+        clear();
+        if (k) v = unordered((unsigned)(k >> 32)), id = (int)~(unsigned)k;
+    }
 };
+
+// The 32 largest of two lists, all falling over the lanes: the larger of each lane and its
+// mirror fall and rise once, which five exchanges sort.
+__device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane)
+{
+    a = max(a, __shfl_sync(~0u, b, 31 - lane));
+#pragma unroll
+    for (int j = 16; j; j /= 2) {
+        const uint64_t o = __shfl_xor_sync(~0u, a, j);
+        a = (lane & j) ? min(a, o) : max(a, o);
+    }
+    return a;
+}
 
 template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) logprob_kernel(const LogprobParams p)
 {
@@ -112,8 +132,7 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     __shared__ int any_bad[kMostWarps];
     __shared__ float floor_value;
     __shared__ float published[64];                               // lanes' maxima, the largest of each warp
-    __shared__ float list_v[kMostWarps][E2_MAX_TOP];
-    __shared__ int list_id[kMostWarps][E2_MAX_TOP];
+    __shared__ uint64_t list[TOP ? kMostWarps : 1][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
     const int rank = blockIdx.x % p.split, row = blockIdx.x / p.split;
     const T *x = static_cast<const T *>(p.logits) + row * p.stride;
@@ -260,7 +279,7 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
         a = merge(a, Sums{__shfl_xor_sync(~0u, a.m, k), __shfl_xor_sync(~0u, a.s, k), __shfl_xor_sync(~0u, a.u, k)});
     bad = __any_sync(~0u, bad);
     if (lane == 0) warp_sums[warp] = a, any_bad[warp] = bad;
-    if (TOP && lane < p.top) list_v[warp][lane] = best.v, list_id[warp][lane] = best.id;
+    if (TOP) list[warp][lane] = best.key();
     __syncthreads();
     // sums of `n` lanes, over the lanes
     auto join = [&](Sums mine, int n) {
@@ -270,18 +289,11 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
             mine = merge(mine, Sums{__shfl_xor_sync(~0u, mine.m, k), __shfl_xor_sync(~0u, mine.s, k), __shfl_xor_sync(~0u, mine.u, k)});
         return mine;
     };
-    // the lists of `n` others, all their elements at once, 32 at a time
-    auto join_lists = [&](int n, float least, auto fetch) {
-        for (int c = lane; c - lane < n * p.top; c += 32) {
-            float v = -INFINITY;
-            int id = 0x7fffffff;
-            if (c < n * p.top) fetch(c / p.top, c % p.top, v, id);
-            unsigned b = __ballot_sync(~0u, v >= least && v > -INFINITY);
-            while (b) {
-                const int from = __ffs(b) - 1;
-                b &= b - 1;
-                best.insert(__shfl_sync(~0u, v, from), __shfl_sync(~0u, id, from), lane);
-            }
+    // the first n lists (a power of two, as many warps at least), pair by pair into the first
+    auto join_lists = [&](int n) {
+        for (n /= 2; n; n /= 2) {
+            if (warp < n) list[warp][lane] = merge_lists(list[warp][lane], list[warp + n][lane], lane);
+            __syncthreads();
         }
     };
     Sums total{-INFINITY, 0.0f, 0.0f};
@@ -289,27 +301,26 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     if (warp == 0) {
         total = join(warp_sums[lane % warps], warps);
         spoilt = __any_sync(~0u, any_bad[lane % warps]);
-        // (its own bound holds for the block; equal ones count)
-        if (TOP)
-            join_lists(warps - 1, last, [&](int w, int j, float &v, int &id) { v = list_v[w + 1][j], id = list_id[w + 1][j]; });
     }
+    if (TOP) join_lists(warps);
     if (p.split > 1) {
-        if (warp == 0) {
-            __syncwarp();
-            if (lane == 0) warp_sums[0] = total, any_bad[0] = spoilt;
-            if (TOP && lane < p.top) list_v[0][lane] = best.v, list_id[0][lane] = best.id;
-        }
+        if (threadIdx.x == 0) warp_sums[0] = total, any_bad[0] = spoilt;
         cluster_barrier();
-        if (rank == 0 && warp == 0) {
-            const int r = lane % p.split;
-            const uint32_t at = peer_addr(smem_addr(&warp_sums[0]), r);
-            total = join(Sums{peer_load(at), peer_load(at + 4), peer_load(at + 8)}, p.split);
-            spoilt = __any_sync(~0u, __float_as_int(peer_load(peer_addr(smem_addr(&any_bad[0]), r))));
-            if (TOP)
-                join_lists(p.split - 1, __shfl_sync(~0u, best.v, p.top - 1), [&](int w, int j, float &v, int &id) {
-                    v = peer_load(peer_addr(smem_addr(&list_v[0][j]), w + 1));
-                    id = __float_as_int(peer_load(peer_addr(smem_addr(&list_id[0][j]), w + 1)));
-                });
+        if (rank == 0) {
+            // (clusters are of blocks with a warp for each)
+            if (TOP && warp < p.split) {
+                const uint32_t at = peer_addr(smem_addr(&list[0][lane]), warp);
+                const uint64_t low = __float_as_uint(peer_load(at)), high = __float_as_uint(peer_load(at + 4));
+                if (warp > 0) list[warp][lane] = high << 32 | low;
+            }
+            if (warp == 0) {
+                const int r = lane % p.split;
+                const uint32_t at = peer_addr(smem_addr(&warp_sums[0]), r);
+                total = join(Sums{peer_load(at), peer_load(at + 4), peer_load(at + 8)}, p.split);
+                spoilt = __any_sync(~0u, __float_as_int(peer_load(peer_addr(smem_addr(&any_bad[0]), r))));
+            }
+            __syncthreads();
+            if (TOP) join_lists(p.split);
         }
         cluster_barrier();                                        // (peers have been read)
     }
@@ -327,6 +338,7 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
         }
     }
     if (TOP && lane < p.top) {
+        best.from(list[0][lane]);
         const bool none = !(best.v > -INFINITY);
         p.values[(int64_t)row * p.top + lane] = spoilt ? nan : none ? -INFINITY : best.v - lse;
         p.ids[(int64_t)row * p.top + lane] = spoilt || none ? -1 : best.id;
@@ -340,17 +352,8 @@ template <class T> int launch_rows(LogprobParams p, int sms, cudaStream_t s)
     while (p.split < 8 && (int64_t)p.rows * p.split * 2 <= (int64_t)sms * 2 && p.vocab / p.split >= 8192) p.split *= 2;
     const int share = p.vocab / p.split;
     const int threads = share <= 2048 ? 128 : share <= 8192 ? 256 : kMostThreads;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)p.split;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)p.rows * p.split);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.stream = s;
-    cfg.attrs = &at;
-    cfg.numAttrs = p.split > 1 ? 1 : 0;
-    return cuda_status(p.top ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true>, p) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false>, p));
+    return launch<LogprobParams>(p.top ? logprob_kernel<T, true> : logprob_kernel<T, false>,
+                                 dim3((unsigned)p.rows * p.split), threads, 0, p.split, false, s, p);
 }
 
 }  // namespace
