@@ -18,6 +18,10 @@ namespace {
 // bound: the `top`-th largest of 64 lanes' maxima so far, the largest few of each warp of the
 // block, which `top` elements reach.  Warps publish theirs at rounds 0, 2, 8 and 32, and
 // the first warp draws the bound, from old ones too, which bound as well.
+// Measured, us, 128,256 logits (none / 5 / 20 alternatives): 8 rows of bf16 6.1 / 11 / 12, 1,152
+// rows of fp32 91 / 109 / 116 (94, 78 and 73% of the memory's rate), of bf16 74 / 100 / 113
+// (the issue of instructions, three quarters of all slots).  512 threads, three blocks on a
+// multiprocessor; 256 and five 110 / 114 / 118, 512 and two 99 / 121 / 131 (fp32).
 
 constexpr int kMostThreads = 512, kMostWarps = kMostThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f, kNegligible = -1e30f;
@@ -49,6 +53,13 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
 {
     float y;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+__device__ __forceinline__ float max_or_nan(float a, float b, float c)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
     return y;
 }
 
@@ -153,9 +164,7 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
 
     // eight elements of each lane, -inf where there are none; element j is index(j)
     auto take = [&](const float (&e)[8], auto index) {
-        float m = e[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) m = max_or_nan(m, e[j]);
+        const float m = max_or_nan(max_or_nan(e[0], e[1], e[2]), max_or_nan(e[3], e[4], e[5]), max_or_nan(e[6], e[7]));
         bad |= !(m < INFINITY);
         if (m > a.m) a = rebase(a, m);
         const float base = a.m == -INFINITY ? 0.0f : a.m;
