@@ -27,8 +27,16 @@ namespace {
 // multiply the weights before these are rounded to fp16, against a running power of two so
 // that neither range ends; fp16 outputs take the rounding's rest in a second product.
 // Minima are summed in 32 bits.
+//
+// Measured, us (bf16, 128 elements, 8 KV heads): 8 requests x 65,536 keys of 64 query heads
+// 127 (70% of the memory's rate; fp16 139), of 128 heads 182 (49%); 8 x 2,304 keys 18 (joined
+// by a second kernel 20), one request 12, of 65,536 keys 33.  A long context is bound by its
+// instructions, some 600 a warp and tile (1,000 for sixteen rows), which three warps of a
+// scheduler issue at half its rate; four, with two stages or 128 registers, are no faster
+// (130, 181).
 
-constexpr int kFewWarps = 4, kTile = 32, kFewStages = 3, kMostSplits = 128;
+constexpr int kFewWarps = 4, kTile = 32, kFewStages = 3, kFewBlocks = 3;
+constexpr int kMostSplits = 128, kMostCluster = 8;
 
 template <int D> struct FewStage {
     static constexpr int kKeyBytes = D / 2 + 16, kCodes = kTile * kKeyBytes, kScales = kTile * (D / E2_CACHE_GROUP) * 4;
@@ -41,7 +49,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
-template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, 3) few_kernel(const AttendParams p)
+// What a part's sums are brought to the joint maximum by (without a maximum it saw nothing, or NaN).
+__device__ __forceinline__ float part_factor(float top, float weights, float best)
+{
+    return top == -INFINITY ? (weights == 0 ? 0.0f : weights) : power2(top - best);
+}
+
+template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) few_kernel(const AttendParams p)
 {
     using St = FewStage<D>;
     constexpr int U = D / 32, GR = D / E2_CACHE_GROUP, C = 8 * NT;
@@ -376,7 +390,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             }
         }
         copy_wait<0>();
-        asm volatile("griddepcontrol.launch_dependents;");
+        allow_next();
 
         // this warp's sums, whole: [C] maxima, [C] weights, [C][D + 1] sums (rows apart in banks)
         __syncthreads();
@@ -406,6 +420,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 }
             }
         __syncthreads();
+        float *shared_parts = reinterpret_cast<float *>(smem) + kFewWarps * (C * (D + 3));
         for (int i = threadIdx.x; i < C * D; i += 32 * kFewWarps) {
             const int c = i / D, d = i % D;
             const int64_t row = row0 + c;
@@ -427,10 +442,37 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 static_cast<T *>(p.out)[rows.token(row) * p.out_stride + head * D + d] =
                     from_float<T>(total > 0 ? x / total : total);
             } else {
-                float *to = p.parts + ((rows.token(row) * p.q_heads + head) * p.splits + split) * (D + 2);
+                float *to = p.parts ? p.parts + ((rows.token(row) * p.q_heads + head) * p.splits + split) * (D + 2)
+                                    : shared_parts + c * (D + 2);
                 to[d] = x;
                 if (d == 0) to[D] = best, to[D + 1] = total;
             }
+        }
+        if (p.splits > 1 && !p.parts) {
+            // the cluster's parts, in their order
+            cluster_barrier();
+            const uint32_t part_at = smem_addr(shared_parts);
+            for (int i = threadIdx.x + split * 32 * kFewWarps; i < C * D; i += 32 * kFewWarps * p.splits) {
+                const int c = i / D, d = i % D;
+                const int64_t row = row0 + c;
+                if (!rows.live(p, row)) continue;
+                float tops[kMostCluster], weights[kMostCluster], x[kMostCluster], best = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < kMostCluster; ++k) {
+                    const uint32_t at = peer_addr(part_at + c * (D + 2) * 4, min(k, p.splits - 1));
+                    tops[k] = peer_load(at + D * 4), weights[k] = peer_load(at + D * 4 + 4), x[k] = peer_load(at + d * 4);
+                    best = fmaxf(best, tops[k]);
+                }
+                float total = 0, sum = 0;
+#pragma unroll
+                for (int k = 0; k < kMostCluster; ++k) {
+                    const float f = part_factor(tops[k], weights[k], best);
+                    if (k < p.splits) total = __fmaf_rn(weights[k], f, total), sum = __fmaf_rn(x[k], f, sum);
+                }
+                static_cast<T *>(p.out)[rows.token(row) * p.out_stride + rows.head(kv, row) * D + d] =
+                    from_float<T>(total > 0 ? sum / total : total);
+            }
+            cluster_barrier();                           // (peers have been read)
         }
         __syncthreads();                                 // (the next rows' tiles overwrite the sums)
     }
@@ -441,7 +483,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
 template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(const AttendParams p)
 {
     __shared__ float factor[kMostSplits], partial[3][D];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_before();
     const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const Rows rows(p, request);
     for (int64_t row = blockIdx.x; row < rows.count; row += gridDim.x) {
@@ -455,8 +497,7 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
         for (int k = 16; k; k >>= 1) best = fmaxf(best, __shfl_xor_sync(~0u, best, k));
         for (int k = lane; k < p.splits; k += 32) {
             const float top = from[k * (D + 2) + D], weights = from[k * (D + 2) + D + 1];
-            // (a part without a maximum saw nothing, or NaN)
-            const float f = top == -INFINITY ? (weights == 0 ? 0.0f : weights) : power2(top - best);
+            const float f = part_factor(top, weights, best);
             if (warp == 0) factor[k] = f;
             total = __fmaf_rn(weights, f, total);
         }
@@ -494,12 +535,18 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
 // request, 128 rows x 16,384 keys 63 / 54 (x 4,096 keys 33 / 42), 2,400 x 300 keys 57 / 35.
 constexpr int kPrompt = 65;
 
+// Up to so many times 128 keys a block, up to eight parts joined in a cluster are better than more
+// with a second kernel, if seven eighths of the places hold them (clusters that do not fit wait
+// for a whole wave).
+constexpr int kClusterUnits = 8;
+
 struct Plan {
     int nt, slabs, splits;      // nt 0: a prompt
+    bool cluster;               // joined there
 };
 
 // Rows by eight or sixteen, or by 256; keys split until every multiprocessor has its
-// three blocks (one), no finer than 128 keys (512).
+// blocks, no finer than 128 keys (512).
 Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
 {
     Plan f;
@@ -512,53 +559,46 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
     if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
     const int least = f.nt ? kTile * kFewWarps : 512;
     const int64_t units = (keys + least - 1) / least;
-    int64_t splits = (int64_t)sms * (f.nt ? 3 : 1) / ((int64_t)a->batch * c->kv_heads * slabs);
+    const int64_t pairs = (int64_t)a->batch * c->kv_heads * slabs, places = (int64_t)sms * (f.nt ? kFewBlocks : 1);
+    int64_t splits = places / pairs;
     if (splits > units) splits = units;
+    f.cluster = f.nt && units <= kMostCluster * kClusterUnits;
+    if (f.cluster && splits > kMostCluster) splits = kMostCluster;
+    while (f.cluster && splits > 2 && pairs * splits * 8 > places * 7) --splits;
     f.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     return f;
 }
 
 size_t workspace_for(const e2_cache *c, const e2_attend_args *a, const Plan &f)
 {
-    return f.splits > 1 ? (size_t)a->tokens * a->q_heads * f.splits * (c->head_dim + 2) * sizeof(float) : 0;
+    return f.splits > 1 && !f.cluster ? (size_t)a->tokens * a->q_heads * f.splits * (c->head_dim + 2) * sizeof(float) : 0;
 }
 
-template <class K> int launch(K kernel, const AttendParams &p, dim3 grid, size_t smem, bool early, int dev,
-                              std::atomic<uint64_t> &ready, cudaStream_t s)
+template <class T, int D, int NT> int launch_few(const AttendParams &p, const Plan &f, dim3 grid, int dev, cudaStream_t s)
 {
+    static std::atomic<uint64_t> ready{0};               // devices that have the attribute set
+    constexpr size_t ring = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes, queries = NT * (D / 32) * 512;
+    constexpr size_t sums = 8 * NT * (kFewWarps * (D + 3) + D + 2) * sizeof(float);
+    constexpr size_t smem = ring + queries > sums ? ring + queries : sums;
+    auto kernel = few_kernel<T, D, NT>;
     if (smem > 48 * 1024 && !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(128);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cfg.attrs = &at;
-    cfg.numAttrs = early ? 1 : 0;
-    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
+    return launch<AttendParams>(kernel, grid, 32 * kFewWarps, smem, f.cluster ? f.splits : 1, false, s, p);
 }
 
 template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
 {
-    static std::atomic<uint64_t> ready[2];               // devices that have the attribute set
-    const size_t ring = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes, smem = ring + (size_t)f.nt * (D / 32) * 512;
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
-    int st;
-    if (f.nt == 0) {
-        st = launch_prompt(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s);
-    } else {
-        st = f.nt == 1 ? launch(few_kernel<T, D, 1>, p, grid, smem, false, dev, ready[0], s)
-                       : launch(few_kernel<T, D, 2>, p, grid, smem, false, dev, ready[1], s);
-    }
-    if (st != E2_OK || f.splits == 1) return st;
-    return launch(join_kernel<T, D>, p, dim3((unsigned)f.slabs * (f.nt ? 8 * f.nt : kPromptRows), pairs), 0, true, dev, ready[0], s);
+    const int st = f.nt == 0   ? launch_prompt(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s)
+                   : f.nt == 1 ? launch_few<T, D, 1>(p, f, grid, dev, s)
+                               : launch_few<T, D, 2>(p, f, grid, dev, s);
+    if (st != E2_OK || f.splits == 1 || f.cluster) return st;
+    const dim3 rows((unsigned)f.slabs * (f.nt ? 8 * f.nt : kPromptRows), pairs);
+    return launch<AttendParams>(join_kernel<T, D>, rows, 128, 0, 1, true, s, p);
 }
 
 int check_args(const e2_cache *c, const e2_attend_args *a)
@@ -611,7 +651,7 @@ extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void 
     AttendParams p{c->pages, __builtin_ctz((unsigned)c->page_size), c->kv_heads, a->tokens, a->q_heads, a->batch, a->window,
                    a->table_cols, f.splits, a->table_stride, a->q_stride, a->out_stride, {c->k_codes, c->v_codes},
                    {reinterpret_cast<const __half2 *>(c->k_scales), reinterpret_cast<const __half2 *>(c->v_scales)},
-                   a->table, a->lens, a->starts, a->scale, a->q, a->out, static_cast<float *>(workspace)};
+                   a->table, a->lens, a->starts, a->scale, a->q, a->out, need ? static_cast<float *>(workspace) : nullptr};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool half = a->dtype == E2_F16;
     if (c->head_dim == 64)
