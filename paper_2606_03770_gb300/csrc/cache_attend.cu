@@ -71,10 +71,11 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
 
     for (int64_t row0 = (int64_t)blockIdx.z * C; row0 < rows.count; row0 += (int64_t)gridDim.z * C) {
         // the keys that some row sees, in tiles; this split's
-        const int64_t last = min(row0 + C, rows.count) - 1;
+        const Slab slab(rows, row0);
+        const int last = (int)min((int64_t)C, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
-        const int lo = p.window > 0 ? (int)max(rows.pos(row0) - p.window + 1, (int64_t)0) : 0;
-        const int hi = (int)min(min(rows.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
+        const int lo = p.window > 0 ? (int)max(slab.pos(0) - p.window + 1, (int64_t)0) : 0;
+        const int hi = (int)min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
         const int tile_lo = lo / kTile, tiles = hi > lo ? (hi + kTile - 1) / kTile - tile_lo : 0;
         const int units = (tiles + kFewWarps - 1) / kFewWarps, per = (units + p.splits - 1) / p.splits * kFewWarps;
         const int first = (int)min((int64_t)tile_lo + (int64_t)split * per, (int64_t)tile_lo + tiles);
@@ -134,9 +135,9 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
         int seen_hi[NT][2], seen_lo[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int64_t row = row0 + 8 * n + g;
-            const bool live = rows.live(p, row);
-            const T *src = static_cast<const T *>(p.q) + (live ? rows.token(row) * p.q_stride + rows.head(kv, row) * D : 0);
+            const int row = 8 * n + g;
+            const bool live = slab.live(p, row);
+            const T *src = static_cast<const T *>(p.q) + (live ? slab.token(row) * p.q_stride + slab.head(kv, row) * D : 0);
             unsigned top = 0;
             uint4 qf[U];
 #pragma unroll
@@ -167,17 +168,17 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 q_scale[n][e] = __shfl_sync(~0u, f, (2 * t + e) * 4);
 #pragma unroll
                 for (int j = 0; j < GR; ++j) q_sum[n][j][e] = __shfl_sync(~0u, sum[j], (2 * t + e) * 4);
-                const int64_t at = row0 + 8 * n + 2 * t + e;
-                const bool seen = rows.live(p, at);
-                seen_hi[n][e] = seen ? (int)rows.pos(at) : -1;
-                seen_lo[n][e] = seen && p.window > 0 ? (int)max(rows.pos(at) - p.window + 1, (int64_t)0) : 0;
+                const int at = 8 * n + 2 * t + e;
+                const bool seen = slab.live(p, at);
+                seen_hi[n][e] = seen ? (int)slab.pos(at) : -1;
+                seen_lo[n][e] = seen && p.window > 0 ? (int)max(slab.pos(at) - p.window + 1, (int64_t)0) : 0;
             }
         }
         __syncthreads();
         // tiles in this range need no mask for any column
-        const int full_lo = p.window > 0 ? (int)max(rows.pos(last) - p.window + 1, (int64_t)0) : 0;
-        const int full_hi = (int)max(rows.pos(row0), (int64_t)-1);
-        const bool all_live = row0 + C <= rows.count && rows.live(p, row0) && rows.live(p, last);
+        const int full_lo = p.window > 0 ? (int)max(slab.pos(last) - p.window + 1, (int64_t)0) : 0;
+        const int full_hi = (int)max(slab.pos(0), (int64_t)-1);
+        const bool all_live = C <= slab.left && slab.live(p, 0) && slab.live(p, last);
 
         float o[U][2][NT][4] = {};                       // sums for dimensions 32 u + 4 g + {0, 1}, {2, 3}
         float low[NT][GR][2] = {}, sum[NT][2] = {};      // minima's sums, weights' sums: this lane's keys
@@ -423,8 +424,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
         float *shared_parts = reinterpret_cast<float *>(smem) + kFewWarps * (C * (D + 3));
         for (int i = threadIdx.x; i < C * D; i += 32 * kFewWarps) {
             const int c = i / D, d = i % D;
-            const int64_t row = row0 + c;
-            if (!rows.live(p, row)) continue;
+            if (!slab.live(p, c)) continue;
             const float *all = reinterpret_cast<const float *>(smem);
             float best = -INFINITY, total = 0, x = 0;
 #pragma unroll
@@ -437,12 +437,13 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 total = __fmaf_rn(from[C + c], f, total);
                 x = __fmaf_rn(from[2 * C + c * (D + 1) + d], f, x);
             }
-            const int head = rows.head(kv, row);
+            const int64_t token = slab.token(c);
+            const int head = slab.head(kv, c);
             if (p.splits == 1) {
-                static_cast<T *>(p.out)[rows.token(row) * p.out_stride + head * D + d] =
+                static_cast<T *>(p.out)[token * p.out_stride + head * D + d] =
                     from_float<T>(total > 0 ? x / total : total);
             } else {
-                float *to = p.parts ? p.parts + ((rows.token(row) * p.q_heads + head) * p.splits + split) * (D + 2)
+                float *to = p.parts ? p.parts + ((token * p.q_heads + head) * p.splits + split) * (D + 2)
                                     : shared_parts + c * (D + 2);
                 to[d] = x;
                 if (d == 0) to[D] = best, to[D + 1] = total;
@@ -454,8 +455,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             const uint32_t part_at = smem_addr(shared_parts);
             for (int i = threadIdx.x + split * 32 * kFewWarps; i < C * D; i += 32 * kFewWarps * p.splits) {
                 const int c = i / D, d = i % D;
-                const int64_t row = row0 + c;
-                if (!rows.live(p, row)) continue;
+                if (!slab.live(p, c)) continue;
                 float tops[kMostCluster], weights[kMostCluster], x[kMostCluster], best = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < kMostCluster; ++k) {
@@ -469,7 +469,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                     const float f = part_factor(tops[k], weights[k], best);
                     if (k < p.splits) total = __fmaf_rn(weights[k], f, total), sum = __fmaf_rn(x[k], f, sum);
                 }
-                static_cast<T *>(p.out)[rows.token(row) * p.out_stride + rows.head(kv, row) * D + d] =
+                static_cast<T *>(p.out)[slab.token(c) * p.out_stride + slab.head(kv, c) * D + d] =
                     from_float<T>(total > 0 ? sum / total : total);
             }
             cluster_barrier();                           // (peers have been read)
@@ -487,9 +487,10 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
     const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const Rows rows(p, request);
     for (int64_t row = blockIdx.x; row < rows.count; row += gridDim.x) {
-        if (!rows.live(p, row)) continue;
-        const int head = rows.head(kv, row);
-        const float *from = p.parts + (rows.token(row) * p.q_heads + head) * p.splits * (D + 2);
+        const Slab slab(rows, row);
+        if (!slab.live(p, 0)) continue;
+        const int head = slab.head(kv, 0);
+        const float *from = p.parts + (slab.token(0) * p.q_heads + head) * p.splits * (D + 2);
         // every warp: the maximum, the parts' factors, the weights' sum
         float best = -INFINITY, total = 0;
         for (int k = lane; k < p.splits; k += 32) best = fmaxf(best, from[k * (D + 2) + D]);
@@ -517,7 +518,7 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
         }
         __syncthreads();
         if (warp == 0) {
-            T *out = static_cast<T *>(p.out) + rows.token(row) * p.out_stride + head * D;
+            T *out = static_cast<T *>(p.out) + slab.token(0) * p.out_stride + head * D;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
                 const int d = 32 * i + lane;

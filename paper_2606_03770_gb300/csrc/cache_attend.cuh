@@ -33,13 +33,22 @@ struct Rows {
         count = queries > 0 ? queries * share : 0;
         first_pos = p.lens[request] - (queries > 0 ? queries : 0);
     }
-    __device__ int64_t pos(int64_t row) const { return first_pos + row / share; }
-    __device__ int64_t token(int64_t row) const { return start + row / share; }
-    __device__ int head(int kv, int64_t row) const { return kv * share + (int)(row % share); }
-    __device__ bool live(const AttendParams &p, int64_t row) const
+};
+
+// Rows row0 + c of them (one division in 64 bits at most, 32 bits for each c).
+struct Slab {
+    unsigned share, over;                    // row0 = query * share + over
+    int start;
+    int64_t left, query, first_pos;          // rows from row0 on
+    __device__ Slab(const Rows &r, int64_t row0) : share(r.share), start(r.start), left(r.count - row0), first_pos(r.first_pos)
     {
-        return row < count && token(row) >= 0 && token(row) < p.tokens;
+        query = row0 >> 32 ? row0 / share : (unsigned)row0 / share;
+        over = (unsigned)(row0 - query * share);
     }
+    __device__ int64_t pos(int c) const { return first_pos + query + (over + c) / share; }
+    __device__ int64_t token(int c) const { return start + query + (over + c) / share; }
+    __device__ int head(int kv, int c) const { return (int)(kv * share + (over + c) % share); }
+    __device__ bool live(const AttendParams &p, int c) const { return c < left && token(c) >= 0 && token(c) < p.tokens; }
 };
 
 __device__ __forceinline__ float power2(float x)

@@ -22,7 +22,7 @@ namespace e2ops {
 namespace {
 
 constexpr int kGroupRows = 128, kKeys = 64, kStages = 3, kRawStages = 3;
-// Warps by fours, one on each scheduler: products (and three that rest), two groups' weights,
+// Warps by fours, one on each scheduler: products (two, and two that rest), two groups' weights,
 // keys, values; and the registers they split a block's 640 x 96 into.
 constexpr int kThreads = 640;
 constexpr int kBarriers = 2 * kStages + 4 + 4 + 2 + 1;
@@ -39,15 +39,14 @@ template <int D> struct PromptShared {
 
 // 256 rows, and the tiles of keys that they see, of this split's.
 struct Span {
-    int64_t row0, last;
+    Slab slab;
     int lo, hi, first, n;
-    __device__ Span(const AttendParams &p, const Rows &rows, int64_t block)
+    __device__ Span(const AttendParams &p, const Rows &rows, int64_t block) : slab(rows, block * kPromptRows)
     {
-        row0 = block * kPromptRows;
-        last = min(row0 + kPromptRows, rows.count) - 1;
+        const int last = (int)min((int64_t)kPromptRows, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
-        lo = p.window > 0 ? (int)max(rows.pos(row0) - p.window + 1, (int64_t)0) : 0;
-        hi = (int)min(min(rows.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
+        lo = p.window > 0 ? (int)max(slab.pos(0) - p.window + 1, (int64_t)0) : 0;
+        hi = (int)min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
         const int tile_lo = lo / kKeys, tiles = hi > lo ? (hi + kKeys - 1) / kKeys - tile_lo : 0;
         const int per = (tiles + p.splits - 1) / p.splits;
         first = (int)min((int64_t)tile_lo + (int64_t)blockIdx.z * per, (int64_t)tile_lo + tiles);
@@ -67,12 +66,12 @@ template <int D> struct Shared {
 
 __device__ __forceinline__ bool finite(uint32_t dm) { return (dm & 0x7c00u) != 0x7c00u && (dm & 0x7c000000u) != 0x7c000000u; }
 
-// One warp: S = q K^T of a tile, then O += P V of the tile before.
-template <int D, bool kRest> __device__ __forceinline__ void products(const Shared<D> &m, int n)
+// A warp, group g: S = q K^T of a tile, then O += P V of the tile before.
+template <int D, bool kRest> __device__ __forceinline__ void products(const Shared<D> &m, int n, int g)
 {
     using Sh = PromptShared<D>;
     const uint32_t score_kind = product_kind(kKeys), sum_kind = product_kind(D, true);
-    const uint64_t query = operand(smem_addr(m.queries)), keys0 = operand(smem_addr(m.stages));
+    const uint64_t query = operand(smem_addr(m.queries + g * Sh::kQuery)), keys0 = operand(smem_addr(m.stages));
     const uint64_t values0 = operand(smem_addr(m.stages) + Sh::kTile, kKeys * 128);
     bool ok = __all_sync(~0u, barrier_wait(m.asked, 0));
     int stage = 0, phase = 0, before = 0;
@@ -85,36 +84,31 @@ template <int D, bool kRest> __device__ __forceinline__ void products(const Shar
                 // (addresses in 16 bytes: a block of 64 elements, then 16 of them)
                 const uint64_t b = keys0 + stage * (2 * Sh::kTile / 16);
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        issue_product(m.memory + g * 128 + (j & 1) * 64, query + g * (Sh::kQuery / 16) + k / 4 * (kGroupRows * 8) + 2 * (k % 4),
-                                      b + k / 4 * (kKeys * 8) + 2 * (k % 4), score_kind, k > 0);
-                    commit_products(m.scored + 8 * (2 * g + (j & 1)));
-                }
+                for (int k = 0; k < D / 16; ++k)
+                    issue_product(m.memory + g * 128 + (j & 1) * 64, query + k / 4 * (kGroupRows * 8) + 2 * (k % 4),
+                                  b + k / 4 * (kKeys * 8) + 2 * (k % 4), score_kind, k > 0);
+                commit_products(m.scored + 8 * (2 * g + (j & 1)));
             }
             __syncwarp();
         }
         if (j > 0) {
             const int i = j - 1;
-            for (int g = 0; g < 2; ++g) {
-                ok = ok && __all_sync(~0u, barrier_wait(m.weighed + 8 * (2 * g + (i & 1)), i / 2 & 1));
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (elected()) {
-                    const uint32_t weights = m.memory + g * 128 + (i & 1) * 64, sums = m.memory + kSums + g * 128;
-                    const uint64_t b = values0 + before * (2 * Sh::kTile / 16);
+            ok = __all_sync(~0u, barrier_wait(m.weighed + 8 * (2 * g + (i & 1)), i / 2 & 1));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (elected()) {
+                const uint32_t weights = m.memory + g * 128 + (i & 1) * 64, sums = m.memory + kSums + g * 128;
+                const uint64_t b = values0 + before * (2 * Sh::kTile / 16);
 #pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 8 * k, b + k * 128, sum_kind, i > 0 || k > 0);
-                    if (kRest) {
+                for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 8 * k, b + k * 128, sum_kind, i > 0 || k > 0);
+                if (kRest) {
 #pragma unroll
-                        for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 32 + 8 * k, b + k * 128, sum_kind, true);
-                    }
-                    commit_products(m.summed + 8 * g);
-                    if (g == 1) commit_products(m.empty + 8 * before);
+                    for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 32 + 8 * k, b + k * 128, sum_kind, true);
                 }
-                __syncwarp();
+                commit_products(m.summed + 8 * g);
+                commit_products(m.empty + 8 * before);
             }
+            __syncwarp();
         }
         before = stage;
         if (++stage == kStages) stage = 0, phase ^= 1;
@@ -124,38 +118,55 @@ template <int D, bool kRest> __device__ __forceinline__ void products(const Shar
 
 // Four warps, group g: weights, a thread a row; then the rows' outputs.
 template <class T, int D>
-__device__ __forceinline__ void weights(const AttendParams &p, const Rows &rows, const Span &span, const Shared<D> &m, int kv, int g, int quarter,
+__device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, int kv, int g, int quarter,
                                         int lane)
 {
     using Sh = PromptShared<D>;
     constexpr int GR = D / E2_CACHE_GROUP;
     constexpr bool kRest = std::is_same<T, __half>::value;
     const int r = 32 * quarter + lane;
-    const int64_t row = span.row0 + g * kGroupRows + r;
-    const bool live = rows.live(p, row);
+    const int row = g * kGroupRows + r;
+    const Slab &slab = span.slab;
+    const bool live = slab.live(p, row);
+    const int64_t token = slab.token(row);
+    const int head = slab.head(kv, row);
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     float scale;
     {
-        // the query, to fp16 times a power of two (and the scale's sign)
-        const T *src = static_cast<const T *>(p.q) + (live ? rows.token(row) * p.q_stride + rows.head(kv, row) * D : 0);
-        unsigned top = 0;
+        // the queries, to fp16 times a power of two each (and the scale's sign): this warp's 32
+        // rows, kAtOnce at a time, a lane an octet
+        constexpr int kOctets = D / 8, kAtOnce = 32 / kOctets, kLoads = 32 / kAtOnce;
+        const int64_t mine = live ? token * p.q_stride + head * D : -1;
+        const int o = lane % kOctets;
+        int power = 0;
 #pragma unroll
-        for (int o = 0; o < D / 8; ++o)
-            if (live) top = max(top, octet_largest(reinterpret_cast<const uint4 *>(src)[o]));
-        const int k = power_for<T>(top);
-        scale = fabsf(p.scale) * 1.4426950408889634f * power_of_two(-k);
+        for (int half = 0; half < 2; ++half) {
+            uint4 v[kLoads / 2];
 #pragma unroll
-        for (int o = 0; o < D / 8; ++o) {
-            uint4 v{0, 0, 0, 0};
-            if (live) v = octet_in_order<T>(reinterpret_cast<const uint4 *>(src)[o], p.scale < 0 ? -power_of_two(k) : power_of_two(k));
-            *reinterpret_cast<uint4 *>(m.queries + g * Sh::kQuery + o / 8 * kGroupRows * 128 + r * 128 + ((o % 8) ^ (r & 7)) * 16) = v;
+            for (int i = 0; i < kLoads / 2; ++i) {
+                const int64_t at = __shfl_sync(~0u, mine, (half * (kLoads / 2) + i) * kAtOnce + lane / kOctets);
+                v[i] = uint4{0, 0, 0, 0};
+                if (at >= 0) v[i] = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + at)[o];
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads / 2; ++i) {
+                const int turn = half * (kLoads / 2) + i, to = 32 * quarter + turn * kAtOnce + lane / kOctets;
+                unsigned top = octet_largest(v[i]);
+#pragma unroll
+                for (int k = 1; k < kOctets; k *= 2) top = max(top, __shfl_xor_sync(~0u, top, k));
+                const int k = power_for<T>(top), theirs = __shfl_sync(~0u, k, lane % kAtOnce * kOctets);
+                if (lane / kAtOnce == turn) power = theirs;
+                *reinterpret_cast<uint4 *>(m.queries + g * Sh::kQuery + o / 8 * kGroupRows * 128 + to * 128 + ((o % 8) ^ (to & 7)) * 16) =
+                    octet_in_order<T>(v[i], p.scale < 0 ? -power_of_two(k) : power_of_two(k));
+            }
         }
+        scale = fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) barrier_arrive(m.asked);
     }
-    const int pos = row < rows.count ? (int)max(rows.pos(row), (int64_t)-1) : -1;
-    const int from = row < rows.count && p.window > 0 ? (int)max(rows.pos(row) - p.window + 1, (int64_t)0) : 0;
+    const int pos = row < slab.left ? (int)max(slab.pos(row), (int64_t)-1) : -1;
+    const int from = row < slab.left && p.window > 0 ? (int)max(slab.pos(row) - p.window + 1, (int64_t)0) : 0;
     float top = -INFINITY, sum = 0;
     unsigned spoilt = 0;                                     // bit j: this row sees a value of group j that is not finite
     bool ok = true;
@@ -258,7 +269,6 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Rows &rows,
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const bool lost = !ok || *m.failed;
     const float nan = __int_as_float(0x7fc00000);
-    const int head = rows.head(kv, row);
     const float inverse = sum > 0 ? 1.0f / sum : 0.0f;
 #pragma unroll
     for (int c = 0; c < D; c += 32) {
@@ -273,7 +283,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Rows &rows,
         for (int k = 0; k < 32; ++k) x[k / 8 * 8 + k % 8 / 2 + k % 2 * 4] = __uint_as_float(v[k]);
         const bool none = lost || (spoilt >> (c / E2_CACHE_GROUP) & 1);
         if (live && p.splits == 1) {
-            T *out = static_cast<T *>(p.out) + rows.token(row) * p.out_stride + head * D + c;
+            T *out = static_cast<T *>(p.out) + token * p.out_stride + head * D + c;
 #pragma unroll
             for (int o = 0; o < 4; ++o) {
                 float y[8];
@@ -282,7 +292,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Rows &rows,
                 *reinterpret_cast<uint4 *>(out + 8 * o) = pack8<T>(y);
             }
         } else if (live) {
-            float *to = p.parts + ((rows.token(row) * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2);
+            float *to = p.parts + ((token * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2);
 #pragma unroll
             for (int k = 0; k < 32; ++k) to[c + k] = none ? nan : x[k];
             if (c == 0) to[D] = top, to[D + 1] = lost ? nan : sum;
@@ -385,10 +395,10 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_
     __shared__ uint32_t tensor_memory;
     __shared__ int failed;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads;
+    const int request = blockIdx.x / p.kv_heads, kv = blockIdx.x % p.kv_heads;
     const Rows rows(p, request);
     const int64_t blocks = (rows.count + kPromptRows - 1) / kPromptRows;
-    if (blocks <= blockIdx.x) return;
+    if (blocks <= blockIdx.y) return;
     Shared<D> m;
     m.queries = dynamic + (1024 - smem_addr(dynamic) % 1024) % 1024;              // (swizzled tiles start on 1024 bytes)
     m.stages = m.queries + 2 * Sh::kQuery;
@@ -403,7 +413,7 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_
     m.bad = bad;
     m.failed = &failed;
     auto set_barriers = [&] {
-        for (int i = 0; i < kStages; ++i) barrier_init(m.full + 8 * i, 8), barrier_init(m.empty + 8 * i, 1);
+        for (int i = 0; i < kStages; ++i) barrier_init(m.full + 8 * i, 8), barrier_init(m.empty + 8 * i, 2);
         for (int i = 0; i < 4; ++i) barrier_init(m.scored + 8 * i, 1), barrier_init(m.weighed + 8 * i, 4);
         for (int i = 0; i < 2; ++i) barrier_init(m.summed + 8 * i, 1);
         barrier_init(m.asked, 8);
@@ -435,13 +445,13 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_
             asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
         }
     };
-    const int64_t start = blocks - 1 - blockIdx.x;
+    const int64_t start = blocks - 1 - blockIdx.y;
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        for (int64_t block = start; block >= 0; block -= gridDim.x) {
+        for (int64_t block = start; block >= 0; block -= gridDim.y) {
             const Span span(p, rows, block);
-            if (warp == 0) products<D, std::is_same<T, __half>::value>(m, span.n);
-            meet(block >= gridDim.x);
+            if (warp < 2) products<D, std::is_same<T, __half>::value>(m, span.n, warp);
+            meet(block >= gridDim.y);
         }
         asm volatile("griddepcontrol.launch_dependents;");
         __syncwarp();
@@ -449,16 +459,16 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(m.memory), "r"(kColumns) : "memory");
     } else if (warp < 12) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
-        for (int64_t block = start; block >= 0; block -= gridDim.x) {
-            weights<T, D>(p, rows, Span(p, rows, block), m, kv, (warp - 4) / 4, warp % 4, lane);
-            meet(block >= gridDim.x);
+        for (int64_t block = start; block >= 0; block -= gridDim.y) {
+            weights<T, D>(p, Span(p, rows, block), m, kv, (warp - 4) / 4, warp % 4, lane);
+            meet(block >= gridDim.y);
         }
         asm volatile("griddepcontrol.launch_dependents;");
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        for (int64_t block = start; block >= 0; block -= gridDim.x) {
+        for (int64_t block = start; block >= 0; block -= gridDim.y) {
             unpack<D>(p, Span(p, rows, block), m, request, kv, (warp - 12) / 4, warp % 4, lane);
-            meet(block >= gridDim.x);
+            meet(block >= gridDim.y);
         }
         asm volatile("griddepcontrol.launch_dependents;");
     }
@@ -474,7 +484,7 @@ template <class T, int D> int launch_as(const AttendParams &p, int blocks, int p
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    kernel<<<dim3((unsigned)blocks, (unsigned)pairs, (unsigned)p.splits), kThreads, smem, s>>>(p);
+    kernel<<<dim3((unsigned)pairs, (unsigned)blocks, (unsigned)p.splits), kThreads, smem, s>>>(p);
     return cuda_status(cudaGetLastError());
 }
 
