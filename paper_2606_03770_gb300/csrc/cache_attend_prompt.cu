@@ -4,7 +4,7 @@
 // block takes 256 rows (queries times the query heads of a KV head), in two groups of
 // 128 so that one group's weights are made while the other's products run, and walks over
 // tiles of 64 keys.  Eight warps dequantise a tile for both (fp16, one rounding: 2^-12 of a
-// value), one issues S = q K^T and O += P V, eight make the weights, a thread a row: scores
+// value), four issue S = q K^T and O += P V of each, eight make the weights, a thread a row: scores
 // come from tensor memory, weights go back into the scores' place, as the operand that P V
 // reads from there.  O stays in tensor memory and is brought to a new maximum only
 // when the old one is exceeded by 2^8.  Elements of eight lie in the order that unpacking
@@ -22,10 +22,10 @@ namespace e2ops {
 namespace {
 
 constexpr int kGroupRows = 128, kKeys = 64, kStages = 3, kRawStages = 3;
-// Warps by fours, one on each scheduler: products (two, and two that rest), two groups' weights,
+// Warps by fours, one on each scheduler: products (scores and sums of two groups), their weights,
 // keys, values; and the registers they split a block's 640 x 96 into.
 constexpr int kThreads = 640;
-constexpr int kBarriers = 2 * kStages + 4 + 4 + 2 + 1;
+constexpr int kBarriers = 2 * kStages + 4 + 4 + 4 + 1;
 constexpr uint32_t kColumns = 512, kSums = 256;             // tensor memory: scores [group][2][64], then sums [group][128]
 
 template <int D> struct PromptShared {
@@ -57,7 +57,7 @@ struct Span {
 // What a block shares.
 template <int D> struct Shared {
     uint8_t *queries, *stages, *raw;
-    uint32_t full, empty, scored, weighed, summed, asked;    // barriers; scored, weighed [group][2], summed [group]
+    uint32_t full, empty, scored, weighed, summed, asked;    // barriers; scored, weighed, summed [group][2]
     uint8_t (*there)[4];                                     // [stage]: whether each 16 keys are there
     uint16_t (*bad)[D / E2_CACHE_GROUP][4];                  // [stage][group]: keys whose values are not finite
     volatile int *failed;
@@ -66,52 +66,61 @@ template <int D> struct Shared {
 
 __device__ __forceinline__ bool finite(uint32_t dm) { return (dm & 0x7c00u) != 0x7c00u && (dm & 0x7c000000u) != 0x7c000000u; }
 
-// A warp, group g: S = q K^T of a tile, then O += P V of the tile before.
-template <int D, bool kRest> __device__ __forceinline__ void products(const Shared<D> &m, int n, int g)
+// A warp, group g: S = q K^T of each tile.
+template <int D> __device__ __forceinline__ void score(const Shared<D> &m, int n, int g)
 {
     using Sh = PromptShared<D>;
-    const uint32_t score_kind = product_kind(kKeys), sum_kind = product_kind(D, true);
+    const uint32_t kind = product_kind(kKeys);
     const uint64_t query = operand(smem_addr(m.queries + g * Sh::kQuery)), keys0 = operand(smem_addr(m.stages));
-    const uint64_t values0 = operand(smem_addr(m.stages) + Sh::kTile, kKeys * 128);
     bool ok = __all_sync(~0u, barrier_wait(m.asked, 0));
-    int stage = 0, phase = 0, before = 0;
-    for (int j = 0; j <= n && ok; ++j) {
-        if (j < n) {
-            ok = __all_sync(~0u, barrier_wait(m.full + 8 * stage, phase));
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (elected()) {
-                // (addresses in 16 bytes: a block of 64 elements, then 16 of them)
-                const uint64_t b = keys0 + stage * (2 * Sh::kTile / 16);
+    int stage = 0, phase = 0;
+    for (int j = 0; j < n && ok; ++j) {
+        ok = __all_sync(~0u, barrier_wait(m.full + 8 * stage, phase));
+        // (the weights in this place have been used)
+        if (ok && j > 1) ok = __all_sync(~0u, barrier_wait(m.summed + 8 * (2 * g + (j & 1)), (j / 2 - 1) & 1));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (elected()) {
+            // (addresses in 16 bytes: a block of 64 elements, then 16 of them)
+            const uint64_t b = keys0 + stage * (2 * Sh::kTile / 16);
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    issue_product(m.memory + g * 128 + (j & 1) * 64, query + k / 4 * (kGroupRows * 8) + 2 * (k % 4),
-                                  b + k / 4 * (kKeys * 8) + 2 * (k % 4), score_kind, k > 0);
-                commit_products(m.scored + 8 * (2 * g + (j & 1)));
-            }
-            __syncwarp();
+            for (int k = 0; k < D / 16; ++k)
+                issue_product(m.memory + g * 128 + (j & 1) * 64, query + k / 4 * (kGroupRows * 8) + 2 * (k % 4),
+                              b + k / 4 * (kKeys * 8) + 2 * (k % 4), kind, k > 0);
+            commit_products(m.scored + 8 * (2 * g + (j & 1)));
         }
-        if (j > 0) {
-            const int i = j - 1;
-            ok = __all_sync(~0u, barrier_wait(m.weighed + 8 * (2 * g + (i & 1)), i / 2 & 1));
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (elected()) {
-                const uint32_t weights = m.memory + g * 128 + (i & 1) * 64, sums = m.memory + kSums + g * 128;
-                const uint64_t b = values0 + before * (2 * Sh::kTile / 16);
-#pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 8 * k, b + k * 128, sum_kind, i > 0 || k > 0);
-                if (kRest) {
-#pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 32 + 8 * k, b + k * 128, sum_kind, true);
-                }
-                commit_products(m.summed + 8 * g);
-                commit_products(m.empty + 8 * before);
-            }
-            __syncwarp();
-        }
-        before = stage;
+        __syncwarp();
         if (++stage == kStages) stage = 0, phase ^= 1;
+    }
+    if (!ok) *m.failed = 1;
+}
+
+// A warp, group g: O += P V of each tile.
+template <int D, bool kRest> __device__ __forceinline__ void sum_up(const Shared<D> &m, int n, int g)
+{
+    using Sh = PromptShared<D>;
+    const uint32_t kind = product_kind(D, true), sums = m.memory + kSums + g * 128;
+    const uint64_t values0 = operand(smem_addr(m.stages) + Sh::kTile, kKeys * 128);
+    bool ok = true;
+    int stage = 0;
+    for (int j = 0; j < n && ok; ++j) {
+        ok = __all_sync(~0u, barrier_wait(m.weighed + 8 * (2 * g + (j & 1)), j / 2 & 1));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (elected()) {
+            const uint32_t weights = m.memory + g * 128 + (j & 1) * 64;
+            const uint64_t b = values0 + stage * (2 * Sh::kTile / 16);
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 8 * k, b + k * 128, kind, j > 0 || k > 0);
+            if (kRest) {
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 32 + 8 * k, b + k * 128, kind, true);
+            }
+            commit_products(m.summed + 8 * (2 * g + (j & 1)));
+            commit_products(m.empty + 8 * stage);
+        }
+        __syncwarp();
+        if (++stage == kStages) stage = 0;
     }
     if (!ok) *m.failed = 1;
 }
@@ -170,6 +179,8 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     float top = -INFINITY, sum = 0;
     unsigned spoilt = 0;                                     // bit j: this row sees a value of group j that is not finite
     bool ok = true;
+    // whether a tile's sums are there, and all before it (the products of a group run in their order)
+    auto summed = [&](int j) { return (bool)__all_sync(~0u, barrier_wait(m.summed + 8 * (2 * g + (j & 1)), j / 2 & 1)); };
     int stage = 0;
     for (int j = 0; j < span.n; ++j) {
         const int key0 = (span.first + j) * kKeys;
@@ -215,7 +226,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
             top = is;
             sum *= back;
             if (j > 0) {
-                ok = __all_sync(~0u, barrier_wait(m.summed + 8 * g, (j - 1) & 1));
+                ok = summed(j - 1);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t o = m.memory + lanes + kSums + g * 128;
@@ -258,13 +269,10 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        // (a tile's scores tell that all sums but the last tile's are there.  So does this, of those,
-        // before the last tile's may begin: the wait after the loop has two phases to tell apart, no more)
-        if (j > 0 && j == span.n - 1) ok = __all_sync(~0u, barrier_wait(m.summed + 8 * g, (j - 1) & 1));
-        if (!ok) break;
         if (lane == 0) barrier_arrive(m.weighed + 8 * (2 * g + (j & 1)));
     }
-    if (ok && span.n > 0) ok = __all_sync(~0u, barrier_wait(m.summed + 8 * g, (span.n - 1) & 1));
+    if (ok && span.n > 1) ok = summed(span.n - 2);
+    if (ok && span.n > 0) ok = summed(span.n - 1);
     if (!ok) *m.failed = 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const bool lost = !ok || *m.failed;
@@ -349,36 +357,55 @@ __device__ __forceinline__ void unpack(const AttendParams &p, const Span &span, 
         place = place == 2 ? 0 : place + 1;
         ok = __all_sync(~0u, barrier_wait(m.empty + 8 * stage, phase));
         if (!ok) break;
+        // a lane looks at one scale and minimum
         const uint32_t *sc = reinterpret_cast<const uint32_t *>(from + Sh::kRawCodes);
+        const uint32_t looked = sc[lane % (16 * GR)];
+        const float2 range = __half22float2(*reinterpret_cast<const __half2 *>(&looked));
+        const bool plain = __all_sync(~0u, __fmaf_rn(15.0f, fabsf(range.x), fabsf(range.y)) <= 65504.0f);
         if (which) {
-            // values' groups that are not finite
+            // values' groups that are not finite: bit key
+            const unsigned mask = plain ? 0 : __ballot_sync(~0u, lane < 16 * GR && !finite(looked));
 #pragma unroll
             for (int i = 0; i < GR; ++i) {
-                const unsigned mask = __ballot_sync(~0u, lane < 16 && !finite(sc[lane % 16 * GR + i]));
-                if (lane == 0) m.bad[stage][i][w] = (uint16_t)mask;
+                unsigned keys = 0;
+                if (mask)
+                    for (int key = 0; key < 16; ++key) keys |= (mask >> (key * GR + i) & 1) << key;
+                if (lane == 0) m.bad[stage][i][w] = (uint16_t)keys;
             }
         } else if (lane == 0) {
             m.there[stage][w] = present;
         }
-        constexpr int kWords = D / 8, kAtOnce = 32 / kWords;                      // of a key; keys at once
-        const int word = lane % kWords;
-        uint8_t *to = m.stages + (stage * 2 + which) * Sh::kTile + word / 8 * kKeys * 128;
+        // four words of a key at a time
+        constexpr int kFours = D / 32;
+        auto all = [&](auto easy) {
 #pragma unroll
-        for (int i = 0; i < 16 / kAtOnce; ++i) {
-            const int key = i * kAtOnce + lane / kWords, r = 16 * w + key;
-            const uint32_t word_codes = reinterpret_cast<const uint32_t *>(from)[key * kWords + word], dm = sc[key * GR + word / 8];
-            const __half2 both = *reinterpret_cast<const __half2 *>(&dm);
-            __half2 d = __low2half2(both), mn = __high2half2(both);
-            if (!finite(dm)) {
-                // keys are NaN then, values 0
-                d = __float2half2_rn(0.0f);
-                mn = which ? d : __float2half2_rn(__int_as_float(0x7fc00000));
+            for (int i = 0; i < kFours / 2; ++i) {
+                const int item = i * 32 + lane, r = 16 * w + item / kFours, word = item % kFours * 4;
+                const uint4 four = reinterpret_cast<const uint4 *>(from)[item];
+                const uint32_t words[4] = {four.x, four.y, four.z, four.w}, dm = sc[item / kFours * GR + word / 8];
+                const __half2 both = *reinterpret_cast<const __half2 *>(&dm);
+                __half2 d = __low2half2(both), mn = __high2half2(both);
+                if (!easy.value && !finite(dm)) {
+                    // keys are NaN then, values 0
+                    d = __float2half2_rn(0.0f);
+                    mn = which ? d : __float2half2_rn(__int_as_float(0x7fc00000));
+                }
+                uint8_t *to = m.stages + (stage * 2 + which) * Sh::kTile + word / 8 * kKeys * 128 + r * 128;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<uint4 *>(to + ((word % 8 + e) ^ (r & 7)) * 16) = unpack_word<!easy.value>(words[e], d, mn);
             }
-            *reinterpret_cast<uint4 *>(to + r * 128 + ((word % 8) ^ (r & 7)) * 16) = unpack_word(word_codes, d, mn);
-        }
+        };
+        if (plain) all(std::true_type{});
+        else all(std::false_type{});
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) barrier_arrive(m.full + 8 * stage);
+        if (++stage == kStages) stage = 0, phase ^= 1;
+    }
+    // (nothing is to arrive at a barrier any more)
+    for (int i = 0; i < kStages && ok; ++i) {
+        ok = __all_sync(~0u, barrier_wait(m.empty + 8 * stage, phase));
         if (++stage == kStages) stage = 0, phase ^= 1;
     }
     if (!ok) *m.failed = 1;
@@ -408,14 +435,14 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_
     m.scored = m.empty + 8 * kStages;
     m.weighed = m.scored + 8 * 4;
     m.summed = m.weighed + 8 * 4;
-    m.asked = m.summed + 8 * 2;
+    m.asked = m.summed + 8 * 4;
     m.there = there;
     m.bad = bad;
     m.failed = &failed;
     auto set_barriers = [&] {
         for (int i = 0; i < kStages; ++i) barrier_init(m.full + 8 * i, 8), barrier_init(m.empty + 8 * i, 2);
-        for (int i = 0; i < 4; ++i) barrier_init(m.scored + 8 * i, 1), barrier_init(m.weighed + 8 * i, 4);
-        for (int i = 0; i < 2; ++i) barrier_init(m.summed + 8 * i, 1);
+        for (int i = 0; i < 4; ++i)
+            barrier_init(m.scored + 8 * i, 1), barrier_init(m.weighed + 8 * i, 4), barrier_init(m.summed + 8 * i, 1);
         barrier_init(m.asked, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     };
@@ -450,7 +477,8 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         for (int64_t block = start; block >= 0; block -= gridDim.y) {
             const Span span(p, rows, block);
-            if (warp < 2) products<D, std::is_same<T, __half>::value>(m, span.n, warp);
+            if (warp < 2) score<D>(m, span.n, warp);
+            else sum_up<D, std::is_same<T, __half>::value>(m, span.n, warp - 2);
             meet(block >= gridDim.y);
         }
         asm volatile("griddepcontrol.launch_dependents;");

@@ -52,8 +52,8 @@ template <class T> __device__ __forceinline__ uint4 octet_in_order(const uint4 &
 // A word's eight codes c as m + d c in fp16, rounded once, in the same order.  A code
 // in the low bits of 1024's fp16 makes 1024 + c, in the next four 1024 + 16 c.  The
 // largest value may pass fp16's range by the rounding of d: it stays fp16's largest
-// (NaN stays NaN).
-__device__ __forceinline__ uint4 unpack_word(uint32_t w, __half2 d, __half2 m)
+// (NaN stays NaN), unless the caller knows that none does.
+template <bool LIMIT = true> __device__ __forceinline__ uint4 unpack_word(uint32_t w, __half2 d, __half2 m)
 {
     const uint32_t v = w >> 8;
     uint32_t q[4] = {(w & 0x000f000fu) | 0x64006400u, (w & 0x00f000f0u) | 0x64006400u, (v & 0x000f000fu) | 0x64006400u,
@@ -66,7 +66,8 @@ __device__ __forceinline__ uint4 unpack_word(uint32_t w, __half2 d, __half2 m)
     for (int i = 0; i < 4; ++i) {
         const __half2 x = *reinterpret_cast<const __half2 *>(&q[i]);
         const __half2 c = i % 2 ? __hfma2(x, sixteenth, high) : __hadd2(x, off);
-        o[i] = __hmin2_nan(__hfma2(c, d, m), most);
+        o[i] = __hfma2(c, d, m);
+        if (LIMIT) o[i] = __hmin2_nan(o[i], most);
     }
     return out;
 }
