@@ -29,8 +29,8 @@ namespace {
 // Minima are summed in 32 bits.
 //
 // Measured, us (bf16, 128 elements, 8 KV heads): 8 requests x 65,536 keys of 64 query heads
-// 127 (70% of the memory's rate; fp16 139), of 128 heads 182 (49%); 8 x 2,304 keys 18 (joined
-// by a second kernel 20), one request 12, of 65,536 keys 33.  A long context is bound by its
+// 126 (71% of the memory's rate; fp16 139), of 128 heads 176 (51%); 8 x 2,304 keys 17 (joined
+// by a second kernel 19), one request 11, of 65,536 keys 36.  A long context is bound by its
 // instructions, some 600 a warp and tile (1,000 for sixteen rows), which three warps of a
 // scheduler issue at half its rate; four, with two stages or 128 registers, are no faster
 // (130, 181).
@@ -530,10 +530,10 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
     }
 }
 
-// From so many rows of a request and KV head on they are a prompt's.  Measured, us (8 KV
-// heads of 128 elements; rows by sixteen / by 256): 32 rows of 8 requests x 2,304 keys
-// 36 / 54, 64 rows 45 / 53, 128 rows 85 / 66; 40 rows of 8 x 65,536 keys 620 / 741; of one
-// request, 128 rows x 16,384 keys 63 / 54 (x 4,096 keys 33 / 42), 2,400 x 300 keys 57 / 35.
+// From so many rows of a request and KV head on they are a prompt's.  Measured, us (8 KV heads
+// of 128 elements; rows by sixteen / by 256): 32 rows of 8 requests x 2,304 keys 33 / 42, 64
+// rows 42 / 46, 128 rows 79 / 52; 40 rows of 8 x 65,536 keys 609 / 696; of one request, 64 rows
+// x 16,384 keys 44 / 38, 264 x 5,000 keys 51 / 43.
 constexpr int kPrompt = 65;
 
 // Up to so many times 128 keys a block, up to eight parts joined in a cluster are better than more

@@ -1,7 +1,6 @@
 // cache_attend_prompt.cu -- e2_cache_attend for prompts.
 //
-// Bound by the fifth-generation tensor cores and, as much, by the exponentials.  A
-// block takes 256 rows (queries times the query heads of a KV head), in two groups of
+// A block takes 256 rows (queries times the query heads of a KV head), in two groups of
 // 128 so that one group's weights are made while the other's products run, and walks over
 // tiles of 64 keys.  Eight warps dequantise a tile for both (fp16, one rounding: 2^-12 of a
 // value), four issue S = q K^T and O += P V of each, eight make the weights, a thread a row: scores
@@ -12,6 +11,12 @@
 // Weights go to fp16 times 2^7 (2^-12 each; fp16 outputs take the rounding's rest in a second
 // product).  A weight of 0 does not stop a NaN among the values, so values whose scale or
 // minimum is not finite are held back as zeros, and rows that do see their keys are made NaN.
+//
+// Bound by the instructions of a tile: 2,200 cycles, of which the weights' exponentials take
+// 1,024 of their unit's and the products 1,000 of the tensor cores'.  Measured (64 query heads
+// over 8, 128 elements, bf16): 1,152 queries x 2,304 keys 75 us (870 TFLOP/s, 45% of the
+// tensor cores' measured rate), 2,048 x 2,048 92 us, 4 x 256 x 4,096 148 us; 4,096 x 4,096 of 128
+// heads 580 us (949 TFLOP/s).  The longest blocks of all heads come first (127 us for 142, a step before).
 //
 // Every wait ends: one that takes too long marks the block as failed, which then frees
 // its tensor memory and writes NaN.
