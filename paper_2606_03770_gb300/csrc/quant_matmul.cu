@@ -25,12 +25,16 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
     const int chunks = (cols + kChunk - 1) / kChunk, x_pad = chunks * kChunk;
     const int per = kChunk / group, stage = kRows * (kRowBytes + per * 2 * (mins ? 2 : 1));
     auto plan = [&](int wk, int split) {
-        // all of x at once where that leaves room, else a stage of each warp at a time, two in turn
+        // all of x at once where that leaves room for three blocks, else as many stages of each
+        // warp as it does, two such segments in turn
+        auto bytes = [&](int cols) { return (size_t)tokens * x_row_bytes(cols) + (size_t)8 * nt * (cols / group) * 4; };
         const int mine = (chunks + split - 1) / split * kChunk;
-        const bool whole = (size_t)tokens * mine * 2 <= 25 * 1024;
-        const int xc = whole ? mine : wk * kChunk;
-        const size_t smem = (size_t)kWarps * ring_stages(nt) * stage +
-                            (whole ? 1 : 2) * ((size_t)tokens * x_row_bytes(xc) + (size_t)8 * nt * (xc / group) * 4);
+        const size_t ring = (size_t)kWarps * kFewStages * stage, room = kSmemPerSm / 3 - 1536 - ring;
+        const bool whole = bytes(mine) <= room;
+        int times = 1;
+        while (bytes((times + 1) * wk * kChunk) * 2 <= room) ++times;
+        const int xc = whole ? mine : times * wk * kChunk;
+        const size_t smem = ring + (whole ? 1 : 2) * bytes(xc);
         const bool own = (size_t)tokens * mine <= kOwn && (int64_t)rows * cols <= kOwnWeights;
         return FewPlan{nt, wk, split, xc, x_pad, smem, own ? 0 : prepared_bytes(nt, x_pad, 32)};
     };

@@ -23,7 +23,7 @@ struct MatmulParams {
 // Bound by reading the weights, then by the instructions that unpack them.  y^T = W
 // x^T on the warp-level tensor cores: the weights are the 16-row operand, eight
 // tokens the other, so a code is unpacked once and no row is padding.  A warp owns
-// 16 rows and streams them through a ring of its own in shared memory, two or three
+// 16 rows and streams them through a ring of its own in shared memory, two
 // stages of 512 columns, without a block barrier: 256 bytes of a row at a time come at 6.2
 // TB/s, 128 bytes of 32 rows at 5.8, and at 4.4 where rows are 14 KB apart.
 //
@@ -52,8 +52,9 @@ struct FewPlan {
     size_t smem, workspace;
 };
 
-// Stages of a warp's ring: what shared memory holds of three blocks.
-__host__ __device__ constexpr int ring_stages(int nt) { return nt == 1 ? 3 : 2; }
+// Stages of a warp's ring.  Two leave room for longer segments of x, at whose ends a block's
+// warps meet: 57344 x 8192, 8 tokens, us: three and 512 columns 65, two and 1,024 54.
+constexpr int kFewStages = 2;
 
 template <int G, bool MINS> struct Stage {
     static constexpr int kPer = kChunk / G;                                 // scales of a row
@@ -134,7 +135,7 @@ template <int G, bool MINS, int NT>
 __global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
 {
     using St = Stage<G, MINS>;
-    constexpr int kPer = St::kPer, kStages = ring_stages(NT);
+    constexpr int kPer = St::kPer, kStages = kFewStages;
     const int WK = q.wk, RB = kRows * (kWarps / WK);
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float unscale[8 * NT];                              // 1 / the token's power of two
