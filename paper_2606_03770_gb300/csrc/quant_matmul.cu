@@ -4,8 +4,8 @@
 namespace e2ops {
 namespace {
 
-// Blocks to have at least: 1.6 per multiprocessor keep the memory busy.
-constexpr int kFewBlocks = 250;
+// Blocks to have at least: 1.6 per multiprocessor keep the memory busy; and those that run at once.
+constexpr int kFewBlocks = 250, kAtOnce = 3 * 152;
 
 // So few elements of x a block prepares for itself: one launch and no workspace, where weights
 // are read in less time than that costs the caller.  Measured, us a call (a graph's; by
@@ -14,11 +14,12 @@ constexpr int kFewBlocks = 250;
 constexpr size_t kOwn = kOwnOctets * 32 * kWarps * 8;
 constexpr int64_t kOwnWeights = 1 << 27;
 
-// Rows alone where they make enough blocks; else columns are split: in two by a
-// cluster, further among the four warps of a block first (no cluster to join), then by
-// clusters of up to eight.  Measured, us (one token, 64 columns a group; joined by warps x
-// clusters): 4096 x 4096 4x1 6.8, 1x4 7.1, 2x2 7.9; 10240 x 8192 1x2 15.8, 2x1 17.6, 4x1
-// 18.9, 1x1 28; 57344 x 8192 1x1 56, 1x2 57, 2x1 62; 1024 x 16384 4x4 8.5, 1x8 11.
+// Rows alone where they make enough blocks; else columns are split: in two by a cluster (three
+// where all run at once), further among the four warps of a block first (no cluster to join), then
+// by clusters of up to eight.  Measured, us (one token, 64 columns a group; joined by warps x
+// clusters): 4096 x 4096 4x1 6.7, 1x4 7.0, 2x2 7.1; 10240 x 8192 1x2 15.4, 2x1 15.7, 1x1 18.9,
+// 4x1 19.9; 8192 x 28672 1x3 31.9, 1x2 34.6, 2x1 35.6; 57344 x 8192 gated 1x1 46.6, 2x1 50.8, 1x2
+// 55; 1024 x 16384 4x4 7.7, 1x8 9.0.
 FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
 {
     const int nt = tokens <= 8 ? 1 : 2;
@@ -43,7 +44,7 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
         return (int64_t)((rows + rb - 1) / rb) * split;
     };
     if (blocks(1, 1) >= kFewBlocks || chunks == 1) return plan(1, 1);
-    if (blocks(1, 2) >= kFewBlocks) return plan(1, 2);
+    if (blocks(1, 2) >= kFewBlocks) return plan(1, blocks(1, 3) <= kAtOnce && chunks > 2 ? 3 : 2);
     int wk = kWarps, split = 1;
     while (wk > 1 && plan(wk, split).smem > (size_t)kSmemPerSm / 2 - 2048) wk /= 2;
     while (split < 8 && blocks(wk, split) < kFewBlocks && wk * split * 2 <= chunks) split *= 2;
