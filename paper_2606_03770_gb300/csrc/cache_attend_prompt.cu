@@ -12,7 +12,7 @@
 // product).  A weight of 0 does not stop a NaN among the values, so values whose scale or
 // minimum is not finite are held back as zeros, and rows that do see their keys are made NaN.
 //
-// Bound by the instructions of a tile: 2,200 cycles, of which the weights' exponentials take
+// Bound by the instructions of a tile: 2,010 cycles, of which the weights' exponentials take
 // 1,024 of their unit's and the products 1,000 of the tensor cores'.  Measured (64 query heads
 // over 8, 128 elements, bf16): 1,152 queries x 2,304 keys 75 us (870 TFLOP/s, 45% of the
 // tensor cores' measured rate), 2,048 x 2,048 92 us, 4 x 256 x 4,096 148 us; 4,096 x 4,096 of 128
