@@ -110,7 +110,7 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
                    a->x, a->residual, a->y, a->x_stride, a->residual_stride, a->y_stride};
     if (a->tokens >= kMany) {
         const ManyPlan f = plan_many(outs, p.gated, w->cols, a->tokens, dev.sms);
-        if (f.tiles > 65535) return fail(E2_EINVAL, "too many tokens for one call");
+        if ((int64_t)f.row_tiles * f.tiles * 8 > 0x7fffffff) return fail(E2_EINVAL, "too many tokens for one call");
         return launch_many(p, f, workspace, outs, dev.id, static_cast<cudaStream_t>(stream));
     }
     const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr);

@@ -470,7 +470,8 @@ template <int G> int launch_few_group(const FewParams &q, const FewPlan &f, int 
 
 // The launch of a prompt (quant_matmul_many.cu).
 struct ManyPlan {
-    int tile, tiles, split, stages, depth;
+    int tile, tiles, row_tiles, split, stages, depth;
+    int whole, rest_split;                 // blocks unsplit, before the rest: whole turns (0: all alike)
     size_t image, workspace;
 };
 ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms);

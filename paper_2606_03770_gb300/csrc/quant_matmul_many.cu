@@ -11,11 +11,11 @@
 // eight), x is put into the same one.  Few rows are split over columns by the blocks of a
 // cluster, whose sums are joined in a fixed order through shared memory.
 //
-// Measured with 1,152 tokens: 8192 x 28672 407 us (1,331 TFLOP/s, 69% of the tensor cores'
-// measured rate; one call after another 483, where the power limit lowers the clock), 57344 x
-// 8192 gated 839 (1,291), 10240 x 8192 160 (1,207), 4096 x 4096 52.  Lost: turns that do not come
-// out even on 152 multiprocessors (384 blocks are 2.5), and 430 cycles of unpacking a stage
-// where its products take 384.
+// Measured with 1,152 tokens: 8192 x 28672 404 us (1,340 TFLOP/s, 70% of the tensor cores'
+// measured rate; one call after another 456, where the power limit lowers the clock), 57344 x
+// 8192 gated 841 (1,286), 10240 x 8192 161 (1,200), 4096 x 4096 49.  Lost: turns that do not come
+// out even on 152 multiprocessors, 430 cycles of unpacking a stage where the products of fewer
+// than 215 tokens take less, and a block's start and end, when its products rest.
 //
 // Every wait ends: one that takes too long marks the block as failed, which then waits
 // for its own copies, frees its tensor memory and writes NaN.
@@ -36,7 +36,8 @@ constexpr int kColumns = 512, kWeightColumns = 256, kWeightStages = 8;
 
 struct ManyParams {
     MatmulParams m;
-    int outs, tile, tiles, split, stages, depth;             // tokens of a tile; stages in flight
+    int outs, tile, row_tiles, split, stages, depth;         // tokens of a tile; stages in flight
+    int first;                                               // of the blocks (row tiles in turn, then tokens'), this launch's
     int scales_by;                                           // scales copied by a chunk's row, by 4 bytes, or one by one (2)
     uint8_t *prepared;                                 // [tiles][cols / 64][tile][128 bytes], then scales per token
     float *unscale;
@@ -102,7 +103,9 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
     __shared__ int failed;
     const MatmulParams &p = q.m;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int rank = blockIdx.x % q.split, block = blockIdx.x / q.split;
+    const int rank = blockIdx.x % q.split, block = (q.first + blockIdx.x / q.split) % q.row_tiles;
+    const int tile = (q.first + blockIdx.x / q.split) / q.row_tiles;
+    allow_next();
     const int rows_out = p.gated ? kTileRows / 2 : kTileRows;
     const uint32_t stage_bytes = (uint32_t)q.tile * 128;
     // this block's stages, whole chunks
@@ -130,7 +133,7 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
     if (warp == 0) {
         // x: a stage's image by one copy
         wait_before();
-        const uint8_t *from = q.prepared + ((size_t)blockIdx.y * q.stages + s0) * stage_bytes;
+        const uint8_t *from = q.prepared + ((size_t)tile * q.stages + s0) * stage_bytes;
         int i = 0, slot = 0, phase = 1;
         for (; i < n; ++i) {
             if (!__all_sync(~0u, barrier_wait(empty + 8 * slot, phase))) break;
@@ -287,7 +290,7 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
 
     // outputs: lanes are rows, columns tokens; the unpacking warps take them, four to 32 lanes.
     // A cluster's sums, and rows that are gated, go through shared memory: [tile][rows].
-    const int token0 = blockIdx.y * q.tile, live = min(q.tile, p.tokens - token0);
+    const int token0 = tile * q.tile, live = min(q.tile, p.tokens - token0);
     const float nan = __int_as_float(0x7fc00000);
     float *sums = reinterpret_cast<float *>(smem);
     const int quarter = warp % 4, row = 32 * quarter + lane;
@@ -357,13 +360,17 @@ template <int G, bool MINS> int launch_many_as(const ManyParams &q, const ManyPl
     if (int st = launch<ManyParams>(q.m.half ? image_kernel<__half> : image_kernel<__nv_bfloat16>,
                                     dim3((unsigned)q.m.tokens), 512, 0, 1, false, s, q))
         return st;
-    const int rows_out = q.m.gated ? kTileRows / 2 : kTileRows;
-    const dim3 grid((unsigned)((q.outs + rows_out - 1) / rows_out * q.split), (unsigned)q.tiles);
     // (never two blocks on a multiprocessor: tensor memory is for one)
     const size_t ring = (size_t)q.depth * q.tile * 128 + kRaw * Chunk<G, MINS>::kBytes + 1024;
-    const size_t sums = q.split > 1 ? (size_t)q.tile * kTileRows * 4 + 1024 : q.m.gated ? (size_t)q.tile * kTileRows * 2 + 1024 : 0;
+    const size_t sums = q.split > 1 || f.rest_split > 1 ? (size_t)q.tile * kTileRows * 4 + 1024 : q.m.gated ? (size_t)q.tile * kTileRows * 2 + 1024 : 0;
     const size_t smem = std::max(std::max(ring, sums), (size_t)kSmemPerSm / 2);
-    return launch<ManyParams>(kernel, grid, kThreads, smem, f.split, true, s, q);
+    const int blocks = q.row_tiles * f.tiles;
+    if (!f.whole) return launch<ManyParams>(kernel, dim3((unsigned)(blocks * f.split)), kThreads, smem, f.split, true, s, q);
+    if (int st = launch<ManyParams>(kernel, dim3((unsigned)f.whole), kThreads, smem, 1, true, s, q)) return st;
+    ManyParams rest = q;
+    rest.first = f.whole;
+    rest.split = f.rest_split;
+    return launch<ManyParams>(kernel, dim3((unsigned)((blocks - f.whole) * f.rest_split)), kThreads, smem, f.rest_split, true, s, rest);
 }
 
 template <int G> int launch_many_group(const ManyParams &q, const ManyPlan &f, int dev, cudaStream_t s)
@@ -375,34 +382,48 @@ template <int G> int launch_many_group(const ManyParams &q, const ManyPlan &f, i
 
 // The tile of tokens (a multiple of 16, up to 256) and the split over columns that
 // take the fewest turns of the multiprocessors times a turn's length: two cycles a token and
-// stage, no fewer than unpacking takes, and a fixed part.
+// stage, no fewer than unpacking takes, and a fixed part.  A last turn that would leave many
+// multiprocessors idle is split over columns instead, by a second launch.  Measured, us (all
+// alike / so): 8192 x 28672, 1,152 tokens 415 / 404 (one call after another 486 / 456), 28672 x 8192
+// 431 / 415; 5000 x 8192, 1,000 tokens 94 / 74; 20000 x 4096, 250 tokens 63 / 47.
 ManyPlan plan_many(int outs, bool gated, int cols, int tokens, int sms)
 {
     ManyPlan best{};
     double least = 1e300;
     const int rows_out = gated ? kTileRows / 2 : kTileRows, row_tiles = (outs + rows_out - 1) / rows_out, stages = (cols + kStageCols - 1) / kStageCols;
+    auto turn = [&](int tile, int split) {
+        const double stage = 2.0 * tile > 430.0 ? 2.0 * tile : 430.0;
+        return stage * ((stages + split - 1) / split) + 4000.0 + 12.0 * tile + (split > 1 ? 3000.0 + 16.0 * tile : 0.0);
+    };
+    auto consider = [&](double t, int tile, int tiles, int split, int whole, int rest) {
+        if (t >= least) return;
+        least = t;
+        const int fit = 140 * 1024 / (tile * 128);
+        best = ManyPlan{tile, tiles, row_tiles, split, stages, fit < kWeightStages ? fit : kWeightStages, whole, rest,
+                        (size_t)tiles * stages * tile * 128, 0};
+        best.workspace = best.image + (size_t)tokens * 4;
+    };
     for (int tile = 32; tile <= 256; tile += 16) {
         const int tiles = (tokens + tile - 1) / tile;
         if (tile > 32 && (tokens + tiles - 1) / tiles <= tile - 16) continue;                  // (a smaller one does as well)
         for (int split = 1; split <= kMostSplit; split *= 2) {
             if (split > 1 && stages / split < 8) continue;
-            const double turns = (double)(((int64_t)row_tiles * tiles * split + sms - 1) / sms);
-            const double stage = 2.0 * tile > 430.0 ? 2.0 * tile : 430.0;
-            const double t = turns * (stage * ((stages + split - 1) / split) + 4000.0 + 12.0 * tile + (split > 1 ? 3000.0 + 16.0 * tile : 0.0));
-            if (t < least) {
-                least = t;
-                const int fit = 140 * 1024 / (tile * 128);
-                best = ManyPlan{tile, tiles, split, stages, fit < kWeightStages ? fit : kWeightStages, (size_t)tiles * stages * tile * 128, 0};
-                best.workspace = best.image + (size_t)tokens * 4;
-            }
+            const double t = (double)(((int64_t)row_tiles * tiles * split + sms - 1) / sms) * turn(tile, split);
+            consider(t, tile, tiles, split, 0, 1);
         }
+        // whole turns unsplit, then what is left split over all multiprocessors
+        const int64_t blocks = (int64_t)row_tiles * tiles, whole = blocks / sms * sms;
+        int rest = 1;
+        while (rest < kMostSplit && (blocks - whole) * rest * 2 <= sms && stages / (rest * 2) >= 8) rest *= 2;
+        if (whole > 0 && rest > 1 && blocks > whole)
+            consider((double)(whole / sms) * turn(tile, 1) + turn(tile, rest) + 3000.0, tile, tiles, 1, (int)whole, rest);
     }
     return best;
 }
 
 int launch_many(const MatmulParams &m, const ManyPlan &f, void *workspace, int outs, int dev, cudaStream_t s)
 {
-    ManyParams q{m, outs, f.tile, f.tiles, f.split, f.stages, f.depth, 0, static_cast<uint8_t *>(workspace),
+    ManyParams q{m, outs, f.tile, f.row_tiles, f.split, f.stages, f.depth, 0, 0, static_cast<uint8_t *>(workspace),
                  reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + f.image)};
     // how a chunk's rows of scales are aligned
     const int wide = kChunkColumns / m.group * 2, groups = m.cols / m.group;

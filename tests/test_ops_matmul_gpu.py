@@ -162,3 +162,10 @@ def test_empty_and_refusals():
         ops.quant_matmul(x, odd, gated=True)
     with pytest.raises(ValueError, match="one column per"):
         ops.QuantWeight(w.codes, torch.ones(64, 16, device="cuda", dtype=HALF))
+
+
+@pytest.mark.parametrize("tokens,rows,cols,form", [(1150, 4001, 4096, {}), (250, 20000, 4096, dict(residual=True)),
+                                                   (230, 2 * 10100, 4096, dict(gated=True, mins=True))])
+def test_a_few_blocks_more_than_multiprocessors(tokens, rows, cols, form):
+    check(tokens, rows, cols, **form)
+    check(tokens, rows, cols, dtype=HALF, **form)
