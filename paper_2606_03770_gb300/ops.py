@@ -133,12 +133,18 @@ def _stride(x):
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
-def _rows(x, name):
-    """Token stride of [tokens][heads][dim], whose heads lie side by side."""
-    tokens, heads, dim = x.shape
-    if heads > 1 and x.stride(1) != dim:
+def _heads(x, name, dtype, shape, device):
+    """Token stride of x [tokens, heads, dim], of one type and this shape, whose
+    heads lie side by side (a single token's does not matter)."""
+    if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.shape == shape and x.device == device):
+        _tensor(x, name, (dtype,), shape, device)
+    _, heads, dim = shape
+    token, head, element = x.stride()
+    if element != 1 and dim > 1:
+        _tensor(x, name, (dtype,), shape, device)
+    if head != dim and heads > 1:
         raise ValueError(f"{name}: a token's heads must lie side by side")
-    return x.stride(0) if tokens > 1 else heads * dim
+    return token if shape[0] > 1 else heads * dim
 
 
 def _stream(device):
@@ -225,12 +231,13 @@ def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
     if residual is not None:
         _like(residual, "residual", dtype, shape, dev)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=dev)
+        out, out_stride = torch.empty(shape, dtype=dtype, device=dev), outs
     else:
         _like(out, "out", dtype, shape, dev)
+        out_stride = _stride(out)
     a = e2_matmul_args(tokens, DTYPES[dtype], bool(gated), x.data_ptr(), _stride(x),
                        residual.data_ptr() if residual is not None else None,
-                       _stride(residual) if residual is not None else 0, out.data_ptr(), _stride(out))
+                       _stride(residual) if residual is not None else 0, out.data_ptr(), out_stride)
     if workspace is None:
         need = (_lib or load()).e2_quant_matmul_workspace(w.rows, w.cols, tokens)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
@@ -276,9 +283,11 @@ def cache_append(cache, k, v, slots, positions, cos, sin, q=None, q_out=None, in
     """Append keys (turned by their positions) and values [tokens, kv_heads,
     head_dim] at ``slots`` (int64; page * page_size + token in page; -1: none).
     Returns the turned queries (``q_out``, allocated unless given), or None."""
-    dev, D, dtype = cache.device, cache.head_dim, k.dtype
-    tokens = _tensor(k, "k", _HALF, (None, cache.kv_heads, D), dev)[0]
-    _like(v, "v", dtype, (tokens, cache.kv_heads, D), dev)
+    dev, D, H = cache.device, cache.head_dim, cache.kv_heads
+    if not (isinstance(k, torch.Tensor) and k.dtype in _HALF and k.dim() == 3):
+        _tensor(k, "k", _HALF, (None, H, D), dev)
+    dtype, tokens = k.dtype, k.shape[0]
+    ks, vs = (_heads(x, n, dtype, (tokens, H, D), dev) for x, n in ((k, "k"), (v, "v")))
     _like(slots, "slots", torch.int64, (tokens,), dev)
     _like(positions, "positions", torch.int32, (tokens,), dev)
     table_rows, half = _tensor(cos, "cos", (torch.float32,), (None, None), dev)
@@ -286,18 +295,20 @@ def cache_append(cache, k, v, slots, positions, cos, sin, q=None, q_out=None, in
     _need(cos.is_contiguous() and sin.is_contiguous(), "cos and sin must be contiguous")
     heads = qs = qos = 0
     if q is not None:
-        heads = _tensor(q, "q", (dtype,), (tokens, None, D), dev)[1]
+        if not (isinstance(q, torch.Tensor) and q.dim() == 3):
+            _tensor(q, "q", (dtype,), (tokens, None, D), dev)
+        heads = q.shape[1]
+        qs = _heads(q, "q", dtype, (tokens, heads, D), dev)
         if q_out is None:
             q_out = torch.empty((tokens, heads, D), dtype=dtype, device=dev)
+            qos = heads * D
         else:
-            _like(q_out, "q_out", dtype, (tokens, heads, D), dev)
-        qs, qos = _rows(q, "q"), _rows(q_out, "q_out")
+            qos = _heads(q_out, "q_out", dtype, (tokens, heads, D), dev)
     else:
         _need(q_out is None, "q_out without q")
     a = e2_append_args(tokens, DTYPES[dtype], heads, 2 * half, bool(interleaved), table_rows, slots.data_ptr(),
-                       positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), k.data_ptr(), _rows(k, "k"),
-                       v.data_ptr(), _rows(v, "v"), q.data_ptr() if heads else None, qs,
-                       q_out.data_ptr() if heads else None, qos)
+                       positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs,
+                       q.data_ptr() if heads else None, qs, q_out.data_ptr() if heads else None, qos)
     _call("e2_cache_append", dev, cache.ref, C.byref(a))
     return q_out
 
@@ -325,7 +336,10 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
     largest counts of queries and of cached tokens, are read from the device
     (a synchronisation) unless given.  scale: 1/sqrt(head_dim) unless given."""
     dev = cache.device
-    tokens, heads, _ = _tensor(q, "q", _HALF, (None, None, cache.head_dim), dev)
+    if not (isinstance(q, torch.Tensor) and q.dtype in _HALF and q.dim() == 3):
+        _tensor(q, "q", _HALF, (None, None, cache.head_dim), dev)
+    tokens, heads, _ = shape = (q.shape[0], q.shape[1], cache.head_dim)
+    q_stride = _heads(q, "q", q.dtype, shape, dev)
     batch, cols = _tensor(table, "table", (torch.int32,), (None, None), dev)
     _like(lens, "lens", torch.int32, (batch,), dev)
     _like(starts, "starts", torch.int32, (batch + 1,), dev)
@@ -335,13 +349,14 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
         max_len = int(lens.max()) if batch else 0
     if out is None:
         # (tokens outside every request are not written)
-        out = (torch.empty if batch else torch.zeros)((tokens, heads, cache.head_dim), dtype=q.dtype, device=dev)
+        out = (torch.empty if batch else torch.zeros)(shape, dtype=q.dtype, device=dev)
+        out_stride = heads * cache.head_dim
     else:
-        _like(out, "out", q.dtype, (tokens, heads, cache.head_dim), dev)
+        out_stride = _heads(out, "out", q.dtype, shape, dev)
     a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), cols, _stride(table),
                        lens.data_ptr(), starts.data_ptr(), max_new, max_len,
-                       cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), _rows(q, "q"),
-                       out.data_ptr(), _rows(out, "out"))
+                       cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), q_stride,
+                       out.data_ptr(), out_stride)
     if workspace is None:
         need = (_lib or load()).e2_cache_attend_workspace(cache.ref, C.byref(a))
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
