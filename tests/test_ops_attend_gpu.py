@@ -250,3 +250,31 @@ def test_empty_and_refusals():
     with pytest.raises(e2ga.E2Error, match="16-byte"):
         ops.cache_attend(cache, torch.zeros(3, 260, device="cuda", dtype=BF)[:, 1:257].unflatten(1, (4, 64)), table, lens,
                          starts, **kw)
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_prompts_longer_than_the_launch_was_told(dtype):
+    from paper_2606_03770_gb300 import ops
+    s = setup([400, 90, 700], [130, 1, 300], 2, 8, 128, 64, dtype)
+    want, lim, _ = R.attend(*s, 128 ** -0.5, 0)
+    for new in (10, 33, 100):                        # several blocks of rows in turn
+        R.close(ops.cache_attend(*s, max_new=new, max_len=700), want, lim, new)
+
+
+@pytest.mark.parametrize("B,length,window", [(2, 2000, 0), (1, 900, 0), (6, 1100, 400), (9, 300, 0), (24, 257, 0)])
+@pytest.mark.parametrize("new", [1, 2])
+def test_parts_joined_in_a_cluster(B, length, window, new):
+    lens = [length - 37 * b % length for b in range(B)]
+    check(lens, [min(new, n) for n in lens], 4, 8, 128, 16, window=window)
+    check(lens, [min(new, n) for n in lens], 3, 5, 64, 64, dtype=HALF, window=window)
+
+
+@pytest.mark.parametrize("length", [700, 5000])
+def test_nan_in_one_part_reaches_its_heads_only(length):
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([length, 40], [1, 1], 2, 4, 128, 64)
+    a = ops.cache_attend(cache, q, table, lens, starts, max_new=1, max_len=length)
+    cache.v_scales[int(table[0, length // 128]), 0, 5, :, 1] = math.nan     # a key near the middle, first KV head
+    b = ops.cache_attend(cache, q, table, lens, starts, max_new=1, max_len=length)
+    assert bool(torch.isnan(b[0, :4]).all())
+    assert torch.equal(a[0, 4:], b[0, 4:]) and torch.equal(a[1], b[1])
