@@ -213,3 +213,21 @@ def test_refusals():
         ops.cache_read(cache, slots.int())
     k0 = k[:0]
     assert ops.cache_append(cache, k0, k0, slots[:0], pos[:0], cos, sin, q=k0).shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("unit", [1.0, 0.75, 3.0, 2.0 ** -14, 5.0 * 2.0 ** 8])
+def test_quotients_at_and_beside_halves(dtype, unit):
+    """Groups whose quotients are whole numbers, halves and the numbers next to them."""
+    from paper_2606_03770_gb300 import ops
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k = torch.randint(0, 31, (96, 2, 128), generator=g, device="cuda") * 0.5
+    k[:, :, 0::64], k[:, :, 1::64] = 0.0, 15.0
+    v = (k * unit).to(dtype)
+    k = k.to(dtype)
+    step = torch.randint(-1, 2, v.shape, generator=g, device="cuda").to(torch.int16)
+    step[(v == 0) | (step < 0) & (v == v.amax())] = 0
+    v = (v.view(torch.int16) + step).view(dtype)
+    cache = ops.Cache.empty(3, 32, 2, 128)
+    slots, pos = torch.arange(96, device="cuda"), torch.zeros(96, device="cuda", dtype=torch.int32)
+    check(cache, k, v, slots, pos, *table(4, 128))
