@@ -14,9 +14,9 @@
 //
 // Bound by the instructions of a tile: 2,010 cycles, of which the weights' exponentials take
 // 1,024 of their unit's and the products 1,000 of the tensor cores'.  Measured (64 query heads
-// over 8, 128 elements, bf16): 1,152 queries x 2,304 keys 75 us (870 TFLOP/s, 45% of the
-// tensor cores' measured rate), 2,048 x 2,048 92 us, 4 x 256 x 4,096 148 us; 4,096 x 4,096 of 128
-// heads 580 us (949 TFLOP/s).  The longest blocks of all heads come first (127 us for 142, a step before).
+// over 8, 128 elements, bf16): 1,152 queries x 2,304 keys 74 us (880 TFLOP/s, 46% of the
+// tensor cores' measured rate), 2,048 x 2,048 90 us, 4 x 256 x 4,096 147 us; 4,096 x 4,096 of 128
+// heads 573 us (959 TFLOP/s).  The longest blocks of all heads come first (127 us for 142, a step before).
 //
 // Every wait ends: one that takes too long marks the block as failed, which then frees
 // its tensor memory and writes NaN.
@@ -144,12 +144,15 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     const bool live = slab.live(p, row);
     const int64_t token = slab.token(row);
     const int head = slab.head(kv, row);
+    // rows as whole lines, a lane an octet: this warp's 32 rows, kAtOnce at a time; and their place in shared memory
+    constexpr int kOctets = D / 8, kAtOnce = 32 / kOctets, kLoads = 32 / kAtOnce;
+    auto place = [&](int r, int o) {
+        return reinterpret_cast<uint4 *>(m.queries + g * Sh::kQuery + o / 8 * kGroupRows * 128 + r * 128 + ((o % 8) ^ (r & 7)) * 16);
+    };
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     float scale;
     {
-        // the queries, to fp16 times a power of two each (and the scale's sign): this warp's 32
-        // rows, kAtOnce at a time, a lane an octet
-        constexpr int kOctets = D / 8, kAtOnce = 32 / kOctets, kLoads = 32 / kAtOnce;
+        // the queries, to fp16 times a power of two each (and the scale's sign)
         const int64_t mine = live ? token * p.q_stride + head * D : -1;
         const int o = lane % kOctets;
         int power = 0;
@@ -170,8 +173,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
                 for (int k = 1; k < kOctets; k *= 2) top = max(top, __shfl_xor_sync(~0u, top, k));
                 const int k = power_for<T>(top), theirs = __shfl_sync(~0u, k, lane % kAtOnce * kOctets);
                 if (lane / kAtOnce == turn) power = theirs;
-                *reinterpret_cast<uint4 *>(m.queries + g * Sh::kQuery + o / 8 * kGroupRows * 128 + to * 128 + ((o % 8) ^ (to & 7)) * 16) =
-                    octet_in_order<T>(v[i], p.scale < 0 ? -power_of_two(k) : power_of_two(k));
+                *place(to, o) = octet_in_order<T>(v[i], p.scale < 0 ? -power_of_two(k) : power_of_two(k));
             }
         }
         scale = fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
@@ -295,14 +297,14 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
 #pragma unroll
         for (int k = 0; k < 32; ++k) x[k / 8 * 8 + k % 8 / 2 + k % 2 * 4] = __uint_as_float(v[k]);
         const bool none = lost || (spoilt >> (c / E2_CACHE_GROUP) & 1);
-        if (live && p.splits == 1) {
-            T *out = static_cast<T *>(p.out) + token * p.out_stride + head * D + c;
+        if (p.splits == 1) {
+            // (the queries' place: this group's last scores are there)
 #pragma unroll
             for (int o = 0; o < 4; ++o) {
                 float y[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) y[k] = none ? nan : sum > 0 ? x[8 * o + k] * inverse : sum;
-                *reinterpret_cast<uint4 *>(out + 8 * o) = pack8<T>(y);
+                *place(r, c / 8 + o) = pack8<T>(y);
             }
         } else if (live) {
             float *to = p.parts + ((token * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2);
@@ -313,6 +315,15 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         __syncwarp();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if (p.splits == 1) {
+        const int64_t mine = live ? token * p.out_stride + head * D : -1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int from = i * kAtOnce + lane / kOctets, o = lane % kOctets;
+            const int64_t at = __shfl_sync(~0u, mine, from);
+            if (at >= 0) reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + at)[o] = *place(32 * quarter + from, o);
+        }
+    }
 }
 
 // Warp w of four, for keys (which 0) or values (1): its 16 of a tile's 64, dequantised.
