@@ -307,7 +307,8 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                         const float was = top[n][e], is = fmaxf(was, x);
                         const float f = was == is || was == -INFINITY ? (was == is ? 1.0f : 0.0f) : power2(was - is);
                         top[n][e] = is;
-                        limit[n][e] = q_scale[n][e] > 0 ? (is + 2.0f) / q_scale[n][e] : INFINITY;
+                        // (a column that has seen nothing takes its first score whatever the scale, 0 too)
+                        limit[n][e] = is == -INFINITY ? -INFINITY : q_scale[n][e] > 0 ? (is + 2.0f) / q_scale[n][e] : INFINITY;
                         sum[n][e] *= f;
 #pragma unroll
                         for (int j = 0; j < GR; ++j) low[n][j][e] *= f;

@@ -278,3 +278,26 @@ def test_nan_in_one_part_reaches_its_heads_only(length):
     b = ops.cache_attend(cache, q, table, lens, starts, max_new=1, max_len=length)
     assert bool(torch.isnan(b[0, :4]).all())
     assert torch.equal(a[0, 4:], b[0, 4:]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("length", [331, 333, 340, 700])
+@pytest.mark.parametrize("scale,size", [(0.0, 1.0), (1e-38, 1e-9)])
+def test_scores_of_zero_with_windows(length, scale, size):
+    """Scores that are 0, or too small for 32 bits: every key seen counts alike, also in rows to which
+    a warp's first tile is hidden (a launch told of short contexts: several tiles a warp)."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([length], [16], 2, 1, 64, 16)
+    q *= size
+    for window in (270, 300, 316):
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=16, max_len=1, scale=scale, window=window)
+        R.close(out, *R.attend(cache, q, table, lens, starts, scale, window)[:2], window)
+
+
+@pytest.mark.parametrize("new,G", [(1, 8), (2, 4), (16, 1), (40, 2)])
+def test_scores_of_zero_with_pages_that_are_not_there(new, G):
+    from paper_2606_03770_gb300 import ops
+    for missing in (1, 4):
+        cache, q, table, lens, starts = setup([700], [new], 2, G, 128, 32)
+        table[0, :missing] = -1
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=1, scale=0.0)
+        R.close(out, *R.attend(cache, q, table, lens, starts, 0.0, 0)[:2], missing)
