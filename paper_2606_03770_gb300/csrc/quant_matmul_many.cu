@@ -43,6 +43,26 @@ struct ManyParams {
     float *unscale;
 };
 
+// Whether eight codes times d plus m stay within fp16's range, for two d and m (NaN: no).
+template <bool MINS> __device__ __forceinline__ bool in_range(__half2 d, __half2 m)
+{
+    // (rounded as the weights are: what rounds to 65,504 here does there)
+    const __half2 most = MINS ? __hfma2(__habs2(d), __float2half2_rn(15.0f), __habs2(m)) : __hmul2(__habs2(d), __float2half2_rn(8.0f));
+    return __hble2(most, __float2half2_rn(65504.0f));
+}
+
+// Weights that became infinite are fp16's largest, unless d or m is not finite itself.
+__device__ __forceinline__ void limit_weights(uint32_t *w, __half d, __half m)
+{
+    const __half largest(65504.0f);
+    const __half2 most = __float2half2_rn(__hle(__habs(d), largest) && __hle(__habs(m), largest) ? 65504.0f : INFINITY);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const __half2 y = __hmin2_nan(__hmax2_nan(*reinterpret_cast<const __half2 *>(&w[i]), __hneg2(most)), most);
+        w[i] = *reinterpret_cast<const uint32_t *>(&y);
+    }
+}
+
 // A word's eight codes, less 8 where there are no minima, times d plus m.
 template <bool MINS> __device__ __forceinline__ void scale_word(uint32_t *out, uint32_t w, __half2 d, __half2 m)
 {
@@ -254,20 +274,25 @@ template <int G, bool MINS> __global__ void __launch_bounds__(kThreads, 1) many_
             const __half *sc = reinterpret_cast<const __half *>(chunk + Ch::kCodes + r * (Ch::kPer * 2));
             const __half *mn = sc + kTileRows * Ch::kPer;
             const int g0 = team * kStageCols / G, g1 = (team * kStageCols + 32) / G;
+            const __half d0 = sc[g0], d1 = sc[g1], m0 = MINS ? mn[g0] : __half(0.0f), m1 = MINS ? mn[g1] : __half(0.0f);
             uint32_t v[32];
             {
-                const __half2 ds = __half2half2(sc[g0]), ms = __half2half2(MINS ? mn[g0] : __half(0.0f));
+                const __half2 ds = __half2half2(d0), ms = __half2half2(m0);
                 scale_word<MINS>(&v[0], w0.x, ds, ms);
                 scale_word<MINS>(&v[4], w0.y, ds, ms);
                 scale_word<MINS>(&v[8], w0.z, ds, ms);
                 scale_word<MINS>(&v[12], w0.w, ds, ms);
             }
             {
-                const __half2 ds = __half2half2(sc[g1]), ms = __half2half2(MINS ? mn[g1] : __half(0.0f));
+                const __half2 ds = __half2half2(d1), ms = __half2half2(m1);
                 scale_word<MINS>(&v[16], w1.x, ds, ms);
                 scale_word<MINS>(&v[20], w1.y, ds, ms);
                 scale_word<MINS>(&v[24], w1.z, ds, ms);
                 scale_word<MINS>(&v[28], w1.w, ds, ms);
+            }
+            if (!__all_sync(~0u, in_range<MINS>(__halves2half2(d0, d1), __halves2half2(m0, m1)))) {
+                limit_weights(&v[0], d0, m0);
+                limit_weights(&v[16], d1, m1);
             }
             ok = __all_sync(~0u, barrier_wait(empty + 8 * here, round));
             if (ok) {

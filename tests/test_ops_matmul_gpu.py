@@ -169,3 +169,40 @@ def test_empty_and_refusals():
 def test_a_few_blocks_more_than_multiprocessors(tokens, rows, cols, form):
     check(tokens, rows, cols, **form)
     check(tokens, rows, cols, dtype=HALF, **form)
+
+
+@pytest.mark.parametrize("tokens", [3, 16, 17, 40, 200])
+@pytest.mark.parametrize("mins", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_weights_beyond_fp16(tokens, mins, group):
+    """Scales and minima whose weights pass 65,504: as they are for a few tokens, no larger than
+    that from 17 on."""
+    from paper_2606_03770_gb300 import ops
+    w, g = make(130, 512, group, mins)
+    w.scales[::3] = 9000.0
+    w.scales[1::5] = -12000.0
+    if mins:
+        w.mins[::2], w.mins[1::2] = 60000.0, -65504.0
+    x = randn(g, tokens, 512)
+    x[0, :7] = 0
+    W, X = R.weight(w), x.double()
+    if tokens >= 17:
+        W = W.clamp(-65504.0, 65504.0)
+    want = X @ W.T
+    off = (2.0 ** -11 + 512 * R.EPS32) * (X.abs() @ W.abs().T)
+    R.close(ops.quant_matmul(x, w), want, off + R.EPS[BF] * (want.abs() + off))
+
+
+@pytest.mark.parametrize("tokens", [2, 30])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_scales_that_are_not_finite_stay_in_their_rows(tokens, value):
+    from paper_2606_03770_gb300 import ops
+    for mins in (False, True):
+        w, g = make(70, 256, 64, mins)
+        x = randn(g, tokens, 256)
+        y0 = ops.quant_matmul(x, w)
+        (w.mins if mins else w.scales)[3, 1] = value
+        y = ops.quant_matmul(x, w)
+        assert not bool(torch.isfinite(y[:, 3]).any())
+        rest = torch.arange(70, device="cuda") != 3
+        assert torch.equal(y[:, rest], y0[:, rest])
