@@ -58,8 +58,9 @@ typedef struct {
  * row stride a multiple of 8.  Sums are in 32 bits, y is rounded once; x goes to
  * the tensor cores as fp16 times a power of two per token (values below 2^-24 of the
  * token's largest lose bits).  From 17 tokens on W does too, rounded once to fp16
- * (2^-12 of a weight; what passes 65,504 stays there).  y may not overlap x or
- * the weights; it may be residual itself.
+ * (2^-12 of a weight; what passes 65,504 stays there).  An x that is infinite or
+ * NaN gives the formula's infinities and NaN, in its own row of y only.  y may not
+ * overlap x or the weights; it may be residual itself.
  * workspace: e2_quant_matmul_workspace() bytes (0: may be NULL), 256-byte
  * aligned, contents of no consequence. */
 typedef struct {

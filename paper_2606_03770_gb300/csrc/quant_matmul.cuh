@@ -92,6 +92,26 @@ __device__ __forceinline__ void finish(const MatmulParams &p, int token, int row
     else finish_as<__nv_bfloat16>(p, token, row, a, b);
 }
 
+// What a token's infinities and NaN among columns col0..col1 - 1 make of a row's sum (the finite
+// ones do not matter then).  The kernel's own sums are NaN there: they hold code x and 8 x apart.
+static __device__ __noinline__ float sum_not_finite(const uint8_t *codes, const __half *scales, const __half *mins, const void *x,
+                                                    int half, int group, int col0, int col1)
+{
+    float sum = 0;
+    for (int c = col0; c < col1; c += 8) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + c);
+        const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t bits = words[j / 2] >> (16 * (j % 2)) & 0xffffu;
+            const float f = half ? __half2float(__ushort_as_half((uint16_t)bits)) : __uint_as_float(bits << 16);
+            if (fabsf(f) < INFINITY) continue;
+            const float code = (float)(codes[(c + j) / 2] >> (4 * (j % 2)) & 15), d = __half2float(scales[c / group]);
+            sum += f * (mins ? __fmaf_rn(d, code, __half2float(mins[c / group])) : d * (code - 8.0f));
+        }
+    }
+    return sum;
+}
+
 // Bytes of 8 nt prepared tokens.
 __host__ __device__ constexpr size_t prepared_bytes(int nt, int x_pad, int group)
 {
@@ -385,10 +405,33 @@ __global__ void __launch_bounds__(32 * kWarps, 3) few_kernel(const FewParams q)
             }
         }
     }
+    float largest_unscale = 0;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[n][e] = y[n][e] * 0x1p24f * unscale[min(8 * n + 2 * t + e % 2, nt - 1)];
+        for (int e = 0; e < 4; ++e) {
+            const float f = unscale[min(8 * n + 2 * t + e % 2, nt - 1)];
+            y[n][e] = y[n][e] * 0x1p24f * f;
+            largest_unscale = fmaxf(largest_unscale, f);
+        }
+    // (no power of two of finite values is as large; one of the warps that share the rows looks)
+    if (largest_unscale > 0x1p113f) {
+#pragma unroll 1
+        for (int i = 0; i < 4 * NT; ++i) {
+            const int tok = min(8 * (i / 4) + 2 * t + i % 2, nt - 1);
+            if (!(unscale[tok] > 0x1p113f)) continue;
+            const int64_t row = row_of(g + 8 * (i / 2 % 2));
+            const float sum = wk ? 0.0f
+                                 : sum_not_finite(p.codes + row * (p.cols / 2), p.scales + row * groups, MINS ? p.mins + row * groups : nullptr,
+                                                  static_cast<const uint16_t *>(p.x) + tok * p.x_stride, p.half, G, c0 * kChunk,
+                                                  min(c1 * kChunk, p.cols));
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (4 * n + e == i) y[n][e] = sum;
+        }
+    }
 
     if (WK == 1 && q.split == 1) {
 #pragma unroll

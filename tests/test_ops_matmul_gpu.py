@@ -206,3 +206,27 @@ def test_scales_that_are_not_finite_stay_in_their_rows(tokens, value):
         assert not bool(torch.isfinite(y[:, 3]).any())
         rest = torch.arange(70, device="cuda") != 3
         assert torch.equal(y[:, rest], y0[:, rest])
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 16, 17, 200])
+@pytest.mark.parametrize("mins", [False, True])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("rows,cols,gated", [(70, 512, False), (33, 8192, False), (66, 1088, True), (8000, 4096, False)])
+def test_infinities_of_x_are_the_formulas(tokens, mins, dtype, rows, cols, gated):
+    """Signed infinities, and NaN where signs meet or a weight is 0, whatever the tokens."""
+    from paper_2606_03770_gb300 import ops
+    w, g = make(rows, cols, 64, mins)
+    if mins:
+        w.mins[:, 0] = -4 * w.scales[:, 0]             # weights of 0
+    x = randn(g, tokens, cols, dtype=dtype)
+    x[0, 5] = math.inf
+    if tokens > 4:
+        x[1, cols - 1] = -math.inf
+        x[2, 40], x[2, 41] = math.inf, -math.inf
+        x[3, 9], x[3, 10] = math.inf, math.nan
+        x[4, 9], x[4, cols // 2] = math.inf, math.inf
+    r = randn(g, tokens, rows // 2 if gated else rows, dtype=dtype)
+    want, lim = R.matmul(x, w, r, gated)
+    assert bool((want[0] == math.inf).any()) and bool(torch.isnan(want[0]).any())
+    assert gated or bool((want[0] == -math.inf).any())
+    R.close(ops.quant_matmul(x, w, residual=r, gated=gated), want, lim)
