@@ -131,7 +131,9 @@ class Measured:
 
 
 def measure(model, NP, ND, b_max, page=64, window=0, repeats=20):
-    """Run and time the block of `model` (a ``workloads.CONFIGS`` entry's)."""
+    """Run and time the block of `model` (a ``workloads.CONFIGS`` entry's, with 4-bit weights)."""
+    if model.get("wbits", 4) != 4:
+        raise ValueError(f"the block has 4-bit weights, the model {model['wbits']}-bit ones")
     block = Block(model["d"], model["ffn"], model["kv_heads"], model["vocab"], NP + ND + 1)
     pages = -(-(NP + ND) // page)
     cache = ops.Cache.empty(b_max * pages, page, block.kv_heads, block.D)
@@ -163,7 +165,8 @@ def as_device(prob, measured):
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    ap.add_argument("--config", default="c2", choices=[c for c in W.CONFIGS])
+    ap.add_argument("--config", default="c2", choices=[c for c, w in W.CONFIGS.items() if w["model"]["wbits"] == 4],
+                    help="a workload with 4-bit weights")
     ap.add_argument("--window", type=int, default=0, help="sliding window of the block (0: full attention)")
     ap.add_argument("--plan", action="store_true", help="search with this GPU in the place of the fleet's first device")
     ap.add_argument("--generations", type=int, default=10)
