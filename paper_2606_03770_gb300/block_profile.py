@@ -16,6 +16,7 @@ from __future__ import annotations
 import argparse
 import dataclasses
 
+import numpy as np
 import torch
 
 from . import ops
@@ -155,6 +156,25 @@ def measure(model, NP, ND, b_max, page=64, window=0, repeats=20):
     return out
 
 
+def planned(prob, model, window=0, group=64):
+    """`prob` with the work of the block that `measure` runs in place of its own: 4-bit weights
+    and a 4-bit cache, each with its scales, and at most `window` keys a token (0: all).  The
+    workloads count 4-bit weights without scales and an fp16 cache."""
+    d = model["d"]
+    d_kv = d if model["kv_heads"] is None else model["kv_heads"] * W.HEAD_DIM
+    params = 2 * d * d + 2 * d * d_kv + 3 * d * model["ffn"]
+    weights = params // 2 + params // group * 2
+    token = 2 * d_kv * (ops.E2_CACHE_GROUP // 2 + 4) // ops.E2_CACHE_GROUP       # keys and values
+    flops, moved = [], []
+    for v in range(prob.V):
+        tokens, length, requests = (prob.NP, prob.NP, 1) if v == 0 else (v, prob.NP + prob.ND, v)
+        seen = min(length, window) if window else length
+        flops.append(2 * params * tokens + 4 * tokens * seen * d)
+        moved.append(weights + requests * seen * token)
+    u64 = lambda x: np.array(x, dtype=np.uint64)
+    return dataclasses.replace(prob, blk_flops=u64(flops), blk_bytes=u64(moved), blk_mem=u64(moved))
+
+
 def as_device(prob, measured):
     """(rate, bandwidth) for which the planner's stage time of one block,
     max(flops / rate, bytes / bandwidth), is the measured prefill time and the
@@ -171,7 +191,7 @@ def main(argv=None):
     ap.add_argument("--plan", action="store_true", help="search with this GPU in the place of the fleet's first device")
     ap.add_argument("--generations", type=int, default=10)
     a = ap.parse_args(argv)
-    prob = W.make_config(a.config)
+    prob = planned(W.make_config(a.config), W.CONFIGS[a.config]["model"], a.window)
     m = measure(W.CONFIGS[a.config]["model"], prob.NP, prob.ND, prob.b_max, window=a.window)
     rate, bw = as_device(prob, m)
     print(f"{a.config}: block of width {W.CONFIGS[a.config]['model']['d']}, prompt {prob.NP}, context {prob.NP + prob.ND}")

@@ -12,3 +12,33 @@ def test_models_with_other_weights_are_refused(capsys):
     with pytest.raises(SystemExit):
         P.main(["--config", "c1_tiny"])
     assert "c1_tiny" in capsys.readouterr().err
+
+
+@pytest.mark.parametrize("config", ["c2", "c4"])
+def test_the_plan_counts_the_work_that_is_timed(config):
+    """Bytes of the block's tensors and of the cache's tokens, as the operators lay them out."""
+    prob, model = W.make_config(config), W.CONFIGS[config]["model"]
+    got = P.planned(prob, model)
+    d, ffn, kv = model["d"], model["ffn"], model["kv_heads"] * W.HEAD_DIM
+    weights = sum(rows * (cols // 2 + cols // 64 * 2) for rows, cols in ((d + 2 * kv, d), (d, d), (2 * ffn, d), (d, ffn)))
+    token = 2 * model["kv_heads"] * (W.HEAD_DIM // 2 + W.HEAD_DIM // 64 * 4)
+    ctx = prob.NP + prob.ND
+    assert int(got.blk_bytes[0]) == weights + prob.NP * token
+    for b in range(1, prob.V):
+        assert int(got.blk_bytes[b]) == int(got.blk_mem[b]) == weights + b * ctx * token
+    assert (got.blk_flops == prob.blk_flops).all() and got.PF is None
+    assert (prob.blk_bytes == W.make_config(config).blk_bytes).all()          # (a copy)
+    # a window: what the workloads with two types of blocks count for the sliding one
+    few = P.planned(prob, model, window=128)
+    two = W.make_config(config, layered="alternate")
+    assert [int(f) for f in few.blk_flops] == [int(f) for f in two.PF[:, 1]]
+    assert int(few.blk_bytes[3]) == weights + 3 * 128 * token and int(few.blk_bytes[0]) == weights + 128 * token
+
+
+def test_main_plans_with_the_work_that_is_timed(monkeypatch, capsys):
+    """The printed bandwidth is bytes that the measured block moves over its time."""
+    monkeypatch.setattr(P, "measure", lambda model, NP, ND, b_max, window=0: P.Measured([1e-3] * 9, [1e-4] * 9, NP, ND))
+    for window in (0, 128):
+        P.main(["--config", "c2", "--window", str(window)])
+        prob = P.planned(W.make_config("c2"), W.CONFIGS["c2"]["model"], window)
+        assert f"{float(prob.blk_bytes[8]) / 1e-3 / 1e9:.0f} GB/s" in capsys.readouterr().out
