@@ -176,11 +176,19 @@ def planned(prob, model, window=0, group=64):
 
 
 def as_device(prob, measured):
-    """(rate, bandwidth) for which the planner's stage time of one block,
-    max(flops / rate, bytes / bandwidth), is the measured prefill time and the
-    measured decode time of the largest batch."""
+    """(rate, bandwidth) of the device: the flops of a prefill over its measured
+    time, the bytes of the largest decode batch over its.  ``planner_times`` has
+    what the planner makes of them."""
     b = prob.b_max
     return float(prob.blk_flops[0]) / measured.block[0], float(prob.blk_bytes[b]) / measured.block[b]
+
+
+def planner_times(prob, rate, bw):
+    """The planner's stage time of one block, max(flops / rate, bytes / bandwidth), per
+    variant.  With ``as_device``'s rates it is the measured one of the prefill and of the
+    largest batch unless the other term is the larger there; the batches between
+    follow from the bandwidth alone."""
+    return [max(float(f) / rate, float(y) / bw) for f, y in zip(prob.blk_flops, prob.blk_bytes)]
 
 
 def main(argv=None):
@@ -195,9 +203,14 @@ def main(argv=None):
     m = measure(W.CONFIGS[a.config]["model"], prob.NP, prob.ND, prob.b_max, window=a.window)
     rate, bw = as_device(prob, m)
     print(f"{a.config}: block of width {W.CONFIGS[a.config]['model']['d']}, prompt {prob.NP}, context {prob.NP + prob.ND}")
-    print(f"{'':12s}{'block us':>10s}{'head us':>10s}")
-    for v, (t, h) in enumerate(zip(m.block, m.head)):
-        print(f"{'prefill' if v == 0 else f'decode {v}':12s}{t * 1e6:10.1f}{h * 1e6:10.1f}")
+    times = planner_times(prob, rate, bw)
+    print(f"{'':12s}{'block us':>10s}{'planner':>10s}{'head us':>10s}")
+    for v, (t, s, h) in enumerate(zip(m.block, times, m.head)):
+        print(f"{'prefill' if v == 0 else f'decode {v}':12s}{t * 1e6:10.1f}{s * 1e6:10.1f}{h * 1e6:10.1f}")
+    for v in (0, prob.b_max):
+        if times[v] > 1.01 * m.block[v]:
+            print(f"no rate and bandwidth give both measured times: the planner takes {times[v] * 1e6:.1f} us for "
+                  f"{'the prefill' if v == 0 else f'decode {v}'}")
     print(f"as a device of the planner: {rate / 1e12:.1f} TFLOP/s, {bw / 1e9:.0f} GB/s")
     if a.plan:
         from .e2ga import Engine

@@ -42,3 +42,21 @@ def test_main_plans_with_the_work_that_is_timed(monkeypatch, capsys):
         P.main(["--config", "c2", "--window", str(window)])
         prob = P.planned(W.make_config("c2"), W.CONFIGS["c2"]["model"], window)
         assert f"{float(prob.blk_bytes[8]) / 1e-3 / 1e9:.0f} GB/s" in capsys.readouterr().out
+
+
+@pytest.mark.parametrize("prefill,decode,said", [(2e-3, 2e-4, []), (1e-4, 2e-4, ["the prefill"]), (2e-3, 2.5e-1, ["the prefill"]),
+                                                 (9.0, 1e-6, ["decode 8"])])
+def test_what_the_planner_makes_of_the_rates(prefill, decode, said, monkeypatch, capsys):
+    """Measured times come back where their own term is the larger; where the other one is, it is said."""
+    prob = P.planned(W.make_config("c2"), W.CONFIGS["c2"]["model"])
+    block = [prefill] + [decode * b / 8 for b in range(1, 9)]
+    monkeypatch.setattr(P, "measure", lambda model, NP, ND, b_max, window=0: P.Measured(block, [1e-4] * 9, NP, ND))
+    rate, bw = P.as_device(prob, P.measure(None, prob.NP, prob.ND, 8))
+    times = P.planner_times(prob, rate, bw)
+    assert times[0] == pytest.approx(max(prefill, float(prob.blk_bytes[0]) / bw))
+    assert times[8] == pytest.approx(max(decode, float(prob.blk_flops[8]) / rate))
+    assert (times[0] == pytest.approx(prefill)) == ("the prefill" not in said)
+    assert (times[8] == pytest.approx(decode)) == ("decode 8" not in said)
+    P.main(["--config", "c2"])
+    out = capsys.readouterr().out
+    assert [w for w in ("the prefill", "decode 8") if f"us for {w}" in out] == said
