@@ -215,6 +215,7 @@ def main(argv=None):
     if a.plan:
         from .e2ga import Engine
         prob.rate[0], prob.bw[0] = rate, bw
+        torch.cuda.empty_cache()             # (the measured block's memory is free again)
         prob.mem[0] = torch.cuda.mem_get_info()[0]
         eng = Engine(prob)
         eng.init_population(seed=2026)

@@ -84,3 +84,42 @@ def test_measure_and_plan(capsys):
     rate, bw = P.as_device(prob, m)
     assert abs(float(prob.blk_flops[0]) / rate - m.block[0]) < 1e-9
     assert abs(float(prob.blk_bytes[2]) / bw - m.block[2]) < 1e-9
+
+
+def test_plan_with_this_device(monkeypatch, capsys):
+    """Measured and planned with from the command line: the fleet's first device has the measured
+    rates and all memory that is free."""
+    from paper_2606_03770_gb300 import block_profile as P
+    from paper_2606_03770_gb300 import e2ga
+    from paper_2606_03770_gb300 import workloads as W
+    seen = []
+
+    class Engine(e2ga.Engine):
+        def __init__(self, prob, *args, **kw):
+            torch.cuda.empty_cache()
+            seen.append((prob, torch.cuda.mem_get_info()[0]))
+            super().__init__(prob, *args, **kw)
+
+    monkeypatch.setattr(e2ga, "Engine", Engine)
+    P.main(["--config", "c2", "--plan", "--generations", "2"])
+    out = capsys.readouterr().out
+    prob, free = seen[0]
+    assert f"{prob.rate[0] / 1e12:.1f} TFLOP/s, {prob.bw[0] / 1e9:.0f} GB/s" in out
+    assert (prob.rate[1:] == W.make_config("c2").rate[1:]).all()
+    assert free - int(prob.mem[0]) < 1 << 26
+    assert "best plan after 2 generations" in out and "inf" not in out and "nan" not in out
+
+
+def test_planned_bytes_are_the_blocks():
+    from paper_2606_03770_gb300 import block_profile as P
+    from paper_2606_03770_gb300 import ops
+    from paper_2606_03770_gb300 import workloads as W
+    prob, model = W.make_config("c2"), W.CONFIGS["c2"]["model"]
+    block = P.Block(model["d"], model["ffn"], model["kv_heads"], 64, 8)
+    held = sum(t.numel() * t.element_size() for w in (block.w_qkv, block.w_out, block.w_gate_up, block.w_down)
+               for t in (w.codes, w.scales))
+    cache = ops.Cache.empty(1, 16, block.kv_heads, block.D)
+    token = sum(t.numel() * t.element_size() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)) // 16
+    got = P.planned(prob, model)
+    assert int(got.blk_bytes[0]) == held + prob.NP * token
+    assert int(got.blk_bytes[5]) == held + 5 * (prob.NP + prob.ND) * token
