@@ -75,7 +75,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
         const int last = (int)min((int64_t)C, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
         const int lo = p.window > 0 ? (int)max(slab.pos(0) - p.window + 1, (int64_t)0) : 0;
-        const int hi = (int)min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
+        const int hi = (int)max(min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0), (int64_t)0);
         const int tile_lo = lo / kTile, tiles = hi > lo ? (hi + kTile - 1) / kTile - tile_lo : 0;
         const int units = (tiles + kFewWarps - 1) / kFewWarps, per = (units + p.splits - 1) / p.splits * kFewWarps;
         const int first = (int)min((int64_t)tile_lo + (int64_t)split * per, (int64_t)tile_lo + tiles);
@@ -136,7 +136,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int row = 8 * n + g;
-            const bool live = slab.live(p, row);
+            const bool live = slab.live(row);
             const T *src = static_cast<const T *>(p.q) + (live ? slab.token(row) * p.q_stride + slab.head(kv, row) * D : 0);
             unsigned top = 0;
             uint4 qf[U];
@@ -169,8 +169,8 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
 #pragma unroll
                 for (int j = 0; j < GR; ++j) q_sum[n][j][e] = __shfl_sync(~0u, sum[j], (2 * t + e) * 4);
                 const int at = 8 * n + 2 * t + e;
-                const bool seen = slab.live(p, at);
-                seen_hi[n][e] = seen ? (int)slab.pos(at) : -1;
+                const bool seen = slab.live(at);
+                seen_hi[n][e] = seen ? (int)max(slab.pos(at), (int64_t)-1) : -1;
                 seen_lo[n][e] = seen && p.window > 0 ? (int)max(slab.pos(at) - p.window + 1, (int64_t)0) : 0;
             }
         }
@@ -178,7 +178,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
         // tiles in this range need no mask for any column
         const int full_lo = p.window > 0 ? (int)max(slab.pos(last) - p.window + 1, (int64_t)0) : 0;
         const int full_hi = (int)max(slab.pos(0), (int64_t)-1);
-        const bool all_live = C <= slab.left && slab.live(p, 0) && slab.live(p, last);
+        const bool all_live = C <= slab.left;
 
         float o[U][2][NT][4] = {};                       // sums for dimensions 32 u + 4 g + {0, 1}, {2, 3}
         float low[NT][GR][2] = {}, sum[NT][2] = {};      // minima's sums, weights' sums: this lane's keys
@@ -425,7 +425,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
         float *shared_parts = reinterpret_cast<float *>(smem) + kFewWarps * (C * (D + 3));
         for (int i = threadIdx.x; i < C * D; i += 32 * kFewWarps) {
             const int c = i / D, d = i % D;
-            if (!slab.live(p, c)) continue;
+            if (!slab.live(c)) continue;
             const float *all = reinterpret_cast<const float *>(smem);
             float best = -INFINITY, total = 0, x = 0;
 #pragma unroll
@@ -456,7 +456,7 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             const uint32_t part_at = smem_addr(shared_parts);
             for (int i = threadIdx.x + split * 32 * kFewWarps; i < C * D; i += 32 * kFewWarps * p.splits) {
                 const int c = i / D, d = i % D;
-                if (!slab.live(p, c)) continue;
+                if (!slab.live(c)) continue;
                 float tops[kMostCluster], weights[kMostCluster], x[kMostCluster], best = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < kMostCluster; ++k) {
@@ -489,7 +489,6 @@ template <class T, int D> __global__ void __launch_bounds__(128) join_kernel(con
     const Rows rows(p, request);
     for (int64_t row = blockIdx.x; row < rows.count; row += gridDim.x) {
         const Slab slab(rows, row);
-        if (!slab.live(p, 0)) continue;
         const int head = slab.head(kv, 0);
         const float *from = p.parts + (slab.token(0) * p.q_heads + head) * p.splits * (D + 2);
         // every warp: the maximum, the parts' factors, the weights' sum

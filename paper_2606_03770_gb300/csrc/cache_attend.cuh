@@ -21,17 +21,19 @@ struct AttendParams {
 };
 
 // One request and KV head: its queries, times the query heads that share the KV head,
-// are rows, row = query * share + head.
+// are rows, row = query * share + head.  Queries that are not tokens of q (`starts` out of
+// range) are none of them; the others keep their positions, which may be far below 0.
 struct Rows {
     int start, share;
     int64_t count, first_pos;                // rows; position of the first query
     __device__ Rows(const AttendParams &p, int request)
     {
-        start = p.starts[request];
+        const int64_t from = p.starts[request], to = p.starts[request + 1];
+        const int64_t first = max(from, (int64_t)0), end = min(to, (int64_t)p.tokens);
+        start = (int)min(first, (int64_t)p.tokens);
         share = p.q_heads / p.kv_heads;
-        const int64_t queries = (int64_t)p.starts[request + 1] - start;
-        count = queries > 0 ? queries * share : 0;
-        first_pos = p.lens[request] - (queries > 0 ? queries : 0);
+        count = end > first ? (end - first) * share : 0;
+        first_pos = p.lens[request] - (to - first);
     }
 };
 
@@ -48,7 +50,7 @@ struct Slab {
     __device__ int64_t pos(int c) const { return first_pos + query + (over + c) / share; }
     __device__ int64_t token(int c) const { return start + query + (over + c) / share; }
     __device__ int head(int kv, int c) const { return (int)(kv * share + (over + c) % share); }
-    __device__ bool live(const AttendParams &p, int c) const { return c < left && token(c) >= 0 && token(c) < p.tokens; }
+    __device__ bool live(int c) const { return c < left; }
 };
 
 __device__ __forceinline__ float power2(float x)

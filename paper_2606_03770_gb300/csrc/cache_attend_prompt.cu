@@ -51,7 +51,7 @@ struct Span {
         const int last = (int)min((int64_t)kPromptRows, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
         lo = p.window > 0 ? (int)max(slab.pos(0) - p.window + 1, (int64_t)0) : 0;
-        hi = (int)min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0);
+        hi = (int)max(min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0), (int64_t)0);
         const int tile_lo = lo / kKeys, tiles = hi > lo ? (hi + kKeys - 1) / kKeys - tile_lo : 0;
         const int per = (tiles + p.splits - 1) / p.splits;
         first = (int)min((int64_t)tile_lo + (int64_t)blockIdx.z * per, (int64_t)tile_lo + tiles);
@@ -141,7 +141,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     const int r = 32 * quarter + lane;
     const int row = g * kGroupRows + r;
     const Slab &slab = span.slab;
-    const bool live = slab.live(p, row);
+    const bool live = slab.live(row);
     const int64_t token = slab.token(row);
     const int head = slab.head(kv, row);
     // rows as whole lines, a lane an octet: this warp's 32 rows, kAtOnce at a time; and their place in shared memory

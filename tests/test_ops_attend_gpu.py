@@ -301,3 +301,37 @@ def test_scores_of_zero_with_pages_that_are_not_there(new, G):
         table[0, :missing] = -1
         out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=1, scale=0.0)
         R.close(out, *R.attend(cache, q, table, lens, starts, 0.0, 0)[:2], missing)
+
+
+LOW, HIGH = -2 ** 31, 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("new", [3, 40, 100])
+@pytest.mark.parametrize("length", [LOW, LOW + 1, -1, HIGH - 64, HIGH])
+def test_lengths_at_the_ends_of_their_type(length, new, dtype):
+    """Below 0 nothing is seen; beyond the table all that it has."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([150, 90], [new, 2], 2, 4, 64, 16, dtype, extra_cols=1)
+    lens[0] = length
+    for window in (0, 70):
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=150, window=window)
+        R.close(out, *R.attend(cache, q, table, lens, starts, 0.125, window)[:2], window)
+        assert length > 0 or bool((out[:new] == 0).all())
+
+
+@pytest.mark.parametrize("tokens", [2, 50, 200])
+@pytest.mark.parametrize("starts", [(LOW, HIGH), (0, HIGH), (LOW, 30), (LOW, -5), (HIGH - 3, HIGH), (20, LOW), (HIGH, LOW), (-7, 13)])
+def test_starts_at_the_ends_of_their_type(starts, tokens):
+    """Queries outside q are none; those inside keep their positions."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, _ = setup([150], [tokens], 2, 4, 128, 16)
+    starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    for length in (150, HIGH, LOW):
+        lens[0] = length
+        want, lim, written = R.attend(cache, q, table, lens, starts, 128 ** -0.5, 0)
+        for new in (1, 30, 120):
+            out = torch.full_like(q, 9.0)
+            ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=150, out=out)
+            R.close(out[written], want[written], lim[written], (length, new))
+            assert bool((out[~written] == 9).all())
