@@ -165,12 +165,31 @@ def _call(name, device, *args):
         raise e2ga.E2Error(status, name, load().e2_ops_error().decode())
 
 
+class _Handle:
+    """What holds tensors and the struct that the library takes of them.  The struct has
+    their addresses and sizes, so nothing is assigned once it is made."""
+
+    def _hold(self, *tensors):
+        """Views of its own, and the memory whatever becomes of any view."""
+        self._memory = [x.untyped_storage() for x in tensors if x is not None]
+        return [x.detach() if x is not None else None for x in tensors]
+
+    def __setattr__(self, name, value):
+        if "ref" in self.__dict__:
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be changed: make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{type(self).__name__}.{name} cannot be deleted")
+
+
 # ---- products with 4-bit weights --------------------------------------------------
-class QuantWeight:
+class QuantWeight(_Handle):
     """4-bit weights [rows][cols]: ``codes`` uint8 [rows, cols / 2] (column 2j
     in the low four bits), ``scales`` float16 [rows, cols / group] and, for
     scale * code + min instead of scale * (code - 8), ``mins`` like scales.
-    Holds views of the tensors, no copies."""
+    Holds views of the tensors, no copies: what is written into them counts, other
+    tensors need another QuantWeight."""
 
     def __init__(self, codes, scales, mins=None):
         _tensor(codes, "codes", (torch.uint8,), (None, None))
@@ -184,7 +203,7 @@ class QuantWeight:
         if mins is not None:
             _tensor(mins, "mins", (torch.float16,), (rows, groups), codes.device)
         self.rows, self.cols, self.group, self.device = rows, cols, cols // groups, codes.device
-        self.codes, self.scales, self.mins = codes, scales, mins
+        self.codes, self.scales, self.mins = self._hold(codes, scales, mins)
         self.struct = e2_quant_weight(rows, cols, self.group, codes.data_ptr(), scales.data_ptr(),
                                       mins.data_ptr() if mins is not None else None)
         self.ref = C.byref(self.struct)
@@ -247,10 +266,11 @@ def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
 
 
 # ---- the cache ------------------------------------------------------------------------
-class Cache:
+class Cache(_Handle):
     """A paged 4-bit cache over four tensors: codes uint8
     [pages, kv_heads, page_size, head_dim / 2] and scales float16
-    [pages, kv_heads, page_size, head_dim / 64, 2] of keys and of values."""
+    [pages, kv_heads, page_size, head_dim / 64, 2] of keys and of values.  Holds
+    views of them: what is written into them counts, others need another Cache."""
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
         _tensor(k_codes, "k_codes", (torch.uint8,), (None,) * 4)
@@ -264,7 +284,7 @@ class Cache:
             _need(x.is_contiguous(), "cache tensors must be contiguous")
         self.pages, self.kv_heads, self.page_size, self.head_dim = pages, heads, page, 2 * half
         self.device = k_codes.device
-        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = self._hold(k_codes, k_scales, v_codes, v_scales)
         self.struct = e2_cache(pages, page, heads, 2 * half, k_codes.data_ptr(), k_scales.data_ptr(),
                                v_codes.data_ptr(), v_scales.data_ptr())
         self.ref = C.byref(self.struct)

@@ -231,3 +231,25 @@ def test_quotients_at_and_beside_halves(dtype, unit):
     cache = ops.Cache.empty(3, 32, 2, 128)
     slots, pos = torch.arange(96, device="cuda"), torch.zeros(96, device="cuda", dtype=torch.int32)
     check(cache, k, v, slots, pos, *table(4, 128))
+
+
+def test_a_cache_keeps_the_memory_it_points_at():
+    from paper_2606_03770_gb300 import ops
+    cache = ops.Cache.empty(2, 16, 2, 64)
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales", "pages", "kv_heads", "page_size", "head_dim", "device",
+                 "struct", "ref"):
+        with pytest.raises(AttributeError, match="Cache"):
+            setattr(cache, name, getattr(cache, name))
+    with pytest.raises(AttributeError, match="Cache"):
+        del cache.v_scales
+    given = [t.clone() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+    other = ops.Cache(*given)
+    for t in given:
+        t.data = torch.ones_like(t)
+    slots = torch.arange(32, device="cuda")
+    k, v = randn(1, 32, 2, 64), randn(2, 32, 2, 64)
+    for c in (cache, other):
+        ops.cache_append(c, k, v, slots, torch.zeros(32, device="cuda", dtype=torch.int32), *table(4, 64))
+    for a, b in zip(ops.cache_read(cache, slots), ops.cache_read(other, slots)):
+        assert torch.equal(a, b)
+    assert all(bool((t == 1).all()) for t in given)

@@ -230,3 +230,26 @@ def test_infinities_of_x_are_the_formulas(tokens, mins, dtype, rows, cols, gated
     assert bool((want[0] == math.inf).any()) and bool(torch.isnan(want[0]).any())
     assert gated or bool((want[0] == -math.inf).any())
     R.close(ops.quant_matmul(x, w, residual=r, gated=gated), want, lim)
+
+
+def test_weights_keep_the_memory_they_point_at():
+    """Nothing is assigned once they are made; other tensors behind the given ones do not matter."""
+    from paper_2606_03770_gb300 import ops
+    w, g = make(64, 256, 64, True)
+    x = randn(g, 3, 256)
+    y = ops.quant_matmul(x, w)
+    for name in ("codes", "scales", "mins", "rows", "cols", "group", "device", "struct", "ref", "other"):
+        with pytest.raises(AttributeError, match="QuantWeight"):
+            setattr(w, name, getattr(w, name, None))
+    with pytest.raises(AttributeError, match="QuantWeight"):
+        del w.codes
+    given = [t.clone() for t in (w.codes, w.scales, w.mins)]
+    v = ops.QuantWeight(*given)
+    for t in given + [v.scales]:
+        t.data = torch.zeros_like(t)
+    del given
+    filler = [torch.full((64, 128), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    assert torch.equal(y, ops.quant_matmul(x, v)) and len(filler) == 64
+    w.scales.mul_(2)                                  # written in place: counts
+    w.mins.mul_(2)
+    R.close(ops.quant_matmul(x, w), *R.matmul(x, w))
