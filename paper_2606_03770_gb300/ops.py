@@ -14,7 +14,8 @@ precisions the deployment search plans with:
 Each function checks its tensors, allocates outputs that are not given, and
 enqueues on the current stream of the tensors' device.  Formulas, layouts and what
 happens to values out of range are in include/e2ops.h.  There is no CPU
-fallback: without the library, or with tensors off the GPU, the calls raise.
+fallback: without the library, or with tensors off the GPU, the calls raise.  Nor are
+there gradients: a tensor that requires one is refused while gradients are recorded.
 """
 from __future__ import annotations
 
@@ -124,6 +125,16 @@ def _like(x, name, dtype, shape, device):
         _tensor(x, name, (dtype,), shape, device)
 
 
+def _no_gradient(handle, **tensors):
+    """The operators have no gradients: what requires one is refused, not left without."""
+    if handle is not None and handle.requires_grad:
+        raise ValueError(f"{type(handle).__name__} was made of tensors that require gradients; there are none here "
+                         "(torch.no_grad(), or detach them)")
+    for name, x in tensors.items():
+        if x is not None and x.requires_grad:
+            raise ValueError(f"{name} requires a gradient; there are none here (torch.no_grad(), or detach it)")
+
+
 _HALF = (torch.float16, torch.bfloat16)
 _FLOAT = (torch.float16, torch.bfloat16, torch.float32)
 
@@ -171,6 +182,7 @@ class _Handle:
 
     def _hold(self, *tensors):
         """Views of its own, and the memory whatever becomes of any view."""
+        self.requires_grad = any(x.requires_grad for x in tensors if x is not None)
         self._memory = [x.untyped_storage() for x in tensors if x is not None]
         return [x.detach() if x is not None else None for x in tensors]
 
@@ -254,6 +266,9 @@ def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
     else:
         _like(out, "out", dtype, shape, dev)
         out_stride = _stride(out)
+    if torch.is_grad_enabled() and (w.requires_grad or x.requires_grad or out.requires_grad
+                                    or residual is not None and residual.requires_grad):
+        _no_gradient(w, x=x, residual=residual, out=out)
     a = e2_matmul_args(tokens, DTYPES[dtype], bool(gated), x.data_ptr(), _stride(x),
                        residual.data_ptr() if residual is not None else None,
                        _stride(residual) if residual is not None else 0, out.data_ptr(), out_stride)
@@ -326,6 +341,9 @@ def cache_append(cache, k, v, slots, positions, cos, sin, q=None, q_out=None, in
             qos = _heads(q_out, "q_out", dtype, (tokens, heads, D), dev)
     else:
         _need(q_out is None, "q_out without q")
+    if torch.is_grad_enabled() and (cache.requires_grad or k.requires_grad or v.requires_grad or cos.requires_grad
+                                    or sin.requires_grad or heads and (q.requires_grad or q_out.requires_grad)):
+        _no_gradient(cache, k=k, v=v, q=q, q_out=q_out, cos=cos, sin=sin)
     a = e2_append_args(tokens, DTYPES[dtype], heads, 2 * half, bool(interleaved), table_rows, slots.data_ptr(),
                        positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs,
                        q.data_ptr() if heads else None, qs, q_out.data_ptr() if heads else None, qos)
@@ -341,6 +359,8 @@ def cache_read(cache, slots, dtype=torch.bfloat16):
     shape = (tokens, cache.kv_heads, cache.head_dim)
     k = torch.empty(shape, dtype=dtype, device=dev)
     v = torch.empty(shape, dtype=dtype, device=dev)
+    if torch.is_grad_enabled() and cache.requires_grad:
+        _no_gradient(cache)
     row = shape[1] * shape[2]
     _call("e2_cache_read", dev, cache.ref, slots.data_ptr(), tokens, DTYPES[dtype], k.data_ptr(), row, v.data_ptr(),
           row)
@@ -373,6 +393,8 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
         out_stride = heads * cache.head_dim
     else:
         out_stride = _heads(out, "out", q.dtype, shape, dev)
+    if torch.is_grad_enabled() and (cache.requires_grad or q.requires_grad or out.requires_grad):
+        _no_gradient(cache, q=q, out=out)
     a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), cols, _stride(table),
                        lens.data_ptr(), starts.data_ptr(), max_new, max_len,
                        cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), q_stride,
@@ -396,6 +418,8 @@ def token_logprobs(logits, tokens=None, top=0, entropy=True):
     _need(0 <= top <= E2_MAX_TOP, f"top must be in 0..{E2_MAX_TOP}")
     if tokens is not None:
         _like(tokens, "tokens", torch.int32, (rows,), dev)
+    if torch.is_grad_enabled() and logits.requires_grad:
+        _no_gradient(None, logits=logits)
     f32 = dict(dtype=torch.float32, device=dev)
     logprob = torch.empty(rows, **f32) if tokens is not None else None
     ent = torch.empty(rows, **f32) if entropy else None

@@ -335,3 +335,17 @@ def test_starts_at_the_ends_of_their_type(starts, tokens):
             ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=150, out=out)
             R.close(out[written], want[written], lim[written], (length, new))
             assert bool((out[~written] == 9).all())
+
+
+def test_gradients_are_refused():
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([20], [3], 2, 2, 64, 16)
+    kw = dict(max_new=3, max_len=20)
+    out = ops.cache_attend(cache, q, table, lens, starts, **kw)
+    grad = q.clone().requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        ops.cache_attend(cache, grad, table, lens, starts, **kw)
+    with pytest.raises(ValueError, match="gradient"):
+        ops.cache_attend(cache, q, table, lens, starts, out=grad, **kw)
+    with torch.no_grad():
+        assert torch.equal(out, ops.cache_attend(cache, grad, table, lens, starts, **kw))

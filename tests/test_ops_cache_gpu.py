@@ -253,3 +253,20 @@ def test_a_cache_keeps_the_memory_it_points_at():
     for a, b in zip(ops.cache_read(cache, slots), ops.cache_read(other, slots)):
         assert torch.equal(a, b)
     assert all(bool((t == 1).all()) for t in given)
+
+
+def test_gradients_are_refused():
+    from paper_2606_03770_gb300 import ops
+    cache = ops.Cache.empty(1, 16, 2, 64)
+    k, (cos, sin) = randn(1, 3, 2, 64), table(4, 64)
+    slots, pos = torch.arange(3, device="cuda"), torch.zeros(3, device="cuda", dtype=torch.int32)
+    ok = dict(k=k, v=k, cos=cos, sin=sin, q=k, q_out=k.clone())
+    for name in ok:
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            ops.cache_append(cache, slots=slots, positions=pos, **dict(ok, **{name: ok[name].clone().requires_grad_()}))
+    other = ops.Cache(cache.k_codes, cache.k_scales.clone().requires_grad_(), cache.v_codes, cache.v_scales)
+    with pytest.raises(ValueError, match="gradient"):
+        ops.cache_read(other, slots)
+    with torch.no_grad():
+        ops.cache_append(cache, slots=slots, positions=pos, **{n: t.clone().requires_grad_() for n, t in ok.items()})
+    assert bool((cache.k_codes[0, :, :3] != 0).any())

@@ -136,3 +136,14 @@ def test_empty_and_refusals():
         ops.token_logprobs(x[:, :0], tokens)
     with pytest.raises(e2ga.E2Error, match="stride"):
         ops.token_logprobs(x[:1].expand(2, 100), tokens)
+
+
+def test_gradients_are_refused():
+    from paper_2606_03770_gb300 import ops
+    x, tokens = logits(4, 300, F32)
+    lp = ops.token_logprobs(x, tokens)[0]
+    grad = x.clone().requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        ops.token_logprobs(grad, tokens)
+    with torch.no_grad():
+        assert torch.equal(lp, ops.token_logprobs(grad, tokens)[0])

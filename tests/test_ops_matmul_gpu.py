@@ -253,3 +253,19 @@ def test_weights_keep_the_memory_they_point_at():
     w.scales.mul_(2)                                  # written in place: counts
     w.mins.mul_(2)
     R.close(ops.quant_matmul(x, w), *R.matmul(x, w))
+
+
+def test_gradients_are_refused():
+    from paper_2606_03770_gb300 import ops
+    w, g = make(64, 256, 64, False)
+    x, r = randn(g, 2, 256), randn(g, 2, 64)
+    y = ops.quant_matmul(x, w, residual=r)
+    v = ops.QuantWeight(w.codes, w.scales.clone().requires_grad_())
+    xg, rg = x.clone().requires_grad_(), r.clone().requires_grad_()
+    for args, kw in (((xg, w), {}), ((x, w), dict(residual=rg)), ((x, w), dict(out=rg)), ((x, v), {})):
+        with pytest.raises(ValueError, match="gradient"):
+            ops.quant_matmul(*args, **kw)
+    with torch.no_grad():
+        assert torch.equal(y, ops.quant_matmul(xg, v, residual=rg))
+    with torch.inference_mode():
+        assert torch.equal(y, ops.quant_matmul(x.clone(), w, residual=r.clone()))
