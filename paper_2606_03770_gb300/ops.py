@@ -195,6 +195,17 @@ class _Handle:
         raise AttributeError(f"{type(self).__name__}.{name} cannot be deleted")
 
 
+def _workspace(name, device, *args):
+    """A workspace of the size that a function of the library says for `device`, None for 0."""
+    f = getattr(_lib or load(), name)
+    if torch._C._cuda_getDevice() == device.index:
+        need = f(*args)
+    else:
+        with torch.cuda.device(device):
+            need = f(*args)
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+
 # ---- products with 4-bit weights --------------------------------------------------
 class QuantWeight(_Handle):
     """4-bit weights [rows][cols]: ``codes`` uint8 [rows, cols / 2] (column 2j
@@ -273,8 +284,7 @@ def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
                        residual.data_ptr() if residual is not None else None,
                        _stride(residual) if residual is not None else 0, out.data_ptr(), out_stride)
     if workspace is None:
-        need = (_lib or load()).e2_quant_matmul_workspace(w.rows, w.cols, tokens)
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        workspace = _workspace("e2_quant_matmul_workspace", dev, w.rows, w.cols, tokens)
     _call("e2_quant_matmul", dev, w.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
           workspace.numel() if workspace is not None else 0)
     return out
@@ -400,8 +410,7 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
                        cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), q_stride,
                        out.data_ptr(), out_stride)
     if workspace is None:
-        need = (_lib or load()).e2_cache_attend_workspace(cache.ref, C.byref(a))
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        workspace = _workspace("e2_cache_attend_workspace", dev, cache.ref, C.byref(a))
     _call("e2_cache_attend", dev, cache.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
           workspace.numel() if workspace is not None else 0)
     return out

@@ -63,3 +63,45 @@ def test_host_tensors_are_refused():
         ops.Cache.empty(2, 16, 1, 64, device="cpu")
     with pytest.raises(ValueError, match="on the GPU"):
         ops.token_logprobs(z(2, 8))
+
+
+def test_workspaces_are_sized_on_the_tensors_device(monkeypatch):
+    """The plan goes by the current device's multiprocessors: the tensors' device is the current one then."""
+    from paper_2606_03770_gb300 import ops
+    current, asked = [0], []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: asked.append((name, args, current[0])) or 0
+
+    class On:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.device.index
+
+        def __exit__(self, *error):
+            current[0] = self.before
+
+    monkeypatch.setattr(ops, "_lib", Library())
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", On)
+    for index in (0, 2):
+        assert ops._workspace("e2_quant_matmul_workspace", torch.device("cuda", index), 5, 64, 1) is None
+        assert asked.pop() == ("e2_quant_matmul_workspace", (5, 64, 1), index) and current == [0]
+
+
+@pytest.mark.gpu
+def test_calls_ask_for_workspaces_there(monkeypatch):
+    from paper_2606_03770_gb300 import ops
+    asked = []
+    real = ops._workspace
+    monkeypatch.setattr(ops, "_workspace", lambda name, device, *args: asked.append((name, device)) or real(name, device, *args))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    w = ops.quantize_weight(torch.randn(64, 64, device="cuda"))
+    ops.quant_matmul(torch.zeros(40, 64, device="cuda", dtype=torch.float16), w)
+    cache = ops.Cache.empty(64, 64, 1, 64)
+    ops.cache_attend(cache, torch.zeros(1, 8, 64, device="cuda", dtype=torch.float16), torch.zeros(1, 64, **i32),
+                     torch.full((1,), 4096, **i32), torch.tensor([0, 1], **i32), max_new=1, max_len=4096)
+    assert asked == [("e2_quant_matmul_workspace", w.device), ("e2_cache_attend_workspace", cache.device)]
