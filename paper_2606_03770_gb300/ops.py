@@ -30,6 +30,7 @@ E2_F16, E2_BF16, E2_F32 = 0, 1, 2
 E2_CACHE_GROUP, E2_MAX_TOP, E2_MAX_COLS = 64, 32, 1 << 20
 DTYPES = {torch.float16: E2_F16, torch.bfloat16: E2_BF16, torch.float32: E2_F32}
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
+_MOST = 2 ** 31 - 1                        # of a c_int32, which takes larger numbers without their high bits
 
 
 class e2_quant_weight(C.Structure):
@@ -406,8 +407,8 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
     if torch.is_grad_enabled() and (cache.requires_grad or q.requires_grad or out.requires_grad):
         _no_gradient(cache, q=q, out=out)
     a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), cols, _stride(table),
-                       lens.data_ptr(), starts.data_ptr(), max_new, max_len,
-                       cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), q_stride,
+                       lens.data_ptr(), starts.data_ptr(), min(max_new, _MOST), min(max_len, _MOST),
+                       cache.head_dim ** -0.5 if scale is None else scale, max(-1, min(window, _MOST)), q.data_ptr(), q_stride,
                        out.data_ptr(), out_stride)
     if workspace is None:
         workspace = _workspace("e2_cache_attend_workspace", dev, cache.ref, C.byref(a))

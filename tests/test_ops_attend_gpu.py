@@ -349,3 +349,17 @@ def test_gradients_are_refused():
         ops.cache_attend(cache, q, table, lens, starts, out=grad, **kw)
     with torch.no_grad():
         assert torch.equal(out, ops.cache_attend(cache, grad, table, lens, starts, **kw))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_windows_and_hints_beyond_32_bits(new):
+    """They are as large as any context, not what is left of them in 32 bits."""
+    from paper_2606_03770_gb300 import e2ga, ops
+    s = setup([300, 90], [new, 1], 2, 4, 64, 16)
+    want = ops.cache_attend(*s, max_new=new, max_len=300)
+    for big in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 5, 2 ** 40):
+        assert torch.equal(want, ops.cache_attend(*s, max_new=new, max_len=300, window=big)), big
+        R.close(ops.cache_attend(*s, max_new=big, max_len=big), *R.attend(*s, 0.125, 0)[:2], big)
+    for small in (-1, -2 ** 31 - 1, -2 ** 32 + 7):
+        with pytest.raises(e2ga.E2Error, match="window"):
+            ops.cache_attend(*s, max_new=new, max_len=300, window=small)
