@@ -395,9 +395,9 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
     _like(lens, "lens", torch.int32, (batch,), dev)
     _like(starts, "starts", torch.int32, (batch + 1,), dev)
     if max_new is None:
-        max_new = int((starts[1:] - starts[:-1]).max()) if batch else 0
+        max_new = max(0, int((starts[1:].long() - starts[:-1].long()).max())) if batch else 0
     if max_len is None:
-        max_len = int(lens.max()) if batch else 0
+        max_len = max(0, int(lens.max())) if batch else 0
     if out is None:
         # (tokens outside every request are not written)
         out = (torch.empty if batch else torch.zeros)(shape, dtype=q.dtype, device=dev)

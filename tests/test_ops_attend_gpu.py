@@ -363,3 +363,18 @@ def test_windows_and_hints_beyond_32_bits(new):
     for small in (-1, -2 ** 31 - 1, -2 ** 32 + 7):
         with pytest.raises(e2ga.E2Error, match="window"):
             ops.cache_attend(*s, max_new=new, max_len=300, window=small)
+
+
+@pytest.mark.parametrize("starts", [(1, 0), (LOW, HIGH), (7, 7)])
+@pytest.mark.parametrize("length", [-20, 20])
+def test_hints_are_read_from_any_lengths(starts, length):
+    """Counts below 0 are none, those beyond 32 bits are not taken for such."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, _ = setup([20], [3], 2, 4, 64, 16)
+    lens[0] = length
+    starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 9.0)
+    ops.cache_attend(cache, q, table, lens, starts, out=out)
+    want, lim, written = R.attend(cache, q, table, lens, starts, 0.125, 0)
+    R.close(out[written], want[written], lim[written])
+    assert bool((out[~written] == 9).all())
