@@ -40,8 +40,9 @@ struct Sums {
 };
 
 // Maxima from here on (in magnitude) do not go through c: its rounding, a power of two
-// in every w, would grow with it.
-constexpr float kHuge = 65536.0f;
+// in every w, would grow with it.  Below, it is 2^-18 at most, and that is what sums of one kind
+// are off by when they are brought to a maximum of the other.
+constexpr float kHuge = 64.0f;
 
 __device__ __forceinline__ float power2(float x)
 {

@@ -147,3 +147,15 @@ def test_gradients_are_refused():
         ops.token_logprobs(grad, tokens)
     with torch.no_grad():
         assert torch.equal(lp, ops.token_logprobs(grad, tokens)[0])
+
+
+@pytest.mark.parametrize("at", [64.0, -64.0, 256.0, 65536.0, -65536.0])
+def test_logits_on_both_sides_of_a_power_of_two(at):
+    """Where a row's maxima, in different lanes, are on both sides of what sums are kept apart by."""
+    x = torch.full((5, 3000), -math.inf, device="cuda")
+    x[0, 5], x[0, 700] = at - 0.5, at + 0.25
+    x[1, 5], x[1, 6], x[1, 2900] = at - 0.25, at + 0.25, at
+    x[2, ::3], x[2, 1::3] = at - 0.125, at + 0.5
+    x[3, 0], x[3, 2999] = at + 0.5, at - 0.125
+    x[4] = at + torch.randn(3000, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    check(x, torch.tensor([5, 6, 0, 0, 17], device="cuda", dtype=torch.int32), 4)
