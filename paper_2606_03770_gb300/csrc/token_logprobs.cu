@@ -280,7 +280,7 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
         float e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = -INFINITY;
-        if (tail + lane < p.vocab) e[0] = to_float(x[tail + lane]);
+        if (lane < p.vocab - tail) e[0] = to_float(x[tail + lane]);
         take(e, [&](int) { return tail + lane; });
     }
 

@@ -159,3 +159,21 @@ def test_logits_on_both_sides_of_a_power_of_two(at):
     x[3, 0], x[3, 2999] = at + 0.5, at - 0.125
     x[4] = at + torch.randn(3000, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
     check(x, torch.tensor([5, 6, 0, 0, 17], device="cuda", dtype=torch.int32), 4)
+
+
+@pytest.mark.parametrize("vocab", [2 ** 31 - 1, 2 ** 31 - 8])
+def test_a_vocabulary_at_the_end_of_its_type(vocab):
+    """A row of 4.3 GB: its first and last elements, and what lies behind it, which is not its own."""
+    from paper_2606_03770_gb300 import ops
+    row = torch.full((1, 2 ** 31 + 64), -math.inf, device="cuda", dtype=BF)
+    row[:, vocab:] = 5.0
+    for at, value in ((0, 1.0), (3, 2.0), (vocab - 1, 3.0), (vocab - 2, 2.0), (vocab - 9, 0.5)):
+        row[0, at] = value
+    lp, ent, vals, ids = ops.token_logprobs(row[:, :vocab], torch.tensor([vocab - 1], device="cuda", dtype=torch.int32), top=6)
+    z = torch.tensor([3.0, 2.0, 2.0, 1.0, 0.5], dtype=torch.float64)
+    want = z - torch.logsumexp(z, 0)
+    assert ids[0].tolist() == [vocab - 1, 3, vocab - 2, 0, vocab - 9, -1]
+    # a handful of terms, each rounded a few times
+    assert torch.allclose(vals[0, :5].double().cpu(), want, rtol=0, atol=64 * R.EPS32) and float(vals[0, 5]) == -math.inf
+    assert abs(float(lp) - float(want[0])) < 64 * R.EPS32
+    assert abs(float(ent) + float((want.exp() * want).sum())) < 64 * R.EPS32
