@@ -41,7 +41,8 @@ const char *e2_ops_error(void);
  *
  * codes [rows][cols / 2]: column 2j in the low four bits of byte j, 2j + 1 in
  * the high ones; 16-byte aligned.  scales, mins: fp16 [rows][cols / group].
- * group is 32, 64 or 128; cols a multiple of group, up to E2_MAX_COLS. */
+ * group is 32, 64 or 128; cols a multiple of group, up to E2_MAX_COLS; rows, and
+ * the tokens of a call, up to 2^31 - 1024. */
 typedef struct {
     int32_t rows, cols, group;
     const uint8_t *codes;

@@ -56,6 +56,9 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
 // 4096 x 4096 12.5 / 11.
 constexpr int kMany = 17;
 
+// Rows and tokens of whole blocks are counted in 32 bits.
+constexpr int kMostRows = 0x7fffffff - 1023;
+
 }  // namespace
 }  // namespace e2ops
 
@@ -64,7 +67,8 @@ using namespace e2ops;
 extern "C" size_t e2_quant_matmul_workspace(int32_t rows, int32_t cols, int32_t tokens)
 {
     Device dev;
-    if (rows < 1 || cols < 1 || cols > E2_MAX_COLS || tokens < 1 || current_device(&dev)) return 0;
+    if (rows < 1 || rows > kMostRows || cols < 1 || cols > E2_MAX_COLS || tokens < 1 || tokens > kMostRows || current_device(&dev))
+        return 0;
     // the larger of what groups of any size, with and without gates, need
     size_t few = 0;
     for (int group = 32; tokens < kMany && group <= 128; group *= 2)
@@ -85,10 +89,10 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
     Device dev;
     if (int st = current_device(&dev)) return st;
     if (w->group != 32 && w->group != 64 && w->group != 128) return fail(E2_EINVAL, "group must be 32, 64 or 128");
-    if (w->rows < 1 || w->cols < w->group || w->cols > E2_MAX_COLS || w->cols % w->group)
-        return fail(E2_EINVAL, "rows must be positive, cols a multiple of group up to E2_MAX_COLS");
+    if (w->rows < 1 || w->rows > kMostRows || w->cols < w->group || w->cols > E2_MAX_COLS || w->cols % w->group)
+        return fail(E2_EINVAL, "rows must be in 1..2^31 - 1024, cols a multiple of group up to E2_MAX_COLS");
     if (a->dtype != E2_F16 && a->dtype != E2_BF16) return fail(E2_EINVAL, "x and y are fp16 or bf16");
-    if (a->tokens < 0) return fail(E2_EINVAL, "tokens must not be negative");
+    if (a->tokens < 0 || a->tokens > kMostRows) return fail(E2_EINVAL, "tokens must be in 0..2^31 - 1024");
     if (a->gated && w->rows % 2) return fail(E2_EINVAL, "gated products need an even number of rows");
     if (!w->codes || !w->scales || !aligned(w->codes, 16) || !aligned(w->scales, 2) || !aligned(w->mins, 2))
         return fail(E2_EINVAL, "codes (16-byte aligned) and scales must be given");

@@ -269,3 +269,18 @@ def test_gradients_are_refused():
         assert torch.equal(y, ops.quant_matmul(xg, v, residual=rg))
     with torch.inference_mode():
         assert torch.equal(y, ops.quant_matmul(x.clone(), w, residual=r.clone()))
+
+
+def test_rows_and_tokens_at_the_end_of_their_type_are_refused():
+    import ctypes as C
+
+    from paper_2606_03770_gb300 import e2ga, ops
+    lib = ops.load()
+    w, g = make(64, 64, 64, False)
+    x, y = randn(g, 64, 64), torch.empty(64, 64, device="cuda", dtype=BF)
+    for rows, tokens in ((2 ** 31 - 1, 1), (2 ** 31 - 1023, 40), (64, 2 ** 31 - 1), (0, 1), (64, -1)):
+        s = ops.e2_quant_weight(rows, 64, 64, w.codes.data_ptr(), w.scales.data_ptr(), None)
+        a = ops.e2_matmul_args(tokens, ops.E2_BF16, 0, x.data_ptr(), 64, None, 0, y.data_ptr(), 2 ** 31)
+        assert lib.e2_quant_matmul_workspace(rows, 64, tokens) == 0
+        assert lib.e2_quant_matmul(C.byref(s), C.byref(a), None, 0, None) == e2ga.E2_EINVAL
+        assert b"rows" in lib.e2_ops_error() or b"tokens" in lib.e2_ops_error()
