@@ -115,6 +115,8 @@ def _tensor(x, name, dtypes, shape, device=None):
         raise ValueError(f"{name} has shape {tuple(s)}, not {tuple('any' if b is None else b for b in shape)}")
     if s[-1] > 1 and x.stride(-1) != 1:
         raise ValueError(f"{name} must be contiguous in its last axis")
+    if x.numel() > _MOST and max(s) > _MOST:
+        raise ValueError(f"{name} has shape {tuple(s)}: sizes are below 2^31")
     return s
 
 

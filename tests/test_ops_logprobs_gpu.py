@@ -177,3 +177,14 @@ def test_a_vocabulary_at_the_end_of_its_type(vocab):
     assert torch.allclose(vals[0, :5].double().cpu(), want, rtol=0, atol=64 * R.EPS32) and float(vals[0, 5]) == -math.inf
     assert abs(float(lp) - float(want[0])) < 64 * R.EPS32
     assert abs(float(ent) + float((want.exp() * want).sum())) < 64 * R.EPS32
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """They would lose their high bits: 2^32 + 5 logits taken for 5."""
+    from paper_2606_03770_gb300 import ops
+    x = torch.zeros(2 ** 32 + 5, device="cuda", dtype=HALF)
+    for shape in ((1, -1), (-1, 1)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            ops.token_logprobs(x.view(shape))
+    with pytest.raises(ValueError, match="2\\^31"):
+        ops.QuantWeight(torch.zeros(1, 1, device="cuda", dtype=torch.uint8).expand(2 ** 32 + 1, 1), x[:1].expand(2 ** 32 + 1, 1))
