@@ -288,8 +288,10 @@ def quant_matmul(x, w, residual=None, gated=False, out=None, workspace=None):
                        _stride(residual) if residual is not None else 0, out.data_ptr(), out_stride)
     if workspace is None:
         workspace = _workspace("e2_quant_matmul_workspace", dev, w.rows, w.cols, tokens)
+    else:
+        _need(workspace.is_contiguous(), "workspace must be contiguous")
     _call("e2_quant_matmul", dev, w.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
-          workspace.numel() if workspace is not None else 0)
+          workspace.nbytes if workspace is not None else 0)
     return out
 
 
@@ -414,8 +416,10 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
                        out.data_ptr(), out_stride)
     if workspace is None:
         workspace = _workspace("e2_cache_attend_workspace", dev, cache.ref, C.byref(a))
+    else:
+        _need(workspace.is_contiguous(), "workspace must be contiguous")
     _call("e2_cache_attend", dev, cache.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
-          workspace.numel() if workspace is not None else 0)
+          workspace.nbytes if workspace is not None else 0)
     return out
 
 

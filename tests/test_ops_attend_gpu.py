@@ -378,3 +378,16 @@ def test_hints_are_read_from_any_lengths(starts, length):
     want, lim, written = R.attend(cache, q, table, lens, starts, 0.125, 0)
     R.close(out[written], want[written], lim[written])
     assert bool((out[~written] == 9).all())
+
+
+def test_workspaces_that_are_given():
+    from paper_2606_03770_gb300 import e2ga, ops
+    s = setup([20000], [1], 1, 8, 128, 64)
+    kw = dict(max_new=1, max_len=20000)
+    want = ops.cache_attend(*s, **kw)
+    one = torch.zeros(1, device="cuda")
+    with pytest.raises(ValueError, match="contiguous"):
+        ops.cache_attend(*s, workspace=one.expand(1 << 26), **kw)
+    with pytest.raises(e2ga.E2Error, match="workspace"):
+        ops.cache_attend(*s, workspace=one, **kw)
+    assert torch.equal(want, ops.cache_attend(*s, workspace=torch.zeros(1 << 20, device="cuda"), **kw))

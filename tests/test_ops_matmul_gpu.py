@@ -284,3 +284,20 @@ def test_rows_and_tokens_at_the_end_of_their_type_are_refused():
         assert lib.e2_quant_matmul_workspace(rows, 64, tokens) == 0
         assert lib.e2_quant_matmul(C.byref(s), C.byref(a), None, 0, None) == e2ga.E2_EINVAL
         assert b"rows" in lib.e2_ops_error() or b"tokens" in lib.e2_ops_error()
+
+
+def test_workspaces_that_are_given():
+    """Any type, as many bytes as are there: one byte repeated is one."""
+    from paper_2606_03770_gb300 import e2ga, ops
+    w, g = make(64, 256, 64, False)
+    x = randn(g, 40, 256)
+    y = ops.quant_matmul(x, w)
+    need = ops.load().e2_quant_matmul_workspace(64, 256, 40)
+    one = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    for view in (one.expand(need), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="contiguous"):
+            ops.quant_matmul(x, w, workspace=view)
+    for short in (one, torch.zeros(need // 4 - 1, device="cuda")):
+        with pytest.raises(e2ga.E2Error, match="workspace"):
+            ops.quant_matmul(x, w, workspace=short)
+    assert torch.equal(y, ops.quant_matmul(x, w, workspace=torch.zeros(-(-need // 4), device="cuda")))
