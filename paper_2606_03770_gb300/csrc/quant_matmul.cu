@@ -56,6 +56,21 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
 // 4096 x 4096 12.5 / 11.
 constexpr int kMany = 17;
 
+// Whether two matrices of `rows` rows of 16-bit elements share memory.  Rows of one stride (side by
+// side in wider ones) are compared as columns; of two strides, all that lies between a matrix's
+// first and last element.
+bool share_memory(const void *a, int a_cols, int64_t a_stride, const void *b, int b_cols, int64_t b_stride, int rows)
+{
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    const uintptr_t a1 = a0 + 2 * ((rows - 1) * a_stride + a_cols), b1 = b0 + 2 * ((rows - 1) * b_stride + b_cols);
+    if (a1 <= b0 || b1 <= a0) return false;
+    if (rows == 1 || a_stride != b_stride) return true;
+    const uintptr_t row = 2 * a_stride;
+    // b's first column, from a's
+    const uintptr_t at = b0 >= a0 ? (b0 - a0) % row : (row - (a0 - b0) % row) % row;
+    return at < 2 * (uintptr_t)a_cols || at + 2 * (uintptr_t)b_cols > row;
+}
+
 // Rows and tokens of whole blocks are counted in 32 bits.
 constexpr int kMostRows = 0x7fffffff - 1023;
 
@@ -102,6 +117,7 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
         return fail(E2_EINVAL, "x: 16-byte aligned, a row stride that is a multiple of 8 and at least cols");
     if (!a->y || !aligned(a->y, 2) || a->y_stride < outs || (a->residual && (!aligned(a->residual, 2) || a->residual_stride < outs)))
         return fail(E2_EINVAL, "y, residual: row strides of at least the outputs");
+    if (share_memory(a->x, w->cols, a->x_stride, a->y, outs, a->y_stride, a->tokens)) return fail(E2_EINVAL, "y may not overlap x");
     const void *ptrs[] = {w->codes, w->scales, w->mins, a->x, a->residual, a->y};
     for (const void *p : ptrs)
         if (p && !on_device(p, dev.id)) return fail(E2_EINVAL, "arrays must be memory of the current device");

@@ -301,3 +301,28 @@ def test_workspaces_that_are_given():
         with pytest.raises(e2ga.E2Error, match="workspace"):
             ops.quant_matmul(x, w, workspace=short)
     assert torch.equal(y, ops.quant_matmul(x, w, workspace=torch.zeros(-(-need // 4), device="cuda")))
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 40])
+def test_outputs_over_x_are_refused(tokens):
+    """Blocks that start later would read outputs; side by side in one buffer they do not meet."""
+    from paper_2606_03770_gb300 import e2ga, ops
+    w, g = make(128, 128, 64, False)
+    buf = randn(g, 2 * tokens, 3 * 128 + 8)
+    kept = buf.clone()
+    x = buf[:tokens, 128:256]
+    flat = buf.view(-1)
+    for out in (x, buf[:tokens, 120:248], buf[:tokens, 255:383], flat[128:].as_strided((tokens, 128), (400, 1)),
+                buf[tokens // 2:][:tokens, 128:256] if tokens > 1 else x):
+        with pytest.raises(e2ga.E2Error, match="overlap"):
+            ops.quant_matmul(x, w, out=out)
+    assert torch.equal(buf, kept)
+    want = R.matmul(x, w)
+    for out in (buf[:tokens, :128], buf[:tokens, 256:384], buf[tokens:, 128:256]):
+        R.close(ops.quant_matmul(x, w, out=out), *want)
+        assert torch.equal(x, kept[:tokens, 128:256])
+    v, _ = make(30, 128, 64, False)
+    for at in (98, 256, 300, 380):                     # close beside x, and across a row's end
+        out = flat[at:].as_strided((tokens, 30), (392, 1))
+        R.close(ops.quant_matmul(x, v, out=out), *R.matmul(x, v))
+        assert torch.equal(x, kept[:tokens, 128:256])
