@@ -245,18 +245,19 @@ class QuantWeight(_Handle):
 
 def quantize_weight(w, group=64, symmetric=True):
     """Round a float weight [rows, cols] to 4 bits with group scales (plain
-    torch; done once, when a model is loaded)."""
+    torch; done once, when a model is loaded).  Scales and minima end at fp16's
+    largest, so weights beyond 7 (symmetric), 15 times that do too."""
     _need(w.dim() == 2 and group in (32, 64, 128) and w.shape[1] % group == 0,
           "w must be [rows, cols], cols a multiple of the group (32, 64 or 128)")
     x = w.float().unflatten(1, (-1, group))
     if symmetric:
-        scales = (x.abs().amax(-1) / 7).half()
+        scales = (x.abs().amax(-1) / 7).clamp(max=65504).half()
         s = scales.float()[..., None]
         q = torch.where(s > 0, torch.round(x / s) + 8, 8.0)
         mins = None
     else:
-        lo = x.amin(-1)
-        mins, scales = lo.half(), ((x.amax(-1) - lo) / 15).half()
+        lo = x.amin(-1).clamp(-65504, 65504)
+        mins, scales = lo.half(), ((x.amax(-1) - lo) / 15).clamp(max=65504).half()
         s = scales.float()[..., None]
         q = torch.where(s > 0, torch.round((x - mins.float()[..., None]) / s), 0.0)
     q = q.clamp(0, 15).to(torch.uint8).flatten(1)

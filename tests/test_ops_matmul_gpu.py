@@ -326,3 +326,23 @@ def test_outputs_over_x_are_refused(tokens):
         out = flat[at:].as_strided((tokens, 30), (392, 1))
         R.close(ops.quant_matmul(x, v, out=out), *R.matmul(x, v))
         assert torch.equal(x, kept[:tokens, 128:256])
+
+
+def test_quantize_weight_beyond_fp16():
+    """Finite weights have finite codes' values: the nearest there are."""
+    from paper_2606_03770_gb300 import ops
+    g = torch.Generator(device="cuda").manual_seed(4)
+    a = torch.randn(6, 256, generator=g, device="cuda")
+    a[0, 3], a[1, 70], a[2, 5], a[3] = 1e6, -1e7, math.inf, 2e5
+    a[4, :64] = torch.linspace(-9e4, 8e5, 64, device="cuda")
+    for symmetric in (True, False):
+        w = ops.quantize_weight(a, 64, symmetric)
+        W, most = R.weight(w), 65504.0
+        assert bool(torch.isfinite(W).all())
+        top = 7 * most if symmetric else (w.mins.double() + 15 * most).repeat_interleave(64, 1)
+        want = a.double().clamp(min=-8 * most if symmetric else -most)
+        want = torch.minimum(want, torch.as_tensor(top, device="cuda", dtype=torch.float64))
+        step = w.scales.double().repeat_interleave(64, 1)
+        # half a step, and the roundings of scale and minimum to fp16
+        lim = step / 2 + 2.0 ** -11 * (16 * step + want.abs().amax(1, keepdim=True)) + 1e-7
+        assert bool(((W - want).abs() <= lim).all())
