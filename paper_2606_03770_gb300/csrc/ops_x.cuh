@@ -50,9 +50,9 @@ template <class T> __device__ __forceinline__ uint4 octet_in_order(const uint4 &
 }
 
 // A word's eight codes c as m + d c in fp16, rounded once, in the same order.  A code
-// in the low bits of 1024's fp16 makes 1024 + c, in the next four 1024 + 16 c.  The
-// largest value may pass fp16's range by the rounding of d: it stays fp16's largest
-// (NaN stays NaN), unless the caller knows that none does.
+// in the low bits of 1024's fp16 makes 1024 + c, in the next four 1024 + 16 c.  A value
+// may pass fp16's range, by the rounding of d or in a cache that was not written here: it
+// stays fp16's largest (NaN stays NaN), unless the caller knows that none does.
 template <bool LIMIT = true> __device__ __forceinline__ uint4 unpack_word(uint32_t w, __half2 d, __half2 m)
 {
     const uint32_t v = w >> 8;
@@ -67,7 +67,7 @@ template <bool LIMIT = true> __device__ __forceinline__ uint4 unpack_word(uint32
         const __half2 x = *reinterpret_cast<const __half2 *>(&q[i]);
         const __half2 c = i % 2 ? __hfma2(x, sixteenth, high) : __hadd2(x, off);
         o[i] = __hfma2(c, d, m);
-        if (LIMIT) o[i] = __hmin2_nan(o[i], most);
+        if (LIMIT) o[i] = __hmin2_nan(__hmax2_nan(o[i], __hneg2(most)), most);
     }
     return out;
 }

@@ -391,3 +391,25 @@ def test_workspaces_that_are_given():
     with pytest.raises(e2ga.E2Error, match="workspace"):
         ops.cache_attend(*s, workspace=one, **kw)
     assert torch.equal(want, ops.cache_attend(*s, workspace=torch.zeros(1 << 20, device="cuda"), **kw))
+
+
+@pytest.mark.parametrize("d", [9000.0, -9000.0])
+@pytest.mark.parametrize("new", [1, 40])
+def test_values_beyond_fp16_in_a_cache(new, d):
+    """A cache with larger scales than appended tokens have: as they are for a few rows, no larger
+    than 65,504 from 65 rows of a request and KV head on."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([90], [new], 1, 4, 64, 16)
+    cache.v_scales[..., 0], cache.v_scales[..., 1] = d, 500.0
+    out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=90)
+    at = torch.arange(90, device="cuda")
+    page = table[0].long()[at // 16]
+    k, v = (R.cache_values(c[page, 0, at % 16], s[page, 0, at % 16]) for c, s in
+            ((cache.k_codes, cache.k_scales), (cache.v_codes, cache.v_scales)))
+    if 4 * new >= 65:
+        v = v.clamp(-65504.0, 65504.0)
+    seen = at[None] <= torch.arange(90 - new, 90, device="cuda")[:, None]
+    a = (q.double() @ k.T / 8).masked_fill(~seen[:, None], -math.inf)
+    p = torch.softmax(a, -1)
+    _, lim, _ = R.attend(cache, q, table, lens, starts, 0.125, 0)      # (of the values as they are: larger ones)
+    R.close(out, p @ v, lim)
