@@ -162,7 +162,8 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 sum[j] += __shfl_xor_sync(~0u, sum[j], 2);
             }
             // scores to base 2; a code 1 counts 2^-24
-            const float f = fabsf(p.scale) * 1.4426950408889634f * power_of_two(-k);
+            // (of a query that is not finite every score is infinite or NaN, and its softmax NaN)
+            const float f = not_finite<T>(top) ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-k);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 q_scale[n][e] = __shfl_sync(~0u, f, (2 * t + e) * 4);

@@ -150,6 +150,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         return reinterpret_cast<uint4 *>(m.queries + g * Sh::kQuery + o / 8 * kGroupRows * 128 + r * 128 + ((o % 8) ^ (r & 7)) * 16);
     };
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+    constexpr int kNotFinite = 1 << 20;
     float scale;
     {
         // the queries, to fp16 times a power of two each (and the scale's sign)
@@ -171,12 +172,13 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
                 unsigned top = octet_largest(v[i]);
 #pragma unroll
                 for (int k = 1; k < kOctets; k *= 2) top = max(top, __shfl_xor_sync(~0u, top, k));
-                const int k = power_for<T>(top), theirs = __shfl_sync(~0u, k, lane % kAtOnce * kOctets);
+                const int k = power_for<T>(top), theirs = __shfl_sync(~0u, not_finite<T>(top) ? kNotFinite : k, lane % kAtOnce * kOctets);
                 if (lane / kAtOnce == turn) power = theirs;
                 *place(to, o) = octet_in_order<T>(v[i], p.scale < 0 ? -power_of_two(k) : power_of_two(k));
             }
         }
-        scale = fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
+        // (of a query that is not finite every score is infinite or NaN, and its softmax NaN)
+        scale = power == kNotFinite ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) barrier_arrive(m.asked);

@@ -2,6 +2,8 @@
 // times a power of two, in the order of the codes' nibbles.
 #pragma once
 
+#include <type_traits>
+
 #include "ops_mma.cuh"
 
 namespace e2ops {
@@ -12,6 +14,11 @@ template <class T> __device__ __forceinline__ int power_for(unsigned bits)
     T top;
     *reinterpret_cast<uint16_t *>(&top) = (uint16_t)bits;
     return bits ? min(14 + 127 - (int)(__float_as_uint(to_float(top)) >> 23), 126) : 0;
+}
+// Whether a magnitude is infinite or NaN.
+template <class T> __device__ __forceinline__ bool not_finite(unsigned bits)
+{
+    return bits >= (std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u);
 }
 __device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
 

@@ -413,3 +413,25 @@ def test_values_beyond_fp16_in_a_cache(new, d):
     p = torch.softmax(a, -1)
     _, lim, _ = R.attend(cache, q, table, lens, starts, 0.125, 0)      # (of the values as they are: larger ones)
     R.close(out, p @ v, lim)
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("new", [1, 2, 40])
+def test_queries_that_are_not_finite_are_nan_where_they_see_keys(new, dtype, value):
+    """Scores that are all -inf (keys of one sign) have no softmax, either."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([200, new - 1], [new, new], 2, 4, 64, 16, dtype)
+    cache.k_scales[..., 1] = 0.5
+    cache.k_codes.bitwise_or_(0x11)
+    y0 = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=200)
+    q[0, 1, 7] = value
+    q[-1, 5, 0], q[-1, 6, 63] = value, -value
+    if new > 1:
+        q[new, 3] = value                              # a query that sees no key
+    for window in (0, 30):
+        out = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=200, window=window)
+        R.close(out, *R.attend(cache, q, table, lens, starts, 0.125, window)[:2])
+    assert bool(torch.isnan(out[0, 1]).all()) and bool((out[new, 3] == 0).all())
+    y = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=200)
+    assert torch.equal(y[0, 2:], y0[0, 2:]) and torch.equal(y[-1, :5], y0[-1, :5])
