@@ -435,3 +435,65 @@ def test_queries_that_are_not_finite_are_nan_where_they_see_keys(new, dtype, val
     assert bool(torch.isnan(out[0, 1]).all()) and bool((out[new, 3] == 0).all())
     y = ops.cache_attend(cache, q, table, lens, starts, max_new=new, max_len=200)
     assert torch.equal(y[0, 2:], y0[0, 2:]) and torch.equal(y[-1, :5], y0[-1, :5])
+
+
+@pytest.mark.parametrize("new,window", [(1, 0), (1, 700), (3, 0), (40, 0), (40, 700)])
+@pytest.mark.parametrize("B,length,D,page", [(1, 1000, 64, 16), (8, 2305, 128, 64), (1, 4097, 128, 64), (3, 9001, 64, 256),
+                                             (1, 20000, 128, 64)])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_every_key_counts(B, length, D, page, new, window, dtype):
+    """Each key has one element of its own that is not 0, so one that is lost, or seen twice, shows.
+
+    Queries of ones and constant keys: a score is its key's level, exact in any form, levels by 64
+    keys.  Weights and their products with values may be rounded to fp16 (2^-11 each), outputs to
+    2^-8 or 2^-11; the rest is in 32 bits."""
+    from paper_2606_03770_gb300 import ops
+    H = 8
+    cache, q, table, lens, starts = setup([length - 5 * b for b in range(B)], [new] * B, H, 2, D, page, dtype)
+    q.fill_(1)
+    g = torch.Generator(device="cuda").manual_seed(length)
+    level = torch.randint(-4, 5, (length,), generator=g, device="cuda")[torch.arange(length, device="cuda") // 64] * 0.5
+    key = torch.arange(length, device="cuda")
+    for s in (cache.k_scales, cache.v_scales):
+        s.zero_()
+    cache.v_scales[..., 0] = 1
+    for b in range(B):
+        cache.k_scales[table[b].long()[key // page], :, key % page, :, 1] = level.half()[:, None, None]
+    scale = 0.5 / D
+    kw = dict(max_new=new, max_len=length, window=window, scale=scale)
+    pos = torch.arange(-new, 0, device="cuda")[:, None]
+    h, d = torch.meshgrid(torch.arange(H, device="cuda"), torch.arange(D, device="cuda"), indexing="ij")
+    tol = 2.0 ** -9 + R.EPS[dtype] + (length + 64) * R.EPS32 / 16
+    for first in range(0, length, H * D):
+        own = (first + h * D + d) % length                                     # the key of element (h, d)
+        cache.v_codes.zero_()
+        for b in range(B):
+            cache.v_codes[table[b].long()[own // page], h, own % page, d // 2] |= (15 << 4 * (d % 2)).byte()
+        out = ops.cache_attend(cache, q, table, lens, starts, **kw).view(B, new, H, 2, D)
+        for b in range(B):
+            at = int(lens[b]) + pos
+            seen = (key <= at) & ((key > at - window) if window else (key >= 0))
+            p = torch.softmax((level.double() * 0.5).masked_fill(~seen, -math.inf), -1)
+            want = (15 * p)[:, own][:, :, None]                                # [new][H][1][D]
+            got = out[b].double()
+            bad = (got - want).abs() > tol * want + R.TINY16
+            assert not bool(bad.any()), (b, first, int(bad.sum()))
+
+
+@pytest.mark.parametrize("lens,news", [([5000, 3000], [1, 1]), ([40000], [1]), ([700, 300], [40, 3])])
+def test_two_streams_at_once(lens, news):
+    """Each call with a workspace of its own, many of both in flight."""
+    from paper_2606_03770_gb300 import ops
+    kw = dict(max_new=max(news), max_len=max(lens))
+    sets = [setup(lens, news, 2, 8, 128, 64, seed=seed) for seed in (1, 2)]
+    want = [ops.cache_attend(*s, **kw) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(ops.cache_attend(*sets[i], **kw))
+    torch.cuda.synchronize()
+    for a, outs in zip(want, got):
+        assert all(torch.equal(a, o) for o in outs)

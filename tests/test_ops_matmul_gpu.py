@@ -346,3 +346,31 @@ def test_quantize_weight_beyond_fp16():
         # half a step, and the roundings of scale and minimum to fp16
         lim = step / 2 + 2.0 ** -11 * (16 * step + want.abs().amax(1, keepdim=True)) + 1e-7
         assert bool(((W - want).abs() <= lim).all())
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 40])
+def test_widths_of_the_largest_workload_and_its_head(tokens):
+    check(tokens, 512, 53248)                        # the 16384-wide model's way back down
+    check(tokens, 2 * 1000, 16384, gated=True, residual=True)
+    check(tokens, 128256, 1024)                      # a head's rows
+
+
+@pytest.mark.parametrize("tokens", [1, 16, 200])
+def test_two_streams_at_once(tokens):
+    """Each call with a workspace of its own, many of both in flight."""
+    from paper_2606_03770_gb300 import ops
+    pairs = []
+    for seed in (1, 2):
+        w, g = make(1024, 4096, 64, seed == 2, seed)
+        x = randn(g, tokens, 4096)
+        pairs.append((x, w, ops.quant_matmul(x, w)))
+    streams = [torch.cuda.Stream() for _ in pairs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(ops.quant_matmul(*pairs[i][:2]))
+    torch.cuda.synchronize()
+    for (_, _, want), outs in zip(pairs, got):
+        assert all(torch.equal(want, y) for y in outs)
