@@ -411,9 +411,11 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
         out_stride = _heads(out, "out", q.dtype, shape, dev)
     if torch.is_grad_enabled() and (cache.requires_grad or q.requires_grad or out.requires_grad):
         _no_gradient(cache, q=q, out=out)
+    if max_new > _MOST or max_len > _MOST or not -1 <= window <= _MOST:
+        max_new, max_len, window = min(max_new, _MOST), min(max_len, _MOST), max(-1, min(window, _MOST))
     a = e2_attend_args(tokens, DTYPES[q.dtype], heads, batch, table.data_ptr(), cols, _stride(table),
-                       lens.data_ptr(), starts.data_ptr(), min(max_new, _MOST), min(max_len, _MOST),
-                       cache.head_dim ** -0.5 if scale is None else scale, max(-1, min(window, _MOST)), q.data_ptr(), q_stride,
+                       lens.data_ptr(), starts.data_ptr(), max_new, max_len,
+                       cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), q_stride,
                        out.data_ptr(), out_stride)
     if workspace is None:
         workspace = _workspace("e2_cache_attend_workspace", dev, cache.ref, C.byref(a))
