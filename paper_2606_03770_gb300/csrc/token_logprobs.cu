@@ -356,11 +356,12 @@ template <class T, bool TOP> __global__ void __launch_bounds__(kMostThreads, 3) 
     }
 }
 
-// Rows fewer than two per multiprocessor are split over clusters of up to eight.
+// While rows have no more blocks than there are multiprocessors they are split in two, over
+// clusters of up to eight: two blocks a multiprocessor at most.
 template <class T> int launch_rows(LogprobParams p, int sms, cudaStream_t s)
 {
     p.split = 1;
-    while (p.split < 8 && (int64_t)p.rows * p.split * 2 <= (int64_t)sms * 2 && p.vocab / p.split >= 8192) p.split *= 2;
+    while (p.split < 8 && (int64_t)p.rows * p.split <= sms && p.vocab / p.split >= 8192) p.split *= 2;
     const int share = p.vocab / p.split;
     const int threads = share <= 2048 ? 128 : share <= 8192 ? 256 : kMostThreads;
     return launch<LogprobParams>(p.top ? logprob_kernel<T, true> : logprob_kernel<T, false>,
