@@ -4,8 +4,9 @@
 namespace e2ops {
 namespace {
 
-// Blocks to have at least: 1.6 per multiprocessor keep the memory busy; and those that run at once.
-constexpr int kFewBlocks = 250, kAtOnce = 3 * 152;
+// Blocks to have at least: 1.6 per multiprocessor keep the memory busy; and those that run at once
+// on one.
+constexpr int kFewBlocks = 250, kAtOnce = 3;
 
 // So few elements of x a block prepares for itself: one launch and no workspace, where weights
 // are read in less time than that costs the caller.  Measured, us a call (a graph's; by
@@ -20,7 +21,7 @@ constexpr int64_t kOwnWeights = 1 << 27;
 // clusters): 4096 x 4096 4x1 6.7, 1x4 7.0, 2x2 7.1; 10240 x 8192 1x2 15.4, 2x1 15.7, 1x1 18.9,
 // 4x1 19.9; 8192 x 28672 1x3 31.9, 1x2 34.6, 2x1 35.6; 57344 x 8192 gated 1x1 46.6, 2x1 50.8, 1x2
 // 55; 1024 x 16384 4x4 7.7, 1x8 9.0.
-FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
+FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins, int sms)
 {
     const int nt = tokens <= 8 ? 1 : 2;
     const int chunks = (cols + kChunk - 1) / kChunk, x_pad = chunks * kChunk;
@@ -44,7 +45,7 @@ FewPlan plan_few(int rows, int cols, int tokens, int group, bool mins)
         return (int64_t)((rows + rb - 1) / rb) * split;
     };
     if (blocks(1, 1) >= kFewBlocks || chunks == 1) return plan(1, 1);
-    if (blocks(1, 2) >= kFewBlocks) return plan(1, blocks(1, 3) <= kAtOnce && chunks > 2 ? 3 : 2);
+    if (blocks(1, 2) >= kFewBlocks) return plan(1, blocks(1, 3) <= kAtOnce * sms && chunks > 2 ? 3 : 2);
     int wk = kWarps, split = 1;
     while (wk > 1 && plan(wk, split).smem > (size_t)kSmemPerSm / 2 - 2048) wk /= 2;
     while (split < 8 && blocks(wk, split) < kFewBlocks && wk * split * 2 <= chunks) split *= 2;
@@ -88,7 +89,7 @@ extern "C" size_t e2_quant_matmul_workspace(int32_t rows, int32_t cols, int32_t 
     size_t few = 0;
     for (int group = 32; tokens < kMany && group <= 128; group *= 2)
         for (int mins = 0; mins < 2; ++mins) {
-            const size_t one = plan_few(rows, cols, tokens, group, mins).workspace;
+            const size_t one = plan_few(rows, cols, tokens, group, mins, dev.sms).workspace;
             few = one > few ? one : few;
         }
     if (tokens < kMany) return few;
@@ -133,7 +134,7 @@ extern "C" int e2_quant_matmul(const e2_quant_weight *w, const e2_matmul_args *a
         if ((int64_t)f.row_tiles * f.tiles * 8 > 0x7fffffff) return fail(E2_EINVAL, "too many tokens for one call");
         return launch_many(p, f, workspace, outs, dev.id, static_cast<cudaStream_t>(stream));
     }
-    const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr);
+    const FewPlan f = plan_few(w->rows, w->cols, a->tokens, w->group, w->mins != nullptr, dev.sms);
     // how the scales' rows are aligned
     const int wide = w->group == 128 ? 8 : 16, groups = w->cols / w->group;
     auto all_aligned = [&](int to) { return groups * 2 % to == 0 && aligned(w->scales, to) && aligned(w->mins, to); };
