@@ -1,11 +1,11 @@
 /*
- * e2ops.h -- the operators of one served decoder block on the GB300 (sm_103a),
- * in the precisions the deployment search plans with: 4-bit weights (the
- * models the paper deploys), a paged key/value cache (here in 4 bits), decode
- * batches of a few requests and prompts of a few thousand tokens.  They are what a
- * user runs to measure a block on this GPU (Sec. 3.1 of the paper: load a
- * reduced number of blocks, time them) and to serve with it.  Same library
- * (libe2ga.so) and conventions as e2ga.h:
+ * e2ops.h -- the operators of one served decoder block on the GB300 (sm_103a):
+ * 4-bit weights (the models the paper deploys), a paged key/value cache in 4
+ * bits (the search's workloads count one of fp16), decode batches of a few
+ * requests and prompts of a few thousand tokens.  They are what a user runs to
+ * measure a block on this GPU (Sec. 3.1 of the paper: load a reduced number of
+ * blocks, time them) and to serve with it.  Same library (libe2ga.so) and
+ * conventions as e2ga.h:
  *
  *  - Every function returns an e2_status; e2_ops_error() has the text of the
  *    calling thread's last failed call of this header.  Nothing aborts or throws.
@@ -20,6 +20,10 @@
  *    numbers, slots, positions, token ids, lengths) are checked by the kernels:
  *    what is out of range is never followed, with the result written below.
  *  - A call with zero tokens, rows or requests does nothing and returns E2_OK.
+ *  - The kernels for prompts (products from 17 tokens, attention from 65 rows of a
+ *    request and KV head) wait for copies and products of their own block.  Such a
+ *    wait ends after some seconds at the latest; the block's outputs are NaN then,
+ *    with E2_OK, which is returned long before.
  */
 #ifndef E2OPS_H
 #define E2OPS_H
@@ -59,8 +63,8 @@ typedef struct {
  * row stride a multiple of 8.  Sums are in 32 bits, y is rounded once; x goes to
  * the tensor cores as fp16 times a power of two per token (values below 2^-24 of the
  * token's largest lose bits).  From 17 tokens on W does too, rounded once to fp16
- * (2^-12 of a weight; what passes 65,504 stays there).  An x that is infinite or
- * NaN gives the formula's infinities and NaN, in its own row of y only.  y may not
+ * (2^-11 of a weight; what passes 65,504 stays there), so 16 and 17 tokens differ
+ * in more than the order of their sums.  An x that is infinite or NaN gives the formula's infinities and NaN, in its own row of y only.  y may not
  * overlap x or the weights; it may be residual itself.
  * workspace: e2_quant_matmul_workspace() bytes (0: may be NULL), 256-byte
  * aligned, contents of no consequence. */
@@ -143,6 +147,16 @@ int e2_cache_read(const e2_cache *c, const int64_t *slots, int32_t tokens, int32
  * j <= p and, with a window > 0, j > p - window.  Query head h reads KV head
  * h / (q_heads / kv_heads).
  *   out[i][h] = sum_j softmax_j(scale * q.k_j) v_j, 0 where no key is seen.
+ * A query that is infinite or NaN gives NaN where it sees a key.  Sums are in 32
+ * bits, out is rounded once; what the tensor cores take is fp16:
+ *  - queries, times a power of two each (elements below 2^-24 of the largest of a
+ *    query and head lose bits);
+ *  - up to 64 rows (queries times query heads) of a request and KV head: weights
+ *    times their values' scales, 2^-11 of each; minima are not rounded, so the
+ *    error is 2^-11 of sum p |d code|, which outputs may be far below;
+ *  - from 65 rows on: keys, values and weights, 2^-11 of each (keys and values that
+ *    pass 65,504, which appended ones do not, stay there);
+ *  - fp16 outputs: what rounding took from the weights is in a product of its own.
  * q, out: fp16 or bf16, [tokens][q_heads][head_dim], token strides multiples of
  * 8, bases 16-byte aligned; out may be q only if a request has one query.
  * max_new and max_len are the largest new and lens: they shape the launch, larger ones on

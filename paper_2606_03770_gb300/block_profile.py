@@ -3,10 +3,13 @@
 The paper's planner takes per-block latencies that are measured by loading a
 reduced number of blocks on each device (Sec. 3.1); the workloads here derive
 them from work and rates instead.  This module runs the block itself, with the
-operators of ``ops``: 4-bit weights, a paged 4-bit cache, the head's output layer.
-It times the prefill of one prompt (l_P) and the decode of b requests (l_D(b)),
-and turns them into the compute rate and memory bandwidth with which the
-planner's stage times of this device are the measured ones.
+operators of ``ops``: 4-bit weights, a paged 4-bit cache, the head's output layer
+(workloads with 16-bit weights are refused).  It times the prefill of one prompt (l_P)
+and the decode of b requests (l_D(b)), and turns the prefill into a compute rate and the
+largest batch into a memory bandwidth, for the block's own flops and bytes; the planner
+takes those two.  The other batches' and the head's times are shown, not planned with.
+The two norms are plain torch: some 28 us of every decode (146 us with one request of
+the 32-device workload).
 
     python -m paper_2606_03770_gb300.block_profile --config c2          # the table
     python -m paper_2606_03770_gb300.block_profile --config c2 --plan   # and a search

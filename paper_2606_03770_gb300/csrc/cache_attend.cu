@@ -29,8 +29,8 @@ namespace {
 // Minima are summed in 32 bits.
 //
 // Measured, us (bf16, 128 elements, 8 KV heads): 8 requests x 65,536 keys of 64 query heads
-// 126 (71% of the memory's rate; fp16 139), of 128 heads 176 (51%); 8 x 2,304 keys 17 (joined
-// by a second kernel 19), one request 11, of 65,536 keys 36.  A long context is bound by its
+// 125 (71% of the memory's rate; fp16 139), of 128 heads 177 (50%); 8 x 2,304 keys 16 (joined
+// by a second kernel 19), one request 11, of 65,536 keys 32.  A long context is bound by its
 // instructions, some 600 a warp and tile (1,000 for sixteen rows), which three warps of a
 // scheduler issue at half its rate; four, with two stages or 128 registers, are no faster
 // (130, 181).

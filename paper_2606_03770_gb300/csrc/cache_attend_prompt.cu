@@ -2,13 +2,13 @@
 //
 // A block takes 256 rows (queries times the query heads of a KV head), in two groups of
 // 128 so that one group's weights are made while the other's products run, and walks over
-// tiles of 64 keys.  Eight warps dequantise a tile for both (fp16, one rounding: 2^-12 of a
+// tiles of 64 keys.  Eight warps dequantise a tile for both (fp16, one rounding: 2^-11 of a
 // value), four issue S = q K^T and O += P V of each, eight make the weights, a thread a row: scores
 // come from tensor memory, weights go back into the scores' place, as the operand that P V
 // reads from there.  O stays in tensor memory and is brought to a new maximum only
 // when the old one is exceeded by 2^8.  Elements of eight lie in the order that unpacking
 // leaves (0, 4, 1, 5, 2, 6, 3, 7) in q, K and V, and are put right in the output.
-// Weights go to fp16 times 2^7 (2^-12 each; fp16 outputs take the rounding's rest in a second
+// Weights go to fp16 times 2^7 (2^-11 each; fp16 outputs take the rounding's rest in a second
 // product).  A weight of 0 does not stop a NaN among the values, so values whose scale or
 // minimum is not finite are held back as zeros, and rows that do see their keys are made NaN.
 //
@@ -16,7 +16,7 @@
 // 1,024 of their unit's and the products 1,000 of the tensor cores'.  Measured (64 query heads
 // over 8, 128 elements, bf16): 1,152 queries x 2,304 keys 74 us (880 TFLOP/s, 46% of the
 // tensor cores' measured rate), 2,048 x 2,048 90 us, 4 x 256 x 4,096 147 us; 4,096 x 4,096 of 128
-// heads 573 us (959 TFLOP/s).  The longest blocks of all heads come first (127 us for 142, a step before).
+// heads 570 us (964 TFLOP/s).  The longest blocks of all heads come first.
 //
 // Every wait ends: one that takes too long marks the block as failed, which then frees
 // its tensor memory and writes NaN.

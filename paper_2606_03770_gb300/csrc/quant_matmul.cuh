@@ -38,7 +38,7 @@ struct MatmulParams {
 // blocks of a cluster (split), and joined in a fixed order.
 //
 // Measured, us (64 columns a group): 57344 x 8192 gated 47 with one token (78% of the memory's
-// rate), 55 with eight; 8192 x 28672 32 and 39; 4096 x 4096 6.6 and 7.1; sixteen tokens 90, 72
+// rate), 55 with eight; 8192 x 28672 32 and 39; 4096 x 4096 6.6 and 7.2; sixteen tokens 92, 63
 // and 10.  With eight tokens three warps a scheduler issue in 45% of all slots; four are no faster.
 
 constexpr int kRows = 16;                    // of a warp

@@ -5,15 +5,17 @@
 // in tensor memory, x in shared memory.  One warp copies x, prepared beforehand
 // as the images of its stages (one bulk copy each), one issues the products, sixteen
 // unpack weights, four a stage: a thread a row's 64 columns, to fp16 with their scale, one
-// rounding (2^-12 of a weight; |W| up to 65504).  (Unpacked into shared memory instead, a
+// rounding (2^-11 of a weight; |W| up to 65504).  (Unpacked into shared memory instead, a
 // stage took 520 ns whatever its tokens, and 370 with each thread loading its own row, a line a
 // lane.)  Elements stay in the order that unpacking leaves (0, 4, 1, 5, 2, 6, 3, 7 of each
 // eight), x is put into the same one.  Few rows are split over columns by the blocks of a
 // cluster, whose sums are joined in a fixed order through shared memory.
 //
-// Measured with 1,152 tokens: 8192 x 28672 404 us (1,340 TFLOP/s, 70% of the tensor cores'
-// measured rate; one call after another 456, where the power limit lowers the clock), 57344 x
-// 8192 gated 841 (1,286), 10240 x 8192 161 (1,200), 4096 x 4096 49.  Lost: turns that do not come
+// Measured with 1,152 tokens, us: 8192 x 28672 399 (1,356 TFLOP/s, 71% of the tensor cores'
+// measured rate; 446 over weights of 300 MB in turn, 453 one call after another, where the power
+// limit lowers the clock), 57344 x 8192 gated 853 (1,269), 10240 x 8192 163 (1,184), 4096 x 4096
+// 49; 17 tokens 69, 118, 39 and 12.  Looking whether a stage's weights stay in range is 0 to 2% of it.
+// Lost: turns that do not come
 // out even on 152 multiprocessors, 430 cycles of unpacking a stage where the products of fewer
 // than 215 tokens take less, and a block's start and end, when its products rest.
 //

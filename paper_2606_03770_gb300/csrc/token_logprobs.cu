@@ -6,7 +6,8 @@ namespace e2ops {
 namespace {
 
 // One pass over a row, by a block or, where there are few rows, by the blocks of a
-// cluster; bound by reading it (fp32) or by its seven operations an element (16 bits).
+// cluster; bound by reading it (fp32) or by instructions (16 bits: some fourteen issue slots an
+// element, seven of them arithmetic).
 // A thread keeps the maximum m of what it has read, sum w and sum w t, with w = 2^t, t = x
 // log2 e - c and c = m log2 e rounded once, all in 32 bits, and brings them to a new
 // maximum when one comes.  The product in t is not rounded before c is taken off, and c is the

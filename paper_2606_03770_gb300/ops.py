@@ -1,7 +1,7 @@
 """Binding of the block operators' C ABI (include/e2ops.h) for torch tensors.
 
-What one served decoder block and its output layer are made of, in the
-precisions the deployment search plans with:
+What one served decoder block and its output layer are made of, with 4-bit
+weights and a 4-bit cache:
 
 * ``quant_matmul``: products with 4-bit weights and group scales, with the
   residual add or the gated (SwiGLU) form;
