@@ -181,7 +181,9 @@ def _call(name, device, *args):
 
 class _Handle:
     """What holds tensors and the struct that the library takes of them.  The struct has
-    their addresses and sizes, so nothing is assigned once it is made."""
+    their addresses and sizes, so none of what it is made of is assigned later."""
+
+    _made = frozenset()                    # names that are not assigned any more
 
     def _hold(self, *tensors):
         """Views of its own, and the memory whatever becomes of any view."""
@@ -190,12 +192,14 @@ class _Handle:
         return [x.detach() if x is not None else None for x in tensors]
 
     def __setattr__(self, name, value):
-        if "ref" in self.__dict__:
+        if name in self._made:
             raise AttributeError(f"{type(self).__name__}.{name} cannot be changed: make another {type(self).__name__}")
         object.__setattr__(self, name, value)
 
     def __delattr__(self, name):
-        raise AttributeError(f"{type(self).__name__}.{name} cannot be deleted")
+        if name in self._made:
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be deleted")
+        object.__delattr__(self, name)
 
 
 def _workspace(name, device, *args):
@@ -233,6 +237,7 @@ class QuantWeight(_Handle):
         self.struct = e2_quant_weight(rows, cols, self.group, codes.data_ptr(), scales.data_ptr(),
                                       mins.data_ptr() if mins is not None else None)
         self.ref = C.byref(self.struct)
+        self._made = frozenset(vars(self)) | {"_made"}
 
     def dequantize(self):
         """The weights in float32 (plain torch; for checks and inspection)."""
@@ -319,6 +324,7 @@ class Cache(_Handle):
         self.struct = e2_cache(pages, page, heads, 2 * half, k_codes.data_ptr(), k_scales.data_ptr(),
                                v_codes.data_ptr(), v_scales.data_ptr())
         self.ref = C.byref(self.struct)
+        self._made = frozenset(vars(self)) | {"_made"}
 
     @classmethod
     def empty(cls, pages, page_size, kv_heads, head_dim, device="cuda"):

@@ -238,11 +238,14 @@ def test_weights_keep_the_memory_they_point_at():
     w, g = make(64, 256, 64, True)
     x = randn(g, 3, 256)
     y = ops.quant_matmul(x, w)
-    for name in ("codes", "scales", "mins", "rows", "cols", "group", "device", "struct", "ref", "other"):
+    for name in ("codes", "scales", "mins", "rows", "cols", "group", "device", "struct", "ref"):
         with pytest.raises(AttributeError, match="QuantWeight"):
             setattr(w, name, getattr(w, name, None))
     with pytest.raises(AttributeError, match="QuantWeight"):
         del w.codes
+    w.name = "down"                                   # a program's own
+    w.name = w.name + "_proj"
+    del w.name
     given = [t.clone() for t in (w.codes, w.scales, w.mins)]
     v = ops.QuantWeight(*given)
     for t in given + [v.scales]:
