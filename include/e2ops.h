@@ -151,7 +151,7 @@ int e2_cache_read(const e2_cache *c, const int64_t *slots, int32_t tokens, int32
  * bits, out is rounded once; what the tensor cores take is fp16:
  *  - queries, times a power of two each (elements below 2^-24 of the largest of a
  *    query and head lose bits);
- *  - up to 64 rows (queries times query heads) of a request and KV head: weights
+ *  - up to 64 rows (max_new times query heads) of a request and KV head: weights
  *    times their values' scales, 2^-11 of each; minima are not rounded, so the
  *    error is 2^-11 of sum p |d code|, which outputs may be far below;
  *  - from 65 rows on: keys, values and weights, 2^-11 of each (keys and values that
