@@ -184,6 +184,82 @@ size_t e2_cache_attend_workspace(const e2_cache *c, const e2_attend_args *a);
 int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace, size_t workspace_bytes,
                     void *stream);
 
+/* ---- a decode step with drafted tokens ----------------------------------------
+ *
+ * Request r's new tokens starts[r]..starts[r+1]-1 are the nodes 0, 1, ... of a tree:
+ * node 0 is the request's last token, the others are drafted, up to E2_MAX_DRAFT in all.
+ * parents[t] of node i is in 0..i-1; anything else counts as -1, no parent.  All nodes'
+ * keys and values have been appended, node i's as token base + i, base = lens[r] -
+ * (starts[r+1] - starts[r]); its position, for the turn and for windows, is base + depth,
+ * depth the steps up to a node without a parent. */
+#define E2_MAX_DRAFT 64
+
+/* e2_cache_attend, but that node i sees the keys before base, its own and those of the
+ * nodes on its way up; with a window > 0 those whose position is above its own minus
+ * window; and that what rounding took from the weights is in a product of its own up to 64
+ * rows for bf16 too.  max_new is at most E2_MAX_DRAFT; nodes beyond (of a request that has more) are
+ * NaN where they see keys.  parents: [tokens]. */
+size_t e2_cache_attend_tree_workspace(const e2_cache *c, const e2_attend_args *a);
+int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* Which drafted tokens the target's probabilities accept.  Row t of logits (and of draft, the
+ * draft model's, or NULL) is of what follows node t; p and q are exp(x / T) over its sum,
+ * T = temperature[r] (NULL: 1).  From node a = 0 on, with P = p of a, the children c of a are
+ * asked in their order, with u = uniforms[c] and x = ids[c]:
+ *   u q(x) < P(x): x is accepted, a = c, P = p of c.
+ *   else P = (P - q)+, over its sum.
+ * Without draft q is 1 at x: x is accepted when u < P(x), or else leaves P.  When no child is
+ * accepted (or there is none) the walk ends, and answers with the first token v at which P's
+ * sum in order is above uniforms of node 0.  T = 0: the child whose id is the first largest
+ * logit is accepted, or else that token answers.
+ *   kept[r]: nodes of the way, node 0 among them (0 for a request without nodes)
+ *   nodes[r][k], k < kept[r]: them; -1 from there on
+ *   answer[r][k]: the token after nodes[r][k], the last the answer; -1 from kept[r] on
+ * Exponentials and sums have some 45 bits, so decisions are those of 64 bits but for numbers
+ * within 2^-40 or so of a border; what (P - q)+ sums to counts as nothing below 2^-36, and P stays.
+ * Exponentials below e^-64 of the largest count as nothing in sums and for the answer, below e^-745 (which 64 bits
+ * do not hold) for a drafted token.
+ * -inf marks a forbidden token.  The walk ends with the answer -1 at a row that holds NaN or
+ * +inf or has no token allowed (of logits; of draft where a child is asked), and at node 0 for a
+ * T that is negative, infinite or NaN.  ids outside the vocabulary are never accepted.
+ * uniforms are taken as 0 to 1, NaN as 0.  Requests whose starts are no rows of the call have no
+ * nodes.  logits and draft: fp16, bf16 or fp32, any row stride.  vocab is at most 2^30. */
+typedef struct {
+    int32_t tokens, vocab, dtype, batch, max_new;   /* max_new: columns of nodes and answer */
+    const void *logits;
+    int64_t logits_stride;
+    const void *draft;
+    int64_t draft_stride;
+    const int32_t *ids, *parents, *starts;
+    const float *uniforms, *temperature;
+    int32_t *kept, *nodes, *answer;
+} e2_verify_args;
+
+int e2_verify_drafts(const e2_verify_args *a, void *stream);
+
+/* Keeps the tokens of such a way: in the cache of each layer token base + nodes[r][k] becomes
+ * token base + k, k < kept[r], codes and scales of keys and values, all read before any is
+ * written; lens_out[r] = base + kept[r].  kept counts as 0..min(cols, the request's nodes);
+ * what is not a node, or not in the cache, is not moved.  lens_out may not be lens.
+ * arrays (device memory): the addresses of each layer's k_codes, k_scales, v_codes, v_scales, as
+ * e2_cache_layers writes them (to host memory) once the caches, all of one shape and of different
+ * memory, have been checked; c is one of them. */
+typedef struct {
+    int32_t layers, batch, cols;                    /* cols: at most E2_MAX_DRAFT */
+    const uint64_t *arrays;
+    const int32_t *table;
+    int32_t table_cols;
+    int64_t table_stride;
+    const int32_t *lens, *starts, *nodes;
+    int64_t nodes_stride;
+    const int32_t *kept;
+    int32_t *lens_out;
+} e2_keep_args;
+
+int e2_cache_layers(const e2_cache *caches, int32_t layers, uint64_t *arrays);
+int e2_cache_keep(const e2_cache *c, const e2_keep_args *a, void *stream);
+
 /* ---- the output layer ---------------------------------------------------------
  *
  * Of each row x of logits [rows][vocab] (fp16, bf16 or fp32, any row stride):

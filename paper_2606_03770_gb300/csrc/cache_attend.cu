@@ -25,7 +25,7 @@ namespace {
 // two each; a key's scale and minimum are applied to its sums in 32 bits.  The values'
 // words are loaded transposed, which pairs two keys of one dimension; their scales
 // multiply the weights before these are rounded to fp16, against a running power of two so
-// that neither range ends; fp16 outputs take the rounding's rest in a second product.
+// that neither range ends; fp16 outputs, and trees, take the rounding's rest in a second product.
 // Minima are summed in 32 bits.
 //
 // Measured, us (bf16, 128 elements, 8 KV heads): 8 requests x 65,536 keys of 64 query heads
@@ -55,11 +55,11 @@ __device__ __forceinline__ float part_factor(float top, float weights, float bes
     return top == -INFINITY ? (weights == 0 ? 0.0f : weights) : power2(top - best);
 }
 
-template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) few_kernel(const AttendParams p)
+template <class T, int D, int NT, bool TREE> __global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) few_kernel(const AttendParams p)
 {
     using St = FewStage<D>;
     constexpr int U = D / 32, GR = D / E2_CACHE_GROUP, C = 8 * NT;
-    constexpr bool kRest = std::is_same<T, __half>::value;
+    constexpr bool kRest = TREE || std::is_same<T, __half>::value;
     extern __shared__ __align__(128) uint8_t smem[];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, split = blockIdx.x;
@@ -68,13 +68,16 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
     const int32_t *table = p.table + request * p.table_stride;
     uint8_t *ring = smem + warp * kFewStages * St::kBytes;
     const uint32_t ring_at = smem_addr(ring);
+    __shared__ int8_t parents[TREE ? E2_MAX_DRAFT : 1];
+    const Tree tree(p, rows, parents);
+    if (TREE) Tree::load(p, request, parents);              // (a barrier follows before they are read)
 
     for (int64_t row0 = (int64_t)blockIdx.z * C; row0 < rows.count; row0 += (int64_t)gridDim.z * C) {
         // the keys that some row sees, in tiles; this split's
         const Slab slab(rows, row0);
         const int last = (int)min((int64_t)C, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
-        const int lo = p.window > 0 ? (int)max(slab.pos(0) - p.window + 1, (int64_t)0) : 0;
+        const int lo = p.window > 0 ? (int)max((TREE ? tree.base : slab.pos(0)) - p.window + 1, (int64_t)0) : 0;
         const int hi = (int)max(min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0), (int64_t)0);
         const int tile_lo = lo / kTile, tiles = hi > lo ? (hi + kTile - 1) / kTile - tile_lo : 0;
         const int units = (tiles + kFewWarps - 1) / kFewWarps, per = (units + p.splits - 1) / p.splits * kFewWarps;
@@ -132,7 +135,8 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
         uint4 *q_shared = reinterpret_cast<uint4 *>(smem + kFewWarps * kFewStages * St::kBytes);   // [NT][U][32]
         __syncthreads();
         float q_sum[NT][GR][2], q_scale[NT][2];          // of columns 2t, 2t + 1
-        int seen_hi[NT][2], seen_lo[NT][2];
+        int seen_hi[NT][2], seen_lo[NT][2];              // (a tree's, of the tokens before it)
+        uint64_t way[TREE ? NT : 1][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int row = 8 * n + g;
@@ -163,7 +167,9 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
             }
             // scores to base 2; a code 1 counts 2^-24
             // (of a query that is not finite every score is infinite or NaN, and its softmax NaN)
-            const float f = not_finite<T>(top) ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-k);
+            bool spoilt = not_finite<T>(top);
+            if (TREE && live && slab.query + rows.skipped + (slab.over + row) / slab.share >= E2_MAX_DRAFT) spoilt = true;
+            const float f = spoilt ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-k);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 q_scale[n][e] = __shfl_sync(~0u, f, (2 * t + e) * 4);
@@ -173,12 +179,18 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                 const bool seen = slab.live(at);
                 seen_hi[n][e] = seen ? (int)max(slab.pos(at), (int64_t)-1) : -1;
                 seen_lo[n][e] = seen && p.window > 0 ? (int)max(slab.pos(at) - p.window + 1, (int64_t)0) : 0;
+                if (TREE) {
+                    const int64_t node = rows.skipped + slab.pos(at) - slab.first_pos;
+                    seen_hi[n][e] = seen ? tree.base - 1 : -1;
+                    way[n][e] = seen ? tree.way(min(node, (int64_t)E2_MAX_DRAFT - 1), seen_lo[n][e]) : 0;
+                }
             }
         }
         __syncthreads();
         // tiles in this range need no mask for any column
+        // (a node is no deeper than its number)
         const int full_lo = p.window > 0 ? (int)max(slab.pos(last) - p.window + 1, (int64_t)0) : 0;
-        const int full_hi = (int)max(slab.pos(0), (int64_t)-1);
+        const int full_hi = (int)max(TREE ? tree.base - 1 : slab.pos(0), (int64_t)-1);
         const bool all_live = C <= slab.left;
 
         float o[U][2][NT][4] = {};                       // sums for dimensions 32 u + 4 g + {0, 1}, {2, 3}
@@ -258,7 +270,8 @@ template <class T, int D, int NT> __global__ void __launch_bounds__(32 * kFewWar
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int e = 0; e < 2; ++e)
-                                if (!in || key > seen_hi[n][e] || key < seen_lo[n][e]) {
+                                if (!in || (TREE && key >= tree.base ? key - tree.base >= 64 || !(way[TREE ? n : 0][e] >> (key - tree.base) & 1)
+                                                                     : key > seen_hi[n][e] || key < seen_lo[n][e])) {
                                     s[m][r][n][e] = -INFINITY;
                                     hidden[n][e] |= 1u << (2 * m + r);
                                 }
@@ -576,13 +589,13 @@ size_t workspace_for(const e2_cache *c, const e2_attend_args *a, const Plan &f)
     return f.splits > 1 && !f.cluster ? (size_t)a->tokens * a->q_heads * f.splits * (c->head_dim + 2) * sizeof(float) : 0;
 }
 
-template <class T, int D, int NT> int launch_few(const AttendParams &p, const Plan &f, dim3 grid, int dev, cudaStream_t s)
+template <class T, int D, int NT, bool TREE> int launch_few(const AttendParams &p, const Plan &f, dim3 grid, int dev, cudaStream_t s)
 {
     static std::atomic<uint64_t> ready{0};               // devices that have the attribute set
     constexpr size_t ring = (size_t)kFewWarps * kFewStages * FewStage<D>::kBytes, queries = NT * (D / 32) * 512;
     constexpr size_t sums = 8 * NT * (kFewWarps * (D + 3) + D + 2) * sizeof(float);
     constexpr size_t smem = ring + queries > sums ? ring + queries : sums;
-    auto kernel = few_kernel<T, D, NT>;
+    auto kernel = few_kernel<T, D, NT, TREE>;
     if (smem > 48 * 1024 && !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return cuda_status(e);
@@ -591,13 +604,13 @@ template <class T, int D, int NT> int launch_few(const AttendParams &p, const Pl
     return launch<AttendParams>(kernel, grid, 32 * kFewWarps, smem, f.cluster ? f.splits : 1, false, s, p);
 }
 
-template <class T, int D> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
+template <class T, int D, bool TREE> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
 {
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
-    const int st = f.nt == 0   ? launch_prompt(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s)
-                   : f.nt == 1 ? launch_few<T, D, 1>(p, f, grid, dev, s)
-                               : launch_few<T, D, 2>(p, f, grid, dev, s);
+    const int st = f.nt == 0   ? launch_prompt(p, D, std::is_same<T, __half>::value, TREE, f.slabs, (int)pairs, dev, s)
+                   : f.nt == 1 ? launch_few<T, D, 1, TREE>(p, f, grid, dev, s)
+                               : launch_few<T, D, 2, TREE>(p, f, grid, dev, s);
     if (st != E2_OK || f.splits == 1 || f.cluster) return st;
     const dim3 rows((unsigned)f.slabs * (f.nt ? 8 * f.nt : kPromptRows), pairs);
     return launch<AttendParams>(join_kernel<T, D>, rows, 128, 0, 1, true, s, p);
@@ -616,32 +629,29 @@ int check_args(const e2_cache *c, const e2_attend_args *a)
     return E2_OK;
 }
 
-}  // namespace
-}  // namespace e2ops
-
-using namespace e2ops;
-
-extern "C" size_t e2_cache_attend_workspace(const e2_cache *c, const e2_attend_args *a)
+size_t workspace_of(const e2_cache *c, const e2_attend_args *a)
 {
     Device dev;
     if (!c || c->kv_heads < 1 || check_args(c, a) || a->tokens == 0 || a->batch == 0 || current_device(&dev)) return 0;
     return workspace_for(c, a, plan(c, a, dev.sms));
 }
 
-extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace, size_t workspace_bytes,
-                               void *stream)
+template <bool TREE> int attend(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
+                                size_t workspace_bytes, void *stream)
 {
     Device dev;
     if (int st = current_device(&dev)) return st;
     if (int st = check_cache(c, dev.id)) return st;
     if (int st = check_args(c, a)) return st;
+    if (TREE && a->max_new > E2_MAX_DRAFT) return fail(E2_EINVAL, "max_new must be in 0..E2_MAX_DRAFT");
     if (a->tokens == 0 || a->batch == 0) return E2_OK;
     const int64_t row = (int64_t)a->q_heads * c->head_dim;
     if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || a->q_stride % 8 || a->out_stride % 8 ||
         a->q_stride < row || a->out_stride < row)
         return fail(E2_EINVAL, "q, out: 16-byte aligned, token strides multiples of 8 and at least a row");
-    if (!a->table || !a->lens || !a->starts) return fail(E2_EINVAL, "table, lens and starts must be given");
-    const void *ptrs[] = {a->q, a->out, a->table, a->lens, a->starts};
+    if (!a->table || !a->lens || !a->starts || (TREE && !parents))
+        return fail(E2_EINVAL, TREE ? "table, lens, starts and parents must be given" : "table, lens and starts must be given");
+    const void *ptrs[] = {a->q, a->out, a->table, a->lens, a->starts, TREE ? parents : a->starts};
     for (const void *p : ptrs)
         if (!on_device(p, dev.id)) return fail(E2_EINVAL, "arrays must be memory of the current device");
     if ((int64_t)a->batch * c->kv_heads > 65535) return fail(E2_EINVAL, "batch * kv_heads must not exceed 65535");
@@ -653,10 +663,31 @@ extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void 
     AttendParams p{c->pages, __builtin_ctz((unsigned)c->page_size), c->kv_heads, a->tokens, a->q_heads, a->batch, a->window,
                    a->table_cols, f.splits, a->table_stride, a->q_stride, a->out_stride, {c->k_codes, c->v_codes},
                    {reinterpret_cast<const __half2 *>(c->k_scales), reinterpret_cast<const __half2 *>(c->v_scales)},
-                   a->table, a->lens, a->starts, a->scale, a->q, a->out, need ? static_cast<float *>(workspace) : nullptr};
+                   a->table, a->lens, a->starts, a->scale, a->q, a->out, need ? static_cast<float *>(workspace) : nullptr, parents};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool half = a->dtype == E2_F16;
     if (c->head_dim == 64)
-        return half ? launch_attend<__half, 64>(p, f, dev.id, s) : launch_attend<__nv_bfloat16, 64>(p, f, dev.id, s);
-    return half ? launch_attend<__half, 128>(p, f, dev.id, s) : launch_attend<__nv_bfloat16, 128>(p, f, dev.id, s);
+        return half ? launch_attend<__half, 64, TREE>(p, f, dev.id, s) : launch_attend<__nv_bfloat16, 64, TREE>(p, f, dev.id, s);
+    return half ? launch_attend<__half, 128, TREE>(p, f, dev.id, s) : launch_attend<__nv_bfloat16, 128, TREE>(p, f, dev.id, s);
+}
+
+}  // namespace
+}  // namespace e2ops
+
+using namespace e2ops;
+
+extern "C" size_t e2_cache_attend_workspace(const e2_cache *c, const e2_attend_args *a) { return workspace_of(c, a); }
+
+extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace, size_t workspace_bytes,
+                               void *stream)
+{
+    return attend<false>(c, a, nullptr, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t e2_cache_attend_tree_workspace(const e2_cache *c, const e2_attend_args *a) { return workspace_of(c, a); }
+
+extern "C" int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
+                                    size_t workspace_bytes, void *stream)
+{
+    return attend<true>(c, a, parents, workspace, workspace_bytes, stream);
 }

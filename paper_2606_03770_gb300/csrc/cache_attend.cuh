@@ -18,6 +18,7 @@ struct AttendParams {
     const void *q;
     void *out;
     float *parts;            // [tokens][q_heads][splits][D + 2]: a split's sums, maximum and sum of weights
+    const int32_t *parents;  // [tokens], of trees
 };
 
 // One request and KV head: its queries, times the query heads that share the KV head,
@@ -25,7 +26,7 @@ struct AttendParams {
 // range) are none of them; the others keep their positions, which may be far below 0.
 struct Rows {
     int start, share;
-    int64_t count, first_pos;                // rows; position of the first query
+    int64_t count, first_pos, skipped;       // rows; position of the first query; queries before it
     __device__ Rows(const AttendParams &p, int request)
     {
         const int64_t from = p.starts[request], to = p.starts[request + 1];
@@ -34,6 +35,7 @@ struct Rows {
         share = p.q_heads / p.kv_heads;
         count = end > first ? (end - first) * share : 0;
         first_pos = p.lens[request] - (to - first);
+        skipped = first - from;
     }
 };
 
@@ -53,6 +55,36 @@ struct Slab {
     __device__ bool live(int c) const { return c < left; }
 };
 
+// A request's tree: what its nodes see.  Keys before `base` are of the tokens before the tree, key
+// base + a is node a's (a tree far below token 0 has no keys, wherever it is).
+struct Tree {
+    int base, window;
+    const int8_t *parents;                   // [E2_MAX_DRAFT], in shared memory
+    __device__ Tree(const AttendParams &p, const Rows &r, const int8_t *parents)
+        : base((int)max(r.first_pos - r.skipped, (int64_t)-E2_MAX_DRAFT)), window(p.window), parents(parents)
+    {
+    }
+    // All threads of a block; a barrier has to follow.
+    static __device__ void load(const AttendParams &p, int request, int8_t *parents)
+    {
+        for (int i = threadIdx.x; i < E2_MAX_DRAFT; i += blockDim.x) {
+            const int64_t t = (int64_t)p.starts[request] + i;
+            const int parent = t >= 0 && t < p.tokens ? p.parents[t] : -1;
+            parents[i] = parent >= 0 && parent < i ? (int8_t)parent : (int8_t)-1;
+        }
+    }
+    // Bit a: whether the node sees node a's key; and the first key of those before `base`.
+    __device__ uint64_t way(int64_t node, int &lowest) const
+    {
+        uint64_t seen = 0;
+        int depth = 0;
+        for (int a = (int)node; a >= 0; a = parents[a], ++depth)
+            if (window == 0 || depth < window) seen |= 1ull << a;
+        lowest = window > 0 ? max(base + (depth - window), 0) : 0;
+        return seen;
+    }
+};
+
 __device__ __forceinline__ float power2(float x)
 {
     float y;
@@ -67,6 +99,6 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
 
 // The rows of a prompt (cache_attend_prompt.cu): blocks of kPromptRows, `splits` parts of the keys.
 constexpr int kPromptRows = 256;
-int launch_prompt(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s);
+int launch_prompt(const AttendParams &p, int head_dim, bool half, bool tree, int blocks, int pairs, int dev, cudaStream_t s);
 
 }  // namespace e2ops

@@ -1,5 +1,5 @@
-// kv_cache.cu -- e2_cache_append and e2_cache_read: tokens into and out of the
-// paged 4-bit cache.
+// kv_cache.cu -- e2_cache_append, e2_cache_read and e2_cache_keep: tokens into, out of and within
+// the paged 4-bit cache.
 //
 // A lane holds eight neighbouring elements of a head (16 bytes in, one word of
 // codes out), eight lanes a group of E2_CACHE_GROUP, so a group's minimum and
@@ -199,6 +199,76 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads) read_kerne
     }
 }
 
+// Tokens of accepted ways, to their places.  A warp has a request's tokens of one layer and head:
+// it reads them all, keys and values, in pieces of 16 bytes (and the scales, four or eight), and
+// writes them then, so that a token may go where another comes from.  Bound by the way to the
+// first byte, of addresses that hang on one another (lengths, nodes, pages).
+struct KeepParams {
+    int layers, batch, cols, pages, page_shift, kv_heads, table_cols;
+    const unsigned long long *arrays;
+    const int32_t *table, *lens, *starts, *nodes, *kept;
+    int64_t table_stride, nodes_stride;
+    int32_t *lens_out;
+};
+
+template <int D> __global__ void __launch_bounds__(kThreads) keep_kernel(const KeepParams p)
+{
+    // of a token: keys' pieces and scales, values' pieces and scales
+    constexpr int kPieces = D / 32, kItems = 2 * (kPieces + 1), kMost = (E2_MAX_DRAFT * kItems + 31) / 32;
+    const int lane = threadIdx.x % 32;
+    const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32;
+    if (unit >= (int64_t)p.layers * p.batch * p.kv_heads) return;
+    const int head = (int)(unit % p.kv_heads), request = (int)(unit / p.kv_heads % p.batch), layer = (int)(unit / p.kv_heads / p.batch);
+    const int64_t count = (int64_t)p.starts[request + 1] - p.starts[request], base = p.lens[request] - count;
+    const int kept = (int)max(min(min((int64_t)p.kept[request], count), (int64_t)p.cols), (int64_t)0);
+    if (layer == 0 && head == 0 && lane == 0) p.lens_out[request] = (int32_t)max(base + kept, (int64_t)0);
+    const int32_t *nodes = p.nodes + request * p.nodes_stride, *table = p.table + request * p.table_stride;
+    const unsigned long long *arrays = p.arrays + 4 * layer;
+    // the head vector of a token, -1 where it is not in the cache
+    auto vector_at = [&](int64_t token) {
+        if (token < 0 || token >> p.page_shift >= p.table_cols) return (int64_t)-1;
+        const int page = table[token >> p.page_shift];
+        if (page < 0 || page >= p.pages) return (int64_t)-1;
+        return (((int64_t)page * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
+    };
+    const int items = kept * kItems;
+    uint4 what[kMost];
+    uint8_t *where[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        where[i] = nullptr;
+        const int item = 32 * i + lane;
+        if (item < items) {
+            const int k = item / kItems, rest = item % kItems, which = rest / (kPieces + 1), piece = rest % (kPieces + 1);
+            const int node = nodes[k];
+            if (node != k && node >= 0 && node < count) {
+                const int64_t from = vector_at(base + node), to = vector_at(base + k);
+                if (from >= 0 && to >= 0) {
+                    const bool scales = piece == kPieces;
+                    uint8_t *array = reinterpret_cast<uint8_t *>(arrays[2 * which + scales]);
+                    constexpr int kScales = D / E2_CACHE_GROUP * 4;
+                    if (scales) {
+                        where[i] = array + to * kScales;
+                        if (kScales == 8) *reinterpret_cast<uint2 *>(&what[i]) = *reinterpret_cast<const uint2 *>(array + from * kScales);
+                        else what[i].x = *reinterpret_cast<const uint32_t *>(array + from * kScales);
+                    } else {
+                        where[i] = array + to * (D / 2) + piece * 16;
+                        what[i] = *reinterpret_cast<const uint4 *>(array + from * (D / 2) + piece * 16);
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();                                          // (all have been read)
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        if (!where[i]) continue;
+        if ((32 * i + lane) % (kPieces + 1) != kPieces) *reinterpret_cast<uint4 *>(where[i]) = what[i];
+        else if (D == 128) *reinterpret_cast<uint2 *>(where[i]) = make_uint2(what[i].x, what[i].y);
+        else *reinterpret_cast<uint32_t *>(where[i]) = what[i].x;
+    }
+}
+
 Cache device_cache(const e2_cache *c)
 {
     Cache d;
@@ -318,5 +388,59 @@ extern "C" int e2_cache_read(const e2_cache *c, const int64_t *slots, int32_t to
                             : dtype == E2_BF16 ? (small ? read_kernel<__nv_bfloat16, 64> : read_kernel<__nv_bfloat16, 128>)
                                                : (small ? read_kernel<float, 64> : read_kernel<float, 128>);
     f<<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
+    return cuda_status(cudaGetLastError());
+}
+
+extern "C" int e2_cache_layers(const e2_cache *caches, int32_t layers, uint64_t *arrays)
+{
+    Device dev;
+    if (!caches || !arrays || layers < 1) return fail(E2_EINVAL, "caches and arrays must be given, layers positive");
+    if (int st = current_device(&dev)) return st;
+    for (int32_t i = 0; i < layers; ++i) {
+        const e2_cache &c = caches[i];
+        if (int st = check_cache(&c, dev.id)) return st;
+        if (c.pages != caches->pages || c.page_size != caches->page_size || c.kv_heads != caches->kv_heads ||
+            c.head_dim != caches->head_dim)
+            return fail(E2_EINVAL, "the layers' caches must be of one shape");
+        // (the codes' arrays, each of this size)
+        const uintptr_t size = (uintptr_t)c.pages * c.page_size * c.kv_heads * (c.head_dim / 2);
+        for (int32_t j = 0; j <= i; ++j) {
+            const uintptr_t mine[2] = {(uintptr_t)c.k_codes, (uintptr_t)c.v_codes};
+            const uintptr_t theirs[2] = {(uintptr_t)caches[j].k_codes, (uintptr_t)caches[j].v_codes};
+            for (int k = 0; k < 4; ++k) {
+                if (j == i && k / 2 == k % 2) continue;
+                const uintptr_t a = mine[k / 2], b = theirs[k % 2];
+                if ((a < b ? b - a : a - b) < size) return fail(E2_EINVAL, "the layers' caches must not share memory");
+            }
+        }
+        const void *of[4] = {c.k_codes, c.k_scales, c.v_codes, c.v_scales};
+        for (int k = 0; k < 4; ++k) arrays[4 * (size_t)i + k] = (uint64_t)(uintptr_t)of[k];
+    }
+    return E2_OK;
+}
+
+extern "C" int e2_cache_keep(const e2_cache *c, const e2_keep_args *a, void *stream)
+{
+    Device dev;
+    if (!a) return fail(E2_EINVAL, "no arguments");
+    if (int st = current_device(&dev)) return st;
+    if (int st = check_cache(c, dev.id)) return st;
+    if (a->batch < 0 || a->layers < 1 || a->cols < 0 || a->cols > E2_MAX_DRAFT)
+        return fail(E2_EINVAL, "batch must not be negative, layers positive, cols in 0..E2_MAX_DRAFT");
+    if (a->table_cols < 1 || a->table_stride < a->table_cols || a->nodes_stride < a->cols)
+        return fail(E2_EINVAL, "table_cols in 1..table_stride, cols up to nodes_stride");
+    if (a->batch == 0) return E2_OK;
+    const void *ptrs[] = {a->arrays, a->table, a->lens, a->starts, a->kept, a->lens_out, a->cols ? a->nodes : a->lens};
+    for (const void *p : ptrs)
+        if (!p || !aligned(p, p == a->arrays ? 8 : 4) || !on_device(p, dev.id))
+            return fail(E2_EINVAL, "arrays must be given, memory of the current device");
+    if (a->lens_out < a->lens + a->batch && a->lens < a->lens_out + a->batch)
+        return fail(E2_EINVAL, "lens_out may not be lens");
+    const int64_t threads = (int64_t)a->layers * a->batch * c->kv_heads * 32, blocks = (threads + kThreads - 1) / kThreads;
+    if (a->layers > (1 << 20) || a->batch > (1 << 20) || blocks > 0x7fffffff) return fail(E2_EINVAL, "too many layers and requests for one call");
+    const KeepParams p{a->layers, a->batch, a->cols, c->pages, __builtin_ctz((unsigned)c->page_size), c->kv_heads, a->table_cols,
+                       reinterpret_cast<const unsigned long long *>(a->arrays), a->table, a->lens, a->starts, a->nodes, a->kept,
+                       a->table_stride, a->nodes_stride, a->lens_out};
+    (c->head_dim == 64 ? keep_kernel<64> : keep_kernel<128>)<<<(unsigned)blocks, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
     return cuda_status(cudaGetLastError());
 }

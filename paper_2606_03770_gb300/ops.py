@@ -8,6 +8,10 @@ weights and a 4-bit cache:
 * ``cache_append`` / ``cache_read`` / ``cache_attend``: a paged 4-bit cache of
   keys and values, written with the position rotation on the way, read back,
   and attended to by decode batches and prompts;
+* ``cache_attend_tree`` / ``verify_drafts`` / ``cache_keep``: a decode step with a tree
+  of drafted tokens for each request: attention in which a node sees its own way
+  only, which of the drafted tokens the target's probabilities accept, and the
+  accepted way's keys and values moved to where they belong;
 * ``token_logprobs``: log probabilities of given tokens, entropy and top
   alternatives.
 
@@ -27,7 +31,7 @@ from . import e2ga
 from .e2ga import E2_OK
 
 E2_F16, E2_BF16, E2_F32 = 0, 1, 2
-E2_CACHE_GROUP, E2_MAX_TOP, E2_MAX_COLS = 64, 32, 1 << 20
+E2_CACHE_GROUP, E2_MAX_TOP, E2_MAX_COLS, E2_MAX_DRAFT = 64, 32, 1 << 20, 64
 DTYPES = {torch.float16: E2_F16, torch.bfloat16: E2_BF16, torch.float32: E2_F32}
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 _MOST = 2 ** 31 - 1                        # of a c_int32, which takes larger numbers without their high bits
@@ -66,6 +70,18 @@ class e2_logprobs_args(C.Structure):
                 ("tokens", _P), ("logprob", _P), ("entropy", _P), ("values", _P), ("ids", _P)]
 
 
+class e2_verify_args(C.Structure):
+    _fields_ = [("tokens", _I), ("vocab", _I), ("dtype", _I), ("batch", _I), ("max_new", _I), ("logits", _P),
+                ("logits_stride", _L), ("draft", _P), ("draft_stride", _L), ("ids", _P), ("parents", _P),
+                ("starts", _P), ("uniforms", _P), ("temperature", _P), ("kept", _P), ("nodes", _P), ("answer", _P)]
+
+
+class e2_keep_args(C.Structure):
+    _fields_ = [("layers", _I), ("batch", _I), ("cols", _I), ("arrays", _P), ("table", _P), ("table_cols", _I),
+                ("table_stride", _L), ("lens", _P), ("starts", _P), ("nodes", _P), ("nodes_stride", _L), ("kept", _P),
+                ("lens_out", _P)]
+
+
 # name -> (restype, argtypes); the exported surface of include/e2ops.h
 SIGNATURES = {
     "e2_ops_error": (C.c_char_p, []),
@@ -75,6 +91,11 @@ SIGNATURES = {
     "e2_cache_read": (C.c_int, [_P, _P, _I, _I, _P, _L, _P, _L, _P]),
     "e2_cache_attend_workspace": (C.c_size_t, [_P, _P]),
     "e2_cache_attend": (C.c_int, [_P, _P, _P, C.c_size_t, _P]),
+    "e2_cache_attend_tree_workspace": (C.c_size_t, [_P, _P]),
+    "e2_cache_attend_tree": (C.c_int, [_P, _P, _P, _P, C.c_size_t, _P]),
+    "e2_verify_drafts": (C.c_int, [_P, _P]),
+    "e2_cache_layers": (C.c_int, [_P, _I, _P]),
+    "e2_cache_keep": (C.c_int, [_P, _P, _P]),
     "e2_token_logprobs": (C.c_int, [_P, _P]),
 }
 _lib = None
@@ -397,6 +418,11 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
     [batch + 1] first query of each request.  ``max_new`` and ``max_len``, the
     largest counts of queries and of cached tokens, are read from the device
     (a synchronisation) unless given.  scale: 1/sqrt(head_dim) unless given."""
+    return _attend("e2_cache_attend", (), cache, q, table, lens, starts, max_new, max_len, scale, window, out, workspace)
+
+
+def _attend(name, more, cache, q, table, lens, starts, max_new, max_len, scale, window, out, workspace):
+    """A function of the library that takes e2_attend_args, and `more` tensors after them."""
     dev = cache.device
     if not (isinstance(q, torch.Tensor) and q.dtype in _HALF and q.dim() == 3):
         _tensor(q, "q", _HALF, (None, None, cache.head_dim), dev)
@@ -424,12 +450,121 @@ def cache_attend(cache, q, table, lens, starts, max_new=None, max_len=None, scal
                        cache.head_dim ** -0.5 if scale is None else scale, window, q.data_ptr(), q_stride,
                        out.data_ptr(), out_stride)
     if workspace is None:
-        workspace = _workspace("e2_cache_attend_workspace", dev, cache.ref, C.byref(a))
+        workspace = _workspace(name + "_workspace", dev, cache.ref, C.byref(a))
     else:
         _need(workspace.is_contiguous(), "workspace must be contiguous")
-    _call("e2_cache_attend", dev, cache.ref, C.byref(a), workspace.data_ptr() if workspace is not None else None,
-          workspace.nbytes if workspace is not None else 0)
+    _call(name, dev, cache.ref, C.byref(a), *(x.data_ptr() for x in more),
+          workspace.data_ptr() if workspace is not None else None, workspace.nbytes if workspace is not None else 0)
     return out
+
+
+# ---- a decode step with drafted tokens ----------------------------------------------------
+def cache_attend_tree(cache, q, parents, table, lens, starts, max_new=None, max_len=None, scale=None, window=0,
+                      out=None, workspace=None):
+    """``cache_attend`` where each request's new tokens are the nodes of a tree:
+    ``parents`` int32 [tokens], a node's parent by its number in its request, -1 for
+    none.  A node sees the tokens before the tree, itself and the nodes on its way up.
+    Up to E2_MAX_DRAFT nodes a request (more are refused where ``max_new`` says so)."""
+    _like(parents, "parents", torch.int32, (q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0,), cache.device)
+    return _attend("e2_cache_attend_tree", (parents,), cache, q, table, lens, starts, max_new, max_len, scale, window, out,
+                   workspace)
+
+
+def verify_drafts(logits, ids, parents, starts, uniforms, draft=None, temperature=None, max_new=None):
+    """(kept, nodes, answer): which tokens of each request's tree the target's
+    probabilities accept.  ``logits`` [tokens, vocab] of what follows each node, ``draft``
+    those that the tokens were drawn from (None: they were not drawn), ``ids`` int32
+    and ``uniforms`` float32 [tokens], ``parents`` and ``starts`` as for
+    ``cache_attend_tree``, ``temperature`` float32 [batch] (None: 1; 0: the largest
+    logit).  ``kept`` int32 [batch] counts the accepted nodes, node 0 among them; ``nodes`` and
+    ``answer`` int32 [batch, max_new] have them and the token after each, -1 behind.  ``max_new``,
+    at most E2_MAX_DRAFT, is read from the device (a synchronisation) unless given."""
+    tokens, vocab = _tensor(logits, "logits", _FLOAT, (None, None))
+    dev = logits.device
+    if draft is not None:
+        _like(draft, "draft", logits.dtype, (tokens, vocab), dev)
+    for x, name, dtype in ((ids, "ids", torch.int32), (parents, "parents", torch.int32), (uniforms, "uniforms", torch.float32)):
+        _like(x, name, dtype, (tokens,), dev)
+    if not (isinstance(starts, torch.Tensor) and starts.dim() == 1 and starts.shape[0] > 0):
+        _tensor(starts, "starts", (torch.int32,), (None,), dev)
+        raise ValueError("starts has one entry more than there are requests")
+    batch = starts.shape[0] - 1
+    _like(starts, "starts", torch.int32, (batch + 1,), dev)
+    if temperature is not None:
+        _like(temperature, "temperature", torch.float32, (batch,), dev)
+    if torch.is_grad_enabled() and (logits.requires_grad or uniforms.requires_grad or draft is not None and draft.requires_grad
+                                    or temperature is not None and temperature.requires_grad):
+        _no_gradient(None, logits=logits, draft=draft, uniforms=uniforms, temperature=temperature)
+    if max_new is None:
+        max_new = max(0, int((starts[1:].long() - starts[:-1].long()).max())) if batch else 0
+    _need(0 <= max_new <= E2_MAX_DRAFT, f"max_new must be in 0..{E2_MAX_DRAFT}")
+    i32 = dict(dtype=torch.int32, device=dev)
+    kept = torch.empty(batch, **i32)
+    nodes, answer = torch.empty((2, batch, max_new), **i32).unbind()
+    a = e2_verify_args(tokens, vocab, DTYPES[logits.dtype], batch, max_new, logits.data_ptr(), _stride(logits),
+                       draft.data_ptr() if draft is not None else None, _stride(draft) if draft is not None else 0,
+                       ids.data_ptr(), parents.data_ptr(), starts.data_ptr(), uniforms.data_ptr(),
+                       temperature.data_ptr() if temperature is not None else None, kept.data_ptr(), nodes.data_ptr(),
+                       answer.data_ptr())
+    _call("e2_verify_drafts", dev, C.byref(a))
+    return kept, nodes, answer
+
+
+class CacheLayers(_Handle):
+    """The caches of a model's layers, all of one shape, for calls that treat them at
+    once.  Their addresses go to the device here, so it is made once and kept."""
+
+    def __init__(self, caches):
+        self.caches = tuple(caches)
+        _need(self.caches and all(isinstance(c, Cache) for c in self.caches), "caches must be Cache objects, one at least")
+        first = self.caches[0]
+        self.device, self.requires_grad = first.device, any(c.requires_grad for c in self.caches)
+        for c in self.caches:
+            _need(c.device == first.device, f"every cache must be on {first.device}")
+        n = len(self.caches)
+        structs, arrays = (e2_cache * n)(*(c.struct for c in self.caches)), (C.c_uint64 * (4 * n))()
+        with torch.cuda.device(self.device):
+            status = load().e2_cache_layers(structs, n, arrays)
+        if status != E2_OK:
+            raise ValueError(load().e2_ops_error().decode())
+        self.arrays = torch.tensor(list(arrays), dtype=torch.int64, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()         # (whatever stream they are used on)
+        self._made = frozenset(vars(self)) | {"_made"}
+
+    def __len__(self):
+        return len(self.caches)
+
+
+def cache_keep(layers, table, lens, starts, nodes, kept, lens_out=None):
+    """Move the accepted nodes' keys and values, in every layer (``CacheLayers``), to where the
+    tokens after the tree's first belong: node ``nodes[r, k]`` of request r to token
+    k of its tree, for k < ``kept[r]``.  Returns the cached tokens of each request after
+    that, int32 [batch] (``lens_out``, allocated unless given; not ``lens``)."""
+    _need(isinstance(layers, CacheLayers), "layers must be a CacheLayers")
+    dev = layers.device
+    batch, cols = _tensor(table, "table", (torch.int32,), (None, None), dev)
+    for x, name, n in ((lens, "lens", batch), (starts, "starts", batch + 1), (kept, "kept", batch)):
+        _like(x, name, torch.int32, (n,), dev)
+    if not (isinstance(nodes, torch.Tensor) and nodes.dim() == 2 and nodes.shape[0] == batch):
+        _tensor(nodes, "nodes", (torch.int32,), (batch, None), dev)
+    most = nodes.shape[1]
+    if most:
+        _like(nodes, "nodes", torch.int32, (batch, most), dev)
+    else:
+        _need(nodes.dtype is torch.int32 and nodes.device == dev, f"nodes must be torch.int32 on {dev}")
+    _need(most <= E2_MAX_DRAFT, f"nodes has more than {E2_MAX_DRAFT} columns")
+    if lens_out is None:
+        lens_out = torch.empty(batch, dtype=torch.int32, device=dev)
+    else:
+        _like(lens_out, "lens_out", torch.int32, (batch,), dev)
+    if torch.is_grad_enabled() and layers.requires_grad:
+        _no_gradient(layers)
+    first = layers.caches[0]
+    a = e2_keep_args(len(layers), batch, most, layers.arrays.data_ptr(), table.data_ptr(), cols, _stride(table),
+                     lens.data_ptr(), starts.data_ptr(), nodes.data_ptr(), _stride(nodes), kept.data_ptr(),
+                     lens_out.data_ptr())
+    _call("e2_cache_keep", dev, first.ref, C.byref(a))
+    return lens_out
 
 
 # ---- the output layer --------------------------------------------------------------------
