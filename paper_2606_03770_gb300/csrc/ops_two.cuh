@@ -95,39 +95,102 @@ struct PowerTable {
     }
 };
 
-// exp((x - m) r) / 2^e, x <= m, r > 0, in 1..2, to some 2^-44 of itself (2^-39 near e^-745); false
-// where it is at most e^lowest.  With t = (x - m) r in two parts and k = rint(t 512 / ln 2), t - k
-// ln2 / 512 is exact in its first part (k times the first part of ln2 / 512 and t are multiples of
-// 2^-34, the rest is below 2^-10), and its exponential takes three terms.  (The second part may be
-// some steps of the first.)
-constexpr float kLowestExp = -64.0f, kLowestWideExp = -745.0f;
-__device__ __forceinline__ bool exp_parts(float x, float m, const Two &r, const float2 *table, float lowest, Two &w, int &e)
+// exp(t + tl) / 2^e, in 1..2 or so, to some 2^-44 of itself (2^-41 at |t| = 256, 2^-39 at 745): with k =
+// rint(t 512 / ln 2), t - k ln2 / 512 is exact in its first part (k times the first part of
+// ln2 / 512 and t are multiples of 2^-34, the rest is below 2^-10), and its exponential takes three
+// terms.  (The second part may be some steps of the first.)
+__device__ __forceinline__ Two exp_parts(float t, float tl, const float2 *table, int &k)
 {
     constexpr double kStep = 0.693147180559945309417 / PowerTable::kSize;
     constexpr float kPer = (float)(1 / kStep), kStep1 = (float)kStep, kStep2 = (float)(kStep - (double)kStep1), kShift = 12582912.0f;
-    const Two d = sum_of(x, -m);
-    const float t = d.h * r.h;
-    const float tl = __fmaf_rn(d.l, r.h, __fmaf_rn(d.h, r.l, __fmaf_rn(d.h, r.h, -t)));
-    const float shifted = __fmaf_rn(fmaxf(t, lowest), kPer, kShift), kf = shifted - kShift;
-    const int k = __float_as_int(shifted) - __float_as_int(kShift);
+    const float shifted = __fmaf_rn(t, kPer, kShift), kf = shifted - kShift;
+    k = __float_as_int(shifted) - __float_as_int(kShift);
     const Two y = sum_of_larger(__fmaf_rn(-kf, kStep1, t), __fmaf_rn(-kf, kStep2, tl));
     const float more = __fmaf_rn(y.h * y.h, __fmaf_rn(y.h, 1.0f / 6, 0.5f), y.l);
     const float2 p = table[k & (PowerTable::kSize - 1)];
     const float a = p.x * y.h;
     const float b = __fmaf_rn(p.x, y.h, -a) + __fmaf_rn(p.x, more, __fmaf_rn(p.y, y.h, p.y));
-    w = sum_of_larger(p.x, a);
+    Two w = sum_of_larger(p.x, a);
     w.l += b;
-    e = k >> PowerTable::kBits;
-    return t > lowest;                   // (of -inf, and of differences that are infinite, the parts are NaN)
+    return w;
 }
-// The same whole, 0 below e^-64.
-__device__ __forceinline__ Two exp_of(float x, float m, const Two &r, const float2 *table)
+
+// (x - m) r in two parts.
+__device__ __forceinline__ void exponent_of(float x, float m, const Two &r, float &t, float &tl)
 {
-    Two w;
-    int e;
-    const bool some = exp_parts(x, m, r, table, kLowestExp, w, e);
-    const float scale = __int_as_float((e + 127) << 23);
-    return some ? Two{w.h * scale, w.l * scale} : Two{0, 0};
+    const Two d = sum_of(x, -m);
+    t = d.h * r.h;
+    tl = __fmaf_rn(d.l, r.h, __fmaf_rn(d.h, r.l, __fmaf_rn(d.h, r.h, -t)));
 }
+
+// exp((x - m) r), times a number that is the same for all x: what a row's elements weigh.  m is one of
+// the larger x, and none is above it by e^44.  Below e^-64 of m: 0.  Where |m r| is small the
+// exponent is x r itself (m's power of two is left out), otherwise x - m in two parts comes first.
+struct Weigher {
+    static constexpr float kLowest = -64.0f, kDirect = 192.0f;
+    Two r;
+    float m, low;
+    int bias;
+    bool direct;
+    __device__ __forceinline__ Weigher(float m, const Two &r) : r(r), m(m)
+    {
+        low = m + __fdiv_rn(kLowest, r.h);
+        direct = fabsf(m * r.h) <= kDirect && low > -3e38f;
+        bias = direct ? (int)rintf(m * r.h * 1.44269504f) : 0;
+    }
+    // N of them (the exponents in one place, for the branch).
+    template <int N> __device__ __forceinline__ void of(const float (&x)[N], const float2 *table, Two (&w)[N]) const
+    {
+        float t[N], tl[N];
+        bool some[N];
+        if (direct) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float a = fmaxf(x[j], low);
+                t[j] = a * r.h;
+                tl[j] = __fmaf_rn(a, r.l, __fmaf_rn(a, r.h, -t[j]));
+                some[j] = x[j] > low;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                exponent_of(x[j], m, r, t[j], tl[j]);
+                // (of -inf, and of differences that are infinite, the second part is NaN)
+                some[j] = t[j] > kLowest;
+                t[j] = fmaxf(t[j], kLowest), tl[j] = some[j] ? tl[j] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            int k;
+            w[j] = exp_parts(t[j], tl[j], table, k);
+            const float scale = some[j] ? __int_as_float(((k >> PowerTable::kBits) + (127 - bias)) << 23) : 0.0f;
+            w[j] = Two{w[j].h * scale, w[j].l * scale};
+        }
+    }
+    __device__ __forceinline__ Two of(float x, const float2 *table) const
+    {
+        const float a[1] = {x};
+        Two w[1];
+        of(a, table, w);
+        return w[0];
+    }
+    // w 2^e is the same, however small; false: it is 0, or below e^-745, which 64 bits do not hold.
+    __device__ __forceinline__ bool wide(float x, const float2 *table, Two &w, int &e) const
+    {
+        float t, tl;
+        int k;
+        exponent_of(x, m, r, t, tl);
+        if (direct) {
+            // (not in these few bits more, but as `of` does)
+            t = x * r.h;
+            tl = __fmaf_rn(x, r.l, __fmaf_rn(x, r.h, -t));
+        }
+        const bool some = x > -INFINITY && (direct ? t - m * r.h : t) > -745.0f;
+        w = exp_parts(some ? t : 0.0f, some ? tl : 0.0f, table, k);
+        e = (k >> PowerTable::kBits) - bias;
+        return some;
+    }
+};
 
 }  // namespace e2ops

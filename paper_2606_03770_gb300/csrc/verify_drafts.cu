@@ -1,6 +1,7 @@
 // verify_drafts.cu -- e2_verify_drafts: which drafted tokens of a tree the target's
 // probabilities accept, and the token after them.
-#include <stddef.h>
+#include <atomic>
+#include <type_traits>
 
 #include "ops_mma.cuh"
 #include "ops_two.cuh"
@@ -17,7 +18,9 @@ namespace {
 // The token after the last is found in the warps' sums, then in the sums of a sixteenth of a
 // warp's run, then element by element.  The numbers that decide have some 45 bits.
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kMostCluster = 8, kRuns = kWarps * kMostCluster / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMostCluster = 16;
+constexpr int kUnit = 256;                       // elements of a run: eight a lane
+constexpr int kRing = 6144;                      // bytes of a warp's copies on their way
 constexpr float kNothing = 0x1p-36f;             // a sum below it, of what it is a part of, is rounding's
 
 struct VerifyParams {
@@ -29,8 +32,8 @@ struct VerifyParams {
     int32_t *kept, *nodes, *answer;
 };
 
-// What a warp tells the others in a pass.
-struct Part {
+// What a warp, or a block, tells the others in a pass.
+struct __align__(16) Part {
     Two p, q;                                    // sums
     float p_top, q_top;
     int first;                                   // of the largest
@@ -38,8 +41,8 @@ struct Part {
 };
 
 struct Shared {
-    float2 table[PowerTable::kSize];
-    Part parts[2][kWarps];                       // (a block may be one pass ahead of another)
+    float2 table[PowerTable::kSize], shared_table[PowerTable::kSize];
+    Part parts[kWarps], blocks[2][kMostCluster];  // (a block may be one pass ahead of another)
     Two sub[kWarps];
     int32_t ids[E2_MAX_DRAFT], parents[E2_MAX_DRAFT];
     float uniforms[E2_MAX_DRAFT];
@@ -47,8 +50,10 @@ struct Shared {
 
 __device__ const PowerTable power_table = PowerTable();
 
-__device__ __forceinline__ int peer_load_int(uint32_t at) { return __float_as_int(peer_load(at)); }
-__device__ __forceinline__ Two peer_load_two(uint32_t at) { return Two{peer_load(at), peer_load(at + 4)}; }
+__device__ __forceinline__ void peer_store4(uint32_t at, const float4 &v)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
 
 // w times 2^e, e <= 0, with its second part in its place; 0 from 2^-120 on.
 __device__ __forceinline__ Two scaled(const Two &w, int e)
@@ -58,152 +63,363 @@ __device__ __forceinline__ Two scaled(const Two &w, int e)
     return sum_of_larger(w.h * f, w.l * f);
 }
 
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t bits_of(const float *x) { return __float_as_uint(*x); }
+__device__ __forceinline__ uint32_t bits_of(const __half *x) { return *reinterpret_cast<const uint16_t *>(x); }
+__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16 *x) { return *reinterpret_cast<const uint16_t *>(x); }
+// The low or the high 16 bits' number.
+template <class T> __device__ __forceinline__ float half_of(uint32_t w, int high)
+{
+    if (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)(high ? w >> 16 : w & 0xffff)));
+    return __uint_as_float(high ? w & 0xffff0000u : w << 16);
+}
+
 template <class T> struct Walk {
+    static constexpr int kWords = 8 * sizeof(T) / 4, kStages = kRing / (2 * kUnit * (int)sizeof(T));
     const VerifyParams &p;
     Shared &m;
     int lane, warp, rank, turn;
     int first, end;                              // this warp's run
+    uint4 *ring;
     const T *x, *y;                              // the node's rows
+    bool wide;                                   // 16-byte loads
     Two heat;                                    // 1 / T
-    float x_top, y_top;
-    Two runs[kRuns];                             // sums of the runs kRuns lane + j
+    float x_top, y_top;                          // one of the largest of each
+    Two run, block;                              // sums of this warp's run, and of the lane's block
 
-    __device__ Walk(const VerifyParams &p, Shared &m) : p(p), m(m), turn(0)
+    __device__ Walk(const VerifyParams &p, Shared &m, uint8_t *dynamic) : p(p), m(m), turn(0)
     {
         lane = threadIdx.x % 32, warp = threadIdx.x / 32, rank = blockIdx.x % p.split;
+        ring = reinterpret_cast<uint4 *>(dynamic + warp * kRing);
         first = run_start(rank * kWarps + warp), end = run_start(rank * kWarps + warp + 1);
     }
     __device__ int run_start(int run) const
     {
-        const int64_t units = ((int64_t)p.vocab + 31) / 32;
-        return (int)min(32 * (units * run / (kWarps * p.split)), (int64_t)p.vocab);
+        const int64_t units = ((int64_t)p.vocab + kUnit - 1) / kUnit;
+        return (int)min(kUnit * (units * run / (kWarps * p.split)), (int64_t)p.vocab);
     }
 
-    // Every warp's part, to all: visit(run, address).  The next pass writes the other half.
-    template <class F> __device__ void exchange(const Part &mine, F visit)
+    // What the lanes have, over the warp, the block and the cluster: join(k) takes in what lanes k apart
+    // have, for powers of two below the lanes that there are.
+    template <class F> __device__ __forceinline__ void exchange(Part &mine, F join)
     {
-        if (lane == 0) m.parts[turn][warp] = mine;
-        cluster_barrier();
-        const uint32_t at = smem_addr(m.parts[turn]);
-#pragma unroll
-        for (int j = 0; j < kRuns; ++j) {
-            const int run = kRuns * lane + j;
-            if (run < kWarps * p.split) visit(j, peer_addr(at + run % kWarps * (int)sizeof(Part), run / kWarps));
+        auto over = [&](int lanes) {
+#pragma unroll 1
+            for (int k = 1; k < lanes; k *= 2) join(k);
+        };
+        over(32);
+        run = mine.p;
+        if (lane == 0) m.parts[warp] = mine;
+        __syncthreads();
+        mine = m.parts[lane % kWarps];
+        over(kWarps);
+        block = mine.p;
+        if (p.split > 1) {
+            if (warp == 0 && lane < p.split) {
+                const uint32_t to = peer_addr(smem_addr(&m.blocks[turn][rank]), lane);
+                peer_store4(to, make_float4(mine.p.h, mine.p.l, mine.q.h, mine.q.l));
+                peer_store4(to + 16, make_float4(mine.p_top, mine.q_top, __int_as_float(mine.first), __int_as_float(mine.bad)));
+            }
+            cluster_barrier();
+            mine = m.blocks[turn][lane % p.split];
+            block = mine.p;
+            over(p.split);
+            turn ^= 1;
+        } else {
+            __syncthreads();                     // (the parts have been read)
         }
-        turn ^= 1;
+    }
+
+    // Eight elements of each lane's.
+    struct Eight {
+        uint32_t w[kWords];
+    };
+    static __device__ __forceinline__ float element(const Eight &e, int j)
+    {
+        return sizeof(T) == 4 ? __uint_as_float(e.w[j]) : half_of<T>(e.w[j / 2], j % 2);
+    }
+    __device__ __forceinline__ Eight from_row(const T *row, int at) const
+    {
+        Eight e;
+        if (wide) {
+#pragma unroll
+            for (int k = 0; k < kWords / 4; ++k) {
+                const uint4 four = reinterpret_cast<const uint4 *>(row + at + 8 * lane)[k];
+                e.w[4 * k] = four.x, e.w[4 * k + 1] = four.y, e.w[4 * k + 2] = four.z, e.w[4 * k + 3] = four.w;
+            }
+        } else {
+            constexpr int kIn = 4 / sizeof(T);
+#pragma unroll
+            for (int k = 0; k < 8 / kIn; ++k) {
+                e.w[k] = bits_of(row + at + 32 * kIn * k + lane);
+                if (kIn == 2) e.w[k] |= bits_of(row + at + 32 * kIn * k + 32 + lane) << 16;
+            }
+        }
+        return e;
+    }
+    // A lane writes and reads its own 16 bytes of the ring only: [stage][row][eights' parts][32].
+    __device__ __forceinline__ uint4 *ring_at(int unit, int row) const
+    {
+        return ring + ((unit % kStages * 2 + row) * (kWords / 4)) * 32 + lane;
+    }
+    __device__ __forceinline__ void to_ring(const T *row, int unit, int which) const
+    {
+        const uint32_t to = smem_addr(ring_at(unit, which));
+#pragma unroll
+        for (int k = 0; k < kWords / 4; ++k)
+            copy_async16(to + 512 * k, reinterpret_cast<const uint4 *>(row + first + unit * kUnit + 8 * lane) + k, true);
+    }
+    __device__ __forceinline__ Eight from_ring(int unit, int which) const
+    {
+        Eight e;
+#pragma unroll
+        for (int k = 0; k < kWords / 4; ++k) {
+            const uint4 four = ring_at(unit, which)[32 * k];
+            e.w[4 * k] = four.x, e.w[4 * k + 1] = four.y, e.w[4 * k + 2] = four.z, e.w[4 * k + 3] = four.w;
+        }
+        return e;
+    }
+
+    // This warp's run of a new node, f(j, an element of x, of y): through the ring, which keeps it where it fits.
+    template <bool BOTH> __device__ __forceinline__ void start_stream() const
+    {
+        const int units = (end - first) / kUnit;
+        if (!wide) return;
+#pragma unroll
+        for (int u = 0; u < kStages; ++u) {
+            if (u < units) {
+                to_ring(x, u, 0);
+                if (BOTH) to_ring(y, u, 1);
+            }
+            copy_commit();
+        }
+    }
+    template <bool BOTH, class F> __device__ __forceinline__ void stream(F f) const
+    {
+        const int units = (end - first) / kUnit;
+#pragma unroll 1
+        for (int u = 0; u < units; ++u) {
+            Eight a, b;
+            if (wide) {
+                copy_wait<kStages - 1>();
+                a = from_ring(u, 0);
+                if (BOTH) b = from_ring(u, 1);
+            } else {
+                a = from_row(x, first + u * kUnit);
+                if (BOTH) b = from_row(y, first + u * kUnit);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f(j, element(a, j), BOTH ? element(b, j) : 0.0f);
+            if (wide) {
+                if (u + kStages < units) {
+                    to_ring(x, u + kStages, 0);
+                    if (BOTH) to_ring(y, u + kStages, 1);
+                }
+                copy_commit();
+            }
+        }
+#pragma unroll 1
+        for (int i = first + units * kUnit + lane; i < end; i += 32) f(0, to_float(x[i]), BOTH ? to_float(y[i]) : 0.0f);
+    }
+    // The same run again, f(two elements of x, of y): a short loop, as f is long.
+    template <bool BOTH, class F> __device__ __forceinline__ void pairs(F f) const
+    {
+        constexpr int kStep = sizeof(T) / 2;                              // words of two
+        const int units = (end - first) / kUnit, rest = end - first - units * kUnit;
+        const bool kept = wide && units <= kStages;
+        Eight a, b;
+        if (units > 0 && !kept) {
+            a = from_row(x, first);
+            if (BOTH) b = from_row(y, first);
+        }
+#pragma unroll 1
+        for (int unit = 0; unit < units + (rest > 0); ++unit) {
+            Eight u = a, v = b;
+            const int at = first + unit * kUnit;
+            if (kept && unit < units) {
+                u = from_ring(unit, 0);
+                if (BOTH) v = from_ring(unit, 1);
+            } else if (unit + 1 < units) {
+                a = from_row(x, at + kUnit);
+                if (BOTH) b = from_row(y, at + kUnit);
+            }
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                float c[2] = {element(u, 0), element(u, 1)}, d[2] = {0, 0};
+                if (BOTH) d[0] = element(v, 0), d[1] = element(v, 1);
+                if (unit == units) {                                          // (the rest of the row)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int i = at + 64 * k + 32 * e + lane;
+                        c[e] = i < end ? to_float(x[i]) : -INFINITY;
+                        if (BOTH) d[e] = i < end ? to_float(y[i]) : -INFINITY;
+                    }
+                }
+                f(c, d);
+#pragma unroll
+                for (int w = 0; w + kStep < kWords; ++w) {
+                    u.w[w] = u.w[w + kStep];
+                    if (BOTH) v.w[w] = v.w[w + kStep];
+                }
+            }
+        }
+    }
+
+    // In 32 bits: sums of 2^((x - x_top) log2 e / T), and of y's; false where these say nothing (no
+    // distribution, or the tops are far from it).  Few of the row stand for the largest.
+    template <bool BOTH> __device__ __forceinline__ bool estimate(float &x_sum, float &y_sum)
+    {
+        start_stream<BOTH>();
+        float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = (int)((int64_t)p.vocab * (4 * lane + j) / 128);
+            a = fmaxf(a, to_float(x[i]));
+            if (BOTH) b = fmaxf(b, to_float(y[i]));
+        }
+#pragma unroll
+        for (int k = 16; k; k /= 2) {
+            a = fmaxf(a, __shfl_xor_sync(~0u, a, k));
+            if (BOTH) b = fmaxf(b, __shfl_xor_sync(~0u, b, k));
+        }
+        x_top = a, y_top = b;
+        const float f = heat.h * 1.44269504f, ca = a * f, cb = b * f;
+        float sa[2] = {0, 0}, sb[2] = {0, 0};
+        stream<BOTH>([&](int j, float u, float v) {
+            sa[j % 2] += power2(__fmaf_rn(u, f, -ca));
+            if (BOTH) sb[j % 2] += power2(__fmaf_rn(v, f, -cb));
+        });
+        Part mine{{sa[0] + sa[1], sb[0] + sb[1]}, {0, 0}, 0, 0, 0, 0};
+        exchange(mine, [&](int k) {
+            mine.p.h += __shfl_xor_sync(~0u, mine.p.h, k);
+            if (BOTH) mine.p.l += __shfl_xor_sync(~0u, mine.p.l, k);
+        });
+        x_sum = mine.p.h, y_sum = mine.p.l;
+        // (a NaN, or +inf, is in the sum; a sample without a token, or with none of the large ones, too)
+        constexpr float kLeast = 0.5f, kMost = 0x1p62f;
+        return x_sum > kLeast && x_sum < kMost && (!BOTH || (y_sum > kLeast && y_sum < kMost));
     }
 
     // The largest of x (and of y): whether both rows have a distribution, and x's first largest.
-    __device__ bool tops(bool both, int &where)
+    __device__ __forceinline__ bool tops(bool both, int &where)
     {
         Part mine{{0, 0}, {0, 0}, -INFINITY, -INFINITY, 0x7fffffff, 0};
-        for (int i = first + lane; i < end; i += 32) {
-            const float a = to_float(x[i]), b = both ? to_float(y[i]) : 0.0f;
-            if (a > mine.p_top) mine.p_top = a, mine.first = i;
-            mine.q_top = fmaxf(mine.q_top, b);
-            mine.bad |= !(a < INFINITY) || !(b < INFINITY);
-        }
+        for (int i0 = first; i0 < end; i0 += kUnit)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 32 * j + lane;
+                const float a = i < end ? to_float(x[i]) : -INFINITY, b = both && i < end ? to_float(y[i]) : -INFINITY;
+                if (a > mine.p_top) mine.p_top = a, mine.first = i;
+                mine.q_top = fmaxf(mine.q_top, b);
+                mine.bad |= !(a < INFINITY) || !(b < INFINITY);
+            }
         auto join = [&](float a, float b, int at, int bad) {
             if (a > mine.p_top || (a == mine.p_top && at < mine.first)) mine.first = at;
             mine.p_top = fmaxf(mine.p_top, a);
             mine.q_top = fmaxf(mine.q_top, b);
             mine.bad |= bad;
         };
-        auto warp_join = [&] {
-#pragma unroll
-            for (int k = 16; k; k /= 2)
-                join(__shfl_xor_sync(~0u, mine.p_top, k), __shfl_xor_sync(~0u, mine.q_top, k), __shfl_xor_sync(~0u, mine.first, k),
-                     __shfl_xor_sync(~0u, mine.bad, k));
-        };
-        warp_join();
-        exchange(mine, [&](int, uint32_t at) {
-            join(peer_load(at + offsetof(Part, p_top)), peer_load(at + offsetof(Part, q_top)), peer_load_int(at + offsetof(Part, first)),
-                 peer_load_int(at + offsetof(Part, bad)));
+        exchange(mine, [&](int k) {
+            join(__shfl_xor_sync(~0u, mine.p_top, k), __shfl_xor_sync(~0u, mine.q_top, k), __shfl_xor_sync(~0u, mine.first, k),
+                 __shfl_xor_sync(~0u, mine.bad, k));
         });
-        warp_join();
         x_top = mine.p_top, y_top = mine.q_top, where = mine.first;
         return !mine.bad && x_top > -INFINITY && (!both || y_top > -INFINITY);
     }
 
-    // One element of what P is of: w, or (w - share of the draft's)+.
-    __device__ __forceinline__ Two weight(int i, bool less, const Two &share) const
+    // What P is of, of an element: w, or (w - the draft's)+.
+    static __device__ __forceinline__ Two less_of(const Two &a, const Two &b)
     {
-        const Two a = exp_of(to_float(x[i]), x_top, heat, m.table);
-        if (!less) return a;
-        const Two b = share * exp_of(to_float(y[i]), y_top, heat, m.table), d = a - b;
+        const Two s = sum_of(a.h, -b.h);
+        const Two d = sum_of_larger(s.h, s.l + (a.l - b.l));
         return d.h > 0 ? d : Two{0, 0};
     }
+    // (the draft's weights carry their share in their table)
+    __device__ __forceinline__ Two weight(int i, bool less, const Weigher of_x, const Weigher of_y) const
+    {
+        const Two a = of_x.of(to_float(x[i]), m.table);
+        return less ? less_of(a, of_y.of(to_float(y[i]), m.shared_table)) : a;
+    }
+    // All threads of the block: from here on the draft's weights are times `share`.
+    __device__ void set_share(const Two &share)
+    {
+        __syncthreads();
+        for (int i = threadIdx.x; i < PowerTable::kSize; i += kThreads) {
+            const Two w = Two{m.table[i].x, m.table[i].y} * share;
+            m.shared_table[i] = float2{w.h, w.l};
+        }
+        __syncthreads();
+    }
 
-    // Sums of x's weights, less `share` of y's where it says so, by runs and whole; and of y's alone.
-    __device__ Two sums(bool less, const Two &share, bool both, Two &q)
+    // Sums by runs and whole: of x's weights, and of y's (LESS: of x's less y's share instead).
+    template <bool BOTH, bool LESS> __device__ __forceinline__ Two sums(const Weigher of_x, const Weigher of_y, Two &q)
     {
         LongSum a, b;
-        for (int i = first + lane; i < end; i += 32) {
-            a.add(weight(i, less, share));
-            if (both) b.add(exp_of(to_float(y[i]), y_top, heat, m.table));
-        }
-        const Part mine{warp_sum(a.value()), both ? warp_sum(b.value()) : Two{0, 0}, 0, 0, 0, 0};
-        Two total{0, 0};
-        q = Two{0, 0};
+        pairs<BOTH || LESS>([&](const float (&u)[2], const float (&v)[2]) {
+            Two w[2], d[2];
+            of_x.of(u, m.table, w);
+            if (BOTH || LESS) of_y.of(v, LESS ? m.shared_table : m.table, d);
 #pragma unroll
-        for (int j = 0; j < kRuns; ++j) runs[j] = Two{0, 0};
-        exchange(mine, [&](int j, uint32_t at) {
-            runs[j] = peer_load_two(at + offsetof(Part, p));
-            total = total + runs[j];
-            if (both) q = q + peer_load_two(at + offsetof(Part, q));
+            for (int j = 0; j < 2; ++j) {
+                a.add(LESS ? less_of(w[j], d[j]) : w[j]);
+                if (BOTH) b.add(d[j]);
+            }
         });
-        if (both) q = warp_sum(q);
-        return warp_sum(total);
+        Part mine{a.value(), b.value(), 0, 0, 0, 0};
+        exchange(mine, [&](int k) {
+            mine.p = mine.p + shuffle_xor(mine.p, k);
+            if (BOTH) mine.q = mine.q + shuffle_xor(mine.q, k);
+        });
+        q = mine.q;
+        return mine.p;
     }
 
     // The first v whose share of the sums in order passes u, in one warp of one block, which it
     // returns true to.  gone(i): tokens that P has lost.
-    template <class F> __device__ bool find(float u, bool less, const Two &share, F gone, int &answer)
+    template <class F> __device__ __forceinline__ bool find(float u, bool less, const Weigher of_x, const Weigher of_y, F gone, int &answer)
     {
-        // the run
-        Two mine{0, 0};
-#pragma unroll
-        for (int j = 0; j < kRuns; ++j) mine = mine + runs[j];
-        const Two up_to = warp_prefix(mine, lane);
-        const Two total{__shfl_sync(~0u, up_to.h, 31), __shfl_sync(~0u, up_to.l, 31)};
-        const Two target = Two{u, 0} * total;
-        Two before = up_to - mine, found_before{0, 0};
-        int found = 0x7fffffff, last = -1;
-        Two last_before{0, 0};
-#pragma unroll
-        for (int j = 0; j < kRuns; ++j) {
-            const Two after = before + runs[j];
-            if (runs[j].h > 0) {
-                if (found == 0x7fffffff && target < after) found = kRuns * lane + j, found_before = before;
-                last = kRuns * lane + j, last_before = before;
-            }
-            before = after;
-        }
-        // (by rounding no run may seem to pass it: the last that has anything)
-        choose(found, found_before, last, last_before);
-        if (found / kWarps != rank) return false;
+        // of `lanes` lanes' sums, one after the other, the first that passes the target: which one, and what is before it
+        // (by rounding none may seem to: the last that has anything)
+        Two target, base{0, 0};
+        auto choose = [&](Two mine, int lanes) {
+            if (lane >= lanes) mine = Two{0, 0};
+            const Two up_to = base + warp_prefix(mine, lane);
+            Two before{__shfl_up_sync(~0u, up_to.h, 1), __shfl_up_sync(~0u, up_to.l, 1)};
+            if (lane == 0) before = base;
+            const unsigned some = __ballot_sync(~0u, mine.h > 0), hit = __ballot_sync(~0u, mine.h > 0 && target < up_to);
+            const int which = hit ? __ffs(hit) - 1 : some ? 31 - __clz(some) : 0;
+            base = Two{__shfl_sync(~0u, before.h, which), __shfl_sync(~0u, before.l, which)};
+            return which;
+        };
+        target = Two{u, 0} * warp_sum(lane < p.split ? block : Two{0, 0});
+        if (choose(block, p.split) != rank) return false;
+        if (lane == 0) m.sub[warp] = run;
+        __syncthreads();
+        const int found = rank * kWarps + choose(m.sub[lane % kWarps], kWarps);
+        __syncthreads();
         // its sixteenths
         const int from = run_start(found), units = (run_start(found + 1) - from + 31) / 32, stop = run_start(found + 1);
         auto sixteenth = [&](int k) { return min(from + 32 * (int)((int64_t)units * k / kWarps), stop); };
         LongSum a;
+#pragma unroll 1
         for (int i = sixteenth(warp) + lane; i < sixteenth(warp + 1); i += 32)
-            if (!gone(i)) a.add(weight(i, less, share));
+            if (!gone(i)) a.add(weight(i, less, of_x, of_y));
         const Two sub = warp_sum(a.value());
         if (lane == 0) m.sub[warp] = sub;
         __syncthreads();
-        mine = lane < kWarps ? m.sub[lane] : Two{0, 0};
-        const Two upto = found_before + warp_prefix(mine, lane);
-        Two was{__shfl_up_sync(~0u, upto.h, 1), __shfl_up_sync(~0u, upto.l, 1)};
-        if (lane == 0) was = found_before;
-        found = mine.h > 0 && target < upto ? lane : 0x7fffffff;
-        Two base = was;
-        choose(found, base, mine.h > 0 ? lane : -1, was);
-        if (found != warp) return false;
+        if (choose(m.sub[lane % kWarps], kWarps) != warp) return false;
         // element by element
         answer = -1;
+#pragma unroll 1
         for (int i0 = sixteenth(warp); i0 < sixteenth(warp + 1); i0 += 32) {
             const int i = i0 + lane;
-            const Two w = i < sixteenth(warp + 1) && !gone(i) ? weight(i, less, share) : Two{0, 0};
+            const Two w = i < sixteenth(warp + 1) && !gone(i) ? weight(i, less, of_x, of_y) : Two{0, 0};
             const Two sum = base + warp_prefix(w, lane);
             const unsigned some = __ballot_sync(~0u, w.h > 0), hit = __ballot_sync(~0u, w.h > 0 && target < sum);
             if (some) answer = i0 + (hit ? __ffs(hit) - 1 : 31 - __clz(some));
@@ -212,30 +428,22 @@ template <class T> struct Walk {
         }
         return true;
     }
-    // The lowest `found` of the lanes, or else the highest `last`, with what came before it.
-    __device__ void choose(int &found, Two &before, int last, const Two &last_before)
-    {
-        const unsigned some = __ballot_sync(~0u, found != 0x7fffffff), any = __ballot_sync(~0u, last >= 0);
-        const int from = some ? __ffs(some) - 1 : any ? 31 - __clz(any) : 0;
-        const int at = some ? found : last;
-        const Two b = some ? before : last_before;
-        found = max(__shfl_sync(~0u, at, from), 0);
-        before = Two{__shfl_sync(~0u, b.h, from), __shfl_sync(~0u, b.l, from)};
-    }
 };
 
-template <class T> __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyParams p)
+template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyParams p)
 {
     __shared__ Shared m;
     const int request = blockIdx.x / p.split;
-    Walk<T> walk(p, m);
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    Walk<T> walk(p, m, dynamic);
     const bool writer = walk.rank == 0 && threadIdx.x == 0;
     const int64_t start = p.starts[request], stop = p.starts[request + 1];
     const int n = start >= 0 && stop <= p.tokens ? (int)min(max(stop - start, (int64_t)0), (int64_t)p.max_new) : 0;
     for (int i = threadIdx.x; i < PowerTable::kSize; i += kThreads) m.table[i] = power_table.v[i];
     if (threadIdx.x < n) {
         m.ids[threadIdx.x] = p.ids[start + threadIdx.x];
-        m.parents[threadIdx.x] = p.parents[start + threadIdx.x];
+        const int parent = p.parents[start + threadIdx.x];
+        m.parents[threadIdx.x] = parent < (int)threadIdx.x ? parent : -1;
         const float u = p.uniforms[start + threadIdx.x];
         m.uniforms[threadIdx.x] = u > 0 ? fminf(u, 1.0f) : 0.0f;
     }
@@ -246,91 +454,124 @@ template <class T> __global__ void __launch_bounds__(kThreads) verify_kernel(con
     walk.heat = heated ? Two{1, 0} / Two{fmaxf(degree, 0x1p-126f), 0} : Two{1, 0};
     auto inside = [&](int v) { return v >= 0 && v < p.vocab; };
 
+    const int parent0 = walk.lane > 0 && walk.lane < n ? m.parents[walk.lane] : -1, parent1 = walk.lane + 32 < n ? m.parents[walk.lane + 32] : -1;
+
     int here = 0, kept = n > 0;
     int token = -1;                                       // the token after the last, in the thread that knows it
     bool knows = writer;
-    while (n > 0) {
+    while (n > 0 && (greedy || heated)) {
         walk.x = static_cast<const T *>(p.logits) + (start + here) * p.logits_stride;
-        walk.y = p.draft ? static_cast<const T *>(p.draft) + (start + here) * p.draft_stride : nullptr;
-        int child = here + 1, first;
-        auto next_child = [&] {
-            while (child < n && m.parents[child] != here) ++child;
-            return child < n;
-        };
-        bool open = next_child();
-        const bool both = p.draft && open && heated;
-        if (!(greedy || heated) || !walk.tops(both, first)) break;
-        int accepted = -1;
+        walk.y = p.draft ? static_cast<const T *>(p.draft) + (start + here) * p.draft_stride : walk.x;
+        walk.wide = (reinterpret_cast<uintptr_t>(walk.x) | reinterpret_cast<uintptr_t>(walk.y)) % 16 == 0;
+        // (bit c: node c is a child)
+        const uint64_t children = __ballot_sync(~0u, parent0 == here) | (uint64_t)__ballot_sync(~0u, parent1 == here) << 32;
+        auto first_of = [](uint64_t set) { return __ffsll(set) - 1; };
+        const bool both = p.draft && children && heated;
+        int accepted = -1, first;
         if (greedy) {
-            for (; open && accepted < 0; ++child, open = next_child())
-                if (m.ids[child] == first) accepted = child;
+            if (!walk.tops(false, first)) break;
+            for (uint64_t set = children; set && accepted < 0; set &= set - 1)
+                if (m.ids[first_of(set)] == first) accepted = first_of(set);
             if (accepted < 0) token = first;
         } else {
+            // In 32 bits first: exponents are off by 2^-18 at most (of 64, and 2^-18 of that in f), sums by less,
+            // so what is clear by one part in 2^14 is clear.
+            constexpr float kClear = 0x1p-14f;
+            float x_sum, y_sum;
+            const int child0 = children ? first_of(children) : 0;
+            const float first_x = children && inside(m.ids[child0]) ? to_float(walk.x[m.ids[child0]]) : -INFINITY;
+            const float first_y = both && inside(m.ids[child0]) ? to_float(walk.y[m.ids[child0]]) : -INFINITY;
+            const bool clear = both ? walk.template estimate<true>(x_sum, y_sum) : walk.template estimate<false>(x_sum, y_sum);
+            if (!clear) {
+                if (!walk.tops(both, first)) break;
+            } else if (children) {
+                const float f = walk.heat.h * 1.44269504f, cx = walk.x_top * f, cy = walk.y_top * f;
+                if (p.draft) {
+                    const float w = power2(__fmaf_rn(first_x, f, -cx)) * y_sum, u = m.uniforms[child0];
+                    const float asked = u * power2(__fmaf_rn(first_y, f, -cy)) * x_sum;
+                    // (numbers that 32 bits do not hold are not clear)
+                    if (w > 0x1p-60f && asked < w * (1 - kClear)) accepted = child0;
+                } else {
+                    float left = x_sum;
+                    bool certain = true;
+                    for (uint64_t set = children; set && certain && accepted < 0; set &= set - 1) {
+                        const int c = first_of(set), v = m.ids[c];
+                        if (!inside(v)) continue;
+                        for (uint64_t done = children ^ set; done; done &= done - 1) certain &= m.ids[first_of(done)] != v;
+                        const float w = power2(__fmaf_rn(c == child0 ? first_x : to_float(walk.x[v]), f, -cx)), asked = m.uniforms[c] * left;
+                        if (!certain || !(w > 0x1p-60f)) certain = false;
+                        else if (asked < w * (1 - kClear)) accepted = c;
+                        else if (asked > w * (1 + kClear) && left - w > 0.25f * x_sum) left -= w;
+                        else certain = false;
+                    }
+                }
+            }
+        }
+        if (!greedy && accepted < 0) {
+            const Weigher of_x(walk.x_top, walk.heat), of_y(both ? walk.y_top : walk.x_top, walk.heat);
             const Two none{0, 0};
-            Two q, share = none, A = none, B{1, 0};
-            const Two all = walk.sums(false, none, both, q);
+            Two q = none, A = none, B{1, 0};
+            const Two all = both ? walk.template sums<true, false>(of_x, of_y, q) : walk.template sums<false, false>(of_x, of_x, q);
             Two left = all;                               // (without the draft's rows)
             uint64_t lost = 0;                            // rejected children whose tokens P has lost
             bool less = false;
             auto gone = [&](int v) {
                 for (uint64_t r = lost; r; r &= r - 1)
-                    if (m.ids[__ffsll(r) - 1] == v) return true;
+                    if (m.ids[first_of(r)] == v) return true;
                 return false;
             };
-            for (; open; ++child, open = next_child()) {
-                const int v = m.ids[child];
+            for (uint64_t set = children; set; set &= set - 1) {
+                const int c = first_of(set), v = m.ids[c];
                 const bool in = inside(v);
-                const float u = m.uniforms[child];
+                const float u = m.uniforms[c];
                 // its weight, however small
                 Two w = none, wq = none;
                 int e = 0, eq = 0;
-                const bool some = in && exp_parts(to_float(walk.x[v]), walk.x_top, walk.heat, m.table, kLowestWideExp, w, e);
+                const bool some = in && of_x.wide(to_float(walk.x[v]), m.table, w, e);
                 if (p.draft) {
                     // u q(v) < P(v), times Z_p Z_q B and a power of two
-                    const bool some_q = in && exp_parts(to_float(walk.y[v]), walk.y_top, walk.heat, m.table, kLowestWideExp, wq, eq);
+                    const bool some_q = in && of_y.wide(to_float(walk.y[v]), m.table, wq, eq);
                     const int most = some && some_q ? max(e, eq) : some ? e : eq;
                     w = scaled(w, some ? e - most : -127);
                     wq = scaled(wq, some_q ? eq - most : -127);
                     const Two mine = w * q - A * wq * all;
                     if ((u == 0 && !less && some) || Two{u, 0} * wq * all * B < (mine.h > 0 ? mine : none)) {
-                        accepted = child;
+                        accepted = c;
                         break;
                     }
-                    Two before[kRuns], unused;
-#pragma unroll
-                    for (int j = 0; j < kRuns; ++j) before[j] = walk.runs[j];
-                    const Two more = A + B, part = more * all / q, sum = walk.sums(true, part, false, unused) / all;
+                    const Two run = walk.run, block = walk.block;
+                    Two unused;
+                    const Two more = A + B;
+                    walk.set_share(more * all / q);
+                    const Two sum = walk.template sums<false, true>(of_x, of_y, unused) / all;
                     if (sum.h > kNothing * B.h) {
-                        A = more, B = sum, share = part, less = true;
+                        A = more, B = sum, less = true;
                     } else {
-#pragma unroll
-                        for (int j = 0; j < kRuns; ++j) walk.runs[j] = before[j];
+                        walk.run = run, walk.block = block;
+                        walk.set_share(A * all / q);
                     }
                 } else if (in && !gone(v)) {
                     w = scaled(w, some ? e : -127);
                     if ((u == 0 && some) || Two{u, 0} * left < w) {
-                        accepted = child;
+                        accepted = c;
                         break;
                     }
                     const Two rest = left - w;
                     if (some && rest.h > kNothing * left.h) {
                         left = rest;
-                        lost |= 1ull << child;
-                        // its run loses it too
-#pragma unroll
-                        for (int j = 0; j < kRuns; ++j) {
-                            const int run = kRuns * walk.lane + j;
-                            if (run < kWarps * p.split && v >= walk.run_start(run) && v < walk.run_start(run + 1)) {
-                                walk.runs[j] = walk.runs[j] - w;
-                                if (!(walk.runs[j].h > 0)) walk.runs[j] = none;
-                            }
-                        }
+                        lost |= 1ull << c;
+                        // its run loses it too, and its block
+                        auto lose = [&](Two &sum) {
+                            sum = sum - w;
+                            if (!(sum.h > 0)) sum = none;
+                        };
+                        if (v >= walk.first && v < walk.end) lose(walk.run);
+                        const int owner = walk.lane % p.split;
+                        if (v >= walk.run_start(owner * kWarps) && v < walk.run_start((owner + 1) * kWarps)) lose(walk.block);
                     }
                 }
             }
-            if (accepted < 0) {
-                knows = walk.find(m.uniforms[0], less, share, gone, token) && walk.lane == 0;
-            }
+            if (accepted < 0) knows = walk.find(m.uniforms[0], less, of_x, of_y, gone, token) && walk.lane == 0;
         }
         if (accepted < 0) break;
         if (writer) nodes[kept] = accepted, answer[kept - 1] = m.ids[accepted];
@@ -346,12 +587,39 @@ template <class T> __global__ void __launch_bounds__(kThreads) verify_kernel(con
     cluster_barrier();                                    // (peers have been read)
 }
 
-// Requests over clusters, while they have no more blocks than there are multiprocessors.
-template <class T> int launch_walks(VerifyParams p, int sms, cudaStream_t s)
+// How many clusters of 2^i blocks run at once.
+template <class T> int clusters_of(int i, int dev)
 {
-    p.split = 1;
-    while (p.split < kMostCluster && (int64_t)p.batch * p.split <= sms && p.vocab / p.split >= 4096) p.split *= 2;
-    return launch<VerifyParams>(verify_kernel<T>, dim3((unsigned)p.batch * p.split), kThreads, 0, p.split, false, s, p);
+    static std::atomic<int> known[64][5];                    // one more
+    int n = known[dev][i].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = 1u << i, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(1u << 10);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kWarps * kRing;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(verify_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaFuncSetAttribute(verify_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarps * kRing) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, verify_kernel<T>, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+        }
+        known[dev][i].store(++n, std::memory_order_relaxed);
+    }
+    return n - 1;
+}
+
+// Requests over clusters, as large as all of them run at once, and as a warp's run is 256 elements.
+template <class T> int launch_walks(VerifyParams p, const Device &dev, cudaStream_t s)
+{
+    int i = 4;
+    while (i > 0 && (p.batch > clusters_of<T>(i, dev.id) || p.vocab < (kWarps * kUnit << i) / 2)) --i;
+    p.split = 1 << i;
+    return launch<VerifyParams>(verify_kernel<T>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, false, s, p);
 }
 
 }  // namespace
@@ -385,7 +653,7 @@ extern "C" int e2_verify_drafts(const e2_verify_args *a, void *stream)
                    a->logits_stride, a->draft_stride, a->ids, a->parents, a->starts, a->uniforms, a->temperature,
                    a->kept, a->nodes, a->answer};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return a->dtype == E2_F16    ? launch_walks<__half>(p, dev.sms, s)
-           : a->dtype == E2_BF16 ? launch_walks<__nv_bfloat16>(p, dev.sms, s)
-                                 : launch_walks<float>(p, dev.sms, s);
+    return a->dtype == E2_F16    ? launch_walks<__half>(p, dev, s)
+           : a->dtype == E2_BF16 ? launch_walks<__nv_bfloat16>(p, dev, s)
+                                 : launch_walks<float>(p, dev, s);
 }
