@@ -555,19 +555,24 @@ constexpr int kPrompt = 65;
 // for a whole wave).
 constexpr int kClusterUnits = 8;
 
+// Trees' rows are by 128 from so many on.
+constexpr int kTree = 17;
+// A block of trees' rows takes the time of so many tiles more, for its start, its end and its part.
+constexpr int kTreeExtra = 12;
+
 struct Plan {
-    int nt, slabs, splits;      // nt 0: a prompt
+    int nt, slabs, splits;      // nt 0: a prompt, or a tree by kTreeRows
     bool cluster;               // joined there
 };
 
 // Rows by eight or sixteen, or by 256; keys split until every multiprocessor has its
 // blocks, no finer than 128 keys (512).
-Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
+Plan plan(const e2_cache *c, const e2_attend_args *a, int sms, bool tree)
 {
     Plan f;
     const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
-    f.nt = rows >= kPrompt ? 0 : rows <= 8 ? 1 : 2;
-    const int at_once = f.nt ? 8 * f.nt : kPromptRows;
+    f.nt = rows >= (tree ? kTree : kPrompt) ? 0 : rows <= 8 ? 1 : 2;
+    const int at_once = f.nt ? 8 * f.nt : tree ? kTreeRows : kPromptRows;
     const int64_t slabs = (rows + at_once - 1) / at_once;
     f.slabs = (int)(slabs < 65535 ? slabs : 65535);
     int64_t keys = a->max_len;
@@ -581,6 +586,15 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms)
     if (f.cluster && splits > kMostCluster) splits = kMostCluster;
     while (f.cluster && splits > 2 && pairs * splits * 8 > places * 7) --splits;
     f.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
+    if (tree && f.nt == 0) {
+        // as many parts as take the least time: rounds of blocks times the tiles of one and what it costs besides
+        const int64_t tiles = (keys + 63) / 64;
+        int64_t least_time = INT64_MAX;
+        for (int64_t s = 1; s <= kMostSplits && (s == 1 || s * 4 <= tiles); ++s) {
+            const int64_t time = (pairs * s + sms - 1) / sms * ((tiles + s - 1) / s + kTreeExtra);
+            if (time < least_time) least_time = time, f.splits = (int)s;
+        }
+    }
     return f;
 }
 
@@ -608,11 +622,11 @@ template <class T, int D, bool TREE> int launch_attend(const AttendParams &p, co
 {
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
-    const int st = f.nt == 0   ? launch_prompt(p, D, std::is_same<T, __half>::value, TREE, f.slabs, (int)pairs, dev, s)
+    const int st = f.nt == 0   ? (TREE ? launch_tree : launch_prompt)(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s)
                    : f.nt == 1 ? launch_few<T, D, 1, TREE>(p, f, grid, dev, s)
                                : launch_few<T, D, 2, TREE>(p, f, grid, dev, s);
     if (st != E2_OK || f.splits == 1 || f.cluster) return st;
-    const dim3 rows((unsigned)f.slabs * (f.nt ? 8 * f.nt : kPromptRows), pairs);
+    const dim3 rows((unsigned)f.slabs * (f.nt ? 8 * f.nt : TREE ? kTreeRows : kPromptRows), pairs);
     return launch<AttendParams>(join_kernel<T, D>, rows, 128, 0, 1, true, s, p);
 }
 
@@ -629,11 +643,11 @@ int check_args(const e2_cache *c, const e2_attend_args *a)
     return E2_OK;
 }
 
-size_t workspace_of(const e2_cache *c, const e2_attend_args *a)
+size_t workspace_of(const e2_cache *c, const e2_attend_args *a, bool tree)
 {
     Device dev;
     if (!c || c->kv_heads < 1 || check_args(c, a) || a->tokens == 0 || a->batch == 0 || current_device(&dev)) return 0;
-    return workspace_for(c, a, plan(c, a, dev.sms));
+    return workspace_for(c, a, plan(c, a, dev.sms, tree));
 }
 
 template <bool TREE> int attend(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
@@ -655,7 +669,7 @@ template <bool TREE> int attend(const e2_cache *c, const e2_attend_args *a, cons
     for (const void *p : ptrs)
         if (!on_device(p, dev.id)) return fail(E2_EINVAL, "arrays must be memory of the current device");
     if ((int64_t)a->batch * c->kv_heads > 65535) return fail(E2_EINVAL, "batch * kv_heads must not exceed 65535");
-    const Plan f = plan(c, a, dev.sms);
+    const Plan f = plan(c, a, dev.sms, TREE);
     const size_t need = workspace_for(c, a, f);
     if (need && (!workspace || workspace_bytes < need)) return fail(E2_ENOMEM, "workspace too small");
     if (need && (!aligned(workspace, 256) || !on_device(workspace, dev.id)))
@@ -676,7 +690,7 @@ template <bool TREE> int attend(const e2_cache *c, const e2_attend_args *a, cons
 
 using namespace e2ops;
 
-extern "C" size_t e2_cache_attend_workspace(const e2_cache *c, const e2_attend_args *a) { return workspace_of(c, a); }
+extern "C" size_t e2_cache_attend_workspace(const e2_cache *c, const e2_attend_args *a) { return workspace_of(c, a, false); }
 
 extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace, size_t workspace_bytes,
                                void *stream)
@@ -684,7 +698,7 @@ extern "C" int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void 
     return attend<false>(c, a, nullptr, workspace, workspace_bytes, stream);
 }
 
-extern "C" size_t e2_cache_attend_tree_workspace(const e2_cache *c, const e2_attend_args *a) { return workspace_of(c, a); }
+extern "C" size_t e2_cache_attend_tree_workspace(const e2_cache *c, const e2_attend_args *a) { return workspace_of(c, a, true); }
 
 extern "C" int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
                                     size_t workspace_bytes, void *stream)

@@ -46,11 +46,11 @@ template <int D> struct PromptShared {
 struct Span {
     Slab slab;
     int lo, hi, first, n;
-    __device__ Span(const AttendParams &p, const Rows &rows, int64_t block, const Tree *tree) : slab(rows, block * kPromptRows)
+    __device__ Span(const AttendParams &p, const Rows &rows, int64_t block) : slab(rows, block * kPromptRows)
     {
         const int last = (int)min((int64_t)kPromptRows, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
-        lo = p.window > 0 ? (int)max((tree ? tree->base : slab.pos(0)) - p.window + 1, (int64_t)0) : 0;
+        lo = p.window > 0 ? (int)max(slab.pos(0) - p.window + 1, (int64_t)0) : 0;
         hi = (int)max(min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0), (int64_t)0);
         const int tile_lo = lo / kKeys, tiles = hi > lo ? (hi + kKeys - 1) / kKeys - tile_lo : 0;
         const int per = (tiles + p.splits - 1) / p.splits;
@@ -131,9 +131,9 @@ template <int D, bool kRest> __device__ __forceinline__ void sum_up(const Shared
 }
 
 // Four warps, group g: weights, a thread a row; then the rows' outputs.
-template <class T, int D, bool TREE>
-__device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, const Tree &tree, int64_t skipped,
-                                        int kv, int g, int quarter, int lane)
+template <class T, int D>
+__device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, int kv, int g, int quarter,
+                                        int lane)
 {
     using Sh = PromptShared<D>;
     constexpr int GR = D / E2_CACHE_GROUP;
@@ -183,15 +183,8 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         __syncwarp();
         if (lane == 0) barrier_arrive(m.asked);
     }
-    int pos = row < slab.left ? (int)max(slab.pos(row), (int64_t)-1) : -1;
-    int from = row < slab.left && p.window > 0 ? (int)max(slab.pos(row) - p.window + 1, (int64_t)0) : 0;
-    uint64_t way = 0;                                        // (a tree's pos and from are of the tokens before it)
-    if (TREE) {
-        const int64_t node = skipped + slab.pos(row) - slab.first_pos;
-        pos = live ? tree.base - 1 : -1;
-        way = live ? tree.way(min(node, (int64_t)E2_MAX_DRAFT - 1), from) : 0;
-        if (live && node >= E2_MAX_DRAFT) scale = NAN;
-    }
+    const int pos = row < slab.left ? (int)max(slab.pos(row), (int64_t)-1) : -1;
+    const int from = row < slab.left && p.window > 0 ? (int)max(slab.pos(row) - p.window + 1, (int64_t)0) : 0;
     float top = -INFINITY, sum = 0;
     unsigned spoilt = 0;                                     // bit j: this row sees a value of group j that is not finite
     bool ok = true;
@@ -222,10 +215,6 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
             const int lowest = from - key0, highest = pos - key0;
             seen = highest < 0 ? 0ull : highest >= 63 ? ~0ull : (2ull << highest) - 1;
             if (lowest > 0) seen &= lowest > 63 ? 0ull : ~0ull << lowest;
-            if (TREE) {
-                const int shift = tree.base - key0;
-                seen |= shift >= 0 ? (shift > 63 ? 0ull : way << shift) : (shift < -63 ? 0ull : way >> -shift);
-            }
 #pragma unroll
             for (int w = 0; w < 4; ++w)
                 if (!(present >> (8 * w) & 1)) seen &= ~(0xffffull << (16 * w));
@@ -441,7 +430,7 @@ __device__ __forceinline__ void unpack(const AttendParams &p, const Span &span, 
     copy_wait<0>();
 }
 
-template <class T, int D, bool TREE> __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttendParams p)
+template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttendParams p)
 {
     using Sh = PromptShared<D>;
     extern __shared__ uint8_t dynamic[];
@@ -450,7 +439,6 @@ template <class T, int D, bool TREE> __global__ void __launch_bounds__(kThreads,
     __shared__ __align__(8) uint16_t bad[kStages][D / E2_CACHE_GROUP][4];
     __shared__ uint32_t tensor_memory;
     __shared__ int failed;
-    __shared__ int8_t parents[TREE ? E2_MAX_DRAFT : 1];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int request = blockIdx.x / p.kv_heads, kv = blockIdx.x % p.kv_heads;
     const Rows rows(p, request);
@@ -469,8 +457,6 @@ template <class T, int D, bool TREE> __global__ void __launch_bounds__(kThreads,
     m.there = there;
     m.bad = bad;
     m.failed = &failed;
-    const Tree tree(p, rows, parents);
-    if (TREE) Tree::load(p, request, parents);
     auto set_barriers = [&] {
         for (int i = 0; i < kStages; ++i) barrier_init(m.full + 8 * i, 8), barrier_init(m.empty + 8 * i, 2);
         for (int i = 0; i < 4; ++i)
@@ -508,7 +494,7 @@ template <class T, int D, bool TREE> __global__ void __launch_bounds__(kThreads,
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         for (int64_t block = start; block >= 0; block -= gridDim.y) {
-            const Span span(p, rows, block, TREE ? &tree : nullptr);
+            const Span span(p, rows, block);
             if (warp < 2) score<D>(m, span.n, warp);
             else sum_up<D, std::is_same<T, __half>::value>(m, span.n, warp - 2);
             meet(block >= gridDim.y);
@@ -520,24 +506,24 @@ template <class T, int D, bool TREE> __global__ void __launch_bounds__(kThreads,
     } else if (warp < 12) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         for (int64_t block = start; block >= 0; block -= gridDim.y) {
-            weights<T, D, TREE>(p, Span(p, rows, block, TREE ? &tree : nullptr), m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane);
+            weights<T, D>(p, Span(p, rows, block), m, kv, (warp - 4) / 4, warp % 4, lane);
             meet(block >= gridDim.y);
         }
         asm volatile("griddepcontrol.launch_dependents;");
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         for (int64_t block = start; block >= 0; block -= gridDim.y) {
-            unpack<D>(p, Span(p, rows, block, TREE ? &tree : nullptr), m, request, kv, (warp - 12) / 4, warp % 4, lane);
+            unpack<D>(p, Span(p, rows, block), m, request, kv, (warp - 12) / 4, warp % 4, lane);
             meet(block >= gridDim.y);
         }
         asm volatile("griddepcontrol.launch_dependents;");
     }
 }
 
-template <class T, int D, bool TREE> int launch_as(const AttendParams &p, int blocks, int pairs, int dev, cudaStream_t s)
+template <class T, int D> int launch_as(const AttendParams &p, int blocks, int pairs, int dev, cudaStream_t s)
 {
     static std::atomic<uint64_t> ready{0};                   // devices that have the attribute set
-    auto kernel = prompt_kernel<T, D, TREE>;
+    auto kernel = prompt_kernel<T, D>;
     const int smem = PromptShared<D>::kBytes > 120 * 1024 ? PromptShared<D>::kBytes : 120 * 1024;   // (tensor memory is for one block)
     if (!(ready.load(std::memory_order_relaxed) >> dev & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -548,18 +534,13 @@ template <class T, int D, bool TREE> int launch_as(const AttendParams &p, int bl
     return cuda_status(cudaGetLastError());
 }
 
-template <bool TREE> int launch_any(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s)
-{
-    if (head_dim == 64)
-        return half ? launch_as<__half, 64, TREE>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 64, TREE>(p, blocks, pairs, dev, s);
-    return half ? launch_as<__half, 128, TREE>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 128, TREE>(p, blocks, pairs, dev, s);
-}
-
 }  // namespace
 
-int launch_prompt(const AttendParams &p, int head_dim, bool half, bool tree, int blocks, int pairs, int dev, cudaStream_t s)
+int launch_prompt(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s)
 {
-    return tree ? launch_any<true>(p, head_dim, half, blocks, pairs, dev, s) : launch_any<false>(p, head_dim, half, blocks, pairs, dev, s);
+    if (head_dim == 64)
+        return half ? launch_as<__half, 64>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 64>(p, blocks, pairs, dev, s);
+    return half ? launch_as<__half, 128>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 128>(p, blocks, pairs, dev, s);
 }
 
 }  // namespace e2ops

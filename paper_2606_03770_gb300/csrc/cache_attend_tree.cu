@@ -1,0 +1,669 @@
+// cache_attend_tree.cu -- e2_cache_attend_tree from 17 rows of a request and KV head on.
+//
+// A block takes 128 rows (nodes times the query heads of a KV head) and walks over tiles of 64
+// keys.  A warp copies them, eight dequantise a tile (fp16, one rounding: 2^-11 of a value), one issues
+// S = q K^T, one O += P V, four make the weights, a thread a row.  Queries, weights and O are in tensor memory:
+// a tile's keys and values are all that the products read from shared memory, which is what bounds a
+// tile: 64 KB written and read there, 512 cycles, next to the 512 that the exponentials of 128 rows
+// take of their unit.  Rows of other requests, and of nobody, are products' ballast: a warp that has
+// none of its own makes no weights.
+// Elements of eight lie in the order that unpacking leaves (0, 4, 1, 5, 2, 6, 3, 7) in q, K and V,
+// and are put right in the output.  Weights go to fp16 times 2^7 (2^-11 each; fp16 outputs take the
+// rounding's rest in a second product).  A weight of 0 does not stop a NaN among the values, so
+// values whose scale or minimum is not finite are held back as zeros, and rows that do see their
+// keys are made NaN.
+//
+// Every wait ends: one that takes too long marks the block as failed, which then frees
+// its tensor memory and writes NaN.
+#include "cache_attend.cuh"
+#include "ops_tensor.cuh"
+
+namespace e2ops {
+namespace {
+
+constexpr int kKeys = 64, kStages = 4, kRawStages = 6, kScores = 3;
+// Warps by fours, one on each scheduler: products and copies, weights of even and of odd tiles, keys, values; and the
+// registers they split a block's 640 x 96 into.
+constexpr int kThreads = 640;
+constexpr int kBarriers = 2 * kStages + 3 * kScores + 1 + 2 * kRawStages;
+constexpr uint32_t kColumns = 512, kSums = 192, kQueries = 448;       // tensor memory: scores [3][64], sums [2][128], queries
+
+template <int D> struct TreeShared {
+    static constexpr int kBlocks = D / 64;                   // of 64 elements: 128-byte rows
+    static constexpr int kTile = kBlocks * kKeys * 128;      // a tile's keys, or values
+    // A tile as it is cached: keys' codes, values' codes, keys' scales, values' scales; 16 keys' parts of them.
+    static constexpr int kCodes = 16 * (D / 2), kScales = 16 * (D / E2_CACHE_GROUP) * 4;
+    static constexpr int kRaw = 8 * (kCodes + kScales);
+    static constexpr int kBytes = kStages * 2 * kTile + kRawStages * kRaw + 1024;
+};
+
+// 128 rows, and the tiles of keys that they see, of this split's.
+struct Span {
+    Slab slab;
+    int hi, first, n;
+    __device__ Span(const AttendParams &p, const Rows &rows, const Tree &tree, int64_t block) : slab(rows, block * kTreeRows)
+    {
+        const int last = (int)min((int64_t)kTreeRows, slab.left) - 1;
+        // (32 bits: lengths stop 64 short of 2^31)
+        const int lo = p.window > 0 ? (int)max((int64_t)tree.base - p.window + 1, (int64_t)0) : 0;
+        hi = (int)max(min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0), (int64_t)0);
+        const int tile_lo = lo / kKeys, tiles = hi > lo ? (hi + kKeys - 1) / kKeys - tile_lo : 0;
+        const int per = (tiles + p.splits - 1) / p.splits;
+        first = (int)min((int64_t)tile_lo + (int64_t)blockIdx.z * per, (int64_t)tile_lo + tiles);
+        n = min(first + per, tile_lo + tiles) - first;
+    }
+};
+
+// What a block shares.
+template <int D> struct Shared {
+    uint8_t *stages, *raw;
+    uint32_t full, empty, scored, weighed, summed, asked;    // barriers; scored, weighed, summed [kScores]
+    uint32_t copied, taken;                                  // [raw stage]
+    uint8_t (*raw_there)[4];                                 // [raw stage]
+    uint8_t (*there)[4];                                     // [stage]: whether each 16 keys are there
+    uint16_t (*bad)[D / E2_CACHE_GROUP][4];                  // [stage][group]: keys whose values are not finite
+    float *states;                                           // [row]: an odd tiles' maximum, sum of weights, spoilt groups
+    volatile int *failed;
+    uint32_t memory;
+};
+
+__device__ __forceinline__ bool warp_wait(uint32_t at, uint32_t parity, int lane)
+{
+    return __all_sync(~0u, barrier_wait(at, parity));
+}
+
+__device__ __forceinline__ bool finite(uint32_t dm) { return (dm & 0x7c00u) != 0x7c00u && (dm & 0x7c000000u) != 0x7c000000u; }
+
+// A warp: S = q K^T of each tile.
+template <int D> __device__ __forceinline__ void score(const Shared<D> &m, int n, int lane)
+{
+    using Sh = TreeShared<D>;
+    const uint32_t kind = product_kind(kKeys);
+    const uint64_t keys0 = operand(smem_addr(m.stages));
+    bool ok = warp_wait(m.asked, 0, lane);
+    int stage = 0, phase = 0, place = 0, used = 1;
+    for (int j = 0; j < n && ok; ++j) {
+        ok = warp_wait(m.full + 8 * stage, phase, lane);
+        // (the weights in this place have been used)
+        if (ok) ok = warp_wait(m.summed + 8 * place, used, lane);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (elected()) {
+            // (addresses in 16 bytes: a block of 64 elements, then 16 of them; queries in columns of two elements)
+            const uint64_t b = keys0 + stage * (2 * Sh::kTile / 16);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                issue_product(m.memory + place * 64, m.memory + kQueries + 8 * k, b + k / 4 * (kKeys * 8) + 2 * (k % 4), kind, k > 0);
+            commit_products(m.scored + 8 * place);
+        }
+        __syncwarp();
+        if (++place == kScores) place = 0, used ^= 1;
+        if (++stage == kStages) stage = 0, phase ^= 1;
+    }
+    if (!ok) *m.failed = 1;
+}
+
+// A warp: O += P V of each tile.
+template <int D, bool kRest> __device__ __forceinline__ void sum_up(const Shared<D> &m, int n, int lane)
+{
+    using Sh = TreeShared<D>;
+    const uint32_t kind = product_kind(D, true);
+    const uint64_t values0 = operand(smem_addr(m.stages) + Sh::kTile, kKeys * 128);
+    bool ok = true;
+    int stage = 0, place = 0, phase = 0;
+    for (int j = 0; j < n && ok; ++j) {
+        ok = warp_wait(m.weighed + 8 * place, phase, lane);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (elected()) {
+            const uint32_t weights = m.memory + place * 64, sums = m.memory + kSums + (j & 1) * 128;
+            const uint64_t b = values0 + stage * (2 * Sh::kTile / 16);
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 8 * k, b + k * 128, kind, j > 1 || k > 0);
+            if (kRest) {
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k) issue_product(sums, weights + 32 + 8 * k, b + k * 128, kind, true);
+            }
+            commit_products(m.summed + 8 * place);
+            commit_products(m.empty + 8 * stage);
+        }
+        __syncwarp();
+        if (++place == kScores) place = 0, phase ^= 1;
+        if (++stage == kStages) stage = 0;
+    }
+    if (!ok) *m.failed = 1;
+}
+
+// Four warps: weights of even tiles (set 0) or odd ones, a thread a row; then the rows' outputs, by set 0.
+template <class T, int D>
+__device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, const Tree &tree, int64_t skipped,
+                                        int kv, int set, int quarter, int lane)
+{
+    constexpr int GR = D / E2_CACHE_GROUP;
+    constexpr bool kRest = std::is_same<T, __half>::value;
+    const int row = 32 * quarter + lane;
+    const Slab &slab = span.slab;
+    const bool live = slab.live(row), any = slab.live(32 * quarter);
+    const int64_t token = slab.token(row);
+    const int head = slab.head(kv, row);
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+    float scale = 0;
+    if (any) {
+        // the queries, to fp16 times a power of two each (and the scale's sign)
+        const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + (live ? token * p.q_stride + head * D : 0));
+        uint4 q[D / 8];
+        unsigned largest = 0;
+#pragma unroll
+        for (int o = 0; o < D / 8; ++o) {
+            q[o] = live ? src[o] : uint4{0, 0, 0, 0};
+            largest = max(largest, octet_largest(q[o]));
+        }
+        const int power = power_for<T>(largest);
+        const float f = p.scale < 0 ? -power_of_two(power) : power_of_two(power);
+#pragma unroll
+        for (int o = 0; o < D / 8; o += 4) {
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint4 v = octet_in_order<T>(q[o + k], f);
+                w[4 * k] = v.x, w[4 * k + 1] = v.y, w[4 * k + 2] = v.z, w[4 * k + 3] = v.w;
+            }
+            if (set == 0) store_columns(m.memory + lanes + kQueries + 4 * o, w);
+        }
+        if (set == 0) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        // (of a query that is not finite every score is infinite or NaN, and its softmax NaN)
+        scale = not_finite<T>(largest) ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    if (set == 0 && lane == 0) barrier_arrive(m.asked);
+    // keys before the tree up to pos, from `from` on; and those of the node's way
+    const int64_t node = skipped + slab.pos(row) - slab.first_pos;
+    // (a row of nobody sees as much as others, so that its warp need not look)
+    const int pos = tree.base - 1;
+    int from = 0;
+    const uint64_t way = live ? tree.way(min(node, (int64_t)E2_MAX_DRAFT - 1), from) : 0;
+    if (live && node >= E2_MAX_DRAFT) scale = NAN;
+    float top = -INFINITY, sum = 0;
+    unsigned spoilt = 0;                                     // bit j: this row sees a value of group j that is not finite
+    bool ok = true;
+    // whether a tile's sums are there, and all before it (products run in their order)
+    auto summed = [&](int j) { return warp_wait(m.summed + 8 * (j % kScores), j / kScores & 1, lane); };
+    const uint32_t sums = m.memory + lanes + kSums + set * 128;
+    int stage = set, next_place = set, next_phase = 0;
+    for (int j = set; j < span.n; j += 2) {
+        const int key0 = (span.first + j) * kKeys, place = next_place;
+        const uint32_t at = m.memory + lanes + place * 64;
+        ok = warp_wait(m.scored + 8 * place, next_phase, lane);
+        if (!ok) break;
+        next_place += 2;
+        if (next_place >= kScores) next_place -= kScores, next_phase ^= 1;
+        if (!any) {
+            if (lane == 0) barrier_arrive(m.weighed + 8 * place);
+            continue;
+        }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        uint32_t half[2][32];
+        load_columns(half[0], at);
+        load_columns(half[1], at + 32);
+        const uint32_t present = *reinterpret_cast<const volatile uint32_t *>(m.there[stage]);
+        unsigned long long spoils[GR];
+#pragma unroll
+        for (int i = 0; i < GR; ++i) spoils[i] = *reinterpret_cast<const volatile unsigned long long *>(m.bad[stage][i]);
+        stage = stage + 2 >= kStages ? stage + 2 - kStages : stage + 2;
+        loaded(half[0]);
+        loaded(half[1]);
+        float *s = reinterpret_cast<float *>(half);
+        // keys this row sees, of the tile's
+        unsigned long long seen = ~0ull;
+        const bool whole = __all_sync(~0u, from <= key0 && key0 + kKeys - 1 <= pos) && present == 0x01010101u;
+        if (!whole) {
+            const int lowest = from - key0, highest = pos - key0, shift = tree.base - key0;
+            seen = highest < 0 ? 0ull : highest >= 63 ? ~0ull : (2ull << highest) - 1;
+            if (lowest > 0) seen &= lowest > 63 ? 0ull : ~0ull << lowest;
+            seen |= shift >= 0 ? (shift > 63 ? 0ull : way << shift) : (shift < -63 ? 0ull : way >> -shift);
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                if (!(present >> (8 * w) & 1)) seen &= ~(0xffffull << (16 * w));
+            // (the table's end, which may be before the tree's)
+            if (key0 + kKeys > span.hi) seen &= span.hi > key0 ? (1ull << (span.hi - key0)) - 1 : 0ull;
+#pragma unroll
+            for (int k = 0; k < kKeys; ++k)
+                if (!(seen >> k & 1)) s[k] = -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < GR; ++i)
+            if (spoils[i] & seen) spoilt |= 1u << i;
+        float part[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int k = 4; k < kKeys; ++k) part[k % 4] = fmaxf(part[k % 4], s[k]);
+        float most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        most = most == -INFINITY ? most : most * scale;      // (hidden is -inf whatever the scale, 0 too)
+        const bool renew = most > top + 8.0f || (top == -INFINITY && most > -INFINITY);
+        if (__any_sync(~0u, renew)) {
+            const float is = fmaxf(top, most), back = top == is ? 1.0f : power2(top - is);
+            top = is;
+            sum *= back;
+            if (j > 1) {
+                ok = summed(j - 2);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t v[16];
+                    load_columns(v, sums + c);
+                    loaded(v);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * back);
+                    store_columns(sums + c, v);
+                }
+            }
+        }
+        const float base = top == -INFINITY ? 0.0f : top - 7.0f;
+        auto weigh = [&](auto masked) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[8], rest[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    float a = power2(__fmaf_rn(s[16 * c + 2 * k], scale, -base)), b = power2(__fmaf_rn(s[16 * c + 2 * k + 1], scale, -base));
+                    if (masked.value) {
+                        if (!(seen >> (16 * c + 2 * k) & 1)) a = 0;
+                        if (!(seen >> (16 * c + 2 * k + 1) & 1)) b = 0;
+                    }
+                    sum += a + b;
+                    w[k] = pack_half(a, b);
+                    if (kRest) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[k]));
+                        rest[k] = pack_half(a - f.x, b - f.y);
+                    }
+                }
+                store_columns(at + 8 * c, w);
+                if (kRest) store_columns(at + 32 + 8 * c, rest);
+            }
+        };
+        if (whole) weigh(std::false_type{});
+        else weigh(std::true_type{});
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) barrier_arrive(m.weighed + 8 * place);
+    }
+    if (ok && span.n > 1) ok = summed(span.n - 2);
+    if (ok && span.n > 0) ok = summed(span.n - 1);
+    if (!ok) *m.failed = 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // both sets' sums, brought to the joint maximum
+    float *other = m.states + row * 4;
+    if (set == 1) other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (set == 1) return;
+    const bool lost = !ok || *m.failed;
+    const float nan = __int_as_float(0x7fc00000);
+    const float best = fmaxf(top, other[0]);
+    // (a set without a maximum saw nothing, or NaN)
+    const float f0 = span.n < 1 ? 0.0f : top == -INFINITY ? (sum == 0 ? 0.0f : sum) : power2(top - best);
+    const float f1 = span.n < 2 ? 0.0f : other[0] == -INFINITY ? (other[1] == 0 ? 0.0f : other[1]) : power2(other[0] - best);
+    sum = (f0 == 0 ? 0.0f : sum * f0) + (f1 == 0 ? 0.0f : other[1] * f1);
+    spoilt |= __float_as_uint(other[2]);
+    top = best;
+    const float inverse = sum > 0 ? 1.0f / sum : 0.0f;
+    // rows as whole lines, a lane an octet, by way of the tiles' place (all products have run)
+    constexpr int kOctets = D / 8, kAtOnce = 32 / kOctets, kLoads = 32 / kAtOnce;
+    auto place = [&](int r, int o) {
+        return reinterpret_cast<uint4 *>(m.stages + o / 8 * kTreeRows * 128 + r * 128 + ((o % 8) ^ (r & 7)) * 16);
+    };
+    auto part_place = [&](int r, int o) { return reinterpret_cast<float4 *>(m.stages + r * D * 4 + ((o & ~7) | ((o ^ r) & 7)) * 16); };
+    if (any) {
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+            // elements 0, 4, 1, 5, 2, 6, 3, 7
+            float x[32] = {};
+            auto take = [&](uint32_t from, float f) {
+                uint32_t v[32];
+                load_columns(v, from + c);
+                loaded(v);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    float &to = x[k / 8 * 8 + k % 8 / 2 + k % 2 * 4];
+                    to = f == 0 ? to : __fmaf_rn(__uint_as_float(v[k]), f, to);
+                }
+            };
+            if (span.n > 0) take(sums, f0);
+            if (span.n > 1) take(sums + 128, f1);
+            const bool none = lost || (spoilt >> (c / E2_CACHE_GROUP) & 1);
+            if (p.splits == 1) {
+#pragma unroll
+                for (int o = 0; o < 4; ++o) {
+                    float y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = none ? nan : sum > 0 ? x[8 * o + k] * inverse : sum;
+                    *place(row, c / 8 + o) = pack8<T>(y);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *part_place(row, c / 4 + k) = none ? make_float4(nan, nan, nan, nan)
+                                                       : make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+            }
+            __syncwarp();
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if (p.splits == 1 && any) {
+        const int64_t mine = live ? token * p.out_stride + head * D : -1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = i * kAtOnce + lane / kOctets, o = lane % kOctets;
+            const int64_t at = __shfl_sync(~0u, mine, r);
+            if (at >= 0) reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + at)[o] = *place(32 * quarter + r, o);
+        }
+    } else if (any) {
+        const int64_t mine = live ? ((token * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2) : -1;
+        if (live) p.parts[mine + D] = top, p.parts[mine + D + 1] = lost ? nan : sum;
+#pragma unroll 4
+        for (int r = 0; r < 32; ++r) {
+            const int64_t at = __shfl_sync(~0u, mine, r);
+            // (8 bytes: rows of parts lie D + 2 apart)
+            if (at >= 0 && lane < D / 4) {
+                const float4 v = *part_place(32 * quarter + r, lane);
+                reinterpret_cast<float2 *>(p.parts + at)[2 * lane] = make_float2(v.x, v.y);
+                reinterpret_cast<float2 *>(p.parts + at)[2 * lane + 1] = make_float2(v.z, v.w);
+            }
+        }
+    }
+}
+
+// A tile's runs of keys that lie side by side: one, or two or four where pages are smaller.
+__device__ __forceinline__ int runs_of(const AttendParams &p) { return p.page_shift >= 6 ? 1 : 64 >> p.page_shift; }
+
+// A warp: tiles as they are cached, kRawStages ahead.  Lane 4 w + part copies a part of run w; pages are looked up
+// for 32 runs at a time, a lane each, and 32 ahead.  (A lane's copy takes some hundred cycles to issue.)
+template <int D> __device__ __forceinline__ void copy(const AttendParams &p, const Span &span, const Shared<D> &m, int request, int kv, int lane)
+{
+    using Sh = TreeShared<D>;
+    constexpr int GR = D / E2_CACHE_GROUP;
+    const int runs = runs_of(p), keys = kKeys / runs, page_mask = (1 << p.page_shift) - 1, w = lane / 4, part = lane % 4;
+    const int which = part % 2, scales = part / 2;
+    const int32_t *table = p.table + request * p.table_stride;
+    const uint8_t *array = scales ? reinterpret_cast<const uint8_t *>(p.scales[which]) : p.codes[which];
+    const int of_key = scales ? GR * 4 : D / 2, bytes = keys * of_key;
+    const uint32_t to = smem_addr(m.raw) + (scales ? 8 * Sh::kCodes + which * 4 * Sh::kScales : which * 4 * Sh::kCodes) + w * bytes;
+    auto look_up = [&](int run) {
+        const int64_t key = (int64_t)span.first * kKeys + (int64_t)run * keys;
+        return run < span.n * runs && key < span.hi ? table[key >> p.page_shift] : -1;
+    };
+    bool ok = true;
+    int stage = 0, phase = 1, pages = look_up(lane), next = look_up(32 + lane);
+    for (int j = 0; j < span.n; ++j) {
+        const int run = (j * runs + w) % 32, page = __shfl_sync(~0u, pages, run);
+        if ((j + 1) * runs % 32 == 0) {
+            pages = next;
+            next = look_up((j + 1) * runs + 32 + lane);
+        }
+        ok = warp_wait(m.taken + 8 * stage, phase, lane);
+        if (!ok) break;
+        if (w < runs) {
+            const bool there = page >= 0 && page < p.pages;
+            if (part == 0)
+                for (int i = 0; i < 4 / runs; ++i) m.raw_there[stage][w * (4 / runs) + i] = there;
+            barrier_expect(m.copied + 8 * stage, there ? bytes : 0);
+            if (there) {
+                const int64_t vec = (((int64_t)page * p.kv_heads + kv) << p.page_shift) + (((span.first + j) * kKeys + w * keys) & page_mask);
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + stage * Sh::kRaw),
+                             "l"(array + vec * of_key), "r"(bytes), "r"(m.copied + 8 * stage)
+                             : "memory");
+            }
+        }
+        __syncwarp();
+        if (++stage == kRawStages) stage = 0, phase ^= 1;
+    }
+    // (no copy is on its way any more when the block ends: all have been taken, or have come)
+    for (int i = 0; i < kRawStages && ok; ++i) {
+        ok = warp_wait(m.taken + 8 * stage, phase, lane);
+        if (++stage == kRawStages) stage = 0, phase ^= 1;
+    }
+    if (!ok) {
+        *m.failed = 1;
+        for (int i = 0; i < kRawStages; ++i) barrier_wait(m.copied + 8 * i, phase ^ (i < stage ? 0 : 1));
+    }
+}
+
+// Warp w of four, for even tiles (set 0) or odd ones: 16 of a tile's 64 keys, and values, dequantised.  A lane
+// has 32 elements of one key, or of two keys eight apart; so that eight lanes write 128 bytes of different
+// banks those of a key's second half write their words in another order.
+template <int D> __device__ __forceinline__ void unpack(const Span &span, const Shared<D> &m, int set, int w, int lane)
+{
+    using Sh = TreeShared<D>;
+    constexpr int GR = D / E2_CACHE_GROUP, kParts = D / 32, kItems = kParts / 2;
+    const int key = lane / kParts, part = lane % kParts, half = part / 2;
+    const uint32_t raw0 = smem_addr(m.raw) + w * Sh::kCodes + lane * 16;
+    const uint32_t scales0 = smem_addr(m.raw) + 8 * Sh::kCodes + w * Sh::kScales + (key * GR + half) * 4;
+    const int row = 16 * w + key;
+    const uint32_t to0 = smem_addr(m.stages) + half * kKeys * 128 + row * 128;
+    const uint32_t chunk = (uint32_t)((part % 2 * 4) ^ (row & 7) ^ (2 * half)) * 16;
+    bool ok = true;
+    int stage = set, phase = 1, raw = set, raw_phase = 0;
+    uint4 four[2][kItems], next_four[2][kItems];
+    uint32_t dm[2][kItems], next_dm[2][kItems];
+    bool next_present = false;
+    // a tile as it is cached, into registers; ahead of the one before it
+    auto take = [&] {
+        ok = warp_wait(m.copied + 8 * raw, raw_phase, lane);
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(next_four[which][i].x), "=r"(next_four[which][i].y), "=r"(next_four[which][i].z), "=r"(next_four[which][i].w)
+                             : "r"(raw0 + raw * Sh::kRaw + which * 4 * Sh::kCodes + i * 512)
+                             : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];"
+                             : "=r"(next_dm[which][i])
+                             : "r"(scales0 + raw * Sh::kRaw + which * 4 * Sh::kScales + i * 8 * GR * 4)
+                             : "memory");
+            }
+        next_present = *reinterpret_cast<const volatile uint8_t *>(&m.raw_there[raw][w]);
+    };
+    auto taken = [&] {
+        __syncwarp();
+        if (lane == 0) barrier_arrive(m.taken + 8 * raw);
+        raw += 2;
+        if (raw >= kRawStages) raw -= kRawStages, raw_phase ^= 1;
+    };
+    if (set < span.n) {
+        take();
+        taken();
+    }
+    for (int j = set; j < span.n && ok; j += 2) {
+        const bool present = next_present;
+        bool easy = present;
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                four[which][i] = next_four[which][i], dm[which][i] = next_dm[which][i];
+                const float2 range = __half22float2(*reinterpret_cast<const __half2 *>(&dm[which][i]));
+                easy = easy && __fmaf_rn(15.0f, fabsf(range.x), fabsf(range.y)) <= 65504.0f;
+            }
+        const bool plain = __all_sync(~0u, easy), more = j + 2 < span.n;
+        if (more) take();
+        if (ok) ok = warp_wait(m.empty + 8 * stage, phase, lane);
+        if (!ok) break;
+        // values' groups that are not finite: bit key
+        unsigned bad[GR] = {};
+        if (!plain) {
+            unsigned votes[kItems];
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) votes[i] = __ballot_sync(~0u, present && !finite(dm[1][i]));
+            for (int k = 0; k < 16; ++k)
+#pragma unroll
+                for (int g = 0; g < GR; ++g)
+                    bad[g] |= (votes[kItems == 1 ? 0 : k / 8] >> (k % (32 / kParts) * kParts + 2 * g) & 1) << k;
+        }
+        if (lane == 0) {
+#pragma unroll
+            for (int g = 0; g < GR; ++g) m.bad[stage][g][w] = (uint16_t)bad[g];
+            m.there[stage][w] = present;
+        }
+        const uint32_t to = to0 + stage * 2 * Sh::kTile;
+        auto all = [&](auto limit) {
+#pragma unroll
+            for (int which = 0; which < 2; ++which)
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                    uint32_t both = dm[which][i];
+                    if (limit.value) {
+                        // keys are NaN then, values 0; what is not there is 0
+                        if (!finite(both)) both = which ? 0u : 0x7e000000u;
+                        if (!present) both = 0;
+                    }
+                    const __half2 h = *reinterpret_cast<const __half2 *>(&both);
+                    const __half2 d = __low2half2(h), mn = __high2half2(h);
+                    // (half: the third word first)
+                    const uint4 &f = four[which][i];
+                    const uint32_t words[4] = {half ? f.z : f.x, half ? f.w : f.y, half ? f.x : f.z, half ? f.y : f.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint4 v = unpack_word<limit.value>(words[e], d, mn);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + which * Sh::kTile + (chunk ^ e * 16) + i * 8 * 128),
+                                     "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                                     : "memory");
+                    }
+                }
+        };
+        if (plain) all(std::false_type{});
+        else all(std::true_type{});
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) barrier_arrive(m.full + 8 * stage);
+        stage += 2;
+        if (stage >= kStages) stage -= kStages, phase ^= 1;
+        if (more) taken();
+    }
+    // (nothing is to arrive at a barrier any more: the last use of each stage)
+    for (int j = max(span.n - kStages, 0); j < span.n && ok; ++j) ok = warp_wait(m.empty + 8 * (j % kStages), j / kStages & 1, lane);
+    if (!ok) *m.failed = 1;
+}
+
+template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const AttendParams p)
+{
+    using Sh = TreeShared<D>;
+    extern __shared__ uint8_t dynamic[];
+    __shared__ __align__(8) uint64_t barriers[kBarriers];
+    __shared__ __align__(4) uint8_t there[kStages][4], raw_there[kRawStages][4];
+    __shared__ __align__(8) uint16_t bad[kStages][D / E2_CACHE_GROUP][4];
+    __shared__ uint32_t tensor_memory;
+    __shared__ int failed;
+    __shared__ float states[kTreeRows * 4];
+    __shared__ int8_t parents[E2_MAX_DRAFT];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int request = blockIdx.x / p.kv_heads, kv = blockIdx.x % p.kv_heads;
+    const Rows rows(p, request);
+    const int64_t blocks = (rows.count + kTreeRows - 1) / kTreeRows;
+    if (blocks <= blockIdx.y) return;
+    const Tree tree(p, rows, parents);
+    Tree::load(p, request, parents);
+    Shared<D> m;
+    m.stages = dynamic + (1024 - smem_addr(dynamic) % 1024) % 1024;               // (swizzled tiles start on 1024 bytes)
+    m.raw = m.stages + kStages * 2 * Sh::kTile;
+    m.full = smem_addr(barriers);
+    m.empty = m.full + 8 * kStages;
+    m.scored = m.empty + 8 * kStages;
+    m.weighed = m.scored + 8 * kScores;
+    m.summed = m.weighed + 8 * kScores;
+    m.asked = m.summed + 8 * kScores;
+    m.copied = m.asked + 8;
+    m.taken = m.copied + 8 * kRawStages;
+    m.raw_there = raw_there;
+    m.there = there;
+    m.bad = bad;
+    m.states = states;
+    m.failed = &failed;
+    auto set_barriers = [&] {
+        for (int i = 0; i < kStages; ++i) barrier_init(m.full + 8 * i, 4), barrier_init(m.empty + 8 * i, 1);
+        for (int i = 0; i < kScores; ++i) barrier_init(m.scored + 8 * i, 1), barrier_init(m.weighed + 8 * i, 4), barrier_init(m.summed + 8 * i, 1);
+        barrier_init(m.asked, 4);
+        for (int i = 0; i < kRawStages; ++i) barrier_init(m.copied + 8 * i, 4 * runs_of(p)), barrier_init(m.taken + 8 * i, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    };
+    if (threadIdx.x == 0) {
+        set_barriers();
+        failed = 0;
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tensor_memory)), "r"(kColumns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    m.memory = *reinterpret_cast<volatile uint32_t *>(&tensor_memory);
+
+    // Blocks of rows; one each, where the launch knew how many.  Between two everyone meets and the
+    // barriers start again.
+    auto meet = [&](bool more) {
+        asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+        if (more) {
+            if (threadIdx.x == 0) {
+                for (int i = 0; i < kBarriers; ++i) asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(m.full + 8 * i) : "memory");
+                set_barriers();
+            }
+            asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+        }
+    };
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
+            const Span span(p, rows, tree, block);
+            if (warp == 0) score<D>(m, span.n, lane);
+            else if (warp == 1) sum_up<D, std::is_same<T, __half>::value>(m, span.n, lane);
+            else if (warp == 2) copy<D>(p, span, m, request, kv, lane);
+            meet(block + gridDim.y < blocks);
+        }
+        allow_next();
+        __syncwarp();
+        if (warp == 0)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(m.memory), "r"(kColumns) : "memory");
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+        for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
+            weights<T, D>(p, Span(p, rows, tree, block), m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane);
+            meet(block + gridDim.y < blocks);
+        }
+        allow_next();
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
+            unpack<D>(Span(p, rows, tree, block), m, (warp - 12) / 4, warp % 4, lane);
+            meet(block + gridDim.y < blocks);
+        }
+        allow_next();
+    }
+}
+
+template <class T, int D> int launch_as(const AttendParams &p, int blocks, int pairs, int dev, cudaStream_t s)
+{
+    static std::atomic<uint64_t> ready{0};                   // devices that have the attribute set
+    auto kernel = tree_kernel<T, D>;
+    const int smem = TreeShared<D>::kBytes > 120 * 1024 ? TreeShared<D>::kBytes : 120 * 1024;       // (tensor memory is for one block)
+    if (!(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return cuda_status(e);
+        ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    kernel<<<dim3((unsigned)pairs, (unsigned)blocks, (unsigned)p.splits), kThreads, smem, s>>>(p);
+    return cuda_status(cudaGetLastError());
+}
+
+}  // namespace
+
+int launch_tree(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s)
+{
+    if (head_dim == 64)
+        return half ? launch_as<__half, 64>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 64>(p, blocks, pairs, dev, s);
+    return half ? launch_as<__half, 128>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 128>(p, blocks, pairs, dev, s);
+}
+
+}  // namespace e2ops
