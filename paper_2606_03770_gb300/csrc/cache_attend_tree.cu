@@ -22,9 +22,9 @@ namespace e2ops {
 namespace {
 
 constexpr int kKeys = 64, kStages = 4, kRawStages = 6, kScores = 3;
-// Warps by fours, one on each scheduler: products and copies, weights of even and of odd tiles, keys, values; and the
-// registers they split a block's 640 x 96 into.
-constexpr int kThreads = 640;
+// Warps by fours, one on each scheduler: products and copies, two sets for weights, three to unpack; and the
+// registers they split a block's 768 x 80 into.
+constexpr int kThreads = 768, kUnpackSets = 3;
 constexpr int kBarriers = 2 * kStages + 3 * kScores + 1 + 2 * kRawStages;
 constexpr uint32_t kColumns = 512, kSums = 192, kQueries = 448;       // tensor memory: scores [3][64], sums [2][128], queries
 
@@ -134,6 +134,33 @@ template <int D, bool kRest> __device__ __forceinline__ void sum_up(const Shared
     if (!ok) *m.failed = 1;
 }
 
+// Pairs of 32-bit numbers.
+__device__ __forceinline__ uint64_t two_of(float a, float b)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void halves_of(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t multiply_add(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float largest_of(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // Four warps: weights of even tiles (set 0) or odd ones, a thread a row; then the rows' outputs, by set 0.
 template <class T, int D>
 __device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, const Tree &tree, int64_t skipped,
@@ -141,14 +168,16 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
 {
     constexpr int GR = D / E2_CACHE_GROUP;
     constexpr bool kRest = std::is_same<T, __half>::value;
-    const int row = 32 * quarter + lane;
+    // (up to 64 rows lie there twice: set 0 has the first ones, set 1 the others, so that all schedulers have some)
     const Slab &slab = span.slab;
-    const bool live = slab.live(row), any = slab.live(32 * quarter);
+    const bool narrow = slab.left <= kTreeRows / 2;
+    const int row = 32 * (narrow ? quarter % 2 : quarter) + lane;
+    const bool live = slab.live(row), some = slab.live(row - lane), any = some && (!narrow || quarter / 2 == set);
     const int64_t token = slab.token(row);
     const int head = slab.head(kv, row);
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     float scale = 0;
-    if (any) {
+    if (some) {
         // the queries, to fp16 times a power of two each (and the scale's sign)
         const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + (live ? token * p.q_stride + head * D : 0));
         uint4 q[D / 8];
@@ -234,10 +263,14 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
 #pragma unroll
         for (int i = 0; i < GR; ++i)
             if (spoils[i] & seen) spoilt |= 1u << i;
-        float part[4] = {s[0], s[1], s[2], s[3]};
+        float part[4];
 #pragma unroll
-        for (int k = 4; k < kKeys; ++k) part[k % 4] = fmaxf(part[k % 4], s[k]);
-        float most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        for (int k = 0; k < 4; ++k) part[k] = fmaxf(s[k], s[k + 4]);
+#pragma unroll
+        for (int k = 8; k < kKeys; k += 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[i] = largest_of(part[i], s[k + i], s[k + i + 4]);
+        float most = fmaxf(largest_of(part[0], part[1], part[2]), part[3]);
         most = most == -INFINITY ? most : most * scale;      // (hidden is -inf whatever the scale, 0 too)
         const bool renew = most > top + 8.0f || (top == -INFINITY && most > -INFINITY);
         if (__any_sync(~0u, renew)) {
@@ -260,18 +293,23 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
             }
         }
         const float base = top == -INFINITY ? 0.0f : top - 7.0f;
+        // (two at a time where there is nothing to it but arithmetic)
+        const uint64_t scales = two_of(scale, scale), bases = two_of(-base, -base);
+        uint64_t sums2 = two_of(0, 0);
         auto weigh = [&](auto masked) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t w[8], rest[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    float a = power2(__fmaf_rn(s[16 * c + 2 * k], scale, -base)), b = power2(__fmaf_rn(s[16 * c + 2 * k + 1], scale, -base));
+                    float a, b;
+                    halves_of(multiply_add(two_of(s[16 * c + 2 * k], s[16 * c + 2 * k + 1]), scales, bases), a, b);
+                    a = power2(a), b = power2(b);
                     if (masked.value) {
                         if (!(seen >> (16 * c + 2 * k) & 1)) a = 0;
                         if (!(seen >> (16 * c + 2 * k + 1) & 1)) b = 0;
                     }
-                    sum += a + b;
+                    sums2 = add(sums2, two_of(a, b));
                     w[k] = pack_half(a, b);
                     if (kRest) {
                         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[k]));
@@ -284,6 +322,9 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         };
         if (whole) weigh(std::false_type{});
         else weigh(std::true_type{});
+        float even, odd;
+        halves_of(sums2, even, odd);
+        sum += even + odd;
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
@@ -293,9 +334,26 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     if (ok && span.n > 0) ok = summed(span.n - 1);
     if (!ok) *m.failed = 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // both sets' sums, brought to the joint maximum
+    // both sets' sums, brought to the joint maximum; set 1's by way of the tiles' place where they are other lanes'
+    // (all products have run)
+    auto part_place = [&](int r, int o) { return reinterpret_cast<float4 *>(m.stages + r * D * 4 + ((o & ~7) | ((o ^ r) & 7)) * 16); };
     float *other = m.states + row * 4;
-    if (set == 1) other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
+    if (set == 1 && (any || !narrow)) {
+        other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
+        if (narrow && span.n > 1) {
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                uint32_t v[32];
+                load_columns(v, sums + c);
+                loaded(v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *part_place(kTreeRows / 2 + row, c / 4 + k) = make_float4(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]),
+                                                                              __uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3]));
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        }
+    }
     asm volatile("bar.sync 1, 256;" ::: "memory");
     if (set == 1) return;
     const bool lost = !ok || *m.failed;
@@ -313,24 +371,37 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     auto place = [&](int r, int o) {
         return reinterpret_cast<uint4 *>(m.stages + o / 8 * kTreeRows * 128 + r * 128 + ((o % 8) ^ (r & 7)) * 16);
     };
-    auto part_place = [&](int r, int o) { return reinterpret_cast<float4 *>(m.stages + r * D * 4 + ((o & ~7) | ((o ^ r) & 7)) * 16); };
     if (any) {
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
             // elements 0, 4, 1, 5, 2, 6, 3, 7
             float x[32] = {};
-            auto take = [&](uint32_t from, float f) {
-                uint32_t v[32];
-                load_columns(v, from + c);
-                loaded(v);
+            auto take = [&](const uint32_t (&v)[32], float f) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k) {
                     float &to = x[k / 8 * 8 + k % 8 / 2 + k % 2 * 4];
                     to = f == 0 ? to : __fmaf_rn(__uint_as_float(v[k]), f, to);
                 }
             };
-            if (span.n > 0) take(sums, f0);
-            if (span.n > 1) take(sums + 128, f1);
+            uint32_t v[32];
+            if (span.n > 0) {
+                load_columns(v, sums + c);
+                loaded(v);
+                take(v, f0);
+            }
+            if (span.n > 1 && narrow) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 four = *part_place(kTreeRows / 2 + row, c / 4 + k);
+                    v[4 * k] = __float_as_uint(four.x), v[4 * k + 1] = __float_as_uint(four.y);
+                    v[4 * k + 2] = __float_as_uint(four.z), v[4 * k + 3] = __float_as_uint(four.w);
+                }
+                take(v, f1);
+            } else if (span.n > 1) {
+                load_columns(v, sums + 128 + c);
+                loaded(v);
+                take(v, f1);
+            }
             const bool none = lost || (spoilt >> (c / E2_CACHE_GROUP) & 1);
             if (p.splits == 1) {
 #pragma unroll
@@ -356,7 +427,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         for (int i = 0; i < kLoads; ++i) {
             const int r = i * kAtOnce + lane / kOctets, o = lane % kOctets;
             const int64_t at = __shfl_sync(~0u, mine, r);
-            if (at >= 0) reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + at)[o] = *place(32 * quarter + r, o);
+            if (at >= 0) reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + at)[o] = *place(row - lane + r, o);
         }
     } else if (any) {
         const int64_t mine = live ? ((token * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2) : -1;
@@ -366,7 +437,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
             const int64_t at = __shfl_sync(~0u, mine, r);
             // (8 bytes: rows of parts lie D + 2 apart)
             if (at >= 0 && lane < D / 4) {
-                const float4 v = *part_place(32 * quarter + r, lane);
+                const float4 v = *part_place(row - lane + r, lane);
                 reinterpret_cast<float2 *>(p.parts + at)[2 * lane] = make_float2(v.x, v.y);
                 reinterpret_cast<float2 *>(p.parts + at)[2 * lane + 1] = make_float2(v.z, v.w);
             }
@@ -377,14 +448,15 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
 // A tile's runs of keys that lie side by side: one, or two or four where pages are smaller.
 __device__ __forceinline__ int runs_of(const AttendParams &p) { return p.page_shift >= 6 ? 1 : 64 >> p.page_shift; }
 
-// A warp: tiles as they are cached, kRawStages ahead.  Lane 4 w + part copies a part of run w; pages are looked up
-// for 32 runs at a time, a lane each, and 32 ahead.  (A lane's copy takes some hundred cycles to issue.)
-template <int D> __device__ __forceinline__ void copy(const AttendParams &p, const Span &span, const Shared<D> &m, int request, int kv, int lane)
+// A warp for keys (which 0) and one for values: tiles as they are cached, kRawStages ahead.  Lane 2 w copies the codes
+// of run w, the next one its scales; pages are looked up for 32 runs at a time, a lane each, and 32 ahead.  (A copy
+// takes some 250 cycles to issue: one warp for all four of a tile was what bound a tile.)
+template <int D> __device__ __forceinline__ void copy(const AttendParams &p, const Span &span, const Shared<D> &m, int request, int kv, int which, int lane)
 {
     using Sh = TreeShared<D>;
     constexpr int GR = D / E2_CACHE_GROUP;
-    const int runs = runs_of(p), keys = kKeys / runs, page_mask = (1 << p.page_shift) - 1, w = lane / 4, part = lane % 4;
-    const int which = part % 2, scales = part / 2;
+    const int runs = runs_of(p), keys = kKeys / runs, page_mask = (1 << p.page_shift) - 1, w = lane / 2, scales = lane % 2;
+    const int groups = keys / 16;                            // of 16 keys, in a run
     const int32_t *table = p.table + request * p.table_stride;
     const uint8_t *array = scales ? reinterpret_cast<const uint8_t *>(p.scales[which]) : p.codes[which];
     const int of_key = scales ? GR * 4 : D / 2, bytes = keys * of_key;
@@ -405,8 +477,8 @@ template <int D> __device__ __forceinline__ void copy(const AttendParams &p, con
         if (!ok) break;
         if (w < runs) {
             const bool there = page >= 0 && page < p.pages;
-            if (part == 0)
-                for (int i = 0; i < 4 / runs; ++i) m.raw_there[stage][w * (4 / runs) + i] = there;
+            if (lane % 2 == 0 && which == 0)
+                for (int i = 0; i < groups; ++i) m.raw_there[stage][w * groups + i] = there;
             barrier_expect(m.copied + 8 * stage, there ? bytes : 0);
             if (there) {
                 const int64_t vec = (((int64_t)page * p.kv_heads + kv) << p.page_shift) + (((span.first + j) * kKeys + w * keys) & page_mask);
@@ -429,7 +501,7 @@ template <int D> __device__ __forceinline__ void copy(const AttendParams &p, con
     }
 }
 
-// Warp w of four, for even tiles (set 0) or odd ones: 16 of a tile's 64 keys, and values, dequantised.  A lane
+// Warp w of four of a set, which has every third tile: 16 of its 64 keys, and values, dequantised.  A lane
 // has 32 elements of one key, or of two keys eight apart; so that eight lanes write 128 bytes of different
 // banks those of a key's second half write their words in another order.
 template <int D> __device__ __forceinline__ void unpack(const Span &span, const Shared<D> &m, int set, int w, int lane)
@@ -444,51 +516,38 @@ template <int D> __device__ __forceinline__ void unpack(const Span &span, const 
     const uint32_t chunk = (uint32_t)((part % 2 * 4) ^ (row & 7) ^ (2 * half)) * 16;
     bool ok = true;
     int stage = set, phase = 1, raw = set, raw_phase = 0;
-    uint4 four[2][kItems], next_four[2][kItems];
-    uint32_t dm[2][kItems], next_dm[2][kItems];
-    bool next_present = false;
-    // a tile as it is cached, into registers; ahead of the one before it
-    auto take = [&] {
+    for (int j = set; j < span.n; j += kUnpackSets) {
         ok = warp_wait(m.copied + 8 * raw, raw_phase, lane);
+        if (!ok) break;
+        uint4 four[2][kItems];
+        uint32_t dm[2][kItems];
 #pragma unroll
         for (int which = 0; which < 2; ++which)
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                             : "=r"(next_four[which][i].x), "=r"(next_four[which][i].y), "=r"(next_four[which][i].z), "=r"(next_four[which][i].w)
+                             : "=r"(four[which][i].x), "=r"(four[which][i].y), "=r"(four[which][i].z), "=r"(four[which][i].w)
                              : "r"(raw0 + raw * Sh::kRaw + which * 4 * Sh::kCodes + i * 512)
                              : "memory");
                 asm volatile("ld.shared.u32 %0, [%1];"
-                             : "=r"(next_dm[which][i])
+                             : "=r"(dm[which][i])
                              : "r"(scales0 + raw * Sh::kRaw + which * 4 * Sh::kScales + i * 8 * GR * 4)
                              : "memory");
             }
-        next_present = *reinterpret_cast<const volatile uint8_t *>(&m.raw_there[raw][w]);
-    };
-    auto taken = [&] {
-        __syncwarp();
-        if (lane == 0) barrier_arrive(m.taken + 8 * raw);
-        raw += 2;
-        if (raw >= kRawStages) raw -= kRawStages, raw_phase ^= 1;
-    };
-    if (set < span.n) {
-        take();
-        taken();
-    }
-    for (int j = set; j < span.n && ok; j += 2) {
-        const bool present = next_present;
-        bool easy = present;
+        const bool present = *reinterpret_cast<const volatile uint8_t *>(&m.raw_there[raw][w]);
+        // (15 |d| + |m| is within fp16's range where |d| is at most 2,048 and |m| below 32,768)
+        uint32_t magnitudes = 0;
 #pragma unroll
         for (int which = 0; which < 2; ++which)
 #pragma unroll
-            for (int i = 0; i < kItems; ++i) {
-                four[which][i] = next_four[which][i], dm[which][i] = next_dm[which][i];
-                const float2 range = __half22float2(*reinterpret_cast<const __half2 *>(&dm[which][i]));
-                easy = easy && __fmaf_rn(15.0f, fabsf(range.x), fabsf(range.y)) <= 65504.0f;
-            }
-        const bool plain = __all_sync(~0u, easy), more = j + 2 < span.n;
-        if (more) take();
-        if (ok) ok = warp_wait(m.empty + 8 * stage, phase, lane);
+            for (int i = 0; i < kItems; ++i) magnitudes = __vmaxu2(magnitudes, dm[which][i] & 0x7fff7fffu);
+        const bool easy = present && (magnitudes & 0xffffu) <= 0x6800u && magnitudes >> 16 < 0x7800u;
+        const bool plain = __all_sync(~0u, easy);
+        __syncwarp();
+        if (lane == 0) barrier_arrive(m.taken + 8 * raw);
+        raw += kUnpackSets;
+        if (raw >= kRawStages) raw -= kRawStages, raw_phase ^= 1;
+        ok = warp_wait(m.empty + 8 * stage, phase, lane);
         if (!ok) break;
         // values' groups that are not finite: bit key
         unsigned bad[GR] = {};
@@ -537,9 +596,8 @@ template <int D> __device__ __forceinline__ void unpack(const Span &span, const 
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) barrier_arrive(m.full + 8 * stage);
-        stage += 2;
+        stage += kUnpackSets;
         if (stage >= kStages) stage -= kStages, phase ^= 1;
-        if (more) taken();
     }
     // (nothing is to arrive at a barrier any more: the last use of each stage)
     for (int j = max(span.n - kStages, 0); j < span.n && ok; ++j) ok = warp_wait(m.empty + 8 * (j % kStages), j / kStages & 1, lane);
@@ -614,12 +672,12 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
         }
     };
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
             const Span span(p, rows, tree, block);
             if (warp == 0) score<D>(m, span.n, lane);
             else if (warp == 1) sum_up<D, std::is_same<T, __half>::value>(m, span.n, lane);
-            else if (warp == 2) copy<D>(p, span, m, request, kv, lane);
+            else copy<D>(p, span, m, request, kv, warp - 2, lane);
             meet(block + gridDim.y < blocks);
         }
         allow_next();
@@ -627,14 +685,14 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
         if (warp == 0)
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(m.memory), "r"(kColumns) : "memory");
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
             weights<T, D>(p, Span(p, rows, tree, block), m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane);
             meet(block + gridDim.y < blocks);
         }
         allow_next();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
             unpack<D>(Span(p, rows, tree, block), m, (warp - 12) / 4, warp % 4, lane);
             meet(block + gridDim.y < blocks);
