@@ -557,8 +557,8 @@ constexpr int kClusterUnits = 8;
 
 // Trees' rows are by 128 from so many on.
 constexpr int kTree = 17;
-// A block of trees' rows takes the time of so many tiles more, for its start, its end and its part.
-constexpr int kTreeExtra = 12;
+// A block of trees' rows takes the time of so many tiles more, for its start and its end; so many the second kernel.
+constexpr int kTreeExtra = 12, kTreeJoin = 10;
 
 struct Plan {
     int nt, slabs, splits;      // nt 0: a prompt, or a tree by kTreeRows
@@ -587,12 +587,14 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms, bool tree)
     while (f.cluster && splits > 2 && pairs * splits * 8 > places * 7) --splits;
     f.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     if (tree && f.nt == 0) {
-        // as many parts as take the least time: rounds of blocks times the tiles of one and what it costs besides
+        // as many parts as take the least time: rounds of blocks times the tiles of one and what it costs besides,
+        // and the second kernel; two or four that run at once are joined in clusters
         const int64_t tiles = (keys + 63) / 64;
         int64_t least_time = INT64_MAX;
         for (int64_t s = 1; s <= kMostSplits && (s == 1 || s * 4 <= tiles); ++s) {
-            const int64_t time = (pairs * s + sms - 1) / sms * ((tiles + s - 1) / s + kTreeExtra);
-            if (time < least_time) least_time = time, f.splits = (int)s;
+            const bool cluster = (s == 2 || s == kTreeCluster) && pairs * s * 16 <= (int64_t)sms * 15;
+            const int64_t time = (pairs * s + sms - 1) / sms * ((tiles + s - 1) / s + kTreeExtra) + (s > 1 && !cluster ? kTreeJoin : 0);
+            if (time < least_time) least_time = time, f.splits = (int)s, f.cluster = cluster;
         }
     }
     return f;

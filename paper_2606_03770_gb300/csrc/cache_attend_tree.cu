@@ -21,7 +21,7 @@
 namespace e2ops {
 namespace {
 
-constexpr int kKeys = 64, kStages = 4, kRawStages = 6, kScores = 3;
+constexpr int kKeys = 64, kStages = 5, kRawStages = 6, kScores = 3;
 // Warps by fours, one on each scheduler: products and copies, two sets for weights, three to unpack; and the
 // registers they split a block's 768 x 80 into.
 constexpr int kThreads = 768, kUnpackSets = 3;
@@ -164,7 +164,7 @@ __device__ __forceinline__ float largest_of(float a, float b, float c)
 // Four warps: weights of even tiles (set 0) or odd ones, a thread a row; then the rows' outputs, by set 0.
 template <class T, int D>
 __device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, const Tree &tree, int64_t skipped,
-                                        int kv, int set, int quarter, int lane)
+                                        int kv, int set, int quarter, int lane, bool join)
 {
     constexpr int GR = D / E2_CACHE_GROUP;
     constexpr bool kRest = std::is_same<T, __half>::value;
@@ -176,8 +176,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     const int64_t token = slab.token(row);
     const int head = slab.head(kv, row);
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
-    float scale = 0;
-    if (some) {
+    if (set == 0 && some) {
         // the queries, to fp16 times a power of two each (and the scale's sign)
         const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + (live ? token * p.q_stride + head * D : 0));
         uint4 q[D / 8];
@@ -197,11 +196,11 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
                 const uint4 v = octet_in_order<T>(q[o + k], f);
                 w[4 * k] = v.x, w[4 * k + 1] = v.y, w[4 * k + 2] = v.z, w[4 * k + 3] = v.w;
             }
-            if (set == 0) store_columns(m.memory + lanes + kQueries + 4 * o, w);
+            store_columns(m.memory + lanes + kQueries + 4 * o, w);
         }
-        if (set == 0) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         // (of a query that is not finite every score is infinite or NaN, and its softmax NaN)
-        scale = not_finite<T>(largest) ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
+        m.states[row * 4 + 3] = not_finite<T>(largest) ? NAN : fabsf(p.scale) * 1.4426950408889634f * power_of_two(-power);
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncwarp();
@@ -212,7 +211,8 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     const int pos = tree.base - 1;
     int from = 0;
     const uint64_t way = live ? tree.way(min(node, (int64_t)E2_MAX_DRAFT - 1), from) : 0;
-    if (live && node >= E2_MAX_DRAFT) scale = NAN;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const float scale = !some ? 0.0f : live && node >= E2_MAX_DRAFT ? NAN : m.states[row * 4 + 3];
     float top = -INFINITY, sum = 0;
     unsigned spoilt = 0;                                     // bit j: this row sees a value of group j that is not finite
     bool ok = true;
@@ -429,6 +429,8 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
             const int64_t at = __shfl_sync(~0u, mine, r);
             if (at >= 0) reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + at)[o] = *place(row - lane + r, o);
         }
+    } else if (join) {
+        other[0] = top, other[1] = lost ? nan : sum;
     } else if (any) {
         const int64_t mine = live ? ((token * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2) : -1;
         if (live) p.parts[mine + D] = top, p.parts[mine + D + 1] = lost ? nan : sum;
@@ -441,6 +443,44 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
                 reinterpret_cast<float2 *>(p.parts + at)[2 * lane] = make_float2(v.x, v.y);
                 reinterpret_cast<float2 *>(p.parts + at)[2 * lane + 1] = make_float2(v.z, v.w);
             }
+        }
+    }
+}
+
+// Eight warps: the parts of a cluster's blocks, in their order.  Block `rank` has every splits-th row.
+template <class T, int D>
+__device__ __forceinline__ void join_parts(const AttendParams &p, const Slab &slab, const Shared<D> &m, int kv, int warp, int lane)
+{
+    const int rank = blockIdx.z;
+    for (int r = warp * p.splits + rank; r < kTreeRows && slab.live(r); r += 8 * p.splits) {
+        const uint32_t state = smem_addr(m.states + r * 4), part = smem_addr(m.stages + r * D * 4 + ((lane & ~7) | ((lane ^ r) & 7)) * 16);
+        float tops[kTreeCluster], weights[kTreeCluster], best = -INFINITY;
+        float4 x[kTreeCluster];
+#pragma unroll
+        for (int k = 0; k < kTreeCluster; ++k) {
+            const int peer = min(k, p.splits - 1);
+            tops[k] = peer_load(peer_addr(state, peer)), weights[k] = peer_load(peer_addr(state, peer) + 4);
+            if (lane < D / 4) x[k] = peer_load4(peer_addr(part, peer));
+            best = fmaxf(best, tops[k]);
+        }
+        float total = 0, y[4] = {};
+#pragma unroll
+        for (int k = 0; k < kTreeCluster; ++k) {
+            // (a part without a maximum saw nothing, or NaN)
+            const float f = tops[k] == -INFINITY ? (weights[k] == 0 ? 0.0f : weights[k]) : power2(tops[k] - best);
+            if (k < p.splits && f != 0) {
+                total = __fmaf_rn(weights[k], f, total);
+                const float v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = __fmaf_rn(v[i], f, y[i]);
+            }
+        }
+        if (lane < D / 4) {
+            T out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[i] = from_float<T>(total > 0 ? y[i] / total : total);
+            *reinterpret_cast<uint2 *>(static_cast<T *>(p.out) + slab.token(r) * p.out_stride + slab.head(kv, r) * D + 4 * lane) =
+                *reinterpret_cast<const uint2 *>(out);
         }
     }
 }
@@ -671,6 +711,8 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
             asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
         }
     };
+    // Parts of a cluster's blocks are joined between two barriers of it.
+    const bool join = p.splits > 1 && !p.parts;
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
@@ -678,6 +720,8 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
             if (warp == 0) score<D>(m, span.n, lane);
             else if (warp == 1) sum_up<D, std::is_same<T, __half>::value>(m, span.n, lane);
             else copy<D>(p, span, m, request, kv, warp - 2, lane);
+            __syncwarp();
+            if (join) cluster_barrier(), cluster_barrier();
             meet(block + gridDim.y < blocks);
         }
         allow_next();
@@ -687,7 +731,13 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     } else if (warp < 12) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
-            weights<T, D>(p, Span(p, rows, tree, block), m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane);
+            const Span span(p, rows, tree, block);
+            weights<T, D>(p, span, m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane, join);
+            if (join) {
+                cluster_barrier();
+                join_parts<T, D>(p, span.slab, m, kv, warp - 4, lane);
+                cluster_barrier();
+            }
             meet(block + gridDim.y < blocks);
         }
         allow_next();
@@ -695,6 +745,7 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
             unpack<D>(Span(p, rows, tree, block), m, (warp - 12) / 4, warp % 4, lane);
+            if (join) cluster_barrier(), cluster_barrier();
             meet(block + gridDim.y < blocks);
         }
         allow_next();
@@ -711,8 +762,17 @@ template <class T, int D> int launch_as(const AttendParams &p, int blocks, int p
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    kernel<<<dim3((unsigned)pairs, (unsigned)blocks, (unsigned)p.splits), kThreads, smem, s>>>(p);
-    return cuda_status(cudaGetLastError());
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = at.val.clusterDim.y = 1, at.val.clusterDim.z = (unsigned)p.splits;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)pairs, (unsigned)blocks, (unsigned)p.splits);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cfg.attrs = &at;
+    cfg.numAttrs = p.splits > 1 && !p.parts;
+    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
 }
 
 }  // namespace
