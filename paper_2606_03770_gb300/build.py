@@ -2,14 +2,17 @@
 
 Each translation unit is compiled in parallel with ``-fmad=false`` (every
 float64 multiply and add rounds once, as the objective's bit-exactness needs)
-and linked into ``_build/libe2ga.so`` with the static CUDA runtime.
+and linked into ``_build/libe2ga.so`` with the static CUDA runtime.  ``_build/e2binding.so``
+is the Python module of the calls whose time is the host's (csrc/binding.cpp).
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -17,6 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libe2ga.so")
+BINDING = os.path.join(OUT_DIR, "e2binding.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-fmad=false", "-Xcompiler", "-fPIC", "-I", INCLUDE,
          "-I", CSRC]
@@ -34,12 +38,27 @@ def sources():
 
 
 def _stale(objs):
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(BINDING):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     deps = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
-    deps += [os.path.join(INCLUDE, f) for f in ("e2ga.h", "e2ops.h")]
+    deps += [os.path.join(INCLUDE, f) for f in ("e2ga.h", "e2ops.h")] + [os.path.join(CSRC, "binding.cpp")]
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _compile_binding():
+    """The module's object, against the torch that is installed; returns what the link takes."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
+    obj = os.path.join(OUT_DIR, "binding.o")
+    includes = [INCLUDE, os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", *(f"-I{i}" for i in includes), "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for binding.cpp:\n{r.stderr}")
+    libs = [f"-L{os.path.join(torch, 'lib')}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    return ["-shared", obj, f"-L{OUT_DIR}", "-l:libe2ga.so", *libs, "-Wl,-rpath,$ORIGIN"]
 
 
 def build(force: bool = False, verbose: bool = False, extra=()) -> str:
@@ -60,8 +79,10 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
             raise RuntimeError(f"nvcc failed for {src}:\n{r.stderr}")
         return r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=len(srcs)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(srcs) + 1) as ex:
+        binding = ex.submit(_compile_binding)
         logs = list(ex.map(compile_one, zip(srcs, objs)))
+        binding = binding.result()
     if verbose:
         for l in logs:
             print(l)
@@ -70,6 +91,11 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB)
+    tmp = BINDING + ".tmp"
+    r = subprocess.run(["g++", "-o", tmp, *binding], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed:\n{r.stderr}")
+    os.replace(tmp, BINDING)
     return LIB
 
 

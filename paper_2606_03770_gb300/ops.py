@@ -24,6 +24,9 @@ there gradients: a tensor that requires one is refused while gradients are recor
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
+import os
 
 import torch
 
@@ -111,6 +114,25 @@ def load():
             f.restype, f.argtypes = res, args
         _lib = lib
     return _lib
+
+
+_binding = None
+
+
+def binding():
+    """The module of the calls whose time is the host's: None from one of its functions says that the
+    call is to go the whole way here."""
+    global _binding
+    if _binding is None:
+        load()
+        path = os.path.join(os.path.dirname(e2ga.LIB_PATH), "e2binding.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built")
+        spec = importlib.util.spec_from_loader("e2binding", importlib.machinery.ExtensionFileLoader("e2binding", path))
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _binding = module
+    return _binding
 
 
 def _need(cond, text):
@@ -345,6 +367,7 @@ class Cache(_Handle):
         self.struct = e2_cache(pages, page, heads, 2 * half, k_codes.data_ptr(), k_scales.data_ptr(),
                                v_codes.data_ptr(), v_scales.data_ptr())
         self.ref = C.byref(self.struct)
+        self.fast = (C.addressof(self.struct), self.device.index, self.requires_grad)
         self._made = frozenset(vars(self)) | {"_made"}
 
     @classmethod
@@ -465,6 +488,10 @@ def cache_attend_tree(cache, q, parents, table, lens, starts, max_new=None, max_
     ``parents`` int32 [tokens], a node's parent by its number in its request, -1 for
     none.  A node sees the tokens before the tree, itself and the nodes on its way up.
     Up to E2_MAX_DRAFT nodes a request (more are refused where ``max_new`` says so)."""
+    done = (_binding or binding()).attend_tree(cache.fast, q, parents, table, lens, starts, max_new, max_len, scale, window, out,
+                                               workspace)
+    if done is not None:
+        return done
     _like(parents, "parents", torch.int32, (q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0,), cache.device)
     return _attend("e2_cache_attend_tree", (parents,), cache, q, table, lens, starts, max_new, max_len, scale, window, out,
                    workspace)
@@ -479,6 +506,9 @@ def verify_drafts(logits, ids, parents, starts, uniforms, draft=None, temperatur
     logit).  ``kept`` int32 [batch] counts the accepted nodes, node 0 among them; ``nodes`` and
     ``answer`` int32 [batch, max_new] have them and the token after each, -1 behind.  ``max_new``,
     at most E2_MAX_DRAFT, is read from the device (a synchronisation) unless given."""
+    done = (_binding or binding()).verify(logits, ids, parents, starts, uniforms, draft, temperature, max_new)
+    if done is not None:
+        return done
     tokens, vocab = _tensor(logits, "logits", _FLOAT, (None, None))
     dev = logits.device
     if draft is not None:
@@ -500,7 +530,7 @@ def verify_drafts(logits, ids, parents, starts, uniforms, draft=None, temperatur
     _need(0 <= max_new <= E2_MAX_DRAFT, f"max_new must be in 0..{E2_MAX_DRAFT}")
     i32 = dict(dtype=torch.int32, device=dev)
     kept = torch.empty(batch, **i32)
-    nodes, answer = torch.empty((2, batch, max_new), **i32).unbind()
+    nodes, answer = torch.empty((batch, max_new), **i32), torch.empty((batch, max_new), **i32)
     a = e2_verify_args(tokens, vocab, DTYPES[logits.dtype], batch, max_new, logits.data_ptr(), _stride(logits),
                        draft.data_ptr() if draft is not None else None, _stride(draft) if draft is not None else 0,
                        ids.data_ptr(), parents.data_ptr(), starts.data_ptr(), uniforms.data_ptr(),
@@ -529,6 +559,7 @@ class CacheLayers(_Handle):
             raise ValueError(load().e2_ops_error().decode())
         self.arrays = torch.tensor(list(arrays), dtype=torch.int64, device=self.device)
         torch.cuda.current_stream(self.device).synchronize()         # (whatever stream they are used on)
+        self.fast = first.fast[:2] + (self.requires_grad, n, self.arrays.data_ptr())
         self._made = frozenset(vars(self)) | {"_made"}
 
     def __len__(self):
@@ -541,6 +572,9 @@ def cache_keep(layers, table, lens, starts, nodes, kept, lens_out=None):
     k of its tree, for k < ``kept[r]``.  Returns the cached tokens of each request after
     that, int32 [batch] (``lens_out``, allocated unless given; not ``lens``)."""
     _need(isinstance(layers, CacheLayers), "layers must be a CacheLayers")
+    done = (_binding or binding()).keep(layers.fast, table, lens, starts, nodes, kept, lens_out)
+    if done is not None:
+        return done
     dev = layers.device
     batch, cols = _tensor(table, "table", (torch.int32,), (None, None), dev)
     for x, name, n in ((lens, "lens", batch), (starts, "starts", batch + 1), (kept, "kept", batch)):

@@ -22,6 +22,15 @@ def test_calls_refuse_without_arguments(lib):  # noqa: F811
     assert b"" != lib.e2_ops_error()
 
 
+def test_the_binding_leaves_what_is_not_plain(lib):  # noqa: F811
+    """The compiled binding loads without a GPU, and goes by for anything but tensors on one."""
+    from paper_2606_03770_gb300 import ops
+    b, z, i32 = ops.binding(), torch.zeros, dict(dtype=torch.int32)
+    assert b.verify(z(2, 8), z(2, **i32), z(2, **i32), z(2, **i32), z(2), None, None, 2) is None
+    for f in (b.verify, b.attend_tree, b.keep):
+        assert f() is None and f(None) is None
+
+
 def test_host_tensors_are_refused():
     from paper_2606_03770_gb300 import ops
     z, i32 = torch.zeros, dict(dtype=torch.int32)

@@ -490,6 +490,33 @@ def test_refusals():
         tree(cache=grad)
 
 
+class NoBinding:
+    """The compiled binding, going by."""
+    attend_tree = verify = keep = staticmethod(lambda *a: None)
+
+
+@pytest.mark.parametrize("G", [1, 8])
+def test_the_binding_in_python_is_the_same(G, monkeypatch):
+    from paper_2606_03770_gb300 import ops
+    s, run = step(3, 9, 70, 2, G, 500, 4)
+    want = run()
+    heat = torch.tensor([0.0, 0.5, 1.0], device="cuda")
+    x = s["x"]
+    more = lambda: (ops.verify_drafts(x[0], x[1], x[2], s["starts"], x[4], draft=x[5], temperature=heat, max_new=20)
+                    + (ops.cache_attend_tree(s["cache"], s["q"], s["parents"], s["table"], s["lens"], s["starts"], max_new=9, max_len=79,
+                                             scale=0.3, window=50, out=torch.empty_like(s["q"])),
+                       ops.cache_attend_tree(s["cache"], s["q"], s["parents"], s["table"], s["lens"], s["starts"], max_new=9, max_len=79,
+                                             workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))))
+    want += more()
+    assert ops.binding().verify(x[0], x[1], x[2], s["starts"], x[4], x[5], None, 9) is not None
+    assert ops.binding().attend_tree(s["cache"].fast, s["q"], s["parents"], s["table"], s["lens"], s["starts"], 9, 79, None, 0, None, None) is not None
+    assert ops.binding().keep(s["layers"].fast, s["table"], s["lens"], s["starts"], want[3][:, :0].new_zeros(3, 2), s["lens"].new_zeros(3), None) is not None
+    monkeypatch.setattr(ops, "_binding", NoBinding)
+    got = run() + more()
+    for a, b in zip(got, want):
+        assert a.dtype is b.dtype and torch.equal(a, b)
+
+
 def test_empty_calls():
     from paper_2606_03770_gb300 import ops
     cache, q, table, lens, starts = setup([40], [3], 2, 2, 64, 16)
