@@ -214,16 +214,20 @@ struct KeepParams {
 template <int D> __global__ void __launch_bounds__(kThreads) keep_kernel(const KeepParams p)
 {
     // of a token: keys' pieces and scales, values' pieces and scales
-    constexpr int kPieces = D / 32, kItems = 2 * (kPieces + 1), kMost = (E2_MAX_DRAFT * kItems + 31) / 32;
+    constexpr int kPieces = D / 32, kItems = 2 * (kPieces + 1), kMost = (E2_MAX_DRAFT * kItems + 31) / 32, kFew = 4;
     const int lane = threadIdx.x % 32;
     const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32;
     if (unit >= (int64_t)p.layers * p.batch * p.kv_heads) return;
     const int head = (int)(unit % p.kv_heads), request = (int)(unit / p.kv_heads % p.batch), layer = (int)(unit / p.kv_heads / p.batch);
+    const int32_t *nodes = p.nodes + request * p.nodes_stride, *table = p.table + request * p.table_stride;
+    const unsigned long long *arrays = p.arrays + 4 * layer;
+    // (what hangs on nothing is asked for at once: the first nodes before it is known how many count)
+    int first_nodes[kFew];
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) first_nodes[i] = (32 * i + lane) / kItems < p.cols ? nodes[(32 * i + lane) / kItems] : -1;
     const int64_t count = (int64_t)p.starts[request + 1] - p.starts[request], base = p.lens[request] - count;
     const int kept = (int)max(min(min((int64_t)p.kept[request], count), (int64_t)p.cols), (int64_t)0);
     if (layer == 0 && head == 0 && lane == 0) p.lens_out[request] = (int32_t)max(base + kept, (int64_t)0);
-    const int32_t *nodes = p.nodes + request * p.nodes_stride, *table = p.table + request * p.table_stride;
-    const unsigned long long *arrays = p.arrays + 4 * layer;
     // the head vector of a token, -1 where it is not in the cache
     auto vector_at = [&](int64_t token) {
         if (token < 0 || token >> p.page_shift >= p.table_cols) return (int64_t)-1;
@@ -232,40 +236,54 @@ template <int D> __global__ void __launch_bounds__(kThreads) keep_kernel(const K
         return (((int64_t)page * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
     };
     const int items = kept * kItems;
-    uint4 what[kMost];
-    uint8_t *where[kMost];
-#pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        where[i] = nullptr;
-        const int item = 32 * i + lane;
-        if (item < items) {
-            const int k = item / kItems, rest = item % kItems, which = rest / (kPieces + 1), piece = rest % (kPieces + 1);
-            const int node = nodes[k];
-            if (node != k && node >= 0 && node < count) {
-                const int64_t from = vector_at(base + node), to = vector_at(base + k);
-                if (from >= 0 && to >= 0) {
-                    const bool scales = piece == kPieces;
-                    uint8_t *array = reinterpret_cast<uint8_t *>(arrays[2 * which + scales]);
-                    constexpr int kScales = D / E2_CACHE_GROUP * 4;
-                    if (scales) {
-                        where[i] = array + to * kScales;
-                        if (kScales == 8) *reinterpret_cast<uint2 *>(&what[i]) = *reinterpret_cast<const uint2 *>(array + from * kScales);
-                        else what[i].x = *reinterpret_cast<const uint32_t *>(array + from * kScales);
-                    } else {
-                        where[i] = array + to * (D / 2) + piece * 16;
-                        what[i] = *reinterpret_cast<const uint4 *>(array + from * (D / 2) + piece * 16);
-                    }
-                }
+    constexpr int kScales = D / E2_CACHE_GROUP * 4;
+    auto read = [&](int item, int node, uint4 &what, uint8_t *&where) {
+        where = nullptr;
+        const int k = item / kItems, rest = item % kItems, which = rest / (kPieces + 1), piece = rest % (kPieces + 1);
+        if (item >= items || node == k || node < 0 || node >= count) return;
+        const int64_t from = vector_at(base + node), to = vector_at(base + k);
+        if (from < 0 || to < 0) return;
+        const bool scales = piece == kPieces;
+        uint8_t *array = reinterpret_cast<uint8_t *>(arrays[2 * which + scales]);
+        if (scales) {
+            where = array + to * kScales;
+            if (kScales == 8) {
+                const uint2 two = *reinterpret_cast<const uint2 *>(array + from * kScales);
+                what = uint4{two.x, two.y, 0, 0};
+            } else {
+                what = uint4{*reinterpret_cast<const uint32_t *>(array + from * kScales), 0, 0, 0};
             }
+        } else {
+            where = array + to * (D / 2) + piece * 16;
+            what = *reinterpret_cast<const uint4 *>(array + from * (D / 2) + piece * 16);
         }
-    }
-    __syncwarp();                                          // (all have been read)
+    };
+    auto write = [&](int item, const uint4 &what, uint8_t *where) {
+        if (!where) return;
+        if (item % (kPieces + 1) != kPieces) *reinterpret_cast<uint4 *>(where) = what;
+        else if (kScales == 8) *reinterpret_cast<uint2 *>(where) = make_uint2(what.x, what.y);
+        else *reinterpret_cast<uint32_t *>(where) = what.x;
+    };
+    if (items <= 32 * kFew) {
+        uint4 what[kFew];
+        uint8_t *where[kFew];
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        if (!where[i]) continue;
-        if ((32 * i + lane) % (kPieces + 1) != kPieces) *reinterpret_cast<uint4 *>(where[i]) = what[i];
-        else if (D == 128) *reinterpret_cast<uint2 *>(where[i]) = make_uint2(what[i].x, what[i].y);
-        else *reinterpret_cast<uint32_t *>(where[i]) = what[i].x;
+        for (int i = 0; i < kFew; ++i) read(32 * i + lane, first_nodes[i], what[i], where[i]);
+        __syncwarp();                                      // (all have been read)
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) write(32 * i + lane, what[i], where[i]);
+    } else {
+        // (long ways: in local memory, which costs the others no registers)
+        uint4 what[kMost];
+        uint8_t *where[kMost];
+#pragma unroll 1
+        for (int i = 0; 32 * i < items; ++i) {
+            const int item = 32 * i + lane;
+            read(item, item < items ? nodes[item / kItems] : -1, what[i], where[i]);
+        }
+        __syncwarp();
+#pragma unroll 1
+        for (int i = 0; 32 * i < items; ++i) write(32 * i + lane, what[i], where[i]);
     }
 }
 
