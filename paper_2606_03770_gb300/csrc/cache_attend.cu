@@ -68,9 +68,9 @@ template <class T, int D, int NT, bool TREE> __global__ void __launch_bounds__(3
     const int32_t *table = p.table + request * p.table_stride;
     uint8_t *ring = smem + warp * kFewStages * St::kBytes;
     const uint32_t ring_at = smem_addr(ring);
-    __shared__ int8_t parents[TREE ? E2_MAX_DRAFT : 1];
-    const Tree tree(p, rows, parents);
-    if (TREE) Tree::load(p, request, parents);              // (a barrier follows before they are read)
+    __shared__ uint64_t ways[TREE ? E2_MAX_DRAFT : 1];
+    const Tree tree(p, rows, ways);
+    if (TREE && warp == 0) Tree::load(p, request, ways);    // (a barrier follows before they are read)
 
     for (int64_t row0 = (int64_t)blockIdx.z * C; row0 < rows.count; row0 += (int64_t)gridDim.z * C) {
         // the keys that some row sees, in tiles; this split's
@@ -181,7 +181,8 @@ template <class T, int D, int NT, bool TREE> __global__ void __launch_bounds__(3
                 seen_lo[n][e] = seen && p.window > 0 ? (int)max(slab.pos(at) - p.window + 1, (int64_t)0) : 0;
                 if (TREE) {
                     const int64_t node = rows.skipped + slab.pos(at) - slab.first_pos;
-                    seen_hi[n][e] = seen ? tree.base - 1 : -1;
+                    // (a column of nobody sees as much as others: a tile need not be looked at for its sake)
+                    seen_hi[n][e] = tree.base - 1;
                     way[n][e] = seen ? tree.way(min(node, (int64_t)E2_MAX_DRAFT - 1), seen_lo[n][e]) : 0;
                 }
             }
@@ -191,7 +192,7 @@ template <class T, int D, int NT, bool TREE> __global__ void __launch_bounds__(3
         // (a node is no deeper than its number)
         const int full_lo = p.window > 0 ? (int)max(slab.pos(last) - p.window + 1, (int64_t)0) : 0;
         const int full_hi = (int)max(TREE ? tree.base - 1 : slab.pos(0), (int64_t)-1);
-        const bool all_live = C <= slab.left;
+        const bool all_live = TREE || C <= slab.left;
 
         float o[U][2][NT][4] = {};                       // sums for dimensions 32 u + 4 g + {0, 1}, {2, 3}
         float low[NT][GR][2] = {}, sum[NT][2] = {};      // minima's sums, weights' sums: this lane's keys
@@ -555,8 +556,11 @@ constexpr int kPrompt = 65;
 // for a whole wave).
 constexpr int kClusterUnits = 8;
 
-// Trees' rows are by 128 from so many on.
-constexpr int kTree = 17;
+// Trees' rows are by 128 from so many on; from nine on where the blocks run at once and all requests' keys, times the
+// KV heads, are so few.  Measured, us (128 elements, bf16; by eight or sixteen / by 128): 24 rows of 8 requests x 8 KV
+// heads x 2,304 keys 40 / 22, 16 rows 29 / 21, 8 rows 19 / 21; 16 rows of 150 keys 19 / 11, 9,000 keys 54 / 52, 65,000
+// keys 222 / 283; 16 rows of 32 x 8 x 517 keys 25 / 29; 8 rows of one request x 150 keys 11 / 11.
+constexpr int kTree = 17, kTreeKeys = 600000;
 // A block of trees' rows takes the time of so many tiles more, for its start and its end; so many the second kernel.
 constexpr int kTreeExtra = 12, kTreeJoin = 10;
 
@@ -572,6 +576,8 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms, bool tree)
     Plan f;
     const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
     f.nt = rows >= (tree ? kTree : kPrompt) ? 0 : rows <= 8 ? 1 : 2;
+    const int64_t heads = (int64_t)a->batch * c->kv_heads;
+    if (tree && f.nt == 2 && heads <= sms && heads * a->max_len <= kTreeKeys) f.nt = 0;
     const int at_once = f.nt ? 8 * f.nt : tree ? kTreeRows : kPromptRows;
     const int64_t slabs = (rows + at_once - 1) / at_once;
     f.slabs = (int)(slabs < 65535 ? slabs : 65535);

@@ -59,28 +59,53 @@ struct Slab {
 // base + a is node a's (a tree far below token 0 has no keys, wherever it is).
 struct Tree {
     int base, window;
-    const int8_t *parents;                   // [E2_MAX_DRAFT], in shared memory
-    __device__ Tree(const AttendParams &p, const Rows &r, const int8_t *parents)
-        : base((int)max(r.first_pos - r.skipped, (int64_t)-E2_MAX_DRAFT)), window(p.window), parents(parents)
+    const uint64_t *ways;                    // [E2_MAX_DRAFT], in shared memory; bit a: node a is on the way up, itself among it
+    __device__ Tree(const AttendParams &p, const Rows &r, const uint64_t *ways)
+        : base((int)max(r.first_pos - r.skipped, (int64_t)-E2_MAX_DRAFT)), window(p.window), ways(ways)
     {
     }
-    // All threads of a block; a barrier has to follow.
-    static __device__ void load(const AttendParams &p, int request, int8_t *parents)
+    // One warp; a barrier has to follow.  Each node takes in what the node at the end of its way so far has, whose way
+    // goes on from there: as many rounds as the logarithm of the longest way.
+    static __device__ void load(const AttendParams &p, int request, uint64_t *ways)
     {
-        for (int i = threadIdx.x; i < E2_MAX_DRAFT; i += blockDim.x) {
+        const int lane = threadIdx.x % 32;
+        int next[2];
+        uint64_t way[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 32 * h;
             const int64_t t = (int64_t)p.starts[request] + i;
             const int parent = t >= 0 && t < p.tokens ? p.parents[t] : -1;
-            parents[i] = parent >= 0 && parent < i ? (int8_t)parent : (int8_t)-1;
+            next[h] = parent >= 0 && parent < i ? parent : -1;
+            way[h] = 1ull << i;
         }
+        while (__any_sync(~0u, next[0] >= 0 || next[1] >= 0)) {
+            uint64_t more[2];
+            int then[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int from = next[h] & 31;
+                const uint64_t w0 = __shfl_sync(~0u, way[0], from), w1 = __shfl_sync(~0u, way[1], from);
+                const int n0 = __shfl_sync(~0u, next[0], from), n1 = __shfl_sync(~0u, next[1], from);
+                more[h] = next[h] < 0 ? 0 : next[h] < 32 ? w0 : w1;
+                then[h] = next[h] < 0 ? -1 : next[h] < 32 ? n0 : n1;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) way[h] |= more[h], next[h] = then[h];
+        }
+        ways[lane] = way[0], ways[lane + 32] = way[1];
     }
-    // Bit a: whether the node sees node a's key; and the first key of those before `base`.
+    // Bit a: whether the node sees node a's key; and the first key of those before `base`.  (A way's nodes stand
+    // in the order of their numbers: the farthest are the lowest bits.)
     __device__ uint64_t way(int64_t node, int &lowest) const
     {
-        uint64_t seen = 0;
-        int depth = 0;
-        for (int a = (int)node; a >= 0; a = parents[a], ++depth)
-            if (window == 0 || depth < window) seen |= 1ull << a;
-        lowest = window > 0 ? max(base + (depth - window), 0) : 0;
+        uint64_t seen = ways[node];
+        int far = __popcll(seen);
+        lowest = 0;
+        if (window > 0) {
+            lowest = max(base + (far - window), 0);
+            for (; far > window; --far) seen &= seen - 1;
+        }
         return seen;
     }
 };

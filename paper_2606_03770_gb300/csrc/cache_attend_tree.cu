@@ -654,14 +654,14 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     __shared__ uint32_t tensor_memory;
     __shared__ int failed;
     __shared__ float states[kTreeRows * 4];
-    __shared__ int8_t parents[E2_MAX_DRAFT];
+    __shared__ uint64_t ways[E2_MAX_DRAFT];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int request = blockIdx.x / p.kv_heads, kv = blockIdx.x % p.kv_heads;
     const Rows rows(p, request);
     const int64_t blocks = (rows.count + kTreeRows - 1) / kTreeRows;
     if (blocks <= blockIdx.y) return;
-    const Tree tree(p, rows, parents);
-    Tree::load(p, request, parents);
+    const Tree tree(p, rows, ways);
+    if (warp == 1) Tree::load(p, request, ways);
     Shared<D> m;
     m.stages = dynamic + (1024 - smem_addr(dynamic) % 1024) % 1024;               // (swizzled tiles start on 1024 bytes)
     m.raw = m.stages + kStages * 2 * Sh::kTile;

@@ -81,7 +81,7 @@ def test_ragged_batches_and_empty_requests():
 def test_chains_are_what_cache_attend_computes():
     """Of a chain the tree's mask is the causal one: where the same kernel computes both, bit for bit."""
     from paper_2606_03770_gb300 import ops
-    for G, new in ((1, 5), (8, 2)):
+    for G, new in ((1, 5), (4, 2)):                              # (up to eight rows)
         cache, q, table, lens, starts = setup([517, 90], [new, new], 4, G, 128, 64, HALF, seed=8)
         parents = i32([i - 1 for _ in range(2) for i in range(new)])
         kw = dict(max_new=new, max_len=517)
