@@ -13,6 +13,13 @@ the 32-device workload).
 
     python -m paper_2606_03770_gb300.block_profile --config c2          # the table
     python -m paper_2606_03770_gb300.block_profile --config c2 --plan   # and a search
+    python -m paper_2606_03770_gb300.block_profile --config c2 --draft 2.1.1   # and steps with drafted tokens
+
+``--draft`` also times a decode step with a tree of drafted tokens for each request, given by its
+branching level by level (2.1.1: two children of a request's last token, one of each of these, one of
+each of those): the block on all nodes, then the head, the verification and the move of the accepted
+way's keys and values.  How many drafted tokens a model accepts is not known here, so what is shown
+is how many tokens a block's step has to give to be worth its time.
 """
 from __future__ import annotations
 
@@ -53,6 +60,19 @@ class Batch:
     slots: torch.Tensor      # int64 [tokens]
     max_new: int
     max_len: int
+    parents: torch.Tensor | None = None      # int32 [tokens] where the new tokens are trees
+
+    @classmethod
+    def of_trees(cls, table, before, parents, page):
+        """The same tree of drafted tokens, by its nodes' parents (-1: none), for each request."""
+        batch = cls.of(table, before, len(parents), page)
+        depth = []
+        for p in parents:
+            depth.append(depth[p] + 1 if p >= 0 else 0)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        batch.positions = (before + torch.tensor(depth, **i32)).repeat(table.shape[0])
+        batch.parents = torch.tensor(list(parents), **i32).repeat(table.shape[0])
+        return batch
 
     @classmethod
     def of(cls, table, before, new, page):
@@ -91,8 +111,12 @@ class Block:
         qkv = ops.quant_matmul(norm(x, self.norms[0]), self.w_qkv).view(T, -1, self.D)
         q, k, v = qkv[:, :self.heads], qkv[:, self.heads:self.heads + kv], qkv[:, self.heads + kv:]
         ops.cache_append(cache, k, v, batch.slots, batch.positions, self.cos, self.sin, q=q, q_out=q)
-        a = ops.cache_attend(cache, q, batch.table, batch.lens, batch.starts, max_new=batch.max_new,
-                             max_len=batch.max_len, window=window)
+        if batch.parents is None:
+            a = ops.cache_attend(cache, q, batch.table, batch.lens, batch.starts, max_new=batch.max_new,
+                                 max_len=batch.max_len, window=window)
+        else:
+            a = ops.cache_attend_tree(cache, q, batch.parents, batch.table, batch.lens, batch.starts,
+                                      max_new=batch.max_new, max_len=batch.max_len, window=window)
         x = ops.quant_matmul(a.view(T, -1), self.w_out, residual=x)
         h = ops.quant_matmul(norm(x, self.norms[1]), self.w_gate_up, gated=True)
         return ops.quant_matmul(h, self.w_down, residual=x)
@@ -102,6 +126,15 @@ class Block:
         `tokens`, entropy, alternatives."""
         logits = ops.quant_matmul(norm(x, self.norms[2]), self.w_head)
         return ops.token_logprobs(logits, tokens, top=top)
+
+    def accept(self, x, ids, batch, uniforms, draft, layers, temperature=None):
+        """The output layer on all nodes' rows of a batch of trees: which drafted tokens are accepted
+        (``ops.verify_drafts``); their keys and values, in the caches of ``layers``, go to where they
+        belong.  Returns (kept, nodes, answer, cached tokens of each request)."""
+        logits = ops.quant_matmul(norm(x, self.norms[2]), self.w_head)
+        kept, nodes, answer = ops.verify_drafts(logits, ids, batch.parents, batch.starts, uniforms, draft=draft,
+                                                temperature=temperature, max_new=batch.max_new)
+        return kept, nodes, answer, ops.cache_keep(layers, batch.table, batch.lens, batch.starts, nodes, kept)
 
 
 def time_graph(f, repeats=20):
@@ -159,6 +192,44 @@ def measure(model, NP, ND, b_max, page=64, window=0, repeats=20):
     return out
 
 
+def branching(text):
+    """The parents of a tree's nodes, numbered level by level, from its branching ("2.1.1")."""
+    parents, level = [-1], [0]
+    for b in text.split("."):
+        if not b.isdigit() or int(b) < 1:
+            raise ValueError(f"{text!r}: a tree is positive numbers with dots between them")
+        if len(parents) + len(level) * int(b) > ops.E2_MAX_DRAFT:
+            raise ValueError(f"{text!r} has more than {ops.E2_MAX_DRAFT} nodes")
+        below = range(len(parents), len(parents) + len(level) * int(b))
+        parents += [p for p in level for _ in range(int(b))]
+        level = below
+    return parents
+
+
+def measure_drafts(model, NP, ND, b_max, parents, page=64, window=0, repeats=20):
+    """Run and time decode steps with a tree of drafted tokens for each request, at the context of
+    `measure`'s: ``block`` and ``head`` (with verification and move) of b requests at index b - 1."""
+    n = len(parents)
+    block = Block(model["d"], model["ffn"], model["kv_heads"], model["vocab"], NP + ND + n)
+    pages = -(-(NP + ND - 1 + n) // page)
+    cache = ops.Cache.empty(b_max * pages, page, block.kv_heads, block.D)
+    layers = ops.CacheLayers([cache])
+    table = torch.randperm(b_max * pages, device="cuda").int().view(b_max, pages)
+    for r in range(b_max):
+        block.forward(torch.randn(NP + ND - 1, block.d, device="cuda").to(block.dtype), cache,
+                      Batch.of(table[r:r + 1], 0, NP + ND - 1, page), window)
+    out = Measured([], [], NP, ND)
+    for b in range(1, b_max + 1):
+        step = Batch.of_trees(table[:b], NP + ND - 1, parents, page)
+        x = torch.randn(b * n, block.d, device="cuda").to(block.dtype)
+        draft = torch.randn(b * n, model["vocab"], device="cuda").to(block.dtype)
+        above = torch.arange(b, device="cuda").repeat_interleave(n) * n + step.parents.clamp(min=0)
+        ids, uniforms = draft[above].argmax(1).int(), torch.rand(b * n, device="cuda")
+        out.block.append(time_graph(lambda: block.forward(x, cache, step, window), repeats))
+        out.head.append(time_graph(lambda: block.accept(x, ids, step, uniforms, draft, layers), repeats))
+    return out
+
+
 def planned(prob, model, window=0, group=64):
     """`prob` with the work of the block that `measure` runs in place of its own: 4-bit weights
     and a 4-bit cache, each with its scales, and at most `window` keys a token (0: all).  The
@@ -199,6 +270,8 @@ def main(argv=None):
     ap.add_argument("--config", default="c2", choices=[c for c, w in W.CONFIGS.items() if w["model"]["wbits"] == 4],
                     help="a workload with 4-bit weights")
     ap.add_argument("--window", type=int, default=0, help="sliding window of the block (0: full attention)")
+    ap.add_argument("--draft", type=branching, metavar="TREE",
+                    help="also a decode step with a tree of drafted tokens for each request, by its branching (2.1.1)")
     ap.add_argument("--plan", action="store_true", help="search with this GPU in the place of the fleet's first device")
     ap.add_argument("--generations", type=int, default=10)
     a = ap.parse_args(argv)
@@ -214,6 +287,11 @@ def main(argv=None):
         if times[v] > 1.01 * m.block[v]:
             print(f"no rate and bandwidth give both measured times: the planner takes {times[v] * 1e6:.1f} us for "
                   f"{'the prefill' if v == 0 else f'decode {v}'}")
+    if a.draft:
+        d = measure_drafts(W.CONFIGS[a.config]["model"], prob.NP, prob.ND, prob.b_max, a.draft, window=a.window)
+        print(f"trees of {len(a.draft)} nodes: {'block us':>10s}{'head us':>10s}  tokens a block's step has to give")
+        for b, (t, h) in enumerate(zip(d.block, d.head), 1):
+            print(f"{f'decode {b}':16s}{t * 1e6:10.1f}{h * 1e6:10.1f}{t / m.block[b]:10.2f}")
     print(f"as a device of the planner: {rate / 1e12:.1f} TFLOP/s, {bw / 1e9:.0f} GB/s")
     if a.plan:
         from .e2ga import Engine

@@ -91,6 +91,33 @@ def test_chains_are_what_cache_attend_computes():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("G", [1, 2, 16])
+@pytest.mark.parametrize("new,before", [(5, 3), (16, 100), (64, 0), (64, 190), (37, 27)])
+@pytest.mark.parametrize("window", [0, 1, 7, 60])
+def test_each_node_sees_its_way_and_no_more(G, new, before, window):
+    """Queries of 0 weigh all keys alike, and node a's value is 1 at element a: an output tells which nodes it is of."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([before + new], [new], 2, G, 64, 16, seed=14)
+    q.zero_()
+    cache.k_scales.zero_()
+    cache.v_codes.zero_()
+    cache.v_scales.zero_()
+    cache.v_scales[..., 0] = 1.0 / 15
+    for a in range(new):
+        at = before + a
+        cache.v_codes[int(table[0, at // 16]), :, at % 16, a // 2] = 15 << (4 * (a % 2))
+    par = random_tree(new, new + before, 0.6)
+    out = ops.cache_attend_tree(cache, q, i32(par), table, lens, starts, max_new=new, max_len=before + new, window=window).float()
+    for i in range(new):
+        up = DR.way(par, 0, i, new)
+        nodes = [a for d, a in enumerate(up) if not window or d < window]
+        context = before if not window else min(before, max(0, window - len(up)))
+        want = torch.zeros(64, device="cuda")
+        want[nodes] = 1.0 / (len(nodes) + context)
+        # (1/15 in fp16 times 15, and the output's rounding)
+        assert torch.allclose(out[i], want.expand_as(out[i]), rtol=2.0 ** -10 + 2.0 ** -8, atol=0), i
+
+
 @pytest.mark.parametrize("G", [1, 4, 16])
 def test_parents_out_of_range_count_as_none(G):
     new = 12
