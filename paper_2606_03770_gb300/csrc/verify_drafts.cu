@@ -38,6 +38,8 @@ struct __align__(16) Part {
     float p_top, q_top;
     int first;                                   // of the largest
     int bad;
+    Two p_more, q_more;                          // sums where p is above the draft's, and p's near the border
+    float border;
 };
 
 struct Shared {
@@ -92,6 +94,8 @@ template <class T> struct Walk {
     Two heat;                                    // 1 / T
     float x_top, y_top;                          // one of the largest of each
     Two run, block;                              // sums of this warp's run, and of the lane's block
+    Two run_q, block_q;                          // split: of the draft's, beside p's, where p is above it
+    float border;
 
     __device__ Walk(const VerifyParams &p, Shared &m, uint8_t *dynamic) : p(p), m(m), turn(0)
     {
@@ -107,7 +111,7 @@ template <class T> struct Walk {
 
     // What the lanes have, over the warp, the block and the cluster: join(k) takes in what lanes k apart
     // have, for powers of two below the lanes that there are.
-    template <class F> __device__ __forceinline__ void exchange(Part &mine, F join)
+    template <bool MORE = false, class F> __device__ __forceinline__ void exchange(Part &mine, F join)
     {
         auto over = [&](int lanes) {
 #pragma unroll 1
@@ -115,20 +119,27 @@ template <class T> struct Walk {
         };
         over(32);
         run = mine.p;
+        if (MORE) run = mine.p_more, run_q = mine.q_more;
         if (lane == 0) m.parts[warp] = mine;
         __syncthreads();
         mine = m.parts[lane % kWarps];
         over(kWarps);
         block = mine.p;
+        if (MORE) block = mine.p_more, block_q = mine.q_more;
         if (p.split > 1) {
             if (warp == 0 && lane < p.split) {
                 const uint32_t to = peer_addr(smem_addr(&m.blocks[turn][rank]), lane);
                 peer_store4(to, make_float4(mine.p.h, mine.p.l, mine.q.h, mine.q.l));
                 peer_store4(to + 16, make_float4(mine.p_top, mine.q_top, __int_as_float(mine.first), __int_as_float(mine.bad)));
+                if (MORE) {
+                    peer_store4(to + 32, make_float4(mine.p_more.h, mine.p_more.l, mine.q_more.h, mine.q_more.l));
+                    peer_store4(to + 48, make_float4(mine.border, 0, 0, 0));
+                }
             }
             cluster_barrier();
             mine = m.blocks[turn][lane % p.split];
             block = mine.p;
+            if (MORE) block = mine.p_more, block_q = mine.q_more;
             over(p.split);
             turn ^= 1;
         } else {
@@ -380,6 +391,56 @@ template <class T> struct Walk {
         return mine.p;
     }
 
+    // x's sum and y's, and by the way what (x - share y)+ sums to, for a share that is known to some 2^-20 only (`near`):
+    // x and y are summed where x is above near y, which is where it is above share y but for elements within the
+    // difference of the two, of which no more than that difference counts; `border` sums x within 2^-20 of it.
+    __device__ __forceinline__ Two split(const Weigher of_x, const Weigher of_y, float near, Two &q)
+    {
+        LongSum a[2], b[2];
+        float edge = 0;
+        pairs<true>([&](const float (&u)[2], const float (&v)[2]) {
+            Two w[2], d[2];
+            of_x.of(u, m.table, w);
+            of_y.of(v, m.table, d);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float over = __fmaf_rn(-near, d[j].h, w[j].h);
+                const bool above = over > 0;
+                if (fabsf(over) < 0x1p-20f * w[j].h) edge += w[j].h;
+                LongSum x{above ? a[1].s : a[0].s, above ? a[1].c : a[0].c}, y{above ? b[1].s : b[0].s, above ? b[1].c : b[0].c};
+                x.add(w[j]);
+                y.add(d[j]);
+                a[1] = above ? x : a[1], b[1] = above ? y : b[1];
+                a[0] = above ? a[0] : x, b[0] = above ? b[0] : y;
+            }
+        });
+        Part mine{a[0].value(), b[0].value(), 0, 0, 0, 0, a[1].value(), b[1].value(), edge};
+        exchange<true>(mine, [&](int k) {
+            mine.p = mine.p + shuffle_xor(mine.p, k);
+            mine.q = mine.q + shuffle_xor(mine.q, k);
+            mine.p_more = mine.p_more + shuffle_xor(mine.p_more, k);
+            mine.q_more = mine.q_more + shuffle_xor(mine.q_more, k);
+            mine.border += __shfl_xor_sync(~0u, mine.border, k);
+        });
+        border = mine.border;
+        q = mine.q + mine.q_more;
+        return mine.p + mine.p_more;
+    }
+    // After it: run and block of (x - share y)+, and its sum; false where the border's part of it may be above 2^-37.
+    __device__ __forceinline__ bool take_split(const Two &share, float near, Two &sum)
+    {
+        auto of = [&](const Two &x, const Two &y) {
+            const Two d = x - share * y;
+            return d.h > 0 ? d : Two{0, 0};
+        };
+        sum = warp_sum(lane < p.split ? of(block, block_q) : Two{0, 0});
+        // (2^-22: what the comparisons were rounded by)
+        const float off = fabsf(__fdiv_rn((share - Two{near, 0}).h, near)) + 0x1p-22f;
+        if (!(off < 0x1p-20f && off * border <= 0x1p-37f * sum.h)) return false;
+        run = of(run, run_q), block = of(block, block_q);
+        return true;
+    }
+
     // The first v whose share of the sums in order passes u, in one warp of one block, which it
     // returns true to.  gone(i): tokens that P has lost.
     template <class F> __device__ __forceinline__ bool find(float u, bool less, const Weigher of_x, const Weigher of_y, F gone, int &answer)
@@ -473,15 +534,17 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
             for (uint64_t set = children; set && accepted < 0; set &= set - 1)
                 if (m.ids[first_of(set)] == first) accepted = first_of(set);
             if (accepted < 0) token = first;
-        } else {
+        }
+        float x_sum = 0, y_sum = 0;
+        bool clear = false;
+        if (!greedy) {
             // In 32 bits first: exponents are off by 2^-18 at most (of 64, and 2^-18 of that in f), sums by less,
             // so what is clear by one part in 2^14 is clear.
             constexpr float kClear = 0x1p-14f;
-            float x_sum, y_sum;
             const int child0 = children ? first_of(children) : 0;
             const float first_x = children && inside(m.ids[child0]) ? to_float(walk.x[m.ids[child0]]) : -INFINITY;
             const float first_y = both && inside(m.ids[child0]) ? to_float(walk.y[m.ids[child0]]) : -INFINITY;
-            const bool clear = both ? walk.template estimate<true>(x_sum, y_sum) : walk.template estimate<false>(x_sum, y_sum);
+            clear = both ? walk.template estimate<true>(x_sum, y_sum) : walk.template estimate<false>(x_sum, y_sum);
             if (!clear) {
                 if (!walk.tops(both, first)) break;
             } else if (children) {
@@ -511,7 +574,18 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
             const Weigher of_x(walk.x_top, walk.heat), of_y(both ? walk.y_top : walk.x_top, walk.heat);
             const Two none{0, 0};
             Two q = none, A = none, B{1, 0};
-            const Two all = both ? walk.template sums<true, false>(of_x, of_y, q) : walk.template sums<false, false>(of_x, of_x, q);
+            // (in 32 bits, of what the weights sum to here)
+            float near = 0;
+            if (both && clear) {
+                const float f = walk.heat.h * 1.44269504f;
+                const float wx = of_x.of(walk.x_top, m.table).h * x_sum * power2(__fmaf_rn(walk.y_top, f, -(walk.y_top * f)));
+                const float wy = of_y.of(walk.y_top, m.table).h * y_sum * power2(__fmaf_rn(walk.x_top, f, -(walk.x_top * f)));
+                near = __fdiv_rn(wx, wy);
+            }
+            const Two all = near > 0 ? walk.split(of_x, of_y, near, q)
+                            : both   ? walk.template sums<true, false>(of_x, of_y, q)
+                                     : walk.template sums<false, false>(of_x, of_x, q);
+            const bool parted = near > 0;
             Two left = all;                               // (without the draft's rows)
             uint64_t lost = 0;                            // rejected children whose tokens P has lost
             bool less = false;
@@ -541,13 +615,19 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                     }
                     const Two run = walk.run, block = walk.block;
                     Two unused;
-                    const Two more = A + B;
-                    walk.set_share(more * all / q);
-                    const Two sum = walk.template sums<false, true>(of_x, of_y, unused) / all;
+                    const Two more = A + B, share = more * all / q;
+                    Two sum;
+                    const bool known = near > 0 && walk.take_split(share, near, sum);
+                    walk.set_share(share);
+                    if (!known) sum = walk.template sums<false, true>(of_x, of_y, unused);
+                    near = 0;                             // (the first child's only)
+                    sum = sum / all;
                     if (sum.h > kNothing * B.h) {
                         A = more, B = sum, less = true;
                     } else {
-                        walk.run = run, walk.block = block;
+                        // (p's own, which a split has not left)
+                        if (parted && !less) walk.template sums<false, false>(of_x, of_x, unused);
+                        else walk.run = run, walk.block = block;
                         walk.set_share(A * all / q);
                     }
                 } else if (in && !gone(v)) {
