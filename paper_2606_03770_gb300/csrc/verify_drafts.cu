@@ -15,12 +15,13 @@ namespace {
 // likewise of the draft's row, after k rejections
 //   P = (p - A q)+ / B,  A_0 = 0, B_0 = 1, A_{k+1} = A_k + B_k, B_{k+1} = sum (p - A_{k+1} q)+,
 // as (P - q)+ is (p - A q - B q)+ / B.  Without the draft's rows a rejected token leaves P.
-// The token after the last is found in the warps' sums, then in the sums of a sixteenth of a
-// warp's run, then element by element.  The numbers that decide have some 45 bits.
+// The token after the last is found in the blocks' sums, the warps', those of an eighth of a
+// warp's run, of a lane's share of it, and then element by element.  The numbers that decide have some 45 bits.
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMostCluster = 16;
-constexpr int kUnit = 256;                       // elements of a run: eight a lane
 constexpr int kRing = 6144;                      // bytes of a warp's copies on their way
+constexpr int kGroup = 4;                        // nodes that are looked at together
+static_assert(kGroup * kWarps == 32, "a lane for each node and warp");
 constexpr float kNothing = 0x1p-36f;             // a sum below it, of what it is a part of, is rounding's
 
 struct VerifyParams {
@@ -46,6 +47,8 @@ struct Shared {
     float2 table[PowerTable::kSize], shared_table[PowerTable::kSize];
     Part parts[kWarps], blocks[2][kMostCluster];  // (a block may be one pass ahead of another)
     Two sub[kWarps];
+    float2 tops[kGroup], sums[kWarps][kGroup], block_sums[2][kMostCluster][kGroup];           // (x, y)
+    int group[kGroup];                           // the nodes
     int32_t ids[E2_MAX_DRAFT], parents[E2_MAX_DRAFT];
     float uniforms[E2_MAX_DRAFT];
 };
@@ -83,13 +86,17 @@ template <class T> __device__ __forceinline__ float half_of(uint32_t w, int high
 }
 
 template <class T> struct Walk {
-    static constexpr int kWords = 8 * sizeof(T) / 4, kStages = kRing / (2 * kUnit * (int)sizeof(T));
+    // A unit of a run: 16 bytes a lane.
+    static constexpr int kEach = 16 / sizeof(T), kUnit = 32 * kEach, kStages = kRing / 1024;
     const VerifyParams &p;
     Shared &m;
     int lane, warp, rank, turn;
     int first, end;                              // this warp's run
     uint4 *ring;
+    int ring_base;                               // the stage of the run's first unit
+    bool ring_fresh;                             // nothing has come into the ring since the group's rows
     const T *x, *y;                              // the node's rows
+    int64_t start;                               // the request's first row
     bool wide;                                   // 16-byte loads
     Two heat;                                    // 1 / T
     float x_top, y_top;                          // one of the largest of each
@@ -147,121 +154,208 @@ template <class T> struct Walk {
         }
     }
 
-    // Eight elements of each lane's.
-    struct Eight {
-        uint32_t w[kWords];
+    // A lane's elements of a unit.
+    struct Lot {
+        uint32_t w[4];
     };
-    static __device__ __forceinline__ float element(const Eight &e, int j)
+    static __device__ __forceinline__ float element(const Lot &e, int j)
     {
         return sizeof(T) == 4 ? __uint_as_float(e.w[j]) : half_of<T>(e.w[j / 2], j % 2);
     }
-    __device__ __forceinline__ Eight from_row(const T *row, int at) const
+    __device__ __forceinline__ Lot from_row(const T *row, int at) const
     {
-        Eight e;
+        Lot e;
         if (wide) {
-#pragma unroll
-            for (int k = 0; k < kWords / 4; ++k) {
-                const uint4 four = reinterpret_cast<const uint4 *>(row + at + 8 * lane)[k];
-                e.w[4 * k] = four.x, e.w[4 * k + 1] = four.y, e.w[4 * k + 2] = four.z, e.w[4 * k + 3] = four.w;
-            }
+            const uint4 four = *reinterpret_cast<const uint4 *>(row + at + kEach * lane);
+            e.w[0] = four.x, e.w[1] = four.y, e.w[2] = four.z, e.w[3] = four.w;
         } else {
             constexpr int kIn = 4 / sizeof(T);
 #pragma unroll
-            for (int k = 0; k < 8 / kIn; ++k) {
+            for (int k = 0; k < 4; ++k) {
                 e.w[k] = bits_of(row + at + 32 * kIn * k + lane);
                 if (kIn == 2) e.w[k] |= bits_of(row + at + 32 * kIn * k + 32 + lane) << 16;
             }
         }
         return e;
     }
-    // A lane writes and reads its own 16 bytes of the ring only: [stage][row][eights' parts][32].
-    __device__ __forceinline__ uint4 *ring_at(int unit, int row) const
+    // A lane writes and reads its own 16 bytes of the ring only: [stage][row][32].
+    __device__ __forceinline__ uint4 *ring_at(int stage, int row) const { return ring + (stage * 2 + row) * 32 + lane; }
+    __device__ __forceinline__ void to_ring(const T *from, int stage, int which) const
     {
-        return ring + ((unit % kStages * 2 + row) * (kWords / 4)) * 32 + lane;
+        copy_async16(smem_addr(ring_at(stage, which)), from, true);
     }
-    __device__ __forceinline__ void to_ring(const T *row, int unit, int which) const
+    __device__ __forceinline__ Lot from_ring(int stage, int which) const
     {
-        const uint32_t to = smem_addr(ring_at(unit, which));
-#pragma unroll
-        for (int k = 0; k < kWords / 4; ++k)
-            copy_async16(to + 512 * k, reinterpret_cast<const uint4 *>(row + first + unit * kUnit + 8 * lane) + k, true);
-    }
-    __device__ __forceinline__ Eight from_ring(int unit, int which) const
-    {
-        Eight e;
-#pragma unroll
-        for (int k = 0; k < kWords / 4; ++k) {
-            const uint4 four = ring_at(unit, which)[32 * k];
-            e.w[4 * k] = four.x, e.w[4 * k + 1] = four.y, e.w[4 * k + 2] = four.z, e.w[4 * k + 3] = four.w;
-        }
-        return e;
+        const uint4 four = *ring_at(stage, which);
+        return Lot{{four.x, four.y, four.z, four.w}};
     }
 
-    // This warp's run of a new node, f(j, an element of x, of y): through the ring, which keeps it where it fits.
-    template <bool BOTH> __device__ __forceinline__ void start_stream() const
+    __device__ __forceinline__ const T *row_of(const void *rows, int64_t stride, int node) const
+    {
+        return static_cast<const T *>(rows) + (start + node) * stride;
+    }
+    __device__ __forceinline__ void at_node(int node)
+    {
+        x = row_of(p.logits, p.logits_stride, node);
+        y = p.draft ? row_of(p.draft, p.draft_stride, node) : x;
+    }
+    // This warp's run of the rows of the group's node `place` into the ring, where it holds them; which may be so still.
+    __device__ __forceinline__ void fill_ring(bool both, int place, int count)
     {
         const int units = (end - first) / kUnit;
-        if (!wide) return;
-#pragma unroll
-        for (int u = 0; u < kStages; ++u) {
-            if (u < units) {
-                to_ring(x, u, 0);
-                if (BOTH) to_ring(y, u, 1);
+        ring_base = 0;
+        if (!wide || units > kStages) return;
+        if (ring_fresh && (count - place) * units <= kStages) {
+            ring_base = place * units % kStages;
+            return;
+        }
+        ring_fresh = false;
+        for (int u = 0; u < units; ++u) {
+            to_ring(x + first + u * kUnit + kEach * lane, u, 0);
+            if (both) to_ring(y + first + u * kUnit + kEach * lane, u, 1);
+        }
+        copy_commit();
+        copy_wait<0>();
+    }
+
+    // In 32 bits, of the group's nodes g < count: sums of 2^((x - top) log2 e / T), and of y's (bit g of `both`).  Lane g kWarps
+    // has node g's.  The tops are the largest of a few of the row.  Rows come through the ring one after the other.
+    __device__ __forceinline__ void estimate(int count, unsigned both, float &x_sum, float &y_sum)
+    {
+        const int units = (end - first) / kUnit;
+        // (where the next copies come from: a node's next unit)
+        int next_node = 0, next_unit = 0;
+        const T *next_x = nullptr, *next_y = nullptr;
+        ring_fresh = true;
+        auto issue = [&](int stage) {
+            if (next_node < count && units > 0) {
+                if (next_unit == 0) {
+                    next_x = row_of(p.logits, p.logits_stride, m.group[next_node]) + first + kEach * lane;
+                    next_y = both >> next_node & 1 ? row_of(p.draft, p.draft_stride, m.group[next_node]) + first + kEach * lane : nullptr;
+                }
+                to_ring(next_x, stage, 0);
+                next_x += kUnit;
+                if (next_y) {
+                    to_ring(next_y, stage, 1);
+                    next_y += kUnit;
+                }
+                if (++next_unit == units) next_unit = 0, ++next_node;
             }
             copy_commit();
-        }
-    }
-    template <bool BOTH, class F> __device__ __forceinline__ void stream(F f) const
-    {
-        const int units = (end - first) / kUnit;
-#pragma unroll 1
-        for (int u = 0; u < units; ++u) {
-            Eight a, b;
-            if (wide) {
-                copy_wait<kStages - 1>();
-                a = from_ring(u, 0);
-                if (BOTH) b = from_ring(u, 1);
-            } else {
-                a = from_row(x, first + u * kUnit);
-                if (BOTH) b = from_row(y, first + u * kUnit);
-            }
+        };
+        if (wide) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f(j, element(a, j), BOTH ? element(b, j) : 0.0f);
-            if (wide) {
-                if (u + kStages < units) {
-                    to_ring(x, u + kStages, 0);
-                    if (BOTH) to_ring(y, u + kStages, 1);
-                }
-                copy_commit();
-            }
+            for (int k = 0; k < kStages; ++k) issue(k);
         }
+        // the tops: a warp for each node's row
+        static_assert(2 * kGroup == kWarps, "a warp for each row");
+        {
+            const int g = warp / 2;
+            float a = -INFINITY;
+            if (g < count && (warp % 2 == 0 || (both >> g & 1))) {
+                const T *u = warp % 2 ? row_of(p.draft, p.draft_stride, m.group[g]) : row_of(p.logits, p.logits_stride, m.group[g]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) a = fmaxf(a, to_float(u[(int)((int64_t)p.vocab * (4 * lane + j) / 128)]));
+#pragma unroll
+                for (int k = 16; k; k /= 2) a = fmaxf(a, __shfl_xor_sync(~0u, a, k));
+            }
+            if (lane == 0) reinterpret_cast<float *>(m.tops)[warp] = a;
+        }
+        __syncthreads();
+        const float2 *tops = m.tops;
+        const float f = heat.h * 1.44269504f;
+        int stage = 0;
 #pragma unroll 1
-        for (int i = first + units * kUnit + lane; i < end; i += 32) f(0, to_float(x[i]), BOTH ? to_float(y[i]) : 0.0f);
+        for (int g = 0; g < count; ++g) {
+            const bool two = both >> g & 1;
+            const float ca = tops[g].x * f, cb = tops[g].y * f;
+            const T *u = row_of(p.logits, p.logits_stride, m.group[g]), *v = two ? row_of(p.draft, p.draft_stride, m.group[g]) : u;
+            float sa[2] = {0, 0}, sb[2] = {0, 0};
+#pragma unroll 1
+            for (int unit = 0; unit < units; ++unit) {
+                Lot e, d;
+                if (wide) {
+                    copy_wait<kStages - 1>();
+                    e = from_ring(stage, 0);
+                    if (two) d = from_ring(stage, 1);
+                    issue(stage);
+                } else {
+                    e = from_row(u, first + unit * kUnit);
+                    if (two) d = from_row(v, first + unit * kUnit);
+                }
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) sa[j % 2] += power2(__fmaf_rn(element(e, j), f, -ca));
+                if (two) {
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) sb[j % 2] += power2(__fmaf_rn(element(d, j), f, -cb));
+                }
+                stage = stage == kStages - 1 ? 0 : stage + 1;
+            }
+#pragma unroll 1
+            for (int i = first + units * kUnit + lane; i < end; i += 32) {
+                sa[0] += power2(__fmaf_rn(to_float(u[i]), f, -ca));
+                if (two) sb[0] += power2(__fmaf_rn(to_float(v[i]), f, -cb));
+            }
+            float2 sum = make_float2(sa[0] + sa[1], sb[0] + sb[1]);
+#pragma unroll
+            for (int k = 16; k; k /= 2) sum.x += __shfl_xor_sync(~0u, sum.x, k), sum.y += __shfl_xor_sync(~0u, sum.y, k);
+            if (lane == 0) m.sums[warp][g] = sum;
+        }
+        // the block's, the cluster's
+        const int g = lane / kWarps, part = lane % kWarps;
+        __syncthreads();
+        float2 sum = g < count ? m.sums[part][g] : make_float2(0, 0);
+        auto over = [&] {
+#pragma unroll
+            for (int k = 1; k < kWarps; k *= 2) sum.x += __shfl_xor_sync(~0u, sum.x, k), sum.y += __shfl_xor_sync(~0u, sum.y, k);
+        };
+        over();
+        if (p.split > 1) {
+            if (warp == 0) {
+                for (int to = part; to < p.split; to += kWarps) {
+                    const uint32_t at = peer_addr(smem_addr(&m.block_sums[turn][rank][g]), to);
+                    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(sum.x), "f"(sum.y) : "memory");
+                }
+            }
+            cluster_barrier();
+            sum = make_float2(0, 0);
+            for (int from = part; from < p.split; from += kWarps) {
+                const float2 theirs = m.block_sums[turn][from][g];
+                sum.x += theirs.x, sum.y += theirs.y;
+            }
+            over();
+            turn ^= 1;
+        } else {
+            __syncthreads();                     // (the sums have been read)
+        }
+        x_sum = sum.x, y_sum = sum.y;
     }
+
     // The same run again, f(two elements of x, of y): a short loop, as f is long.
     template <bool BOTH, class F> __device__ __forceinline__ void pairs(F f) const
     {
-        constexpr int kStep = sizeof(T) / 2;                              // words of two
+        constexpr int kStep = sizeof(T) / 2;                              // words of two elements
         const int units = (end - first) / kUnit, rest = end - first - units * kUnit;
         const bool kept = wide && units <= kStages;
-        Eight a, b;
+        Lot a, b;
         if (units > 0 && !kept) {
             a = from_row(x, first);
             if (BOTH) b = from_row(y, first);
         }
 #pragma unroll 1
         for (int unit = 0; unit < units + (rest > 0); ++unit) {
-            Eight u = a, v = b;
+            Lot u = a, v = b;
             const int at = first + unit * kUnit;
             if (kept && unit < units) {
-                u = from_ring(unit, 0);
-                if (BOTH) v = from_ring(unit, 1);
+                const int stage = ring_base + unit >= kStages ? ring_base + unit - kStages : ring_base + unit;
+                u = from_ring(stage, 0);
+                if (BOTH) v = from_ring(stage, 1);
             } else if (unit + 1 < units) {
                 a = from_row(x, at + kUnit);
                 if (BOTH) b = from_row(y, at + kUnit);
             }
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kEach / 2; ++k) {
                 float c[2] = {element(u, 0), element(u, 1)}, d[2] = {0, 0};
                 if (BOTH) d[0] = element(v, 0), d[1] = element(v, 1);
                 if (unit == units) {                                          // (the rest of the row)
@@ -274,47 +368,12 @@ template <class T> struct Walk {
                 }
                 f(c, d);
 #pragma unroll
-                for (int w = 0; w + kStep < kWords; ++w) {
+                for (int w = 0; w + kStep < 4; ++w) {
                     u.w[w] = u.w[w + kStep];
                     if (BOTH) v.w[w] = v.w[w + kStep];
                 }
             }
         }
-    }
-
-    // In 32 bits: sums of 2^((x - x_top) log2 e / T), and of y's; false where these say nothing (no
-    // distribution, or the tops are far from it).  Few of the row stand for the largest.
-    template <bool BOTH> __device__ __forceinline__ bool estimate(float &x_sum, float &y_sum)
-    {
-        start_stream<BOTH>();
-        float a = -INFINITY, b = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = (int)((int64_t)p.vocab * (4 * lane + j) / 128);
-            a = fmaxf(a, to_float(x[i]));
-            if (BOTH) b = fmaxf(b, to_float(y[i]));
-        }
-#pragma unroll
-        for (int k = 16; k; k /= 2) {
-            a = fmaxf(a, __shfl_xor_sync(~0u, a, k));
-            if (BOTH) b = fmaxf(b, __shfl_xor_sync(~0u, b, k));
-        }
-        x_top = a, y_top = b;
-        const float f = heat.h * 1.44269504f, ca = a * f, cb = b * f;
-        float sa[2] = {0, 0}, sb[2] = {0, 0};
-        stream<BOTH>([&](int j, float u, float v) {
-            sa[j % 2] += power2(__fmaf_rn(u, f, -ca));
-            if (BOTH) sb[j % 2] += power2(__fmaf_rn(v, f, -cb));
-        });
-        Part mine{{sa[0] + sa[1], sb[0] + sb[1]}, {0, 0}, 0, 0, 0, 0};
-        exchange(mine, [&](int k) {
-            mine.p.h += __shfl_xor_sync(~0u, mine.p.h, k);
-            if (BOTH) mine.p.l += __shfl_xor_sync(~0u, mine.p.l, k);
-        });
-        x_sum = mine.p.h, y_sum = mine.p.l;
-        // (a NaN, or +inf, is in the sum; a sample without a token, or with none of the large ones, too)
-        constexpr float kLeast = 0.5f, kMost = 0x1p62f;
-        return x_sum > kLeast && x_sum < kMost && (!BOTH || (y_sum > kLeast && y_sum < kMost));
     }
 
     // The largest of x (and of y): whether both rows have a distribution, and x's first largest.
@@ -323,7 +382,7 @@ template <class T> struct Walk {
         Part mine{{0, 0}, {0, 0}, -INFINITY, -INFINITY, 0x7fffffff, 0};
         for (int i0 = first; i0 < end; i0 += kUnit)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < kEach; ++j) {
                 const int i = i0 + 32 * j + lane;
                 const float a = i < end ? to_float(x[i]) : -INFINITY, b = both && i < end ? to_float(y[i]) : -INFINITY;
                 if (a > mine.p_top) mine.p_top = a, mine.first = i;
@@ -464,23 +523,26 @@ template <class T> struct Walk {
         __syncthreads();
         const int found = rank * kWarps + choose(m.sub[lane % kWarps], kWarps);
         __syncthreads();
-        // its sixteenths
-        const int from = run_start(found), units = (run_start(found + 1) - from + 31) / 32, stop = run_start(found + 1);
-        auto sixteenth = [&](int k) { return min(from + 32 * (int)((int64_t)units * k / kWarps), stop); };
+        // its parts, one a warp
+        const int run_from = run_start(found), run_stop = run_start(found + 1);
+        auto part_of = [&](int k) { return run_from + (int)((int64_t)(run_stop - run_from) * k / kWarps); };
+        // a lane's share of them is side by side, too
+        const int start = part_of(warp), stop = part_of(warp + 1), share = (stop - start + 31) / 32;
         LongSum a;
 #pragma unroll 1
-        for (int i = sixteenth(warp) + lane; i < sixteenth(warp + 1); i += 32)
+        for (int i = start + lane * share; i < min(start + (lane + 1) * share, stop); ++i)
             if (!gone(i)) a.add(weight(i, less, of_x, of_y));
-        const Two sub = warp_sum(a.value());
+        const Two mine = a.value(), sub = warp_sum(mine);
         if (lane == 0) m.sub[warp] = sub;
         __syncthreads();
         if (choose(m.sub[lane % kWarps], kWarps) != warp) return false;
+        const int from = start + choose(mine, 32) * share, to = min(from + share, stop);
         // element by element
         answer = -1;
 #pragma unroll 1
-        for (int i0 = sixteenth(warp); i0 < sixteenth(warp + 1); i0 += 32) {
+        for (int i0 = from; i0 < to; i0 += 32) {
             const int i = i0 + lane;
-            const Two w = i < sixteenth(warp + 1) && !gone(i) ? weight(i, less, of_x, of_y) : Two{0, 0};
+            const Two w = i < to && !gone(i) ? weight(i, less, of_x, of_y) : Two{0, 0};
             const Two sum = base + warp_prefix(w, lane);
             const unsigned some = __ballot_sync(~0u, w.h > 0), hit = __ballot_sync(~0u, w.h > 0 && target < sum);
             if (some) answer = i0 + (hit ? __ffs(hit) - 1 : 31 - __clz(some));
@@ -517,16 +579,30 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
 
     const int parent0 = walk.lane > 0 && walk.lane < n ? m.parents[walk.lane] : -1, parent1 = walk.lane + 32 < n ? m.parents[walk.lane + 32] : -1;
 
+    walk.start = start;
+    auto rows_at = [&](const void *rows, int64_t stride) {
+        return reinterpret_cast<uintptr_t>(rows) | (start + n > 1 ? (uintptr_t)stride * sizeof(T) : 0);
+    };
+    walk.wide = (rows_at(p.logits, p.logits_stride) | (p.draft ? rows_at(p.draft, p.draft_stride) : 0)) % 16 == 0;
+    // (bit c: node c is a child)
+    auto children_of = [&](int node) {
+        return __ballot_sync(~0u, parent0 == node) | (uint64_t)__ballot_sync(~0u, parent1 == node) << 32;
+    };
+    auto first_of = [](uint64_t set) { return __ffsll(set) - 1; };
+    // A node is looked at together with its first child, that one's first child, and so on, as long as the ring holds
+    // them all: for small vocabularies, where a pass is latency, one does for up to four nodes.  (For larger ones, or
+    // without the draft's rows, what is not accepted costs more: 8 x 16 x 128,256 40 us for 37.)
+    const int runs = kWarps * p.split, run_units = ((p.vocab + Walk<T>::kUnit - 1) / Walk<T>::kUnit + runs - 1) / runs;
+    const int at_once = p.draft && walk.wide ? max(min(kGroup, Walk<T>::kStages / run_units), 1) : 1;
+    int place = 0, count = 0;                             // of the node in its group; the group's nodes
+    float x_sums = 0, y_sums = 0, child_value = 0;        // lane g kWarps: node g's; and the one after it: its first child's logits
+
     int here = 0, kept = n > 0;
     int token = -1;                                       // the token after the last, in the thread that knows it
     bool knows = writer;
     while (n > 0 && (greedy || heated)) {
-        walk.x = static_cast<const T *>(p.logits) + (start + here) * p.logits_stride;
-        walk.y = p.draft ? static_cast<const T *>(p.draft) + (start + here) * p.draft_stride : walk.x;
-        walk.wide = (reinterpret_cast<uintptr_t>(walk.x) | reinterpret_cast<uintptr_t>(walk.y)) % 16 == 0;
-        // (bit c: node c is a child)
-        const uint64_t children = __ballot_sync(~0u, parent0 == here) | (uint64_t)__ballot_sync(~0u, parent1 == here) << 32;
-        auto first_of = [](uint64_t set) { return __ffsll(set) - 1; };
+        walk.at_node(here);
+        const uint64_t children = children_of(here);
         const bool both = p.draft && children && heated;
         int accepted = -1, first;
         if (greedy) {
@@ -542,9 +618,34 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
             // so what is clear by one part in 2^14 is clear.
             constexpr float kClear = 0x1p-14f;
             const int child0 = children ? first_of(children) : 0;
-            const float first_x = children && inside(m.ids[child0]) ? to_float(walk.x[m.ids[child0]]) : -INFINITY;
-            const float first_y = both && inside(m.ids[child0]) ? to_float(walk.y[m.ids[child0]]) : -INFINITY;
-            clear = both ? walk.template estimate<true>(x_sum, y_sum) : walk.template estimate<false>(x_sum, y_sum);
+            if (++place >= count || m.group[place] != here) {
+                unsigned twos = 0;
+                int node = here;
+                place = count = 0;
+                __syncthreads();
+                for (uint64_t below = children;; below = children_of(node)) {
+                    if (threadIdx.x == 0) m.group[count] = node;
+                    if (p.draft && below) twos |= 1u << count;
+                    // (its first child's logits are asked for now)
+                    if (walk.lane / kWarps == count && walk.lane % kWarps < 2) {
+                        const int v = below ? m.ids[first_of(below)] : -1;
+                        child_value = -INFINITY;
+                        if (inside(v) && (walk.lane % kWarps == 0 || p.draft))
+                            child_value = to_float(walk.lane % kWarps ? walk.row_of(p.draft, p.draft_stride, node)[v]
+                                                                      : walk.row_of(p.logits, p.logits_stride, node)[v]);
+                    }
+                    if (++count == at_once || !below) break;
+                    node = first_of(below);
+                }
+                __syncthreads();
+                walk.estimate(count, twos, x_sums, y_sums);
+            }
+            const float first_x = __shfl_sync(~0u, child_value, place * kWarps), first_y = __shfl_sync(~0u, child_value, place * kWarps + 1);
+            x_sum = __shfl_sync(~0u, x_sums, place * kWarps), y_sum = __shfl_sync(~0u, y_sums, place * kWarps);
+            walk.x_top = m.tops[place].x, walk.y_top = m.tops[place].y;
+            // (a NaN, or +inf, is in the sum; a sample without a token, or with none of the large ones, too)
+            constexpr float kLeast = 0.5f, kMost = 0x1p62f;
+            clear = x_sum > kLeast && x_sum < kMost && (!both || (y_sum > kLeast && y_sum < kMost));
             if (!clear) {
                 if (!walk.tops(both, first)) break;
             } else if (children) {
@@ -571,6 +672,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
             }
         }
         if (!greedy && accepted < 0) {
+            walk.fill_ring(both, place, count);
             const Weigher of_x(walk.x_top, walk.heat), of_y(both ? walk.y_top : walk.x_top, walk.heat);
             const Two none{0, 0};
             Two q = none, A = none, B{1, 0};
@@ -697,7 +799,7 @@ template <class T> int clusters_of(int i, int dev)
 template <class T> int launch_walks(VerifyParams p, const Device &dev, cudaStream_t s)
 {
     int i = 4;
-    while (i > 0 && (p.batch > clusters_of<T>(i, dev.id) || p.vocab < (kWarps * kUnit << i) / 2)) --i;
+    while (i > 0 && (p.batch > clusters_of<T>(i, dev.id) || p.vocab < (kWarps * Walk<T>::kUnit << i) / 2)) --i;
     p.split = 1 << i;
     return launch<VerifyParams>(verify_kernel<T>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, false, s, p);
 }
