@@ -63,6 +63,7 @@ template <class T, int D, int NT, bool TREE> __global__ void __launch_bounds__(3
     extern __shared__ __align__(128) uint8_t smem[];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     const int request = blockIdx.y / p.kv_heads, kv = blockIdx.y % p.kv_heads, split = blockIdx.x;
+    if (TREE) wait_before(), allow_next();
     const Rows rows(p, request);
     const int page_mask = (1 << p.page_shift) - 1;
     const int32_t *table = p.table + request * p.table_stride;
@@ -566,6 +567,7 @@ constexpr int kTreeExtra = 12, kTreeJoin = 10;
 
 struct Plan {
     int nt, slabs, splits;      // nt 0: a prompt, or a tree by kTreeRows
+    int rows;                   // of a request and KV head, of trees (64 x 4096 at most)
     bool cluster;               // joined there
 };
 
@@ -579,6 +581,7 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms, bool tree)
     const int64_t heads = (int64_t)a->batch * c->kv_heads;
     if (tree && f.nt == 2 && heads <= sms && heads * a->max_len <= kTreeKeys) f.nt = 0;
     const int at_once = f.nt ? 8 * f.nt : tree ? kTreeRows : kPromptRows;
+    f.rows = (int)(rows < (1 << 18) ? rows : 1 << 18);
     const int64_t slabs = (rows + at_once - 1) / at_once;
     f.slabs = (int)(slabs < 65535 ? slabs : 65535);
     int64_t keys = a->max_len;
@@ -623,7 +626,7 @@ template <class T, int D, int NT, bool TREE> int launch_few(const AttendParams &
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    return launch<AttendParams>(kernel, grid, 32 * kFewWarps, smem, f.cluster ? f.splits : 1, false, s, p);
+    return launch<AttendParams>(kernel, grid, 32 * kFewWarps, smem, f.cluster ? f.splits : 1, TREE, s, p);
 }
 
 template <class T, int D, bool TREE> int launch_attend(const AttendParams &p, const Plan &f, int dev, cudaStream_t s)
@@ -634,7 +637,8 @@ template <class T, int D, bool TREE> int launch_attend(const AttendParams &p, co
                    : f.nt == 1 ? launch_few<T, D, 1, TREE>(p, f, grid, dev, s)
                                : launch_few<T, D, 2, TREE>(p, f, grid, dev, s);
     if (st != E2_OK || f.splits == 1 || f.cluster) return st;
-    const dim3 rows((unsigned)f.slabs * (f.nt ? 8 * f.nt : TREE ? kTreeRows : kPromptRows), pairs);
+    dim3 rows((unsigned)f.slabs * (f.nt ? 8 * f.nt : TREE ? kTreeRows : kPromptRows), pairs);
+    if (TREE) rows.x = (unsigned)f.rows;
     return launch<AttendParams>(join_kernel<T, D>, rows, 128, 0, 1, true, s, p);
 }
 

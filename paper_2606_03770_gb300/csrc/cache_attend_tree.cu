@@ -657,6 +657,8 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     __shared__ uint64_t ways[E2_MAX_DRAFT];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int request = blockIdx.x / p.kv_heads, kv = blockIdx.x % p.kv_heads;
+    wait_before();
+    allow_next();
     const Rows rows(p, request);
     const int64_t blocks = (rows.count + kTreeRows - 1) / kTreeRows;
     if (blocks <= blockIdx.y) return;
@@ -724,8 +726,6 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
             if (join) cluster_barrier(), cluster_barrier();
             meet(block + gridDim.y < blocks);
         }
-        allow_next();
-        __syncwarp();
         if (warp == 0)
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(m.memory), "r"(kColumns) : "memory");
     } else if (warp < 12) {
@@ -740,7 +740,6 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
             }
             meet(block + gridDim.y < blocks);
         }
-        allow_next();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
@@ -748,7 +747,6 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
             if (join) cluster_barrier(), cluster_barrier();
             meet(block + gridDim.y < blocks);
         }
-        allow_next();
     }
 }
 
@@ -762,16 +760,18 @@ template <class T, int D> int launch_as(const AttendParams &p, int blocks, int p
         if (e != cudaSuccess) return cuda_status(e);
         ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = at.val.clusterDim.y = 1, at.val.clusterDim.z = (unsigned)p.splits;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = (unsigned)p.splits;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)pairs, (unsigned)blocks, (unsigned)p.splits);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
-    cfg.attrs = &at;
-    cfg.numAttrs = p.splits > 1 && !p.parts;
+    cfg.attrs = at;
+    cfg.numAttrs = p.splits > 1 && !p.parts ? 2 : 1;
     return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
 }
 

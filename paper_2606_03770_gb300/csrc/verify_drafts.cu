@@ -557,6 +557,8 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
 {
     __shared__ Shared m;
     const int request = blockIdx.x / p.split;
+    wait_before();
+    allow_next();
     extern __shared__ __align__(16) uint8_t dynamic[];
     Walk<T> walk(p, m, dynamic);
     const bool writer = walk.rank == 0 && threadIdx.x == 0;
@@ -801,7 +803,7 @@ template <class T> int launch_walks(VerifyParams p, const Device &dev, cudaStrea
     int i = 4;
     while (i > 0 && (p.batch > clusters_of<T>(i, dev.id) || p.vocab < (kWarps * Walk<T>::kUnit << i) / 2)) --i;
     p.split = 1 << i;
-    return launch<VerifyParams>(verify_kernel<T>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, false, s, p);
+    return launch<VerifyParams>(verify_kernel<T>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, true, s, p);
 }
 
 }  // namespace
