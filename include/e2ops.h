@@ -21,7 +21,7 @@
  *    what is out of range is never followed, with the result written below.
  *  - A call with zero tokens, rows or requests does nothing and returns E2_OK.
  *  - The kernels for prompts (products from 17 tokens, attention from 65 rows of a
- *    request and KV head) wait for copies and products of their own block.  Such a
+ *    request and KV head, of trees from nine) wait for copies and products of their own block.  Such a
  *    wait ends after some seconds at the latest; the block's outputs are NaN then,
  *    with E2_OK, which is returned long before.
  */
@@ -196,8 +196,9 @@ int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace,
 
 /* e2_cache_attend, but that node i sees the keys before base, its own and those of the
  * nodes on its way up; with a window > 0 those whose position is above its own minus
- * window; and that what rounding took from the weights is in a product of its own up to 64
- * rows for bf16 too.  max_new is at most E2_MAX_DRAFT; nodes beyond (of a request that has more) are
+ * window.  Up to eight rows what rounding took from the weights is in a product of its own for
+ * bf16 too; from 17 on, and from nine on where the launch is small, keys and values are rounded
+ * to fp16, as e2_cache_attend's from 65 rows on.  max_new is at most E2_MAX_DRAFT; nodes beyond (of a request that has more) are
  * NaN where they see keys.  parents: [tokens]. */
 size_t e2_cache_attend_tree_workspace(const e2_cache *c, const e2_attend_args *a);
 int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
@@ -217,9 +218,9 @@ int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32
  *   nodes[r][k], k < kept[r]: them; -1 from there on
  *   answer[r][k]: the token after nodes[r][k], the last the answer; -1 from kept[r] on
  * Exponentials and sums have some 45 bits, so decisions are those of 64 bits but for numbers
- * within 2^-40 or so of a border; what (P - q)+ sums to counts as nothing below 2^-36, and P stays.
- * Exponentials below e^-64 of the largest count as nothing in sums and for the answer, below e^-745 (which 64 bits
- * do not hold) for a drafted token.
+ * within 2^-36 or so of a border; what (P - q)+ sums to counts as nothing below 2^-36, and P stays.
+ * Exponentials below e^-64 of the largest may count as nothing in sums and for the answer, and do
+ * below e^-745 (which 64 bits do not hold) for a drafted token.
  * -inf marks a forbidden token.  The walk ends with the answer -1 at a row that holds NaN or
  * +inf or has no token allowed (of logits; of draft where a child is asked), and at node 0 for a
  * T that is negative, infinite or NaN.  ids outside the vocabulary are never accepted.

@@ -34,6 +34,8 @@ namespace {
 // instructions, some 600 a warp and tile (1,000 for sixteen rows), which three warps of a
 // scheduler issue at half its rate; four, with two stages or 128 registers, are no faster
 // (130, 181).
+// A tree's columns have their ways as bits, and see all keys before the tree (TREE): 1 request of 32 KV heads x 5 nodes x
+// 517 keys 9.4, 8 x 8 KV heads x 8 rows x 65,000 keys 138, 2 rows 133.
 
 constexpr int kFewWarps = 4, kTile = 32, kFewStages = 3, kFewBlocks = 3;
 constexpr int kMostSplits = 128, kMostCluster = 8;

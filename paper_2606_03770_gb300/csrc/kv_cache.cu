@@ -202,7 +202,8 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads) read_kerne
 // Tokens of accepted ways, to their places.  A warp has a request's tokens of one layer and head:
 // it reads them all, keys and values, in pieces of 16 bytes (and the scales, four or eight), and
 // writes them then, so that a token may go where another comes from.  Bound by the way to the
-// first byte, of addresses that hang on one another (lengths, nodes, pages).
+// first byte, of addresses that hang on one another (lengths, nodes, pages): 2.6 us for one layer of a
+// request, 4.3 for 80 layers of 8 requests (3.6 MB read), where registers for ways of 64 nodes took 8.4.
 struct KeepParams {
     int layers, batch, cols, pages, page_shift, kv_heads, table_cols;
     const unsigned long long *arrays;

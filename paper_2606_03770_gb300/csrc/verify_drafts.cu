@@ -9,14 +9,24 @@
 namespace e2ops {
 namespace {
 
+// Bound by latency where there are few requests: some five dependent steps a node (its rows, the block's sums, the
+// cluster's barrier, the decision), two microseconds; by the rows' bytes and, at a walk's end, by instructions where
+// there are many.  Measured, us: 1 request x 5 nodes of 32,000 tokens 19, 8 x 16 of 128,256 (bf16) 40, 64 x 8 of
+// 128,256 (fp32) 132, of which the levels of the longest walk 60 at 5 TB/s, then 30 for the sums in 45 bits (85% of
+// issue slots, some 55 an element); 13 x 13 of 50,001 without the draft's rows 20.
+//
 // A cluster of blocks walks a request's tree, and all its warps take the same decisions.  Each
-// warp has a run of the vocabulary; what a pass over a row gives is the warps' sums, which every
-// warp reads after one barrier of the cluster.  With p = w / Z, w = exp((x - max x) / T), and q
-// likewise of the draft's row, after k rejections
+// warp has a run of the vocabulary; what a pass over a row gives is sums, the blocks' of which
+// every block gets before one barrier of the cluster.  A node's rows are summed in 32 bits first, and a first child
+// that is clear by one part in 2^14 is taken; only what is not, and a walk's end, goes through 45 bits.
+// With p = w / Z, w = exp((x - max x) / T), and q likewise of the draft's row, after k rejections
 //   P = (p - A q)+ / B,  A_0 = 0, B_0 = 1, A_{k+1} = A_k + B_k, B_{k+1} = sum (p - A_{k+1} q)+,
-// as (P - q)+ is (p - A q - B q)+ / B.  Without the draft's rows a rejected token leaves P.
+// as (P - q)+ is (p - A q - B q)+ / B.  Without the draft's rows a rejected token leaves P.  The first of these sums comes
+// out of the pass that gives Z: by the 32-bit sums it is known well enough which p are above q.
 // The token after the last is found in the blocks' sums, the warps', those of an eighth of a
-// warp's run, of a lane's share of it, and then element by element.  The numbers that decide have some 45 bits.
+// warp's run, of a lane's share of it, and then element by element.
+// Tried: 512 threads of 128 registers (spills went through the caches: 287 for 64 x 8), all parts read from their blocks by
+// every warp (5 us a pass), four likely nodes at once whatever the vocabulary (64 x 8 205, 8 x 16 40).
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMostCluster = 16;
 constexpr int kRing = 6144;                      // bytes of a warp's copies on their way
