@@ -58,6 +58,7 @@ struct Shared {
     Part parts[kWarps], blocks[2][kMostCluster];  // (a block may be one pass ahead of another)
     Two sub[kWarps];
     float2 tops[kGroup], sums[kWarps][kGroup], block_sums[2][kMostCluster][kGroup];           // (x, y)
+    float2 lane_sums[kWarps][kGroup][32];
     int group[kGroup];                           // the nodes
     int32_t ids[E2_MAX_DRAFT], parents[E2_MAX_DRAFT];
     float uniforms[E2_MAX_DRAFT];
@@ -306,20 +307,30 @@ template <class T> struct Walk {
                 sa[0] += power2(__fmaf_rn(to_float(u[i]), f, -ca));
                 if (two) sb[0] += power2(__fmaf_rn(to_float(v[i]), f, -cb));
             }
-            float2 sum = make_float2(sa[0] + sa[1], sb[0] + sb[1]);
-#pragma unroll
-            for (int k = 16; k; k /= 2) sum.x += __shfl_xor_sync(~0u, sum.x, k), sum.y += __shfl_xor_sync(~0u, sum.y, k);
-            if (lane == 0) m.sums[warp][g] = sum;
+            m.lane_sums[warp][g][lane] = make_float2(sa[0] + sa[1], sb[0] + sb[1]);
         }
-        // the block's, the cluster's
+        // the warp's, the block's, the cluster's
         const int g = lane / kWarps, part = lane % kWarps;
-        __syncthreads();
-        float2 sum = g < count ? m.sums[part][g] : make_float2(0, 0);
-        auto over = [&] {
+        auto over = [&](float2 &sum) {
 #pragma unroll
             for (int k = 1; k < kWarps; k *= 2) sum.x += __shfl_xor_sync(~0u, sum.x, k), sum.y += __shfl_xor_sync(~0u, sum.y, k);
         };
-        over();
+        __syncwarp();
+        {
+            float2 mine = make_float2(0, 0);
+            if (g < count) {
+#pragma unroll
+                for (int k = 0; k < 32; k += kWarps) {
+                    const float2 theirs = m.lane_sums[warp][g][part + k];
+                    mine.x += theirs.x, mine.y += theirs.y;
+                }
+            }
+            over(mine);
+            if (part == 0) m.sums[warp][g] = mine;
+        }
+        __syncthreads();
+        float2 sum = g < count ? m.sums[part][g] : make_float2(0, 0);
+        over(sum);
         if (p.split > 1) {
             if (warp == 0) {
                 for (int to = part; to < p.split; to += kWarps) {
@@ -333,7 +344,7 @@ template <class T> struct Walk {
                 const float2 theirs = m.block_sums[turn][from][g];
                 sum.x += theirs.x, sum.y += theirs.y;
             }
-            over();
+            over(sum);
             turn ^= 1;
         } else {
             __syncthreads();                     // (the sums have been read)
@@ -623,7 +634,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                 if (m.ids[first_of(set)] == first) accepted = first_of(set);
             if (accepted < 0) token = first;
         }
-        float x_sum = 0, y_sum = 0;
+        float x_sum = 0, y_sum = 0, first_x = 0, first_y = 0;
         bool clear = false;
         if (!greedy) {
             // In 32 bits first: exponents are off by 2^-18 at most (of 64, and 2^-18 of that in f), sums by less,
@@ -632,27 +643,26 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
             const int child0 = children ? first_of(children) : 0;
             if (++place >= count || m.group[place] != here) {
                 unsigned twos = 0;
-                int node = here;
+                int node = here, my_node = 0, my_child = -1;
                 place = count = 0;
                 __syncthreads();
                 for (uint64_t below = children;; below = children_of(node)) {
                     if (threadIdx.x == 0) m.group[count] = node;
                     if (p.draft && below) twos |= 1u << count;
-                    // (its first child's logits are asked for now)
-                    if (walk.lane / kWarps == count && walk.lane % kWarps < 2) {
-                        const int v = below ? m.ids[first_of(below)] : -1;
-                        child_value = -INFINITY;
-                        if (inside(v) && (walk.lane % kWarps == 0 || p.draft))
-                            child_value = to_float(walk.lane % kWarps ? walk.row_of(p.draft, p.draft_stride, node)[v]
-                                                                      : walk.row_of(p.logits, p.logits_stride, node)[v]);
-                    }
+                    if (walk.lane / kWarps == count) my_node = node, my_child = below ? first_of(below) : -1;
                     if (++count == at_once || !below) break;
                     node = first_of(below);
                 }
+                // (the first children's logits are asked for now, looked at later)
+                T value = from_float<T>(-INFINITY);
+                const int v = my_child >= 0 ? m.ids[my_child] : -1;
+                if (inside(v) && (walk.lane % kWarps == 0 || (walk.lane % kWarps == 1 && p.draft)))
+                    value = walk.lane % kWarps ? walk.row_of(p.draft, p.draft_stride, my_node)[v] : walk.row_of(p.logits, p.logits_stride, my_node)[v];
                 __syncthreads();
                 walk.estimate(count, twos, x_sums, y_sums);
+                child_value = to_float(value);
             }
-            const float first_x = __shfl_sync(~0u, child_value, place * kWarps), first_y = __shfl_sync(~0u, child_value, place * kWarps + 1);
+            first_x = __shfl_sync(~0u, child_value, place * kWarps), first_y = __shfl_sync(~0u, child_value, place * kWarps + 1);
             x_sum = __shfl_sync(~0u, x_sums, place * kWarps), y_sum = __shfl_sync(~0u, y_sums, place * kWarps);
             walk.x_top = m.tops[place].x, walk.y_top = m.tops[place].y;
             // (a NaN, or +inf, is in the sum; a sample without a token, or with none of the large ones, too)
@@ -715,10 +725,11 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                 // its weight, however small
                 Two w = none, wq = none;
                 int e = 0, eq = 0;
-                const bool some = in && of_x.wide(to_float(walk.x[v]), m.table, w, e);
+                const bool known = c == first_of(children);
+                const bool some = in && of_x.wide(known ? first_x : to_float(walk.x[v]), m.table, w, e);
                 if (p.draft) {
                     // u q(v) < P(v), times Z_p Z_q B and a power of two
-                    const bool some_q = in && of_y.wide(to_float(walk.y[v]), m.table, wq, eq);
+                    const bool some_q = in && of_y.wide(known ? first_y : to_float(walk.y[v]), m.table, wq, eq);
                     const int most = some && some_q ? max(e, eq) : some ? e : eq;
                     w = scaled(w, some ? e - most : -127);
                     wq = scaled(wq, some_q ? eq - most : -127);
@@ -731,9 +742,9 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                     Two unused;
                     const Two more = A + B, share = more * all / q;
                     Two sum;
-                    const bool known = near > 0 && walk.take_split(share, near, sum);
+                    const bool enough = near > 0 && walk.take_split(share, near, sum);
                     walk.set_share(share);
-                    if (!known) sum = walk.template sums<false, true>(of_x, of_y, unused);
+                    if (!enough) sum = walk.template sums<false, true>(of_x, of_y, unused);
                     near = 0;                             // (the first child's only)
                     sum = sum / all;
                     if (sum.h > kNothing * B.h) {
@@ -778,7 +789,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
         if (kept) nodes[0] = 0;
         for (int i = kept; i < p.max_new; ++i) nodes[i] = answer[i] = -1;
     }
-    cluster_barrier();                                    // (peers have been read)
+    // (what goes to other blocks goes before a barrier of the cluster, so blocks may end one by one)
 }
 
 // How many clusters of 2^i blocks run at once.
