@@ -73,6 +73,45 @@ def test_long_contexts():
     check_tree([30011], [3], 1, 2, 64, 32, HALF, seed=5)
 
 
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,G,new,ctx", [(8, 2, 16, 700), (8, 8, 16, 700), (4, 8, 16, 1100), (4, 3, 9, 1100), (3, 64, 3, 2000)])
+def test_contexts_joined_in_clusters(dtype, D, B, G, new, ctx):
+    """Parts of two and of four blocks, of a few rows and of many, some of them empty."""
+    check_tree([ctx - 90 * r if r != 2 else new for r in range(B)], [new] * B, 8, G, D, 64, dtype, seed=B + G)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window", [0, 70])
+def test_pages(page, D, window):
+    """Copies of a tile in one piece, two and four."""
+    check_tree([777, 64, 320], [20, 3, 64], 2, 4, D, page, window=window, seed=page)
+
+
+def test_more_requests_than_multiprocessors():
+    news = [1 + r % 5 for r in range(60)]
+    check_tree([200 + 7 * r for r in range(60)], news, 4, 8, 64, 32, seed=15)
+    check_tree([20 + r for r in range(60)], news, 4, 1, 128, 16, seed=16)
+
+
+def test_tables_with_columns_to_spare():
+    from paper_2606_03770_gb300 import ops
+    for G in (1, 8):
+        cache, q, table, lens, starts = setup([300, 90], [9, 4], 2, G, 128, 64, seed=17, extra_cols=3)
+        parents = trees([9, 4])
+        kw = dict(max_new=9, max_len=300)
+        want = ops.cache_attend_tree(cache, q, parents, table.contiguous(), lens, starts, **kw)
+        wide = torch.full((2, table.shape[1] + 5), 10 ** 6, **I32)
+        wide[:, 2:2 + table.shape[1]] = table
+        assert torch.equal(ops.cache_attend_tree(cache, q, parents, wide[:, 2:2 + table.shape[1]], lens, starts, **kw), want)
+        # a table that ends within the context, and one that ends within the tree
+        for cols in (1, 4):
+            out = ops.cache_attend_tree(cache, q, parents, table[:, :cols], lens, starts, **kw)
+            ref, bound, _ = DR.attend_tree(cache, q, parents, table[:, :cols], lens, starts, 128 ** -0.5, 0)
+            R.close(out, ref, bound)
+
+
 def test_ragged_batches_and_empty_requests():
     check_tree([0, 517, 1, 90, 64], [0, 12, 1, 64, 3], 3, 7, 64, 16, HALF, seed=6)
     check_tree([5, 700], [0, 1], 8, 1, 128, 64, seed=7)
@@ -372,6 +411,28 @@ def test_ties_go_to_the_first():
     check_verify(*s, temperature=torch.zeros(3, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", [HALF, BF, F32])
+def test_rows_where_they_lie(dtype):
+    """Rows of other strides and alignments than one another's, and of a call with a single row."""
+    V = 6001
+    for seed, (a, b) in enumerate(((0, 3), (8, 0), (5, 1), (16, 16))):
+        s = batch_of([5, 3, 8], V, dtype, seed=seed)
+        x, y = (torch.full((16, V + 2 * k + 1), math.nan, device="cuda", dtype=dtype) for k in (a, b))
+        x[:, a:a + V], y[:, b:b + V] = s[0], s[5]
+        check_verify(x[:, a:a + V], *s[1:5], y[:, b:b + V])
+    s = batch_of([1], V, dtype, seed=5)
+    wide = torch.full((3, V + 3), math.nan, device="cuda", dtype=dtype)
+    for at in (0, 1, 2):
+        wide[1, at:at + V] = s[0][0]
+        check_verify(wide[1:2, at:at + V], *s[1:5], None)
+
+
+def test_many_requests():
+    s = batch_of([2] * 400, 3000, BF, seed=13)
+    check_verify(*s)
+    check_verify(*batch_of([1, 0, 3] * 100, 9001, F32, seed=14, draft=False))
+
+
 def test_starts_out_of_range():
     s = batch_of([4] * 4, 300, seed=10)
     for starts in ([0, 0, 16, 16, 16], [-4, 4, 8, 12, 20], [8, 4, 0, 16, 12], [0, 4, 8, 2 ** 31 - 1, 16]):
@@ -503,6 +564,9 @@ def test_refusals():
             keep(**kw)
     with pytest.raises(e2ga.E2Error):
         keep(lens_out=lens)
+    big = setup([9000], [9], 2, 4, 64, 16)
+    with pytest.raises(e2ga.E2Error, match="workspace"):
+        ops.cache_attend_tree(*big[:2], trees([9]), *big[2:], max_new=9, max_len=9000, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     with pytest.raises(AttributeError):
         layers.arrays = None
     other = ops.Cache.empty(4, 16, 1, 64)
