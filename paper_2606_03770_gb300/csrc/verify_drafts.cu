@@ -580,6 +580,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
     const int request = blockIdx.x / p.split;
     wait_before();
     allow_next();
+    if (p.split > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     extern __shared__ __align__(16) uint8_t dynamic[];
     Walk<T> walk(p, m, dynamic);
     const bool writer = walk.rank == 0 && threadIdx.x == 0;
@@ -620,6 +621,8 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
     int place = 0, count = 0;                             // of the node in its group; the group's nodes
     float x_sums = 0, y_sums = 0, child_value = 0;        // lane g kWarps: node g's; and the one after it: its first child's logits
 
+    // (the cluster's blocks run, so that what goes to them has a place)
+    if (p.split > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     int here = 0, kept = n > 0;
     int token = -1;                                       // the token after the last, in the thread that knows it
     bool knows = writer;
