@@ -242,7 +242,7 @@ int e2_verify_drafts(const e2_verify_args *a, void *stream);
 /* Keeps the tokens of such a way: in the cache of each layer token base + nodes[r][k] becomes
  * token base + k, k < kept[r], codes and scales of keys and values, all read before any is
  * written; lens_out[r] = base + kept[r].  kept counts as 0..min(cols, the request's nodes);
- * what is not a node, or not in the cache, is not moved.  lens_out may not be lens.
+ * what is not a node, or not in the cache, is not moved.  lens_out shares no memory with what is read.
  * arrays (device memory): the addresses of each layer's k_codes, k_scales, v_codes, v_scales, as
  * e2_cache_layers writes them (to host memory) once the caches, all of one shape and of different
  * memory, have been checked; c is one of them. */

@@ -453,8 +453,12 @@ extern "C" int e2_cache_keep(const e2_cache *c, const e2_keep_args *a, void *str
     for (const void *p : ptrs)
         if (!p || !aligned(p, p == a->arrays ? 8 : 4) || !on_device(p, dev.id))
             return fail(E2_EINVAL, "arrays must be given, memory of the current device");
-    if (a->lens_out < a->lens + a->batch && a->lens < a->lens_out + a->batch)
-        return fail(E2_EINVAL, "lens_out may not be lens");
+    // (what others may still have to read when a request's length is written)
+    auto apart = [&](const int32_t *of, int64_t n) { return a->lens_out + a->batch <= of || of + n <= a->lens_out; };
+    if (!apart(a->lens, a->batch) || !apart(a->starts, (int64_t)a->batch + 1) || !apart(a->kept, a->batch) ||
+        !apart(a->table, (a->batch - 1) * a->table_stride + a->table_cols) ||
+        (a->cols && !apart(a->nodes, (a->batch - 1) * a->nodes_stride + a->cols)))
+        return fail(E2_EINVAL, "lens_out may not share memory with lens, starts, kept, nodes or table");
     const int64_t threads = (int64_t)a->layers * a->batch * c->kv_heads * 32, blocks = (threads + kThreads - 1) / kThreads;
     if (a->layers > (1 << 20) || a->batch > (1 << 20) || blocks > 0x7fffffff) return fail(E2_EINVAL, "too many layers and requests for one call");
     const KeepParams p{a->layers, a->batch, a->cols, c->pages, __builtin_ctz((unsigned)c->page_size), c->kv_heads, a->table_cols,

@@ -570,7 +570,7 @@ def cache_keep(layers, table, lens, starts, nodes, kept, lens_out=None):
     """Move the accepted nodes' keys and values, in every layer (``CacheLayers``), to where the
     tokens after the tree's first belong: node ``nodes[r, k]`` of request r to token
     k of its tree, for k < ``kept[r]``.  Returns the cached tokens of each request after
-    that, int32 [batch] (``lens_out``, allocated unless given; not ``lens``)."""
+    that, int32 [batch] (``lens_out``, allocated unless given; of memory of its own)."""
     _need(isinstance(layers, CacheLayers), "layers must be a CacheLayers")
     done = (_binding or binding()).keep(layers.fast, table, lens, starts, nodes, kept, lens_out)
     if done is not None:

@@ -564,6 +564,9 @@ def test_refusals():
             keep(**kw)
     with pytest.raises(e2ga.E2Error):
         keep(lens_out=lens)
+    for shared in (kept, starts[:-1], starts[1:], nodes.view(-1)[1:3], table.view(-1)[:2], table.view(-1)[-2:]):
+        with pytest.raises(e2ga.E2Error, match="lens_out"):
+            keep(lens_out=shared)
     big = setup([9000], [9], 2, 4, 64, 16)
     with pytest.raises(e2ga.E2Error, match="workspace"):
         ops.cache_attend_tree(*big[:2], trees([9]), *big[2:], max_new=9, max_len=9000, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
@@ -705,6 +708,46 @@ def test_captured_steps_replay():
             got = [x.clone() for x in got]
             for x, y in zip(got, f()):
                 assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("G", [1, 8])
+def test_captured_between_other_work(G):
+    """Calls whose graph nodes follow copies, fills and another stream's work."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([300, 90], [9, 4], 2, G, 64, 64, seed=18)
+    layers = ops.CacheLayers([cache])
+    parents, s = trees([9, 4]), batch_of([9, 4], 9001, BF, seed=18)
+    here, there = torch.empty_like(q), torch.zeros_like(s[0])
+    side = torch.cuda.Stream()
+
+    def step():
+        main = torch.cuda.current_stream()
+        here.copy_(q)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            there.copy_(s[0])
+            there.mul_(1)
+        out = ops.cache_attend_tree(cache, here, parents, table, lens, starts, max_new=9, max_len=300)
+        main.wait_stream(side)
+        kept, nodes, answer = ops.verify_drafts(there, *s[1:5], draft=s[5], max_new=9)
+        there.zero_()
+        return out, kept, nodes, answer, ops.cache_keep(layers, table, lens, starts, nodes.clone(), kept)
+
+    before = {k: getattr(cache, k).clone() for k in ("k_codes", "k_scales", "v_codes", "v_scales")}
+    restore = lambda: [getattr(cache, k).copy_(v) for k, v in before.items()]
+    want = [x.clone() for x in step()]
+    torch.cuda.synchronize()
+    restore()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        restore()
+        here.zero_(), there.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
 
 
 def test_two_streams_at_once():
