@@ -635,7 +635,9 @@ template <class T, int D, bool TREE> int launch_attend(const AttendParams &p, co
 {
     const unsigned pairs = (unsigned)p.batch * p.kv_heads;
     const dim3 grid((unsigned)f.splits, pairs, (unsigned)f.slabs);
-    const int st = f.nt == 0   ? (TREE ? launch_tree : launch_prompt)(p, D, std::is_same<T, __half>::value, f.slabs, (int)pairs, dev, s)
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    const int st = f.nt == 0   ? TREE ? launch_tree(p, D, kHalf, f.rows <= kTreeRows / 2, f.slabs, (int)pairs, dev, s)
+                                      : launch_prompt(p, D, kHalf, f.slabs, (int)pairs, dev, s)
                    : f.nt == 1 ? launch_few<T, D, 1, TREE>(p, f, grid, dev, s)
                                : launch_few<T, D, 2, TREE>(p, f, grid, dev, s);
     if (st != E2_OK || f.splits == 1 || f.cluster) return st;

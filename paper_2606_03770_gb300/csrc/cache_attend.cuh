@@ -125,9 +125,9 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
 // The rows of a prompt (cache_attend_prompt.cu): blocks of kPromptRows, `splits` parts of the keys.
 constexpr int kPromptRows = 256;
 int launch_prompt(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s);
-// The rows of trees (cache_attend_tree.cu), likewise by kTreeRows; without room for parts (p.parts) up to kTreeCluster
+// The rows of trees (cache_attend_tree.cu), likewise by kTreeRows, or by half as many (few); without room for parts (p.parts) up to kTreeCluster
 // of them are joined in a cluster.
 constexpr int kTreeRows = 128, kTreeCluster = 4;
-int launch_tree(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s);
+int launch_tree(const AttendParams &p, int head_dim, bool half, bool few, int blocks, int pairs, int dev, cudaStream_t s);
 
 }  // namespace e2ops

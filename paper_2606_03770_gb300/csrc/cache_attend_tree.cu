@@ -43,13 +43,16 @@ template <int D> struct TreeShared {
     static constexpr int kBytes = kStages * 2 * kTile + kRawStages * kRaw + 1024;
 };
 
-// 128 rows, and the tiles of keys that they see, of this split's.
+// Rows of a block: 64 that lie there twice, or 128.
+template <bool TWICE> constexpr int kRowsOf = TWICE ? kTreeRows / 2 : kTreeRows;
+
+// So many rows, and the tiles of keys that they see, of this split's.
 struct Span {
     Slab slab;
     int hi, first, n;
-    __device__ Span(const AttendParams &p, const Rows &rows, const Tree &tree, int64_t block) : slab(rows, block * kTreeRows)
+    __device__ Span(const AttendParams &p, const Rows &rows, const Tree &tree, int64_t block, int at_once) : slab(rows, block * at_once)
     {
-        const int last = (int)min((int64_t)kTreeRows, slab.left) - 1;
+        const int last = (int)min((int64_t)at_once, slab.left) - 1;
         // (32 bits: lengths stop 64 short of 2^31)
         const int lo = p.window > 0 ? (int)max((int64_t)tree.base - p.window + 1, (int64_t)0) : 0;
         hi = (int)max(min(min(slab.pos(last) + 1, (int64_t)p.table_cols << p.page_shift), (int64_t)0x7fffffc0), (int64_t)0);
@@ -168,17 +171,16 @@ __device__ __forceinline__ float largest_of(float a, float b, float c)
 }
 
 // Four warps: weights of even tiles (set 0) or odd ones, a thread a row; then the rows' outputs, by set 0.
-template <class T, int D>
+template <class T, int D, bool TWICE>
 __device__ __forceinline__ void weights(const AttendParams &p, const Span &span, const Shared<D> &m, const Tree &tree, int64_t skipped,
                                         int kv, int set, int quarter, int lane, bool join)
 {
     constexpr int GR = D / E2_CACHE_GROUP;
     constexpr bool kRest = std::is_same<T, __half>::value;
-    // (up to 64 rows lie there twice: set 0 has the first ones, set 1 the others, so that all schedulers have some)
+    // (up to 64 rows lie there twice: the first ones have a tile's first 32 keys, the others the last)
     const Slab &slab = span.slab;
-    const bool narrow = slab.left <= kTreeRows / 2;
-    const int row = 32 * (narrow ? quarter % 2 : quarter) + lane;
-    const bool live = slab.live(row), some = slab.live(row - lane), any = some && (!narrow || quarter / 2 == set);
+    const int row = 32 * (TWICE ? quarter % 2 : quarter) + lane, keys_part = TWICE ? quarter / 2 : 0;
+    const bool live = slab.live(row), some = slab.live(row - lane);
     const int64_t token = slab.token(row);
     const int head = slab.head(kv, row);
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
@@ -225,45 +227,49 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     // whether a tile's sums are there, and all before it (products run in their order)
     auto summed = [&](int j) { return warp_wait(m.summed + 8 * (j % kScores), j / kScores & 1, lane); };
     const uint32_t sums = m.memory + lanes + kSums + set * 128;
+    // a set's tiles: all 64 keys of each, or this warp's 32 of them
+    constexpr int kMine = TWICE ? 32 : 64;
+    using Bits = typename std::conditional<TWICE, uint32_t, unsigned long long>::type;
     int stage = set, next_place = set, next_phase = 0;
     for (int j = set; j < span.n; j += 2) {
-        const int key0 = (span.first + j) * kKeys, place = next_place;
+        const int key0 = (span.first + j) * kKeys + 32 * keys_part, place = next_place;
         const uint32_t at = m.memory + lanes + place * 64;
         ok = warp_wait(m.scored + 8 * place, next_phase, lane);
         if (!ok) break;
         next_place += 2;
         if (next_place >= kScores) next_place -= kScores, next_phase ^= 1;
-        if (!any) {
+        if (!some) {
             if (lane == 0) barrier_arrive(m.weighed + 8 * place);
             continue;
         }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        uint32_t half[2][32];
-        load_columns(half[0], at);
-        load_columns(half[1], at + 32);
-        const uint32_t present = *reinterpret_cast<const volatile uint32_t *>(m.there[stage]);
-        unsigned long long spoils[GR];
+        uint32_t half[kMine / 32][32];
 #pragma unroll
-        for (int i = 0; i < GR; ++i) spoils[i] = *reinterpret_cast<const volatile unsigned long long *>(m.bad[stage][i]);
+        for (int i = 0; i < kMine / 32; ++i) load_columns(half[i], at + 32 * (keys_part + i));
+        const uint32_t all_there = TWICE ? 0x0101u : 0x01010101u;
+        const uint32_t present = *reinterpret_cast<const volatile uint32_t *>(m.there[stage]) >> (16 * keys_part) & all_there;
+        Bits spoils[GR];
+#pragma unroll
+        for (int i = 0; i < GR; ++i) spoils[i] = *reinterpret_cast<const volatile Bits *>(&m.bad[stage][i][2 * keys_part]);
         stage = stage + 2 >= kStages ? stage + 2 - kStages : stage + 2;
-        loaded(half[0]);
-        loaded(half[1]);
+#pragma unroll
+        for (int i = 0; i < kMine / 32; ++i) loaded(half[i]);
         float *s = reinterpret_cast<float *>(half);
-        // keys this row sees, of the tile's
-        unsigned long long seen = ~0ull;
-        const bool whole = __all_sync(~0u, from <= key0 && key0 + kKeys - 1 <= pos) && present == 0x01010101u;
+        // keys this row sees, of these
+        Bits seen = ~(Bits)0;
+        const bool whole = __all_sync(~0u, from <= key0 && key0 + kMine - 1 <= pos) && present == all_there;
         if (!whole) {
             const int lowest = from - key0, highest = pos - key0, shift = tree.base - key0;
-            seen = highest < 0 ? 0ull : highest >= 63 ? ~0ull : (2ull << highest) - 1;
-            if (lowest > 0) seen &= lowest > 63 ? 0ull : ~0ull << lowest;
-            seen |= shift >= 0 ? (shift > 63 ? 0ull : way << shift) : (shift < -63 ? 0ull : way >> -shift);
+            seen = highest < 0 ? 0 : highest >= kMine - 1 ? ~(Bits)0 : ((Bits)2 << highest) - 1;
+            if (lowest > 0) seen &= lowest > kMine - 1 ? 0 : ~(Bits)0 << lowest;
+            seen |= (Bits)(shift >= 0 ? (shift > 63 ? 0 : way << shift) : (shift < -63 ? 0 : way >> -shift));
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                if (!(present >> (8 * w) & 1)) seen &= ~(0xffffull << (16 * w));
+            for (int w = 0; w < kMine / 16; ++w)
+                if (!(present >> (8 * w) & 1)) seen &= ~((Bits)0xffff << (16 * w));
             // (the table's end, which may be before the tree's)
-            if (key0 + kKeys > span.hi) seen &= span.hi > key0 ? (1ull << (span.hi - key0)) - 1 : 0ull;
+            if (key0 + kMine > span.hi) seen &= span.hi > key0 ? ((Bits)1 << (span.hi - key0)) - 1 : 0;
 #pragma unroll
-            for (int k = 0; k < kKeys; ++k)
+            for (int k = 0; k < kMine; ++k)
                 if (!(seen >> k & 1)) s[k] = -INFINITY;
         }
 #pragma unroll
@@ -273,11 +279,11 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
 #pragma unroll
         for (int k = 0; k < 4; ++k) part[k] = fmaxf(s[k], s[k + 4]);
 #pragma unroll
-        for (int k = 8; k < kKeys; k += 8)
+        for (int k = 8; k < kMine; k += 8)
 #pragma unroll
             for (int i = 0; i < 4; ++i) part[i] = largest_of(part[i], s[k + i], s[k + i + 4]);
         float most = fmaxf(largest_of(part[0], part[1], part[2]), part[3]);
-        most = most == -INFINITY ? most : most * scale;      // (hidden is -inf whatever the scale, 0 too)
+        most = most == -INFINITY ? most : most * scale;  // (hidden is -inf whatever the scale, 0 too)
         const bool renew = most > top + 8.0f || (top == -INFINITY && most > -INFINITY);
         if (__any_sync(~0u, renew)) {
             const float is = fmaxf(top, most), back = top == is ? 1.0f : power2(top - is);
@@ -302,9 +308,10 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         // (two at a time where there is nothing to it but arithmetic)
         const uint64_t scales = two_of(scale, scale), bases = two_of(-base, -base);
         uint64_t sums2 = two_of(0, 0);
+        const uint32_t to = at + 16 * keys_part;
         auto weigh = [&](auto masked) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kMine / 16; ++c) {
                 uint32_t w[8], rest[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -322,12 +329,18 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
                         rest[k] = pack_half(a - f.x, b - f.y);
                     }
                 }
-                store_columns(at + 8 * c, w);
-                if (kRest) store_columns(at + 32 + 8 * c, rest);
+                store_columns(to + 8 * c, w);
+                if (kRest) store_columns(to + 32 + 8 * c, rest);
             }
         };
         if (whole) weigh(std::false_type{});
         else weigh(std::true_type{});
+        if (TWICE) {
+            // (of the other keys the row's other place has the weights)
+            const uint32_t zeros[16] = {}, others = at + 16 * (1 - keys_part);
+            store_columns(others, zeros);
+            if (kRest) store_columns(others + 32, zeros);
+        }
         float even, odd;
         halves_of(sums2, even, odd);
         sum += even + odd;
@@ -340,37 +353,61 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     if (ok && span.n > 0) ok = summed(span.n - 1);
     if (!ok) *m.failed = 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // both sets' sums, brought to the joint maximum; set 1's by way of the tiles' place where they are other lanes'
+    // both sets' sums, brought to the joint maximum; then those of a row's two places, by way of the tiles' place
     // (all products have run)
     auto part_place = [&](int r, int o) { return reinterpret_cast<float4 *>(m.stages + r * D * 4 + ((o & ~7) | ((o ^ r) & 7)) * 16); };
-    float *other = m.states + row * 4;
-    if (set == 1 && (any || !narrow)) {
-        other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
-        if (narrow && span.n > 1) {
-#pragma unroll
-            for (int c = 0; c < D; c += 32) {
-                uint32_t v[32];
-                load_columns(v, sums + c);
-                loaded(v);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    *part_place(kTreeRows / 2 + row, c / 4 + k) = make_float4(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]),
-                                                                              __uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3]));
-            }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        }
-    }
+    float *other = m.states + (32 * quarter + lane) * 4;
+    if (set == 1) other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
     asm volatile("bar.sync 1, 256;" ::: "memory");
     if (set == 1) return;
     const bool lost = !ok || *m.failed;
     const float nan = __int_as_float(0x7fc00000);
+    // (what saw nothing has no maximum, or what saw NaN)
+    auto factor = [](float top, float sum, float best) { return top == -INFINITY ? (sum == 0 ? 0.0f : sum) : power2(top - best); };
+    auto join_sums = [](float a, float fa, float b, float fb) { return (fa == 0 ? 0.0f : a * fa) + (fb == 0 ? 0.0f : b * fb); };
     const float best = fmaxf(top, other[0]);
-    // (a set without a maximum saw nothing, or NaN)
-    const float f0 = span.n < 1 ? 0.0f : top == -INFINITY ? (sum == 0 ? 0.0f : sum) : power2(top - best);
-    const float f1 = span.n < 2 ? 0.0f : other[0] == -INFINITY ? (other[1] == 0 ? 0.0f : other[1]) : power2(other[0] - best);
-    sum = (f0 == 0 ? 0.0f : sum * f0) + (f1 == 0 ? 0.0f : other[1] * f1);
+    const float f0 = span.n < 1 ? 0.0f : factor(top, sum, best), f1 = span.n < 2 ? 0.0f : factor(other[0], other[1], best);
+    sum = join_sums(sum, f0, other[1], f1);
     spoilt |= __float_as_uint(other[2]);
     top = best;
+    // elements c and on, 0, 4, 1, 5, 2, 6, 3, 7 of each eight put right
+    auto both_sets = [&](int c, float (&x)[32]) {
+        auto take = [&](uint32_t from, float f) {
+            uint32_t v[32];
+            load_columns(v, from + c);
+            loaded(v);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+                float &to = x[k / 8 * 8 + k % 8 / 2 + k % 2 * 4];
+                to = f == 0 ? to : __fmaf_rn(__uint_as_float(v[k]), f, to);
+            }
+        };
+        if (span.n > 0) take(sums, f0);
+        if (span.n > 1) take(sums + 128, f1);
+    };
+    float g0 = 1, g1 = 0;
+    if (TWICE) {
+        if (keys_part && some) {
+            other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                float x[32] = {};
+                both_sets(c, x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) *part_place(kTreeRows / 2 + row, c / 4 + k) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+            }
+        }
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+        if (!keys_part && some) {
+            const float *theirs = other + kTreeRows / 2 * 4;
+            const float most = fmaxf(top, theirs[0]);
+            g0 = factor(top, sum, most), g1 = factor(theirs[0], theirs[1], most);
+            sum = join_sums(sum, g0, theirs[1], g1);
+            spoilt |= __float_as_uint(theirs[2]);
+            top = most;
+        }
+    }
+    const bool any = some && !keys_part;
     const float inverse = sum > 0 ? 1.0f / sum : 0.0f;
     // rows as whole lines, a lane an octet, by way of the tiles' place (all products have run)
     constexpr int kOctets = D / 8, kAtOnce = 32 / kOctets, kLoads = 32 / kAtOnce;
@@ -380,33 +417,16 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     if (any) {
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
-            // elements 0, 4, 1, 5, 2, 6, 3, 7
             float x[32] = {};
-            auto take = [&](const uint32_t (&v)[32], float f) {
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    float &to = x[k / 8 * 8 + k % 8 / 2 + k % 2 * 4];
-                    to = f == 0 ? to : __fmaf_rn(__uint_as_float(v[k]), f, to);
-                }
-            };
-            uint32_t v[32];
-            if (span.n > 0) {
-                load_columns(v, sums + c);
-                loaded(v);
-                take(v, f0);
-            }
-            if (span.n > 1 && narrow) {
+            both_sets(c, x);
+            if (TWICE) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const float4 four = *part_place(kTreeRows / 2 + row, c / 4 + k);
-                    v[4 * k] = __float_as_uint(four.x), v[4 * k + 1] = __float_as_uint(four.y);
-                    v[4 * k + 2] = __float_as_uint(four.z), v[4 * k + 3] = __float_as_uint(four.w);
+                    const float theirs[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[4 * k + i] = join_sums(x[4 * k + i], g0, theirs[i], g1);
                 }
-                take(v, f1);
-            } else if (span.n > 1) {
-                load_columns(v, sums + 128 + c);
-                loaded(v);
-                take(v, f1);
             }
             const bool none = lost || (spoilt >> (c / E2_CACHE_GROUP) & 1);
             if (p.splits == 1) {
@@ -436,7 +456,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
             if (at >= 0) reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + at)[o] = *place(row - lane + r, o);
         }
     } else if (join) {
-        other[0] = top, other[1] = lost ? nan : sum;
+        if (!keys_part) other[0] = top, other[1] = lost ? nan : sum;
     } else if (any) {
         const int64_t mine = live ? ((token * p.q_heads + head) * p.splits + blockIdx.z) * (D + 2) : -1;
         if (live) p.parts[mine + D] = top, p.parts[mine + D + 1] = lost ? nan : sum;
@@ -454,11 +474,11 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
 }
 
 // Eight warps: the parts of a cluster's blocks, in their order.  Block `rank` has every splits-th row.
-template <class T, int D>
+template <class T, int D, bool TWICE>
 __device__ __forceinline__ void join_parts(const AttendParams &p, const Slab &slab, const Shared<D> &m, int kv, int warp, int lane)
 {
     const int rank = blockIdx.z;
-    for (int r = warp * p.splits + rank; r < kTreeRows && slab.live(r); r += 8 * p.splits) {
+    for (int r = warp * p.splits + rank; r < kRowsOf<TWICE> && slab.live(r); r += 8 * p.splits) {
         const uint32_t state = smem_addr(m.states + r * 4), part = smem_addr(m.stages + r * D * 4 + ((lane & ~7) | ((lane ^ r) & 7)) * 16);
         float tops[kTreeCluster], weights[kTreeCluster], best = -INFINITY;
         float4 x[kTreeCluster];
@@ -494,57 +514,90 @@ __device__ __forceinline__ void join_parts(const AttendParams &p, const Slab &sl
 // A tile's runs of keys that lie side by side: one, or two or four where pages are smaller.
 __device__ __forceinline__ int runs_of(const AttendParams &p) { return p.page_shift >= 6 ? 1 : 64 >> p.page_shift; }
 
-// A warp for keys (which 0) and one for values: tiles as they are cached, kRawStages ahead.  Lane 2 w copies the codes
-// of run w, the next one its scales; pages are looked up for 32 runs at a time, a lane each, and 32 ahead.  (A copy
-// takes some 250 cycles to issue: one warp for all four of a tile was what bound a tile.)
-template <int D> __device__ __forceinline__ void copy(const AttendParams &p, const Span &span, const Shared<D> &m, int request, int kv, int which, int lane)
+// A warp for keys (which 0) and one for values: tiles as they are cached, kRawStages ahead, two at a time: what such a warp
+// needs for a tile, one instruction after the other, is what bounds a tile.  So one lane, which the compiler knows to be one, asks
+// for all copies, and pages are looked up for 32 runs at a time, a lane each, and 32 ahead.
+template <int D, int RUNS>
+__device__ __forceinline__ void copy_runs(const AttendParams &p, const Span &span, const Shared<D> &m, int request, int kv, int which, int lane)
 {
     using Sh = TreeShared<D>;
-    constexpr int GR = D / E2_CACHE_GROUP;
-    const int runs = runs_of(p), keys = kKeys / runs, page_mask = (1 << p.page_shift) - 1, w = lane / 2, scales = lane % 2;
-    const int groups = keys / 16;                            // of 16 keys, in a run
+    constexpr int GR = D / E2_CACHE_GROUP, kRun = kKeys / RUNS;
+    constexpr uint32_t kCodeBytes = kRun * (D / 2), kScaleBytes = kRun * (GR * 4);
+    static_assert(kRawStages % 2 == 0 && kCodeBytes == 8 * kScaleBytes, "tiles by twos; a run's scales an eighth of its codes");
+    const int page_mask = (1 << p.page_shift) - 1;
     const int32_t *table = p.table + request * p.table_stride;
-    const uint8_t *array = scales ? reinterpret_cast<const uint8_t *>(p.scales[which]) : p.codes[which];
-    const int of_key = scales ? GR * 4 : D / 2, bytes = keys * of_key;
-    const uint32_t to = smem_addr(m.raw) + (scales ? 8 * Sh::kCodes + which * 4 * Sh::kScales : which * 4 * Sh::kCodes) + w * bytes;
-    auto look_up = [&](int run) {
-        const int64_t key = (int64_t)span.first * kKeys + (int64_t)run * keys;
-        return run < span.n * runs && key < span.hi ? table[key >> p.page_shift] : -1;
+    const uint8_t *codes = p.codes[which], *scales = reinterpret_cast<const uint8_t *>(p.scales[which]);
+    const uint32_t to_codes = smem_addr(m.raw) + which * 4 * Sh::kCodes, to_scales = smem_addr(m.raw) + 8 * Sh::kCodes + which * 4 * Sh::kScales;
+    auto key_of = [&](int run) { return (int64_t)span.first * kKeys + (int64_t)run * kRun; };
+    // (what is loaded here is not touched before its turn)
+    auto look_up = [&](int run) { return table[min(key_of(run), (int64_t)span.hi - 1) >> p.page_shift]; };
+    // a run's place among the codes, in bytes; -1 where it is not there
+    auto place_of = [&](int run, int page) {
+        const int64_t key = key_of(run);
+        if (key >= span.hi || page < 0 || page >= p.pages) return (int64_t)-1;
+        return ((((int64_t)page * p.kv_heads + kv) << p.page_shift) + (key & page_mask)) * (D / 2);
+    };
+    auto bring = [](uint32_t to, const uint8_t *from, uint32_t bytes, uint32_t barrier) {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes),
+                     "r"(barrier)
+                     : "memory");
     };
     bool ok = true;
-    int stage = 0, phase = 1, pages = look_up(lane), next = look_up(32 + lane);
-    for (int j = 0; j < span.n; ++j) {
-        const int run = (j * runs + w) % 32, page = __shfl_sync(~0u, pages, run);
-        if ((j + 1) * runs % 32 == 0) {
-            pages = next;
-            next = look_up((j + 1) * runs + 32 + lane);
-        }
-        ok = warp_wait(m.taken + 8 * stage, phase, lane);
-        if (!ok) break;
-        if (w < runs) {
-            const bool there = page >= 0 && page < p.pages;
-            if (lane % 2 == 0 && which == 0)
-                for (int i = 0; i < groups; ++i) m.raw_there[stage][w * groups + i] = there;
-            barrier_expect(m.copied + 8 * stage, there ? bytes : 0);
-            if (there) {
-                const int64_t vec = (((int64_t)page * p.kv_heads + kv) << p.page_shift) + (((span.first + j) * kKeys + w * keys) & page_mask);
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + stage * Sh::kRaw),
-                             "l"(array + vec * of_key), "r"(bytes), "r"(m.copied + 8 * stage)
-                             : "memory");
+    int issued = 0;
+    if (span.n > 0) {
+        int64_t places = place_of(lane, look_up(lane));
+        int next = look_up(32 + lane), stage = 0, phase = 1;
+        for (int run = 0; issued < span.n; run += 2 * RUNS) {
+            const bool two = issued + 1 < span.n;
+            ok = warp_wait(m.taken + 8 * (stage + (two ? lane % 2 : 0)), phase, lane);
+            if (!ok) break;
+            int64_t at[2 * RUNS];
+#pragma unroll
+            for (int i = 0; i < 2 * RUNS; ++i) at[i] = __shfl_sync(~0u, places, run % 32 + i);
+            if (elected()) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (t && !two) break;
+                    const uint32_t barrier = m.copied + 8 * (stage + t);
+                    uint32_t bytes = 0, there = 0;
+#pragma unroll
+                    for (int w = 0; w < RUNS; ++w) {
+                        bytes += at[t * RUNS + w] < 0 ? 0 : kCodeBytes + kScaleBytes;
+                        there |= at[t * RUNS + w] < 0 ? 0 : (RUNS == 1 ? 0x01010101u : RUNS == 2 ? 0x0101u << (16 * w) : 1u << (8 * w));
+                    }
+                    if (which == 0) *reinterpret_cast<uint32_t *>(m.raw_there[stage + t]) = there;
+                    barrier_expect(barrier, bytes);
+#pragma unroll
+                    for (int w = 0; w < RUNS; ++w) {
+                        const int64_t from = at[t * RUNS + w];
+                        if (from < 0) continue;
+                        bring(to_codes + (stage + t) * Sh::kRaw + w * kCodeBytes, codes + from, kCodeBytes, barrier);
+                        bring(to_scales + (stage + t) * Sh::kRaw + w * kScaleBytes, scales + from / 8, kScaleBytes, barrier);
+                    }
+                }
             }
+            __syncwarp();
+            issued += two ? 2 : 1;
+            if ((run + 2 * RUNS) % 32 == 0) {
+                places = place_of(run + 2 * RUNS + lane, next);
+                next = look_up(run + 2 * RUNS + 32 + lane);
+            }
+            stage += 2;
+            if (stage == kRawStages) stage = 0, phase ^= 1;
         }
-        __syncwarp();
-        if (++stage == kRawStages) stage = 0, phase ^= 1;
     }
     // (no copy is on its way any more when the block ends: all have been taken, or have come)
-    for (int i = 0; i < kRawStages && ok; ++i) {
-        ok = warp_wait(m.taken + 8 * stage, phase, lane);
-        if (++stage == kRawStages) stage = 0, phase ^= 1;
+    for (int j = max(issued - kRawStages, 0); j < issued; ++j) {
+        if (ok) ok = warp_wait(m.taken + 8 * (j % kRawStages), j / kRawStages & 1, lane);
+        if (!ok) barrier_wait(m.copied + 8 * (j % kRawStages), j / kRawStages & 1);
     }
-    if (!ok) {
-        *m.failed = 1;
-        for (int i = 0; i < kRawStages; ++i) barrier_wait(m.copied + 8 * i, phase ^ (i < stage ? 0 : 1));
-    }
+    if (!ok) *m.failed = 1;
+}
+template <int D> __device__ __forceinline__ void copy(const AttendParams &p, const Span &span, const Shared<D> &m, int request, int kv, int which, int lane)
+{
+    if (runs_of(p) == 1) copy_runs<D, 1>(p, span, m, request, kv, which, lane);
+    else if (runs_of(p) == 2) copy_runs<D, 2>(p, span, m, request, kv, which, lane);
+    else copy_runs<D, 4>(p, span, m, request, kv, which, lane);
 }
 
 // Warp w of four of a set, which has every third tile: 16 of its 64 keys, and values, dequantised.  A lane
@@ -650,7 +703,7 @@ template <int D> __device__ __forceinline__ void unpack(const Span &span, const 
     if (!ok) *m.failed = 1;
 }
 
-template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const AttendParams p)
+template <class T, int D, bool TWICE> __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const AttendParams p)
 {
     using Sh = TreeShared<D>;
     extern __shared__ uint8_t dynamic[];
@@ -666,7 +719,8 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     wait_before();
     allow_next();
     const Rows rows(p, request);
-    const int64_t blocks = (rows.count + kTreeRows - 1) / kTreeRows;
+    constexpr int kRows = kRowsOf<TWICE>;
+    const int64_t blocks = (rows.count + kRows - 1) / kRows;
     if (blocks <= blockIdx.y) return;
     const Tree tree(p, rows, ways);
     if (warp == 1) Tree::load(p, request, ways);
@@ -690,7 +744,7 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
         for (int i = 0; i < kStages; ++i) barrier_init(m.full + 8 * i, 4), barrier_init(m.empty + 8 * i, 1);
         for (int i = 0; i < kScores; ++i) barrier_init(m.scored + 8 * i, 1), barrier_init(m.weighed + 8 * i, 4), barrier_init(m.summed + 8 * i, 1);
         barrier_init(m.asked, 4);
-        for (int i = 0; i < kRawStages; ++i) barrier_init(m.copied + 8 * i, 4 * runs_of(p)), barrier_init(m.taken + 8 * i, 4);
+        for (int i = 0; i < kRawStages; ++i) barrier_init(m.copied + 8 * i, 2), barrier_init(m.taken + 8 * i, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     };
     if (threadIdx.x == 0) {
@@ -724,7 +778,7 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
-            const Span span(p, rows, tree, block);
+            const Span span(p, rows, tree, block, kRows);
             if (warp == 0) score<D>(m, span.n, lane);
             else if (warp == 1) sum_up<D, std::is_same<T, __half>::value>(m, span.n, lane);
             else copy<D>(p, span, m, request, kv, warp - 2, lane);
@@ -737,11 +791,11 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     } else if (warp < 12) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
-            const Span span(p, rows, tree, block);
-            weights<T, D>(p, span, m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane, join);
+            const Span span(p, rows, tree, block, kRows);
+            weights<T, D, TWICE>(p, span, m, tree, rows.skipped, kv, (warp - 4) / 4, warp % 4, lane, join);
             if (join) {
                 cluster_barrier();
-                join_parts<T, D>(p, span.slab, m, kv, warp - 4, lane);
+                join_parts<T, D, TWICE>(p, span.slab, m, kv, warp - 4, lane);
                 cluster_barrier();
             }
             meet(block + gridDim.y < blocks);
@@ -749,17 +803,17 @@ template <class T, int D> __global__ void __launch_bounds__(kThreads, 1) tree_ke
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         for (int64_t block = blockIdx.y; block < blocks; block += gridDim.y) {
-            unpack<D>(Span(p, rows, tree, block), m, (warp - 12) / 4, warp % 4, lane);
+            unpack<D>(Span(p, rows, tree, block, kRows), m, (warp - 12) / 4, warp % 4, lane);
             if (join) cluster_barrier(), cluster_barrier();
             meet(block + gridDim.y < blocks);
         }
     }
 }
 
-template <class T, int D> int launch_as(const AttendParams &p, int blocks, int pairs, int dev, cudaStream_t s)
+template <class T, int D, bool TWICE> int launch_as(const AttendParams &p, int blocks, int pairs, int dev, cudaStream_t s)
 {
     static std::atomic<uint64_t> ready{0};                   // devices that have the attribute set
-    auto kernel = tree_kernel<T, D>;
+    auto kernel = tree_kernel<T, D, TWICE>;
     const int smem = TreeShared<D>::kBytes > 120 * 1024 ? TreeShared<D>::kBytes : 120 * 1024;       // (tensor memory is for one block)
     if (!(ready.load(std::memory_order_relaxed) >> dev & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -783,11 +837,15 @@ template <class T, int D> int launch_as(const AttendParams &p, int blocks, int p
 
 }  // namespace
 
-int launch_tree(const AttendParams &p, int head_dim, bool half, int blocks, int pairs, int dev, cudaStream_t s)
+int launch_tree(const AttendParams &p, int head_dim, bool half, bool few, int blocks, int pairs, int dev, cudaStream_t s)
 {
-    if (head_dim == 64)
-        return half ? launch_as<__half, 64>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 64>(p, blocks, pairs, dev, s);
-    return half ? launch_as<__half, 128>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 128>(p, blocks, pairs, dev, s);
+    auto as = [&](auto twice) {
+        constexpr bool kTwice = decltype(twice)::value;
+        if (head_dim == 64)
+            return half ? launch_as<__half, 64, kTwice>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 64, kTwice>(p, blocks, pairs, dev, s);
+        return half ? launch_as<__half, 128, kTwice>(p, blocks, pairs, dev, s) : launch_as<__nv_bfloat16, 128, kTwice>(p, blocks, pairs, dev, s);
+    };
+    return few ? as(std::true_type{}) : as(std::false_type{});
 }
 
 }  // namespace e2ops
