@@ -176,6 +176,18 @@ def test_more_nodes_than_a_tree_holds(G):
     assert torch.isnan(out[64:]).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,told,ctx", [(1, 2, 700), (8, 5, 300), (8, 5, 3000), (8, 9, 300), (4, 16, 5000)])
+def test_more_nodes_and_keys_than_the_launch_was_told_of(G, told, ctx, D):
+    """max_new and max_len choose the launch; what the device's arrays say is what is done."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([ctx, 70], [64, 37], 2, G, D, 16, seed=told)
+    parents = trees([64, 37])
+    out = ops.cache_attend_tree(cache, q, parents, table, lens, starts, max_new=told, max_len=ctx // 2)
+    want, bound, _ = DR.attend_tree(cache, q, parents, table, lens, starts, D ** -0.5, 0)
+    R.close(out, want, bound)
+
+
 @pytest.mark.parametrize("G", [2, 16])
 def test_starts_and_lengths_out_of_range(G):
     """Queries that are not tokens of q are left out; trees longer than what is cached see less; rows behind stay."""
