@@ -276,8 +276,23 @@ template <class T> struct Walk {
         const float2 *tops = m.tops;
         const float f = heat.h * 1.44269504f;
         int stage = 0;
+        // (a unit each, and all in the ring: two nodes side by side)
+        const bool side_by_side = wide && end - first == kUnit && count > 1;
+        if (side_by_side) {
+            copy_wait<0>();
+#pragma unroll 2
+            for (int g = 0; g < count; ++g) {
+                const float ca = tops[g].x * f, cb = tops[g].y * f;
+                const Lot e = from_ring(g, 0), d = from_ring(g, 1);
+                float sa[2] = {0, 0}, sb[2] = {0, 0};
+#pragma unroll
+                for (int j = 0; j < kEach; ++j)
+                    sa[j % 2] += power2(__fmaf_rn(element(e, j), f, -ca)), sb[j % 2] += power2(__fmaf_rn(element(d, j), f, -cb));
+                m.lane_sums[warp][g][lane] = make_float2(sa[0] + sa[1], both >> g & 1 ? sb[0] + sb[1] : 0.0f);
+            }
+        }
 #pragma unroll 1
-        for (int g = 0; g < count; ++g) {
+        for (int g = side_by_side ? count : 0; g < count; ++g) {
             const bool two = both >> g & 1;
             const float ca = tops[g].x * f, cb = tops[g].y * f;
             const T *u = row_of(p.logits, p.logits_stride, m.group[g]), *v = two ? row_of(p.draft, p.draft_stride, m.group[g]) : u;
