@@ -561,8 +561,9 @@ constexpr int kClusterUnits = 8;
 
 // Trees' rows are by 128 from so many on; from nine on where the blocks run at once and all requests' keys, times the
 // KV heads, are so few.  Measured, us (128 elements, bf16; by eight or sixteen / by 128): 24 rows of 8 requests x 8 KV
-// heads x 2,304 keys 40 / 22, 16 rows 29 / 21, 8 rows 19 / 21; 16 rows of 150 keys 19 / 11, 9,000 keys 54 / 52, 65,000
-// keys 222 / 283; 16 rows of 32 x 8 x 517 keys 25 / 29; 8 rows of one request x 150 keys 11 / 11.
+// heads x 2,304 keys 40 / 22, 16 rows 31 / 22, 8 rows 18 / 22; 16 rows of 150 keys 20 / 13, 9,000 keys 54 / 51 (fp16 57),
+// 65,000 keys 221 / 268 (fp16 307); 16 rows of 32 x 8 x 517 keys 29 / 33, x 9,000 204 / 173 (fp16 201); 8 rows of one
+// request x 150 keys 11 / 13.
 constexpr int kTree = 17, kTreeKeys = 600000;
 // A block of trees' rows takes the time of so many tiles more, for its start and its end; so many the second kernel.
 constexpr int kTreeExtra = 12, kTreeJoin = 10;

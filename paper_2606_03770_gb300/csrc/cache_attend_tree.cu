@@ -3,16 +3,19 @@
 // A block takes 128 rows (nodes times the query heads of a KV head) and walks over tiles of 64
 // keys.  A warp copies them, eight dequantise a tile (fp16, one rounding: 2^-11 of a value), one issues
 // S = q K^T, one O += P V, four make the weights, a thread a row.  Queries, weights and O are in tensor memory:
-// a tile's keys and values are all that the products read from shared memory.  Up to 64 rows lie in it twice, so that
-// all four schedulers have weights to make; a warp that has no rows makes none.
+// a tile's keys and values are all that the products read from shared memory.  Up to 64 rows lie in it twice (TWICE), the
+// first ones with the weights of a tile's first 32 keys and zeros, the others with those of the last, so that all eight warps
+// have weights to make; their sums are joined at the end.  A warp that has no rows makes none.
 // Even and odd tiles have weights' warps, maxima and sums of their own, joined at the end.
-// Bound by a tile's instructions (some 2,900 of a block's warps; 63% of issue slots) and the waits between its steps
-// (copied, unpacked, scored, weighed, summed: 100 to 400 cycles each, three to five tiles on their way).  Measured, us
-// (128 elements, bf16): 8 requests x 8 KV heads x 56 rows x 65,536 keys 300 (1,250 cycles a tile; the cache alone 89 at
-// the memory's rate), 2 x 8 x 1,024 rows x 16,384 keys 170 (806 TFLOP/s, 42% of the tensor cores' measured rate), 8 x 8 x
-// 128 rows x 2,304 keys 25, of which 6 before the first product and 4 after the last; 13 x 3 x 77 rows, window 128, 10.
+// Bound by a tile's instructions (65 to 69% of issue slots) and the waits between its steps (copied, unpacked, scored,
+// weighed, summed: 100 to 400 cycles each, three to five tiles on their way); half the unpacking would give 5%, half the
+// weights 0 to 4, half of either product 2.  Measured, us (128 elements, bf16): 8 requests x 8 KV heads x 56 rows x 65,536
+// keys 270 (1,110 cycles a tile; the cache alone 89 at the memory's rate), 2 x 8 x 1,024 rows x 16,384 keys 150 (912 TFLOP/s,
+// 48% of the tensor cores' measured rate), 8 x 8 x 128 rows x 2,304 keys 23.5, of which 6 before the first product and 4 after
+// the last; 13 x 3 x 77 rows, window 128, 9.6.
 // On the way: one set of weights' warps 400 for the first, copies by 16 keys 360, by one warp 320, eight warps that unpack
-// 315, a barrier polled by one lane for its warp twice as long.
+// 315, a barrier polled by one lane for its warp twice as long, copies of one tile after the other 304, both widths of
+// weights in one kernel 284, sixteen warps that unpack 274.
 // Elements of eight lie in the order that unpacking leaves (0, 4, 1, 5, 2, 6, 3, 7) in q, K and V,
 // and are put right in the output.  Weights go to fp16 times 2^7 (2^-11 each; fp16 outputs take the
 // rounding's rest in a second product).  A weight of 0 does not stop a NaN among the values, so

@@ -11,8 +11,8 @@ namespace {
 
 // Bound by latency where there are few requests: some five dependent steps a node (its rows, the block's sums, the
 // cluster's barrier, the decision), two microseconds; by the rows' bytes and, at a walk's end, by instructions where
-// there are many.  Measured, us: 1 request x 5 nodes of 32,000 tokens 19, 8 x 16 of 128,256 (bf16) 40, 64 x 8 of
-// 128,256 (fp32) 132, of which the levels of the longest walk 60 at 5 TB/s, then 30 for the sums in 45 bits (85% of
+// there are many.  Measured, us: 1 request x 5 nodes of 32,000 tokens 17, 8 x 16 of 128,256 (bf16) 40, 64 x 8 of
+// 128,256 (fp32) 135, of which the levels of the longest walk 60 at 5 TB/s, then 30 for the sums in 45 bits (85% of
 // issue slots, some 55 an element); 13 x 13 of 50,001 without the draft's rows 20.
 //
 // A cluster of blocks walks a request's tree, and all its warps take the same decisions.  Each
@@ -26,7 +26,8 @@ namespace {
 // The token after the last is found in the blocks' sums, the warps', those of an eighth of a
 // warp's run, of a lane's share of it, and then element by element.
 // Tried: 512 threads of 128 registers (spills went through the caches: 287 for 64 x 8), all parts read from their blocks by
-// every warp (5 us a pass), four likely nodes at once whatever the vocabulary (64 x 8 205, 8 x 16 40).
+// every warp (5 us a pass), four likely nodes at once whatever the vocabulary (64 x 8 205, 8 x 16 40), two elements in each
+// instruction of the 45-bit sums (64 x 8 145: half the independent chains, and spills), groups of six nodes (no faster for ways of two).
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMostCluster = 16;
 constexpr int kRing = 6144;                      // bytes of a warp's copies on their way
