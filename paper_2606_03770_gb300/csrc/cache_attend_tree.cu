@@ -392,7 +392,7 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     if (TWICE) {
         if (keys_part && some) {
             other[0] = top, other[1] = sum, other[2] = __uint_as_float(spoilt);
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 float x[32] = {};
                 both_sets(c, x);
@@ -418,7 +418,8 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
         return reinterpret_cast<uint4 *>(m.stages + o / 8 * kTreeRows * 128 + r * 128 + ((o % 8) ^ (r & 7)) * 16);
     };
     if (any) {
-#pragma unroll
+        // (one copy of the code: where it runs once, fetching it is what it costs)
+#pragma unroll (TWICE ? 1 : 2)
         for (int c = 0; c < D; c += 32) {
             float x[32] = {};
             both_sets(c, x);
