@@ -561,10 +561,10 @@ constexpr int kClusterUnits = 8;
 
 // Trees' rows are by 128 from so many on; from nine on where the blocks run at once and all requests' keys, times the
 // KV heads, are so few.  Measured, us (128 elements, bf16; by eight or sixteen / by 128): 24 rows of 8 requests x 8 KV
-// heads x 2,304 keys 40 / 22, 16 rows 31 / 22, 8 rows 18 / 22; 16 rows of 150 keys 20 / 13, 9,000 keys 54 / 51 (fp16 57),
-// 65,000 keys 221 / 268 (fp16 307); 16 rows of 32 x 8 x 517 keys 29 / 33, x 9,000 204 / 173 (fp16 201); 8 rows of one
-// request x 150 keys 11 / 13.
-constexpr int kTree = 17, kTreeKeys = 600000;
+// heads x 2,304 keys 40 / 20, 16 rows 31 / 20, 8 rows 18 / 20; 16 rows of 150 keys 20 / 11, 9,000 keys 54 / 48 (fp16 53),
+// 65,000 keys 221 / 258 (fp16 293), of 16 x 8 x 9,000 91 / 84 (fp16 94), of one request x 32 x 30,000 73 / 72 (fp16 81); of
+// more heads than multiprocessors, 48 x 8 x 2,304 71 / 86; 8 rows of one request x 8 x 150 11 / 10, x 2,304 11 / 14.
+constexpr int kTree = 17, kTreeKeys = 1200000, kTreeKeysHalf = 600000;         // (of bf16; of fp16, which has two products for sums)
 // A block of trees' rows takes the time of so many tiles more, for its start and its end; so many the second kernel.
 constexpr int kTreeExtra = 12, kTreeJoin = 10;
 
@@ -582,7 +582,7 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms, bool tree)
     const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
     f.nt = rows >= (tree ? kTree : kPrompt) ? 0 : rows <= 8 ? 1 : 2;
     const int64_t heads = (int64_t)a->batch * c->kv_heads;
-    if (tree && f.nt == 2 && heads <= sms && heads * a->max_len <= kTreeKeys) f.nt = 0;
+    if (tree && f.nt == 2 && heads <= sms && heads * a->max_len <= (a->dtype == E2_F16 ? kTreeKeysHalf : kTreeKeys)) f.nt = 0;
     const int at_once = f.nt ? 8 * f.nt : tree ? kTreeRows : kPromptRows;
     f.rows = (int)(rows < (1 << 18) ? rows : 1 << 18);
     const int64_t slabs = (rows + at_once - 1) / at_once;
