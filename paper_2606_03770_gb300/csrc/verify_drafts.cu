@@ -21,8 +21,9 @@ namespace {
 // that is clear by one part in 2^14 is taken; only what is not, and a walk's end, goes through 45 bits.
 // With p = w / Z, w = exp((x - max x) / T), and q likewise of the draft's row, after k rejections
 //   P = (p - A q)+ / B,  A_0 = 0, B_0 = 1, A_{k+1} = A_k + B_k, B_{k+1} = sum (p - A_{k+1} q)+,
-// as (P - q)+ is (p - A q - B q)+ / B.  Without the draft's rows a rejected token leaves P.  The first of these sums comes
-// out of the pass that gives Z: by the 32-bit sums it is known well enough which p are above q.
+// as (P - q)+ is (p - A q - B q)+ / B.  Without the draft's rows a rejected token leaves P: all children's are left out of
+// the sums and come to what is left one by one, as a difference would leave its rounding where nothing is.  The first of the
+// sums of (p - q)+ comes out of the pass that gives Z: by the 32-bit sums it is known well enough which p are above q.
 // The token after the last is found in the blocks' sums, the warps', those of an eighth of a
 // warp's run, of a lane's share of it, and then element by element.
 // Tried: 512 threads of 128 registers (spills went through the caches: 287 for 64 x 8), all parts read from their blocks by
@@ -63,6 +64,8 @@ struct Shared {
     int group[kGroup];                           // the nodes
     int32_t ids[E2_MAX_DRAFT], parents[E2_MAX_DRAFT];
     float uniforms[E2_MAX_DRAFT];
+    Two asked[E2_MAX_DRAFT], counted[E2_MAX_DRAFT];            // without the draft's rows: children's weights, alone and in sums
+    bool some[E2_MAX_DRAFT];
 };
 
 __device__ const PowerTable power_table = PowerTable();
@@ -368,12 +371,20 @@ template <class T> struct Walk {
         x_sum = sum.x, y_sum = sum.y;
     }
 
-    // The same run again, f(two elements of x, of y): a short loop, as f is long.
-    template <bool BOTH, class F> __device__ __forceinline__ void pairs(F f) const
+    // Whether a token is one of these nodes'.
+    __device__ __forceinline__ bool among(uint64_t nodes, int v) const
+    {
+        for (; nodes; nodes &= nodes - 1)
+            if (m.ids[__ffsll(nodes) - 1] == v) return true;
+        return false;
+    }
+    // The same run again, f(two elements of x, of y): a short loop, as f is long.  LEAVE: without the tokens of `out`'s nodes.
+    template <bool BOTH, bool LEAVE = false, class F> __device__ __forceinline__ void pairs(F f, uint64_t out = 0) const
     {
         constexpr int kStep = sizeof(T) / 2;                              // words of two elements
         const int units = (end - first) / kUnit, rest = end - first - units * kUnit;
         const bool kept = wide && units <= kStages;
+        const int leave = LEAVE && out ? m.ids[__ffsll(out) - 1] : -1;        // (a run has one at most, as a rule)
         Lot a, b;
         if (units > 0 && !kept) {
             a = from_row(x, first);
@@ -401,6 +412,13 @@ template <class T> struct Walk {
                         const int i = at + 64 * k + 32 * e + lane;
                         c[e] = i < end ? to_float(x[i]) : -INFINITY;
                         if (BOTH) d[e] = i < end ? to_float(y[i]) : -INFINITY;
+                    }
+                }
+                if (LEAVE && out) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int i = at + (wide && unit < units ? kEach * lane + 2 * k + e : 64 * k + 32 * e + lane);
+                        if (i == leave || among(out & (out - 1), i)) c[e] = -INFINITY;
                     }
                 }
                 f(c, d);
@@ -464,11 +482,16 @@ template <class T> struct Walk {
         __syncthreads();
     }
 
-    // Sums by runs and whole: of x's weights, and of y's (LESS: of x's less y's share instead).
-    template <bool BOTH, bool LESS> __device__ __forceinline__ Two sums(const Weigher of_x, const Weigher of_y, Two &q)
+    // Sums by runs and whole: of x's weights, and of y's (LESS: of x's less y's share instead); x's without the tokens
+    // of `out`'s nodes.
+    template <bool BOTH, bool LESS> __device__ __forceinline__ Two sums(const Weigher of_x, const Weigher of_y, Two &q, uint64_t out = 0)
     {
         LongSum a, b;
-        pairs<BOTH || LESS>([&](const float (&u)[2], const float (&v)[2]) {
+        if (out) {
+            auto mine = [&](int c) { return __ballot_sync(~0u, out >> c & 1 && m.ids[c] >= first && m.ids[c] < end); };
+            out = mine(lane) | (uint64_t)mine(lane + 32) << 32;
+        }
+        pairs<BOTH || LESS, !BOTH && !LESS>([&](const float (&u)[2], const float (&v)[2]) {
             Two w[2], d[2];
             of_x.of(u, m.table, w);
             if (BOTH || LESS) of_y.of(v, LESS ? m.shared_table : m.table, d);
@@ -477,7 +500,7 @@ template <class T> struct Walk {
                 a.add(LESS ? less_of(w[j], d[j]) : w[j]);
                 if (BOTH) b.add(d[j]);
             }
-        });
+        }, out);
         Part mine{a.value(), b.value(), 0, 0, 0, 0};
         exchange(mine, [&](int k) {
             mine.p = mine.p + shuffle_xor(mine.p, k);
@@ -523,17 +546,19 @@ template <class T> struct Walk {
         return mine.p + mine.p_more;
     }
     // After it: run and block of (x - share y)+, and its sum; false where the border's part of it may be above 2^-37.
+    // What is so little of x that it may be all rounding is nothing, so that whoever has something has an element with
+    // something (the sums and weights are off by 2^-43; a block that has something has a run that does).
     __device__ __forceinline__ bool take_split(const Two &share, float near, Two &sum)
     {
-        auto of = [&](const Two &x, const Two &y) {
+        auto of = [&](const Two &x, const Two &y, float least) {
             const Two d = x - share * y;
-            return d.h > 0 ? d : Two{0, 0};
+            return d.h > least * x.h ? d : Two{0, 0};
         };
-        sum = warp_sum(lane < p.split ? of(block, block_q) : Two{0, 0});
+        sum = warp_sum(lane < p.split ? of(block, block_q, 0x1p-39f) : Two{0, 0});
         // (2^-22: what the comparisons were rounded by)
         const float off = fabsf(__fdiv_rn((share - Two{near, 0}).h, near)) + 0x1p-22f;
         if (!(off < 0x1p-20f && off * border <= 0x1p-37f * sum.h)) return false;
-        run = of(run, run_q), block = of(block, block_q);
+        run = of(run, run_q, 0x1p-40f), block = of(block, block_q, 0x1p-39f);
         return true;
     }
 
@@ -590,7 +615,8 @@ template <class T> struct Walk {
     }
 };
 
-template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyParams p)
+// (two kernels, as one for rows with and without the draft's keeps more than its registers)
+template <class T, bool DRAFT> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyParams p)
 {
     __shared__ Shared m;
     const int request = blockIdx.x / p.split;
@@ -623,7 +649,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
     auto rows_at = [&](const void *rows, int64_t stride) {
         return reinterpret_cast<uintptr_t>(rows) | (start + n > 1 ? (uintptr_t)stride * sizeof(T) : 0);
     };
-    walk.wide = (rows_at(p.logits, p.logits_stride) | (p.draft ? rows_at(p.draft, p.draft_stride) : 0)) % 16 == 0;
+    walk.wide = (rows_at(p.logits, p.logits_stride) | (DRAFT ? rows_at(p.draft, p.draft_stride) : 0)) % 16 == 0;
     // (bit c: node c is a child)
     auto children_of = [&](int node) {
         return __ballot_sync(~0u, parent0 == node) | (uint64_t)__ballot_sync(~0u, parent1 == node) << 32;
@@ -633,7 +659,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
     // them all: for small vocabularies, where a pass is latency, one does for up to four nodes.  (For larger ones, or
     // without the draft's rows, what is not accepted costs more: 8 x 16 x 128,256 40 us for 37.)
     const int runs = kWarps * p.split, run_units = ((p.vocab + Walk<T>::kUnit - 1) / Walk<T>::kUnit + runs - 1) / runs;
-    const int at_once = p.draft && walk.wide ? max(min(kGroup, Walk<T>::kStages / run_units), 1) : 1;
+    const int at_once = DRAFT && walk.wide ? max(min(kGroup, Walk<T>::kStages / run_units), 1) : 1;
     int place = 0, count = 0;                             // of the node in its group; the group's nodes
     float x_sums = 0, y_sums = 0, child_value = 0;        // lane g kWarps: node g's; and the one after it: its first child's logits
 
@@ -645,7 +671,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
     while (n > 0 && (greedy || heated)) {
         walk.at_node(here);
         const uint64_t children = children_of(here);
-        const bool both = p.draft && children && heated;
+        const bool both = DRAFT && children && heated;
         int accepted = -1, first;
         if (greedy) {
             if (!walk.tops(false, first)) break;
@@ -667,7 +693,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                 __syncthreads();
                 for (uint64_t below = children;; below = children_of(node)) {
                     if (threadIdx.x == 0) m.group[count] = node;
-                    if (p.draft && below) twos |= 1u << count;
+                    if (DRAFT && below) twos |= 1u << count;
                     if (walk.lane / kWarps == count) my_node = node, my_child = below ? first_of(below) : -1;
                     if (++count == at_once || !below) break;
                     node = first_of(below);
@@ -675,7 +701,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                 // (the first children's logits are asked for now, looked at later)
                 T value = from_float<T>(-INFINITY);
                 const int v = my_child >= 0 ? m.ids[my_child] : -1;
-                if (inside(v) && (walk.lane % kWarps == 0 || (walk.lane % kWarps == 1 && p.draft)))
+                if (inside(v) && (walk.lane % kWarps == 0 || (walk.lane % kWarps == 1 && DRAFT)))
                     value = walk.lane % kWarps ? walk.row_of(p.draft, p.draft_stride, my_node)[v] : walk.row_of(p.logits, p.logits_stride, my_node)[v];
                 __syncthreads();
                 walk.estimate(count, twos, x_sums, y_sums);
@@ -691,7 +717,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                 if (!walk.tops(both, first)) break;
             } else if (children) {
                 const float f = walk.heat.h * 1.44269504f, cx = walk.x_top * f, cy = walk.y_top * f;
-                if (p.draft) {
+                if (DRAFT) {
                     const float w = power2(__fmaf_rn(first_x, f, -cx)) * y_sum, u = m.uniforms[child0];
                     const float asked = u * power2(__fmaf_rn(first_y, f, -cy)) * x_sum;
                     // (numbers that 32 bits do not hold are not clear)
@@ -725,28 +751,55 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                 const float wy = of_y.of(walk.y_top, m.table).h * y_sum * power2(__fmaf_rn(walk.x_top, f, -(walk.x_top * f)));
                 near = __fdiv_rn(wx, wy);
             }
+            // without the draft's rows: the children whose tokens are some, a thread each (its logit is asked for now)
+            uint64_t drafted = 0;
+            T value = from_float<T>(-INFINITY);
+            if (!DRAFT && children) {
+                const int a = walk.lane, b = walk.lane + 32, c = threadIdx.x;
+                drafted = __ballot_sync(~0u, children >> a & 1 && inside(m.ids[a])) |
+                          (uint64_t)__ballot_sync(~0u, children >> b & 1 && inside(m.ids[b])) << 32;
+                if (c < E2_MAX_DRAFT && drafted >> c & 1) value = walk.x[m.ids[c]];
+            }
             const Two all = near > 0 ? walk.split(of_x, of_y, near, q)
                             : both   ? walk.template sums<true, false>(of_x, of_y, q)
-                                     : walk.template sums<false, false>(of_x, of_x, q);
+                                     : walk.template sums<false, false>(of_x, of_x, q, drafted);
             const bool parted = near > 0;
-            Two left = all;                               // (without the draft's rows)
+            // what P has: what is no child's, and the children's tokens that are not lost (bits k: this lane's nodes lane + 32 k)
+            auto left_of = [&](unsigned out) {
+                return all + warp_sum((out & 1 ? none : m.counted[walk.lane]) + (out & 2 ? none : m.counted[walk.lane + 32]));
+            };
+            unsigned out = 0;
+            Two left = all;
+            if (drafted) {
+                const int c = threadIdx.x;
+                if (c < E2_MAX_DRAFT) {
+                    Two w = none, in_sums = none;
+                    bool some = false;
+                    if (drafted >> c & 1) {
+                        int e;
+                        some = of_x.wide(to_float(value), m.table, w, e);
+                        w = scaled(w, some ? e : -127);
+                        // (a token of several children is in the sums once)
+                        if (!walk.among(drafted & ((1ull << c) - 1), m.ids[c])) in_sums = of_x.of(to_float(value), m.table);
+                    }
+                    m.asked[c] = w, m.counted[c] = in_sums, m.some[c] = some;
+                }
+                __syncthreads();
+                left = left_of(out);
+            }
             uint64_t lost = 0;                            // rejected children whose tokens P has lost
             bool less = false;
-            auto gone = [&](int v) {
-                for (uint64_t r = lost; r; r &= r - 1)
-                    if (m.ids[first_of(r)] == v) return true;
-                return false;
-            };
+            auto gone = [&](int v) { return walk.among(lost, v); };
             for (uint64_t set = children; set; set &= set - 1) {
                 const int c = first_of(set), v = m.ids[c];
                 const bool in = inside(v);
                 const float u = m.uniforms[c];
-                // its weight, however small
-                Two w = none, wq = none;
-                int e = 0, eq = 0;
-                const bool known = c == first_of(children);
-                const bool some = in && of_x.wide(known ? first_x : to_float(walk.x[v]), m.table, w, e);
-                if (p.draft) {
+                if (DRAFT) {
+                    // its weight, however small
+                    Two w = none, wq = none;
+                    int e = 0, eq = 0;
+                    const bool known = c == first_of(children);
+                    const bool some = in && of_x.wide(known ? first_x : to_float(walk.x[v]), m.table, w, e);
                     // u q(v) < P(v), times Z_p Z_q B and a power of two
                     const bool some_q = in && of_y.wide(known ? first_y : to_float(walk.y[v]), m.table, wq, eq);
                     const int most = some && some_q ? max(e, eq) : some ? e : eq;
@@ -775,24 +828,23 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
                         walk.set_share(A * all / q);
                     }
                 } else if (in && !gone(v)) {
-                    w = scaled(w, some ? e : -127);
-                    if ((u == 0 && some) || Two{u, 0} * left < w) {
+                    const Two w = m.asked[c];
+                    if ((u == 0 && m.some[c]) || Two{u, 0} * left < w) {
                         accepted = c;
                         break;
                     }
-                    const Two rest = left - w;
-                    if (some && rest.h > kNothing * left.h) {
-                        left = rest;
-                        lost |= 1ull << c;
-                        // its run loses it too, and its block
-                        auto lose = [&](Two &sum) {
-                            sum = sum - w;
-                            if (!(sum.h > 0)) sum = none;
-                        };
-                        if (v >= walk.first && v < walk.end) lose(walk.run);
-                        const int owner = walk.lane % p.split;
-                        if (v >= walk.run_start(owner * kWarps) && v < walk.run_start((owner + 1) * kWarps)) lose(walk.block);
-                    }
+                    const unsigned more = out | (m.ids[walk.lane] == v) | (m.ids[walk.lane + 32] == v) << 1;
+                    const Two rest = left_of(more);
+                    if (m.some[c] && rest.h > kNothing * left.h) left = rest, out = more, lost |= 1ull << c;
+                }
+            }
+            if (accepted < 0) {
+                // the children's tokens that P has kept, in their runs and blocks
+                for (uint64_t set = drafted; set; set &= set - 1) {
+                    const int c = first_of(set), v = m.ids[c], owner = walk.lane % p.split;
+                    if (gone(v)) continue;
+                    if (v >= walk.first && v < walk.end) walk.run = walk.run + m.counted[c];
+                    if (v >= walk.run_start(owner * kWarps) && v < walk.run_start((owner + 1) * kWarps)) walk.block = walk.block + m.counted[c];
                 }
             }
             if (accepted < 0) knows = walk.find(m.uniforms[0], less, of_x, of_y, gone, token) && walk.lane == 0;
@@ -812,7 +864,7 @@ template <class T> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(
 }
 
 // How many clusters of 2^i blocks run at once.
-template <class T> int clusters_of(int i, int dev)
+template <class T, bool DRAFT> int clusters_of(int i, int dev)
 {
     static std::atomic<int> known[64][5];                    // one more
     int n = known[dev][i].load(std::memory_order_relaxed);
@@ -826,9 +878,9 @@ template <class T> int clusters_of(int i, int dev)
         cfg.dynamicSmemBytes = kWarps * kRing;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(verify_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-            cudaFuncSetAttribute(verify_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarps * kRing) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, verify_kernel<T>, &cfg) != cudaSuccess) {
+        if (cudaFuncSetAttribute(verify_kernel<T, DRAFT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaFuncSetAttribute(verify_kernel<T, DRAFT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarps * kRing) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, verify_kernel<T, DRAFT>, &cfg) != cudaSuccess) {
             cudaGetLastError();
             n = 0;
         }
@@ -838,12 +890,12 @@ template <class T> int clusters_of(int i, int dev)
 }
 
 // Requests over clusters, as large as all of them run at once, and as a warp's run is 256 elements.
-template <class T> int launch_walks(VerifyParams p, const Device &dev, cudaStream_t s)
+template <class T, bool DRAFT> int launch_walks(VerifyParams p, const Device &dev, cudaStream_t s)
 {
     int i = 4;
-    while (i > 0 && (p.batch > clusters_of<T>(i, dev.id) || p.vocab < (kWarps * Walk<T>::kUnit << i) / 2)) --i;
+    while (i > 0 && (p.batch > clusters_of<T, DRAFT>(i, dev.id) || p.vocab < (kWarps * Walk<T>::kUnit << i) / 2)) --i;
     p.split = 1 << i;
-    return launch<VerifyParams>(verify_kernel<T>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, true, s, p);
+    return launch<VerifyParams>(verify_kernel<T, DRAFT>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, true, s, p);
 }
 
 }  // namespace
@@ -877,7 +929,11 @@ extern "C" int e2_verify_drafts(const e2_verify_args *a, void *stream)
                    a->logits_stride, a->draft_stride, a->ids, a->parents, a->starts, a->uniforms, a->temperature,
                    a->kept, a->nodes, a->answer};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return a->dtype == E2_F16    ? launch_walks<__half>(p, dev, s)
-           : a->dtype == E2_BF16 ? launch_walks<__nv_bfloat16>(p, dev, s)
-                                 : launch_walks<float>(p, dev, s);
+    auto as = [&](auto draft) {
+        constexpr bool kDraft = decltype(draft)::value;
+        return a->dtype == E2_F16    ? launch_walks<__half, kDraft>(p, dev, s)
+               : a->dtype == E2_BF16 ? launch_walks<__nv_bfloat16, kDraft>(p, dev, s)
+                                     : launch_walks<float, kDraft>(p, dev, s);
+    };
+    return a->draft ? as(std::true_type{}) : as(std::false_type{});
 }

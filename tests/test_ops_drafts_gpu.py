@@ -479,6 +479,100 @@ def test_a_token_is_the_same_however_rows_are_split():
             assert g.tolist() == w * B
 
 
+def only(V, tokens, logits):
+    """A row in which all but these are forbidden."""
+    row = torch.full((V,), -math.inf, device="cuda")
+    row[tokens] = logits
+    return row
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF, F32])
+@pytest.mark.parametrize("V", [700, 20000])
+@pytest.mark.parametrize("u0", [0.0, 1.0])
+def test_rejected_tokens_alone_in_their_part_of_a_row(dtype, V, u0):
+    """Rejected tokens leave nothing where nothing else is allowed: the answer is the first token that is left, or the last."""
+    n, B = 6, 40
+    g = torch.Generator(device="cuda").manual_seed(20)
+    s = batch_of([n] * B, V, F32, seed=20, draft=False)
+    s[2] = i32(([-1] + [0] * (n - 1)) * B)
+    s[4][:] = 1.0
+    s[4][::n] = u0
+    for r in range(B):
+        far = 60 + 3 * r % 40
+        drafted = torch.randperm(60, generator=g, device="cuda")[:n - 1 - r % 3]
+        left = far + torch.randperm(V - 160, generator=g, device="cuda")[:2 + r % 9]
+        if u0:
+            drafted, left = V - 1 - drafted, V - 1 - left
+        tokens = torch.cat([drafted, left])
+        s[0][r * n] = only(V, tokens, 2 * torch.randn(len(tokens), generator=g, device="cuda"))
+        s[1][r * n + 1:(r + 1) * n] = drafted[torch.arange(n - 1, device="cuda") % len(drafted)].int()
+    s[0] = s[0].to(dtype)
+    kept, _, answer = check_verify(*s)
+    assert kept.tolist() == [1] * B and (answer[:, 0] >= 0).all()
+    check_verify(*s, temperature=torch.full((B,), 0.7, device="cuda"))
+
+
+@pytest.mark.parametrize("V", [300, 20000])
+def test_what_is_left_beside_a_rejected_token_of_nearly_all(V):
+    """The others' shares, and the next child's, next to their borders after a token of 1 - 2^-10 to 1 - 2^-33 was rejected."""
+    n, B = 3, 96
+    g = torch.Generator(device="cuda").manual_seed(21)
+    s = batch_of([n] * B, V, F32, seed=21, draft=False)
+    x, ids, _, _, u, _ = s
+    s[2] = i32([-1, 0, 0] * B)
+    for r in range(B):
+        tokens = torch.randperm(V, generator=g, device="cuda")[:40]
+        logits = torch.randn(40, generator=g, device="cuda")
+        logits[0] = torch.logsumexp(logits[1:], 0) + (10 + r % 24) * math.log(2.0)
+        x[n * r] = only(V, tokens, logits)
+        p = DR.probabilities(x[n * r], 1.0)
+        p[tokens[0]] = 0
+        p /= p.sum()
+        ids[n * r + 1], u[n * r + 1] = tokens[0].int(), 1.0
+        ids[n * r + 2] = tokens[1].int()
+        if r % 2:
+            u[n * r + 2] = neighbours(float(p[tokens[1]]))[r // 2 % 2]
+        else:
+            # (the second is rejected, too)
+            u[n * r + 2] = 1.0
+            p[tokens[1]] = 0
+            border = torch.cumsum(p / p.sum(), 0)[tokens[2 + r // 2 % 30]]
+            u[n * r] = neighbours(float(border))[r // 2 % 2]
+    check_verify(*s)
+
+
+@pytest.mark.parametrize("V", [1000, 20000])
+@pytest.mark.parametrize("u0", [0.0, 1.0])
+def test_parts_of_a_row_that_draft_and_target_share(V, u0):
+    """The same logits in both rows where nothing is left of P, and others elsewhere that sum to the same."""
+    n, B = 2, 120
+    g = torch.Generator(device="cuda").manual_seed(22)
+    s = batch_of([n] * B, V, F32, seed=22)
+    x, ids, _, _, u, y = s
+    s[2] = i32([-1, 0] * B)
+    at = torch.arange(V, device="cuda") if u0 == 0 else torch.arange(V - 1, -1, -1, device="cuda")
+    for r in range(B):
+        # light and shared; heavy in pairs that change places
+        x[n * r] = -math.inf
+        light, heavy = at[:V // 4], at[V // 2:V // 2 + 2 + 2 * (r % 3)]
+        x[n * r, light] = -25.0 + torch.randn(len(light), generator=g, device="cuda")
+        x[n * r, heavy] = torch.randn(len(heavy), generator=g, device="cuda")
+        y[n * r] = x[n * r]
+        y[n * r, heavy] = x[n * r, heavy.view(-1, 2).flip(1).flatten()]
+        ids[n * r + 1] = heavy[int(x[n * r, heavy[0]] > x[n * r, heavy[1]])].int()          # (of less in the target)
+    u[1::2] = 1.0
+    u[::2] = u0
+    from paper_2606_03770_gb300 import ops
+    kept, _, answer = ops.verify_drafts(*s[:5], draft=y, max_new=n)
+    assert kept.tolist() == [1] * B
+    # (of tokens that have as much in both rows 64 bits, too, may leave their rounding)
+    for r in range(B):
+        p, q = (DR.probabilities(z[n * r], 1.0) for z in (x, y))
+        clear = torch.nonzero(p - q > 2.0 ** -36)[0 if u0 == 0 else -1]
+        got = int(answer[r, 0])
+        assert got >= 0 and (got == int(clear) or abs(float(p[got] - q[got])) < 2.0 ** -36), (r, got, int(clear))
+
+
 # ---- keeping ----------------------------------------------------------------------------------------
 def a_way(parents, n, g):
     path = [0] if n else []
