@@ -100,7 +100,12 @@ template <class T> __device__ __forceinline__ float half_of(uint32_t w, int high
     return __uint_as_float(high ? w & 0xffff0000u : w << 16);
 }
 
-template <class T> struct Walk {
+// LONG: runs of which a lane has more than kShort elements, whose sums are closed on the way.  (Of 128,256 tokens that is one
+// block a request.  In one kernel for all, 1 x 5 x 32,000 takes 17.5 us for 16.4, 64 x 8 x 128,256 in 32 bits 146 for 139.)
+constexpr int kShort = 256;
+
+template <class T, bool LONG> struct Walk {
+    using Sum = typename std::conditional<LONG, LongerSum, LongSum>::type;
     // A unit of a run: 16 bytes a lane.
     static constexpr int kEach = 16 / sizeof(T), kUnit = 32 * kEach, kStages = kRing / 1024;
     const VerifyParams &p;
@@ -279,6 +284,8 @@ template <class T> struct Walk {
         __syncthreads();
         const float2 *tops = m.tops;
         const float f = heat.h * 1.44269504f;
+        // (a sum of n is off by n 2^-24 at most: 128 at a time, these with what rounding takes)
+        constexpr int kClose = kShort / kEach;
         int stage = 0;
         // (a unit each, and all in the ring: two nodes side by side)
         const bool side_by_side = wide && end - first == kUnit && count > 1;
@@ -301,9 +308,15 @@ template <class T> struct Walk {
             const float ca = tops[g].x * f, cb = tops[g].y * f;
             const T *u = row_of(p.logits, p.logits_stride, m.group[g]), *v = two ? row_of(p.draft, p.draft_stride, m.group[g]) : u;
             float sa[2] = {0, 0}, sb[2] = {0, 0};
+            LongSum closed_a, closed_b;
+            auto close = [&] {
+                closed_a.add(Two{sa[0] + sa[1], 0}), closed_b.add(Two{sb[0] + sb[1], 0});
+                sa[0] = sa[1] = sb[0] = sb[1] = 0;
+            };
 #pragma unroll 1
             for (int unit = 0; unit < units; ++unit) {
                 Lot e, d;
+                if (LONG && unit % kClose == kClose - 1) close();
                 if (wide) {
                     copy_wait<kStages - 1>();
                     e = from_ring(stage, 0);
@@ -325,6 +338,10 @@ template <class T> struct Walk {
             for (int i = first + units * kUnit + lane; i < end; i += 32) {
                 sa[0] += power2(__fmaf_rn(to_float(u[i]), f, -ca));
                 if (two) sb[0] += power2(__fmaf_rn(to_float(v[i]), f, -cb));
+            }
+            if (LONG) {
+                close();
+                sa[0] = closed_a.value().h, sb[0] = closed_b.value().h;
             }
             m.lane_sums[warp][g][lane] = make_float2(sa[0] + sa[1], sb[0] + sb[1]);
         }
@@ -378,8 +395,9 @@ template <class T> struct Walk {
             if (m.ids[__ffsll(nodes) - 1] == v) return true;
         return false;
     }
-    // The same run again, f(two elements of x, of y): a short loop, as f is long.  LEAVE: without the tokens of `out`'s nodes.
-    template <bool BOTH, bool LEAVE = false, class F> __device__ __forceinline__ void pairs(F f, uint64_t out = 0) const
+    // The same run again, f(two elements of x, of y): a short loop, as f is long; close(times) after every 32 of a lane's
+    // elements.  LEAVE: without the tokens of `out`'s nodes.
+    template <bool BOTH, bool LEAVE = false, class F, class G> __device__ __forceinline__ void pairs(F f, G close, uint64_t out = 0) const
     {
         constexpr int kStep = sizeof(T) / 2;                              // words of two elements
         const int units = (end - first) / kUnit, rest = end - first - units * kUnit;
@@ -428,6 +446,8 @@ template <class T> struct Walk {
                     if (BOTH) v.w[w] = v.w[w + kStep];
                 }
             }
+            constexpr int kClose = 32 / kEach;
+            if (LONG && unit % kClose == kClose - 1) close(unit / kClose);
         }
     }
 
@@ -486,7 +506,7 @@ template <class T> struct Walk {
     // of `out`'s nodes.
     template <bool BOTH, bool LESS> __device__ __forceinline__ Two sums(const Weigher of_x, const Weigher of_y, Two &q, uint64_t out = 0)
     {
-        LongSum a, b;
+        Sum a, b;
         if (out) {
             auto mine = [&](int c) { return __ballot_sync(~0u, out >> c & 1 && m.ids[c] >= first && m.ids[c] < end); };
             out = mine(lane) | (uint64_t)mine(lane + 32) << 32;
@@ -500,8 +520,11 @@ template <class T> struct Walk {
                 a.add(LESS ? less_of(w[j], d[j]) : w[j]);
                 if (BOTH) b.add(d[j]);
             }
+        }, [&](int times) {
+            a.close(times);
+            if (BOTH) b.close(times);
         }, out);
-        Part mine{a.value(), b.value(), 0, 0, 0, 0};
+        Part mine{a.total(), BOTH ? b.total() : Two{0, 0}, 0, 0, 0, 0};
         exchange(mine, [&](int k) {
             mine.p = mine.p + shuffle_xor(mine.p, k);
             if (BOTH) mine.q = mine.q + shuffle_xor(mine.q, k);
@@ -515,7 +538,7 @@ template <class T> struct Walk {
     // difference of the two, of which no more than that difference counts; `border` sums x within 2^-20 of it.
     __device__ __forceinline__ Two split(const Weigher of_x, const Weigher of_y, float near, Two &q)
     {
-        LongSum a[2], b[2];
+        Sum a[2], b[2];
         float edge = 0;
         pairs<true>([&](const float (&u)[2], const float (&v)[2]) {
             Two w[2], d[2];
@@ -529,11 +552,11 @@ template <class T> struct Walk {
                 LongSum x{above ? a[1].s : a[0].s, above ? a[1].c : a[0].c}, y{above ? b[1].s : b[0].s, above ? b[1].c : b[0].c};
                 x.add(w[j]);
                 y.add(d[j]);
-                a[1] = above ? x : a[1], b[1] = above ? y : b[1];
-                a[0] = above ? a[0] : x, b[0] = above ? b[0] : y;
+                a[1].s = above ? x.s : a[1].s, a[1].c = above ? x.c : a[1].c, b[1].s = above ? y.s : b[1].s, b[1].c = above ? y.c : b[1].c;
+                a[0].s = above ? a[0].s : x.s, a[0].c = above ? a[0].c : x.c, b[0].s = above ? b[0].s : y.s, b[0].c = above ? b[0].c : y.c;
             }
-        });
-        Part mine{a[0].value(), b[0].value(), 0, 0, 0, 0, a[1].value(), b[1].value(), edge};
+        }, [&](int times) { a[0].close(times), a[1].close(times), b[0].close(times), b[1].close(times); });
+        Part mine{a[0].total(), b[0].total(), 0, 0, 0, 0, a[1].total(), b[1].total(), edge};
         exchange<true>(mine, [&](int k) {
             mine.p = mine.p + shuffle_xor(mine.p, k);
             mine.q = mine.q + shuffle_xor(mine.q, k);
@@ -547,18 +570,18 @@ template <class T> struct Walk {
     }
     // After it: run and block of (x - share y)+, and its sum; false where the border's part of it may be above 2^-37.
     // What is so little of x that it may be all rounding is nothing, so that whoever has something has an element with
-    // something (the sums and weights are off by 2^-43; a block that has something has a run that does).
+    // something (sums are off by some 2^-41; a block that has something has a run that does).
     __device__ __forceinline__ bool take_split(const Two &share, float near, Two &sum)
     {
         auto of = [&](const Two &x, const Two &y, float least) {
             const Two d = x - share * y;
             return d.h > least * x.h ? d : Two{0, 0};
         };
-        sum = warp_sum(lane < p.split ? of(block, block_q, 0x1p-39f) : Two{0, 0});
+        sum = warp_sum(lane < p.split ? of(block, block_q, 0x1p-37f) : Two{0, 0});
         // (2^-22: what the comparisons were rounded by)
         const float off = fabsf(__fdiv_rn((share - Two{near, 0}).h, near)) + 0x1p-22f;
         if (!(off < 0x1p-20f && off * border <= 0x1p-37f * sum.h)) return false;
-        run = of(run, run_q, 0x1p-40f), block = of(block, block_q, 0x1p-39f);
+        run = of(run, run_q, 0x1p-38f), block = of(block, block_q, 0x1p-37f);
         return true;
     }
 
@@ -590,11 +613,13 @@ template <class T> struct Walk {
         auto part_of = [&](int k) { return run_from + (int)((int64_t)(run_stop - run_from) * k / kWarps); };
         // a lane's share of them is side by side, too
         const int start = part_of(warp), stop = part_of(warp + 1), share = (stop - start + 31) / 32;
-        LongSum a;
+        Sum a;
 #pragma unroll 1
-        for (int i = start + lane * share; i < min(start + (lane + 1) * share, stop); ++i)
+        for (int k = 0, i = start + lane * share; k < share && i < stop; ++k, ++i) {
             if (!gone(i)) a.add(weight(i, less, of_x, of_y));
-        const Two mine = a.value(), sub = warp_sum(mine);
+            if (LONG && k % 32 == 31) a.close(k / 32);
+        }
+        const Two mine = a.total(), sub = warp_sum(mine);
         if (lane == 0) m.sub[warp] = sub;
         __syncthreads();
         if (choose(m.sub[lane % kWarps], kWarps) != warp) return false;
@@ -616,7 +641,7 @@ template <class T> struct Walk {
 };
 
 // (two kernels, as one for rows with and without the draft's keeps more than its registers)
-template <class T, bool DRAFT> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyParams p)
+template <class T, bool DRAFT, bool LONG> __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyParams p)
 {
     __shared__ Shared m;
     const int request = blockIdx.x / p.split;
@@ -624,7 +649,7 @@ template <class T, bool DRAFT> __global__ void __launch_bounds__(kThreads, 2) ve
     allow_next();
     if (p.split > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     extern __shared__ __align__(16) uint8_t dynamic[];
-    Walk<T> walk(p, m, dynamic);
+    Walk<T, LONG> walk(p, m, dynamic);
     const bool writer = walk.rank == 0 && threadIdx.x == 0;
     const int64_t start = p.starts[request], stop = p.starts[request + 1];
     const int n = start >= 0 && stop <= p.tokens ? (int)min(max(stop - start, (int64_t)0), (int64_t)p.max_new) : 0;
@@ -658,8 +683,8 @@ template <class T, bool DRAFT> __global__ void __launch_bounds__(kThreads, 2) ve
     // A node is looked at together with its first child, that one's first child, and so on, as long as the ring holds
     // them all: for small vocabularies, where a pass is latency, one does for up to four nodes.  (For larger ones, or
     // without the draft's rows, what is not accepted costs more: 8 x 16 x 128,256 40 us for 37.)
-    const int runs = kWarps * p.split, run_units = ((p.vocab + Walk<T>::kUnit - 1) / Walk<T>::kUnit + runs - 1) / runs;
-    const int at_once = DRAFT && walk.wide ? max(min(kGroup, Walk<T>::kStages / run_units), 1) : 1;
+    const int runs = kWarps * p.split, run_units = ((p.vocab + Walk<T, LONG>::kUnit - 1) / Walk<T, LONG>::kUnit + runs - 1) / runs;
+    const int at_once = DRAFT && walk.wide ? max(min(kGroup, Walk<T, LONG>::kStages / run_units), 1) : 1;
     int place = 0, count = 0;                             // of the node in its group; the group's nodes
     float x_sums = 0, y_sums = 0, child_value = 0;        // lane g kWarps: node g's; and the one after it: its first child's logits
 
@@ -682,7 +707,7 @@ template <class T, bool DRAFT> __global__ void __launch_bounds__(kThreads, 2) ve
         float x_sum = 0, y_sum = 0, first_x = 0, first_y = 0;
         bool clear = false;
         if (!greedy) {
-            // In 32 bits first: exponents are off by 2^-18 at most (of 64, and 2^-18 of that in f), sums by less,
+            // In 32 bits first: exponents are off by 2^-18 at most (of 64, and 2^-18 of that in f), sums by 2^-17,
             // so what is clear by one part in 2^14 is clear.
             constexpr float kClear = 0x1p-14f;
             const int child0 = children ? first_of(children) : 0;
@@ -864,7 +889,7 @@ template <class T, bool DRAFT> __global__ void __launch_bounds__(kThreads, 2) ve
 }
 
 // How many clusters of 2^i blocks run at once.
-template <class T, bool DRAFT> int clusters_of(int i, int dev)
+template <class T, bool DRAFT, bool LONG> int clusters_of(int i, int dev)
 {
     static std::atomic<int> known[64][5];                    // one more
     int n = known[dev][i].load(std::memory_order_relaxed);
@@ -878,9 +903,9 @@ template <class T, bool DRAFT> int clusters_of(int i, int dev)
         cfg.dynamicSmemBytes = kWarps * kRing;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(verify_kernel<T, DRAFT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-            cudaFuncSetAttribute(verify_kernel<T, DRAFT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarps * kRing) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, verify_kernel<T, DRAFT>, &cfg) != cudaSuccess) {
+        if (cudaFuncSetAttribute(verify_kernel<T, DRAFT, LONG>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaFuncSetAttribute(verify_kernel<T, DRAFT, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarps * kRing) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, verify_kernel<T, DRAFT, LONG>, &cfg) != cudaSuccess) {
             cudaGetLastError();
             n = 0;
         }
@@ -890,12 +915,17 @@ template <class T, bool DRAFT> int clusters_of(int i, int dev)
 }
 
 // Requests over clusters, as large as all of them run at once, and as a warp's run is 256 elements.
-template <class T, bool DRAFT> int launch_walks(VerifyParams p, const Device &dev, cudaStream_t s)
+template <class T, bool DRAFT, bool LONG> int launch_walks(VerifyParams p, const Device &dev, cudaStream_t s)
 {
+    constexpr int kUnit = Walk<T, LONG>::kUnit;
     int i = 4;
-    while (i > 0 && (p.batch > clusters_of<T, DRAFT>(i, dev.id) || p.vocab < (kWarps * Walk<T>::kUnit << i) / 2)) --i;
+    while (i > 0 && (p.batch > clusters_of<T, DRAFT, LONG>(i, dev.id) || p.vocab < (kWarps * kUnit << i) / 2)) --i;
     p.split = 1 << i;
-    return launch<VerifyParams>(verify_kernel<T, DRAFT>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, true, s, p);
+    if constexpr (!LONG) {
+        const int runs = kWarps * p.split, run_units = ((p.vocab + kUnit - 1) / kUnit + runs - 1) / runs;
+        if (run_units > kShort / Walk<T, LONG>::kEach) return launch_walks<T, DRAFT, true>(p, dev, s);
+    }
+    return launch<VerifyParams>(verify_kernel<T, DRAFT, LONG>, dim3((unsigned)p.batch * p.split), kThreads, kWarps * kRing, p.split, true, s, p);
 }
 
 }  // namespace
@@ -931,9 +961,9 @@ extern "C" int e2_verify_drafts(const e2_verify_args *a, void *stream)
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     auto as = [&](auto draft) {
         constexpr bool kDraft = decltype(draft)::value;
-        return a->dtype == E2_F16    ? launch_walks<__half, kDraft>(p, dev, s)
-               : a->dtype == E2_BF16 ? launch_walks<__nv_bfloat16, kDraft>(p, dev, s)
-                                     : launch_walks<float, kDraft>(p, dev, s);
+        return a->dtype == E2_F16    ? launch_walks<__half, kDraft, false>(p, dev, s)
+               : a->dtype == E2_BF16 ? launch_walks<__nv_bfloat16, kDraft, false>(p, dev, s)
+                                     : launch_walks<float, kDraft, false>(p, dev, s);
     };
     return a->draft ? as(std::true_type{}) : as(std::false_type{});
 }

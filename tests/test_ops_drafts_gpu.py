@@ -573,6 +573,34 @@ def test_parts_of_a_row_that_draft_and_target_share(V, u0):
         assert got >= 0 and (got == int(clear) or abs(float(p[got] - q[got])) < 2.0 ** -36), (r, got, int(clear))
 
 
+@pytest.mark.parametrize("B,V,dtype", [(160, 1 << 22, BF), (160, 65536, BF), (160, 262144, F32), (2, (1 << 26) + 1357, HALF)])
+@pytest.mark.parametrize("draft", [False, True])
+def test_long_rows_of_equal_logits(B, V, dtype, draft):
+    """The rows whose sums lose most, long ones in one block: random numbers by 2^-13.5 and less beside a child's border, the
+    nearest to it, and answers."""
+    if draft:
+        V //= 2
+    g = torch.Generator(device="cuda").manual_seed(23)
+    far = [-2 ** -13.5, 2 ** -13.5, -2 ** -14.5, 2 ** -14.5, -2 ** -17, 2 ** -17, -2 ** -20, 2 ** -20, 0.0, 0.0]
+    rounds = 1 if B > 2 else 6
+    for k in range(rounds):
+        s = [torch.empty(2 * B, V, dtype=dtype, device="cuda"), torch.zeros(2 * B, **I32), i32([-1, 0] * B), i32(range(0, 2 * B + 1, 2)),
+             torch.rand(2 * B, generator=g, device="cuda"), torch.empty(2 * B, V, dtype=dtype, device="cuda") if draft else None]
+        for r in range(B):
+            for z in s[0::5] if draft else s[:1]:
+                z[2 * r:2 * r + 2] = -3 * torch.rand(2, 1, generator=g, device="cuda")
+                z[2 * r:2 * r + 2, 0] = 0.0
+            if draft:
+                s[5][2 * r, V // 2:] = -math.inf             # (so that q is some 2 p)
+            token = 1 + (7919 * r + 31 * k) % (V // 3)
+            p = DR.probabilities(s[0][2 * r], 1.0)[token]
+            if draft:
+                p /= DR.probabilities(s[5][2 * r], 1.0)[token]
+            s[1][2 * r + 1] = token
+            s[4][2 * r + 1] = float(p) * (1 + far[(r + 2 * k) % len(far)])
+        check_verify(*s)
+
+
 # ---- keeping ----------------------------------------------------------------------------------------
 def a_way(parents, n, g):
     path = [0] if n else []
