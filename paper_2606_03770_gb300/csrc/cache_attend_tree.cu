@@ -366,8 +366,8 @@ __device__ __forceinline__ void weights(const AttendParams &p, const Span &span,
     if (set == 1) return;
     const bool lost = !ok || *m.failed;
     const float nan = __int_as_float(0x7fc00000);
-    // (what saw nothing has no maximum, or what saw NaN)
-    auto factor = [](float top, float sum, float best) { return top == -INFINITY ? (sum == 0 ? 0.0f : sum) : power2(top - best); };
+    // (what saw nothing has no maximum, or what saw NaN; a NaN among others is in the sum, and stays whatever they weigh)
+    auto factor = [](float top, float sum, float best) { return sum == 0 || sum != sum ? sum : power2(top - best); };
     auto join_sums = [](float a, float fa, float b, float fb) { return (fa == 0 ? 0.0f : a * fa) + (fb == 0 ? 0.0f : b * fb); };
     const float best = fmaxf(top, other[0]);
     const float f0 = span.n < 1 ? 0.0f : factor(top, sum, best), f1 = span.n < 2 ? 0.0f : factor(other[0], other[1], best);
@@ -497,9 +497,9 @@ __device__ __forceinline__ void join_parts(const AttendParams &p, const Slab &sl
         float total = 0, y[4] = {};
 #pragma unroll
         for (int k = 0; k < kTreeCluster; ++k) {
-            // (a part without a maximum saw nothing, or NaN)
+            // (a part without a maximum saw nothing, or NaN; NaN stays whatever its part weighs)
             const float f = tops[k] == -INFINITY ? (weights[k] == 0 ? 0.0f : weights[k]) : power2(tops[k] - best);
-            if (k < p.splits && f != 0) {
+            if (k < p.splits) {
                 total = __fmaf_rn(weights[k], f, total);
                 const float v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll

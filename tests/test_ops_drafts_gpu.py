@@ -236,6 +236,25 @@ def test_not_finite_in_hidden_places(G):
     assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
 
 
+@pytest.mark.parametrize("B,G,new,ctx", [(2, 1, 12, 200), (2, 16, 12, 200), (2, 8, 7, 200), (8, 8, 16, 700), (4, 8, 7, 1100), (1, 8, 7, 20000),
+                                         (1, 16, 12, 20000)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_not_finite_far_below_the_largest_score(B, G, new, ctx, D):
+    """A NaN among seen keys or values spoils every row, however little the tiles around it weigh beside the others."""
+    from paper_2606_03770_gb300 import ops
+    cache, q, table, lens, starts = setup([ctx] * B, [new] * B, 2, G, D, 16, seed=ctx)
+    q *= 60                                                  # (scores hundreds apart: far tiles' factors are 0 in 32 bits)
+    parents, kw = trees([new] * B), dict(max_new=new, max_len=ctx)
+    assert torch.isfinite(ops.cache_attend_tree(cache, q, parents, table, lens, starts, **kw)).all()
+    for at in (0, 5, 40, 64 + 3, 64 + 37, 130, ctx // 2, ctx - new - 1):
+        for scales in (cache.k_scales, cache.v_scales):
+            kept = scales.clone()
+            scales[table[:, at // 16].long(), :, at % 16] = math.nan
+            out = ops.cache_attend_tree(cache, q, parents, table, lens, starts, **kw)
+            assert torch.isnan(out).all(), at
+            scales.copy_(kept)
+
+
 def test_strided_queries_and_given_outputs():
     from paper_2606_03770_gb300 import ops
     cache, q, table, lens, starts = setup([300, 90], [9, 4], 2, 4, 128, 64, seed=13)
