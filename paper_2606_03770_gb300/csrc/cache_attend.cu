@@ -559,8 +559,8 @@ constexpr int kPrompt = 65;
 // for a whole wave).
 constexpr int kClusterUnits = 8;
 
-// Trees' rows are by 128 from so many on; from nine on where the blocks run at once and all requests' keys, times the
-// KV heads, are so few.  Measured, us (128 elements, bf16; by eight or sixteen / by 128): 24 rows of 8 requests x 8 KV
+// Trees' rows are by 128 from so many on; from nine on where the blocks run at once and the keys that all requests see
+// (max_len, or a window's), times the KV heads, are so few.  Measured, us (128 elements, bf16; by eight or sixteen / by 128): 24 rows of 8 requests x 8 KV
 // heads x 2,304 keys 40 / 20, 16 rows 31 / 20, 8 rows 18 / 20; 16 rows of 150 keys 20 / 11, 9,000 keys 54 / 48 (fp16 53),
 // 65,000 keys 221 / 258 (fp16 293), of 16 x 8 x 9,000 91 / 84 (fp16 94), of one request x 32 x 30,000 73 / 72 (fp16 81); of
 // more heads than multiprocessors, 48 x 8 x 2,304 71 / 86; 8 rows of one request x 8 x 150 11 / 10, x 2,304 11 / 14.
@@ -582,13 +582,13 @@ Plan plan(const e2_cache *c, const e2_attend_args *a, int sms, bool tree)
     const int64_t rows = (int64_t)(a->max_new > 0 ? a->max_new : 1) * (a->q_heads / c->kv_heads);
     f.nt = rows >= (tree ? kTree : kPrompt) ? 0 : rows <= 8 ? 1 : 2;
     const int64_t heads = (int64_t)a->batch * c->kv_heads;
-    if (tree && f.nt == 2 && heads <= sms && heads * a->max_len <= (a->dtype == E2_F16 ? kTreeKeysHalf : kTreeKeys)) f.nt = 0;
+    int64_t keys = a->max_len;
+    if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
+    if (tree && f.nt == 2 && heads <= sms && heads * keys <= (a->dtype == E2_F16 ? kTreeKeysHalf : kTreeKeys)) f.nt = 0;
     const int at_once = f.nt ? 8 * f.nt : tree ? kTreeRows : kPromptRows;
     f.rows = (int)(rows < (1 << 18) ? rows : 1 << 18);
     const int64_t slabs = (rows + at_once - 1) / at_once;
     f.slabs = (int)(slabs < 65535 ? slabs : 65535);
-    int64_t keys = a->max_len;
-    if (a->window > 0 && keys > (int64_t)a->window + a->max_new) keys = (int64_t)a->window + a->max_new;
     const int least = f.nt ? kTile * kFewWarps : 512;
     const int64_t units = (keys + least - 1) / least;
     const int64_t pairs = (int64_t)a->batch * c->kv_heads * slabs, places = (int64_t)sms * (f.nt ? kFewBlocks : 1);

@@ -255,6 +255,23 @@ def test_not_finite_far_below_the_largest_score(B, G, new, ctx, D):
             scales.copy_(kept)
 
 
+def test_windows_choose_the_launch():
+    """What is chosen goes by the keys that are seen, not by a context that a window hides."""
+    import ctypes
+    from paper_2606_03770_gb300 import e2ga, ops
+    cache = ops.Cache.empty(4, 16, 8, 128)
+
+    def workspace(new, max_len, window, dtype):
+        a = ops.e2_attend_args(new, dtype, 8, 1, None, 1, 1, None, None, new, max_len, 1.0, window)
+        return e2ga.load().e2_cache_attend_tree_workspace(cache.ref, ctypes.byref(a))
+
+    ops.load()
+    for dtype in (ops.E2_F16, ops.E2_BF16):
+        for new in (1, 8, 9, 16, 17, 64):
+            for window in (100, 9000, 30000):
+                assert workspace(new, 10 ** 6, window, dtype) == workspace(new, window + new, window, dtype)
+
+
 def test_strided_queries_and_given_outputs():
     from paper_2606_03770_gb300 import ops
     cache, q, table, lens, starts = setup([300, 90], [9, 4], 2, 4, 128, 64, seed=13)
