@@ -9,6 +9,10 @@
 // a launch; 2,048 tokens 24 in (3.2 TB/s, 48% of the memory's rate), 7 out.  Bound by
 // instructions: the divisions were 4 us of 2,048 tokens' time; four heads a lane, which share
 // their cosines, are no faster (25), eight slower (36).
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "ops_common.cuh"
 
 namespace e2ops {
@@ -415,26 +419,29 @@ extern "C" int e2_cache_layers(const e2_cache *caches, int32_t layers, uint64_t 
     Device dev;
     if (!caches || !arrays || layers < 1) return fail(E2_EINVAL, "caches and arrays must be given, layers positive");
     if (int st = current_device(&dev)) return st;
+    struct Place {
+        uintptr_t from, to;
+    };
+    const size_t n = 4 * (size_t)layers;
+    const std::unique_ptr<Place[]> places(new (std::nothrow) Place[n]);
+    if (!places) return fail(E2_ENOMEM, "no host memory");
     for (int32_t i = 0; i < layers; ++i) {
         const e2_cache &c = caches[i];
         if (int st = check_cache(&c, dev.id)) return st;
         if (c.pages != caches->pages || c.page_size != caches->page_size || c.kv_heads != caches->kv_heads ||
             c.head_dim != caches->head_dim)
             return fail(E2_EINVAL, "the layers' caches must be of one shape");
-        // (the codes' arrays, each of this size)
-        const uintptr_t size = (uintptr_t)c.pages * c.page_size * c.kv_heads * (c.head_dim / 2);
-        for (int32_t j = 0; j <= i; ++j) {
-            const uintptr_t mine[2] = {(uintptr_t)c.k_codes, (uintptr_t)c.v_codes};
-            const uintptr_t theirs[2] = {(uintptr_t)caches[j].k_codes, (uintptr_t)caches[j].v_codes};
-            for (int k = 0; k < 4; ++k) {
-                if (j == i && k / 2 == k % 2) continue;
-                const uintptr_t a = mine[k / 2], b = theirs[k % 2];
-                if ((a < b ? b - a : a - b) < size) return fail(E2_EINVAL, "the layers' caches must not share memory");
-            }
-        }
+        const uintptr_t vectors = (uintptr_t)c.pages * c.page_size * c.kv_heads;
         const void *of[4] = {c.k_codes, c.k_scales, c.v_codes, c.v_scales};
-        for (int k = 0; k < 4; ++k) arrays[4 * (size_t)i + k] = (uint64_t)(uintptr_t)of[k];
+        for (int k = 0; k < 4; ++k) {
+            const uintptr_t at = (uintptr_t)of[k];
+            places[4 * (size_t)i + k] = {at, at + vectors * (k % 2 ? c.head_dim / E2_CACHE_GROUP * 4 : c.head_dim / 2)};
+            arrays[4 * (size_t)i + k] = (uint64_t)at;
+        }
     }
+    std::sort(places.get(), places.get() + n, [](const Place &a, const Place &b) { return a.from < b.from; });
+    for (size_t i = 1; i < n; ++i)
+        if (places[i].from < places[i - 1].to) return fail(E2_EINVAL, "the layers' caches must not share memory");
     return E2_OK;
 }
 

@@ -754,6 +754,29 @@ def test_refusals():
         tree(cache=grad)
 
 
+def test_layers_that_share_memory_are_refused():
+    """Codes or scales, of two layers or within one, whole or in part."""
+    from paper_2606_03770_gb300 import ops
+    shape = (6, 2, 16)
+    codes = lambda: torch.zeros(*shape, 64, dtype=torch.uint8, device="cuda")
+    scales = lambda: torch.zeros(*shape, 2, 2, dtype=torch.float16, device="cuda")
+    a = (codes(), scales(), codes(), scales())
+    assert len(ops.CacheLayers([ops.Cache(*a), ops.Cache(codes(), scales(), codes(), scales())])) == 2
+    inside = a[0].view(-1)[256:256 + scales().nbytes].view(torch.float16).view(*shape, 2, 2)
+    longer = torch.zeros(2 * scales().numel() - 8, dtype=torch.float16, device="cuda")
+    first, second = longer[:scales().numel()].view(*shape, 2, 2), longer[scales().numel() - 8:].view(*shape, 2, 2)
+    for caches in ([a, (codes(), a[1], codes(), scales())], [a, (codes(), scales(), codes(), a[3])], [a, (codes(), a[3], codes(), scales())],
+                   [(codes(), a[1], codes(), a[1])], [a, (codes(), inside, codes(), scales())], [(codes(), first, codes(), second)],
+                   [a, (codes(), scales(), codes(), scales()), (codes(), scales(), a[0], scales())], [a, (codes(), first, codes(), scales()),
+                                                                                                     (codes(), second, codes(), scales())]):
+        with pytest.raises(ValueError, match="share memory"):
+            ops.CacheLayers([ops.Cache(*c) for c in caches])
+    # (next to one another is apart)
+    whole = torch.zeros(4, scales().numel(), dtype=torch.float16, device="cuda")
+    s = [whole[i].view(*shape, 2, 2) for i in range(4)]
+    assert len(ops.CacheLayers([ops.Cache(codes(), s[2], codes(), s[0]), ops.Cache(codes(), s[1], codes(), s[3])])) == 2
+
+
 class NoBinding:
     """The compiled binding, going by."""
     attend_tree = verify = keep = staticmethod(lambda *a: None)
@@ -779,6 +802,12 @@ def test_the_binding_in_python_is_the_same(G, monkeypatch):
     got = run() + more()
     for a, b in zip(got, want):
         assert a.dtype is b.dtype and torch.equal(a, b)
+
+
+def test_refusals_without_the_binding(monkeypatch):
+    from paper_2606_03770_gb300 import ops
+    monkeypatch.setattr(ops, "_binding", NoBinding)
+    test_refusals()
 
 
 def test_empty_calls():
