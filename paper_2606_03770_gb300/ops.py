@@ -26,11 +26,11 @@ from __future__ import annotations
 import ctypes as C
 import importlib.machinery
 import importlib.util
-import os
+import warnings
 
 import torch
 
-from . import e2ga
+from . import build, e2ga
 from .e2ga import E2_OK
 
 E2_F16, E2_BF16, E2_F32 = 0, 1, 2
@@ -119,19 +119,24 @@ def load():
 _binding = None
 
 
+class _NoBinding:
+    """In the module's place where it is not built: every call goes the whole way here."""
+    attend_tree = verify = keep = staticmethod(lambda *a: None)
+
+
 def binding():
     """The module of the calls whose time is the host's: None from one of its functions says that the
-    call is to go the whole way here."""
+    call is to go the whole way here.  Where there is none for this Python and torch, all do."""
     global _binding
     if _binding is None:
         load()
-        path = os.path.join(os.path.dirname(e2ga.LIB_PATH), "e2binding.so")
-        if not os.path.exists(path):
-            raise RuntimeError(f"{path} is not built")
-        spec = importlib.util.spec_from_loader("e2binding", importlib.machinery.ExtensionFileLoader("e2binding", path))
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
-        _binding = module
+        if build.binding_built_for() is not None and build.binding_built_for() == build.binding_for():
+            spec = importlib.util.spec_from_loader("e2binding", importlib.machinery.ExtensionFileLoader("e2binding", build.BINDING))
+            _binding = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(_binding)
+        else:
+            warnings.warn("e2binding.so is not built for this Python and torch: calls take some 15 us longer")
+            _binding = _NoBinding
     return _binding
 
 
