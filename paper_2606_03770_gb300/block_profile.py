@@ -18,8 +18,9 @@ the 32-device workload).
 ``--draft`` also times a decode step with a tree of drafted tokens for each request, given by its
 branching level by level (2.1.1: two children of a request's last token, one of each of these, one of
 each of those): the block on all nodes, then the head, the verification and the move of the accepted
-way's keys and values.  How many drafted tokens a model accepts is not known here, so what is shown
-is how many tokens a block's step has to give to be worth its time.
+way's keys and values.  How many drafted tokens a model accepts is not known here.  The head's steps
+are those of a draft that is nearly the target, whose ways are accepted to their ends as a rule (how many tokens
+they gave is shown), and what a block's step has to give to be worth its time is shown.
 """
 from __future__ import annotations
 
@@ -165,6 +166,7 @@ class Measured:
     head: list
     NP: int
     ND: int
+    given: list = dataclasses.field(default_factory=list)     # tokens a request and step, of steps with drafts
 
 
 def measure(model, NP, ND, b_max, page=64, window=0, repeats=20):
@@ -208,7 +210,9 @@ def branching(text):
 
 def measure_drafts(model, NP, ND, b_max, parents, page=64, window=0, repeats=20):
     """Run and time decode steps with a tree of drafted tokens for each request, at the context of
-    `measure`'s: ``block`` and ``head`` (with verification and move) of b requests at index b - 1."""
+    `measure`'s: ``block`` and ``head`` (with verification and move) of b requests at index b - 1, and
+    ``given``, the tokens that such a step gave a request.  Drafted tokens are drawn, each by itself, from a
+    draft whose logits are the target's and a little noise."""
     n = len(parents)
     block = Block(model["d"], model["ffn"], model["kv_heads"], model["vocab"], NP + ND + n)
     pages = -(-(NP + ND - 1 + n) // page)
@@ -222,11 +226,15 @@ def measure_drafts(model, NP, ND, b_max, parents, page=64, window=0, repeats=20)
     for b in range(1, b_max + 1):
         step = Batch.of_trees(table[:b], NP + ND - 1, parents, page)
         x = torch.randn(b * n, block.d, device="cuda").to(block.dtype)
-        draft = torch.randn(b * n, model["vocab"], device="cuda").to(block.dtype)
-        above = torch.arange(b, device="cuda").repeat_interleave(n) * n + step.parents.clamp(min=0)
-        ids, uniforms = draft[above].argmax(1).int(), torch.rand(b * n, device="cuda")
+        logits = ops.quant_matmul(norm(x, block.norms[2]), block.w_head)
+        draft = logits + 0.01 * logits.float().std().to(block.dtype) * torch.randn_like(logits)
+        ids, uniforms = torch.empty(b * n, dtype=torch.int32, device="cuda"), torch.rand(b * n, device="cuda")
+        for t in range(b * n):
+            p = torch.softmax(draft[t // n * n + max(parents[t % n], 0)].float(), 0)
+            ids[t] = torch.multinomial(p, 1)[0]
         out.block.append(time_graph(lambda: block.forward(x, cache, step, window), repeats))
         out.head.append(time_graph(lambda: block.accept(x, ids, step, uniforms, draft, layers), repeats))
+        out.given.append(float(block.accept(x, ids, step, uniforms, draft, layers)[0].float().mean()))
     return out
 
 
@@ -289,9 +297,9 @@ def main(argv=None):
                   f"{'the prefill' if v == 0 else f'decode {v}'}")
     if a.draft:
         d = measure_drafts(W.CONFIGS[a.config]["model"], prob.NP, prob.ND, prob.b_max, a.draft, window=a.window)
-        print(f"trees of {len(a.draft)} nodes: {'block us':>10s}{'head us':>10s}  tokens a block's step has to give")
-        for b, (t, h) in enumerate(zip(d.block, d.head), 1):
-            print(f"{f'decode {b}':16s}{t * 1e6:10.1f}{h * 1e6:10.1f}{t / m.block[b]:10.2f}")
+        print(f"trees of {len(a.draft)} nodes: {'block us':>10s}{'head us':>10s}  (giving)  tokens a block's step has to give")
+        for b, (t, h, g) in enumerate(zip(d.block, d.head, d.given), 1):
+            print(f"{f'decode {b}':16s}{t * 1e6:10.1f}{h * 1e6:10.1f}{g:10.2f}{t / m.block[b]:10.2f}")
     print(f"as a device of the planner: {rate / 1e12:.1f} TFLOP/s, {bw / 1e9:.0f} GB/s")
     if a.plan:
         from .e2ga import Engine

@@ -94,6 +94,17 @@ def test_measured_drafts(capsys, monkeypatch):
     assert "trees of 5 nodes" in out and out.count("decode 2") == 2
 
 
+@pytest.mark.parametrize("tree", ["1.1.1", "3.2.1"])
+def test_measured_steps_are_accepted(tree):
+    """The head that is timed verifies ways, and moves them: nearly all of a tree's depth."""
+    from paper_2606_03770_gb300 import block_profile as P
+    model = dict(N=2, d=512, ffn=1408, kv_heads=2, vocab=1000, wbits=4)
+    m = P.measure_drafts(model, 40, 24, 8, P.branching(tree), page=16, repeats=2)
+    assert len(m.given) == 8 and all(1 <= g <= 4 for g in m.given)
+    # (a node's first child is accepted but in the draft's distance from the target, some 1%; 36 requests)
+    assert sum(g * (b + 1) for b, g in enumerate(m.given)) / 36 > 3.5
+
+
 def test_batches_without_trees_are_as_they_were():
     from paper_2606_03770_gb300.block_profile import Batch
     table = torch.arange(4, device="cuda").int().view(1, 4)
