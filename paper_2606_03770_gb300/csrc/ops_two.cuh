@@ -78,17 +78,17 @@ struct LongSum {
     __device__ __forceinline__ void close(int) {}
     __device__ __forceinline__ Two total() const { return value(); }
 };
-// One of as many as 2^30: close() after every 32 of them (2^-39), and what that gives, off by 2^-47 each time, is put by
-// after 64 more.
+// One of as many as 2^30: close() after every 32 of them brings c back to half a step of s (512 are off by 2^-35 at most),
+// and after 512 puts what there is by, which is off by 2^-47 each time.
 struct LongerSum : LongSum {
-    Two closed{0, 0}, by{0, 0};
+    Two by{0, 0};
     __device__ __forceinline__ void close(int times)
     {
-        closed = closed + value();
-        s = c = 0;
-        if (times % 64 == 63) by = by + closed, closed = Two{0, 0};
+        const Two t = value();
+        s = t.h, c = t.l;
+        if (times % 16 == 15) by = by + t, s = c = 0;
     }
-    __device__ __forceinline__ Two total() const { return by + (closed + value()); }
+    __device__ __forceinline__ Two total() const { return by + value(); }
 };
 
 // 2^(j / 512), j < 512, in two parts, from the exponential's series; made by the host's compiler.

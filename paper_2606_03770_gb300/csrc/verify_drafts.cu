@@ -100,8 +100,9 @@ template <class T> __device__ __forceinline__ float half_of(uint32_t w, int high
     return __uint_as_float(high ? w & 0xffff0000u : w << 16);
 }
 
-// LONG: runs of which a lane has more than kShort elements, whose sums are closed on the way.  (Of 128,256 tokens that is one
-// block a request.  In one kernel for all, 1 x 5 x 32,000 takes 17.5 us for 16.4, 64 x 8 x 128,256 in 32 bits 146 for 139.)
+// LONG: runs of which a lane has more than kShort elements, whose sums are closed on the way.  Of 128,256 tokens that is one
+// block a request: 160 x 2 in 16 bits 234 us, 216 without.  (One kernel for all would take 1 x 5 x 32,000 17.5 us for 16.4 and
+// 64 x 8 x 128,256 in 32 bits 146 for 137.)
 constexpr int kShort = 256;
 
 template <class T, bool LONG> struct Walk {
@@ -314,25 +315,29 @@ template <class T, bool LONG> struct Walk {
                 sa[0] = sa[1] = sb[0] = sb[1] = 0;
             };
 #pragma unroll 1
-            for (int unit = 0; unit < units; ++unit) {
-                Lot e, d;
-                if (LONG && unit % kClose == kClose - 1) close();
-                if (wide) {
-                    copy_wait<kStages - 1>();
-                    e = from_ring(stage, 0);
-                    if (two) d = from_ring(stage, 1);
-                    issue(stage);
-                } else {
-                    e = from_row(u, first + unit * kUnit);
-                    if (two) d = from_row(v, first + unit * kUnit);
-                }
+            for (int unit = 0; unit < units;) {
+                if (LONG && unit > 0) close();
+                const int until = LONG ? min(unit + kClose, units) : units;
+#pragma unroll 1
+                for (; unit < until; ++unit) {
+                    Lot e, d;
+                    if (wide) {
+                        copy_wait<kStages - 1>();
+                        e = from_ring(stage, 0);
+                        if (two) d = from_ring(stage, 1);
+                        issue(stage);
+                    } else {
+                        e = from_row(u, first + unit * kUnit);
+                        if (two) d = from_row(v, first + unit * kUnit);
+                    }
 #pragma unroll
-                for (int j = 0; j < kEach; ++j) sa[j % 2] += power2(__fmaf_rn(element(e, j), f, -ca));
-                if (two) {
+                    for (int j = 0; j < kEach; ++j) sa[j % 2] += power2(__fmaf_rn(element(e, j), f, -ca));
+                    if (two) {
 #pragma unroll
-                    for (int j = 0; j < kEach; ++j) sb[j % 2] += power2(__fmaf_rn(element(d, j), f, -cb));
+                        for (int j = 0; j < kEach; ++j) sb[j % 2] += power2(__fmaf_rn(element(d, j), f, -cb));
+                    }
+                    stage = stage == kStages - 1 ? 0 : stage + 1;
                 }
-                stage = stage == kStages - 1 ? 0 : stage + 1;
             }
 #pragma unroll 1
             for (int i = first + units * kUnit + lane; i < end; i += 32) {
