@@ -196,10 +196,15 @@ int e2_cache_attend(const e2_cache *c, const e2_attend_args *a, void *workspace,
 
 /* e2_cache_attend, but that node i sees the keys before base, its own and those of the
  * nodes on its way up; with a window > 0 those whose position is above its own minus
- * window.  Up to eight rows what rounding took from the weights is in a product of its own for
- * bf16 too; from 17 on, and from nine on where the launch is small, keys and values are rounded
- * to fp16, as e2_cache_attend's from 65 rows on.  max_new is at most E2_MAX_DRAFT; nodes beyond (of a request that has more) are
- * NaN where they see keys.  parents: [tokens]. */
+ * window.  Up to eight rows codes are not rounded, and what rounding took from the weights is in a
+ * product of its own for bf16 too.  From 17 rows on keys and values are rounded to fp16, as
+ * e2_cache_attend's from 65 rows on; nine to 16 rows go one way or the other: by fp16 where
+ * batch * kv_heads is at most the device's multiprocessors, and times the keys that are seen (max_len, or
+ * window + max_new if that is less) at most 1,200,000 (600,000 for fp16).  So a request's last bits
+ * may differ from batch to batch; fp16 outputs of rounded keys and values are 3e-4 to 6e-4 off (of
+ * their norm), where their own rounding is 2e-4, bf16 ones 1.7e-3 either way.
+ * A NaN among a row's keys or values gives NaN.  max_new is at most E2_MAX_DRAFT; nodes beyond (of a request
+ * that has more) are NaN where they see keys.  parents: [tokens]. */
 size_t e2_cache_attend_tree_workspace(const e2_cache *c, const e2_attend_args *a);
 int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32_t *parents, void *workspace,
                          size_t workspace_bytes, void *stream);
@@ -213,7 +218,12 @@ int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32
  * Without draft q is 1 at x: x is accepted when u < P(x), or else leaves P.  When no child is
  * accepted (or there is none) the walk ends, and answers with the first token v at which P's
  * sum in order is above uniforms of node 0.  T = 0: the child whose id is the first largest
- * logit is accepted, or else that token answers.
+ * logit is accepted, or else that token answers (draft is not looked at).
+ * What comes out has the target's probabilities where a node's children were drawn from its draft
+ * row at the same T, each by itself (the same token twice, perhaps), or without draft, however they
+ * were chosen, if the uniforms had no part in it.  With draft, children that were drawn without
+ * putting back come out with other probabilities.
+ * A request's tree is its first max_new nodes, the others are not looked at.
  *   kept[r]: nodes of the way, node 0 among them (0 for a request without nodes)
  *   nodes[r][k], k < kept[r]: them; -1 from there on
  *   answer[r][k]: the token after nodes[r][k], the last the answer; -1 from kept[r] on
@@ -222,12 +232,12 @@ int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32
  * Exponentials below e^-64 of the largest may count as nothing in sums and for the answer, and do
  * below e^-745 (which 64 bits do not hold) for a drafted token.
  * -inf marks a forbidden token.  The walk ends with the answer -1 at a row that holds NaN or
- * +inf or has no token allowed (of logits; of draft where a child is asked), and at node 0 for a
- * T that is negative, infinite or NaN.  ids outside the vocabulary are never accepted.
+ * +inf or has no token allowed (of logits; of draft where a child is asked and T is not 0), and at
+ * node 0 for a T that is negative, infinite or NaN; nowhere else.  ids outside the vocabulary are never accepted.
  * uniforms are taken as 0 to 1, NaN as 0.  Requests whose starts are no rows of the call have no
  * nodes.  logits and draft: fp16, bf16 or fp32, any row stride.  vocab is at most 2^30. */
 typedef struct {
-    int32_t tokens, vocab, dtype, batch, max_new;   /* max_new: columns of nodes and answer */
+    int32_t tokens, vocab, dtype, batch, max_new;   /* max_new: columns of nodes and answer, nodes of a tree */
     const void *logits;
     int64_t logits_stride;
     const void *draft;

@@ -10,9 +10,9 @@
 // Bound by a tile's instructions (65 to 69% of issue slots) and the waits between its steps (copied, unpacked, scored,
 // weighed, summed: 100 to 400 cycles each, three to five tiles on their way); half the unpacking would give 5%, half the
 // weights 0 to 4, half of either product 2.  Measured, us (128 elements, bf16): 8 requests x 8 KV heads x 56 rows x 65,536
-// keys 264 (1,080 cycles a tile; the cache alone 89 at the memory's rate), 2 x 8 x 1,024 rows x 16,384 keys 150 (912 TFLOP/s,
-// 48% of the tensor cores' measured rate), 8 x 8 x 128 rows x 2,304 keys 23.5, of which 6 before the first product and 4 after
-// the last; 13 x 3 x 77 rows, window 128, 9.4.
+// keys 265 (1,080 cycles a tile; the cache alone 89 at the memory's rate), 2 x 8 x 1,024 rows x 16,384 keys 151 (907 TFLOP/s,
+// 48% of the tensor cores' measured rate), 8 x 8 x 128 rows x 2,304 keys 24, of which 6 before the first product and 4 after
+// the last; 13 x 3 x 77 rows, window 128, 9.6; 8 x 8 x 16 rows, window 128 of 65,000 keys, 11.4.
 // On the way: one set of weights' warps 400 for the first, copies by 16 keys 360, by one warp 320, eight warps that unpack
 // 315, a barrier polled by one lane for its warp twice as long, copies of one tile after the other 304, both widths of
 // weights in one kernel 284, sixteen warps that unpack 274, four copies of the code for the rows' end 270 (and 2.5 us of

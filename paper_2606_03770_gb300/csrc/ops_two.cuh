@@ -1,5 +1,6 @@
 // ops_two.cuh -- numbers of some 45 bits as sums of two 32-bit ones, and exponentials of that
-// precision (64-bit arithmetic runs at a sixty-fourth of the 32-bit rate here).
+// precision (64-bit arithmetic runs at a sixty-fourth of the 32-bit rate here).  Sums without
+// error are Knuth's, where one is the larger Dekker's, as are products and quotients of pairs.
 #pragma once
 
 #include "ops_common.cuh"

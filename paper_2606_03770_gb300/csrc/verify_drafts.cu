@@ -11,9 +11,9 @@ namespace {
 
 // Bound by latency where there are few requests: some five dependent steps a node (its rows, the block's sums, the
 // cluster's barrier, the decision), two microseconds; by the rows' bytes and, at a walk's end, by instructions where
-// there are many.  Measured, us: 1 request x 5 nodes of 32,000 tokens 17, 8 x 16 of 128,256 (bf16) 40, 64 x 8 of
-// 128,256 (fp32) 135, of which the levels of the longest walk 60 at 5 TB/s, then 30 for the sums in 45 bits (85% of
-// issue slots, some 55 an element); 13 x 13 of 50,001 without the draft's rows 20.
+// there are many.  Measured, us: 1 request x 5 nodes of 32,000 tokens 16, 8 x 16 of 128,256 (bf16) 39, 64 x 8 of
+// 128,256 (fp32) 137, of which the levels of the longest walk 60 at 5 TB/s, then 30 for the sums in 45 bits (85% of
+// issue slots, some 55 an element); 13 x 13 of 50,001 without the draft's rows 20; T = 0, 8 x 16 of 128,256 (bf16) 17.
 //
 // A cluster of blocks walks a request's tree, and all its warps take the same decisions.  Each
 // warp has a run of the vocabulary; what a pass over a row gives is sums, the blocks' of which
