@@ -575,18 +575,18 @@ template <class T, bool LONG> struct Walk {
     }
     // After it: run and block of (x - share y)+, and its sum; false where the border's part of it may be above 2^-37.
     // What is so little of x that it may be all rounding is nothing, so that whoever has something has an element with
-    // something (sums are off by some 2^-41; a block that has something has a run that does).
+    // something: sums of the two are off by 2^-36.8 each at worst, and a block that has something has a run that does.
     __device__ __forceinline__ bool take_split(const Two &share, float near, Two &sum)
     {
         auto of = [&](const Two &x, const Two &y, float least) {
             const Two d = x - share * y;
             return d.h > least * x.h ? d : Two{0, 0};
         };
-        sum = warp_sum(lane < p.split ? of(block, block_q, 0x1p-37f) : Two{0, 0});
+        sum = warp_sum(lane < p.split ? of(block, block_q, 0x1p-34f) : Two{0, 0});
         // (2^-22: what the comparisons were rounded by)
         const float off = fabsf(__fdiv_rn((share - Two{near, 0}).h, near)) + 0x1p-22f;
         if (!(off < 0x1p-20f && off * border <= 0x1p-37f * sum.h)) return false;
-        run = of(run, run_q, 0x1p-38f), block = of(block, block_q, 0x1p-37f);
+        run = of(run, run_q, 0x1p-35f), block = of(block, block_q, 0x1p-34f);
         return true;
     }
 

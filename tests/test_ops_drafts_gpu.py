@@ -609,6 +609,36 @@ def test_parts_of_a_row_that_draft_and_target_share(V, u0):
         assert got >= 0 and (got == int(clear) or abs(float(p[got] - q[got])) < 2.0 ** -36), (r, got, int(clear))
 
 
+@pytest.mark.parametrize("u0", [0.0, 1.0])
+def test_long_parts_of_a_row_that_draft_and_target_share(u0):
+    """As above for parts of 192 equal tokens a lane, the draft's logits all a little higher: sums of the two round apart."""
+    n, B, V = 2, 160, 65536
+    g = torch.Generator(device="cuda").manual_seed(24)
+    s = batch_of([n] * B, 8, F32, seed=24)
+    s[0], s[5] = torch.full((n * B, V), -math.inf, device="cuda"), torch.full((n * B, V), -math.inf, device="cuda")
+    x, ids, _, _, u, y = s
+    s[2] = i32([-1, 0] * B)
+    sixteenths = lambda *size: torch.randint(-16, 17, size, generator=g, device="cuda") / 16
+    at = torch.arange(V, device="cuda") if u0 == 0 else torch.arange(V - 1, -1, -1, device="cuda")
+    for r in range(B):
+        x[n * r, at[:3 * V // 4]] = -25.0 + sixteenths(1)
+        heavy = at[-2:]
+        x[n * r, heavy[0]], x[n * r, heavy[1]] = 0.0, 1.0 + r % 3
+        y[n * r] = x[n * r]
+        y[n * r, heavy] = x[n * r, heavy.flip(0)]
+        y[n * r] += sixteenths(1)
+        ids[n * r + 1] = heavy[0].int()                      # (of less in the target)
+    u[1::2] = 1.0
+    u[::2] = u0
+    from paper_2606_03770_gb300 import ops
+    kept, _, answer = ops.verify_drafts(*s[:5], draft=y, max_new=n)
+    assert kept.tolist() == [1] * B
+    # (the equal tokens, or the one that has more in the target)
+    for r in range(B):
+        got = int(answer[r, 0])
+        assert got >= 0 and (got == int(at[-1]) or float(x[n * r, got]) < -20), (r, got)
+
+
 @pytest.mark.parametrize("B,V,dtype", [(160, 1 << 22, BF), (160, 65536, BF), (160, 262144, F32), (2, (1 << 26) + 1357, HALF)])
 @pytest.mark.parametrize("draft", [False, True])
 def test_long_rows_of_equal_logits(B, V, dtype, draft):
