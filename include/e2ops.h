@@ -228,7 +228,8 @@ int e2_cache_attend_tree(const e2_cache *c, const e2_attend_args *a, const int32
  *   nodes[r][k], k < kept[r]: them; -1 from there on
  *   answer[r][k]: the token after nodes[r][k], the last the answer; -1 from kept[r] on
  * Exponentials and sums have some 45 bits, so decisions are those of 64 bits but for numbers
- * within 2^-34 or so of a border; what (P - q)+ sums to counts as nothing below 2^-36, and P stays.
+ * within 2^-34 or so of a border, or 2^-34 / B where rejections have left B of p (which has probability B,
+ * if children are drawn); what (P - q)+ sums to counts as nothing below 2^-36, or below 2^-40 of p, and P stays.
  * Exponentials below e^-64 of the largest may count as nothing in sums and for the answer, and do
  * below e^-745 (which 64 bits do not hold) for a drafted token.
  * -inf marks a forbidden token.  The walk ends with the answer -1 at a row that holds NaN or

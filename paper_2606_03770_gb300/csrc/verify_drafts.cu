@@ -35,6 +35,7 @@ constexpr int kRing = 6144;                      // bytes of a warp's copies on 
 constexpr int kGroup = 4;                        // nodes that are looked at together
 static_assert(kGroup * kWarps == 32, "a lane for each node and warp");
 constexpr float kNothing = 0x1p-36f;             // a sum below it, of what it is a part of, is rounding's
+constexpr float kLeast = 0x1p-40f;               // and what several rejections have left of p below that (p and A q are known to 2^-44)
 
 struct VerifyParams {
     int tokens, vocab, batch, max_new, split;
@@ -741,8 +742,8 @@ template <class T, bool DRAFT, bool LONG> __global__ void __launch_bounds__(kThr
             x_sum = __shfl_sync(~0u, x_sums, place * kWarps), y_sum = __shfl_sync(~0u, y_sums, place * kWarps);
             walk.x_top = m.tops[place].x, walk.y_top = m.tops[place].y;
             // (a NaN, or +inf, is in the sum; a sample without a token, or with none of the large ones, too)
-            constexpr float kLeast = 0.5f, kMost = 0x1p62f;
-            clear = x_sum > kLeast && x_sum < kMost && (!both || (y_sum > kLeast && y_sum < kMost));
+            constexpr float kSome = 0.5f, kMost = 0x1p62f;
+            clear = x_sum > kSome && x_sum < kMost && (!both || (y_sum > kSome && y_sum < kMost));
             if (!clear) {
                 if (!walk.tops(both, first)) break;
             } else if (children) {
@@ -849,7 +850,7 @@ template <class T, bool DRAFT, bool LONG> __global__ void __launch_bounds__(kThr
                     if (!enough) sum = walk.template sums<false, true>(of_x, of_y, unused);
                     near = 0;                             // (the first child's only)
                     sum = sum / all;
-                    if (sum.h > kNothing * B.h) {
+                    if (sum.h > fmaxf(kNothing * B.h, kLeast)) {
                         A = more, B = sum, less = true;
                     } else {
                         // (p's own, which a split has not left)

@@ -639,6 +639,32 @@ def test_long_parts_of_a_row_that_draft_and_target_share(u0):
         assert got >= 0 and (got == int(at[-1]) or float(x[n * r, got]) < -20), (r, got)
 
 
+@pytest.mark.parametrize("V", [7, 900, 20000])
+def test_rejections_that_leave_next_to_nothing(V):
+    """A token of the draft that the target forbids, again and again, where both agree on the rest: each rejection leaves some
+    5e-4 of P and P as it was, until what is left is rounding's."""
+    n, B = 9, 100
+    g = torch.Generator(device="cuda").manual_seed(25)
+    rand = lambda: torch.rand(1, generator=g, device="cuda")
+    x, y = torch.full((n * B, V), -math.inf, device="cuda"), torch.full((n * B, V), -math.inf, device="cuda")
+    ids, u = torch.zeros(n * B, **I32), torch.rand(n * B, generator=g, device="cuda")
+    for r in range(B):
+        a, b, out = torch.randperm(V, generator=g, device="cuda")[:3]
+        x[n * r, a], x[n * r, b] = rand(), -11 + 2 * rand()
+        y[n * r] = x[n * r]
+        y[n * r, out] = -8 + rand()
+        ids[n * r + 1:n * (r + 1)] = out
+        # (token a has all but e^-9 at most, and is the answer but for what that leaves)
+        u[n * r] = 0.01 + 0.98 * u[n * r]
+    parents, starts = i32(([-1] + [0] * (n - 1)) * B), i32(range(0, n * B + 1, n))
+    from paper_2606_03770_gb300 import ops
+    for children in range(1, n):
+        par = torch.where(torch.arange(n * B, device="cuda") % n <= children, parents, -1).int()
+        kept, _, answer = ops.verify_drafts(x, ids, par, starts, u, draft=y, max_new=n)
+        assert kept.tolist() == [1] * B
+        assert answer[:, 0].tolist() == x[::n].argmax(1).tolist(), children
+
+
 @pytest.mark.parametrize("B,V,dtype", [(160, 1 << 22, BF), (160, 65536, BF), (160, 262144, F32), (2, (1 << 26) + 1357, HALF)])
 @pytest.mark.parametrize("draft", [False, True])
 def test_long_rows_of_equal_logits(B, V, dtype, draft):
